@@ -366,6 +366,139 @@ int gms_kv_verify(const gms_kv_pool *pool, const int32_t *d_block_ids, uint32_t 
                   void *stream);
 
 /*
+ * gms_kv_attention / gms_kv_attention_shared / gms_kv_evict -- what an engine does next with the paged KV state that
+ * the calls above put back (Section 6, "Preserving KV state"): attention that reads the pool where it lies, and the
+ * choice of the tokens that stay in it.  All asynchronous on `stream`; no allocation, no host synchronisation; can be
+ * captured into a CUDA graph.  Integer arrays on the device (lengths, tables) are read by the kernels only.
+ *
+ * gms_kv_layout: how one layer's tokens lie inside the pool's blocks.  Element (token, kv head, d) of block b is at
+ *   base + plane*plane_stride + b*block_stride + token*token_stride + head*head_stride + d*2 bytes,
+ * tokens outside heads or heads outside tokens, whichever the strides say.
+ */
+#define GMS_DTYPE_BF16 0u
+#define GMS_DTYPE_F16 1u
+typedef struct {
+    uint32_t k_plane, v_plane;            /* planes of the layer's keys and values                       */
+    uint32_t n_kv_heads;                  /* >= 1                                                        */
+    uint32_t head_dim;                    /* 64 or 128                                                   */
+    uint32_t block_tokens;                /* tokens in a block: a power of two, 16 .. 1024               */
+    uint32_t dtype;                       /* GMS_DTYPE_* of pool, queries and outputs                    */
+    uint32_t token_stride, head_stride;   /* bytes, multiples of 16; rows must not overlap and must end
+                                             inside block_bytes                                          */
+} gms_kv_layout;
+
+/*
+ * One batch of queries over cached tokens.  Sequence s has kv_lens[s] tokens in the pool, token t in slot
+ * t % block_tokens of block block_table[s*table_stride + t / block_tokens]; its queries are the rows
+ * cu_q[s] .. cu_q[s+1]-1 of `q`, and they belong to the LAST of those tokens (the tokens' own keys and values are
+ * already in the pool).  A query at position p sees token t if t <= p and, when window > 0, t > p - window or
+ * t < sinks; an id outside [0, pool->n_blocks) is a hole whose tokens nobody sees.  With c = h / (n_heads/n_kv_heads):
+ *   x_t = scale * q[i,h] . K[t,c];  lse[i,h] = log sum_t exp(x_t);  out[i,h] = sum_t exp(x_t - lse) V[t,c]
+ * over the t that it sees; if there are none, out is 0 and lse is -infinity.  What a query does not see cannot reach
+ * its output, whatever bits it holds (NaN, infinities).  Products are taken in the pool's type with 32-bit sums; the
+ * softmax weights are rounded to the pool's type before the product with V.
+ * kv_lens above max_kv, and queries of a sequence beyond max_q, are not processed (the host sizes the launch by
+ * these); rows of q that no sequence owns leave out and lse as they are.
+ */
+typedef struct {
+    const void *q;                 /* (device) [total_q][n_heads][head_dim], 16-byte aligned             */
+    void *out;                     /* (device) the same shape                                            */
+    float *lse;                    /* (device) [total_q][n_heads], may be NULL                           */
+    const int32_t *cu_q;           /* (device) n_seq + 1 ascending offsets; NULL: one query a sequence   */
+    const int32_t *kv_lens;        /* (device) n_seq                                                     */
+    const int32_t *block_table;    /* (device) n_seq rows of table_stride ids                            */
+    void *workspace;               /* (device) gms_kv_attention*_workspace bytes, 256-byte aligned; contents
+                                      before and after are meaningless; calls that overlap on the GPU must not
+                                      share it                                                           */
+    uint64_t *status;              /* (device) may be NULL; GMS_DEV_TIMEOUT is or-ed in if a bounded wait
+                                      inside a kernel ran out (outputs are then incomplete)              */
+    uint64_t workspace_bytes;
+    uint64_t q_token_stride, q_head_stride;     /* bytes, multiples of 16                                */
+    uint64_t out_token_stride, out_head_stride; /* bytes, multiples of 16                                */
+    uint64_t table_stride;         /* entries; table_stride * block_tokens >= max_kv                     */
+    uint32_t n_seq, n_heads;       /* n_heads: a multiple of n_kv_heads                                  */
+    uint32_t total_q, max_q;       /* rows of q; longest query run of a sequence                         */
+    uint32_t max_kv;               /* longest kv_lens                                                    */
+    uint32_t window, sinks;        /* window 0: every token up to the query's own is seen                */
+    float scale;
+} gms_kv_attn;
+
+/*
+ * Accumulated attention weights, the quantity that gms_kv_evict goes by.  For t < kv_lens[s]
+ *   out[s][c][t] = decay * in[s][c][t] + sum over the call's queries i of s and the heads h of c of exp(x_t - lse[i,h])
+ * (0 for tokens a query does not see); other entries of `out` are left alone.  `in` may equal `out`.  Sums are taken in
+ * a fixed order: equal calls give equal bits.
+ */
+typedef struct {
+    const float *in;                    /* (device) NULL: zeros                                          */
+    float *out;                         /* (device)                                                      */
+    uint64_t seq_stride, head_stride;   /* elements, of both                                             */
+    float decay;
+    uint32_t reserved;                  /* 0                                                             */
+} gms_kv_weight;
+
+/* Errors: NULL, ALIGN, ARG, RANGE (index limits; table_stride; workspace_bytes too small), CUDA. */
+int gms_kv_attention_workspace(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
+                               const gms_kv_weight *weight, uint64_t *nbytes);
+int gms_kv_attention(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
+                     const gms_kv_weight *weight /* may be NULL */, void *stream);
+
+/*
+ * gms_kv_attention_shared -- the same for a batch in which whole groups of sequences begin with the same tokens (a
+ * system prompt, a document).  Sequences group_start[g] .. group_start[g+1]-1 share the prefix of prefix_lens[g] tokens
+ * that lies in the blocks prefix_table[g*prefix_stride + ...]; block_table and kv_lens describe what each sequence has
+ * after it.  Every query sees the whole prefix, then its own sequence's tokens up to its own.  The prefix is read once
+ * for all rows of the group, not once a sequence.  attn->window and attn->sinks must be 0.
+ * group_start[0] = 0 and group_start[n_groups] = n_seq: a sequence outside every group gets the tokens of its own
+ * alone.  Errors: as gms_kv_attention.
+ */
+typedef struct {
+    const int32_t *group_start;   /* (device) n_groups + 1, ascending                                    */
+    const int32_t *prefix_lens;   /* (device) n_groups                                                   */
+    const int32_t *prefix_table;  /* (device) n_groups rows of prefix_stride ids                         */
+    uint64_t prefix_stride;       /* entries; prefix_stride * block_tokens >= max_prefix                 */
+    uint32_t n_groups;
+    uint32_t max_prefix;          /* longest prefix_lens                                                 */
+    uint32_t max_group_q;         /* most query rows in a group                                          */
+    uint32_t reserved;            /* 0                                                                   */
+} gms_kv_prefix;
+int gms_kv_attention_shared_workspace(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
+                                      const gms_kv_prefix *prefix, uint64_t *nbytes);
+int gms_kv_attention_shared(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
+                            const gms_kv_prefix *prefix, void *stream);
+
+/*
+ * gms_kv_evict -- shrinks the cache of n_seq sequences to at most `budget` tokens a sequence, for n_layers layers at
+ * once (layer l: planes k_plane + l*layer_planes and v_plane + l*layer_planes).  Of n = lens[s] tokens, n' = min(n, budget)
+ * stay; each layer and KV head chooses its own: the first `sinks`, the last `recent`, and of those between the
+ * n' - sinks - recent with the largest weights (equal weights: the earlier token; NaN counts below every number).
+ * When n <= budget all stay.  The kept tokens keep their order:
+ *   kept[l][s][c][j]         position of the j-th kept token, j < n' (-1 for n' <= j < budget)
+ *   weights_out[l][s][c][j]  its weight (entries from n' on are left alone)
+ *   lens_out[s] = n'
+ *   K and V of token kept[j] are copied to token j of the blocks dst_table[s*dst_stride + ...]
+ * Destination blocks must be distinct and must not be source blocks (the old ones are free once the call has run); a row
+ * whose source or destination id lies outside the pool is not copied.  Keys carry their positions (rotary embeddings)
+ * with them; afterwards the sequence is n' tokens long for gms_kv_attention.  Lens above max_len count as max_len.
+ * Errors: NULL, ALIGN, ARG (sinks + recent > budget; planes outside the pool), RANGE, CUDA.
+ */
+typedef struct {
+    const float *weights;               /* (device) w_*_stride elements between layers, sequences, heads */
+    float *weights_out;                 /* (device) may be NULL; o_*_stride; not `weights` itself        */
+    const int32_t *lens;                /* (device) n_seq                                                */
+    int32_t *lens_out;                  /* (device) n_seq, may be NULL                                   */
+    const int32_t *src_table, *dst_table;
+    int32_t *kept;                      /* (device) [n_layers][n_seq][n_kv_heads][budget]                */
+    uint64_t w_layer_stride, w_seq_stride, w_head_stride;
+    uint64_t o_layer_stride, o_seq_stride, o_head_stride;
+    uint64_t src_stride, dst_stride;    /* entries; * block_tokens >= max_len and >= min(max_len, budget) */
+    uint32_t n_layers, layer_planes, n_seq, max_len;
+    uint32_t budget, sinks, recent;
+    uint32_t reserved;                  /* 0                                                             */
+} gms_kv_evict_args;
+int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_evict_args *args, void *stream);
+
+/*
  * Pinned, device-mapped host memory for a GMS_SRC_HOST_MAPPED image (the
  * host-resident snapshot of Section 3.1 step 3 / Section 6).  *device_view is
  * the address to pass as `image`.

@@ -34,7 +34,9 @@ KV_MISMATCH_DTYPE = np.dtype([("block_id", "<u4"), ("plane", "<u4"), ("sub_block
 EXPORTS = (
     "gms_manifest_build", "gms_manifest_destroy", "gms_manifest_info", "gms_manifest_block_base",
     "gms_manifest_chunk_count", "gms_manifest_chunk", "gms_manifest_set_expected", "gms_restore", "gms_capture", "gms_digest",
-    "gms_verify", "gms_digest_verify", "gms_restore_verify", "gms_verify_tensors", "gms_verify_flat_noalloc", "gms_last_device_status", "gms_kv_restore", "gms_kv_capture", "gms_kv_digest", "gms_kv_verify", "gms_host_image_alloc", "gms_host_image_free",
+    "gms_verify", "gms_digest_verify", "gms_restore_verify", "gms_verify_tensors", "gms_verify_flat_noalloc", "gms_last_device_status", "gms_kv_restore", "gms_kv_capture", "gms_kv_digest", "gms_kv_verify",
+    "gms_kv_attention_workspace", "gms_kv_attention", "gms_kv_attention_shared_workspace", "gms_kv_attention_shared", "gms_kv_evict",
+    "gms_host_image_alloc", "gms_host_image_free",
     "gms_pipe_create", "gms_pipe_direct_io", "gms_pipe_mapped_writes", "gms_pipe_destroy", "gms_restore_fd", "gms_capture_fd", "gms_stage_create", "gms_stage_destroy", "gms_restore_staged",
     "gms_service_create", "gms_service_destroy", "gms_service_acquire_rw", "gms_service_alloc", "gms_service_commit",
     "gms_service_abort", "gms_service_acquire_ro", "gms_service_release_ro", "gms_service_info", "gms_service_access",
@@ -59,6 +61,50 @@ class KvPool(C.Structure):
 
 
 KV_IMAGE_BY_ID = 1
+DTYPE_BF16, DTYPE_F16 = 0, 1
+
+
+class KvLayout(C.Structure):
+    _fields_ = [("k_plane", C.c_uint32), ("v_plane", C.c_uint32), ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("block_tokens", C.c_uint32), ("dtype", C.c_uint32), ("token_stride", C.c_uint32), ("head_stride", C.c_uint32)]
+
+
+class KvAttn(C.Structure):
+    """``gms_kv_attn``; usually made by :func:`kv_attn`, which also keeps the tensors alive."""
+
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("cu_q", C.c_void_p), ("kv_lens", C.c_void_p),
+                ("block_table", C.c_void_p), ("workspace", C.c_void_p), ("status", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("q_token_stride", C.c_uint64), ("q_head_stride", C.c_uint64), ("out_token_stride", C.c_uint64),
+                ("out_head_stride", C.c_uint64), ("table_stride", C.c_uint64), ("n_seq", C.c_uint32), ("n_heads", C.c_uint32),
+                ("total_q", C.c_uint32), ("max_q", C.c_uint32), ("max_kv", C.c_uint32), ("window", C.c_uint32),
+                ("sinks", C.c_uint32), ("scale", C.c_float)]
+
+    def set_workspace(self, t):
+        """Hands over a uint8 device tensor of at least gms_kv_attention*_workspace bytes."""
+        self._workspace = t
+        self.workspace, self.workspace_bytes = t.data_ptr(), t.numel() * t.element_size()
+
+
+class KvWeight(C.Structure):
+    # ("in" is a keyword: the field is called in_)
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("seq_stride", C.c_uint64), ("head_stride", C.c_uint64),
+                ("decay", C.c_float), ("reserved", C.c_uint32)]
+
+
+class KvPrefix(C.Structure):
+    _fields_ = [("group_start", C.c_void_p), ("prefix_lens", C.c_void_p), ("prefix_table", C.c_void_p),
+                ("prefix_stride", C.c_uint64), ("n_groups", C.c_uint32), ("max_prefix", C.c_uint32),
+                ("max_group_q", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class KvEvictArgs(C.Structure):
+    _fields_ = [("weights", C.c_void_p), ("weights_out", C.c_void_p), ("lens", C.c_void_p), ("lens_out", C.c_void_p),
+                ("src_table", C.c_void_p), ("dst_table", C.c_void_p), ("kept", C.c_void_p), ("w_layer_stride", C.c_uint64),
+                ("w_seq_stride", C.c_uint64), ("w_head_stride", C.c_uint64), ("o_layer_stride", C.c_uint64),
+                ("o_seq_stride", C.c_uint64), ("o_head_stride", C.c_uint64), ("src_stride", C.c_uint64),
+                ("dst_stride", C.c_uint64), ("n_layers", C.c_uint32), ("layer_planes", C.c_uint32), ("n_seq", C.c_uint32),
+                ("max_len", C.c_uint32), ("budget", C.c_uint32), ("sinks", C.c_uint32), ("recent", C.c_uint32),
+                ("reserved", C.c_uint32)]
 
 
 _lib = None
@@ -95,6 +141,11 @@ def lib():
             "gms_kv_capture": (i, [C.POINTER(KvPool), p, u64, u64, u32, p, u32, p, p, p, p]),
             "gms_kv_digest": (i, [C.POINTER(KvPool), p, u32, p, p, p, p]),
             "gms_kv_verify": (i, [C.POINTER(KvPool), p, u32, p, p, p, u32, p, p, p]),
+            "gms_kv_attention_workspace": (i, [p, p, p, p, pu64]),
+            "gms_kv_attention": (i, [p, p, p, p, p]),
+            "gms_kv_attention_shared_workspace": (i, [p, p, p, p, pu64]),
+            "gms_kv_attention_shared": (i, [p, p, p, p, p]),
+            "gms_kv_evict": (i, [p, p, p, p]),
             "gms_host_image_alloc": (i, [u64, pp, pp]),
             "gms_host_image_free": (i, [p]),
             "gms_pipe_create": (i, [u32, u64, u32, pp]),
@@ -292,6 +343,120 @@ def gms_kv_verify(pool: KvPool, d_block_ids, n_sel: int, d_computed, d_expected,
                   stream=None):
     _check(lib().gms_kv_verify(C.byref(pool), _dev(d_block_ids), n_sel, _dev(d_computed), _dev(d_expected), _dev(d_out), cap,
                                _dev(d_count), _dev(d_scratch), _stream(stream)), "gms_kv_verify")
+
+
+def _int32(*tensors):
+    for t in tensors:
+        if t is not None and (t.element_size() != 4 or t.is_floating_point() or t.stride(-1) not in (0, 1) and t.shape[-1] > 1):
+            raise ValueError("lengths, offsets and tables are int32 with contiguous rows")
+
+
+def _float32(*tensors):
+    for t in tensors:
+        if t is not None and (t.element_size() != 4 or not t.is_floating_point() or t.stride(-1) != 1 and t.shape[-1] > 1):
+            raise ValueError("weights and log-sum-exps are float32 with contiguous rows")
+
+
+def kv_attn(*, q, out, kv_lens, block_table, max_kv: int, scale: float, lse=None, cu_q=None, max_q: int = 1, window: int = 0,
+            sinks: int = 0, workspace=None, status=None) -> KvAttn:
+    """gms_kv_attn from torch tensors: ``q`` and ``out`` [tokens, heads, dim] (any strides with a contiguous last
+    dimension), ``lse`` float32 [tokens, heads] contiguous, ``kv_lens`` and ``cu_q`` int32, ``block_table`` int32
+    [sequences, blocks].  The result keeps the tensors alive."""
+    for t in (q, out):
+        if t.dim() != 3 or t.element_size() != 2 or t.stride(2) != 1:
+            raise ValueError("q and out are 16-bit [tokens, heads, dim] with a contiguous last dimension")
+    if out.shape != q.shape or out.dtype != q.dtype or block_table.dim() != 2:
+        raise ValueError("out must match q, block_table is [sequences, blocks]")
+    _int32(kv_lens, cu_q, block_table)
+    _float32(lse)
+    n_seq = kv_lens.shape[0]
+    if block_table.shape[0] != n_seq or (cu_q is not None and cu_q.shape[0] != n_seq + 1):
+        raise ValueError("kv_lens, cu_q and block_table disagree about the number of sequences")
+    if lse is not None and (tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_contiguous()):
+        raise ValueError("lse is float32 [tokens, heads], contiguous")
+    a = KvAttn(q=_dev(q), out=_dev(out), lse=_dev(lse), cu_q=_dev(cu_q), kv_lens=_dev(kv_lens), block_table=_dev(block_table),
+               status=_dev(status), q_token_stride=q.stride(0) * 2, q_head_stride=q.stride(1) * 2,
+               out_token_stride=out.stride(0) * 2, out_head_stride=out.stride(1) * 2, table_stride=block_table.stride(0),
+               n_seq=n_seq, n_heads=q.shape[1], total_q=q.shape[0], max_q=max_q, max_kv=max_kv, window=window, sinks=sinks,
+               scale=scale)
+    a._keep = (q, out, lse, cu_q, kv_lens, block_table, status)
+    if workspace is not None:
+        a.set_workspace(workspace)
+    return a
+
+
+def kv_weights(w_in, w_out, decay: float = 1.0) -> KvWeight:
+    """gms_kv_weight from float32 tensors [sequences, kv heads, tokens]; ``w_in`` None counts as zeros."""
+    _float32(w_in, w_out)
+    if w_in is not None and w_in.stride() != w_out.stride():
+        raise ValueError("w_in and w_out need equal strides")
+    w = KvWeight(in_=_dev(w_in), out=_dev(w_out), seq_stride=w_out.stride(0), head_stride=w_out.stride(1), decay=decay)
+    w._keep = (w_in, w_out)
+    return w
+
+
+def kv_prefix(*, group_start, prefix_lens, prefix_table, max_prefix: int, max_group_q: int) -> KvPrefix:
+    """gms_kv_prefix from int32 tensors; ``prefix_table`` [groups, blocks]."""
+    _int32(group_start, prefix_lens, prefix_table)
+    g = prefix_lens.shape[0]
+    if group_start.shape[0] != g + 1 or prefix_table.shape[0] != g:
+        raise ValueError("group_start, prefix_lens and prefix_table disagree about the number of groups")
+    p = KvPrefix(group_start=_dev(group_start), prefix_lens=_dev(prefix_lens), prefix_table=_dev(prefix_table),
+                 prefix_stride=prefix_table.stride(0), n_groups=g, max_prefix=max_prefix, max_group_q=max_group_q)
+    p._keep = (group_start, prefix_lens, prefix_table)
+    return p
+
+
+def kv_evict_args(*, weights, lens, src_table, dst_table, kept, max_len: int, budget: int, sinks: int = 0, recent: int = 0,
+                  weights_out=None, lens_out=None, layer_planes: int = 2) -> KvEvictArgs:
+    """gms_kv_evict_args from tensors: ``weights`` and ``weights_out`` float32 [layers, sequences, kv heads, tokens],
+    ``kept`` int32 [layers, sequences, kv heads, budget] contiguous, tables int32 [sequences, blocks]."""
+    _int32(lens, lens_out, src_table, dst_table, kept)
+    _float32(weights, weights_out)
+    n_layers, n_seq, n_kv, _ = weights.shape
+    if tuple(kept.shape) != (n_layers, n_seq, n_kv, budget) or not kept.is_contiguous():
+        raise ValueError("kept is int32 [layers, sequences, kv heads, budget], contiguous")
+    if src_table.shape[0] != n_seq or dst_table.shape[0] != n_seq or lens.shape[0] != n_seq:
+        raise ValueError("lens and tables disagree about the number of sequences")
+    o = (0, 0, 0, 1) if weights_out is None else weights_out.stride()
+    a = KvEvictArgs(weights=_dev(weights), weights_out=_dev(weights_out), lens=_dev(lens), lens_out=_dev(lens_out),
+                    src_table=_dev(src_table), dst_table=_dev(dst_table), kept=_dev(kept), w_layer_stride=weights.stride(0),
+                    w_seq_stride=weights.stride(1), w_head_stride=weights.stride(2), o_layer_stride=o[0], o_seq_stride=o[1],
+                    o_head_stride=o[2], src_stride=src_table.stride(0), dst_stride=dst_table.stride(0), n_layers=n_layers,
+                    layer_planes=layer_planes, n_seq=n_seq, max_len=max_len, budget=budget, sinks=sinks, recent=recent)
+    a._keep = (weights, weights_out, lens, lens_out, src_table, dst_table, kept)
+    return a
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
+
+
+def gms_kv_attention_workspace(pool: KvPool, layout: KvLayout, attn: KvAttn, weight: KvWeight | None = None) -> int:
+    v = C.c_uint64()
+    _check(lib().gms_kv_attention_workspace(_ref(pool), _ref(layout), _ref(attn), _ref(weight), C.byref(v)),
+           "gms_kv_attention_workspace")
+    return v.value
+
+
+def gms_kv_attention(pool: KvPool, layout: KvLayout, attn: KvAttn, weight: KvWeight | None = None, stream=None):
+    _check(lib().gms_kv_attention(_ref(pool), _ref(layout), _ref(attn), _ref(weight), _stream(stream)), "gms_kv_attention")
+
+
+def gms_kv_attention_shared_workspace(pool: KvPool, layout: KvLayout, attn: KvAttn, prefix: KvPrefix) -> int:
+    v = C.c_uint64()
+    _check(lib().gms_kv_attention_shared_workspace(_ref(pool), _ref(layout), _ref(attn), _ref(prefix), C.byref(v)),
+           "gms_kv_attention_shared_workspace")
+    return v.value
+
+
+def gms_kv_attention_shared(pool: KvPool, layout: KvLayout, attn: KvAttn, prefix: KvPrefix, stream=None):
+    _check(lib().gms_kv_attention_shared(_ref(pool), _ref(layout), _ref(attn), _ref(prefix), _stream(stream)),
+           "gms_kv_attention_shared")
+
+
+def gms_kv_evict(pool: KvPool, layout: KvLayout, args: KvEvictArgs, stream=None):
+    _check(lib().gms_kv_evict(_ref(pool), _ref(layout), _ref(args), _stream(stream)), "gms_kv_evict")
 
 
 def gms_host_image_alloc(nbytes: int):
