@@ -1,4 +1,4 @@
-// Attention over the paged KV pool: host entry points, and the row kernel.
+// Attention over the paged KV pool: host entry points, the plan of a call, and the weights pass.
 #include <cmath>
 
 #include "gms_internal.h"
@@ -6,58 +6,6 @@
 
 namespace gms {
 namespace {
-
-// One warp computes one (query row, head) in 32 bits, token by token: the definition, written down.  Lanes split the
-// head dimension; the running maximum m, sum l and weighted values o are rescaled when the maximum moves.
-template <class T, int D>
-__device__ void attend_tokens(const AttnArgs &a, const float *q, uint32_t c, const int32_t *table, int n, int pos, bool whole,
-                              float &m, float &l, float *o)
-{
-    constexpr int E = D / 32;
-    const uint32_t lane = threadIdx.x & 31u;
-    for (int t = 0; t < n; ++t) {
-        if (!whole && !sees(a, pos, t)) continue;
-        const int id = table[t >> a.block_shift];
-        if ((uint32_t)id >= a.n_blocks) continue;
-        const uint64_t off = (uint64_t)id * a.block_stride + (uint64_t)(t & ((1 << a.block_shift) - 1)) * a.token_stride +
-                             (uint64_t)c * a.head_stride;
-        const T *k = reinterpret_cast<const T *>(a.k_base + off), *v = reinterpret_cast<const T *>(a.v_base + off);
-        float x = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x += q[e] * to_f32(k[lane + 32 * e]);
-        x = warp_sum(x) * a.scale * kLog2e;
-        const float mn = fmaxf(m, x), f = mn == neg_inf() ? 1.f : exp2f(m - mn), p = exp2f(x - (mn == neg_inf() ? 0.f : mn));
-        l = l * f + p;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + p * to_f32(v[lane + 32 * e]);
-        m = mn;
-    }
-}
-
-template <class T, int D>
-__global__ void __launch_bounds__(128) kv_attention_rows_kernel(AttnArgs a)
-{
-    constexpr int E = D / 32;
-    const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t row = (uint64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    if (row >= (uint64_t)a.total_q * a.n_heads) return;
-    const int tok = (int)(row / a.n_heads);
-    const uint32_t h = (uint32_t)(row % a.n_heads), c = h / a.group, s = owner_of_row(a, tok);
-    if (s >= a.n_seq) return;
-    const T *qp = reinterpret_cast<const T *>(a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)h * a.q_head_stride);
-    float q[E], o[E], m = neg_inf(), l = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) q[e] = to_f32(qp[lane + 32 * e]), o[e] = 0.f;
-    const uint32_t g = group_of_seq(a, s);
-    if (g < a.n_groups) attend_tokens<T, D>(a, q, c, a.prefix_table + g * a.prefix_stride, prefix_len(a, g), 0, true, m, l, o);
-    const int n = seq_kv_len(a, s);
-    attend_tokens<T, D>(a, q, c, a.table + s * a.table_stride, n, n - seq_q_len(a, s) + tok - seq_q_begin(a, s), false, m, l, o);
-    T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int e = 0; e < E; ++e) op[lane + 32 * e] = from_f32<T>(l == 0.f ? 0.f : o[e] * inv);
-    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
-}
 
 // One warp accumulates the weight of one (sequence, KV head, token), rows in order.
 template <class T, int D>
@@ -102,16 +50,6 @@ __global__ void __launch_bounds__(128) kv_weights_kernel(AttnArgs a, const float
             if (head_dim == 64) K<__half, 64> __VA_ARGS__; else K<__half, 128> __VA_ARGS__; \
         }                                                                             \
     } while (0)
-
-cudaError_t launch_kv_attention_rows(const AttnArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
-{
-    const uint64_t rows = (uint64_t)a.total_q * a.n_heads;
-    const uint32_t grid = (uint32_t)((rows + 3) / 4);
-    if (grid == 0) return cudaSuccess;
-    GMS_BY_TYPE(kv_attention_rows_kernel, <<<grid, 128, 0, s>>>(a));
-    count_launches(1);
-    return cudaGetLastError();
-}
 
 cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
@@ -238,27 +176,135 @@ int make_args(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv
     return GMS_OK;
 }
 
-uint64_t workspace_bytes(const AttnArgs &a)
+// One layer's keys or values as a 4-d tensor (d, token of block, head, block); boxes of 64 elements x `box_tokens` tokens.
+int encode_map(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, uint32_t plane, uint32_t box_tokens)
 {
-    uint64_t n = 0;
-    if (a.w_out && !a.lse) n += (uint64_t)a.total_q * a.n_heads * 4;  // the weights pass needs the log-sum-exps
-    return (n + 255) / 256 * 256;
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<Encode>(p);
+    }();
+    if (!encode) return report_cuda_error(cudaErrorNotSupported);
+    const cuuint64_t dims[4] = {l->head_dim, l->block_tokens, l->n_kv_heads, pool->n_blocks};
+    // a stride along a dimension of one element is never used, but has to be a legal one
+    const cuuint64_t strides[3] = {l->token_stride, l->n_kv_heads > 1 ? l->head_stride : l->token_stride,
+                                   pool->n_blocks > 1 ? pool->block_stride : pool->block_bytes};
+    const cuuint32_t box[4] = {64, box_tokens, 1, 1}, one[4] = {1, 1, 1, 1};
+    uint8_t *base = static_cast<uint8_t *>(pool->base) + plane * pool->plane_stride;
+    const CUresult r = encode(m, l->dtype == GMS_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base,
+                              dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? GMS_OK : report_cuda_error(cudaErrorInvalidValue);
+}
+
+struct Carve {  // hands out 256-byte aligned pieces of the workspace; with a null base it only counts
+    uint8_t *base;
+    uint64_t used = 0;
+    template <class T> T *take(uint64_t n)
+    {
+        T *p = base ? reinterpret_cast<T *>(base + used) : nullptr;
+        used += (n * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+struct Plan {
+    Pass own, prefix;
+    bool shared, logits;
+    float *lse;  // where the weights pass finds the log-sum-exps
+};
+
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// Most tiles a pass can have, from what the host knows.
+uint64_t most_tiles(const AttnArgs &a, const Pass &p)
+{
+    uint64_t span = p.prefix ? a.max_prefix : a.max_kv;
+    if (!p.prefix && a.window) {
+        const uint64_t seen = (uint64_t)a.window + a.sinks + 2 * p.tile + (p.rows - 1) / a.group;
+        if (seen < span) span = seen;
+    }
+    return p.n_units * (uint64_t)a.n_kv * ceil_div(span, p.tile);
+}
+
+void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
+{
+    *p = {};
+    const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
+    p->prefix = prefix;
+    p->rows = kFewRows;
+    p->tile = kFewTile;
+    p->n_rt = (uint32_t)ceil_div(rows, p->rows);
+    if (p->n_rt == 0) p->n_rt = 1;
+    p->n_units = (prefix ? a.n_groups : a.n_seq) * p->n_rt;
+    // two CTAs an SM; fewer where they would have fewer than eight tiles (two a warp)
+    const uint64_t want = ceil_div(most_tiles(a, *p), 8);
+    p->n_cta = (uint32_t)(want < 1 ? 1 : want < kFewMaxCtas ? want : kFewMaxCtas);
+    p->begin = c->take<uint64_t>(p->n_units + 1);
+    p->part_ml = c->take<float2>(2ull * p->n_cta * p->rows);
+    p->part_o = c->take<float>(2ull * p->n_cta * p->rows * head_dim);
+    if (rows_out) {
+        p->row_ml = c->take<float2>((uint64_t)a.total_q * a.n_heads);
+        p->row_o = c->take<float>((uint64_t)a.total_q * a.n_heads * head_dim);
+    }
+    p->redo = a.max_q > 1;  // with one query a sequence, what its rows do not see is cleared before the product
+}
+
+void plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace, Plan *pl, uint64_t *bytes)
+{
+    *pl = {};
+    Carve c{static_cast<uint8_t *>(workspace)};
+    pl->shared = shared;
+    plan_pass(a, head_dim, false, shared, &c, &pl->own);
+    if (shared) plan_pass(a, head_dim, true, true, &c, &pl->prefix);
+    pl->lse = a.lse;
+    if (a.w_out) {
+        if (!a.lse) pl->lse = c.take<float>((uint64_t)a.total_q * a.n_heads);
+        if (pl->own.n_rt == 1) {
+            pl->logits = true;
+            pl->own.logit_stride = (a.max_kv + kFewTile - 1) / kFewTile * kFewTile;
+            pl->own.logits = c.take<float>((uint64_t)a.n_seq * a.n_heads * a.max_q * pl->own.logit_stride);
+        }
+    }
+    *bytes = c.used;
 }
 
 int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *t, const gms_kv_weight *w,
                    const gms_kv_prefix *x, void *stream)
 {
     AttnArgs a;
-    const int rc = make_args(pool, layout, t, w, x, &a);
+    int rc = make_args(pool, layout, t, w, x, &a);
     if (rc != GMS_OK) return rc;
-    const uint64_t need = workspace_bytes(a);
-    if (need && !t->workspace) return GMS_ERR_NULL;
-    if (need > t->workspace_bytes) return GMS_ERR_RANGE;
+    Plan pl;
+    uint64_t need = 0;
+    plan_call(a, layout->head_dim, x != nullptr, t->workspace, &pl, &need);
     if (a.n_seq == 0) return GMS_OK;
+    if (!t->workspace) return GMS_ERR_NULL;
+    if (need > t->workspace_bytes) return GMS_ERR_RANGE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (w && !a.lse) a.lse = static_cast<float *>(t->workspace);
-    cudaError_t e = launch_kv_attention_rows(a, layout->dtype, layout->head_dim, s);
-    if (e == cudaSuccess && w) e = launch_kv_weights(a, a.lse, layout->dtype, layout->head_dim, s);
+    const uint32_t dtype = layout->dtype, dim = layout->head_dim;
+    cudaError_t e = cudaSuccess;
+    if (a.total_q) {
+        CUtensorMap kmap, vmap;
+        rc = encode_map(&kmap, pool, layout, layout->k_plane, kFewTile);
+        if (rc == GMS_OK) rc = encode_map(&vmap, pool, layout, layout->v_plane, kFewTile);
+        if (rc != GMS_OK) return rc;
+        AttnArgs b = a;
+        b.lse = pl.lse;
+        if (pl.shared && pl.prefix.n_units) e = launch_kv_attn_few(b, pl.prefix, kmap, vmap, dtype, dim, s);
+        if (e == cudaSuccess) e = launch_kv_attn_few(b, pl.own, kmap, vmap, dtype, dim, s);
+        if (e == cudaSuccess)
+            e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s) : launch_kv_attn_join(b, pl.own, dtype, dim, s);
+        if (e == cudaSuccess && w && pl.logits) e = launch_kv_few_weights(b, pl.own, s);
+    }
+    if (e == cudaSuccess && w && !(a.total_q && pl.logits)) e = launch_kv_weights(a, pl.lse, dtype, dim, s);
     return e == cudaSuccess ? GMS_OK : report_cuda_error(e);
 }
 
@@ -273,7 +319,8 @@ int gms_kv_attention_workspace(const gms_kv_pool *pool, const gms_kv_layout *lay
     if (!nbytes) return GMS_ERR_NULL;
     gms::AttnArgs a;
     const int rc = gms::make_args(pool, layout, attn, weight, nullptr, &a);
-    if (rc == GMS_OK) *nbytes = gms::workspace_bytes(a);
+    gms::Plan plan;
+    if (rc == GMS_OK) gms::plan_call(a, layout->head_dim, false, nullptr, &plan, nbytes);
     return rc;
 }
 
@@ -289,7 +336,8 @@ int gms_kv_attention_shared_workspace(const gms_kv_pool *pool, const gms_kv_layo
     if (!nbytes || !prefix) return GMS_ERR_NULL;
     gms::AttnArgs a;
     const int rc = gms::make_args(pool, layout, attn, nullptr, prefix, &a);
-    if (rc == GMS_OK) *nbytes = gms::workspace_bytes(a);
+    gms::Plan plan;
+    if (rc == GMS_OK) gms::plan_call(a, layout->head_dim, true, nullptr, &plan, nbytes);
     return rc;
 }
 

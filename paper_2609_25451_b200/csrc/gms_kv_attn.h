@@ -2,6 +2,7 @@
 #pragma once
 #include <cstdint>
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -9,6 +10,8 @@
 #include "gms.h"
 
 namespace gms {
+
+void count_launches(uint32_t n);
 
 // What every attention kernel gets (by value).  Strides of pool and of q / out are in bytes.
 struct AttnArgs {
@@ -36,6 +39,26 @@ struct AttnArgs {
     unsigned long long *status;  // may be null
 };
 
+// How a pass over cached tokens is cut.  A unit is a run of up to ROWS query rows (token-major, the heads of one KV head
+// inside a token) of one sequence (or, in a prefix pass, of one group); an item is a unit for one KV head; an item's work
+// is the list of token tiles that at least one of its rows sees.  All items' tiles, one after the other, are dealt out
+// evenly: CTA i of n takes tiles [T*i/n, T*(i+1)/n), whatever items they fall into, so ragged lengths cost no balance.
+// An item that one CTA has whole is finished there; the at most two pieces a CTA has of others go to its two slots of
+// part_o / part_ml and are joined by kv_attn_join.
+struct Pass {
+    uint32_t prefix;       // 1: units are groups' query rows over their prefix, all of it seen
+    uint32_t n_units, n_rt, n_cta;  // n_rt units a sequence (group)
+    uint32_t rows, tile;   // rows a unit, tokens a tile
+    uint64_t *begin;       // [n_units + 1] tiles before each unit (written by CTA 0 for the join)
+    float *part_o;         // [2 * n_cta][rows][head_dim], not normalised
+    float2 *part_ml;       // [2 * n_cta][rows]: running maximum (base 2) and sum
+    float *row_o;          // null: finished rows go to out / lse; else [total_q * n_heads][head_dim], not normalised
+    float2 *row_ml;        // [total_q * n_heads]
+    float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2 (few-row pass only)
+    uint32_t logit_stride;
+    uint32_t redo;         // 1: rows that come out non-finite are done again by the row kernel's method
+};
+
 struct EvictArgs {
     uint8_t *base;
     uint64_t plane_stride, block_stride;
@@ -50,13 +73,40 @@ struct EvictArgs {
     uint32_t n_layers, layer_planes, n_seq, n_kv, max_len, budget, sinks, recent;
 };
 
-cudaError_t launch_kv_attention_rows(const AttnArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+// Joins the two passes of a shared-prefix call, row by row.
+cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, const Pass &own, uint32_t dtype, uint32_t head_dim,
+                                       cudaStream_t s);
+// Few query rows a unit (at most 16): kv_attn_few; many: kv_attn_tc.
+constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewMaxCtas = 2 * 148;
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
+                               uint32_t head_dim, cudaStream_t s);
+cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);
+
+// Launches a kernel that may start before the one ahead of it in the stream has drained (it waits for it itself).
+template <class K, class... A>
+cudaError_t launch_dependent(K kernel, uint32_t grid, uint32_t block, uint32_t smem, cudaStream_t s, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e == cudaSuccess) count_launches(1);
+    return e;
+}
 
 #ifdef __CUDACC__
 // ------------------------------------------------------------------ device helpers
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kHuge = 3.4e38f;
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -111,11 +161,186 @@ __device__ __forceinline__ uint32_t group_of_seq(const AttnArgs &a, uint32_t s)
     if (a.n_groups == 0 || (int)s < a.group_start[0] || (int)s >= a.group_start[a.n_groups]) return a.n_groups;
     return last_not_above(a.group_start, a.n_groups, (int)s);
 }
+struct Unit {
+    const int32_t *table;
+    int q0, row0, rows;      // first query row of the sequence (group); first row of the unit and their number
+    int n, first;            // cached tokens; position of the sequence's first query
+    int pos_min, pos_max;    // of the unit's rows
+    int n_sink_tiles, first_tile, tiles;  // tile list: 0 .. n_sink_tiles-1, then first_tile ..; `tiles` in all
+    bool whole;              // every row sees every token
+};
+__device__ __forceinline__ int unit_tile(const Unit &u, int k) { return k < u.n_sink_tiles ? k : u.first_tile + k - u.n_sink_tiles; }
+__device__ __forceinline__ int unit_row_pos(const AttnArgs &a, const Unit &u, int r)
+{
+    return u.whole ? u.n - 1 : u.first + (u.row0 + r) / (int)a.group;
+}
+// Query row and head of row r of a unit.
+__device__ __forceinline__ int unit_tok(const AttnArgs &a, const Unit &u, int r) { return u.q0 + (u.row0 + r) / (int)a.group; }
+__device__ __forceinline__ uint32_t unit_head(const AttnArgs &a, const Unit &u, uint32_t c, int r)
+{
+    return c * a.group + (uint32_t)(u.row0 + r) % a.group;
+}
+// `s`: sequence or group, `rt`: row tile of it.
+template <int ROWS, int TILE>
+__device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint32_t s, uint32_t rt)
+{
+    Unit u;
+    int q_len;
+    if (p.prefix) {
+        const int s0 = min(max(a.group_start[s], 0), (int)a.n_seq), s1 = min(max(a.group_start[s + 1], s0), (int)a.n_seq);
+        u.q0 = a.cu_q ? min(max(a.cu_q[s0], 0), (int)a.total_q) : s0;
+        const int end = a.cu_q ? min(max(a.cu_q[s1], u.q0), (int)a.total_q) : s1;
+        q_len = min(end - u.q0, (int)a.max_group_q);
+        u.n = prefix_len(a, s);
+        u.table = a.prefix_table + s * a.prefix_stride;
+        u.whole = true;
+    } else {
+        u.q0 = seq_q_begin(a, s);
+        q_len = seq_q_len(a, s);
+        u.n = seq_kv_len(a, s);
+        u.table = a.table + s * a.table_stride;
+        u.whole = false;
+    }
+    u.first = u.n - q_len;
+    u.row0 = (int)rt * ROWS;
+    u.rows = (int)min(max((long long)q_len * a.group - u.row0, 0ll), (long long)ROWS);
+    u.n_sink_tiles = u.first_tile = u.tiles = 0;
+    u.pos_min = u.pos_max = u.n - 1;
+    if (u.rows > 0) {
+        if (!u.whole) {
+            u.pos_min = u.first + u.row0 / (int)a.group;
+            u.pos_max = u.first + (u.row0 + u.rows - 1) / (int)a.group;
+        }
+        if (u.pos_max >= 0) {
+            int lo = 0;
+            if (!u.whole && a.window) lo = (int)max(0ll, (long long)u.pos_min - (long long)a.window + 1);
+            u.first_tile = lo / TILE;
+            u.n_sink_tiles = (int)min((long long)u.first_tile, ((long long)a.sinks + TILE - 1) / TILE);
+            u.tiles = u.n_sink_tiles + u.pos_max / TILE + 1 - u.first_tile;
+        }
+    }
+    return u;
+}
+// The part of the work that a CTA has, item by item.
+struct Walk {
+    uint64_t pos, end;   // tiles still to do, in the order over all items
+    uint64_t base;       // tiles before the current unit
+    uint32_t s, rt;
+};
+// Scans all units, finds CTA `cta`'s share.  Every thread of the CTA calls it and gets the same result; `sh` is 8 * (warps + 3)
+// bytes of shared memory.  CTA 0 also writes p.begin.
+template <int ROWS, int TILE, int THREADS>
+__device__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint64_t *sh)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t per = (p.n_units + THREADS - 1) / THREADS, u0 = min(tid * per, p.n_units), u1 = min(u0 + per, p.n_units);
+    uint64_t mine = 0;
+#pragma unroll 4
+    for (uint32_t u = u0; u < u1; ++u) mine += (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
+    uint64_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= (uint32_t)o) inc += x;
+    }
+    if (lane == 31) sh[warp] = inc;
+    if (tid == 0) sh[THREADS / 32 + 1] = p.n_units;
+    __syncthreads();
+    uint64_t before = inc - mine, total = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < THREADS / 32; ++i) {
+        if (i < warp) before += sh[i];
+        total += sh[i];
+    }
+    Walk w;
+    w.pos = total * cta / p.n_cta;
+    w.end = total * (cta + 1) / p.n_cta;
+    if (mine && before <= w.pos && w.pos < before + mine) {
+        uint64_t b = before;
+        for (uint32_t u = u0; u < u1; ++u) {
+            const uint64_t t = (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
+            if (w.pos < b + t) {
+                sh[THREADS / 32] = b;
+                sh[THREADS / 32 + 1] = u;
+                break;
+            }
+            b += t;
+        }
+    }
+    if (cta == 0) {
+        uint64_t b = before;
+        for (uint32_t u = u0; u < u1; ++u) {
+            p.begin[u] = b;
+            b += (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
+        }
+        if (tid == 0) p.begin[p.n_units] = total;
+    }
+    __syncthreads();
+    w.base = sh[THREADS / 32];
+    const uint32_t u = (uint32_t)sh[THREADS / 32 + 1];
+    w.s = u / p.n_rt;
+    w.rt = u % p.n_rt;
+    return w;
+}
+// Which CTA's share holds tile t of T.
+__device__ __forceinline__ uint32_t tile_owner(uint64_t t, uint64_t total, uint32_t n_cta)
+{
+    return (uint32_t)(((t + 1) * n_cta - 1) / total);
+}
 __device__ __forceinline__ float warp_sum(float x)
 {
 #pragma unroll
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
+}
+
+// One warp computes one (query row, head) in 32 bits, token by token: the definition, written down.  Lanes split the
+// head dimension; the running maximum m, sum l and weighted values o are rescaled when the maximum moves.
+template <class T, int D>
+__device__ __noinline__ void attend_tokens(const AttnArgs &a, const float *q, uint32_t c, const int32_t *table, int n, int pos,
+                                           bool whole, float &m, float &l, float *o)
+{
+    constexpr int E = D / 32;
+    const uint32_t lane = threadIdx.x & 31u;
+    for (int t = 0; t < n; ++t) {
+        if (!whole && !sees(a, pos, t)) continue;
+        const int id = table[t >> a.block_shift];
+        if ((uint32_t)id >= a.n_blocks) continue;
+        const uint64_t off = (uint64_t)id * a.block_stride + (uint64_t)(t & ((1 << a.block_shift) - 1)) * a.token_stride +
+                             (uint64_t)c * a.head_stride;
+        const T *k = reinterpret_cast<const T *>(a.k_base + off), *v = reinterpret_cast<const T *>(a.v_base + off);
+        float x = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x += q[e] * to_f32(k[lane + 32 * e]);
+        x = warp_sum(x) * a.scale * kLog2e;
+        const float mn = fmaxf(m, x), f = mn == neg_inf() ? 1.f : exp2f(m - mn), p = exp2f(x - (mn == neg_inf() ? 0.f : mn));
+        l = l * f + p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * f + p * to_f32(v[lane + 32 * e]);
+        m = mn;
+    }
+}
+// The matrix-product kernels multiply a weight of 0 with the values of tokens that some rows of a tile see and others do
+// not; where such a value is NaN or infinite the product is NaN.  Rows that come out non-finite are therefore done again
+// by this, which never touches what a row does not see (called by a whole warp).
+template <class T, int D>
+__device__ __noinline__ void attend_row(const AttnArgs &a, int tok, uint32_t h)
+{
+    constexpr int E = D / 32;
+    const uint32_t lane = threadIdx.x & 31u, c = h / a.group, s = owner_of_row(a, tok);
+    if (s >= a.n_seq) return;
+    const T *qp = reinterpret_cast<const T *>(a.q + (uint64_t)tok * a.q_token_stride + (uint64_t)h * a.q_head_stride);
+    float q[E], o[E], m = neg_inf(), l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) q[e] = to_f32(qp[lane + 32 * e]), o[e] = 0.f;
+    const uint32_t g = group_of_seq(a, s);
+    if (g < a.n_groups) attend_tokens<T, D>(a, q, c, a.prefix_table + g * a.prefix_stride, prefix_len(a, g), 0, true, m, l, o);
+    const int n = seq_kv_len(a, s);
+    attend_tokens<T, D>(a, q, c, a.table + s * a.table_stride, n, n - seq_q_len(a, s) + tok - seq_q_begin(a, s), false, m, l, o);
+    T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride);
+#pragma unroll
+    for (int e = 0; e < E; ++e) op[lane + 32 * e] = from_f32<T>(l == 0.f ? 0.f : o[e] / l);
+    if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
 }
 #endif
 

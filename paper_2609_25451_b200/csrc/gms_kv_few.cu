@@ -1,0 +1,458 @@
+// Attention of few query rows (at most 16 a KV head: one token of a grouped-query model, or a few) over the paged pool.
+//
+// Bound: memory.  Every visible K and V row is read once; 16 rows of mma.sync per 256-byte row are far below the tensor
+// rate, so the legacy matrix instruction is enough and what counts is bytes in flight and an even deal (see Pass).
+// Every warp is its own pipeline, as in the streaming kernels: tiles of 16 tokens come by TMA through the block table into
+// the warp's ring (K and V of one KV head, 128-byte swizzle, so that ldmatrix has no bank conflicts), no warp waits for
+// another before an item ends.  S = Q K^T, the online softmax and O += P V stay in registers; the four warps of the CTA
+// take every fourth tile and are joined in shared memory at the end of an item.
+#include "gms_internal.h"
+#include "gms_kv_attn.h"
+#include "gms_ptx.h"
+
+namespace gms {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+
+__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __nv_bfloat16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __half)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <int D, bool HI>
+struct Few {
+    static constexpr int kHalves = D / 64;
+    static constexpr uint32_t kStageBytes = 2 * kHalves * 2048;          // K then V, 16 tokens x 128 bytes a half
+    static constexpr int kStages = D == 128 ? (HI ? 2 : 3) : 6;       // so that two CTAs share an SM
+    static constexpr uint32_t kRing = kStages * kStageBytes;             // a warp's
+    static constexpr int kFrag = D / 8 * (HI ? 4 : 2);                   // floats of O a lane carries into the join
+    static constexpr uint32_t kJoin = 2 * kFrag * 32 * 4;
+    static constexpr uint32_t kSmem = kWarps * kRing + kJoin + 2 * 32 * (HI ? 16 : 8) + kWarps * kStages * 8 + 8 * (kWarps + 3) + 1024;
+};
+
+// Registers of a warp's running softmax over its share of an item.
+template <int D>
+struct Acc {
+    float o[D / 8][4], m[2], l[2];
+};
+
+template <int D, bool HI>
+__device__ __forceinline__ void join_from(Acc<D> &x, const float *o, const float *ml, uint32_t lane)
+{
+    constexpr int R = HI ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const float m2 = ml[(i * 2 + 0) * 32 + lane], l2 = ml[(i * 2 + 1) * 32 + lane], mn = fmaxf(x.m[i], m2);
+        const float f1 = x.m[i] == mn ? 1.f : ex2(x.m[i] - mn), f2 = m2 == mn ? 1.f : ex2(m2 - mn);
+        x.m[i] = mn;
+        x.l[i] = x.l[i] * f1 + l2 * f2;
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                x.o[j][i * 2 + e] = x.o[j][i * 2 + e] * f1 + o[((j * R + i) * 2 + e) * 32 + lane] * f2;
+    }
+}
+template <int D, bool HI>
+__device__ __forceinline__ void join_put(const Acc<D> &x, float *o, float *ml, uint32_t lane)
+{
+    constexpr int R = HI ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        ml[(i * 2 + 0) * 32 + lane] = x.m[i];
+        ml[(i * 2 + 1) * 32 + lane] = x.l[i];
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) o[((j * R + i) * 2 + e) * 32 + lane] = x.o[j][i * 2 + e];
+    }
+}
+
+// HI: the units have more than 8 rows (the upper half of the 16-row fragments is in use).
+template <class T, int D, bool HI>
+__global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_constant__ CUtensorMap kmap,
+                                                                  const __grid_constant__ CUtensorMap vmap,
+                                                                  const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p)
+{
+    using F = Few<D, HI>;
+    constexpr int S = F::kStages, NJ = D / 8;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *sm = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t ring = base + warp * F::kRing;
+    float *jo = reinterpret_cast<float *>(sm + kWarps * F::kRing);           // two buffers of F::kFrag * 32 floats
+    float *jml = jo + 2 * F::kFrag * 32;                                      // two of (HI ? 4 : 2) * 32
+    uint64_t *bars = reinterpret_cast<uint64_t *>(jml + 2 * 32 * (HI ? 4 : 2));
+    uint64_t *plan = bars + kWarps * S;
+    const uint32_t bar = smem_u32(bars + warp * S);
+    if (lane == 0) {
+        for (int i = 0; i < S; ++i) mbar_init(bar + 8 * i, 1);
+        fence_mbar_init();
+        if (warp == 0) {
+            tma_prefetch_map(&kmap);
+            tma_prefetch_map(&vmap);
+        }
+    }
+    grid_launch_dependents();
+    Walk w = plan_walk<kFewRows, kFewTile, kThreads>(a, p, blockIdx.x, plan);
+
+    // units that see nothing: zero rows (the join knows nothing of them)
+    for (uint32_t u = blockIdx.x; u < p.n_units; u += gridDim.x) {
+        const Unit un = get_unit<kFewRows, kFewTile>(a, p, u / p.n_rt, u % p.n_rt);
+        if (un.rows == 0 || un.tiles != 0) continue;
+        for (uint32_t i = tid; i < un.rows * a.n_kv; i += kThreads) {
+            const int r = i % un.rows;
+            const uint32_t h = unit_head(a, un, i / un.rows, r);
+            const uint64_t tok = unit_tok(a, un, r);
+            if (p.row_o) {
+                p.row_ml[tok * a.n_heads + h] = make_float2(neg_inf(), 0.f);
+            } else {
+                uint4 *op = reinterpret_cast<uint4 *>(a.out + tok * a.out_token_stride + h * a.out_head_stride);
+                for (int d = 0; d < D / 8; ++d) op[d] = make_uint4(0, 0, 0, 0);
+                if (a.lse) a.lse[tok * a.n_heads + h] = neg_inf();
+            }
+        }
+    }
+
+    const float c2 = a.scale * kLog2e;
+    const uint32_t tok_mask = (1u << a.block_shift) - 1u;
+    uint32_t put = 0, got = 0;  // stages issued / consumed since the start
+    bool failed = false;
+    Unit un;
+    uint32_t c = 0;
+    int k0 = 0, k1 = 0;          // the CTA's tiles of the item's list
+    int ids = 0, ids_old = 0;    // block ids of the warp's tiles 32b + lane: current and previous batch
+
+    auto segment = [&]() -> bool {  // the next run of tiles of one item
+        if (w.pos >= w.end) return false;
+        for (;;) {
+            un = get_unit<kFewRows, kFewTile>(a, p, w.s, w.rt);
+            const uint64_t t = (uint64_t)un.tiles * a.n_kv;
+            if (w.pos < w.base + t) break;
+            w.base += t;
+            if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+        }
+        const uint64_t in = w.pos - w.base;
+        c = (uint32_t)(in / (uint32_t)un.tiles);
+        k0 = (int)(in % (uint32_t)un.tiles);
+        k1 = (int)min((uint64_t)un.tiles, (uint64_t)k0 + (w.end - w.pos));
+        return true;
+    };
+    auto count = [&]() { return (k1 - k0 - (int)warp + kWarps - 1) / kWarps; };  // tiles of this warp (may be <= 0)
+    auto issue = [&](int i) {  // i: index among the warp's tiles
+        if ((i & 31) == 0) {
+            ids_old = ids;
+            const int k = k0 + (int)warp + kWarps * (i + (int)lane);
+            ids = k < k1 ? un.table[(uint32_t)(unit_tile(un, k) * kFewTile) >> a.block_shift] : -1;
+        }
+        const int id = __shfl_sync(0xffffffffu, ids, i & 31);
+        if (lane == 0) {
+            const uint32_t st = put % S, dst = ring + st * F::kStageBytes, b = bar + 8 * st;
+            const int y = (int)((uint32_t)(unit_tile(un, k0 + (int)warp + kWarps * i) * kFewTile) & tok_mask);
+            const int blk = (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;  // a hole: out of range, zeros arrive
+            mbar_expect(b, F::kStageBytes);
+#pragma unroll
+            for (int h = 0; h < F::kHalves; ++h) {
+                tma_load_4d(dst + h * 2048, &kmap, h * 64, y, (int)c, blk, b);
+                tma_load_4d(dst + (F::kHalves + h) * 2048, &vmap, h * 64, y, (int)c, blk, b);
+            }
+        }
+        ++put;
+    };
+
+    bool live = segment();
+    if (live)
+        for (int i = 0; i < S && i < count(); ++i) issue(i);
+    while (live) {
+        const int nt = count();
+        const int r0 = lane / 4, r1 = r0 + 8;
+        // the item's query rows as matrix fragments; rows that do not exist are zero
+        uint32_t q[D / 16][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = i ? r1 : r0;
+            const bool on = r < un.rows;
+            const uint64_t tok = unit_tok(a, un, on ? r : 0);
+            const uint32_t h = unit_head(a, un, c, on ? r : 0);
+            const uint32_t *qp = reinterpret_cast<const uint32_t *>(a.q + tok * a.q_token_stride + h * a.q_head_stride) + (lane & 3u);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                q[kk][i] = on ? qp[kk * 8] : 0u;
+                q[kk][i + 2] = on ? qp[kk * 8 + 4] : 0u;
+            }
+        }
+        const int p0 = unit_row_pos(a, un, r0), p1 = unit_row_pos(a, un, r1);
+        Acc<D> x;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.o[j][e] = 0.f;
+        x.m[0] = x.m[1] = neg_inf();
+        x.l[0] = x.l[1] = 0.f;
+
+        for (int i = 0; i < nt && !failed; ++i) {
+            const uint32_t st = got % S, kt = ring + st * F::kStageBytes, vt = kt + F::kHalves * 2048;
+            if (!__all_sync(0xffffffffu, mbar_wait(bar + 8 * st, (got / S) & 1u))) {
+                failed = true;
+                break;
+            }
+            ++got;
+            // the batch that i belongs to is the current one unless the issue side has moved on
+            const int last = min(i + S, nt) - 1;  // newest tile issued so far
+            const int id = __shfl_sync(0xffffffffu, (last >> 5) == (i >> 5) ? ids : ids_old, i & 31);
+            const int t0 = unit_tile(un, k0 + (int)warp + kWarps * i) * kFewTile;
+            float s[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[j][e] = 0.f;
+            const uint32_t krow = (lane & 7u) + ((lane >> 4) << 3);  // token of this lane's ldmatrix row
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t ch = (kk & 3) * 2 + ((lane >> 3) & 1u);
+                uint32_t b[4];
+                ldmatrix_x4(kt + (kk / 4) * 2048 + krow * 128 + ((ch ^ (krow & 7u)) << 4), b);
+                mma16816(s[0], q[kk], b[0], b[1], T());
+                mma16816(s[1], q[kk], b[2], b[3], T());
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[j][e] *= c2;
+            const int t1 = t0 + kFewTile - 1;
+            const bool hole = (uint32_t)id >= a.n_blocks;
+            const bool full = !hole && t1 <= un.pos_min &&
+                              (un.whole || a.window == 0 || (long long)t0 > (long long)un.pos_max - (long long)a.window || (uint32_t)t1 < a.sinks);
+            if (!full) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int t = t0 + j * 8 + (int)(lane & 3u) * 2 + (e & 1);
+                        const bool on = !hole && (un.whole ? t < un.n : sees(a, e < 2 ? p0 : p1, t));
+                        if (!on) s[j][e] = neg_inf();
+                    }
+                // values that no row sees must not meet the matrix product, whatever bits they are
+                if (lane < kFewTile) {
+                    const int t = t0 + (int)lane;
+                    const bool none = t > un.pos_max || (!un.whole && !sees(a, max(un.pos_min, t), t));
+                    if (none)
+#pragma unroll
+                        for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) st_shared_zero16(vt + h * 2048 + lane * 128 + e * 16);
+                }
+                fence_proxy_async();  // before a later copy lands in this slot
+                __syncwarp();
+            }
+            if (p.logits) {
+                float *lp = p.logits + ((uint64_t)w.s * a.n_kv + c) * a.max_q * a.group * p.logit_stride;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t t = t0 + j * 8 + (lane & 3u) * 2;
+                    if (r0 < un.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r0 * p.logit_stride + t) = make_float2(s[j][0], s[j][1]);
+                    if (HI && r1 < un.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r1 * p.logit_stride + t) = make_float2(s[j][2], s[j][3]);
+                }
+            }
+            // online softmax; a row's 16 logits lie in the four lanes of a quad
+            float mn[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float v = fmaxf(fmaxf(s[0][r * 2], s[0][r * 2 + 1]), fmaxf(s[1][r * 2], s[1][r * 2 + 1]));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+                mn[r] = fmaxf(x.m[r], v);
+            }
+            if (__any_sync(0xffffffffu, mn[0] != x.m[0] || mn[1] != x.m[1])) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float f = x.m[r] == mn[r] ? 1.f : ex2(x.m[r] - mn[r]);
+                    x.m[r] = mn[r];
+                    x.l[r] *= f;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        x.o[j][r * 2] *= f;
+                        x.o[j][r * 2 + 1] *= f;
+                    }
+                }
+            }
+            const float z0 = x.m[0] == neg_inf() ? 0.f : x.m[0], z1 = x.m[1] == neg_inf() ? 0.f : x.m[1];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[j][e] = (HI || e < 2) ? ex2(s[j][e] - (e < 2 ? z0 : z1)) : 0.f;
+                    x.l[e / 2] += s[j][e];
+                }
+            // P is rounded to the pool's type for the matrix product; the sums l keep the unrounded weights
+            const uint32_t pa[4] = {pack2(s[0][0], s[0][1], T()), pack2(s[0][2], s[0][3], T()), pack2(s[1][0], s[1][1], T()),
+                                    pack2(s[1][2], s[1][3], T())};
+            const uint32_t vrow = (lane & 7u) + ((lane >> 3) & 1u) * 8;
+#pragma unroll
+            for (int j = 0; j < NJ; j += 2) {
+                const uint32_t ch = (j & 7) + (lane >> 4);
+                uint32_t b[4];
+                ldmatrix_x4_trans(vt + (j / 8) * 2048 + vrow * 128 + ((ch ^ (vrow & 7u)) << 4), b);
+                mma16816(x.o[j], pa, b[0], b[1], T());
+                mma16816(x.o[j + 1], pa, b[2], b[3], T());
+            }
+            __syncwarp();  // every lane has read the slot
+            if (i + S < nt) issue(i + S);
+        }
+        if (failed) {  // give up: no more copies; those in flight are waited for (bounded)
+            if (lane == 0 && a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+            for (int i = 0; i < S && got != put; ++i, ++got) (void)mbar_wait(bar + 8 * (got % S), (got / S) & 1u);
+            got = put;
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 1);
+            x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 2);
+        }
+        const Unit done = un;
+        const uint32_t dc = c;
+        const bool starts = k0 == 0, ends = k1 == un.tiles;
+        w.pos += (uint32_t)(k1 - k0);
+        live = segment();
+        if (live && !failed)  // the next item's first tiles are on their way while this one is joined
+            for (int i = 0; i < S && i < count(); ++i) issue(i);
+
+        __syncthreads();
+        constexpr int kMl = HI ? 4 : 2;
+        if (warp >= 2) join_put<D, HI>(x, jo + (warp - 2) * F::kFrag * 32, jml + (warp - 2) * kMl * 32, lane);
+        __syncthreads();
+        if (warp < 2) join_from<D, HI>(x, jo + warp * F::kFrag * 32, jml + warp * kMl * 32, lane);
+        __syncthreads();
+        if (warp == 1) join_put<D, HI>(x, jo, jml, lane);
+        __syncthreads();
+        if (warp != 0) continue;
+        join_from<D, HI>(x, jo, jml, lane);
+        uint32_t again = 0;  // finished rows to be done once more
+#pragma unroll
+        for (int r = 0; r < (HI ? 2 : 1); ++r) {
+            const int row = r ? r1 : r0;
+            if (row >= done.rows) continue;
+            const uint64_t tok = unit_tok(a, done, row);
+            const uint32_t h = unit_head(a, done, dc, row);
+            const float m = x.m[r], l = x.l[r];
+            if (starts && ends && !p.row_o) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                uint32_t *op = reinterpret_cast<uint32_t *>(a.out + tok * a.out_token_stride + h * a.out_head_stride) + (lane & 3u);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const float lo = x.o[j][r * 2] * inv, hi = x.o[j][r * 2 + 1] * inv;
+                    again |= !(fabsf(lo) < kHuge && fabsf(hi) < kHuge) ? 1u << r : 0u;
+                    op[j * 4] = l == 0.f ? 0u : pack2(lo, hi, T());
+                }
+                if (a.lse && (lane & 3u) == 0) a.lse[tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
+            } else {
+                uint64_t at;
+                float *po;
+                if (starts && ends) {
+                    at = tok * a.n_heads + h;
+                    po = p.row_o + at * D;
+                    if ((lane & 3u) == 0) p.row_ml[at] = make_float2(m, l);
+                } else {
+                    at = ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * kFewRows + row;
+                    po = p.part_o + at * D;
+                    if ((lane & 3u) == 0) p.part_ml[at] = make_float2(m, l);
+                }
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    *reinterpret_cast<float2 *>(po + j * 8 + (lane & 3u) * 2) = make_float2(x.o[j][r * 2], x.o[j][r * 2 + 1]);
+            }
+        }
+        if (p.redo) {
+            for (int r = 0; r < 2; ++r) {
+                const uint32_t rows = __ballot_sync(0xffffffffu, again >> r & 1u);
+                for (int row = 0; row < 8; ++row)
+                    if (rows >> (row * 4) & 15u) {
+                        __syncwarp();
+                        attend_row<T, D>(a, unit_tok(a, done, row + 8 * r), unit_head(a, done, dc, row + 8 * r));
+                    }
+            }
+        }
+    }
+}
+
+template <class T, int D, bool HI>
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
+{
+    constexpr uint32_t smem = Few<D, HI>::kSmem;
+    static const cudaError_t ready =
+        cudaFuncSetAttribute(kv_attn_few_kernel<T, D, HI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (ready != cudaSuccess) return ready;
+    kv_attn_few_kernel<T, D, HI><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, a, p);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+// One thread a token: the logits that the attention kernel left, against the finished log-sum-exps, rows in order.
+__global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p, uint32_t chunks)
+{
+    __shared__ float lse[kFewRows];
+    const uint32_t item = blockIdx.x / chunks, s = item / a.n_kv, c = item % a.n_kv;
+    const Unit u = get_unit<kFewRows, kFewTile>(a, p, s, 0);
+    grid_wait();
+    if ((int)threadIdx.x < u.rows)
+        lse[threadIdx.x] = a.lse[(uint64_t)(u.q0 + threadIdx.x / a.group) * a.n_heads + c * a.group + threadIdx.x % a.group] * kLog2e;
+    __syncthreads();
+    const int t = (int)(blockIdx.x % chunks * 256 + threadIdx.x);
+    if (t >= u.n) return;
+    const uint64_t at = s * a.w_seq_stride + c * a.w_head_stride + t;
+    const float *lp = p.logits + (uint64_t)item * a.max_q * a.group * p.logit_stride + t;
+    float sum = 0.f;
+    const int tile = t / (int)kFewTile;
+    if (u.rows > 0 && (tile < u.n_sink_tiles || (tile >= u.first_tile && tile < u.first_tile + u.tiles - u.n_sink_tiles)))
+        for (int r = 0; r < u.rows; ++r) {
+            const float x = lp[(uint64_t)r * p.logit_stride];
+            if (x != neg_inf()) sum += ex2(x - lse[r]);
+        }
+    a.w_out[at] = (a.w_in ? a.decay * a.w_in[at] : 0.f) + sum;
+}
+
+}  // namespace
+
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
+                               uint32_t head_dim, cudaStream_t s)
+{
+    const bool hi = (p.prefix ? a.max_group_q : a.max_q) * a.group > 8;
+    if (dtype == GMS_DTYPE_BF16) {
+        if (head_dim == 64)
+            return hi ? launch<__nv_bfloat16, 64, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 64, false>(a, p, kmap, vmap, s);
+        return hi ? launch<__nv_bfloat16, 128, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 128, false>(a, p, kmap, vmap, s);
+    }
+    if (head_dim == 64) return hi ? launch<__half, 64, true>(a, p, kmap, vmap, s) : launch<__half, 64, false>(a, p, kmap, vmap, s);
+    return hi ? launch<__half, 128, true>(a, p, kmap, vmap, s) : launch<__half, 128, false>(a, p, kmap, vmap, s);
+}
+
+cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s)
+{
+    const uint32_t chunks = (a.max_kv + 255) / 256;
+    if (chunks == 0) return cudaSuccess;
+    return launch_dependent(kv_few_weights_kernel, a.n_seq * a.n_kv * chunks, 256, 0, s, a, p, chunks);
+}
+
+}  // namespace gms

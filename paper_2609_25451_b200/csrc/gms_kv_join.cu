@@ -1,0 +1,172 @@
+// Joining the pieces of attention items that were cut across CTAs, and the two passes of a shared-prefix call.
+//
+// Pieces carry a running maximum m (base 2), a sum l and unnormalised values o:  M = max m_i,  L = sum l_i 2^(m_i - M),
+// out = sum o_i 2^(m_i - M) / L,  in the order of the pieces, so equal calls give equal bits.  One warp a row; the pieces
+// are a few MB at most and still in L2.
+#include <cmath>
+#include <type_traits>
+
+#include "gms_internal.h"
+#include "gms_kv_attn.h"
+#include "gms_ptx.h"
+
+namespace gms {
+namespace {
+
+using namespace ptx;
+
+constexpr uint32_t kWarps = 4;
+
+template <int D>
+struct Row {
+    float m = -INFINITY, l = 0.f, o[D / 32] = {};
+};
+
+// Adds n pieces; piece i lies at slot(i) of ml and o.
+template <int D, class F>
+__device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const float *o, uint32_t n, F slot)
+{
+    using V = typename std::conditional<D == 128, float4, float2>::type;
+    const uint32_t lane = threadIdx.x & 31u;
+    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+        float2 mine = make_float2(neg_inf(), 0.f);
+        if (i0 + lane < n) mine = ml[slot(i0 + lane)];
+        float top = fmaxf(x.m, mine.x);
+#pragma unroll
+        for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        const float f = x.m == top ? 1.f : ex2(x.m - top), g = mine.x == top ? 1.f : ex2(mine.x - top);
+        x.m = top;
+        x.l = x.l * f + warp_sum(mine.y * g);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) x.o[e] *= f;
+        const uint32_t k = min(32u, n - i0);
+#pragma unroll 8
+        for (uint32_t i = 0; i < k; ++i) {
+            const float gi = __shfl_sync(0xffffffffu, g, i), li = __shfl_sync(0xffffffffu, mine.y, i);
+            if (li == 0.f) continue;  // nothing seen there
+            const V v = reinterpret_cast<const V *>(o + slot(i0 + i) * D)[lane];
+            const float *vf = reinterpret_cast<const float *>(&v);
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) x.o[e] += vf[e] * gi;
+        }
+    }
+}
+
+// Writes a finished row; non-finite rows go through attend_row when `redo` asks for it.
+template <class T, int D>
+__device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int tok, uint32_t h, bool redo)
+{
+    const uint32_t lane = threadIdx.x & 31u;
+    T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride) + lane * (D / 32);
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    bool bad = false;
+    T v[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+        const float y = x.l == 0.f ? 0.f : x.o[e] * inv;
+        bad |= !(fabsf(y) < kHuge);
+        v[e] = from_f32<T>(y);
+    }
+    if (D == 128) *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(v);
+    else *reinterpret_cast<uint32_t *>(op) = *reinterpret_cast<const uint32_t *>(v);
+    if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = x.l == 0.f ? neg_inf() : (x.m + log2f(x.l)) * kLn2;
+    if (redo && __any_sync(0xffffffffu, bad)) {
+        __syncwarp();
+        attend_row<T, D>(a, tok, h);
+    }
+}
+
+// Block (i, part): the item into which the border between CTA i and CTA i + 1 falls, if that is its first border.
+template <class T, int D, int ROWS, int TILE>
+__global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
+                                                                   uint32_t parts)
+{
+    grid_launch_dependents();
+    grid_wait();
+    const uint32_t i = blockIdx.x / parts + 1, part = blockIdx.x % parts, warp = threadIdx.x / 32;
+    const uint64_t total = p.begin[p.n_units], at = total * i / p.n_cta;
+    if (at >= total) return;
+    uint32_t lo = 0, hi = p.n_units;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (p.begin[mid] <= at) lo = mid; else hi = mid;
+    }
+    const Unit u = get_unit<ROWS, TILE>(a, p, lo / p.n_rt, lo % p.n_rt);
+    if (u.tiles == 0) return;
+    const uint32_t c = (uint32_t)((at - p.begin[lo]) / (uint32_t)u.tiles);
+    const uint64_t first = p.begin[lo] + (uint64_t)c * (uint32_t)u.tiles;
+    if (at == first) return;  // the border lies between two items
+    const uint32_t c0 = tile_owner(first, total, p.n_cta), c1 = tile_owner(first + u.tiles - 1, total, p.n_cta);
+    if (c0 + 1 != i) return;
+    for (int r = part * kWarps + warp; r < u.rows; r += parts * kWarps) {
+        Row<D> x;
+        add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
+        finish<T, D>(a, x, unit_tok(a, u, r), unit_head(a, u, c, r), p.redo);
+    }
+}
+
+// Adds what a pass has for one (query row, head); s: sequence, or group in the prefix pass.
+template <int D, int ROWS, int TILE>
+__device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s, int tok, uint32_t h)
+{
+    const uint64_t row = (uint64_t)tok * a.n_heads + h;
+    const uint32_t c = h / a.group;
+    Unit u = get_unit<ROWS, TILE>(a, p, s, 0);
+    const uint32_t in = (uint32_t)(tok - u.q0) * a.group + h % a.group, rt = in / ROWS, r = in % ROWS;
+    if (rt >= p.n_rt) return;
+    if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
+    if (u.tiles == 0 || (int)r >= u.rows) return;
+    const uint64_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + (uint64_t)c * (uint32_t)u.tiles;
+    const uint32_t c0 = tile_owner(first, total, p.n_cta), c1 = tile_owner(first + u.tiles - 1, total, p.n_cta);
+    if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 1, [&](uint32_t) { return row; });
+    else
+        add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass pre,
+                                                                          const __grid_constant__ Pass own)
+{
+    const uint64_t row = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32;
+    grid_wait();
+    if (row >= (uint64_t)a.total_q * a.n_heads) return;
+    const int tok = (int)(row / a.n_heads);
+    const uint32_t h = (uint32_t)(row % a.n_heads), s = owner_of_row(a, tok);
+    if (s >= a.n_seq) return;
+    Row<D> x;
+    const uint32_t g = group_of_seq(a, s);
+    if (g < a.n_groups) add_pass<D, kFewRows, kFewTile>(a, pre, x, g, tok, h);
+    add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);
+    finish<T, D>(a, x, tok, h, own.redo);
+}
+
+}  // namespace
+
+#define GMS_BY_TYPE(CALL)                                                               \
+    do {                                                                                \
+        if (dtype == GMS_DTYPE_BF16) {                                                  \
+            using T = __nv_bfloat16;                                                    \
+            if (head_dim == 64) { constexpr int D = 64; return CALL; }                  \
+            constexpr int D = 128;                                                      \
+            return CALL;                                                                \
+        }                                                                               \
+        using T = __half;                                                               \
+        if (head_dim == 64) { constexpr int D = 64; return CALL; }                      \
+        constexpr int D = 128;                                                          \
+        return CALL;                                                                    \
+    } while (0)
+
+cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+{
+    if (p.n_cta < 2) return cudaSuccess;
+    const uint32_t parts = p.rows / kFewRows;
+    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, (p.n_cta - 1) * parts, kWarps * 32, 0, s, a, p, parts)));
+}
+
+cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &pre, const Pass &own, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+{
+    const uint32_t grid = (uint32_t)(((uint64_t)a.total_q * a.n_heads + kWarps - 1) / kWarps);
+    GMS_BY_TYPE((launch_dependent(kv_attn_join_shared_kernel<T, D>, grid, kWarps * 32, 0, s, a, pre, own)));
+}
+
+}  // namespace gms

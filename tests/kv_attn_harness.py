@@ -6,7 +6,7 @@ works in float64; it shares nothing with the library.  `bounds` derives how far 
   logits: products of 16-bit numbers are exact in 32 bits, their sum of D terms and the scaling are off by at most
           dx = (D + 8) 2^-24 scale sum|q k| + 2^-22 (|x| + |m|)  (exponent argument formed in 32 bits)
   softmax weights p: relative 2 dx (its own logit and the normaliser's) + 2^-21 (exponential, quotient)
-          + n 2^-24 (the sum of n terms), then one rounding to the pool's type, u = 2^-9 (bf16) or 2^-12 (f16; below
+          + n 2^-24 (the sum of n terms), then one rounding to the pool's type, u = eps / 2 of the type: 2^-8 (bf16) or 2^-11 (f16; below
           2^-14 of the running maximum absolute 2^-25)
   out:    sum p |v| times (that + u + n 2^-24) for the products' sum, plus u |out| for the last rounding
 """
@@ -19,7 +19,7 @@ import torch
 
 from paper_2609_25451_b200 import gms
 
-U = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12}
+U = {t: torch.finfo(t).eps / 2 for t in (torch.bfloat16, torch.float16)}  # unit roundoff, round to nearest
 
 
 class Problem:
