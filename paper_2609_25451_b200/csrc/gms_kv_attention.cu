@@ -239,14 +239,15 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     *p = {};
     const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
     p->prefix = prefix;
-    p->rows = kFewRows;
-    p->tile = kFewTile;
+    const bool tc = rows > kFewRows;
+    p->rows = tc ? kTcRows : kFewRows;
+    p->tile = tc ? kTcTile : kFewTile;
     p->n_rt = (uint32_t)ceil_div(rows, p->rows);
     if (p->n_rt == 0) p->n_rt = 1;
     p->n_units = (prefix ? a.n_groups : a.n_seq) * p->n_rt;
-    // two CTAs an SM; fewer where they would have fewer than eight tiles (two a warp)
-    const uint64_t want = ceil_div(most_tiles(a, *p), 8);
-    p->n_cta = (uint32_t)(want < 1 ? 1 : want < kFewMaxCtas ? want : kFewMaxCtas);
+    // as many CTAs as the SMs hold; fewer where they would have fewer than eight tiles of 16 tokens (two a warp), or two of 128
+    const uint64_t want = ceil_div(most_tiles(a, *p), tc ? 2 : 8), most = tc ? kTcMaxCtas : kFewMaxCtas;
+    p->n_cta = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
     p->begin = c->take<uint64_t>(p->n_units + 1);
     p->part_ml = c->take<float2>(2ull * p->n_cta * p->rows);
     p->part_o = c->take<float>(2ull * p->n_cta * p->rows * head_dim);
@@ -267,7 +268,7 @@ void plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspac
     pl->lse = a.lse;
     if (a.w_out) {
         if (!a.lse) pl->lse = c.take<float>((uint64_t)a.total_q * a.n_heads);
-        if (pl->own.n_rt == 1) {
+        if (pl->own.rows == kFewRows) {
             pl->logits = true;
             pl->own.logit_stride = (a.max_kv + kFewTile - 1) / kFewTile * kFewTile;
             pl->own.logits = c.take<float>((uint64_t)a.n_seq * a.n_heads * a.max_q * pl->own.logit_stride);
@@ -292,14 +293,24 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
     const uint32_t dtype = layout->dtype, dim = layout->head_dim;
     cudaError_t e = cudaSuccess;
     if (a.total_q) {
-        CUtensorMap kmap, vmap;
-        rc = encode_map(&kmap, pool, layout, layout->k_plane, kFewTile);
-        if (rc == GMS_OK) rc = encode_map(&vmap, pool, layout, layout->v_plane, kFewTile);
-        if (rc != GMS_OK) return rc;
         AttnArgs b = a;
         b.lse = pl.lse;
-        if (pl.shared && pl.prefix.n_units) e = launch_kv_attn_few(b, pl.prefix, kmap, vmap, dtype, dim, s);
-        if (e == cudaSuccess) e = launch_kv_attn_few(b, pl.own, kmap, vmap, dtype, dim, s);
+        CUtensorMap kmap[2], vmap[2];  // boxes of the few-row and of the many-row kernel
+        const uint32_t box = layout->block_tokens < kTcTile ? layout->block_tokens : kTcTile;
+        const bool prefix = pl.shared && pl.prefix.n_units;
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t rows = i ? kTcRows : kFewRows;
+            if (pl.own.rows != rows && !(prefix && pl.prefix.rows == rows)) continue;
+            rc = encode_map(&kmap[i], pool, layout, layout->k_plane, i ? box : kFewTile);
+            if (rc == GMS_OK) rc = encode_map(&vmap[i], pool, layout, layout->v_plane, i ? box : kFewTile);
+            if (rc != GMS_OK) return rc;
+        }
+        auto launch = [&](const Pass &p) {
+            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], box, dtype, dim, s)
+                                     : launch_kv_attn_few(b, p, kmap[0], vmap[0], dtype, dim, s);
+        };
+        if (prefix) e = launch(pl.prefix);
+        if (e == cudaSuccess) e = launch(pl.own);
         if (e == cudaSuccess)
             e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s) : launch_kv_attn_join(b, pl.own, dtype, dim, s);
         if (e == cudaSuccess && w && pl.logits) e = launch_kv_few_weights(b, pl.own, s);

@@ -42,7 +42,7 @@ struct AttnArgs {
 // How a pass over cached tokens is cut.  A unit is a run of up to ROWS query rows (token-major, the heads of one KV head
 // inside a token) of one sequence (or, in a prefix pass, of one group); an item is a unit for one KV head; an item's work
 // is the list of token tiles that at least one of its rows sees.  All items' tiles, one after the other, are dealt out
-// evenly: CTA i of n takes tiles [T*i/n, T*(i+1)/n), whatever items they fall into, so ragged lengths cost no balance.
+// evenly: CTA i of n (n = n_cta, or T if that is less) takes tiles [T*i/n, T*(i+1)/n), whatever items they fall into, so ragged lengths cost no balance.
 // An item that one CTA has whole is finished there; the at most two pieces a CTA has of others go to its two slots of
 // part_o / part_ml and are joined by kv_attn_join.
 struct Pass {
@@ -81,6 +81,10 @@ cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, co
 constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewMaxCtas = 2 * 148;
 cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
                                uint32_t head_dim, cudaStream_t s);
+// Many query rows a unit; box_tokens: tokens a TMA box of the maps holds.
+constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxCtas = 148;
+cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens,
+                              uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);
@@ -221,6 +225,8 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
     }
     return u;
 }
+// CTAs that get work: no share is empty, so a piece lies in every slot that the join looks at.
+__device__ __forceinline__ uint32_t used_ctas(uint64_t total, const Pass &p) { return (uint32_t)min(total, (uint64_t)p.n_cta); }
 // The part of the work that a CTA has, item by item.
 struct Walk {
     uint64_t pos, end;   // tiles still to do, in the order over all items
@@ -253,8 +259,9 @@ __device__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint64
         total += sh[i];
     }
     Walk w;
-    w.pos = total * cta / p.n_cta;
-    w.end = total * (cta + 1) / p.n_cta;
+    const uint32_t n = used_ctas(total, p);
+    w.pos = cta < n ? total * cta / n : total;
+    w.end = cta < n ? total * (cta + 1) / n : total;
     if (mine && before <= w.pos && w.pos < before + mine) {
         uint64_t b = before;
         for (uint32_t u = u0; u < u1; ++u) {
@@ -282,7 +289,7 @@ __device__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint64
     w.rt = u % p.n_rt;
     return w;
 }
-// Which CTA's share holds tile t of T.
+// Which CTA's share holds tile t of T, with n_cta of them used.
 __device__ __forceinline__ uint32_t tile_owner(uint64_t t, uint64_t total, uint32_t n_cta)
 {
     return (uint32_t)(((t + 1) * n_cta - 1) / total);

@@ -84,8 +84,10 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     grid_launch_dependents();
     grid_wait();
     const uint32_t i = blockIdx.x / parts + 1, part = blockIdx.x % parts, warp = threadIdx.x / 32;
-    const uint64_t total = p.begin[p.n_units], at = total * i / p.n_cta;
-    if (at >= total) return;
+    const uint64_t total = p.begin[p.n_units];
+    const uint32_t n = used_ctas(total, p);
+    if (i >= n) return;
+    const uint64_t at = total * i / n;
     uint32_t lo = 0, hi = p.n_units;
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     const uint32_t c = (uint32_t)((at - p.begin[lo]) / (uint32_t)u.tiles);
     const uint64_t first = p.begin[lo] + (uint64_t)c * (uint32_t)u.tiles;
     if (at == first) return;  // the border lies between two items
-    const uint32_t c0 = tile_owner(first, total, p.n_cta), c1 = tile_owner(first + u.tiles - 1, total, p.n_cta);
+    const uint32_t c0 = tile_owner(first, total, n), c1 = tile_owner(first + u.tiles - 1, total, n);
     if (c0 + 1 != i) return;
     for (int r = part * kWarps + warp; r < u.rows; r += parts * kWarps) {
         Row<D> x;
@@ -117,7 +119,7 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
     if (u.tiles == 0 || (int)r >= u.rows) return;
     const uint64_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + (uint64_t)c * (uint32_t)u.tiles;
-    const uint32_t c0 = tile_owner(first, total, p.n_cta), c1 = tile_owner(first + u.tiles - 1, total, p.n_cta);
+    const uint32_t n = used_ctas(total, p), c0 = tile_owner(first, total, n), c1 = tile_owner(first + u.tiles - 1, total, n);
     if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 1, [&](uint32_t) { return row; });
     else
         add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
@@ -135,8 +137,12 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
     if (s >= a.n_seq) return;
     Row<D> x;
     const uint32_t g = group_of_seq(a, s);
-    if (g < a.n_groups) add_pass<D, kFewRows, kFewTile>(a, pre, x, g, tok, h);
-    add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);
+    if (g < a.n_groups) {
+        if (pre.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, pre, x, g, tok, h);
+        else add_pass<D, kFewRows, kFewTile>(a, pre, x, g, tok, h);
+    }
+    if (own.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, own, x, s, tok, h);
+    else add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);
     finish<T, D>(a, x, tok, h, own.redo);
 }
 
@@ -160,6 +166,8 @@ cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype
 {
     if (p.n_cta < 2) return cudaSuccess;
     const uint32_t parts = p.rows / kFewRows;
+    if (p.rows == kTcRows)
+        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, (p.n_cta - 1) * parts, kWarps * 32, 0, s, a, p, parts)));
     GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, (p.n_cta - 1) * parts, kWarps * 32, 0, s, a, p, parts)));
 }
 

@@ -1,0 +1,485 @@
+// Attention of many query rows (prompts, chunks, batches behind one prefix) over the paged pool, on tcgen05.
+//
+// A unit is 256 query rows (tokens x the heads that share a KV head), two slots of 128: while the tensor core works for one
+// slot, the other's softmax runs.  Per tile of 128 tokens and slot
+//   S = Q K^T      (128 x 128 x D, both operands in shared memory, S in tensor memory)
+//   P = 2^(S c - m), rounded to the pool's type, written over S in tensor memory; l += sum P in 32 bits
+//   O += P V       (128 x D x 128, P from tensor memory, V as it lies in the pool: token rows, "MN-major" operand)
+// O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
+// are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
+// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles).  Warp 8 issues the products, warp 9 the TMA
+// loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane a box.
+// Tensor memory: S0 S1 (128 columns each) O0 O1 (D each) = 512 columns at D = 128, hence P over S: the product with the next
+// K tile waits until P V of the slot is complete.
+// Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
+#include "gms_internal.h"
+#include "gms_kv_attn.h"
+#include "gms_tcgen05.h"
+
+namespace gms {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 320, kRows = (int)kTcRows, kTile = (int)kTcTile;
+constexpr float kLag = 8.f;  // log2 of how far a maximum may have grown before O is rescaled
+
+template <int D>
+struct Tc {
+    static constexpr int kHalves = D / 64;
+    static constexpr uint32_t kHalfBytes = 128 * 128;             // 128 rows x 64 elements
+    static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;  // a K, V or Q tile
+    static constexpr int kStages = D == 128 ? 4 : 8;
+    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 2 + 2 + 1) * 8;
+    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kBars + 8 * (kThreads / 32 + 3) + 64 + 1024;
+    static constexpr uint32_t kO = 256;                            // first column of O0
+    static constexpr uint32_t kCols = 512;
+};
+
+struct Segment {  // a run of tiles of one item
+    Unit un;
+    uint32_t c;
+    int k0, k1;
+    __device__ bool starts() const { return k0 == 0; }
+    __device__ bool ends() const { return k1 == un.tiles; }
+};
+__device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, Walk &w, Segment &g)
+{
+    if (w.pos >= w.end) return false;
+    for (;;) {
+        g.un = get_unit<kRows, kTile>(a, p, w.s, w.rt);
+        const uint64_t t = (uint64_t)g.un.tiles * a.n_kv;
+        if (w.pos < w.base + t) break;
+        w.base += t;
+        if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+    }
+    const uint64_t in = w.pos - w.base;
+    g.c = (uint32_t)(in / (uint32_t)g.un.tiles);
+    g.k0 = (int)(in % (uint32_t)g.un.tiles);
+    g.k1 = (int)min((uint64_t)g.un.tiles, (uint64_t)g.k0 + (w.end - w.pos));
+    w.pos += (uint32_t)(g.k1 - g.k0);
+    return true;
+}
+
+template <class T> struct IsBf16 { static constexpr bool value = false; };
+template <> struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// Changes the sign of (or clears) two packed 16-bit values.
+__device__ __forceinline__ uint4 with_sign(uint4 v, uint32_t flip, uint32_t keep)
+{
+    return make_uint4((v.x ^ flip) & keep, (v.y ^ flip) & keep, (v.z ^ flip) & keep, (v.w ^ flip) & keep);
+}
+
+// A wait that every role uses: bounded, and cut short when another role has given up.
+__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t *abort, unsigned long long *status)
+{
+    if (mbar_try(bar, parity)) return true;
+    const uint64_t end = now_ns() + kWaitLimitNs;
+    for (uint32_t n = 1; n < (1u << 28); ++n) {
+        if (mbar_try(bar, parity)) return true;
+        if ((n & 31u) == 0) {
+            if (*abort) return false;
+            if (now_ns() > end) break;
+        }
+    }
+    *abort = 1;
+    if (status) atomicOr(status, (unsigned long long)GMS_DEV_TIMEOUT);
+    return false;
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_constant__ CUtensorMap kmap,
+                                                                 const __grid_constant__ CUtensorMap vmap,
+                                                                 const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
+                                                                 uint32_t box_tokens)
+{
+    using F = Tc<D>;
+    constexpr int NS = F::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *sm = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t q_smem = base, ring = base + 2 * F::kTileBytes;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, s_full = q_full + 16, p_full = s_full + 16,
+                   o_done = p_full + 16, drain = o_done + 16;
+    uint64_t *plan = bars + 2 * NS + 9;
+    volatile uint32_t *shared_words = reinterpret_cast<volatile uint32_t *>(plan + kThreads / 32 + 3);  // [0] tensor memory, [1] abort
+    volatile uint32_t *abort = shared_words + 1;
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(q_full + 8 * i, 128);
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 128);
+            mbar_init(o_done + 8 * i, 1);
+        }
+        mbar_init(drain, 1);
+        *abort = 0;
+        fence_mbar_init();
+        tma_prefetch_map(&kmap);
+        tma_prefetch_map(&vmap);
+    }
+    if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(shared_words)), F::kCols);
+    grid_launch_dependents();
+    tc_fence_before();
+    Walk w = plan_walk<kRows, kTile, kThreads>(a, p, blockIdx.x, plan);  // ends with __syncthreads
+    tc_fence_after();
+    const uint32_t tmem = shared_words[0];
+
+    // units that see nothing: zero rows (the join knows nothing of them)
+    for (uint32_t u = blockIdx.x; u < p.n_units; u += gridDim.x) {
+        const Unit un = get_unit<kRows, kTile>(a, p, u / p.n_rt, u % p.n_rt);
+        if (un.rows == 0 || un.tiles != 0) continue;
+        for (uint32_t i = tid; i < un.rows * a.n_kv; i += kThreads) {
+            const int r = i % un.rows;
+            const uint32_t h = unit_head(a, un, i / un.rows, r);
+            const uint64_t tok = unit_tok(a, un, r);
+            if (p.row_o) {
+                p.row_ml[tok * a.n_heads + h] = make_float2(neg_inf(), 0.f);
+            } else {
+                uint4 *op = reinterpret_cast<uint4 *>(a.out + tok * a.out_token_stride + h * a.out_head_stride);
+                for (int d = 0; d < D / 8; ++d) op[d] = make_uint4(0, 0, 0, 0);
+                if (a.lse) a.lse[tok * a.n_heads + h] = neg_inf();
+            }
+        }
+    }
+
+    Segment g;
+    if (warp == 9) {
+        // ------------------------------------------------------------------ loads
+        const int per = kTile / (int)box_tokens, boxes = per * F::kHalves;  // boxes a tile: at most 16
+        const int half = (int)lane % F::kHalves, part = (int)lane / F::kHalves;
+        const uint32_t tok_mask = (1u << a.block_shift) - 1u;
+        uint32_t n = 0;  // stages filled
+        bool ok = true;
+        while (ok && next_segment(a, p, w, g)) {
+            auto block_of = [&](int k) -> int {  // a hole, or nothing left to read: out of range, zeros arrive
+                const int t = unit_tile(g.un, k) * kTile + part * (int)box_tokens;
+                int id = -1;
+                if ((int)lane < boxes && t < g.un.n) id = g.un.table[(uint32_t)t >> a.block_shift];
+                return (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;
+            };
+            int next = block_of(g.k0);
+            for (int k = g.k0; ok && k < g.k1; ++k) {
+                const int blk = next, t = unit_tile(g.un, k) * kTile + part * (int)box_tokens;
+                if (k + 1 < g.k1) next = block_of(k + 1);
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const uint32_t st = n % NS;
+                    ok = __all_sync(0xffffffffu, wait_or_abort(empty + 8 * st, ((n / NS) & 1u) ^ 1u, abort, a.status));
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect(full + 8 * st, F::kTileBytes);
+                    __syncwarp();
+                    if ((int)lane < boxes)
+                        tma_load_4d(ring + st * F::kTileBytes + half * F::kHalfBytes + part * box_tokens * 128, v ? &vmap : &kmap, half * 64,
+                                    (int)((uint32_t)t & tok_mask), (int)g.c, blk, full + 8 * st);
+                    ++n;
+                }
+            }
+        }
+        if (!ok)  // give up: wait (bounded) for what is still on its way into this CTA's shared memory
+            for (uint32_t i = n > (uint32_t)NS ? n - NS : 0; i < n; ++i) (void)mbar_wait(full + 8 * (i % NS), (i / NS) & 1u);
+    } else if (warp == 8) {
+        // ------------------------------------------------------------------ products
+        constexpr uint32_t id_s = f16_idesc(128, 128, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
+        uint32_t n = 0, seg = 0, done0 = 0, done1 = 0;  // tiles of K and V taken; segments; P V products of each slot
+        uint32_t seg1 = 0;
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            ok = ok && wait_or_abort(bar, parity, abort, a.status);
+            return ok;
+        };
+        auto scores = [&](int slot, uint32_t stage) {
+            const uint32_t kt = ring + stage * F::kTileBytes, qt = q_smem + slot * F::kTileBytes;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t off = (kk / 4) * F::kHalfBytes + (kk % 4) * 32;
+                mma_ss(tmem + slot * 128, smem_desc(qt + off, 16, 1024), smem_desc(kt + off, 16, 1024), id_s, kk > 0);
+            }
+            tc_commit(s_full + 8 * slot);
+        };
+        auto values = [&](int slot, uint32_t stage, bool add) {
+            const uint32_t vt = ring + stage * F::kTileBytes;
+#pragma unroll
+            for (int kk = 0; kk < kTile / 16; ++kk)
+                mma_ts(tmem + F::kO + slot * D, tmem + slot * 128 + kk * 8, smem_desc(vt + kk * 2048, F::kHalfBytes, 1024), id_o,
+                       add || kk > 0);
+            tc_commit(o_done + 8 * slot);
+        };
+        if (lane == 0) {
+            while (ok && next_segment(a, p, w, g)) {
+                const bool two = g.un.rows > 128;
+                const int nt = g.k1 - g.k0;
+                if (!wait(full + 8 * (n % NS), (n / NS) & 1u)) break;  // K of the first tile
+                if (!wait(q_full, seg & 1u)) break;
+                tc_fence_after();
+                scores(0, n % NS);
+                if (two) {
+                    if (!wait(q_full + 8, seg1 & 1u)) break;
+                    tc_fence_after();
+                    scores(1, n % NS);
+                    ++seg1;
+                }
+                tc_commit(empty + 8 * (n % NS));
+                ++seg;
+                for (int j = 0; j < nt; ++j) {
+                    const uint32_t vs = n + 1, ks = n + 2;  // V of this tile, K of the next
+                    const bool more = j + 1 < nt;
+                    if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
+                    if (!wait(p_full, done0 & 1u)) break;
+                    tc_fence_after();
+                    values(0, vs % NS, j > 0);
+                    if (more) {
+                        if (!wait(full + 8 * (ks % NS), (ks / NS) & 1u)) break;
+                        if (!wait(o_done, done0 & 1u)) break;  // P lies over S
+                        tc_fence_after();
+                        scores(0, ks % NS);
+                    }
+                    ++done0;
+                    if (two) {
+                        if (!wait(p_full + 8, done1 & 1u)) break;
+                        tc_fence_after();
+                        values(1, vs % NS, j > 0);
+                        if (more) {
+                            if (!wait(o_done + 8, done1 & 1u)) break;
+                            tc_fence_after();
+                            scores(1, ks % NS);
+                        }
+                        ++done1;
+                    }
+                    tc_commit(empty + 8 * (vs % NS));
+                    if (more) tc_commit(empty + 8 * (ks % NS));
+                    n += 2;
+                }
+            }
+            tc_commit(drain);  // nothing of this thread's is in flight when the CTA ends
+            (void)mbar_wait(drain, 0);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------------ softmax, one thread a row
+        const int slot = (int)warp / 4, row_in = (int)(warp % 4) * 32 + (int)lane, row = slot * 128 + row_in;
+        const uint32_t lanes = ((warp % 4) * 32) << 16;
+        const uint32_t s_col = tmem + lanes + slot * 128, o_col = tmem + lanes + F::kO + slot * D;
+        const float scale2 = a.scale * kLog2e, c2 = a.scale == 0.f ? 1.f : fabsf(scale2);
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : 0xffffffffu;
+        uint32_t n = 0, tiles = 0;  // tiles of all segments so far; of this slot
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            ok = __all_sync(0xffffffffu, ok && wait_or_abort(bar, parity, abort, a.status));
+            return ok;
+        };
+        while (ok && next_segment(a, p, w, g)) {
+            const int nt = g.k1 - g.k0;
+            if (slot == 1 && g.un.rows <= 128) {
+                n += (uint32_t)nt;
+                continue;
+            }
+            // Q: 16-byte pieces, a row's in neighbouring lanes; rows that do not exist are zero
+            const uint32_t qt = q_smem + slot * F::kTileBytes;
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+                const int idx = i * 128 + row_in, r = idx / (D / 8), ch = idx % (D / 8);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (slot * 128 + r < g.un.rows)
+                    v = with_sign(*reinterpret_cast<const uint4 *>(a.q + (uint64_t)unit_tok(a, g.un, slot * 128 + r) * a.q_token_stride +
+                                                                   (uint64_t)unit_head(a, g.un, g.c, slot * 128 + r) * a.q_head_stride + ch * 16),
+                                  flip, keep);
+                *reinterpret_cast<uint4 *>(sm + slot * F::kTileBytes + (ch / 8) * F::kHalfBytes + r * 128 + (((ch % 8) ^ (r & 7)) << 4)) = v;
+            }
+            (void)qt;
+            fence_proxy_async();
+            mbar_arrive(q_full + 8 * slot);
+
+            const bool live = row < g.un.rows;
+            const int pos = unit_row_pos(a, g.un, live ? row : g.un.rows - 1);
+            const int pos_lo = unit_row_pos(a, g.un, slot * 128), pos_hi = unit_row_pos(a, g.un, min(slot * 128 + 127, g.un.rows - 1));
+            float m = neg_inf(), l = 0.f;
+            int id_next = -1;
+            auto tile_id = [&](int k) -> int {  // the block of each 16 tokens of the tile, one lane each
+                const int t = unit_tile(g.un, k) * kTile + (int)lane * 16;
+                return lane < 8 && t < g.un.n ? g.un.table[(uint32_t)t >> a.block_shift] : -1;
+            };
+            id_next = tile_id(g.k0);
+            for (int k = g.k0; k < g.k1; ++k) {
+                const int t0 = unit_tile(g.un, k) * kTile;
+                const uint32_t valid = __ballot_sync(0xffffffffu, (uint32_t)id_next < a.n_blocks) & 0xffu;
+                if (k + 1 < g.k1) id_next = tile_id(k + 1);
+                if (!wait(s_full + 8 * slot, tiles & 1u)) break;
+                tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld32(s_col + i * 32, s[i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_wait32(s[i]);
+                const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo &&
+                                   (g.un.whole || a.window == 0 || (long long)t0 > (long long)pos_hi - (long long)a.window ||
+                                    (uint32_t)(t0 + kTile - 1) < a.sinks);
+                if (!whole) {
+                    const int hi = pos - t0;  // columns up to hi; from lo on or below sink
+                    const int lo = (int)(g.un.whole || a.window == 0 ? 0ll : max(0ll, min((long long)kTile, (long long)pos - (long long)a.window + 1 - t0)));
+                    const int sink = (int)max(0ll, min((long long)kTile, (long long)a.sinks - t0));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const int col = i * 32 + j;
+                            const bool on = col <= hi && (col >= lo || col < sink) && (valid >> (col / 16) & 1u);
+                            if (!on) s[i][j] = 0xff800000u;
+                        }
+                }
+                float top = neg_inf();
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(s[i][j]));
+                top *= c2;
+                const bool grow = top > m + kLag || (m == neg_inf() && top != m);
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
+                    if (grow) m = top;
+                    l *= f;
+                    if (k != g.k0) {  // S of this tile is issued after P V of the last: O is at rest
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t o[32];
+                            tmem_ld32(o_col + i * 32, o);
+                            tmem_wait32(o);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                            tmem_st32(o_col + i * 32, o);
+                        }
+                    }
+                }
+                const float z = m == neg_inf() ? 0.f : m;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float x0 = ex2(fmaf(__uint_as_float(s[i * 2 + j / 16][(j * 2) % 32]), c2, -z));
+                        const float x1 = ex2(fmaf(__uint_as_float(s[i * 2 + j / 16][(j * 2 + 1) % 32]), c2, -z));
+                        part[j & 3] += x0 + x1;
+                        pk[j] = pack2(x0, x1, T());
+                    }
+                    tmem_st32(s_col + i * 32, pk);
+                }
+                l += (part[0] + part[1]) + (part[2] + part[3]);
+                // values of tokens that no row of the unit sees must not meet the product, whatever bits they are (slot 0's
+                // thread r clears token r; slot 1's product comes after slot 0's)
+                if (slot == 0 && !whole) {
+                    const int t = t0 + row_in;
+                    const bool none = t > g.un.pos_max || (!g.un.whole && !sees(a, max(g.un.pos_min, t), t));
+                    const uint32_t vs = 2 * n + 1;
+                    if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
+                    if (none)
+#pragma unroll
+                        for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + e * 16);
+                    fence_proxy_async();
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(p_full + 8 * slot);
+                ++n;
+                ++tiles;
+            }
+            if (!ok) break;
+            // the item's rows (or this CTA's piece of them)
+            if (!wait(o_done + 8 * slot, (tiles - 1) & 1u)) break;
+            tc_fence_after();
+            const uint64_t tok = unit_tok(a, g.un, live ? row : 0);
+            const uint32_t h = unit_head(a, g.un, g.c, live ? row : 0);
+            const bool finished = g.starts() && g.ends() && !p.row_o;
+            uint8_t *dst;
+            if (finished) {
+                dst = a.out + tok * a.out_token_stride + h * a.out_head_stride;
+                if (live && a.lse) a.lse[tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
+            } else {
+                const bool mine = g.starts() && g.ends();
+                const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (g.starts() ? 1 : 0)) * kRows + row;
+                dst = reinterpret_cast<uint8_t *>((mine ? p.row_o : p.part_o) + at * D);
+                if (live) (mine ? p.row_ml : p.part_ml)[at] = make_float2(m, l);
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                uint32_t o[32];
+                tmem_ld32(o_col + i * 32, o);
+                tmem_wait32(o);
+                if (!live) continue;
+                if (finished) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float lo = l == 0.f ? 0.f : __uint_as_float(o[j + 2 * e]) * inv, hi = l == 0.f ? 0.f : __uint_as_float(o[j + 2 * e + 1]) * inv;
+                            bad |= !(fabsf(lo) < kHuge && fabsf(hi) < kHuge);
+                            v[e] = pack2(lo, hi, T());
+                        }
+                        *reinterpret_cast<uint4 *>(dst + i * 64 + j * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4 *>(dst + i * 128 + j * 4) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                }
+            }
+            tc_fence_before();
+            if (p.redo && finished) {
+                uint32_t again = __ballot_sync(0xffffffffu, live && bad);
+                __syncwarp();
+                while (again) {
+                    const int r = __ffs(again) - 1;
+                    again &= again - 1;
+                    const int rr = slot * 128 + (int)(warp % 4) * 32 + r;
+                    attend_row<T, D>(a, unit_tok(a, g.un, rr), unit_head(a, g.un, g.c, rr));
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        tmem_free(tmem, F::kCols);
+    }
+}
+
+template <class T, int D>
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens, cudaStream_t s)
+{
+    constexpr uint32_t smem = Tc<D>::kSmem;
+    static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (ready != cudaSuccess) return ready;
+    kv_attn_tc_kernel<T, D><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, a, p, box_tokens);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens,
+                              uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+{
+    if (dtype == GMS_DTYPE_BF16)
+        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, box_tokens, s)
+                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, box_tokens, s);
+    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, box_tokens, s) : launch<__half, 128>(a, p, kmap, vmap, box_tokens, s);
+}
+
+}  // namespace gms
