@@ -176,12 +176,11 @@ int make_args(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv
     return GMS_OK;
 }
 
-// One layer's keys or values as a 4-d tensor (d, token of block, head, block); boxes of 64 elements x `box_tokens` tokens.
-int encode_map(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, uint32_t plane, uint32_t box_tokens)
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                            const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                            CUtensorMapFloatOOBfill);
+Encode encoder()
 {
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static const Encode encode = [] {
         void *p = nullptr;
         cudaDriverEntryPointQueryResult q;
@@ -191,17 +190,41 @@ int encode_map(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, 
         }
         return reinterpret_cast<Encode>(p);
     }();
+    return encode;
+}
+int encode_map(CUtensorMap *m, uint32_t dtype, uint32_t rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides,
+               const cuuint32_t *box)
+{
+    const Encode encode = encoder();
     if (!encode) return report_cuda_error(cudaErrorNotSupported);
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const CUresult r = encode(m, dtype == GMS_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
+                              const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? GMS_OK : report_cuda_error(cudaErrorInvalidValue);
+}
+// One layer's keys or values as a 4-d tensor (d, token of block, head, block); boxes of 64 elements x `box_tokens` tokens.
+int encode_pool(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, uint32_t plane, uint32_t box_tokens)
+{
     const cuuint64_t dims[4] = {l->head_dim, l->block_tokens, l->n_kv_heads, pool->n_blocks};
     // a stride along a dimension of one element is never used, but has to be a legal one
     const cuuint64_t strides[3] = {l->token_stride, l->n_kv_heads > 1 ? l->head_stride : l->token_stride,
                                    pool->n_blocks > 1 ? pool->block_stride : pool->block_bytes};
-    const cuuint32_t box[4] = {64, box_tokens, 1, 1}, one[4] = {1, 1, 1, 1};
-    uint8_t *base = static_cast<uint8_t *>(pool->base) + plane * pool->plane_stride;
-    const CUresult r = encode(m, l->dtype == GMS_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base,
-                              dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? GMS_OK : report_cuda_error(cudaErrorInvalidValue);
+    const cuuint32_t box[4] = {64, box_tokens, 1, 1};
+    return encode_map(m, l->dtype, 4, static_cast<const uint8_t *>(pool->base) + plane * pool->plane_stride, dims, strides, box);
+}
+// The queries as (d, head, token): 128 rows are the `group` heads of 128 / group tokens.  False where that does not come out even,
+// where the strides are not a tensor map's (heads or tokens that share bytes), or where the scale's sign has to go into Q.
+bool q_boxes(const AttnArgs &a, uint32_t head_dim)
+{
+    return a.scale > 0.f && 128 % a.group == 0 && a.q_head_stride >= head_dim * 2 && a.q_token_stride >= head_dim * 2 &&
+           a.q_head_stride < (1ull << 40) && a.q_token_stride < (1ull << 40);
+}
+int encode_q(CUtensorMap *m, const AttnArgs &a, uint32_t dtype, uint32_t head_dim)
+{
+    const cuuint64_t dims[3] = {head_dim, a.n_heads, a.total_q}, strides[2] = {a.q_head_stride, a.q_token_stride};
+    const cuuint32_t box[3] = {64, a.group, 128 / a.group};
+    return encode_map(m, dtype, 3, a.q, dims, strides, box);
 }
 
 struct Carve {  // hands out 256-byte aligned pieces of the workspace; with a null base it only counts
@@ -255,7 +278,8 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
         p->row_ml = c->take<float2>((uint64_t)a.total_q * a.n_heads);
         p->row_o = c->take<float>((uint64_t)a.total_q * a.n_heads * head_dim);
     }
-    p->redo = a.max_q > 1;  // with one query a sequence, what its rows do not see is cleared before the product
+    p->again = a.max_q > 1;  // with one query a sequence, what its rows do not see is cleared before the product
+    if (tc && p->again && !rows_out) p->redo = c->take<uint32_t>((uint64_t)p->n_units * a.n_kv * (kTcRows / 32));
 }
 
 void plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace, Plan *pl, uint64_t *bytes)
@@ -301,12 +325,16 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         for (int i = 0; i < 2; ++i) {
             const uint32_t rows = i ? kTcRows : kFewRows;
             if (pl.own.rows != rows && !(prefix && pl.prefix.rows == rows)) continue;
-            rc = encode_map(&kmap[i], pool, layout, layout->k_plane, i ? box : kFewTile);
-            if (rc == GMS_OK) rc = encode_map(&vmap[i], pool, layout, layout->v_plane, i ? box : kFewTile);
+            rc = encode_pool(&kmap[i], pool, layout, layout->k_plane, i ? box : kFewTile);
+            if (rc == GMS_OK) rc = encode_pool(&vmap[i], pool, layout, layout->v_plane, i ? box : kFewTile);
             if (rc != GMS_OK) return rc;
         }
+        CUtensorMap qmap;
+        const bool tc = pl.own.rows == kTcRows || (prefix && pl.prefix.rows == kTcRows), q_tma = tc && q_boxes(a, dim);
+        if (q_tma) rc = encode_q(&qmap, a, dtype, dim);
+        if (rc != GMS_OK) return rc;
         auto launch = [&](const Pass &p) {
-            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], box, dtype, dim, s)
+            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], q_tma ? &qmap : nullptr, box, dtype, dim, s)
                                      : launch_kv_attn_few(b, p, kmap[0], vmap[0], dtype, dim, s);
         };
         if (prefix) e = launch(pl.prefix);

@@ -56,7 +56,8 @@ struct Pass {
     float2 *row_ml;        // [total_q * n_heads]
     float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2 (few-row pass only)
     uint32_t logit_stride;
-    uint32_t redo;         // 1: rows that come out non-finite are done again by the row kernel's method
+    uint32_t again;        // 1: rows that come out non-finite are done again (attend_row)
+    uint32_t *redo;        // many-row pass: null, or [n_units * n_kv][8], a bit for each such row of a finished item
 };
 
 struct EvictArgs {
@@ -81,10 +82,11 @@ cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, co
 constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewMaxCtas = 2 * 148;
 cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
                                uint32_t head_dim, cudaStream_t s);
-// Many query rows a unit; box_tokens: tokens a TMA box of the maps holds.
+// Many query rows a unit; box_tokens: tokens a TMA box of the maps holds; qmap: null, or boxes of 64 elements x group heads
+// x 128 / group tokens of the queries.
 constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxCtas = 148;
-cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens,
-                              uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
+                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);

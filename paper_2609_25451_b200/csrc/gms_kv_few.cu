@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                     *reinterpret_cast<float2 *>(po + j * 8 + (lane & 3u) * 2) = make_float2(x.o[j][r * 2], x.o[j][r * 2 + 1]);
             }
         }
-        if (p.redo) {
+        if (p.again) {
             for (int r = 0; r < 2; ++r) {
                 const uint32_t rows = __ballot_sync(0xffffffffu, again >> r & 1u);
                 for (int row = 0; row < 8; ++row)

@@ -86,6 +86,20 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     const uint32_t i = blockIdx.x / parts + 1, part = blockIdx.x % parts, warp = threadIdx.x / 32;
     const uint64_t total = p.begin[p.n_units];
     const uint32_t n = used_ctas(total, p);
+    if (p.redo) {  // rows of finished items that came out non-finite; a cut item's words are zero
+        for (uint32_t w = blockIdx.x * kWarps + warp; w < p.n_units * a.n_kv; w += gridDim.x * kWarps) {
+            const uint32_t unit = w / a.n_kv;
+            if (p.begin[unit] == p.begin[unit + 1]) continue;  // sees nothing: no words were written
+            const uint32_t mine = (threadIdx.x & 31u) < 8 ? p.redo[(uint64_t)w * 8 + (threadIdx.x & 31u)] : 0u;
+            if (!__any_sync(0xffffffffu, mine)) continue;
+            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+            for (uint32_t k = 0; k < 8; ++k)
+                for (uint32_t rows = __shfl_sync(0xffffffffu, mine, k); rows; rows &= rows - 1) {
+                    const int r = (int)k * 32 + __ffs(rows) - 1;
+                    attend_row<T, D>(a, unit_tok(a, u, r), unit_head(a, u, w % a.n_kv, r));
+                }
+        }
+    }
     if (i >= n) return;
     const uint64_t at = total * i / n;
     uint32_t lo = 0, hi = p.n_units;
@@ -103,7 +117,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     for (int r = part * kWarps + warp; r < u.rows; r += parts * kWarps) {
         Row<D> x;
         add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
-        finish<T, D>(a, x, unit_tok(a, u, r), unit_head(a, u, c, r), p.redo);
+        finish<T, D>(a, x, unit_tok(a, u, r), unit_head(a, u, c, r), p.again);
     }
 }
 
@@ -143,7 +157,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
     }
     if (own.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, own, x, s, tok, h);
     else add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);
-    finish<T, D>(a, x, tok, h, own.redo);
+    finish<T, D>(a, x, tok, h, own.again);
 }
 
 }  // namespace
@@ -164,11 +178,11 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
 
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
-    if (p.n_cta < 2) return cudaSuccess;
-    const uint32_t parts = p.rows / kFewRows;
+    if (p.n_cta < 2 && !p.redo) return cudaSuccess;
+    const uint32_t cuts = p.n_cta < 2 ? 1 : p.n_cta - 1, parts = p.rows / kFewRows;
     if (p.rows == kTcRows)
-        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, (p.n_cta - 1) * parts, kWarps * 32, 0, s, a, p, parts)));
-    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, (p.n_cta - 1) * parts, kWarps * 32, 0, s, a, p, parts)));
+        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));
+    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));
 }
 
 cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &pre, const Pass &own, uint32_t dtype, uint32_t head_dim, cudaStream_t s)

@@ -7,8 +7,9 @@
 //   O += P V       (128 x D x 128, P from tensor memory, V as it lies in the pool: token rows, "MN-major" operand)
 // O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
 // are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
-// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles).  Warp 8 issues the products, warp 9 the TMA
-// loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane a box.
+// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 216 registers a thread.  Warp 8 issues the
+// products, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
+// a box; warp 10 deals out the items (a ring of descriptors in shared memory); Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the softmax threads copy it).
 // Tensor memory: S0 S1 (128 columns each) O0 O1 (D each) = 512 columns at D = 128, hence P over S: the product with the next
 // K tile waits until P V of the slot is complete.
 // Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
@@ -21,8 +22,16 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 320, kRows = (int)kTcRows, kTile = (int)kTcTile;
+constexpr int kThreads = 384, kRows = (int)kTcRows, kTile = (int)kTcTile;
 constexpr float kLag = 8.f;  // log2 of how far a maximum may have grown before O is rescaled
+
+// A run of tiles of one item, as the roles read it from shared memory.  k0 == k1: no more.
+struct Segment {
+    const int32_t *table;
+    int q0, row0, rows, n, first, pos_min, pos_max, n_sink_tiles, first_tile, tiles, k0, k1;
+    uint32_t c, item, whole, pad;
+};
+constexpr uint32_t kSegments = 4;
 
 template <int D>
 struct Tc {
@@ -30,35 +39,39 @@ struct Tc {
     static constexpr uint32_t kHalfBytes = 128 * 128;             // 128 rows x 64 elements
     static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;  // a K, V or Q tile
     static constexpr int kStages = D == 128 ? 4 : 8;
-    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 2 + 2 + 1) * 8;
-    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kBars + 8 * (kThreads / 32 + 3) + 64 + 1024;
+    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 2 + 2 + 2 + 1 + 2 * kSegments) * 8;
+    static constexpr uint32_t kOutBytes = 8 * 2048;               // 32 rows x 64 bytes a softmax warp, for coalesced stores
+    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 8 * (kThreads / 32 + 3) + 16 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
     static constexpr uint32_t kCols = 512;
 };
 
-struct Segment {  // a run of tiles of one item
-    Unit un;
-    uint32_t c;
-    int k0, k1;
-    __device__ bool starts() const { return k0 == 0; }
-    __device__ bool ends() const { return k1 == un.tiles; }
-};
 __device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, Walk &w, Segment &g)
 {
+    g.k0 = g.k1 = 0;
     if (w.pos >= w.end) return false;
+    Unit u;
     for (;;) {
-        g.un = get_unit<kRows, kTile>(a, p, w.s, w.rt);
-        const uint64_t t = (uint64_t)g.un.tiles * a.n_kv;
+        u = get_unit<kRows, kTile>(a, p, w.s, w.rt);
+        const uint64_t t = (uint64_t)u.tiles * a.n_kv;
         if (w.pos < w.base + t) break;
         w.base += t;
         if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
     }
     const uint64_t in = w.pos - w.base;
-    g.c = (uint32_t)(in / (uint32_t)g.un.tiles);
-    g.k0 = (int)(in % (uint32_t)g.un.tiles);
-    g.k1 = (int)min((uint64_t)g.un.tiles, (uint64_t)g.k0 + (w.end - w.pos));
+    g.table = u.table;
+    g.q0 = u.q0, g.row0 = u.row0, g.rows = u.rows, g.n = u.n, g.first = u.first, g.pos_min = u.pos_min, g.pos_max = u.pos_max;
+    g.n_sink_tiles = u.n_sink_tiles, g.first_tile = u.first_tile, g.tiles = u.tiles, g.whole = u.whole;
+    g.c = (uint32_t)(in / (uint32_t)u.tiles);
+    g.k0 = (int)(in % (uint32_t)u.tiles);
+    g.k1 = (int)min((uint64_t)u.tiles, (uint64_t)g.k0 + (w.end - w.pos));
+    g.item = (w.s * p.n_rt + w.rt) * a.n_kv + g.c;
     w.pos += (uint32_t)(g.k1 - g.k0);
     return true;
+}
+__device__ __forceinline__ int seg_tile(const volatile Segment &g, int k)
+{
+    return k < g.n_sink_tiles ? k : g.first_tile + k - g.n_sink_tiles;
 }
 
 template <class T> struct IsBf16 { static constexpr bool value = false; };
@@ -80,14 +93,20 @@ __device__ __forceinline__ uint4 with_sign(uint4 v, uint32_t flip, uint32_t keep
     return make_uint4((v.x ^ flip) & keep, (v.y ^ flip) & keep, (v.z ^ flip) & keep, (v.w ^ flip) & keep);
 }
 
+// The lowest n bits (n may lie outside 0 .. 32).
+__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
 // A wait that every role uses: bounded, and cut short when another role has given up.
 __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t *abort, unsigned long long *status)
 {
-    if (mbar_try(bar, parity)) return true;
-    const uint64_t end = now_ns() + kWaitLimitNs;
-    for (uint32_t n = 1; n < (1u << 28); ++n) {
+    for (uint32_t n = 0; n < 4096; ++n) {
         if (mbar_try(bar, parity)) return true;
-        if ((n & 31u) == 0) {
+        if ((n & 63u) == 63u && *abort) return false;
+    }
+    const uint64_t end = now_ns() + kWaitLimitNs;
+    for (uint32_t n = 0; n < (1u << 28); ++n) {
+        if (mbar_try(bar, parity)) return true;
+        if ((n & 63u) == 63u) {
             if (*abort) return false;
             if (now_ns() > end) break;
         }
@@ -100,8 +119,9 @@ __device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, vol
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                  const __grid_constant__ CUtensorMap vmap,
+                                                                 const __grid_constant__ CUtensorMap qmap,
                                                                  const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
-                                                                 uint32_t box_tokens)
+                                                                 uint32_t box_tokens, uint32_t q_tma)
 {
     using F = Tc<D>;
     constexpr int NS = F::kStages;
@@ -110,25 +130,29 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *sm = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t q_smem = base, ring = base + 2 * F::kTileBytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, s_full = q_full + 16, p_full = s_full + 16,
-                   o_done = p_full + 16, drain = o_done + 16;
-    uint64_t *plan = bars + 2 * NS + 9;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes + F::kOutBytes);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, q_empty = q_full + 16, s_full = q_empty + 16,
+                   p_full = s_full + 16, o_done = p_full + 16, drain = o_done + 16, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
+    uint64_t *plan = bars + 2 * NS + 11 + 2 * kSegments;
     volatile uint32_t *shared_words = reinterpret_cast<volatile uint32_t *>(plan + kThreads / 32 + 3);  // [0] tensor memory, [1] abort
     volatile uint32_t *abort = shared_words + 1;
+    Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(q_full + 8 * i, 128);
+            mbar_init(q_full + 8 * i, q_tma ? 1 : 128);
+            mbar_init(q_empty + 8 * i, 1);
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 128);
             mbar_init(o_done + 8 * i, 1);
         }
         mbar_init(drain, 1);
+        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_empty + 8 * i, 10);  // 8 softmax warps, 2 more
         *abort = 0;
         fence_mbar_init();
         tma_prefetch_map(&kmap);
         tma_prefetch_map(&vmap);
+        if (q_tma) tma_prefetch_map(&qmap);
     }
     if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(shared_words)), F::kCols);
     grid_launch_dependents();
@@ -155,25 +179,61 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         }
     }
 
-    Segment g;
-    if (warp == 9) {
+    // 384 threads x 168 registers = 128 x 72 + 256 x 216
+    uint32_t seg = 0;  // segments seen
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 10) {
+        // ------------------------------------------------------------------ items
+        if (lane == 0)
+            for (bool more = true; more; ++seg) {
+                const uint32_t at = seg % kSegments;
+                if (!wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status)) break;
+                Segment g;
+                more = next_segment(a, p, w, g);
+                segs[at] = g;
+                mbar_arrive(seg_full + 8 * at);
+            }
+        __syncwarp();
+    } else if (warp == 9) {
         // ------------------------------------------------------------------ loads
         const int per = kTile / (int)box_tokens, boxes = per * F::kHalves;  // boxes a tile: at most 16
         const int half = (int)lane % F::kHalves, part = (int)lane / F::kHalves;
         const uint32_t tok_mask = (1u << a.block_shift) - 1u;
-        uint32_t n = 0;  // stages filled
+        uint32_t n = 0, q_n[2] = {0, 0};  // stages filled; times each slot's Q was
         bool ok = true;
-        while (ok && next_segment(a, p, w, g)) {
+        for (;; ++seg) {
+            ok = __all_sync(0xffffffffu, ok && wait_or_abort(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u, abort, a.status));
+            if (!ok) break;
+            const Segment &g = segs[seg % kSegments];
+            if (g.k0 == g.k1) break;
+            const int32_t *table = g.table;
+            const int len = g.n, k1 = g.k1, head = (int)g.c;
             auto block_of = [&](int k) -> int {  // a hole, or nothing left to read: out of range, zeros arrive
-                const int t = unit_tile(g.un, k) * kTile + part * (int)box_tokens;
+                const int t = seg_tile(g, k) * kTile + part * (int)box_tokens;
                 int id = -1;
-                if ((int)lane < boxes && t < g.un.n) id = g.un.table[(uint32_t)t >> a.block_shift];
+                if ((int)lane < boxes && t < len) id = table[(uint32_t)t >> a.block_shift];
                 return (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;
             };
             int next = block_of(g.k0);
-            for (int k = g.k0; ok && k < g.k1; ++k) {
-                const int blk = next, t = unit_tile(g.un, k) * kTile + part * (int)box_tokens;
-                if (k + 1 < g.k1) next = block_of(k + 1);
+            if (q_tma) {
+#pragma unroll
+                for (int slot = 0; slot < 2; ++slot) {
+                    if (!ok || slot * 128 >= g.rows) continue;
+                    ok = __all_sync(0xffffffffu, wait_or_abort(q_empty + 8 * slot, (q_n[slot] & 1u) ^ 1u, abort, a.status));
+                    if (!ok) continue;
+                    if (lane == 0) {
+                        mbar_expect(q_full + 8 * slot, F::kTileBytes);
+                        for (int h = 0; h < F::kHalves; ++h)
+                            tma_load_3d(q_smem + slot * F::kTileBytes + h * F::kHalfBytes, &qmap, h * 64, head * (int)a.group,
+                                        g.q0 + (g.row0 + slot * 128) / (int)a.group, q_full + 8 * slot);
+                    }
+                    ++q_n[slot];
+                }
+            }
+            for (int k = g.k0; ok && k < k1; ++k) {
+                const int blk = next, t = seg_tile(g, k) * kTile + part * (int)box_tokens;
+                if (k + 1 < k1) next = block_of(k + 1);
 #pragma unroll
                 for (int v = 0; v < 2; ++v) {
                     const uint32_t st = n % NS;
@@ -183,24 +243,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     __syncwarp();
                     if ((int)lane < boxes)
                         tma_load_4d(ring + st * F::kTileBytes + half * F::kHalfBytes + part * box_tokens * 128, v ? &vmap : &kmap, half * 64,
-                                    (int)((uint32_t)t & tok_mask), (int)g.c, blk, full + 8 * st);
+                                    (int)((uint32_t)t & tok_mask), head, blk, full + 8 * st);
                     ++n;
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
         }
         if (!ok)  // give up: wait (bounded) for what is still on its way into this CTA's shared memory
             for (uint32_t i = n > (uint32_t)NS ? n - NS : 0; i < n; ++i) (void)mbar_wait(full + 8 * (i % NS), (i / NS) & 1u);
+        for (int slot = 0; !ok && slot < 2; ++slot)
+            if (q_n[slot]) (void)mbar_wait(q_full + 8 * slot, (q_n[slot] - 1) & 1u);
     } else if (warp == 8) {
         // ------------------------------------------------------------------ products
         constexpr uint32_t id_s = f16_idesc(128, 128, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
-        uint32_t n = 0, seg = 0, done0 = 0, done1 = 0;  // tiles of K and V taken; segments; P V products of each slot
-        uint32_t seg1 = 0;
+        uint32_t n = 0, done0 = 0, done1 = 0, seg1 = 0;  // tiles of K and V taken; P V products of each slot; segments of slot 1
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {
             ok = ok && wait_or_abort(bar, parity, abort, a.status);
             return ok;
         };
-        auto scores = [&](int slot, uint32_t stage) {
+        auto scores = [&](int slot, uint32_t stage, bool last) {  // `last`: of the item, Q is free afterwards
             const uint32_t kt = ring + stage * F::kTileBytes, qt = q_smem + slot * F::kTileBytes;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
@@ -208,6 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 mma_ss(tmem + slot * 128, smem_desc(qt + off, 16, 1024), smem_desc(kt + off, 16, 1024), id_s, kk > 0);
             }
             tc_commit(s_full + 8 * slot);
+            if (last) tc_commit(q_empty + 8 * slot);
         };
         auto values = [&](int slot, uint32_t stage, bool add) {
             const uint32_t vt = ring + stage * F::kTileBytes;
@@ -218,21 +282,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             tc_commit(o_done + 8 * slot);
         };
         if (lane == 0) {
-            while (ok && next_segment(a, p, w, g)) {
-                const bool two = g.un.rows > 128;
+            for (; ok; ++seg) {
+                if (!wait(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u)) break;
+                const Segment &g = segs[seg % kSegments];
+                const bool two = g.rows > 128;
                 const int nt = g.k1 - g.k0;
+                mbar_arrive(seg_empty + 8 * (seg % kSegments));
+                if (nt == 0) break;
                 if (!wait(full + 8 * (n % NS), (n / NS) & 1u)) break;  // K of the first tile
                 if (!wait(q_full, seg & 1u)) break;
                 tc_fence_after();
-                scores(0, n % NS);
+                scores(0, n % NS, nt == 1);
                 if (two) {
                     if (!wait(q_full + 8, seg1 & 1u)) break;
                     tc_fence_after();
-                    scores(1, n % NS);
+                    scores(1, n % NS, nt == 1);
                     ++seg1;
                 }
                 tc_commit(empty + 8 * (n % NS));
-                ++seg;
                 for (int j = 0; j < nt; ++j) {
                     const uint32_t vs = n + 1, ks = n + 2;  // V of this tile, K of the next
                     const bool more = j + 1 < nt;
@@ -244,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                         if (!wait(full + 8 * (ks % NS), (ks / NS) & 1u)) break;
                         if (!wait(o_done, done0 & 1u)) break;  // P lies over S
                         tc_fence_after();
-                        scores(0, ks % NS);
+                        scores(0, ks % NS, j + 2 == nt);
                     }
                     ++done0;
                     if (two) {
@@ -254,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                         if (more) {
                             if (!wait(o_done + 8, done1 & 1u)) break;
                             tc_fence_after();
-                            scores(1, ks % NS);
+                            scores(1, ks % NS, j + 2 == nt);
                         }
                         ++done1;
                     }
@@ -267,7 +334,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             (void)mbar_wait(drain, 0);
         }
         __syncwarp();
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------------------------ softmax, one thread a row
         const int slot = (int)warp / 4, row_in = (int)(warp % 4) * 32 + (int)lane, row = slot * 128 + row_in;
         const uint32_t lanes = ((warp % 4) * 32) << 16;
@@ -280,42 +349,51 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             ok = __all_sync(0xffffffffu, ok && wait_or_abort(bar, parity, abort, a.status));
             return ok;
         };
-        while (ok && next_segment(a, p, w, g)) {
-            const int nt = g.k1 - g.k0;
-            if (slot == 1 && g.un.rows <= 128) {
-                n += (uint32_t)nt;
+        for (;; ++seg) {
+            if (!wait(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u)) break;
+            const Segment &g = segs[seg % kSegments];
+            const int k0 = g.k0, k1 = g.k1, rows = g.rows, row0 = g.row0, q0 = g.q0, len = g.n;
+            if (k0 == k1) break;
+            const uint32_t head0 = g.c * a.group;
+            const bool all = g.whole != 0;
+            if (slot == 1 && rows <= 128) {
+                n += (uint32_t)(k1 - k0);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
                 continue;
             }
-            // Q: 16-byte pieces, a row's in neighbouring lanes; rows that do not exist are zero
-            const uint32_t qt = q_smem + slot * F::kTileBytes;
+            auto tok_of = [&](int r) { return q0 + (row0 + r) / (int)a.group; };
+            auto head_of = [&](int r) { return head0 + (uint32_t)(row0 + r) % a.group; };
+            auto pos_of = [&](int r) { return all ? len - 1 : g.first + (row0 + r) / (int)a.group; };
+            if (!q_tma) {  // 16-byte pieces, a row's in neighbouring lanes; rows that do not exist are zero
 #pragma unroll 4
-            for (int i = 0; i < D / 8; ++i) {
-                const int idx = i * 128 + row_in, r = idx / (D / 8), ch = idx % (D / 8);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (slot * 128 + r < g.un.rows)
-                    v = with_sign(*reinterpret_cast<const uint4 *>(a.q + (uint64_t)unit_tok(a, g.un, slot * 128 + r) * a.q_token_stride +
-                                                                   (uint64_t)unit_head(a, g.un, g.c, slot * 128 + r) * a.q_head_stride + ch * 16),
-                                  flip, keep);
-                *reinterpret_cast<uint4 *>(sm + slot * F::kTileBytes + (ch / 8) * F::kHalfBytes + r * 128 + (((ch % 8) ^ (r & 7)) << 4)) = v;
+                for (int i = 0; i < D / 8; ++i) {
+                    const int idx = i * 128 + row_in, r = idx / (D / 8), ch = idx % (D / 8);
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (slot * 128 + r < rows)
+                        v = with_sign(*reinterpret_cast<const uint4 *>(a.q + (uint64_t)tok_of(slot * 128 + r) * a.q_token_stride +
+                                                                       (uint64_t)head_of(slot * 128 + r) * a.q_head_stride + ch * 16),
+                                      flip, keep);
+                    *reinterpret_cast<uint4 *>(sm + slot * F::kTileBytes + (ch / 8) * F::kHalfBytes + r * 128 + (((ch % 8) ^ (r & 7)) << 4)) = v;
+                }
+                fence_proxy_async();
+                mbar_arrive(q_full + 8 * slot);
             }
-            (void)qt;
-            fence_proxy_async();
-            mbar_arrive(q_full + 8 * slot);
 
-            const bool live = row < g.un.rows;
-            const int pos = unit_row_pos(a, g.un, live ? row : g.un.rows - 1);
-            const int pos_lo = unit_row_pos(a, g.un, slot * 128), pos_hi = unit_row_pos(a, g.un, min(slot * 128 + 127, g.un.rows - 1));
+            const bool live = row < rows;
+            const int pos = pos_of(live ? row : rows - 1), pos_lo = pos_of(slot * 128), pos_hi = pos_of(min(slot * 128 + 127, rows - 1));
+            const int32_t *table = g.table;
             float m = neg_inf(), l = 0.f;
             int id_next = -1;
             auto tile_id = [&](int k) -> int {  // the block of each 16 tokens of the tile, one lane each
-                const int t = unit_tile(g.un, k) * kTile + (int)lane * 16;
-                return lane < 8 && t < g.un.n ? g.un.table[(uint32_t)t >> a.block_shift] : -1;
+                const int t = seg_tile(g, k) * kTile + (int)lane * 16;
+                return lane < 8 && t < len ? table[(uint32_t)t >> a.block_shift] : -1;
             };
-            id_next = tile_id(g.k0);
-            for (int k = g.k0; k < g.k1; ++k) {
-                const int t0 = unit_tile(g.un, k) * kTile;
+            id_next = tile_id(k0);
+            for (int k = k0; k < k1; ++k) {
+                const int t0 = seg_tile(g, k) * kTile;
                 const uint32_t valid = __ballot_sync(0xffffffffu, (uint32_t)id_next < a.n_blocks) & 0xffu;
-                if (k + 1 < g.k1) id_next = tile_id(k + 1);
+                if (k + 1 < k1) id_next = tile_id(k + 1);
                 if (!wait(s_full + 8 * slot, tiles & 1u)) break;
                 tc_fence_after();
                 uint32_t s[4][32];
@@ -324,20 +402,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tmem_wait32(s[i]);
                 const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo &&
-                                   (g.un.whole || a.window == 0 || (long long)t0 > (long long)pos_hi - (long long)a.window ||
+                                   (all || a.window == 0 || (long long)t0 > (long long)pos_hi - (long long)a.window ||
                                     (uint32_t)(t0 + kTile - 1) < a.sinks);
                 if (!whole) {
-                    const int hi = pos - t0;  // columns up to hi; from lo on or below sink
-                    const int lo = (int)(g.un.whole || a.window == 0 ? 0ll : max(0ll, min((long long)kTile, (long long)pos - (long long)a.window + 1 - t0)));
+                    const int hi = pos - t0 + 1;  // columns below hi, from lo on or below sink
+                    const int lo = (int)(all || a.window == 0 ? 0ll : max(0ll, min((long long)kTile, (long long)pos - (long long)a.window + 1 - t0)));
                     const int sink = (int)max(0ll, min((long long)kTile, (long long)a.sinks - t0));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t held = ((valid >> (2 * i) & 1u) ? 0xffffu : 0u) | ((valid >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
+                        const uint32_t on = held & first_bits(hi - i * 32) & (~first_bits(lo - i * 32) | first_bits(sink - i * 32));
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int col = i * 32 + j;
-                            const bool on = col <= hi && (col >= lo || col < sink) && (valid >> (col / 16) & 1u);
-                            if (!on) s[i][j] = 0xff800000u;
-                        }
+                        for (int j = 0; j < 32; ++j)
+                            if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
+                    }
                 }
                 float top = neg_inf();
 #pragma unroll
@@ -350,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
                     if (grow) m = top;
                     l *= f;
-                    if (k != g.k0) {  // S of this tile is issued after P V of the last: O is at rest
+                    if (k != k0) {  // S of this tile is issued after P V of the last: O is at rest
 #pragma unroll
                         for (int i = 0; i < D / 32; ++i) {
                             uint32_t o[32];
@@ -381,14 +459,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 // thread r clears token r; slot 1's product comes after slot 0's)
                 if (slot == 0 && !whole) {
                     const int t = t0 + row_in;
-                    const bool none = t > g.un.pos_max || (!g.un.whole && !sees(a, max(g.un.pos_min, t), t));
+                    const bool none = t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t));
                     const uint32_t vs = 2 * n + 1;
                     if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
                     if (none)
 #pragma unroll
                         for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + e * 16);
+                            for (int e = 0; e < 8; ++e) st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
                     fence_proxy_async();
                 }
                 tmem_wait_st();
@@ -401,55 +479,67 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             // the item's rows (or this CTA's piece of them)
             if (!wait(o_done + 8 * slot, (tiles - 1) & 1u)) break;
             tc_fence_after();
-            const uint64_t tok = unit_tok(a, g.un, live ? row : 0);
-            const uint32_t h = unit_head(a, g.un, g.c, live ? row : 0);
-            const bool finished = g.starts() && g.ends() && !p.row_o;
-            uint8_t *dst;
-            if (finished) {
-                dst = a.out + tok * a.out_token_stride + h * a.out_head_stride;
-                if (live && a.lse) a.lse[tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
-            } else {
-                const bool mine = g.starts() && g.ends();
-                const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (g.starts() ? 1 : 0)) * kRows + row;
-                dst = reinterpret_cast<uint8_t *>((mine ? p.row_o : p.part_o) + at * D);
-                if (live) (mine ? p.row_ml : p.part_ml)[at] = make_float2(m, l);
-            }
+            const uint64_t tok = tok_of(live ? row : 0);
+            const uint32_t h = head_of(live ? row : 0);
+            const bool starts = k0 == 0, mine = starts && k1 == g.tiles, finished = mine && !p.row_o;
             const float inv = l == 0.f ? 0.f : 1.f / l;
             bool bad = false;
+            if (finished) {
+                // through shared memory, so that four lanes write 64 bytes of a row at a time
+                const uint64_t at = tok * a.out_token_stride + h * a.out_head_stride;
+                uint8_t *stage = sm + (2 + NS) * F::kTileBytes + warp * 2048;
+                if (live && a.lse) a.lse[tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
+                const uint32_t rows_here = (uint32_t)max(0, min(32, rows - slot * 128 - (int)(warp % 4) * 32));
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                uint32_t o[32];
-                tmem_ld32(o_col + i * 32, o);
-                tmem_wait32(o);
-                if (!live) continue;
-                if (finished) {
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32];
+                    tmem_ld32(o_col + i * 32, o);
+                    tmem_wait32(o);
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
+                    for (int j = 0; j < 4; ++j) {
                         uint32_t v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float lo = l == 0.f ? 0.f : __uint_as_float(o[j + 2 * e]) * inv, hi = l == 0.f ? 0.f : __uint_as_float(o[j + 2 * e + 1]) * inv;
+                            float lo = __uint_as_float(o[j * 8 + 2 * e]) * inv, hi = __uint_as_float(o[j * 8 + 2 * e + 1]) * inv;
+                            if (l == 0.f) lo = hi = 0.f;
                             bad |= !(fabsf(lo) < kHuge && fabsf(hi) < kHuge);
                             v[e] = pack2(lo, hi, T());
                         }
-                        *reinterpret_cast<uint4 *>(dst + i * 64 + j * 2) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4 *>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
-                } else {
+                    __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) *reinterpret_cast<uint4 *>(dst + i * 128 + j * 4) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t r = e * 8 + lane / 4, ch = lane & 3u;
+                        const uint64_t to = __shfl_sync(0xffffffffu, at, r);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((ch ^ (r >> 1 & 3)) << 4));
+                        if (r < rows_here) *reinterpret_cast<uint4 *>(a.out + to + i * 64 + ch * 16) = v;
+                    }
+                    __syncwarp();
+                }
+            } else {
+                const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * kRows + row;
+                float *dst = (mine ? p.row_o : p.part_o) + at * D;
+                if (live) (mine ? p.row_ml : p.part_ml)[at] = make_float2(m, l);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32];
+                    tmem_ld32(o_col + i * 32, o);
+                    tmem_wait32(o);
+                    if (live)
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            *reinterpret_cast<uint4 *>(dst + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                 }
             }
             tc_fence_before();
-            if (p.redo && finished) {
-                uint32_t again = __ballot_sync(0xffffffffu, live && bad);
-                __syncwarp();
-                while (again) {
-                    const int r = __ffs(again) - 1;
-                    again &= again - 1;
-                    const int rr = slot * 128 + (int)(warp % 4) * 32 + r;
-                    attend_row<T, D>(a, unit_tok(a, g.un, rr), unit_head(a, g.un, g.c, rr));
-                }
+            if (p.redo) {  // which of the warp's rows the join has to do again
+                const uint32_t again = __ballot_sync(0xffffffffu, live && bad);
+                if (lane == 0) p.redo[(uint64_t)g.item * 8 + warp] = again;
+                if (rows <= 128 && lane == 1) p.redo[(uint64_t)g.item * 8 + 4 + warp] = 0;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
         }
     }
     tc_fence_before();
@@ -461,25 +551,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
 }
 
 template <class T, int D>
-cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens, cudaStream_t s)
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
+                   uint32_t box_tokens, cudaStream_t s)
 {
     constexpr uint32_t smem = Tc<D>::kSmem;
     static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
-    kv_attn_tc_kernel<T, D><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, a, p, box_tokens);
+    kv_attn_tc_kernel<T, D><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, qmap ? *qmap : kmap, a, p, box_tokens, qmap != nullptr);
     count_launches(1);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t box_tokens,
-                              uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
+                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
     if (dtype == GMS_DTYPE_BF16)
-        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, box_tokens, s)
-                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, box_tokens, s);
-    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, box_tokens, s) : launch<__half, 128>(a, p, kmap, vmap, box_tokens, s);
+        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, qmap, box_tokens, s)
+                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
+    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, qmap, box_tokens, s) : launch<__half, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
 }
 
 }  // namespace gms

@@ -43,13 +43,15 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-// Waits for a phase; false once the limit has passed.
+// Waits for a phase; false once the limit has passed.  The clock is looked at after the first few thousand tries only.
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity)
 {
+    for (uint32_t n = 0; n < 4096; ++n)
+        if (mbar_try(bar, parity)) return true;
     const uint64_t end = now_ns() + kWaitLimitNs;
     for (uint32_t n = 0; n < (1u << 28); ++n) {
         if (mbar_try(bar, parity)) return true;
-        if ((n & 31u) == 31u && now_ns() > end) return false;
+        if ((n & 255u) == 255u && now_ns() > end) return false;
     }
     return false;
 }
@@ -68,6 +70,13 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *m, 
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
         "l"(m), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(m), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
 
