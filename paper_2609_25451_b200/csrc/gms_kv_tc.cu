@@ -1,17 +1,18 @@
 // Attention of many query rows (prompts, chunks, batches behind one prefix) over the paged pool, on tcgen05.
 //
-// A unit is 256 query rows (tokens x the heads that share a KV head), two slots of 128: while the tensor core works for one
-// slot, the other's softmax runs.  Per tile of 128 tokens and slot
-//   S = Q K^T      (128 x 128 x D, both operands in shared memory, S in tensor memory)
+// A unit is 256 query rows (tokens x the heads that share a KV head), two slots of 128.  Per step of 64 tokens and slot
+//   S = Q K^T      (128 x 64 x D, both operands in shared memory, S in tensor memory)
 //   P = 2^(S c - m), rounded to the pool's type, written over S in tensor memory; l += sum P in 32 bits
-//   O += P V       (128 x D x 128, P from tensor memory, V as it lies in the pool: token rows, "MN-major" operand)
+//   O += P V       (128 x D x 64, P from tensor memory, V as it lies in the pool: token rows, "MN-major" operand)
+// Each slot has two S buffers, so that the product for its next step is done while its softmax works on this one, and the two
+// slots take turns at the tensor core; a buffer is written again once P V of the step that used it is complete.
+// (128-token steps with one buffer a slot: 976 us for 2,048 new tokens over 16k, the softmax waiting 40 % of the time.)
 // O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
 // are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
 // Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 216 registers a thread.  Warp 8 issues the
 // products, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
 // a box; warp 10 deals out the items (a ring of descriptors in shared memory); Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the softmax threads copy it).
-// Tensor memory: S0 S1 (128 columns each) O0 O1 (D each) = 512 columns at D = 128, hence P over S: the product with the next
-// K tile waits until P V of the slot is complete.
+// Tensor memory: 2 x 2 S buffers of 64 columns, O0 O1 (D each) = 512 columns at D = 128, hence P over S.
 // Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
 #include "gms_internal.h"
 #include "gms_kv_attn.h"
@@ -39,7 +40,7 @@ struct Tc {
     static constexpr uint32_t kHalfBytes = 128 * 128;             // 128 rows x 64 elements
     static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;  // a K, V or Q tile
     static constexpr int kStages = D == 128 ? 4 : 8;
-    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 2 + 2 + 2 + 1 + 2 * kSegments) * 8;
+    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 2 * kSegments) * 8;
     static constexpr uint32_t kOutBytes = 8 * 2048;               // 32 rows x 64 bytes a softmax warp, for coalesced stores
     static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 8 * (kThreads / 32 + 3) + 16 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
@@ -132,8 +133,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     const uint32_t q_smem = base, ring = base + 2 * F::kTileBytes;
     uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes + F::kOutBytes);
     const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, q_empty = q_full + 16, s_full = q_empty + 16,
-                   p_full = s_full + 16, o_done = p_full + 16, drain = o_done + 16, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
-    uint64_t *plan = bars + 2 * NS + 11 + 2 * kSegments;
+                   p_full = s_full + 32, o_done = p_full + 32, drain = o_done + 32, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
+    uint64_t *plan = bars + 2 * NS + 17 + 2 * kSegments;
     volatile uint32_t *shared_words = reinterpret_cast<volatile uint32_t *>(plan + kThreads / 32 + 3);  // [0] tensor memory, [1] abort
     volatile uint32_t *abort = shared_words + 1;
     Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
@@ -142,9 +143,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         for (int i = 0; i < 2; ++i) {
             mbar_init(q_full + 8 * i, q_tma ? 1 : 128);
             mbar_init(q_empty + 8 * i, 1);
-            mbar_init(s_full + 8 * i, 1);
-            mbar_init(p_full + 8 * i, 128);
-            mbar_init(o_done + 8 * i, 1);
+            for (int b = 0; b < 2; ++b) {  // one of each a buffer: no one is ever two phases behind
+                mbar_init(s_full + 8 * (2 * i + b), 1);
+                mbar_init(p_full + 8 * (2 * i + b), 128);
+                mbar_init(o_done + 8 * (2 * i + b), 1);
+            }
         }
         mbar_init(drain, 1);
         for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_empty + 8 * i, 10);  // 8 softmax warps, 2 more
@@ -256,83 +259,78 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             if (q_n[slot]) (void)mbar_wait(q_full + 8 * slot, (q_n[slot] - 1) & 1u);
     } else if (warp == 8) {
         // ------------------------------------------------------------------ products
-        constexpr uint32_t id_s = f16_idesc(128, 128, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
-        uint32_t n = 0, done0 = 0, done1 = 0, seg1 = 0;  // tiles of K and V taken; P V products of each slot; segments of slot 1
+        constexpr uint32_t id_s = f16_idesc(128, 64, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
+        uint32_t n = 0, steps[2] = {0, 0}, items[2] = {0, 0};  // stages of finished segments; steps and segments of each slot
         bool ok = true;
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-            ok = ok && wait_or_abort(bar, parity, abort, a.status);
-            return ok;
+        auto wait = [&](uint32_t bar, uint32_t parity) {  // the whole warp waits and issues as one
+            ok = __all_sync(0xffffffffu, ok && wait_or_abort(bar, parity, abort, a.status));
         };
-        auto scores = [&](int slot, uint32_t stage, bool last) {  // `last`: of the item, Q is free afterwards
-            const uint32_t kt = ring + stage * F::kTileBytes, qt = q_smem + slot * F::kTileBytes;
+        const uint32_t on = one_lane();
+        constexpr uint32_t hi = desc_hi(1024);
+        const uint32_t q_lo = desc_lo(q_smem, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
+        int nt = 0, last_slot = 0;
+        // S of step i of the segment (tile i / 2, its half i % 2)
+        auto scores = [&](int slot, int i) {
+            const uint32_t st = (n + 2 * (i >> 1)) % NS, half = i & 1, idx = n + 2 * (i >> 1);
+            if (half == 0) wait(full + 8 * st, (idx / NS) & 1u);
+            if (i >= 2) wait(o_done + 8 * (2 * slot + half), (((steps[slot] + i) >> 1) - 1) & 1u);  // P of step i - 2 lies in this buffer
+            if (!ok) return;
+            tc_fence_after();
+            const uint32_t kt = k_lo + ((st * F::kTileBytes + half * 64 * 128) >> 4), qt = q_lo + (slot * F::kTileBytes >> 4);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = (kk / 4) * F::kHalfBytes + (kk % 4) * 32;
-                mma_ss(tmem + slot * 128, smem_desc(qt + off, 16, 1024), smem_desc(kt + off, 16, 1024), id_s, kk > 0);
+                const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
+                mma_ss(on, tmem + slot * 128 + half * 64, qt + off, kt + off, hi, id_s, kk > 0);
             }
-            tc_commit(s_full + 8 * slot);
-            if (last) tc_commit(q_empty + 8 * slot);
+            tc_commit(on, s_full + 8 * (2 * slot + half));
+            if (half && slot == last_slot) tc_commit(on, empty + 8 * st);
+            if (i + 1 == 2 * nt) tc_commit(on, q_empty + 8 * slot);
         };
-        auto values = [&](int slot, uint32_t stage, bool add) {
-            const uint32_t vt = ring + stage * F::kTileBytes;
+        auto values = [&](int slot, int i) {
+            const uint32_t idx = n + 2 * (i >> 1) + 1, st = idx % NS, half = i & 1;
+            if (half == 0) wait(full + 8 * st, (idx / NS) & 1u);
+            wait(p_full + 8 * (2 * slot + half), ((steps[slot] + i) >> 1) & 1u);
+            if (!ok) return;
+            tc_fence_after();
+            const uint32_t vt = v_lo + ((st * F::kTileBytes + half * 4 * 2048) >> 4);
 #pragma unroll
-            for (int kk = 0; kk < kTile / 16; ++kk)
-                mma_ts(tmem + F::kO + slot * D, tmem + slot * 128 + kk * 8, smem_desc(vt + kk * 2048, F::kHalfBytes, 1024), id_o,
-                       add || kk > 0);
-            tc_commit(o_done + 8 * slot);
+            for (int kk = 0; kk < 4; ++kk)
+                mma_ts(on, tmem + F::kO + slot * D, tmem + slot * 128 + half * 64 + kk * 8, vt + (kk * 2048 >> 4), hi, id_o, i > 0 || kk > 0);
+            tc_commit(on, o_done + 8 * (2 * slot + half));
+            if (half && slot == last_slot) tc_commit(on, empty + 8 * st);
         };
-        if (lane == 0) {
-            for (; ok; ++seg) {
-                if (!wait(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u)) break;
-                const Segment &g = segs[seg % kSegments];
-                const bool two = g.rows > 128;
-                const int nt = g.k1 - g.k0;
-                mbar_arrive(seg_empty + 8 * (seg % kSegments));
-                if (nt == 0) break;
-                if (!wait(full + 8 * (n % NS), (n / NS) & 1u)) break;  // K of the first tile
-                if (!wait(q_full, seg & 1u)) break;
-                tc_fence_after();
-                scores(0, n % NS, nt == 1);
-                if (two) {
-                    if (!wait(q_full + 8, seg1 & 1u)) break;
-                    tc_fence_after();
-                    scores(1, n % NS, nt == 1);
-                    ++seg1;
-                }
-                tc_commit(empty + 8 * (n % NS));
-                for (int j = 0; j < nt; ++j) {
-                    const uint32_t vs = n + 1, ks = n + 2;  // V of this tile, K of the next
-                    const bool more = j + 1 < nt;
-                    if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
-                    if (!wait(p_full, done0 & 1u)) break;
-                    tc_fence_after();
-                    values(0, vs % NS, j > 0);
-                    if (more) {
-                        if (!wait(full + 8 * (ks % NS), (ks / NS) & 1u)) break;
-                        if (!wait(o_done, done0 & 1u)) break;  // P lies over S
-                        tc_fence_after();
-                        scores(0, ks % NS, j + 2 == nt);
-                    }
-                    ++done0;
-                    if (two) {
-                        if (!wait(p_full + 8, done1 & 1u)) break;
-                        tc_fence_after();
-                        values(1, vs % NS, j > 0);
-                        if (more) {
-                            if (!wait(o_done + 8, done1 & 1u)) break;
-                            tc_fence_after();
-                            scores(1, ks % NS, j + 2 == nt);
-                        }
-                        ++done1;
-                    }
-                    tc_commit(empty + 8 * (vs % NS));
-                    if (more) tc_commit(empty + 8 * (ks % NS));
-                    n += 2;
-                }
+        for (; ok; ++seg) {
+            wait(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
+            if (!ok) break;
+            const Segment &g = segs[seg % kSegments];
+            last_slot = __shfl_sync(0xffffffffu, g.rows > 128, 0);
+            nt = g.k1 - g.k0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
+            if (nt == 0) break;
+#pragma unroll
+            for (int slot = 0; slot < 2; ++slot) {
+                if (slot > last_slot) continue;
+                wait(q_full + 8 * slot, items[slot] & 1u);
+                for (int b = 0; b < 2 && steps[slot]; ++b)  // the last item's P V: both buffers are free
+                    wait(o_done + 8 * (2 * slot + b), ((steps[slot] >> 1) - 1) & 1u);
+                scores(slot, 0);
             }
-            tc_commit(drain);  // nothing of this thread's is in flight when the CTA ends
-            (void)mbar_wait(drain, 0);
+            scores(0, 1);
+            for (int i = 0; ok && i < 2 * nt; ++i) {
+                values(0, i);
+                if (last_slot) {
+                    if (i + 1 < 2 * nt) scores(1, i + 1);
+                    values(1, i);
+                }
+                if (i + 2 < 2 * nt) scores(0, i + 2);
+            }
+            steps[0] += 2 * nt, ++items[0];
+            if (last_slot) steps[1] += 2 * nt, ++items[1];
+            n += 2 * nt;
         }
+        tc_commit(on, drain);  // nothing of this warp's is in flight when the CTA ends
+        (void)mbar_wait(drain, 0);
         __syncwarp();
     }
     } else {
@@ -383,6 +381,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             const bool live = row < rows;
             const int pos = pos_of(live ? row : rows - 1), pos_lo = pos_of(slot * 128), pos_hi = pos_of(min(slot * 128 + 127, rows - 1));
             const int32_t *table = g.table;
+            // the row's window starts at low; low_hi: the latest start among the slot's rows; sink: tokens always seen
+            auto low_of = [&](int ps) { return all || a.window == 0 || (uint32_t)max(ps, 0) < a.window ? 0 : ps - (int)a.window + 1; };
+            const int low = low_of(pos), low_hi = low_of(pos_hi), sink = (int)min(a.sinks, 0x7fffffffu);
             float m = neg_inf(), l = 0.f;
             int id_next = -1;
             auto tile_id = [&](int k) -> int {  // the block of each 16 tokens of the tile, one lane each
@@ -394,90 +395,96 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 const int t0 = seg_tile(g, k) * kTile;
                 const uint32_t valid = __ballot_sync(0xffffffffu, (uint32_t)id_next < a.n_blocks) & 0xffu;
                 if (k + 1 < k1) id_next = tile_id(k + 1);
-                if (!wait(s_full + 8 * slot, tiles & 1u)) break;
-                tc_fence_after();
-                uint32_t s[4][32];
+                const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo && (t0 >= low_hi || t0 + kTile - 1 < sink);
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t s_at = s_col + half * 64;
+                    if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) break;
+                    tc_fence_after();
+                    uint32_t s[2][32];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(s_col + i * 32, s[i]);
+                    for (int i = 0; i < 2; ++i) tmem_ld32(s_at + i * 32, s[i]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_wait32(s[i]);
-                const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo &&
-                                   (all || a.window == 0 || (long long)t0 > (long long)pos_hi - (long long)a.window ||
-                                    (uint32_t)(t0 + kTile - 1) < a.sinks);
-                if (!whole) {
-                    const int hi = pos - t0 + 1;  // columns below hi, from lo on or below sink
-                    const int lo = (int)(all || a.window == 0 ? 0ll : max(0ll, min((long long)kTile, (long long)pos - (long long)a.window + 1 - t0)));
-                    const int sink = (int)max(0ll, min((long long)kTile, (long long)a.sinks - t0));
+                    for (int i = 0; i < 2; ++i) tmem_wait32(s[i]);
+                    if (!whole) {
+                        const uint32_t v4 = valid >> (4 * half);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t held = ((valid >> (2 * i) & 1u) ? 0xffffu : 0u) | ((valid >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
-                        const uint32_t on = held & first_bits(hi - i * 32) & (~first_bits(lo - i * 32) | first_bits(sink - i * 32));
+                        for (int i = 0; i < 2; ++i) {
+                            const int c0 = t0 + half * 64 + i * 32;
+                            const uint32_t held = ((v4 >> (2 * i) & 1u) ? 0xffffu : 0u) | ((v4 >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
+                            const uint32_t on = held & first_bits(pos + 1 - c0) & (~first_bits(low - c0) | first_bits(sink - c0));
+                            if (__all_sync(0xffffffffu, on == 0xffffffffu)) continue;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
-                    }
-                }
-                float top = neg_inf();
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(s[i][j]));
-                top *= c2;
-                const bool grow = top > m + kLag || (m == neg_inf() && top != m);
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
-                    if (grow) m = top;
-                    l *= f;
-                    if (k != k0) {  // S of this tile is issued after P V of the last: O is at rest
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t o[32];
-                            tmem_ld32(o_col + i * 32, o);
-                            tmem_wait32(o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                            tmem_st32(o_col + i * 32, o);
+                            for (int j = 0; j < 32; ++j)
+                                if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
                         }
                     }
-                }
-                const float z = m == neg_inf() ? 0.f : m;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    float top = neg_inf();
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(s[i][j]));
+                    top *= c2;
+                    const bool grow = top > m + kLag || (m == neg_inf() && top != m);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
+                        if (grow) m = top;
+                        l *= f;
+                        if (k != k0 || half) {
+                            if (!wait(o_done + 8 * (2 * slot + (half ^ 1)), (tiles + (half ^ 1)) & 1u)) break;  // O is at rest until this step's P is handed over
+                            tc_fence_after();
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i) {
+                                uint32_t o[32];
+                                tmem_ld32(o_col + i * 32, o);
+                                tmem_wait32(o);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_st32(o_col + i * 32, o);
+                            }
+                        }
+                    }
+                    const float z = m == neg_inf() ? 0.f : m;
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
                     uint32_t pk[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        const float x0 = ex2(fmaf(__uint_as_float(s[i * 2 + j / 16][(j * 2) % 32]), c2, -z));
-                        const float x1 = ex2(fmaf(__uint_as_float(s[i * 2 + j / 16][(j * 2 + 1) % 32]), c2, -z));
+                        const float x0 = ex2(fmaf(__uint_as_float(s[j / 16][(j * 2) % 32]), c2, -z));
+                        const float x1 = ex2(fmaf(__uint_as_float(s[j / 16][(j * 2 + 1) % 32]), c2, -z));
                         part[j & 3] += x0 + x1;
                         pk[j] = pack2(x0, x1, T());
                     }
-                    tmem_st32(s_col + i * 32, pk);
-                }
-                l += (part[0] + part[1]) + (part[2] + part[3]);
-                // values of tokens that no row of the unit sees must not meet the product, whatever bits they are (slot 0's
-                // thread r clears token r; slot 1's product comes after slot 0's)
-                if (slot == 0 && !whole) {
-                    const int t = t0 + row_in;
-                    const bool none = t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t));
-                    const uint32_t vs = 2 * n + 1;
-                    if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
-                    if (none)
+                    tmem_st32(s_at, pk);
+                    l += (part[0] + part[1]) + (part[2] + part[3]);
+                    // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
+                    // of the unit sees, where rows are not done again (slot 0's thread r clears token r of the tile before its
+                    // first half is handed over; slot 1's product comes after slot 0's).
+                    if (slot == 0 && half == 0 && !whole) {
+                        const int t = t0 + row_in;
+                        const bool none = t >= len || (!p.again && (t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t))));
+                        if (__any_sync(0xffffffffu, none)) {
+                            const uint32_t vs = 2 * n + 1;
+                            if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
+                            if (none)
 #pragma unroll
-                        for (int h = 0; h < F::kHalves; ++h)
+                                for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
-                    fence_proxy_async();
+                                    for (int e = 0; e < 8; ++e)
+                                        st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
+                            fence_proxy_async();
+                        }
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(p_full + 8 * (2 * slot + half));
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(p_full + 8 * slot);
+                if (!ok) break;
                 ++n;
                 ++tiles;
             }
             if (!ok) break;
             // the item's rows (or this CTA's piece of them)
-            if (!wait(o_done + 8 * slot, (tiles - 1) & 1u)) break;
+            if (!wait(o_done + 16 * slot, (tiles - 1) & 1u) || !wait(o_done + 16 * slot + 8, (tiles - 1) & 1u)) break;
             tc_fence_after();
             const uint64_t tok = tok_of(live ? row : 0);
             const uint32_t h = head_of(live ? row : 0);

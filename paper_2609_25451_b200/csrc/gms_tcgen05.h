@@ -5,40 +5,51 @@
 namespace gms {
 namespace ptx {
 
-// Shared-memory operand descriptor, 128-byte swizzle.  K-major operands: `sbo` bytes between groups of 8 rows (lbo unused).
+// Shared-memory operand descriptor, 128-byte swizzle, as two words; (offset >> 4) may be added to the low one.  K-major operands: `sbo` bytes between groups of 8 rows (lbo unused).
 // MN-major operands: `lbo` bytes between groups of 64 elements, `sbo` bytes between groups of 8 k.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo)
-{
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (uint64_t)((lbo >> 4) & 0x3fffu) << 16 | (uint64_t)((sbo >> 4) & 0x3fffu) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+__host__ __device__ constexpr uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return (addr >> 4 & 0x3fffu) | (lbo >> 4 & 0x3fffu) << 16; }
+__host__ __device__ constexpr uint32_t desc_hi(uint32_t sbo) { return (sbo >> 4 & 0x3fffu) | 1u << 14 | 2u << 29; }
 // kind::f16 instruction descriptor: 32-bit accumulators, A K-major; `bf16` else f16, `b_mn` B is MN-major.
 __host__ __device__ constexpr uint32_t f16_idesc(uint32_t m, uint32_t n, bool bf16, bool b_mn)
 {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (b_mn ? 1u : 0u) << 16 | (n >> 3) << 17 | (m >> 4) << 24;
 }
-// d (tensor memory) = a b (+ d), a in shared memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// The instructions below are issued by one lane of a warp whose lanes all get here with the same operands: `on` is 1 in that
+// lane (see one_lane).  Kept out of a branch on the lane, the operands stay in uniform registers.
+__device__ __forceinline__ uint32_t one_lane()
+{
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on;
+}
+// d (tensor memory) = a b (+ d), a in shared memory.  Descriptors as low words; the high word is shared.
+__device__ __forceinline__ void mma_ss(uint32_t on, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 q, %0, 0;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+        "mov.b64 da, {%2, %4};\n\tmov.b64 db, {%3, %4};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%1], da, db, %5, p;\n\t}" ::"r"(on),
+        "r"(d), "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)add)
         : "memory");
 }
 // The same with a in tensor memory (two 16-bit elements a column).
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+__device__ __forceinline__ void mma_ts(uint32_t on, uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\tsetp.ne.u32 q, %0, 0;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+        "mov.b64 db, {%3, %4};\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], db, %5, p;\n\t}" ::"r"(on),
+        "r"(d), "r"(a), "r"(b), "r"(hi), "r"(idesc), "r"((uint32_t)add)
         : "memory");
 }
-// One arrival on `bar` once everything this thread has issued to the tensor core is done.
-__device__ __forceinline__ void tc_commit(uint32_t bar)
+// One arrival on `bar` once everything this lane has issued to the tensor core is done.
+__device__ __forceinline__ void tc_commit(uint32_t on, uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %0, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}" ::"r"(on),
+        "r"(bar)
+        : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
