@@ -9,7 +9,7 @@
 // (128-token steps with one buffer a slot: 976 us for 2,048 new tokens over 16k, the softmax waiting 40 % of the time.)
 // O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
 // are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
-// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 216 registers a thread.  Warp 8 issues the
+// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 200 registers a thread.  Warp 8 issues the
 // products, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
 // a box; warp 10 deals out the items (a ring of descriptors in shared memory); Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the softmax threads copy it).
 // Tensor memory: 2 x 2 S buffers of 64 columns, O0 O1 (D each) = 512 columns at D = 128, hence P over S.
@@ -98,23 +98,20 @@ __device__ __forceinline__ uint4 with_sign(uint4 v, uint32_t flip, uint32_t keep
 __device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 // A wait that every role uses: bounded, and cut short when another role has given up.
-__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t *abort, unsigned long long *status)
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t *abort, unsigned long long *status)
 {
-    for (uint32_t n = 0; n < 4096; ++n) {
-        if (mbar_try(bar, parity)) return true;
-        if ((n & 63u) == 63u && *abort) return false;
-    }
     const uint64_t end = now_ns() + kWaitLimitNs;
-    for (uint32_t n = 0; n < (1u << 28); ++n) {
-        if (mbar_try(bar, parity)) return true;
-        if ((n & 63u) == 63u) {
-            if (*abort) return false;
-            if (now_ns() > end) break;
-        }
+    for (uint32_t n = 0; n < (1u << 24) && now_ns() <= end; ++n) {
+        if (mbar_spin(bar, parity, 256)) return true;
+        if (*abort) return false;
     }
     *abort = 1;
     if (status) atomicOr(status, (unsigned long long)GMS_DEV_TIMEOUT);
     return false;
+}
+__device__ __forceinline__ bool wait_or_abort(uint32_t bar, uint32_t parity, volatile uint32_t *abort, unsigned long long *status)
+{
+    return mbar_spin(bar, parity, 4096) || wait_slow(bar, parity, abort, status);
 }
 
 template <class T, int D>
@@ -182,10 +179,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         }
     }
 
-    // 384 threads x 168 registers = 128 x 72 + 256 x 216
+    // 384 threads x 168 registers = 128 x 104 + 256 x 200
     uint32_t seg = 0;  // segments seen
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 10) {
         // ------------------------------------------------------------------ items
         if (lane == 0)
@@ -260,81 +257,116 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     } else if (warp == 8) {
         // ------------------------------------------------------------------ products
         constexpr uint32_t id_s = f16_idesc(128, 64, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
-        uint32_t n = 0, steps[2] = {0, 0}, items[2] = {0, 0};  // stages of finished segments; steps and segments of each slot
-        bool ok = true;
-        auto wait = [&](uint32_t bar, uint32_t parity) {  // the whole warp waits and issues as one
-            ok = __all_sync(0xffffffffu, ok && wait_or_abort(bar, parity, abort, a.status));
-        };
+        // Straight-line code a tile: this warp competes for issue with two softmax warps, every instruction counts.
+#define GMS_WAIT(bar, parity) \
+    if (!mbar_spin(bar, parity, 4096) && !wait_slow(bar, parity, abort, a.status)) goto products_done
         const uint32_t on = one_lane();
-        constexpr uint32_t hi = desc_hi(1024);
+        constexpr uint32_t hi = desc_hi(1024), half_k = 64 * 128 >> 4, half_v = 4 * 2048 >> 4;
         const uint32_t q_lo = desc_lo(q_smem, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
-        int nt = 0, last_slot = 0;
-        // S of step i of the segment (tile i / 2, its half i % 2)
-        auto scores = [&](int slot, int i) {
-            const uint32_t st = (n + 2 * (i >> 1)) % NS, half = i & 1, idx = n + 2 * (i >> 1);
-            if (half == 0) wait(full + 8 * st, (idx / NS) & 1u);
-            if (i >= 2) wait(o_done + 8 * (2 * slot + half), (((steps[slot] + i) >> 1) - 1) & 1u);  // P of step i - 2 lies in this buffer
-            if (!ok) return;
-            tc_fence_after();
-            const uint32_t kt = k_lo + ((st * F::kTileBytes + half * 64 * 128) >> 4), qt = q_lo + (slot * F::kTileBytes >> 4);
+        // S of one half of a K tile (k: its descriptor) into the slot's buffer `b`
+        auto scores = [&](int slot, int b, uint32_t k) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
-                mma_ss(on, tmem + slot * 128 + half * 64, qt + off, kt + off, hi, id_s, kk > 0);
+                mma_ss(on, tmem + slot * 128 + b * 64, q_lo + (slot * F::kTileBytes >> 4) + off, k + b * half_k + off, hi, id_s, kk > 0);
             }
-            tc_commit(on, s_full + 8 * (2 * slot + half));
-            if (half && slot == last_slot) tc_commit(on, empty + 8 * st);
-            if (i + 1 == 2 * nt) tc_commit(on, q_empty + 8 * slot);
+            tc_commit(on, s_full + 8 * (2 * slot + b));
         };
-        auto values = [&](int slot, int i) {
-            const uint32_t idx = n + 2 * (i >> 1) + 1, st = idx % NS, half = i & 1;
-            if (half == 0) wait(full + 8 * st, (idx / NS) & 1u);
-            wait(p_full + 8 * (2 * slot + half), ((steps[slot] + i) >> 1) & 1u);
-            if (!ok) return;
-            tc_fence_after();
-            const uint32_t vt = v_lo + ((st * F::kTileBytes + half * 4 * 2048) >> 4);
+        auto values = [&](int slot, int b, uint32_t v, bool add) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-                mma_ts(on, tmem + F::kO + slot * D, tmem + slot * 128 + half * 64 + kk * 8, vt + (kk * 2048 >> 4), hi, id_o, i > 0 || kk > 0);
-            tc_commit(on, o_done + 8 * (2 * slot + half));
-            if (half && slot == last_slot) tc_commit(on, empty + 8 * st);
+                mma_ts(on, tmem + F::kO + slot * D, tmem + slot * 128 + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o,
+                       add || kk > 0);
+            tc_commit(on, o_done + 8 * (2 * slot + b));
         };
-        for (; ok; ++seg) {
-            wait(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
-            if (!ok) break;
+        uint32_t ks = 0, kph = 0;            // stage of the next K tile (V follows it) and its phase
+        uint32_t t0 = 0, t1 = 0, i0 = 0, i1 = 0;  // tiles and items of each slot so far (low bits count)
+        for (;; ++seg) {
+            GMS_WAIT(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
             const Segment &g = segs[seg % kSegments];
-            last_slot = __shfl_sync(0xffffffffu, g.rows > 128, 0);
-            nt = g.k1 - g.k0;
+            const bool two = __shfl_sync(0xffffffffu, g.rows, 0) > 128;
+            const int nt = __shfl_sync(0xffffffffu, g.k1 - g.k0, 0);
             __syncwarp();
             if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
             if (nt == 0) break;
-#pragma unroll
-            for (int slot = 0; slot < 2; ++slot) {
-                if (slot > last_slot) continue;
-                wait(q_full + 8 * slot, items[slot] & 1u);
-                for (int b = 0; b < 2 && steps[slot]; ++b)  // the last item's P V: both buffers are free
-                    wait(o_done + 8 * (2 * slot + b), ((steps[slot] >> 1) - 1) & 1u);
-                scores(slot, 0);
+            uint32_t k = k_lo + (ks * F::kTileBytes >> 4);
+            GMS_WAIT(full + 8 * ks, kph);
+            GMS_WAIT(q_full, i0 & 1u);
+            GMS_WAIT(o_done, (t0 & 1u) ^ 1u);  // P V of the last item: its buffers are free
+            GMS_WAIT(o_done + 8, (t0 & 1u) ^ 1u);
+            tc_fence_after();
+            scores(0, 0, k);
+            if (two) {
+                GMS_WAIT(q_full + 8, i1 & 1u);
+                GMS_WAIT(o_done + 16, (t1 & 1u) ^ 1u);
+                GMS_WAIT(o_done + 24, (t1 & 1u) ^ 1u);
+                tc_fence_after();
+                scores(1, 0, k);
             }
-            scores(0, 1);
-            for (int i = 0; ok && i < 2 * nt; ++i) {
-                values(0, i);
-                if (last_slot) {
-                    if (i + 1 < 2 * nt) scores(1, i + 1);
-                    values(1, i);
+            scores(0, 1, k);
+            if (nt == 1) tc_commit(on, q_empty);
+            for (int j = 0; j < nt; ++j) {
+                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4), kold = ks, vph = kph;
+                const bool more = j + 1 < nt;
+                const uint32_t know = k;
+                ks += 2;
+                if (ks == NS) ks = 0, kph ^= 1u;
+                k = k_lo + (ks * F::kTileBytes >> 4);
+                GMS_WAIT(full + 8 * vs, vph);
+                GMS_WAIT(p_full, t0 & 1u);
+                tc_fence_after();
+                values(0, 0, v, j > 0);
+                if (two) {
+                    if (j) GMS_WAIT(o_done + 24, (t1 & 1u) ^ 1u);
+                    scores(1, 1, know);
+                    tc_commit(on, empty + 8 * kold);
+                    if (!more) tc_commit(on, q_empty + 8);
+                    GMS_WAIT(p_full + 16, t1 & 1u);
+                    tc_fence_after();
+                    values(1, 0, v, j > 0);
+                } else {
+                    tc_commit(on, empty + 8 * kold);
                 }
-                if (i + 2 < 2 * nt) scores(0, i + 2);
+                if (more) {
+                    GMS_WAIT(full + 8 * ks, kph);
+                    GMS_WAIT(o_done, t0 & 1u);
+                    tc_fence_after();
+                    scores(0, 0, k);
+                }
+                GMS_WAIT(p_full + 8, t0 & 1u);
+                tc_fence_after();
+                values(0, 1, v, true);
+                if (two) {
+                    if (more) {
+                        GMS_WAIT(o_done + 16, t1 & 1u);
+                        tc_fence_after();
+                        scores(1, 0, k);
+                    }
+                    GMS_WAIT(p_full + 24, t1 & 1u);
+                    tc_fence_after();
+                    values(1, 1, v, true);
+                    ++t1;
+                }
+                tc_commit(on, empty + 8 * vs);
+                if (more) {
+                    GMS_WAIT(o_done + 8, t0 & 1u);
+                    tc_fence_after();
+                    scores(0, 1, k);
+                    if (j + 2 == nt) tc_commit(on, q_empty);
+                }
+                ++t0;
             }
-            steps[0] += 2 * nt, ++items[0];
-            if (last_slot) steps[1] += 2 * nt, ++items[1];
-            n += 2 * nt;
+            ++i0;
+            if (two) ++i1;
         }
+    products_done:
+#undef GMS_WAIT
         tc_commit(on, drain);  // nothing of this warp's is in flight when the CTA ends
         (void)mbar_wait(drain, 0);
         __syncwarp();
     }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ------------------------------------------------------------------ softmax, one thread a row
         const int slot = (int)warp / 4, row_in = (int)(warp % 4) * 32 + (int)lane, row = slot * 128 + row_in;
         const uint32_t lanes = ((warp % 4) * 32) << 16;
@@ -344,7 +376,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         uint32_t n = 0, tiles = 0;  // tiles of all segments so far; of this slot
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            ok = __all_sync(0xffffffffu, ok && wait_or_abort(bar, parity, abort, a.status));
+            if (!__all_sync(0xffffffffu, mbar_spin(bar, parity, 4096)))
+                ok = __all_sync(0xffffffffu, wait_slow(bar, parity, abort, a.status));
             return ok;
         };
         for (;; ++seg) {
@@ -419,12 +452,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                                 if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
                         }
                     }
-                    float top = neg_inf();
+                    float tops[4];  // four chains
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(s[i / 2][(i % 2) * 16]);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(s[i][j]));
-                    top *= c2;
+                    for (int j = 1; j < 16; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + j]));
+                    const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), neg_inf()) * c2;
                     const bool grow = top > m + kLag || (m == neg_inf() && top != m);
                     if (__any_sync(0xffffffffu, grow)) {
                         const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
@@ -445,17 +480,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                         }
                     }
                     const float z = m == neg_inf() ? 0.f : m;
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     uint32_t pk[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        const float x0 = ex2(fmaf(__uint_as_float(s[j / 16][(j * 2) % 32]), c2, -z));
-                        const float x1 = ex2(fmaf(__uint_as_float(s[j / 16][(j * 2 + 1) % 32]), c2, -z));
-                        part[j & 3] += x0 + x1;
-                        pk[j] = pack2(x0, x1, T());
+                        float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
+                        x = fma2(x, cc, zz);
+                        x.x = ex2(x.x);
+                        x.y = ex2(x.y);
+                        part[j & 1] = add2(part[j & 1], x);
+                        pk[j] = pack2(x.x, x.y, T());
                     }
                     tmem_st32(s_at, pk);
-                    l += (part[0] + part[1]) + (part[2] + part[3]);
+                    part[0] = add2(part[0], part[1]);
+                    l += part[0].x + part[0].y;
                     // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
                     // of the unit sees, where rows are not done again (slot 0's thread r clears token r of the tile before its
                     // first half is handed over; slot 1's product comes after slot 0's).

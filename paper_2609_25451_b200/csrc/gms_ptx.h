@@ -43,21 +43,51 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
+// Tries for a phase up to `tries` times (a try suspends the thread for a while by itself).
+__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, uint32_t tries)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+        "AGAIN:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, %3;\n\t@q bra AGAIN;\n"
+        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(tries)
+        : "memory");
+    return ok != 0;
+}
 // Waits for a phase; false once the limit has passed.  The clock is looked at after the first few thousand tries only.
 static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity)
 {
-    for (uint32_t n = 0; n < 4096; ++n)
-        if (mbar_try(bar, parity)) return true;
     const uint64_t end = now_ns() + kWaitLimitNs;
-    for (uint32_t n = 0; n < (1u << 28); ++n) {
-        if (mbar_try(bar, parity)) return true;
-        if ((n & 255u) == 255u && now_ns() > end) return false;
+    for (uint32_t n = 0; n < (1u << 24); ++n) {
+        if (mbar_spin(bar, parity, 256)) return true;
+        if (now_ns() > end) return false;
     }
     return false;
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
 {
-    return mbar_try(bar, parity) || mbar_wait_slow(bar, parity);
+    return mbar_spin(bar, parity, 4096) || mbar_wait_slow(bar, parity);
+}
+// Two 32-bit sums or products at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *m)
