@@ -9,8 +9,8 @@
 // (128-token steps with one buffer a slot: 976 us for 2,048 new tokens over 16k, the softmax waiting 40 % of the time.)
 // O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
 // are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
-// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 200 registers a thread.  Warp 8 issues the
-// products, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
+// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 200 registers a thread.  Warps 8 and 11
+// issue the products of slots 0 and 1, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
 // a box; warp 10 deals out the items (a ring of descriptors in shared memory); Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the softmax threads copy it).
 // Tensor memory: 2 x 2 S buffers of 64 columns, O0 O1 (D each) = 512 columns at D = 128, hence P over S.
 // Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
@@ -30,7 +30,7 @@ constexpr float kLag = 8.f;  // log2 of how far a maximum may have grown before 
 struct Segment {
     const int32_t *table;
     int q0, row0, rows, n, first, pos_min, pos_max, n_sink_tiles, first_tile, tiles, k0, k1;
-    uint32_t c, item, whole, pad;
+    uint32_t c, item, whole, holes;
 };
 constexpr uint32_t kSegments = 4;
 
@@ -70,7 +70,7 @@ __device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, W
     w.pos += (uint32_t)(g.k1 - g.k0);
     return true;
 }
-__device__ __forceinline__ int seg_tile(const volatile Segment &g, int k)
+__device__ __forceinline__ int seg_tile(const Segment &g, int k)
 {
     return k < g.n_sink_tiles ? k : g.first_tile + k - g.n_sink_tiles;
 }
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     volatile uint32_t *abort = shared_words + 1;
     Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
     if (tid == 0) {
-        for (int i = 0; i < NS; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, 1);
+        for (int i = 0; i < NS; ++i) mbar_init(full + 8 * i, 1), mbar_init(empty + 8 * i, 2);  // both product warps
         for (int i = 0; i < 2; ++i) {
             mbar_init(q_full + 8 * i, q_tma ? 1 : 128);
             mbar_init(q_empty + 8 * i, 1);
@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 mbar_init(o_done + 8 * (2 * i + b), 1);
             }
         }
-        mbar_init(drain, 1);
-        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_empty + 8 * i, 10);  // 8 softmax warps, 2 more
+        mbar_init(drain, 2);
+        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_empty + 8 * i, 11);  // 8 softmax warps, 3 more
         *abort = 0;
         fence_mbar_init();
         tma_prefetch_map(&kmap);
@@ -185,15 +185,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 10) {
         // ------------------------------------------------------------------ items
-        if (lane == 0)
-            for (bool more = true; more; ++seg) {
-                const uint32_t at = seg % kSegments;
-                if (!wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status)) break;
-                Segment g;
-                more = next_segment(a, p, w, g);
+        for (bool more = true; more; ++seg) {
+            const uint32_t at = seg % kSegments;
+            if (!__all_sync(0xffffffffu, wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status))) break;
+            Segment g;
+            more = next_segment(a, p, w, g);
+            if (more) {  // whether any id of its tiles lies outside the pool (then the softmax looks at every tile's)
+                bool hole = false;
+                const int t_end = min(g.n, (seg_tile(g, g.k1 - 1) + 1) * kTile), step = 1 << a.block_shift;
+                for (int k = g.k0; k < min(g.k1, g.n_sink_tiles); ++k)
+                    for (int t = k * kTile + (int)lane * step; t < (k + 1) * kTile; t += 32 * step)
+                        hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
+                for (int t = (seg_tile(g, max(g.k0, g.n_sink_tiles)) * kTile & ~(step - 1)) + (int)lane * step; t < t_end; t += 32 * step)
+                    hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
+                g.holes = __any_sync(0xffffffffu, hole);
+            }
+            if (lane == 0) {
                 segs[at] = g;
                 mbar_arrive(seg_full + 8 * at);
             }
+        }
         __syncwarp();
     } else if (warp == 9) {
         // ------------------------------------------------------------------ loads
@@ -254,110 +265,90 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             for (uint32_t i = n > (uint32_t)NS ? n - NS : 0; i < n; ++i) (void)mbar_wait(full + 8 * (i % NS), (i / NS) & 1u);
         for (int slot = 0; !ok && slot < 2; ++slot)
             if (q_n[slot]) (void)mbar_wait(q_full + 8 * slot, (q_n[slot] - 1) & 1u);
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------ products
+    } else {
+        // ------------------------------------------------------------------ products of one slot (warp 8: slot 0, warp 11: slot 1)
         constexpr uint32_t id_s = f16_idesc(128, 64, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
-        // Straight-line code a tile: this warp competes for issue with two softmax warps, every instruction counts.
+        // Straight-line code a tile: these warps compete for issue with two softmax warps each, every instruction counts.
 #define GMS_WAIT(bar, parity) \
     if (!mbar_spin(bar, parity, 4096) && !wait_slow(bar, parity, abort, a.status)) goto products_done
-        const uint32_t on = one_lane();
+        const uint32_t on = one_lane(), slot = warp == 8 ? 0u : 1u;
         constexpr uint32_t hi = desc_hi(1024), half_k = 64 * 128 >> 4, half_v = 4 * 2048 >> 4;
-        const uint32_t q_lo = desc_lo(q_smem, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
-        // S of one half of a K tile (k: its descriptor) into the slot's buffer `b`
-        auto scores = [&](int slot, int b, uint32_t k) {
+        const uint32_t q_lo = desc_lo(q_smem + slot * F::kTileBytes, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
+        const uint32_t s_tm = tmem + slot * 128, o_tm = tmem + F::kO + slot * D;
+        const uint32_t my_s = s_full + 16 * slot, my_p = p_full + 16 * slot, my_o = o_done + 16 * slot, my_q = 8 * slot;
+        // S of one half of a K tile (k: its descriptor) into buffer b
+        auto scores = [&](int b, uint32_t k) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
-                mma_ss(on, tmem + slot * 128 + b * 64, q_lo + (slot * F::kTileBytes >> 4) + off, k + b * half_k + off, hi, id_s, kk > 0);
+                mma_ss(on, s_tm + b * 64, q_lo + off, k + b * half_k + off, hi, id_s, kk > 0);
             }
-            tc_commit(on, s_full + 8 * (2 * slot + b));
+            tc_commit(on, my_s + 8 * b);
         };
-        auto values = [&](int slot, int b, uint32_t v, bool add) {
+        auto values = [&](int b, uint32_t v, bool add) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-                mma_ts(on, tmem + F::kO + slot * D, tmem + slot * 128 + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o,
-                       add || kk > 0);
-            tc_commit(on, o_done + 8 * (2 * slot + b));
+            for (int kk = 0; kk < 4; ++kk) mma_ts(on, o_tm, s_tm + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o, add || kk > 0);
+            tc_commit(on, my_o + 8 * b);
         };
-        uint32_t ks = 0, kph = 0;            // stage of the next K tile (V follows it) and its phase
-        uint32_t t0 = 0, t1 = 0, i0 = 0, i1 = 0;  // tiles and items of each slot so far (low bits count)
+        uint32_t ks = 0, kph = 0;       // stage of the next K tile (V follows it) and its phase
+        uint32_t tiles = 0, items = 0;  // of this slot so far (low bits count)
         for (;; ++seg) {
             GMS_WAIT(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
             const Segment &g = segs[seg % kSegments];
-            const bool two = __shfl_sync(0xffffffffu, g.rows, 0) > 128;
+            const bool mine = slot == 0 || __shfl_sync(0xffffffffu, g.rows, 0) > 128;
             const int nt = __shfl_sync(0xffffffffu, g.k1 - g.k0, 0);
             __syncwarp();
             if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
             if (nt == 0) break;
+            if (!mine) {  // no rows here: only hand the stages back
+                for (int j = 0; j < 2 * nt; ++j) {
+                    GMS_WAIT(full + 8 * ks, kph);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(empty + 8 * ks);
+                    if (++ks == NS) ks = 0, kph ^= 1u;
+                }
+                continue;
+            }
             uint32_t k = k_lo + (ks * F::kTileBytes >> 4);
             GMS_WAIT(full + 8 * ks, kph);
-            GMS_WAIT(q_full, i0 & 1u);
-            GMS_WAIT(o_done, (t0 & 1u) ^ 1u);  // P V of the last item: its buffers are free
-            GMS_WAIT(o_done + 8, (t0 & 1u) ^ 1u);
+            GMS_WAIT(q_full + my_q, items & 1u);
+            GMS_WAIT(my_o, (tiles & 1u) ^ 1u);  // P V of the last item: its buffers are free
+            GMS_WAIT(my_o + 8, (tiles & 1u) ^ 1u);
             tc_fence_after();
-            scores(0, 0, k);
-            if (two) {
-                GMS_WAIT(q_full + 8, i1 & 1u);
-                GMS_WAIT(o_done + 16, (t1 & 1u) ^ 1u);
-                GMS_WAIT(o_done + 24, (t1 & 1u) ^ 1u);
-                tc_fence_after();
-                scores(1, 0, k);
-            }
-            scores(0, 1, k);
-            if (nt == 1) tc_commit(on, q_empty);
+            scores(0, k);
+            scores(1, k);
+            tc_commit(on, empty + 8 * ks);
+            if (nt == 1) tc_commit(on, q_empty + my_q);
             for (int j = 0; j < nt; ++j) {
-                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4), kold = ks, vph = kph;
+                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4), vph = kph;
                 const bool more = j + 1 < nt;
-                const uint32_t know = k;
                 ks += 2;
                 if (ks == NS) ks = 0, kph ^= 1u;
                 k = k_lo + (ks * F::kTileBytes >> 4);
                 GMS_WAIT(full + 8 * vs, vph);
-                GMS_WAIT(p_full, t0 & 1u);
+                GMS_WAIT(my_p, tiles & 1u);
                 tc_fence_after();
-                values(0, 0, v, j > 0);
-                if (two) {
-                    if (j) GMS_WAIT(o_done + 24, (t1 & 1u) ^ 1u);
-                    scores(1, 1, know);
-                    tc_commit(on, empty + 8 * kold);
-                    if (!more) tc_commit(on, q_empty + 8);
-                    GMS_WAIT(p_full + 16, t1 & 1u);
-                    tc_fence_after();
-                    values(1, 0, v, j > 0);
-                } else {
-                    tc_commit(on, empty + 8 * kold);
-                }
+                values(0, v, j > 0);
                 if (more) {
                     GMS_WAIT(full + 8 * ks, kph);
-                    GMS_WAIT(o_done, t0 & 1u);
+                    GMS_WAIT(my_o, tiles & 1u);
                     tc_fence_after();
-                    scores(0, 0, k);
+                    scores(0, k);
                 }
-                GMS_WAIT(p_full + 8, t0 & 1u);
+                GMS_WAIT(my_p + 8, tiles & 1u);
                 tc_fence_after();
-                values(0, 1, v, true);
-                if (two) {
-                    if (more) {
-                        GMS_WAIT(o_done + 16, t1 & 1u);
-                        tc_fence_after();
-                        scores(1, 0, k);
-                    }
-                    GMS_WAIT(p_full + 24, t1 & 1u);
-                    tc_fence_after();
-                    values(1, 1, v, true);
-                    ++t1;
-                }
+                values(1, v, true);
                 tc_commit(on, empty + 8 * vs);
                 if (more) {
-                    GMS_WAIT(o_done + 8, t0 & 1u);
+                    GMS_WAIT(my_o + 8, tiles & 1u);
                     tc_fence_after();
-                    scores(0, 1, k);
-                    if (j + 2 == nt) tc_commit(on, q_empty);
+                    scores(1, k);
+                    tc_commit(on, empty + 8 * ks);
+                    if (j + 2 == nt) tc_commit(on, q_empty + my_q);
                 }
-                ++t0;
+                ++tiles;
             }
-            ++i0;
-            if (two) ++i1;
+            ++items;
         }
     products_done:
 #undef GMS_WAIT
@@ -418,106 +409,105 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             auto low_of = [&](int ps) { return all || a.window == 0 || (uint32_t)max(ps, 0) < a.window ? 0 : ps - (int)a.window + 1; };
             const int low = low_of(pos), low_hi = low_of(pos_hi), sink = (int)min(a.sinks, 0x7fffffffu);
             float m = neg_inf(), l = 0.f;
-            int id_next = -1;
-            auto tile_id = [&](int k) -> int {  // the block of each 16 tokens of the tile, one lane each
-                const int t = seg_tile(g, k) * kTile + (int)lane * 16;
-                return lane < 8 && t < len ? table[(uint32_t)t >> a.block_shift] : -1;
-            };
-            id_next = tile_id(k0);
-            for (int k = k0; k < k1; ++k) {
-                const int t0 = seg_tile(g, k) * kTile;
-                const uint32_t valid = __ballot_sync(0xffffffffu, (uint32_t)id_next < a.n_blocks) & 0xffu;
-                if (k + 1 < k1) id_next = tile_id(k + 1);
-                const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo && (t0 >= low_hi || t0 + kTile - 1 < sink);
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t s_at = s_col + half * 64;
-                    if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) break;
-                    tc_fence_after();
-                    uint32_t s[2][32];
+            const int n_sink_tiles = g.n_sink_tiles, past_sinks = g.first_tile - n_sink_tiles;
+            const bool holes = g.holes != 0;
+            // One step: 64 columns of S to P.
+            auto step = [&](int half, int k, int t0, bool whole, uint32_t valid) {
+                if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) return;
+                tc_fence_after();
+                uint32_t s[2][32];
+                tmem_ld32(s_col + half * 64, s[0]);
+                tmem_ld32(s_col + half * 64 + 32, s[1]);
+                tmem_wait32(s[0]);
+                tmem_wait32(s[1]);
+                if (!whole) {
+                    const uint32_t v4 = valid >> (4 * half);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) tmem_ld32(s_at + i * 32, s[i]);
+                    for (int i = 0; i < 2; ++i) {
+                        const int c0 = t0 + half * 64 + i * 32;
+                        const uint32_t held = ((v4 >> (2 * i) & 1u) ? 0xffffu : 0u) | ((v4 >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
+                        const uint32_t on = held & first_bits(pos + 1 - c0) & (~first_bits(low - c0) | first_bits(sink - c0));
+                        if (__all_sync(0xffffffffu, on == 0xffffffffu)) continue;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) tmem_wait32(s[i]);
-                    if (!whole) {
-                        const uint32_t v4 = valid >> (4 * half);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int c0 = t0 + half * 64 + i * 32;
-                            const uint32_t held = ((v4 >> (2 * i) & 1u) ? 0xffffu : 0u) | ((v4 >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
-                            const uint32_t on = held & first_bits(pos + 1 - c0) & (~first_bits(low - c0) | first_bits(sink - c0));
-                            if (__all_sync(0xffffffffu, on == 0xffffffffu)) continue;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
-                        }
+                        for (int j = 0; j < 32; ++j)
+                            if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
                     }
-                    float tops[4];  // four chains
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(s[i / 2][(i % 2) * 16]);
-#pragma unroll
-                    for (int j = 1; j < 16; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + j]));
-                    const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), neg_inf()) * c2;
-                    const bool grow = top > m + kLag || (m == neg_inf() && top != m);
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
-                        if (grow) m = top;
-                        l *= f;
-                        if (k != k0 || half) {
-                            if (!wait(o_done + 8 * (2 * slot + (half ^ 1)), (tiles + (half ^ 1)) & 1u)) break;  // O is at rest until this step's P is handed over
-                            tc_fence_after();
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {
-                                uint32_t o[32];
-                                tmem_ld32(o_col + i * 32, o);
-                                tmem_wait32(o);
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                                tmem_st32(o_col + i * 32, o);
-                            }
-                        }
-                    }
+                }
+                // The exponentials are taken against the maximum so far while this step's own is being found; only if a row's has
+                // outgrown it by more than kLag (or it has none yet) are they taken again.
+                uint32_t pk[32];
+                float2 part[2];
+                for (;;) {
                     const float z = m == neg_inf() ? 0.f : m;
                     const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
-                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t pk[32];
+                    part[0] = part[1] = make_float2(0.f, 0.f);
+                    float tops[2] = {neg_inf(), neg_inf()};
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
+                        tops[j & 1] = fmaxf(tops[j & 1], fmaxf(x.x, x.y));
                         x = fma2(x, cc, zz);
                         x.x = ex2(x.x);
                         x.y = ex2(x.y);
                         part[j & 1] = add2(part[j & 1], x);
                         pk[j] = pack2(x.x, x.y, T());
                     }
-                    tmem_st32(s_at, pk);
-                    part[0] = add2(part[0], part[1]);
-                    l += part[0].x + part[0].y;
-                    // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
-                    // of the unit sees, where rows are not done again (slot 0's thread r clears token r of the tile before its
-                    // first half is handed over; slot 1's product comes after slot 0's).
-                    if (slot == 0 && half == 0 && !whole) {
-                        const int t = t0 + row_in;
-                        const bool none = t >= len || (!p.again && (t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t))));
-                        if (__any_sync(0xffffffffu, none)) {
-                            const uint32_t vs = 2 * n + 1;
-                            if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) break;
-                            if (none)
+                    const float top = fmaxf(tops[0], tops[1]) * c2;
+                    const bool grow = top > m + kLag || (m == neg_inf() && top != m);
+                    if (!__any_sync(0xffffffffu, grow)) break;
+                    const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
+                    if (grow) m = top;
+                    l *= f;
+                    if (k != k0 || half) {  // O is at rest between the last step's product and this step's handing over
+                        if (!wait(o_done + 8 * (2 * slot + (half ^ 1)), (tiles + (half ^ 1)) & 1u)) return;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t o[32];
+                            tmem_ld32(o_col + i * 32, o);
+                            tmem_wait32(o);
 #pragma unroll
-                                for (int h = 0; h < F::kHalves; ++h)
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
-                            fence_proxy_async();
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                            tmem_st32(o_col + i * 32, o);
                         }
                     }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(p_full + 8 * (2 * slot + half));
                 }
-                if (!ok) break;
+                tmem_st32(s_col + half * 64, pk);
+                part[0] = add2(part[0], part[1]);
+                l += part[0].x + part[0].y;
+                // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
+                // of the unit sees, where rows are not done again.  Thread r of each slot clears token r of the tile before
+                // its slot's first half is handed over (the other slot may clear it too: the same zeros).
+                if (half == 0 && !whole) {
+                    const int t = t0 + row_in;
+                    const bool none = t >= len || (!p.again && (t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t))));
+                    if (__any_sync(0xffffffffu, none)) {
+                        const uint32_t vs = 2 * n + 1;
+                        if (!wait(full + 8 * (vs % NS), (vs / NS) & 1u)) return;
+                        if (none)
+#pragma unroll
+                            for (int h = 0; h < F::kHalves; ++h)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
+                        fence_proxy_async();
+                    }
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(p_full + 8 * (2 * slot + half));
+            };
+            for (int k = k0; ok && k < k1; ++k) {
+                const int t0 = (k < n_sink_tiles ? k : past_sinks + k) * kTile;
+                uint32_t valid = 0xffu;
+                if (holes) {  // the block of each 16 tokens of the tile, one lane each
+                    const int t = t0 + (int)lane * 16;
+                    const int id = lane < 8 && t < len ? table[(uint32_t)t >> a.block_shift] : -1;
+                    valid = __ballot_sync(0xffffffffu, (uint32_t)id < a.n_blocks) & 0xffu;
+                }
+                const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo && (t0 >= low_hi || t0 + kTile - 1 < sink);
+#pragma unroll 1
+                for (int half = 0; ok && half < 2; ++half) step(half, k, t0, whole, valid);
                 ++n;
                 ++tiles;
             }
