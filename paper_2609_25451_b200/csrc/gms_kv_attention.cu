@@ -254,7 +254,7 @@ uint64_t most_tiles(const AttnArgs &a, const Pass &p)
         const uint64_t seen = (uint64_t)a.window + a.sinks + 2 * p.tile + (p.rows - 1) / a.group;
         if (seen < span) span = seen;
     }
-    return p.n_units * (uint64_t)a.n_kv * ceil_div(span, p.tile);
+    return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * ceil_div(span, p.tile);
 }
 
 void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
@@ -267,11 +267,13 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     p->tile = tc ? kTcTile : kFewTile;
     p->n_rt = (uint32_t)ceil_div(rows, p->rows);
     if (p->n_rt == 0) p->n_rt = 1;
-    p->n_units = (prefix ? a.n_groups : a.n_seq) * p->n_rt;
+    const uint64_t units = (uint64_t)(prefix ? a.n_groups : a.n_seq) * p->n_rt;
+    p->n_units = (uint32_t)(units < 0xffffffffull ? units : 0xffffffffull);  // too many: most_tiles refuses them
     // as many CTAs as the SMs hold; fewer where they would have fewer than eight tiles of 16 tokens (two a warp), or two of 128
     const uint64_t want = ceil_div(most_tiles(a, *p), tc ? 2 : 8), most = tc ? kTcMaxCtas : kFewMaxCtas;
     p->n_cta = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
-    p->begin = c->take<uint64_t>(p->n_units + 1);
+    if (rows_out) p->begin = c->take<uint32_t>(p->n_units + 1);
+    p->cuts = c->take<Cut>(p->n_cta);
     p->part_ml = c->take<float2>(2ull * p->n_cta * p->rows);
     p->part_o = c->take<float>(2ull * p->n_cta * p->rows * head_dim);
     if (rows_out) {
@@ -282,7 +284,7 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     if (tc && p->again && !rows_out) p->redo = c->take<uint32_t>((uint64_t)p->n_units * a.n_kv * (kTcRows / 32));
 }
 
-void plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace, Plan *pl, uint64_t *bytes)
+int plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace, Plan *pl, uint64_t *bytes)
 {
     *pl = {};
     Carve c{static_cast<uint8_t *>(workspace)};
@@ -299,6 +301,9 @@ void plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspac
         }
     }
     *bytes = c.used;
+    // the kernels count tiles in 31 bits
+    const bool fits = most_tiles(a, pl->own) >> 31 == 0 && (!shared || most_tiles(a, pl->prefix) >> 31 == 0);
+    return fits ? GMS_OK : GMS_ERR_RANGE;
 }
 
 int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *t, const gms_kv_weight *w,
@@ -309,7 +314,8 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
     if (rc != GMS_OK) return rc;
     Plan pl;
     uint64_t need = 0;
-    plan_call(a, layout->head_dim, x != nullptr, t->workspace, &pl, &need);
+    rc = plan_call(a, layout->head_dim, x != nullptr, t->workspace, &pl, &need);
+    if (rc != GMS_OK) return rc;
     if (a.n_seq == 0) return GMS_OK;
     if (!t->workspace) return GMS_ERR_NULL;
     if (need > t->workspace_bytes) return GMS_ERR_RANGE;
@@ -357,9 +363,9 @@ int gms_kv_attention_workspace(const gms_kv_pool *pool, const gms_kv_layout *lay
 {
     if (!nbytes) return GMS_ERR_NULL;
     gms::AttnArgs a;
-    const int rc = gms::make_args(pool, layout, attn, weight, nullptr, &a);
+    int rc = gms::make_args(pool, layout, attn, weight, nullptr, &a);
     gms::Plan plan;
-    if (rc == GMS_OK) gms::plan_call(a, layout->head_dim, false, nullptr, &plan, nbytes);
+    if (rc == GMS_OK) rc = gms::plan_call(a, layout->head_dim, false, nullptr, &plan, nbytes);
     return rc;
 }
 
@@ -374,9 +380,9 @@ int gms_kv_attention_shared_workspace(const gms_kv_pool *pool, const gms_kv_layo
 {
     if (!nbytes || !prefix) return GMS_ERR_NULL;
     gms::AttnArgs a;
-    const int rc = gms::make_args(pool, layout, attn, nullptr, prefix, &a);
+    int rc = gms::make_args(pool, layout, attn, nullptr, prefix, &a);
     gms::Plan plan;
-    if (rc == GMS_OK) gms::plan_call(a, layout->head_dim, true, nullptr, &plan, nbytes);
+    if (rc == GMS_OK) rc = gms::plan_call(a, layout->head_dim, true, nullptr, &plan, nbytes);
     return rc;
 }
 

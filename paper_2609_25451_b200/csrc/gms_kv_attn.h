@@ -42,14 +42,20 @@ struct AttnArgs {
 // How a pass over cached tokens is cut.  A unit is a run of up to ROWS query rows (token-major, the heads of one KV head
 // inside a token) of one sequence (or, in a prefix pass, of one group); an item is a unit for one KV head; an item's work
 // is the list of token tiles that at least one of its rows sees.  All items' tiles, one after the other, are dealt out
-// evenly: CTA i of n (n = n_cta, or T if that is less) takes tiles [T*i/n, T*(i+1)/n), whatever items they fall into, so ragged lengths cost no balance.
-// An item that one CTA has whole is finished there; the at most two pieces a CTA has of others go to its two slots of
-// part_o / part_ml and are joined by kv_attn_join.
+// evenly: CTA i of n (n = n_cta, or T if that is less) gets T / n or T / n + 1 tiles, whatever items they fall into, so
+// ragged lengths cost no balance.  An item that one CTA has whole is finished there; the at most two pieces a CTA has of
+// others go to its two slots of part_o / part_ml and are joined by kv_attn_join.
+struct Cut {               // the item into which the border before CTA i falls (c1 = 0: the border lies between items)
+    int q0, row0, rows;
+    uint32_t c, c0, c1;    // KV head; first and last CTA that has a piece
+    uint32_t pad[2];
+};
 struct Pass {
     uint32_t prefix;       // 1: units are groups' query rows over their prefix, all of it seen
     uint32_t n_units, n_rt, n_cta;  // n_rt units a sequence (group)
     uint32_t rows, tile;   // rows a unit, tokens a tile
-    uint64_t *begin;       // [n_units + 1] tiles before each unit (written by CTA 0 for the join)
+    uint32_t *begin;       // null, or [n_units + 1] tiles before each unit (written by CTA 0 for those who look items up)
+    Cut *cuts;             // [n_cta], written by CTA i for its own border
     float *part_o;         // [2 * n_cta][rows][head_dim], not normalised
     float2 *part_ml;       // [2 * n_cta][rows]: running maximum (base 2) and sum
     float *row_o;          // null: finished rows go to out / lse; else [total_q * n_heads][head_dim], not normalised
@@ -209,92 +215,132 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
     }
     u.first = u.n - q_len;
     u.row0 = (int)rt * ROWS;
-    u.rows = (int)min(max((long long)q_len * a.group - u.row0, 0ll), (long long)ROWS);
+    u.rows = max(min(q_len * (int)a.group - u.row0, ROWS), 0);  // total_q * n_heads < 2^31
     u.n_sink_tiles = u.first_tile = u.tiles = 0;
     u.pos_min = u.pos_max = u.n - 1;
     if (u.rows > 0) {
         if (!u.whole) {
-            u.pos_min = u.first + u.row0 / (int)a.group;
-            u.pos_max = u.first + (u.row0 + u.rows - 1) / (int)a.group;
+            u.pos_min = u.first;
+            if (p.n_rt > 1) {
+                u.pos_min += u.row0 / (int)a.group;
+                u.pos_max = u.first + (u.row0 + u.rows - 1) / (int)a.group;
+            }
         }
         if (u.pos_max >= 0) {
-            int lo = 0;
-            if (!u.whole && a.window) lo = (int)max(0ll, (long long)u.pos_min - (long long)a.window + 1);
-            u.first_tile = lo / TILE;
-            u.n_sink_tiles = (int)min((long long)u.first_tile, ((long long)a.sinks + TILE - 1) / TILE);
+            if (!u.whole && a.window != 0 && u.pos_min >= 0 && (uint32_t)u.pos_min >= a.window) {
+                u.first_tile = (u.pos_min - (int)a.window + 1) / TILE;
+                u.n_sink_tiles = (int)min((uint32_t)u.first_tile, a.sinks / TILE + (a.sinks % TILE != 0));
+            }
             u.tiles = u.n_sink_tiles + u.pos_max / TILE + 1 - u.first_tile;
         }
     }
     return u;
 }
-// CTAs that get work: no share is empty, so a piece lies in every slot that the join looks at.
-__device__ __forceinline__ uint32_t used_ctas(uint64_t total, const Pass &p) { return (uint32_t)min(total, (uint64_t)p.n_cta); }
 // The part of the work that a CTA has, item by item.
 struct Walk {
-    uint64_t pos, end;   // tiles still to do, in the order over all items
-    uint64_t base;       // tiles before the current unit
+    uint32_t pos, end;   // tiles still to do, in the order over all items
+    uint32_t base;       // tiles before the current unit
     uint32_t s, rt;
+    uint32_t total, per, more;  // tiles in all; every share has `per`, the first `more` shares one more
 };
-// Scans all units, finds CTA `cta`'s share.  Every thread of the CTA calls it and gets the same result; `sh` is 8 * (warps + 3)
-// bytes of shared memory.  CTA 0 also writes p.begin.
+// CTAs that get work: no share is empty, so a piece lies in every slot that the join looks at.
+__device__ __forceinline__ uint32_t used_ctas(uint32_t total, uint32_t n_cta) { return min(total, n_cta); }
+// Which CTA's share holds tile t.
+__device__ __forceinline__ uint32_t tile_owner(uint32_t t, uint32_t per, uint32_t more)
+{
+    const uint32_t high = more * (per + 1);
+    return t < high ? t / (per + 1) : more + (t - high) / per;
+}
+// Scans all units (fewer than 2^31 tiles in all), finds CTA `cta`'s share.  Every thread of the CTA calls it and gets the
+// same result; `sh` is 4 * (warps + 2) bytes of shared memory.
 template <int ROWS, int TILE, int THREADS>
-__device__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint64_t *sh)
+__device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint32_t *sh)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
     const uint32_t per = (p.n_units + THREADS - 1) / THREADS, u0 = min(tid * per, p.n_units), u1 = min(u0 + per, p.n_units);
-    uint64_t mine = 0;
-#pragma unroll 4
-    for (uint32_t u = u0; u < u1; ++u) mine += (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
-    uint64_t inc = mine;
+    auto tiles_of = [&](uint32_t u) {
+        return (uint32_t)get_unit<ROWS, TILE>(a, p, p.n_rt > 1 ? u / p.n_rt : u, p.n_rt > 1 ? u % p.n_rt : 0).tiles * a.n_kv;
+    };
+    uint32_t mine = 0;
+    for (uint32_t u = u0; u < u1; ++u) mine += tiles_of(u);
+    uint32_t inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t x = __shfl_up_sync(0xffffffffu, inc, o);
+        const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= (uint32_t)o) inc += x;
     }
     if (lane == 31) sh[warp] = inc;
-    if (tid == 0) sh[THREADS / 32 + 1] = p.n_units;
     __syncthreads();
-    uint64_t before = inc - mine, total = 0;
+    uint32_t before = inc - mine;
+    Walk w;
+    w.total = 0;
 #pragma unroll
     for (uint32_t i = 0; i < THREADS / 32; ++i) {
         if (i < warp) before += sh[i];
-        total += sh[i];
+        w.total += sh[i];
     }
-    Walk w;
-    const uint32_t n = used_ctas(total, p);
-    w.pos = cta < n ? total * cta / n : total;
-    w.end = cta < n ? total * (cta + 1) / n : total;
-    if (mine && before <= w.pos && w.pos < before + mine) {
-        uint64_t b = before;
-        for (uint32_t u = u0; u < u1; ++u) {
-            const uint64_t t = (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
-            if (w.pos < b + t) {
-                sh[THREADS / 32] = b;
-                sh[THREADS / 32 + 1] = u;
-                break;
-            }
-            b += t;
-        }
+    const uint32_t n = used_ctas(w.total, p.n_cta);
+    w.pos = w.end = w.total;
+    w.per = w.more = 0;
+    if (cta < n) {
+        w.per = w.total / n;
+        w.more = w.total - w.per * n;
+        w.pos = cta * w.per + min(cta, w.more);
+        w.end = w.pos + w.per + (cta < w.more);
     }
-    if (cta == 0) {
-        uint64_t b = before;
+    if (w.pos - before < mine) {  // before <= pos < before + mine
+        uint32_t b = before, u = u0;
+        if (per > 1)
+            for (uint32_t t = tiles_of(u); w.pos - b >= t; t = tiles_of(++u)) b += t;
+        sh[THREADS / 32] = b;
+        sh[THREADS / 32 + 1] = u;
+    }
+    if (p.begin && cta == 0) {
+        uint32_t b = before;
         for (uint32_t u = u0; u < u1; ++u) {
             p.begin[u] = b;
-            b += (uint64_t)get_unit<ROWS, TILE>(a, p, u / p.n_rt, u % p.n_rt).tiles * a.n_kv;
+            b += tiles_of(u);
         }
-        if (tid == 0) p.begin[p.n_units] = total;
+        if (tid == 0) p.begin[p.n_units] = w.total;
     }
     __syncthreads();
-    w.base = sh[THREADS / 32];
-    const uint32_t u = (uint32_t)sh[THREADS / 32 + 1];
-    w.s = u / p.n_rt;
-    w.rt = u % p.n_rt;
+    w.base = w.s = w.rt = 0;
+    if (w.pos < w.end) {
+        w.base = sh[THREADS / 32];
+        const uint32_t u = sh[THREADS / 32 + 1];
+        w.s = p.n_rt > 1 ? u / p.n_rt : u;
+        w.rt = p.n_rt > 1 ? u % p.n_rt : 0;
+    }
     return w;
 }
-// Which CTA's share holds tile t of T, with n_cta of them used.
-__device__ __forceinline__ uint32_t tile_owner(uint64_t t, uint64_t total, uint32_t n_cta)
+// Unit and KV head in which the walk stands, and the first tile of its list that is the CTA's.
+template <int ROWS, int TILE>
+__device__ __forceinline__ Unit walk_item(const AttnArgs &a, const Pass &p, Walk &w, uint32_t *c, uint32_t *k0)
 {
-    return (uint32_t)(((t + 1) * n_cta - 1) / total);
+    Unit u;
+    for (;;) {
+        u = get_unit<ROWS, TILE>(a, p, w.s, w.rt);
+        const uint32_t t = (uint32_t)u.tiles * a.n_kv;
+        if (w.pos < w.base + t) break;
+        w.base += t;
+        if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+    }
+    const uint32_t in = w.pos - w.base;
+    *c = a.n_kv > 1 ? in / (uint32_t)u.tiles : 0;
+    *k0 = in - *c * (uint32_t)u.tiles;
+    return u;
+}
+// One thread of CTA `cta`, for the border before its share: what the join needs to know.
+__device__ __forceinline__ void write_cut(const Pass &p, uint32_t cta, const Walk &w, const Unit &u, uint32_t c, uint32_t k0)
+{
+    Cut x = {};
+    if (w.pos < w.end && k0) {
+        const uint32_t first = w.pos - k0;
+        x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows, x.c = c;
+        x.c0 = tile_owner(first, w.per, w.more);
+        x.c1 = tile_owner(first + u.tiles - 1, w.per, w.more);
+    }
+    p.cuts[cta] = x;
 }
 __device__ __forceinline__ float warp_sum(float x)
 {

@@ -48,7 +48,7 @@ struct Few {
     static constexpr uint32_t kRing = kStages * kStageBytes;             // a warp's
     static constexpr int kFrag = D / 8 * (HI ? 4 : 2);                   // floats of O a lane carries into the join
     static constexpr uint32_t kJoin = 2 * kFrag * 32 * 4;
-    static constexpr uint32_t kSmem = kWarps * kRing + kJoin + 2 * 32 * (HI ? 16 : 8) + kWarps * kStages * 8 + 8 * (kWarps + 3) + 1024;
+    static constexpr uint32_t kSmem = kWarps * kRing + kJoin + 2 * 32 * (HI ? 16 : 8) + kWarps * kStages * 8 + 4 * (kWarps + 2) + 1024;
 };
 
 // Registers of a warp's running softmax over its share of an item.
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     float *jo = reinterpret_cast<float *>(sm + kWarps * F::kRing);           // two buffers of F::kFrag * 32 floats
     float *jml = jo + 2 * F::kFrag * 32;                                      // two of (HI ? 4 : 2) * 32
     uint64_t *bars = reinterpret_cast<uint64_t *>(jml + 2 * 32 * (HI ? 4 : 2));
-    uint64_t *plan = bars + kWarps * S;
+    uint32_t *plan = reinterpret_cast<uint32_t *>(bars + kWarps * S);
     const uint32_t bar = smem_u32(bars + warp * S);
     if (lane == 0) {
         for (int i = 0; i < S; ++i) mbar_init(bar + 8 * i, 1);
@@ -118,46 +118,21 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     grid_launch_dependents();
     Walk w = plan_walk<kFewRows, kFewTile, kThreads>(a, p, blockIdx.x, plan);
 
-    // units that see nothing: zero rows (the join knows nothing of them)
-    for (uint32_t u = blockIdx.x; u < p.n_units; u += gridDim.x) {
-        const Unit un = get_unit<kFewRows, kFewTile>(a, p, u / p.n_rt, u % p.n_rt);
-        if (un.rows == 0 || un.tiles != 0) continue;
-        for (uint32_t i = tid; i < un.rows * a.n_kv; i += kThreads) {
-            const int r = i % un.rows;
-            const uint32_t h = unit_head(a, un, i / un.rows, r);
-            const uint64_t tok = unit_tok(a, un, r);
-            if (p.row_o) {
-                p.row_ml[tok * a.n_heads + h] = make_float2(neg_inf(), 0.f);
-            } else {
-                uint4 *op = reinterpret_cast<uint4 *>(a.out + tok * a.out_token_stride + h * a.out_head_stride);
-                for (int d = 0; d < D / 8; ++d) op[d] = make_uint4(0, 0, 0, 0);
-                if (a.lse) a.lse[tok * a.n_heads + h] = neg_inf();
-            }
-        }
-    }
-
     const float c2 = a.scale * kLog2e;
     const uint32_t tok_mask = (1u << a.block_shift) - 1u;
     uint32_t put = 0, got = 0;  // stages issued / consumed since the start
     bool failed = false;
-    Unit un;
+    Unit un = {};
     uint32_t c = 0;
     int k0 = 0, k1 = 0;          // the CTA's tiles of the item's list
     int ids = 0, ids_old = 0;    // block ids of the warp's tiles 32b + lane: current and previous batch
 
     auto segment = [&]() -> bool {  // the next run of tiles of one item
         if (w.pos >= w.end) return false;
-        for (;;) {
-            un = get_unit<kFewRows, kFewTile>(a, p, w.s, w.rt);
-            const uint64_t t = (uint64_t)un.tiles * a.n_kv;
-            if (w.pos < w.base + t) break;
-            w.base += t;
-            if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
-        }
-        const uint64_t in = w.pos - w.base;
-        c = (uint32_t)(in / (uint32_t)un.tiles);
-        k0 = (int)(in % (uint32_t)un.tiles);
-        k1 = (int)min((uint64_t)un.tiles, (uint64_t)k0 + (w.end - w.pos));
+        uint32_t k;
+        un = walk_item<kFewRows, kFewTile>(a, p, w, &c, &k);
+        k0 = (int)k;
+        k1 = (int)min((uint32_t)un.tiles, k + (w.end - w.pos));
         return true;
     };
     auto count = [&]() { return (k1 - k0 - (int)warp + kWarps - 1) / kWarps; };  // tiles of this warp (may be <= 0)
@@ -185,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     bool live = segment();
     if (live)
         for (int i = 0; i < S && i < count(); ++i) issue(i);
+    if (tid == 0) write_cut(p, blockIdx.x, w, un, c, (uint32_t)k0);
     while (live) {
         const int nt = count();
         const int r0 = lane / 4, r1 = r0 + 8;

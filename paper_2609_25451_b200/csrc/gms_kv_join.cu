@@ -76,23 +76,34 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int t
     }
 }
 
+// Also: rows of units that see nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
 // Block (i, part): the item into which the border between CTA i and CTA i + 1 falls, if that is its first border.
 template <class T, int D, int ROWS, int TILE>
 __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
                                                                    uint32_t parts)
 {
     grid_launch_dependents();
+    for (uint32_t x = blockIdx.x; x < p.n_units; x += gridDim.x) {  // while the attention kernel still runs
+        const Unit u = get_unit<ROWS, TILE>(a, p, x / p.n_rt, x % p.n_rt);
+        if (u.rows == 0 || u.tiles != 0) continue;
+        for (uint32_t k = threadIdx.x; k < u.rows * a.n_kv; k += kWarps * 32) {
+            const int r = k % u.rows;
+            const uint32_t h = unit_head(a, u, k / u.rows, r);
+            const uint64_t tok = unit_tok(a, u, r);
+            uint4 *op = reinterpret_cast<uint4 *>(a.out + tok * a.out_token_stride + h * a.out_head_stride);
+            for (int d = 0; d < D / 8; ++d) op[d] = make_uint4(0, 0, 0, 0);
+            if (a.lse) a.lse[tok * a.n_heads + h] = neg_inf();
+        }
+    }
     grid_wait();
     const uint32_t i = blockIdx.x / parts + 1, part = blockIdx.x % parts, warp = threadIdx.x / 32;
-    const uint64_t total = p.begin[p.n_units];
-    const uint32_t n = used_ctas(total, p);
     if (p.redo) {  // rows of finished items that came out non-finite; a cut item's words are zero
         for (uint32_t w = blockIdx.x * kWarps + warp; w < p.n_units * a.n_kv; w += gridDim.x * kWarps) {
             const uint32_t unit = w / a.n_kv;
-            if (p.begin[unit] == p.begin[unit + 1]) continue;  // sees nothing: no words were written
+            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+            if (u.tiles == 0) continue;  // sees nothing: no words were written
             const uint32_t mine = (threadIdx.x & 31u) < 8 ? p.redo[(uint64_t)w * 8 + (threadIdx.x & 31u)] : 0u;
             if (!__any_sync(0xffffffffu, mine)) continue;
-            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
             for (uint32_t k = 0; k < 8; ++k)
                 for (uint32_t rows = __shfl_sync(0xffffffffu, mine, k); rows; rows &= rows - 1) {
                     const int r = (int)k * 32 + __ffs(rows) - 1;
@@ -100,24 +111,14 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
                 }
         }
     }
-    if (i >= n) return;
-    const uint64_t at = total * i / n;
-    uint32_t lo = 0, hi = p.n_units;
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (p.begin[mid] <= at) lo = mid; else hi = mid;
-    }
-    const Unit u = get_unit<ROWS, TILE>(a, p, lo / p.n_rt, lo % p.n_rt);
-    if (u.tiles == 0) return;
-    const uint32_t c = (uint32_t)((at - p.begin[lo]) / (uint32_t)u.tiles);
-    const uint64_t first = p.begin[lo] + (uint64_t)c * (uint32_t)u.tiles;
-    if (at == first) return;  // the border lies between two items
-    const uint32_t c0 = tile_owner(first, total, n), c1 = tile_owner(first + u.tiles - 1, total, n);
-    if (c0 + 1 != i) return;
-    for (int r = part * kWarps + warp; r < u.rows; r += parts * kWarps) {
-        Row<D> x;
-        add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
-        finish<T, D>(a, x, unit_tok(a, u, r), unit_head(a, u, c, r), p.again);
+    if (i >= p.n_cta) return;  // only here for the above
+    const Cut x = p.cuts[i];
+    if (x.c1 == 0 || x.c0 + 1 != i) return;  // the border lies between two items, or is not the item's first
+    for (int r = part * kWarps + warp; r < x.rows; r += parts * kWarps) {
+        Row<D> sum;
+        add_pieces<D>(sum, p.part_ml, p.part_o, x.c1 - x.c0 + 1, [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * ROWS + r; });
+        const int row = x.row0 + r;
+        finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
     }
 }
 
@@ -132,8 +133,9 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (rt >= p.n_rt) return;
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
     if (u.tiles == 0 || (int)r >= u.rows) return;
-    const uint64_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + (uint64_t)c * (uint32_t)u.tiles;
-    const uint32_t n = used_ctas(total, p), c0 = tile_owner(first, total, n), c1 = tile_owner(first + u.tiles - 1, total, n);
+    const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * (uint32_t)u.tiles;
+    const uint32_t n = used_ctas(total, p.n_cta), per = total / n, more = total % n;
+    const uint32_t c0 = tile_owner(first, per, more), c1 = tile_owner(first + u.tiles - 1, per, more);
     if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 1, [&](uint32_t) { return row; });
     else
         add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
@@ -178,7 +180,6 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
 
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
-    if (p.n_cta < 2 && !p.redo) return cudaSuccess;
     const uint32_t cuts = p.n_cta < 2 ? 1 : p.n_cta - 1, parts = p.rows / kFewRows;
     if (p.rows == kTcRows)
         GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));

@@ -42,30 +42,26 @@ struct Tc {
     static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 2 * kSegments) * 8;
     static constexpr uint32_t kOutBytes = 8 * 2048;               // 32 rows x 64 bytes a softmax warp, for coalesced stores
-    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 8 * (kThreads / 32 + 3) + 16 + kSegments * sizeof(Segment) + 1024;
+    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 8 * (kThreads / 32 + 3) + 32 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
     static constexpr uint32_t kCols = 512;
 };
 
-__device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, Walk &w, Segment &g)
+__device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, Walk &w, Segment &g, bool first)
 {
     g.k0 = g.k1 = 0;
-    if (w.pos >= w.end) return false;
-    Unit u;
-    for (;;) {
-        u = get_unit<kRows, kTile>(a, p, w.s, w.rt);
-        const uint64_t t = (uint64_t)u.tiles * a.n_kv;
-        if (w.pos < w.base + t) break;
-        w.base += t;
-        if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+    if (w.pos >= w.end) {
+        if (first && (threadIdx.x & 31u) == 0) write_cut(p, blockIdx.x, w, Unit(), 0, 0);
+        return false;
     }
-    const uint64_t in = w.pos - w.base;
+    uint32_t k;
+    const Unit u = walk_item<kRows, kTile>(a, p, w, &g.c, &k);
+    if (first && (threadIdx.x & 31u) == 0) write_cut(p, blockIdx.x, w, u, g.c, k);
     g.table = u.table;
     g.q0 = u.q0, g.row0 = u.row0, g.rows = u.rows, g.n = u.n, g.first = u.first, g.pos_min = u.pos_min, g.pos_max = u.pos_max;
     g.n_sink_tiles = u.n_sink_tiles, g.first_tile = u.first_tile, g.tiles = u.tiles, g.whole = u.whole;
-    g.c = (uint32_t)(in / (uint32_t)u.tiles);
-    g.k0 = (int)(in % (uint32_t)u.tiles);
-    g.k1 = (int)min((uint64_t)u.tiles, (uint64_t)g.k0 + (w.end - w.pos));
+    g.k0 = (int)k;
+    g.k1 = (int)min((uint32_t)u.tiles, k + (w.end - w.pos));
     g.item = (w.s * p.n_rt + w.rt) * a.n_kv + g.c;
     w.pos += (uint32_t)(g.k1 - g.k0);
     return true;
@@ -131,8 +127,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes + F::kOutBytes);
     const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, q_empty = q_full + 16, s_full = q_empty + 16,
                    p_full = s_full + 32, o_done = p_full + 32, drain = o_done + 32, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
-    uint64_t *plan = bars + 2 * NS + 17 + 2 * kSegments;
-    volatile uint32_t *shared_words = reinterpret_cast<volatile uint32_t *>(plan + kThreads / 32 + 3);  // [0] tensor memory, [1] abort
+    uint32_t *plan = reinterpret_cast<uint32_t *>(bars + 2 * NS + 17 + 2 * kSegments);
+    volatile uint32_t *shared_words = plan + 16;  // [0] tensor memory, [1] abort
     volatile uint32_t *abort = shared_words + 1;
     Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
     if (tid == 0) {
@@ -161,24 +157,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     tc_fence_after();
     const uint32_t tmem = shared_words[0];
 
-    // units that see nothing: zero rows (the join knows nothing of them)
-    for (uint32_t u = blockIdx.x; u < p.n_units; u += gridDim.x) {
-        const Unit un = get_unit<kRows, kTile>(a, p, u / p.n_rt, u % p.n_rt);
-        if (un.rows == 0 || un.tiles != 0) continue;
-        for (uint32_t i = tid; i < un.rows * a.n_kv; i += kThreads) {
-            const int r = i % un.rows;
-            const uint32_t h = unit_head(a, un, i / un.rows, r);
-            const uint64_t tok = unit_tok(a, un, r);
-            if (p.row_o) {
-                p.row_ml[tok * a.n_heads + h] = make_float2(neg_inf(), 0.f);
-            } else {
-                uint4 *op = reinterpret_cast<uint4 *>(a.out + tok * a.out_token_stride + h * a.out_head_stride);
-                for (int d = 0; d < D / 8; ++d) op[d] = make_uint4(0, 0, 0, 0);
-                if (a.lse) a.lse[tok * a.n_heads + h] = neg_inf();
-            }
-        }
-    }
-
     // 384 threads x 168 registers = 128 x 104 + 256 x 200
     uint32_t seg = 0;  // segments seen
     if (warp >= 8) {
@@ -189,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             const uint32_t at = seg % kSegments;
             if (!__all_sync(0xffffffffu, wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status))) break;
             Segment g;
-            more = next_segment(a, p, w, g);
+            more = next_segment(a, p, w, g, seg == 0);
             if (more) {  // whether any id of its tiles lies outside the pool (then the softmax looks at every tile's)
                 bool hole = false;
                 const int t_end = min(g.n, (seg_tile(g, g.k1 - 1) + 1) * kTile), step = 1 << a.block_shift;
@@ -367,8 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         uint32_t n = 0, tiles = 0;  // tiles of all segments so far; of this slot
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (!__all_sync(0xffffffffu, mbar_spin(bar, parity, 4096)))
-                ok = __all_sync(0xffffffffu, wait_slow(bar, parity, abort, a.status));
+            if (!mbar_spin(bar, parity, 4096)) ok = wait_slow(bar, parity, abort, a.status);
+            __syncwarp();
             return ok;
         };
         for (;; ++seg) {
@@ -411,8 +389,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             float m = neg_inf(), l = 0.f;
             const int n_sink_tiles = g.n_sink_tiles, past_sinks = g.first_tile - n_sink_tiles;
             const bool holes = g.holes != 0;
-            // One step: 64 columns of S to P.
-            auto step = [&](int half, int k, int t0, bool whole, uint32_t valid) {
+            // One step: 64 columns of S to P.  `half` and `edge` are constants where it is called.
+            auto step = [&](const int half, const bool edge, int k, int t0, uint32_t valid) {
                 if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) return;
                 tc_fence_after();
                 uint32_t s[2][32];
@@ -420,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 tmem_ld32(s_col + half * 64 + 32, s[1]);
                 tmem_wait32(s[0]);
                 tmem_wait32(s[1]);
-                if (!whole) {
+                if (edge) {
                     const uint32_t v4 = valid >> (4 * half);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -433,28 +411,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                             if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
                     }
                 }
-                // The exponentials are taken against the maximum so far while this step's own is being found; only if a row's has
-                // outgrown it by more than kLag (or it has none yet) are they taken again.
-                uint32_t pk[32];
-                float2 part[2];
-                for (;;) {
-                    const float z = m == neg_inf() ? 0.f : m;
-                    const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
-                    part[0] = part[1] = make_float2(0.f, 0.f);
-                    float tops[2] = {neg_inf(), neg_inf()};
+                float tops[4];  // four chains
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
-                        tops[j & 1] = fmaxf(tops[j & 1], fmaxf(x.x, x.y));
-                        x = fma2(x, cc, zz);
-                        x.x = ex2(x.x);
-                        x.y = ex2(x.y);
-                        part[j & 1] = add2(part[j & 1], x);
-                        pk[j] = pack2(x.x, x.y, T());
-                    }
-                    const float top = fmaxf(tops[0], tops[1]) * c2;
-                    const bool grow = top > m + kLag || (m == neg_inf() && top != m);
-                    if (!__any_sync(0xffffffffu, grow)) break;
+                for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(s[i / 2][(i % 2) * 16]);
+#pragma unroll
+                for (int j = 1; j < 15; j += 2)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + j])), __uint_as_float(s[i / 2][(i % 2) * 16 + j + 1]));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + 15]));
+                const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), neg_inf()) * c2;
+                const bool grow = top > m + kLag || (m == neg_inf() && top != m);
+                if (__any_sync(0xffffffffu, grow)) {
                     const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
                     if (grow) m = top;
                     l *= f;
@@ -472,13 +441,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                         }
                     }
                 }
+                const float z = m == neg_inf() ? 0.f : m;
+                const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
+                float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                uint32_t pk[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
+                    x = fma2(x, cc, zz);
+                    x.x = ex2(x.x);
+                    x.y = ex2(x.y);
+                    part[j & 1] = add2(part[j & 1], x);
+                    pk[j] = pack2(x.x, x.y, T());
+                }
                 tmem_st32(s_col + half * 64, pk);
                 part[0] = add2(part[0], part[1]);
                 l += part[0].x + part[0].y;
                 // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
                 // of the unit sees, where rows are not done again.  Thread r of each slot clears token r of the tile before
                 // its slot's first half is handed over (the other slot may clear it too: the same zeros).
-                if (half == 0 && !whole) {
+                if (half == 0 && edge) {
                     const int t = t0 + row_in;
                     const bool none = t >= len || (!p.again && (t > g.pos_max || (!all && !sees(a, max(g.pos_min, t), t))));
                     if (__any_sync(0xffffffffu, none)) {
@@ -506,8 +488,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     valid = __ballot_sync(0xffffffffu, (uint32_t)id < a.n_blocks) & 0xffu;
                 }
                 const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo && (t0 >= low_hi || t0 + kTile - 1 < sink);
+                if (whole) {
+                    step(0, false, k, t0, valid);
+                    if (!ok) break;
+                    step(1, false, k, t0, valid);
+                } else {
 #pragma unroll 1
-                for (int half = 0; ok && half < 2; ++half) step(half, k, t0, whole, valid);
+                    for (int half = 0; ok && half < 2; ++half) step(half, true, k, t0, valid);
+                }
                 ++n;
                 ++tiles;
             }
