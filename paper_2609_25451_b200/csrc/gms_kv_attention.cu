@@ -269,13 +269,14 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     if (p->n_rt == 0) p->n_rt = 1;
     const uint64_t units = (uint64_t)(prefix ? a.n_groups : a.n_seq) * p->n_rt;
     p->n_units = (uint32_t)(units < 0xffffffffull ? units : 0xffffffffull);  // too many: most_tiles refuses them
-    // as many CTAs as the SMs hold; fewer where they would have fewer than eight tiles of 16 tokens (two a warp), or two of 128
-    const uint64_t want = ceil_div(most_tiles(a, *p), tc ? 2 : 8), most = tc ? kTcMaxCtas : kFewMaxCtas;
-    p->n_cta = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
+    // as many workers as the SMs hold; fewer where they would have fewer than two tiles
+    const uint64_t want = ceil_div(most_tiles(a, *p), 2), most = tc ? kTcMaxWorkers : kFewMaxWorkers;
+    p->workers = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
+    p->slot_rows = rows < p->rows ? (uint32_t)(rows < 1 ? 1 : rows) : p->rows;
     if (rows_out) p->begin = c->take<uint32_t>(p->n_units + 1);
-    p->cuts = c->take<Cut>(p->n_cta);
-    p->part_ml = c->take<float2>(2ull * p->n_cta * p->rows);
-    p->part_o = c->take<float>(2ull * p->n_cta * p->rows * head_dim);
+    p->cuts = c->take<Cut>(p->workers);
+    p->part_ml = c->take<float2>(2ull * p->workers * p->slot_rows);
+    p->part_o = c->take<float>(2ull * p->workers * p->slot_rows * head_dim);
     if (rows_out) {
         p->row_ml = c->take<float2>((uint64_t)a.total_q * a.n_heads);
         p->row_o = c->take<float>((uint64_t)a.total_q * a.n_heads * head_dim);

@@ -42,22 +42,24 @@ struct AttnArgs {
 // How a pass over cached tokens is cut.  A unit is a run of up to ROWS query rows (token-major, the heads of one KV head
 // inside a token) of one sequence (or, in a prefix pass, of one group); an item is a unit for one KV head; an item's work
 // is the list of token tiles that at least one of its rows sees.  All items' tiles, one after the other, are dealt out
-// evenly: CTA i of n (n = n_cta, or T if that is less) gets T / n or T / n + 1 tiles, whatever items they fall into, so
-// ragged lengths cost no balance.  An item that one CTA has whole is finished there; the at most two pieces a CTA has of
-// others go to its two slots of part_o / part_ml and are joined by kv_attn_join.
-struct Cut {               // the item into which the border before CTA i falls (c1 = 0: the border lies between items)
+// evenly: worker i of n (n = workers, or T if that is less) gets T / n or T / n + 1 tiles, whatever items they fall into, so
+// ragged lengths cost no balance.  A worker is a CTA of the many-row kernel, a warp of the few-row kernel.  An item that one
+// worker has whole is finished there; the at most two pieces a worker has of others go to its two slots of part_o / part_ml
+// and are joined by kv_attn_join.
+struct Cut {               // the item into which the border before worker i falls (c1 = 0: the border lies between items)
     int q0, row0, rows;
-    uint32_t c, c0, c1;    // KV head; first and last CTA that has a piece
+    uint32_t c, c0, c1;    // KV head; first and last worker that has a piece
     uint32_t pad[2];
 };
 struct Pass {
     uint32_t prefix;       // 1: units are groups' query rows over their prefix, all of it seen
-    uint32_t n_units, n_rt, n_cta;  // n_rt units a sequence (group)
+    uint32_t n_units, n_rt, workers;  // n_rt units a sequence (group)
     uint32_t rows, tile;   // rows a unit, tokens a tile
+    uint32_t slot_rows;    // rows a slot of part_o has room for (at most `rows`)
     uint32_t *begin;       // null, or [n_units + 1] tiles before each unit (written by CTA 0 for those who look items up)
-    Cut *cuts;             // [n_cta], written by CTA i for its own border
-    float *part_o;         // [2 * n_cta][rows][head_dim], not normalised
-    float2 *part_ml;       // [2 * n_cta][rows]: running maximum (base 2) and sum
+    Cut *cuts;             // [workers], written by worker i for its own border
+    float *part_o;         // [2 * workers][slot_rows][head_dim], not normalised
+    float2 *part_ml;       // [2 * workers][slot_rows]: running maximum (base 2) and sum
     float *row_o;          // null: finished rows go to out / lse; else [total_q * n_heads][head_dim], not normalised
     float2 *row_ml;        // [total_q * n_heads]
     float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2 (few-row pass only)
@@ -85,12 +87,12 @@ cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtyp
 cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, const Pass &own, uint32_t dtype, uint32_t head_dim,
                                        cudaStream_t s);
 // Few query rows a unit (at most 16): kv_attn_few; many: kv_attn_tc.
-constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewMaxCtas = 2 * 148;
+constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewWarps = 4, kFewMaxWorkers = 2 * 148 * kFewWarps;
 cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
                                uint32_t head_dim, cudaStream_t s);
 // Many query rows a unit; box_tokens: tokens a TMA box of the maps holds; qmap: null, or boxes of 64 elements x group heads
 // x 128 / group tokens of the queries.
-constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxCtas = 148;
+constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxWorkers = 148;
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
                               uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
@@ -236,27 +238,27 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
     }
     return u;
 }
-// The part of the work that a CTA has, item by item.
+// The part of the work that a worker has, item by item.
 struct Walk {
     uint32_t pos, end;   // tiles still to do, in the order over all items
     uint32_t base;       // tiles before the current unit
     uint32_t s, rt;
     uint32_t total, per, more;  // tiles in all; every share has `per`, the first `more` shares one more
 };
-// CTAs that get work: no share is empty, so a piece lies in every slot that the join looks at.
-__device__ __forceinline__ uint32_t used_ctas(uint32_t total, uint32_t n_cta) { return min(total, n_cta); }
-// Which CTA's share holds tile t.
+// Workers that get work: no share is empty, so a piece lies in every slot that the join looks at.
+__device__ __forceinline__ uint32_t used_workers(uint32_t total, uint32_t workers) { return min(total, workers); }
+// Which worker's share holds tile t.
 __device__ __forceinline__ uint32_t tile_owner(uint32_t t, uint32_t per, uint32_t more)
 {
     const uint32_t high = more * (per + 1);
     return t < high ? t / (per + 1) : more + (t - high) / per;
 }
-// Scans all units (fewer than 2^31 tiles in all), finds CTA `cta`'s share.  Every thread of the CTA calls it and gets the
-// same result; `sh` is 4 * (warps + 2) bytes of shared memory.
-template <int ROWS, int TILE, int THREADS>
-__device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t cta, uint32_t *sh)
+// Scans all units (fewer than 2^31 tiles in all) and finds the share of the caller's worker.  A CTA is WORKERS workers
+// (1, or one a warp); every thread calls it.  `sh` is 4 * (warps + 2 * WORKERS) bytes of shared memory.
+template <int ROWS, int TILE, int THREADS, int WORKERS>
+__device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint32_t *sh)
 {
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32, worker = WORKERS > 1 ? warp : 0;
     const uint32_t per = (p.n_units + THREADS - 1) / THREADS, u0 = min(tid * per, p.n_units), u1 = min(u0 + per, p.n_units);
     auto tiles_of = [&](uint32_t u) {
         return (uint32_t)get_unit<ROWS, TILE>(a, p, p.n_rt > 1 ? u / p.n_rt : u, p.n_rt > 1 ? u % p.n_rt : 0).tiles * a.n_kv;
@@ -271,49 +273,52 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
     }
     if (lane == 31) sh[warp] = inc;
     __syncthreads();
-    uint32_t before = inc - mine;
-    Walk w;
-    w.total = 0;
+    uint32_t before = inc - mine, total = 0;
 #pragma unroll
     for (uint32_t i = 0; i < THREADS / 32; ++i) {
         if (i < warp) before += sh[i];
-        w.total += sh[i];
+        total += sh[i];
     }
-    const uint32_t n = used_ctas(w.total, p.n_cta);
-    w.pos = w.end = w.total;
-    w.per = w.more = 0;
-    if (cta < n) {
-        w.per = w.total / n;
-        w.more = w.total - w.per * n;
-        w.pos = cta * w.per + min(cta, w.more);
-        w.end = w.pos + w.per + (cta < w.more);
+    const uint32_t n = used_workers(total, p.workers);
+    Walk w;
+    w.total = total;
+    w.per = n ? total / n : 0;
+    w.more = total - w.per * n;
+    w.pos = w.end = total;
+#pragma unroll
+    for (uint32_t k = 0; k < WORKERS; ++k) {
+        const uint32_t i = blockIdx.x * WORKERS + k, pos = i < n ? i * w.per + min(i, w.more) : total;
+        if (k == worker && i < n) {
+            w.pos = pos;
+            w.end = pos + w.per + (i < w.more);
+        }
+        if (pos - before < mine) {  // before <= pos < before + mine
+            uint32_t b = before, u = u0;
+            if (per > 1)
+                for (uint32_t t = tiles_of(u); pos - b >= t; t = tiles_of(++u)) b += t;
+            sh[THREADS / 32 + 2 * k] = b;
+            sh[THREADS / 32 + 2 * k + 1] = u;
+        }
     }
-    if (w.pos - before < mine) {  // before <= pos < before + mine
-        uint32_t b = before, u = u0;
-        if (per > 1)
-            for (uint32_t t = tiles_of(u); w.pos - b >= t; t = tiles_of(++u)) b += t;
-        sh[THREADS / 32] = b;
-        sh[THREADS / 32 + 1] = u;
-    }
-    if (p.begin && cta == 0) {
+    if (p.begin && blockIdx.x == 0) {
         uint32_t b = before;
         for (uint32_t u = u0; u < u1; ++u) {
             p.begin[u] = b;
             b += tiles_of(u);
         }
-        if (tid == 0) p.begin[p.n_units] = w.total;
+        if (tid == 0) p.begin[p.n_units] = total;
     }
     __syncthreads();
     w.base = w.s = w.rt = 0;
     if (w.pos < w.end) {
-        w.base = sh[THREADS / 32];
-        const uint32_t u = sh[THREADS / 32 + 1];
+        w.base = sh[THREADS / 32 + 2 * worker];
+        const uint32_t u = sh[THREADS / 32 + 2 * worker + 1];
         w.s = p.n_rt > 1 ? u / p.n_rt : u;
         w.rt = p.n_rt > 1 ? u % p.n_rt : 0;
     }
     return w;
 }
-// Unit and KV head in which the walk stands, and the first tile of its list that is the CTA's.
+// Unit and KV head in which the walk stands, and the first tile of its list that is the worker's.
 template <int ROWS, int TILE>
 __device__ __forceinline__ Unit walk_item(const AttnArgs &a, const Pass &p, Walk &w, uint32_t *c, uint32_t *k0)
 {
@@ -330,8 +335,8 @@ __device__ __forceinline__ Unit walk_item(const AttnArgs &a, const Pass &p, Walk
     *k0 = in - *c * (uint32_t)u.tiles;
     return u;
 }
-// One thread of CTA `cta`, for the border before its share: what the join needs to know.
-__device__ __forceinline__ void write_cut(const Pass &p, uint32_t cta, const Walk &w, const Unit &u, uint32_t c, uint32_t k0)
+// One thread of a worker, for the border before its share: what the join needs to know.
+__device__ __forceinline__ void write_cut(const Pass &p, uint32_t worker, const Walk &w, const Unit &u, uint32_t c, uint32_t k0)
 {
     Cut x = {};
     if (w.pos < w.end && k0) {
@@ -340,7 +345,7 @@ __device__ __forceinline__ void write_cut(const Pass &p, uint32_t cta, const Wal
         x.c0 = tile_owner(first, w.per, w.more);
         x.c1 = tile_owner(first + u.tiles - 1, w.per, w.more);
     }
-    p.cuts[cta] = x;
+    p.cuts[worker] = x;
 }
 __device__ __forceinline__ float warp_sum(float x)
 {

@@ -2,10 +2,10 @@
 //
 // Bound: memory.  Every visible K and V row is read once; 16 rows of mma.sync per 256-byte row are far below the tensor
 // rate, so the legacy matrix instruction is enough and what counts is bytes in flight and an even deal (see Pass).
-// Every warp is its own pipeline, as in the streaming kernels: tiles of 16 tokens come by TMA through the block table into
-// the warp's ring (K and V of one KV head, 128-byte swizzle, so that ldmatrix has no bank conflicts), no warp waits for
-// another before an item ends.  S = Q K^T, the online softmax and O += P V stay in registers; the four warps of the CTA
-// take every fourth tile and are joined in shared memory at the end of an item.
+// Every warp is a worker of its own, as in the streaming kernels: tiles of 16 tokens come by TMA through the block table into
+// the warp's ring (K and V of one KV head, 128-byte swizzle, so that ldmatrix has no bank conflicts), and no warp waits for
+// another.  S = Q K^T, the online softmax and O += P V stay in registers.  (Four warps sharing an item and joining in shared
+// memory at its end: 78 us against XX for 48 sequences of up to 2,052 visible tokens, 60 against XX for 64 of up to 512.)
 #include "gms_internal.h"
 #include "gms_kv_attn.h"
 #include "gms_ptx.h"
@@ -15,7 +15,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kWarps = (int)kFewWarps, kThreads = kWarps * 32;
 
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __nv_bfloat16)
 {
@@ -40,15 +40,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-template <int D, bool HI>
+template <int D>
 struct Few {
     static constexpr int kHalves = D / 64;
     static constexpr uint32_t kStageBytes = 2 * kHalves * 2048;          // K then V, 16 tokens x 128 bytes a half
-    static constexpr int kStages = D == 128 ? (HI ? 2 : 3) : 6;       // so that two CTAs share an SM
+    static constexpr int kStages = D == 128 ? 3 : 6;                      // so that two CTAs share an SM
     static constexpr uint32_t kRing = kStages * kStageBytes;             // a warp's
-    static constexpr int kFrag = D / 8 * (HI ? 4 : 2);                   // floats of O a lane carries into the join
-    static constexpr uint32_t kJoin = 2 * kFrag * 32 * 4;
-    static constexpr uint32_t kSmem = kWarps * kRing + kJoin + 2 * 32 * (HI ? 16 : 8) + kWarps * kStages * 8 + 4 * (kWarps + 2) + 1024;
+    static constexpr uint32_t kSmem = kWarps * kRing + kWarps * kStages * 8 + 4 * (kWarps + 2 * kWarps) + 1024;
 };
 
 // Registers of a warp's running softmax over its share of an item.
@@ -57,54 +55,20 @@ struct Acc {
     float o[D / 8][4], m[2], l[2];
 };
 
-template <int D, bool HI>
-__device__ __forceinline__ void join_from(Acc<D> &x, const float *o, const float *ml, uint32_t lane)
-{
-    constexpr int R = HI ? 2 : 1;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const float m2 = ml[(i * 2 + 0) * 32 + lane], l2 = ml[(i * 2 + 1) * 32 + lane], mn = fmaxf(x.m[i], m2);
-        const float f1 = x.m[i] == mn ? 1.f : ex2(x.m[i] - mn), f2 = m2 == mn ? 1.f : ex2(m2 - mn);
-        x.m[i] = mn;
-        x.l[i] = x.l[i] * f1 + l2 * f2;
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                x.o[j][i * 2 + e] = x.o[j][i * 2 + e] * f1 + o[((j * R + i) * 2 + e) * 32 + lane] * f2;
-    }
-}
-template <int D, bool HI>
-__device__ __forceinline__ void join_put(const Acc<D> &x, float *o, float *ml, uint32_t lane)
-{
-    constexpr int R = HI ? 2 : 1;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        ml[(i * 2 + 0) * 32 + lane] = x.m[i];
-        ml[(i * 2 + 1) * 32 + lane] = x.l[i];
-#pragma unroll
-        for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) o[((j * R + i) * 2 + e) * 32 + lane] = x.o[j][i * 2 + e];
-    }
-}
-
 // HI: the units have more than 8 rows (the upper half of the 16-row fragments is in use).
 template <class T, int D, bool HI>
 __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                   const __grid_constant__ CUtensorMap vmap,
                                                                   const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p)
 {
-    using F = Few<D, HI>;
+    using F = Few<D>;
     constexpr int S = F::kStages, NJ = D / 8;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *sm = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t ring = base + warp * F::kRing;
-    float *jo = reinterpret_cast<float *>(sm + kWarps * F::kRing);           // two buffers of F::kFrag * 32 floats
-    float *jml = jo + 2 * F::kFrag * 32;                                      // two of (HI ? 4 : 2) * 32
-    uint64_t *bars = reinterpret_cast<uint64_t *>(jml + 2 * 32 * (HI ? 4 : 2));
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + kWarps * F::kRing);
     uint32_t *plan = reinterpret_cast<uint32_t *>(bars + kWarps * S);
     const uint32_t bar = smem_u32(bars + warp * S);
     if (lane == 0) {
@@ -116,7 +80,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
         }
     }
     grid_launch_dependents();
-    Walk w = plan_walk<kFewRows, kFewTile, kThreads>(a, p, blockIdx.x, plan);
+    Walk w = plan_walk<kFewRows, kFewTile, kThreads, kWarps>(a, p, plan);
+    const uint32_t worker = blockIdx.x * kWarps + warp;
 
     const float c2 = a.scale * kLog2e;
     const uint32_t tok_mask = (1u << a.block_shift) - 1u;
@@ -124,8 +89,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     bool failed = false;
     Unit un = {};
     uint32_t c = 0;
-    int k0 = 0, k1 = 0;          // the CTA's tiles of the item's list
-    int ids = 0, ids_old = 0;    // block ids of the warp's tiles 32b + lane: current and previous batch
+    int k0 = 0, k1 = 0;          // the warp's tiles of the item's list
+    int ids = 0, ids_old = 0;    // block ids of tiles 32b + lane: current and previous batch
 
     auto segment = [&]() -> bool {  // the next run of tiles of one item
         if (w.pos >= w.end) return false;
@@ -135,17 +100,16 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
         k1 = (int)min((uint32_t)un.tiles, k + (w.end - w.pos));
         return true;
     };
-    auto count = [&]() { return (k1 - k0 - (int)warp + kWarps - 1) / kWarps; };  // tiles of this warp (may be <= 0)
     auto issue = [&](int i) {  // i: index among the warp's tiles
         if ((i & 31) == 0) {
             ids_old = ids;
-            const int k = k0 + (int)warp + kWarps * (i + (int)lane);
+            const int k = k0 + i + (int)lane;
             ids = k < k1 ? un.table[(uint32_t)(unit_tile(un, k) * kFewTile) >> a.block_shift] : -1;
         }
         const int id = __shfl_sync(0xffffffffu, ids, i & 31);
         if (lane == 0) {
             const uint32_t st = put % S, dst = ring + st * F::kStageBytes, b = bar + 8 * st;
-            const int y = (int)((uint32_t)(unit_tile(un, k0 + (int)warp + kWarps * i) * kFewTile) & tok_mask);
+            const int y = (int)((uint32_t)(unit_tile(un, k0 + i) * kFewTile) & tok_mask);
             const int blk = (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;  // a hole: out of range, zeros arrive
             mbar_expect(b, F::kStageBytes);
 #pragma unroll
@@ -159,10 +123,10 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 
     bool live = segment();
     if (live)
-        for (int i = 0; i < S && i < count(); ++i) issue(i);
-    if (tid == 0) write_cut(p, blockIdx.x, w, un, c, (uint32_t)k0);
+        for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);
+    if (lane == 0 && worker < p.workers) write_cut(p, worker, w, un, c, (uint32_t)k0);
     while (live) {
-        const int nt = count();
+        const int nt = k1 - k0;
         const int r0 = lane / 4, r1 = r0 + 8;
         // the item's query rows as matrix fragments; rows that do not exist are zero
         uint32_t q[D / 16][4];
@@ -198,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             // the batch that i belongs to is the current one unless the issue side has moved on
             const int last = min(i + S, nt) - 1;  // newest tile issued so far
             const int id = __shfl_sync(0xffffffffu, (last >> 5) == (i >> 5) ? ids : ids_old, i & 31);
-            const int t0 = unit_tile(un, k0 + (int)warp + kWarps * i) * kFewTile;
+            const int t0 = unit_tile(un, k0 + i) * kFewTile;
             float s[2][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -313,18 +277,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
         w.pos += (uint32_t)(k1 - k0);
         live = segment();
         if (live && !failed)  // the next item's first tiles are on their way while this one is joined
-            for (int i = 0; i < S && i < count(); ++i) issue(i);
+            for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);
 
-        __syncthreads();
-        constexpr int kMl = HI ? 4 : 2;
-        if (warp >= 2) join_put<D, HI>(x, jo + (warp - 2) * F::kFrag * 32, jml + (warp - 2) * kMl * 32, lane);
-        __syncthreads();
-        if (warp < 2) join_from<D, HI>(x, jo + warp * F::kFrag * 32, jml + warp * kMl * 32, lane);
-        __syncthreads();
-        if (warp == 1) join_put<D, HI>(x, jo, jml, lane);
-        __syncthreads();
-        if (warp != 0) continue;
-        join_from<D, HI>(x, jo, jml, lane);
         uint32_t again = 0;  // finished rows to be done once more
 #pragma unroll
         for (int r = 0; r < (HI ? 2 : 1); ++r) {
@@ -351,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                     po = p.row_o + at * D;
                     if ((lane & 3u) == 0) p.row_ml[at] = make_float2(m, l);
                 } else {
-                    at = ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * kFewRows + row;
+                    at = ((uint64_t)worker * 2 + (starts ? 1 : 0)) * p.slot_rows + row;
                     po = p.part_o + at * D;
                     if ((lane & 3u) == 0) p.part_ml[at] = make_float2(m, l);
                 }
@@ -376,11 +330,11 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 template <class T, int D, bool HI>
 cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
 {
-    constexpr uint32_t smem = Few<D, HI>::kSmem;
+    constexpr uint32_t smem = Few<D>::kSmem;
     static const cudaError_t ready =
         cudaFuncSetAttribute(kv_attn_few_kernel<T, D, HI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
-    kv_attn_few_kernel<T, D, HI><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, a, p);
+    kv_attn_few_kernel<T, D, HI><<<(p.workers + kWarps - 1) / kWarps, kThreads, smem, s>>>(kmap, vmap, a, p);
     count_launches(1);
     return cudaGetLastError();
 }

@@ -1,4 +1,4 @@
-// Joining the pieces of attention items that were cut across CTAs, and the two passes of a shared-prefix call.
+// Joining the pieces of attention items that were cut across workers, and the two passes of a shared-prefix call.
 //
 // Pieces carry a running maximum m (base 2), a sum l and unnormalised values o:  M = max m_i,  L = sum l_i 2^(m_i - M),
 // out = sum o_i 2^(m_i - M) / L,  in the order of the pieces, so equal calls give equal bits.  One warp a row; the pieces
@@ -15,22 +15,23 @@ namespace {
 
 using namespace ptx;
 
-constexpr uint32_t kWarps = 4;
+constexpr uint32_t kWarps = 8;
 
 template <int D>
 struct Row {
     float m = -INFINITY, l = 0.f, o[D / 32] = {};
 };
 
-// Adds n pieces; piece i lies at slot(i) of ml and o.
+// Adds pieces first, first + step, ... < n; piece i lies at slot(i) of ml and o.  Eight loads of o are in flight.
 template <int D, class F>
-__device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const float *o, uint32_t n, F slot)
+__device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const float *o, uint32_t first, uint32_t step, uint32_t n, F slot)
 {
     using V = typename std::conditional<D == 128, float4, float2>::type;
     const uint32_t lane = threadIdx.x & 31u;
-    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+    for (uint32_t i0 = first; i0 < n; i0 += 32 * step) {
+        const uint32_t me = i0 + lane * step;
         float2 mine = make_float2(neg_inf(), 0.f);
-        if (i0 + lane < n) mine = ml[slot(i0 + lane)];
+        if (me < n) mine = ml[slot(me)];
         float top = fmaxf(x.m, mine.x);
 #pragma unroll
         for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
@@ -39,15 +40,19 @@ __device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const fl
         x.l = x.l * f + warp_sum(mine.y * g);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) x.o[e] *= f;
-        const uint32_t k = min(32u, n - i0);
-#pragma unroll 8
-        for (uint32_t i = 0; i < k; ++i) {
-            const float gi = __shfl_sync(0xffffffffu, g, i), li = __shfl_sync(0xffffffffu, mine.y, i);
-            if (li == 0.f) continue;  // nothing seen there
-            const V v = reinterpret_cast<const V *>(o + slot(i0 + i) * D)[lane];
-            const float *vf = reinterpret_cast<const float *>(&v);
+        const uint32_t left = min(32u, (n - i0 + step - 1) / step);
+        for (uint32_t b = 0; b < left; b += 8) {
+            V v[8];
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) x.o[e] += vf[e] * gi;
+            for (uint32_t j = 0; j < 8; ++j) v[j] = reinterpret_cast<const V *>(o + slot(i0 + min(b + j, left - 1) * step) * D)[lane];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                const float gi = __shfl_sync(0xffffffffu, g, (b + j) & 31u), li = __shfl_sync(0xffffffffu, mine.y, (b + j) & 31u);
+                if (b + j >= left || li == 0.f) continue;  // nothing seen there
+                const float *vf = reinterpret_cast<const float *>(&v[j]);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) x.o[e] += vf[e] * gi;
+            }
         }
     }
 }
@@ -77,7 +82,7 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int t
 }
 
 // Also: rows of units that see nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
-// Block (i, part): the item into which the border between CTA i and CTA i + 1 falls, if that is its first border.
+// Block (i, part): the item into which the border before worker i falls, if that is its first border.
 template <class T, int D, int ROWS, int TILE>
 __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
                                                                    uint32_t parts)
@@ -111,13 +116,43 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
                 }
         }
     }
-    if (i >= p.n_cta) return;  // only here for the above
+    if (i >= p.workers) return;  // only here for the above
     const Cut x = p.cuts[i];
     if (x.c1 == 0 || x.c0 + 1 != i) return;  // the border lies between two items, or is not the item's first
-    for (int r = part * kWarps + warp; r < x.rows; r += parts * kWarps) {
+    // few rows: several warps share a row's pieces
+    const uint32_t here = min((uint32_t)max(x.rows - (int)(part * kFewRows), 0), kFewRows);  // rows of this block
+    const uint32_t share = here == 0 || here >= kWarps ? 1 : kWarps / here;
+    __shared__ float m_sh[kWarps], l_sh[kWarps];
+    __shared__ float o_sh[kWarps][D];
+    const uint32_t lane = threadIdx.x & 31u;
+    if (share > 1) {
         Row<D> sum;
-        add_pieces<D>(sum, p.part_ml, p.part_o, x.c1 - x.c0 + 1, [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * ROWS + r; });
-        const int row = x.row0 + r;
+        const uint32_t r = warp % here, g = warp / here;
+        if (g < share)
+            add_pieces<D>(sum, p.part_ml, p.part_o, g, share, x.c1 - x.c0 + 1,
+                          [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + part * kFewRows + r; });
+        if (lane == 0) m_sh[warp] = sum.m, l_sh[warp] = sum.l;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o_sh[warp][lane * (D / 32) + e] = sum.o[e];
+        __syncthreads();
+        if (warp >= here) return;
+        for (uint32_t k = 1; k < share; ++k) {
+            const uint32_t other = warp + k * here;
+            const float m2 = m_sh[other], top = fmaxf(sum.m, m2), f1 = sum.m == top ? 1.f : ex2(sum.m - top), f2 = m2 == top ? 1.f : ex2(m2 - top);
+            sum.m = top;
+            sum.l = sum.l * f1 + l_sh[other] * f2;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) sum.o[e] = sum.o[e] * f1 + o_sh[other][lane * (D / 32) + e] * f2;
+        }
+        const int row = x.row0 + (int)(part * kFewRows + warp);
+        finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
+        return;
+    }
+    for (uint32_t r = warp; r < here; r += kWarps) {
+        Row<D> sum;
+        add_pieces<D>(sum, p.part_ml, p.part_o, 0, 1, x.c1 - x.c0 + 1,
+                      [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + part * kFewRows + r; });
+        const int row = x.row0 + (int)(part * kFewRows + r);
         finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
     }
 }
@@ -134,11 +169,11 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
     if (u.tiles == 0 || (int)r >= u.rows) return;
     const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * (uint32_t)u.tiles;
-    const uint32_t n = used_ctas(total, p.n_cta), per = total / n, more = total % n;
+    const uint32_t n = used_workers(total, p.workers), per = total / n, more = total % n;
     const uint32_t c0 = tile_owner(first, per, more), c1 = tile_owner(first + u.tiles - 1, per, more);
-    if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 1, [&](uint32_t) { return row; });
+    if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 0, 1, 1, [&](uint32_t) { return row; });
     else
-        add_pieces<D>(x, p.part_ml, p.part_o, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * ROWS + r; });
+        add_pieces<D>(x, p.part_ml, p.part_o, 0, 1, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * p.slot_rows + r; });
 }
 
 template <class T, int D>
@@ -180,7 +215,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
 
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
-    const uint32_t cuts = p.n_cta < 2 ? 1 : p.n_cta - 1, parts = p.rows / kFewRows;
+    const uint32_t cuts = p.workers < 2 ? 1 : p.workers - 1, parts = p.rows / kFewRows;
     if (p.rows == kTcRows)
         GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));
     GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));

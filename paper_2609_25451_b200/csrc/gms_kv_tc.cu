@@ -42,7 +42,7 @@ struct Tc {
     static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 2 * kSegments) * 8;
     static constexpr uint32_t kOutBytes = 8 * 2048;               // 32 rows x 64 bytes a softmax warp, for coalesced stores
-    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 8 * (kThreads / 32 + 3) + 32 + kSegments * sizeof(Segment) + 1024;
+    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 128 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
     static constexpr uint32_t kCols = 512;
 };
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, q_empty = q_full + 16, s_full = q_empty + 16,
                    p_full = s_full + 32, o_done = p_full + 32, drain = o_done + 32, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
     uint32_t *plan = reinterpret_cast<uint32_t *>(bars + 2 * NS + 17 + 2 * kSegments);
-    volatile uint32_t *shared_words = plan + 16;  // [0] tensor memory, [1] abort
+    volatile uint32_t *shared_words = plan + 16;  // behind the plan's 14  // [0] tensor memory, [1] abort
     volatile uint32_t *abort = shared_words + 1;
     Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
     if (tid == 0) {
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(shared_words)), F::kCols);
     grid_launch_dependents();
     tc_fence_before();
-    Walk w = plan_walk<kRows, kTile, kThreads>(a, p, blockIdx.x, plan);  // ends with __syncthreads
+    Walk w = plan_walk<kRows, kTile, kThreads, 1>(a, p, plan);  // ends with __syncthreads
     tc_fence_after();
     const uint32_t tmem = shared_words[0];
 
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     __syncwarp();
                 }
             } else {
-                const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * kRows + row;
+                const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * p.slot_rows + row;
                 float *dst = (mine ? p.row_o : p.part_o) + at * D;
                 if (live) (mine ? p.row_ml : p.part_ml)[at] = make_float2(m, l);
 #pragma unroll
@@ -581,7 +581,7 @@ cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, co
     constexpr uint32_t smem = Tc<D>::kSmem;
     static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
-    kv_attn_tc_kernel<T, D><<<p.n_cta, kThreads, smem, s>>>(kmap, vmap, qmap ? *qmap : kmap, a, p, box_tokens, qmap != nullptr);
+    kv_attn_tc_kernel<T, D><<<p.workers, kThreads, smem, s>>>(kmap, vmap, qmap ? *qmap : kmap, a, p, box_tokens, qmap != nullptr);
     count_launches(1);
     return cudaGetLastError();
 }
