@@ -1,66 +1,10 @@
-// Attention over the paged KV pool: host entry points, the plan of a call, and the weights pass.
+// Attention over the paged KV pool: host entry points and the plan of a call.
 #include <cmath>
 
 #include "gms_internal.h"
 #include "gms_kv_attn.h"
 
 namespace gms {
-namespace {
-
-// One warp accumulates the weight of one (sequence, KV head, token), rows in order.
-template <class T, int D>
-__global__ void __launch_bounds__(128) kv_weights_kernel(AttnArgs a, const float *lse)
-{
-    constexpr int E = D / 32;
-    const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t w = (uint64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    const int t = (int)(w % a.max_kv);
-    const uint32_t c = (uint32_t)(w / a.max_kv % a.n_kv), s = (uint32_t)(w / a.max_kv / a.n_kv);
-    if (s >= a.n_seq || t >= seq_kv_len(a, s)) return;
-    const int id = a.table[s * a.table_stride + (t >> a.block_shift)];
-    const int q0 = seq_q_begin(a, s), ql = seq_q_len(a, s), first = seq_kv_len(a, s) - ql;
-    const uint64_t at = s * a.w_seq_stride + c * a.w_head_stride + t;
-    float sum = 0.f;
-    if ((uint32_t)id < a.n_blocks) {
-        const T *k = reinterpret_cast<const T *>(a.k_base + (uint64_t)id * a.block_stride +
-                                                 (uint64_t)(t & ((1 << a.block_shift) - 1)) * a.token_stride +
-                                                 (uint64_t)c * a.head_stride);
-        for (int i = 0; i < ql; ++i) {
-            if (!sees(a, first + i, t)) continue;
-            for (uint32_t h = c * a.group; h < (c + 1) * a.group; ++h) {
-                const T *q = reinterpret_cast<const T *>(a.q + (uint64_t)(q0 + i) * a.q_token_stride + (uint64_t)h * a.q_head_stride);
-                float x = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) x += to_f32(q[lane + 32 * e]) * to_f32(k[lane + 32 * e]);
-                const float ls = lse[(uint64_t)(q0 + i) * a.n_heads + h];
-                if (ls != neg_inf()) sum += exp2f((warp_sum(x) * a.scale - ls) * kLog2e);
-            }
-        }
-    }
-    if (lane == 0) a.w_out[at] = (a.w_in ? a.decay * a.w_in[at] : 0.f) + sum;
-}
-
-}  // namespace
-
-#define GMS_BY_TYPE(K, ...)                                                           \
-    do {                                                                              \
-        if (dtype == GMS_DTYPE_BF16) {                                                \
-            if (head_dim == 64) K<__nv_bfloat16, 64> __VA_ARGS__; else K<__nv_bfloat16, 128> __VA_ARGS__; \
-        } else {                                                                      \
-            if (head_dim == 64) K<__half, 64> __VA_ARGS__; else K<__half, 128> __VA_ARGS__; \
-        }                                                                             \
-    } while (0)
-
-cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
-{
-    const uint64_t warps = (uint64_t)a.n_seq * a.n_kv * a.max_kv;
-    const uint32_t grid = (uint32_t)((warps + 3) / 4);
-    if (grid == 0) return cudaSuccess;
-    GMS_BY_TYPE(kv_weights_kernel, <<<grid, 128, 0, s>>>(a, lse));
-    count_launches(1);
-    return cudaGetLastError();
-}
-
 namespace {
 
 int bad_pool(const gms_kv_pool *p)
@@ -273,7 +217,7 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     const uint64_t want = ceil_div(most_tiles(a, *p), 2), most = tc ? kTcMaxWorkers : kFewMaxWorkers;
     p->workers = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
     p->slot_rows = rows < p->rows ? (uint32_t)(rows < 1 ? 1 : rows) : p->rows;
-    if (rows_out) p->begin = c->take<uint32_t>(p->n_units + 1);
+    p->begin = c->take<uint32_t>(p->n_units + 1);
     p->cuts = c->take<Cut>(p->workers);
     p->part_ml = c->take<float2>(2ull * p->workers * p->slot_rows);
     p->part_o = c->take<float>(2ull * p->workers * p->slot_rows * head_dim);
@@ -340,12 +284,12 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         const bool tc = pl.own.rows == kTcRows || (prefix && pl.prefix.rows == kTcRows), q_tma = tc && q_boxes(a, dim);
         if (q_tma) rc = encode_q(&qmap, a, dtype, dim);
         if (rc != GMS_OK) return rc;
-        auto launch = [&](const Pass &p) {
-            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], q_tma ? &qmap : nullptr, box, dtype, dim, s)
-                                     : launch_kv_attn_few(b, p, kmap[0], vmap[0], dtype, dim, s);
+        auto launch = [&](const Pass &p, bool after_prefix) {
+            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], q_tma ? &qmap : nullptr, box, after_prefix, dtype, dim, s)
+                                     : launch_kv_attn_few(b, p, kmap[0], vmap[0], after_prefix, dtype, dim, s);
         };
-        if (prefix) e = launch(pl.prefix);
-        if (e == cudaSuccess) e = launch(pl.own);
+        if (prefix) e = launch(pl.prefix, false);
+        if (e == cudaSuccess) e = launch(pl.own, prefix);
         if (e == cudaSuccess)
             e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s) : launch_kv_attn_join(b, pl.own, dtype, dim, s);
         if (e == cudaSuccess && w && pl.logits) e = launch_kv_few_weights(b, pl.own, s);

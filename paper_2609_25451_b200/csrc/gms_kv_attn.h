@@ -56,7 +56,7 @@ struct Pass {
     uint32_t n_units, n_rt, workers;  // n_rt units a sequence (group)
     uint32_t rows, tile;   // rows a unit, tokens a tile
     uint32_t slot_rows;    // rows a slot of part_o has room for (at most `rows`)
-    uint32_t *begin;       // null, or [n_units + 1] tiles before each unit (written by CTA 0 for those who look items up)
+    uint32_t *begin;       // [n_units + 1] tiles before each unit (written by CTA 0 for the join)
     Cut *cuts;             // [workers], written by worker i for its own border
     float *part_o;         // [2 * workers][slot_rows][head_dim], not normalised
     float2 *part_ml;       // [2 * workers][slot_rows]: running maximum (base 2) and sum
@@ -88,13 +88,14 @@ cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, co
                                        cudaStream_t s);
 // Few query rows a unit (at most 16): kv_attn_few; many: kv_attn_tc.
 constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewWarps = 4, kFewMaxWorkers = 2 * 148 * kFewWarps;
-cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
-                               uint32_t head_dim, cudaStream_t s);
+// after_prefix: launched behind the prefix pass of the same call, on which it does not depend.
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix,
+                               uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 // Many query rows a unit; box_tokens: tokens a TMA box of the maps holds; qmap: null, or boxes of 64 elements x group heads
 // x 128 / group tokens of the queries.
 constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxWorkers = 148;
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+                              uint32_t box_tokens, bool after_prefix, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);
@@ -300,7 +301,7 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
             sh[THREADS / 32 + 2 * k + 1] = u;
         }
     }
-    if (p.begin && blockIdx.x == 0) {
+    if (blockIdx.x == 0) {
         uint32_t b = before;
         for (uint32_t u = u0; u < u1; ++u) {
             p.begin[u] = b;
@@ -347,6 +348,30 @@ __device__ __forceinline__ void write_cut(const Pass &p, uint32_t worker, const 
     }
     p.cuts[worker] = x;
 }
+// c += a b: one 16 x 8 x 16 product a warp; the last argument only names the type.
+__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __nv_bfloat16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __half)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
 __device__ __forceinline__ float warp_sum(float x)
 {
 #pragma unroll

@@ -17,29 +17,6 @@ using namespace ptx;
 
 constexpr int kWarps = (int)kFewWarps, kThreads = kWarps * 32;
 
-__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __nv_bfloat16)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1, __half)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
 template <int D>
 struct Few {
     static constexpr int kHalves = D / 64;
@@ -325,16 +302,19 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             }
         }
     }
+    grid_wait();  // behind a prefix pass: this kernel's end stands for both
 }
 
 template <class T, int D, bool HI>
-cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix, cudaStream_t s)
 {
     constexpr uint32_t smem = Few<D>::kSmem;
     static const cudaError_t ready =
         cudaFuncSetAttribute(kv_attn_few_kernel<T, D, HI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
-    kv_attn_few_kernel<T, D, HI><<<(p.workers + kWarps - 1) / kWarps, kThreads, smem, s>>>(kmap, vmap, a, p);
+    const uint32_t grid = (p.workers + kWarps - 1) / kWarps;
+    if (after_prefix) return launch_dependent(kv_attn_few_kernel<T, D, HI>, grid, kThreads, smem, s, kmap, vmap, a, p);
+    kv_attn_few_kernel<T, D, HI><<<grid, kThreads, smem, s>>>(kmap, vmap, a, p);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -365,17 +345,17 @@ __global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_consta
 
 }  // namespace
 
-cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
-                               uint32_t head_dim, cudaStream_t s)
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix,
+                               uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
     const bool hi = (p.prefix ? a.max_group_q : a.max_q) * a.group > 8;
     if (dtype == GMS_DTYPE_BF16) {
         if (head_dim == 64)
-            return hi ? launch<__nv_bfloat16, 64, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 64, false>(a, p, kmap, vmap, s);
-        return hi ? launch<__nv_bfloat16, 128, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 128, false>(a, p, kmap, vmap, s);
+            return hi ? launch<__nv_bfloat16, 64, true>(a, p, kmap, vmap, after_prefix, s) : launch<__nv_bfloat16, 64, false>(a, p, kmap, vmap, after_prefix, s);
+        return hi ? launch<__nv_bfloat16, 128, true>(a, p, kmap, vmap, after_prefix, s) : launch<__nv_bfloat16, 128, false>(a, p, kmap, vmap, after_prefix, s);
     }
-    if (head_dim == 64) return hi ? launch<__half, 64, true>(a, p, kmap, vmap, s) : launch<__half, 64, false>(a, p, kmap, vmap, s);
-    return hi ? launch<__half, 128, true>(a, p, kmap, vmap, s) : launch<__half, 128, false>(a, p, kmap, vmap, s);
+    if (head_dim == 64) return hi ? launch<__half, 64, true>(a, p, kmap, vmap, after_prefix, s) : launch<__half, 64, false>(a, p, kmap, vmap, after_prefix, s);
+    return hi ? launch<__half, 128, true>(a, p, kmap, vmap, after_prefix, s) : launch<__half, 128, false>(a, p, kmap, vmap, after_prefix, s);
 }
 
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s)

@@ -81,11 +81,13 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int t
     }
 }
 
-// Also: rows of units that see nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
-// Block (i, part): the item into which the border before worker i falls, if that is its first border.
+// A block does `rows_a_block` rows (part `part` of them) of one cut item: of item i (by_item: fewer items than borders), or of
+// the item into which the border before worker i + 1 falls, if that is its first border.  Also: rows of units that see
+// nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
 template <class T, int D, int ROWS, int TILE>
 __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
-                                                                   uint32_t parts)
+                                                                   uint32_t parts, uint32_t rows_a_block,
+                                                                   uint32_t by_item)
 {
     grid_launch_dependents();
     for (uint32_t x = blockIdx.x; x < p.n_units; x += gridDim.x) {  // while the attention kernel still runs
@@ -101,7 +103,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
         }
     }
     grid_wait();
-    const uint32_t i = blockIdx.x / parts + 1, part = blockIdx.x % parts, warp = threadIdx.x / 32;
+    const uint32_t i = blockIdx.x / parts, row_first = blockIdx.x % parts * rows_a_block, warp = threadIdx.x / 32;
     if (p.redo) {  // rows of finished items that came out non-finite; a cut item's words are zero
         for (uint32_t w = blockIdx.x * kWarps + warp; w < p.n_units * a.n_kv; w += gridDim.x * kWarps) {
             const uint32_t unit = w / a.n_kv;
@@ -116,11 +118,24 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
                 }
         }
     }
-    if (i >= p.workers) return;  // only here for the above
-    const Cut x = p.cuts[i];
-    if (x.c1 == 0 || x.c0 + 1 != i) return;  // the border lies between two items, or is not the item's first
+    Cut x;
+    if (by_item) {
+        const uint32_t unit = i / a.n_kv, first_tile = p.begin[unit], all = p.begin[unit + 1] - first_tile, total = p.begin[p.n_units];
+        if (all == 0) return;
+        const uint32_t n = used_workers(total, p.workers), per = total / n, more = total - per * n, tiles = all / a.n_kv;
+        x.c = i % a.n_kv;
+        x.c0 = tile_owner(first_tile + x.c * tiles, per, more);
+        x.c1 = tile_owner(first_tile + x.c * tiles + tiles - 1, per, more);
+        if (x.c0 == x.c1) return;
+        const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+        x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows;
+    } else {
+        if (i + 1 >= p.workers) return;
+        x = p.cuts[i + 1];
+        if (x.c1 == 0 || x.c0 != i) return;  // the border lies between two items, or is not the item's first
+    }
     // few rows: several warps share a row's pieces
-    const uint32_t here = min((uint32_t)max(x.rows - (int)(part * kFewRows), 0), kFewRows);  // rows of this block
+    const uint32_t here = min((uint32_t)max(x.rows - (int)row_first, 0), rows_a_block);  // rows of this block
     const uint32_t share = here == 0 || here >= kWarps ? 1 : kWarps / here;
     __shared__ float m_sh[kWarps], l_sh[kWarps];
     __shared__ float o_sh[kWarps][D];
@@ -130,7 +145,7 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
         const uint32_t r = warp % here, g = warp / here;
         if (g < share)
             add_pieces<D>(sum, p.part_ml, p.part_o, g, share, x.c1 - x.c0 + 1,
-                          [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + part * kFewRows + r; });
+                          [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
         if (lane == 0) m_sh[warp] = sum.m, l_sh[warp] = sum.l;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) o_sh[warp][lane * (D / 32) + e] = sum.o[e];
@@ -144,15 +159,15 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
 #pragma unroll
             for (int e = 0; e < D / 32; ++e) sum.o[e] = sum.o[e] * f1 + o_sh[other][lane * (D / 32) + e] * f2;
         }
-        const int row = x.row0 + (int)(part * kFewRows + warp);
+        const int row = x.row0 + (int)(row_first + warp);
         finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
         return;
     }
     for (uint32_t r = warp; r < here; r += kWarps) {
         Row<D> sum;
         add_pieces<D>(sum, p.part_ml, p.part_o, 0, 1, x.c1 - x.c0 + 1,
-                      [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + part * kFewRows + r; });
-        const int row = x.row0 + (int)(part * kFewRows + r);
+                      [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
+        const int row = x.row0 + (int)(row_first + r);
         finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
     }
 }
@@ -215,10 +230,15 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
 
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
-    const uint32_t cuts = p.workers < 2 ? 1 : p.workers - 1, parts = p.rows / kFewRows;
+    const uint32_t borders = p.workers < 2 ? 1 : p.workers - 1;
+    const uint64_t items = (uint64_t)p.n_units * a.n_kv;
+    const uint32_t by_item = items <= borders;
+    // sixteen rows a block; one row a block, its pieces spread over all warps, where an item is in many pieces
+    const uint32_t rows_a_block = by_item && p.workers / items >= 16 && p.slot_rows <= kFewRows ? 1 : kFewRows;
+    const uint32_t parts = (p.slot_rows + rows_a_block - 1) / rows_a_block, grid = (by_item ? (uint32_t)items : borders) * parts;
     if (p.rows == kTcRows)
-        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));
-    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, cuts * parts, kWarps * 32, 0, s, a, p, parts)));
+        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)));
+    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)));
 }
 
 cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &pre, const Pass &own, uint32_t dtype, uint32_t head_dim, cudaStream_t s)

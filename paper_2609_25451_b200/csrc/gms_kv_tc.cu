@@ -41,7 +41,7 @@ struct Tc {
     static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;  // a K, V or Q tile
     static constexpr int kStages = D == 128 ? 4 : 8;
     static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 2 * kSegments) * 8;
-    static constexpr uint32_t kOutBytes = 8 * 2048;               // 32 rows x 64 bytes a softmax warp, for coalesced stores
+    static constexpr uint32_t kOutBytes = 8 * 4096;               // 32 rows x 128 bytes a softmax warp, for coalesced stores
     static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 128 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
     static constexpr uint32_t kCols = 512;
@@ -74,16 +74,6 @@ __device__ __forceinline__ int seg_tile(const Segment &g, int k)
 template <class T> struct IsBf16 { static constexpr bool value = false; };
 template <> struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
 // Changes the sign of (or clears) two packed 16-bit values.
 __device__ __forceinline__ uint4 with_sign(uint4 v, uint32_t flip, uint32_t keep)
 {
@@ -511,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             if (finished) {
                 // through shared memory, so that four lanes write 64 bytes of a row at a time
                 const uint64_t at = tok * a.out_token_stride + h * a.out_head_stride;
-                uint8_t *stage = sm + (2 + NS) * F::kTileBytes + warp * 2048;
+                uint8_t *stage = sm + (2 + NS) * F::kTileBytes + warp * 4096;
                 if (live && a.lse) a.lse[tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
                 const uint32_t rows_here = (uint32_t)max(0, min(32, rows - slot * 128 - (int)(warp % 4) * 32));
 #pragma unroll
@@ -543,17 +533,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 }
             } else {
                 const uint64_t at = mine ? tok * a.n_heads + h : ((uint64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * p.slot_rows + row;
-                float *dst = (mine ? p.row_o : p.part_o) + at * D;
+                float *dst = mine ? p.row_o : p.part_o;
+                uint8_t *stage = sm + (2 + NS) * F::kTileBytes + warp * 4096;
                 if (live) (mine ? p.row_ml : p.part_ml)[at] = make_float2(m, l);
-#pragma unroll
+                const uint32_t rows_here = (uint32_t)max(0, min(32, rows - slot * 128 - (int)(warp % 4) * 32));
+#pragma unroll 1
                 for (int i = 0; i < D / 32; ++i) {
                     uint32_t o[32];
                     tmem_ld32(o_col + i * 32, o);
                     tmem_wait32(o);
-                    if (live)
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            *reinterpret_cast<uint4 *>(dst + i * 32 + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t r = e * 4 + lane / 8, ch = lane & 7u;
+                        const uint64_t to = __shfl_sync(0xffffffffu, at, r);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((ch ^ (r & 7)) << 4));
+                        if (r < rows_here) *reinterpret_cast<uint4 *>(dst + to * D + i * 32 + ch * 4) = v;
+                    }
+                    __syncwarp();
                 }
             }
             tc_fence_before();
@@ -572,16 +572,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         tc_fence_after();
         tmem_free(tmem, F::kCols);
     }
+    grid_wait();  // behind a prefix pass: this kernel's end stands for both
 }
 
 template <class T, int D>
 cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                   uint32_t box_tokens, cudaStream_t s)
+                   uint32_t box_tokens, bool after_prefix, cudaStream_t s)
 {
     constexpr uint32_t smem = Tc<D>::kSmem;
     static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
-    kv_attn_tc_kernel<T, D><<<p.workers, kThreads, smem, s>>>(kmap, vmap, qmap ? *qmap : kmap, a, p, box_tokens, qmap != nullptr);
+    const CUtensorMap &qm = qmap ? *qmap : kmap;
+    const uint32_t q_tma = qmap != nullptr;
+    if (after_prefix) return launch_dependent(kv_attn_tc_kernel<T, D>, p.workers, kThreads, smem, s, kmap, vmap, qm, a, p, box_tokens, q_tma);
+    kv_attn_tc_kernel<T, D><<<p.workers, kThreads, smem, s>>>(kmap, vmap, qm, a, p, box_tokens, q_tma);
     count_launches(1);
     return cudaGetLastError();
 }
@@ -589,12 +593,12 @@ cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, co
 }  // namespace
 
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+                              uint32_t box_tokens, bool after_prefix, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
     if (dtype == GMS_DTYPE_BF16)
-        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, qmap, box_tokens, s)
-                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
-    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, qmap, box_tokens, s) : launch<__half, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
+        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s)
+                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s);
+    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s) : launch<__half, 128>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s);
 }
 
 }  // namespace gms

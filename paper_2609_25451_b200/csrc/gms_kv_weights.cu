@@ -1,0 +1,141 @@
+// Accumulated attention weights where the logits were not kept (many query rows): a second pass over the keys alone.
+//
+//   out[t] = decay * in[t] + sum over rows r that see t of 2^(c q_r.k_t - lse2_r)
+//
+// A CTA owns 128 tokens of one sequence and KV head: every warp keeps 32 tokens' keys in registers as matrix fragments and
+// walks all query rows, 64 at a time through shared memory (S^T = K Q^T, so a token's sum stays in a quad of lanes).  Each sum
+// has one owner and one order: no atomics, equal calls give equal bits.  Bound by the exponentials and the matrix unit for
+// many rows, by reading K for few.
+#include "gms_internal.h"
+#include "gms_kv_attn.h"
+#include "gms_ptx.h"
+
+namespace gms {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 4, kThreads = kWarps * 32, kTokens = kWarps * 32, kRows = 64;
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_constant__ AttnArgs a, const float *lse, uint32_t chunks)
+{
+    constexpr int kStride = D / 2 + 4;  // words a row: rows of a fragment fall into different banks
+    __shared__ uint32_t q_sh[kRows][kStride];
+    __shared__ float lse_sh[kRows];
+    __shared__ int pos_sh[kRows];
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t item = blockIdx.x / chunks, c = item % a.n_kv, s = item / a.n_kv;
+    const int t0 = (int)(blockIdx.x % chunks) * kTokens, n = seq_kv_len(a, s);
+    if (t0 >= n) return;
+    const int q0 = seq_q_begin(a, s), rows = seq_q_len(a, s) * (int)a.group, first = n - seq_q_len(a, s);
+    const float c2 = a.scale * kLog2e;
+
+    // keys of tokens base + lane/4 + 8 i, i < 4, as two 16-row fragments; tokens that nobody can see stay zero
+    const int base = t0 + (int)warp * 32 + (int)lane / 4;
+    uint32_t k[2][D / 16][4];
+    uint32_t seen = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = base + 8 * i;
+        const int id = t < n ? a.table[s * a.table_stride + ((uint32_t)t >> a.block_shift)] : -1;
+        const bool on = (uint32_t)id < a.n_blocks;
+        seen |= on ? 1u << i : 0u;
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(a.k_base + (on ? (uint64_t)id * a.block_stride : 0) +
+                                                               (uint64_t)((uint32_t)t & ((1u << a.block_shift) - 1u)) * a.token_stride +
+                                                               (uint64_t)c * a.head_stride) + (lane & 3u);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            k[i / 2][kk][i % 2] = on ? p[kk * 8] : 0u;
+            k[i / 2][kk][i % 2 + 2] = on ? p[kk * 8 + 4] : 0u;
+        }
+    }
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const int t_last = min(t0 + kTokens, n) - 1;
+    for (int r0 = 0; r0 < rows; r0 += kRows) {
+        const int here = min(kRows, rows - r0), p_min = first + r0 / (int)a.group, p_max = first + (r0 + here - 1) / (int)a.group;
+        if (p_max < t0) continue;  // all of these rows come before all of these tokens
+        if (a.window && p_min >= 0 && (uint32_t)p_min >= a.window && t_last <= p_min - (int)a.window && (uint32_t)t0 >= a.sinks) continue;
+        __syncthreads();
+        for (int x = (int)tid; x < kRows * (D / 8); x += kThreads) {
+            const int r = x / (D / 8), ch = x % (D / 8), row = r0 + r;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < here)
+                v = *reinterpret_cast<const uint4 *>(a.q + (uint64_t)(q0 + row / (int)a.group) * a.q_token_stride +
+                                                     (uint64_t)(c * a.group + (uint32_t)row % a.group) * a.q_head_stride + ch * 16);
+            *reinterpret_cast<uint4 *>(&q_sh[r][ch * 4]) = v;
+        }
+        if (tid < kRows) {
+            const int row = r0 + (int)tid;
+            float x = __int_as_float(0x7f800000);  // rows that do not exist or see nothing: weight 0
+            if ((int)tid < here) x = lse[(uint64_t)(q0 + row / (int)a.group) * a.n_heads + c * a.group + (uint32_t)row % a.group] * kLog2e;
+            lse_sh[tid] = x == neg_inf() ? -x : x;
+            pos_sh[tid] = first + row / (int)a.group;
+        }
+        __syncthreads();
+        const bool whole = t_last <= p_min && seen == 15u &&
+                           (a.window == 0 || p_max < 0 || (uint32_t)p_max < a.window || t0 > p_max - (int)a.window || (uint32_t)t_last < a.sinks);
+        const bool all_whole = __all_sync(0xffffffffu, whole);
+        for (int j = 0; j < here; j += 8) {
+            float acc[2][4];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
+            const uint32_t *qp = &q_sh[j + lane / 4][lane & 3u];
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t b0 = qp[kk * 8], b1 = qp[kk * 8 + 4];
+                mma16816(acc[0], k[0][kk], b0, b1, T());
+                mma16816(acc[1], k[1][kk], b0, b1, T());
+            }
+            const int r = j + (int)(lane & 3u) * 2;
+            const float l0 = lse_sh[r], l1 = lse_sh[r + 1];
+            if (all_whole) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    sum[2 * m] += ex2(fmaf(acc[m][0], c2, -l0)) + ex2(fmaf(acc[m][1], c2, -l1));
+                    sum[2 * m + 1] += ex2(fmaf(acc[m][2], c2, -l0)) + ex2(fmaf(acc[m][3], c2, -l1));
+                }
+            } else {
+                const int p0 = pos_sh[r], p1 = pos_sh[r + 1];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = base + 8 * i;
+                    if (!(seen >> i & 1u)) continue;
+                    if (r < here && sees(a, p0, t)) sum[i] += ex2(fmaf(acc[i / 2][(i % 2) * 2], c2, -l0));
+                    if (r + 1 < here && sees(a, p1, t)) sum[i] += ex2(fmaf(acc[i / 2][(i % 2) * 2 + 1], c2, -l1));
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+        sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+        const int t = base + 8 * i;
+        if ((lane & 3u) == (uint32_t)i && t < n) {
+            const uint64_t at = s * a.w_seq_stride + c * a.w_head_stride + t;
+            a.w_out[at] = (a.w_in ? a.decay * a.w_in[at] : 0.f) + sum[i];
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+{
+    const uint32_t chunks = (a.max_kv + kTokens - 1) / kTokens, grid = a.n_seq * a.n_kv * chunks;
+    if (grid == 0) return cudaSuccess;
+    if (dtype == GMS_DTYPE_BF16) {
+        if (head_dim == 64) kv_weights_kernel<__nv_bfloat16, 64><<<grid, kThreads, 0, s>>>(a, lse, chunks);
+        else kv_weights_kernel<__nv_bfloat16, 128><<<grid, kThreads, 0, s>>>(a, lse, chunks);
+    } else {
+        if (head_dim == 64) kv_weights_kernel<__half, 64><<<grid, kThreads, 0, s>>>(a, lse, chunks);
+        else kv_weights_kernel<__half, 128><<<grid, kThreads, 0, s>>>(a, lse, chunks);
+    }
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+}  // namespace gms
