@@ -198,7 +198,7 @@ uint64_t most_tiles(const AttnArgs &a, const Pass &p)
         const uint64_t seen = (uint64_t)a.window + a.sinks + 2 * p.tile + (p.rows - 1) / a.group;
         if (seen < span) span = seen;
     }
-    return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * ceil_div(span, p.tile);
+    return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * (ceil_div(span, p.tile) + (p.tile == kTcTile ? kTcExtra : 0));
 }
 
 void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)

@@ -43,7 +43,9 @@ struct AttnArgs {
 // inside a token) of one sequence (or, in a prefix pass, of one group); an item is a unit for one KV head; an item's work
 // is the list of token tiles that at least one of its rows sees.  All items' tiles, one after the other, are dealt out
 // evenly: worker i of n (n = workers, or T if that is less) gets T / n or T / n + 1 tiles, whatever items they fall into, so
-// ragged lengths cost no balance.  A worker is a CTA of the many-row kernel, a warp of the few-row kernel.  An item that one
+// ragged lengths cost no balance.  (Of the many-row kernel's items each counts kTcExtra tiles more, which stand for loading Q
+// and writing the result: without them the worker with 38 short items of a windowed prompt took 1.2 times the others' time.)
+// A worker is a CTA of the many-row kernel, a warp of the few-row kernel.  An item that one
 // worker has whole is finished there; the at most two pieces a worker has of others go to its two slots of part_o / part_ml
 // and are joined by kv_attn_join.
 struct Cut {               // the item into which the border before worker i falls (c1 = 0: the border lies between items)
@@ -93,7 +95,7 @@ cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorM
                                uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 // Many query rows a unit; box_tokens: tokens a TMA box of the maps holds; qmap: null, or boxes of 64 elements x group heads
 // x 128 / group tokens of the queries.
-constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxWorkers = 148;
+constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxWorkers = 148, kTcExtra = 2;
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
                               uint32_t box_tokens, bool after_prefix, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
@@ -239,6 +241,11 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
     }
     return u;
 }
+// What an item counts in the deal: its tiles come after kTcExtra (many-row kernel) that stand for its fixed cost.
+template <int TILE>
+__device__ __forceinline__ uint32_t item_extra() { return TILE == (int)kTcTile ? kTcExtra : 0; }
+template <int TILE>
+__device__ __forceinline__ uint32_t item_cost(int tiles) { return tiles ? (uint32_t)tiles + item_extra<TILE>() : 0; }
 // The part of the work that a worker has, item by item.
 struct Walk {
     uint32_t pos, end;   // tiles still to do, in the order over all items
@@ -262,7 +269,7 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32, worker = WORKERS > 1 ? warp : 0;
     const uint32_t per = (p.n_units + THREADS - 1) / THREADS, u0 = min(tid * per, p.n_units), u1 = min(u0 + per, p.n_units);
     auto tiles_of = [&](uint32_t u) {
-        return (uint32_t)get_unit<ROWS, TILE>(a, p, p.n_rt > 1 ? u / p.n_rt : u, p.n_rt > 1 ? u % p.n_rt : 0).tiles * a.n_kv;
+        return item_cost<TILE>(get_unit<ROWS, TILE>(a, p, p.n_rt > 1 ? u / p.n_rt : u, p.n_rt > 1 ? u % p.n_rt : 0).tiles) * a.n_kv;
     };
     uint32_t mine = 0;
     for (uint32_t u = u0; u < u1; ++u) mine += tiles_of(u);
@@ -319,32 +326,42 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
     }
     return w;
 }
-// Unit and KV head in which the walk stands, and the first tile of its list that is the worker's.
+// The next run of tiles k0 .. k1-1 of one item (unit u, KV head c) that is the worker's; false: no more.  `at` is the place of
+// the item's tile 0 in the order over all items.
 template <int ROWS, int TILE>
-__device__ __forceinline__ Unit walk_item(const AttnArgs &a, const Pass &p, Walk &w, uint32_t *c, uint32_t *k0)
+__device__ __forceinline__ bool walk_next(const AttnArgs &a, const Pass &p, Walk &w, Unit &u, uint32_t &c, int &k0, int &k1, uint32_t &at,
+                                          uint32_t &item)
 {
-    Unit u;
-    for (;;) {
-        u = get_unit<ROWS, TILE>(a, p, w.s, w.rt);
-        const uint32_t t = (uint32_t)u.tiles * a.n_kv;
-        if (w.pos < w.base + t) break;
-        w.base += t;
-        if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+    constexpr int E = TILE == (int)kTcTile ? (int)kTcExtra : 0;
+    while (w.pos < w.end) {
+        uint32_t size;
+        for (;;) {
+            u = get_unit<ROWS, TILE>(a, p, w.s, w.rt);
+            size = item_cost<TILE>(u.tiles);
+            if (w.pos < w.base + size * a.n_kv) break;
+            w.base += size * a.n_kv;
+            if (++w.rt == p.n_rt) w.rt = 0, ++w.s;
+        }
+        const uint32_t in = w.pos - w.base;
+        c = a.n_kv > 1 ? in / size : 0;
+        const uint32_t from = in - c * size, to = min(size, from + (w.end - w.pos));
+        at = w.pos - from + E;
+        item = (w.s * p.n_rt + w.rt) * a.n_kv + c;
+        w.pos += to - from;
+        k0 = max((int)from - E, 0);
+        k1 = (int)to - E;
+        if (k1 > k0) return true;
     }
-    const uint32_t in = w.pos - w.base;
-    *c = a.n_kv > 1 ? in / (uint32_t)u.tiles : 0;
-    *k0 = in - *c * (uint32_t)u.tiles;
-    return u;
+    return false;
 }
-// One thread of a worker, for the border before its share: what the join needs to know.
-__device__ __forceinline__ void write_cut(const Pass &p, uint32_t worker, const Walk &w, const Unit &u, uint32_t c, uint32_t k0)
+// One thread of a worker, for the border before its share (its first run of tiles): what the join needs to know.
+__device__ __forceinline__ void write_cut(const Pass &p, uint32_t worker, const Walk &w, const Unit &u, uint32_t c, int k0, uint32_t at)
 {
     Cut x = {};
-    if (w.pos < w.end && k0) {
-        const uint32_t first = w.pos - k0;
+    if (k0 > 0) {
         x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows, x.c = c;
-        x.c0 = tile_owner(first, w.per, w.more);
-        x.c1 = tile_owner(first + u.tiles - 1, w.per, w.more);
+        x.c0 = tile_owner(at, w.per, w.more);
+        x.c1 = tile_owner(at + u.tiles - 1, w.per, w.more);
     }
     p.cuts[worker] = x;
 }

@@ -69,13 +69,11 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     int k0 = 0, k1 = 0;          // the warp's tiles of the item's list
     int ids = 0, ids_old = 0;    // block ids of tiles 32b + lane: current and previous batch
 
+    uint32_t at = 0, item = 0, seq = 0;
     auto segment = [&]() -> bool {  // the next run of tiles of one item
-        if (w.pos >= w.end) return false;
-        uint32_t k;
-        un = walk_item<kFewRows, kFewTile>(a, p, w, &c, &k);
-        k0 = (int)k;
-        k1 = (int)min((uint32_t)un.tiles, k + (w.end - w.pos));
-        return true;
+        const bool more = walk_next<kFewRows, kFewTile>(a, p, w, un, c, k0, k1, at, item);
+        seq = w.s;
+        return more;
     };
     auto issue = [&](int i) {  // i: index among the warp's tiles
         if ((i & 31) == 0) {
@@ -101,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     bool live = segment();
     if (live)
         for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);
-    if (lane == 0 && worker < p.workers) write_cut(p, worker, w, un, c, (uint32_t)k0);
+    if (lane == 0 && worker < p.workers) write_cut(p, worker, w, un, c, live ? k0 : 0, at);
     while (live) {
         const int nt = k1 - k0;
         const int r0 = lane / 4, r1 = r0 + 8;
@@ -185,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 __syncwarp();
             }
             if (p.logits) {
-                float *lp = p.logits + ((uint64_t)w.s * a.n_kv + c) * a.max_q * a.group * p.logit_stride;
+                float *lp = p.logits + ((uint64_t)seq * a.n_kv + c) * a.max_q * a.group * p.logit_stride;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t t = t0 + j * 8 + (lane & 3u) * 2;
@@ -251,7 +249,6 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
         const Unit done = un;
         const uint32_t dc = c;
         const bool starts = k0 == 0, ends = k1 == un.tiles;
-        w.pos += (uint32_t)(k1 - k0);
         live = segment();
         if (live && !failed)  // the next item's first tiles are on their way while this one is joined
             for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);

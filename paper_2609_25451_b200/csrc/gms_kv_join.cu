@@ -122,10 +122,10 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     if (by_item) {
         const uint32_t unit = i / a.n_kv, first_tile = p.begin[unit], all = p.begin[unit + 1] - first_tile, total = p.begin[p.n_units];
         if (all == 0) return;
-        const uint32_t n = used_workers(total, p.workers), per = total / n, more = total - per * n, tiles = all / a.n_kv;
+        const uint32_t n = used_workers(total, p.workers), per = total / n, more = total - per * n, size = all / a.n_kv, extra = item_extra<TILE>();
         x.c = i % a.n_kv;
-        x.c0 = tile_owner(first_tile + x.c * tiles, per, more);
-        x.c1 = tile_owner(first_tile + x.c * tiles + tiles - 1, per, more);
+        x.c0 = tile_owner(first_tile + x.c * size + extra, per, more);
+        x.c1 = tile_owner(first_tile + x.c * size + size - 1, per, more);
         if (x.c0 == x.c1) return;
         const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
         x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows;
@@ -183,7 +183,7 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (rt >= p.n_rt) return;
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
     if (u.tiles == 0 || (int)r >= u.rows) return;
-    const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * (uint32_t)u.tiles;
+    const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * item_cost<TILE>(u.tiles) + item_extra<TILE>();
     const uint32_t n = used_workers(total, p.workers), per = total / n, more = total % n;
     const uint32_t c0 = tile_owner(first, per, more), c1 = tile_owner(first + u.tiles - 1, per, more);
     if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 0, 1, 1, [&](uint32_t) { return row; });

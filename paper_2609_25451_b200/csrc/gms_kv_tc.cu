@@ -49,22 +49,16 @@ struct Tc {
 
 __device__ __forceinline__ bool next_segment(const AttnArgs &a, const Pass &p, Walk &w, Segment &g, bool first)
 {
-    g.k0 = g.k1 = 0;
-    if (w.pos >= w.end) {
-        if (first && (threadIdx.x & 31u) == 0) write_cut(p, blockIdx.x, w, Unit(), 0, 0);
-        return false;
-    }
-    uint32_t k;
-    const Unit u = walk_item<kRows, kTile>(a, p, w, &g.c, &k);
-    if (first && (threadIdx.x & 31u) == 0) write_cut(p, blockIdx.x, w, u, g.c, k);
+    Unit u = {};
+    uint32_t at = 0;
+    g.c = 0, g.k0 = g.k1 = 0;
+    const bool more = walk_next<kRows, kTile>(a, p, w, u, g.c, g.k0, g.k1, at, g.item);
+    if (!more) g.k0 = g.k1 = 0;
+    if (first && (threadIdx.x & 31u) == 0) write_cut(p, blockIdx.x, w, u, g.c, g.k0, at);
     g.table = u.table;
     g.q0 = u.q0, g.row0 = u.row0, g.rows = u.rows, g.n = u.n, g.first = u.first, g.pos_min = u.pos_min, g.pos_max = u.pos_max;
     g.n_sink_tiles = u.n_sink_tiles, g.first_tile = u.first_tile, g.tiles = u.tiles, g.whole = u.whole;
-    g.k0 = (int)k;
-    g.k1 = (int)min((uint32_t)u.tiles, k + (w.end - w.pos));
-    g.item = (w.s * p.n_rt + w.rt) * a.n_kv + g.c;
-    w.pos += (uint32_t)(g.k1 - g.k0);
-    return true;
+    return more;
 }
 __device__ __forceinline__ int seg_tile(const Segment &g, int k)
 {
@@ -370,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 mbar_arrive(q_full + 8 * slot);
             }
 
-            const bool live = row < rows;
+            const bool live = row < rows, busy = slot * 128 + (int)(warp % 4) * 32 < rows;  // a warp without rows computes nothing
             const int pos = pos_of(live ? row : rows - 1), pos_lo = pos_of(slot * 128), pos_hi = pos_of(min(slot * 128 + 127, rows - 1));
             const int32_t *table = g.table;
             // the row's window starts at low; low_hi: the latest start among the slot's rows; sink: tokens always seen
@@ -383,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             auto step = [&](const int half, const bool edge, int k, int t0, uint32_t valid) {
                 if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) return;
                 tc_fence_after();
+                if (busy) {
                 uint32_t s[2][32];
                 tmem_ld32(s_col + half * 64, s[0]);
                 tmem_ld32(s_col + half * 64 + 32, s[1]);
@@ -447,6 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 tmem_st32(s_col + half * 64, pk);
                 part[0] = add2(part[0], part[1]);
                 l += part[0].x + part[0].y;
+                }
                 // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
                 // of the unit sees, where rows are not done again.  Thread r of each slot clears token r of the tile before
                 // its slot's first half is handed over (the other slot may clear it too: the same zeros).

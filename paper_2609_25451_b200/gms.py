@@ -199,11 +199,20 @@ def _dev(x):
     return int(x)
 
 
+_cuda_seen = False
+
+
 def _stream(stream):
+    global _cuda_seen
     if stream is None:
         import torch
 
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        if not _cuda_seen:
+            if not torch.cuda.is_available():
+                return None
+            _cuda_seen = True
+        # the address alone: building the Stream object costs 3 us a call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return getattr(stream, "cuda_stream", stream)
 
 
