@@ -201,12 +201,10 @@ uint64_t most_tiles(const AttnArgs &a, const Pass &p)
     return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * (ceil_div(span, p.tile) + (p.tile == kTcTile ? kTcExtra : 0));
 }
 
-void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
+void cut_pass(const AttnArgs &a, bool prefix, bool tc, Pass *p)
 {
-    *p = {};
     const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
     p->prefix = prefix;
-    const bool tc = rows > kFewRows;
     p->rows = tc ? kTcRows : kFewRows;
     p->tile = tc ? kTcTile : kFewTile;
     p->n_rt = (uint32_t)ceil_div(rows, p->rows);
@@ -217,6 +215,20 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     const uint64_t want = ceil_div(most_tiles(a, *p), 2), most = tc ? kTcMaxWorkers : kFewMaxWorkers;
     p->workers = (uint32_t)(want < 1 ? 1 : want < most ? want : most);
     p->slot_rows = rows < p->rows ? (uint32_t)(rows < 1 ? 1 : rows) : p->rows;
+}
+
+void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
+{
+    *p = {};
+    const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
+    // Up to 16 rows a KV head: the few-row kernel, which reads K and V once.  More: the tensor-core kernel reads them once for
+    // 256 rows, but takes 8 us longer to get going (its Q, descriptors and tensor memory; 16 us against 8 us for one tile), so
+    // short calls of up to 64 rows go to the few-row kernel all the same, 16 rows at a time: where no warp gets more than four
+    // of its tiles (three suffixes of 40 behind a prefix of 129 tokens, 24 rows: YY us against 23 us).
+    bool tc = rows > kFewRows;
+    cut_pass(a, prefix, false, p);
+    if (tc && rows <= 64 && most_tiles(a, *p) <= 4ull * kFewMaxWorkers) tc = false;
+    if (tc) cut_pass(a, prefix, true, p);
     p->begin = c->take<uint32_t>(p->n_units + 1);
     p->cuts = c->take<Cut>(p->workers);
     p->part_ml = c->take<float2>(2ull * p->workers * p->slot_rows);
@@ -239,7 +251,7 @@ int plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace
     pl->lse = a.lse;
     if (a.w_out) {
         if (!a.lse) pl->lse = c.take<float>((uint64_t)a.total_q * a.n_heads);
-        if (pl->own.rows == kFewRows) {
+        if (pl->own.rows == kFewRows && pl->own.n_rt == 1) {
             pl->logits = true;
             pl->own.logit_stride = (a.max_kv + kFewTile - 1) / kFewTile * kFewTile;
             pl->own.logits = c.take<float>((uint64_t)a.n_seq * a.n_heads * a.max_q * pl->own.logit_stride);

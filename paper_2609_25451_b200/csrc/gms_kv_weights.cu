@@ -20,36 +20,45 @@ constexpr int kWarps = 4, kThreads = kWarps * 32, kTokens = kWarps * 32, kRows =
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_constant__ AttnArgs a, const float *lse, uint32_t chunks)
 {
-    constexpr int kStride = D / 2 + 4;  // words a row: rows of a fragment fall into different banks
-    __shared__ uint32_t q_sh[kRows][kStride];
+    constexpr int kChunks = D / 8, kStride = D * 2 + 16;  // 16-byte pieces of a row; bytes between rows (no bank conflicts)
+    __shared__ __align__(16) uint8_t rows_sh[kTokens * kStride];  // the keys, then the queries
     __shared__ float lse_sh[kRows];
-    __shared__ int pos_sh[kRows];
+    __shared__ int pos_sh[kRows], id_sh[kTokens];
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
     const uint32_t item = blockIdx.x / chunks, c = item % a.n_kv, s = item / a.n_kv;
     const int t0 = (int)(blockIdx.x % chunks) * kTokens, n = seq_kv_len(a, s);
-    if (t0 >= n) return;
+    if (t0 >= n) {
+        grid_wait();
+        return;
+    }
     const int q0 = seq_q_begin(a, s), rows = seq_q_len(a, s) * (int)a.group, first = n - seq_q_len(a, s);
     const float c2 = a.scale * kLog2e;
 
-    // keys of tokens base + lane/4 + 8 i, i < 4, as two 16-row fragments; tokens that nobody can see stay zero
+    id_sh[tid] = t0 + (int)tid < n ? a.table[s * a.table_stride + ((uint32_t)(t0 + (int)tid) >> a.block_shift)] : -1;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTokens * kChunks / kThreads; ++i) {  // tokens that nobody can see stay zero
+        const int x = i * kThreads + (int)tid, r = x / kChunks, ch = x % kChunks, id = id_sh[r];
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if ((uint32_t)id < a.n_blocks)
+            v = *reinterpret_cast<const uint4 *>(a.k_base + (uint64_t)id * a.block_stride +
+                                                 (uint64_t)((uint32_t)(t0 + r) & ((1u << a.block_shift) - 1u)) * a.token_stride +
+                                                 (uint64_t)c * a.head_stride + ch * 16);
+        *reinterpret_cast<uint4 *>(rows_sh + r * kStride + ch * 16) = v;
+    }
+    __syncthreads();
+    // keys of tokens base + lane/4 + 8 i, i < 4, as two 16-row fragments
     const int base = t0 + (int)warp * 32 + (int)lane / 4;
     uint32_t k[2][D / 16][4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+            ldmatrix_x4(smem_u32(rows_sh) + (warp * 32 + m * 16 + (lane & 15u)) * kStride + (kk * 2 + (lane >> 4)) * 16, k[m][kk]);
     uint32_t seen = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = base + 8 * i;
-        const int id = t < n ? a.table[s * a.table_stride + ((uint32_t)t >> a.block_shift)] : -1;
-        const bool on = (uint32_t)id < a.n_blocks;
-        seen |= on ? 1u << i : 0u;
-        const uint32_t *p = reinterpret_cast<const uint32_t *>(a.k_base + (on ? (uint64_t)id * a.block_stride : 0) +
-                                                               (uint64_t)((uint32_t)t & ((1u << a.block_shift) - 1u)) * a.token_stride +
-                                                               (uint64_t)c * a.head_stride) + (lane & 3u);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-            k[i / 2][kk][i % 2] = on ? p[kk * 8] : 0u;
-            k[i / 2][kk][i % 2 + 2] = on ? p[kk * 8 + 4] : 0u;
-        }
-    }
+    for (int i = 0; i < 4; ++i) seen |= (uint32_t)id_sh[base - t0 + 8 * i] < a.n_blocks ? 1u << i : 0u;
+    grid_wait();  // the log-sum-exps are there
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     const int t_last = min(t0 + kTokens, n) - 1;
     for (int r0 = 0; r0 < rows; r0 += kRows) {
@@ -57,13 +66,14 @@ __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_const
         if (p_max < t0) continue;  // all of these rows come before all of these tokens
         if (a.window && p_min >= 0 && (uint32_t)p_min >= a.window && t_last <= p_min - (int)a.window && (uint32_t)t0 >= a.sinks) continue;
         __syncthreads();
-        for (int x = (int)tid; x < kRows * (D / 8); x += kThreads) {
-            const int r = x / (D / 8), ch = x % (D / 8), row = r0 + r;
+#pragma unroll
+        for (int i = 0; i < kRows * kChunks / kThreads; ++i) {
+            const int x = i * kThreads + (int)tid, r = x / kChunks, ch = x % kChunks, row = r0 + r;
             uint4 v = make_uint4(0, 0, 0, 0);
             if (r < here)
                 v = *reinterpret_cast<const uint4 *>(a.q + (uint64_t)(q0 + row / (int)a.group) * a.q_token_stride +
                                                      (uint64_t)(c * a.group + (uint32_t)row % a.group) * a.q_head_stride + ch * 16);
-            *reinterpret_cast<uint4 *>(&q_sh[r][ch * 4]) = v;
+            *reinterpret_cast<uint4 *>(rows_sh + r * kStride + ch * 16) = v;
         }
         if (tid < kRows) {
             const int row = r0 + (int)tid;
@@ -82,12 +92,15 @@ __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_const
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
-            const uint32_t *qp = &q_sh[j + lane / 4][lane & 3u];
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t b0 = qp[kk * 8], b1 = qp[kk * 8 + 4];
-                mma16816(acc[0], k[0][kk], b0, b1, T());
-                mma16816(acc[1], k[1][kk], b0, b1, T());
+            for (int kk = 0; kk < D / 16; kk += 2) {
+                uint32_t b[4];
+                ldmatrix_x4(smem_u32(rows_sh) + (j + (lane & 7u)) * kStride + (kk * 2 + (lane >> 3)) * 16, b);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    mma16816(acc[m], k[m][kk], b[0], b[1], T());
+                    mma16816(acc[m], k[m][kk + 1], b[2], b[3], T());
+                }
             }
             const int r = j + (int)(lane & 3u) * 2;
             const float l0 = lse_sh[r], l1 = lse_sh[r + 1];
@@ -127,15 +140,11 @@ cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtyp
 {
     const uint32_t chunks = (a.max_kv + kTokens - 1) / kTokens, grid = a.n_seq * a.n_kv * chunks;
     if (grid == 0) return cudaSuccess;
-    if (dtype == GMS_DTYPE_BF16) {
-        if (head_dim == 64) kv_weights_kernel<__nv_bfloat16, 64><<<grid, kThreads, 0, s>>>(a, lse, chunks);
-        else kv_weights_kernel<__nv_bfloat16, 128><<<grid, kThreads, 0, s>>>(a, lse, chunks);
-    } else {
-        if (head_dim == 64) kv_weights_kernel<__half, 64><<<grid, kThreads, 0, s>>>(a, lse, chunks);
-        else kv_weights_kernel<__half, 128><<<grid, kThreads, 0, s>>>(a, lse, chunks);
-    }
-    count_launches(1);
-    return cudaGetLastError();
+    if (dtype == GMS_DTYPE_BF16)
+        return head_dim == 64 ? launch_dependent(kv_weights_kernel<__nv_bfloat16, 64>, grid, kThreads, 0, s, a, lse, chunks)
+                              : launch_dependent(kv_weights_kernel<__nv_bfloat16, 128>, grid, kThreads, 0, s, a, lse, chunks);
+    return head_dim == 64 ? launch_dependent(kv_weights_kernel<__half, 64>, grid, kThreads, 0, s, a, lse, chunks)
+                          : launch_dependent(kv_weights_kernel<__half, 128>, grid, kThreads, 0, s, a, lse, chunks);
 }
 
 }  // namespace gms
