@@ -272,6 +272,7 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
         return item_cost<TILE>(get_unit<ROWS, TILE>(a, p, p.n_rt > 1 ? u / p.n_rt : u, p.n_rt > 1 ? u % p.n_rt : 0).tiles) * a.n_kv;
     };
     uint32_t mine = 0;
+#pragma unroll 1
     for (uint32_t u = u0; u < u1; ++u) mine += tiles_of(u);
     uint32_t inc = mine;
 #pragma unroll
@@ -293,28 +294,28 @@ __device__ __forceinline__ Walk plan_walk(const AttnArgs &a, const Pass &p, uint
     w.per = n ? total / n : 0;
     w.more = total - w.per * n;
     w.pos = w.end = total;
+    uint32_t at[WORKERS];  // where each worker's share begins
 #pragma unroll
     for (uint32_t k = 0; k < WORKERS; ++k) {
-        const uint32_t i = blockIdx.x * WORKERS + k, pos = i < n ? i * w.per + min(i, w.more) : total;
+        const uint32_t i = blockIdx.x * WORKERS + k;
+        at[k] = i < n ? i * w.per + min(i, w.more) : total;
         if (k == worker && i < n) {
-            w.pos = pos;
-            w.end = pos + w.per + (i < w.more);
-        }
-        if (pos - before < mine) {  // before <= pos < before + mine
-            uint32_t b = before, u = u0;
-            if (per > 1)
-                for (uint32_t t = tiles_of(u); pos - b >= t; t = tiles_of(++u)) b += t;
-            sh[THREADS / 32 + 2 * k] = b;
-            sh[THREADS / 32 + 2 * k + 1] = u;
+            w.pos = at[k];
+            w.end = at[k] + w.per + (i < w.more);
         }
     }
-    if (blockIdx.x == 0) {
-        uint32_t b = before;
-        for (uint32_t u = u0; u < u1; ++u) {
-            p.begin[u] = b;
-            b += tiles_of(u);
-        }
-        if (tid == 0) p.begin[p.n_units] = total;
+    if (blockIdx.x == 0 && tid == 0) p.begin[p.n_units] = total;
+#pragma unroll 1
+    for (uint32_t u = u0, b = before; u < u1; ++u) {
+        const uint32_t t = per > 1 ? tiles_of(u) : mine;
+        if (blockIdx.x == 0) p.begin[u] = b;
+#pragma unroll
+        for (uint32_t k = 0; k < WORKERS; ++k)
+            if (at[k] - b < t) {  // b <= at < b + t
+                sh[THREADS / 32 + 2 * k] = b;
+                sh[THREADS / 32 + 2 * k + 1] = u;
+            }
+        b += t;
     }
     __syncthreads();
     w.base = w.s = w.rt = 0;

@@ -17,13 +17,20 @@ using namespace ptx;
 
 constexpr int kWarps = (int)kFewWarps, kThreads = kWarps * 32;
 
+// A run of tiles of one item, from the issue side to the arithmetic side of a warp (which may be several short items behind).
+struct Run {
+    int q0, row0, rows, n, first, pos_min, pos_max, n_sink_tiles, first_tile, tiles, k0, k1;
+    uint32_t c, seq, whole, pad;
+};
+constexpr uint32_t kRuns = 8;  // more than stages
+
 template <int D>
 struct Few {
     static constexpr int kHalves = D / 64;
     static constexpr uint32_t kStageBytes = 2 * kHalves * 2048;          // K then V, 16 tokens x 128 bytes a half
     static constexpr int kStages = D == 128 ? 3 : 6;                      // so that two CTAs share an SM
     static constexpr uint32_t kRing = kStages * kStageBytes;             // a warp's
-    static constexpr uint32_t kSmem = kWarps * kRing + kWarps * kStages * 8 + 4 * (kWarps + 2 * kWarps) + 1024;
+    static constexpr uint32_t kSmem = kWarps * kRing + kWarps * (kStages * 8 + kRuns * sizeof(Run)) + 4 * (kWarps + 2 * kWarps) + 1024;
 };
 
 // Registers of a warp's running softmax over its share of an item.
@@ -46,7 +53,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     uint8_t *sm = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t ring = base + warp * F::kRing;
     uint64_t *bars = reinterpret_cast<uint64_t *>(sm + kWarps * F::kRing);
-    uint32_t *plan = reinterpret_cast<uint32_t *>(bars + kWarps * S);
+    Run *runs = reinterpret_cast<Run *>(bars + kWarps * S) + warp * kRuns;
+    uint32_t *plan = reinterpret_cast<uint32_t *>(reinterpret_cast<Run *>(bars + kWarps * S) + kWarps * kRuns);
     const uint32_t bar = smem_u32(bars + warp * S);
     if (lane == 0) {
         for (int i = 0; i < S; ++i) mbar_init(bar + 8 * i, 1);
@@ -62,82 +70,105 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 
     const float c2 = a.scale * kLog2e;
     const uint32_t tok_mask = (1u << a.block_shift) - 1u;
-    uint32_t put = 0, got = 0;  // stages issued / consumed since the start
-    bool failed = false;
-    Unit un = {};
-    uint32_t c = 0;
-    int k0 = 0, k1 = 0;          // the warp's tiles of the item's list
-    int ids = 0, ids_old = 0;    // block ids of tiles 32b + lane: current and previous batch
-
-    uint32_t at = 0, item = 0, seq = 0;
-    auto segment = [&]() -> bool {  // the next run of tiles of one item
-        const bool more = walk_next<kFewRows, kFewTile>(a, p, w, un, c, k0, k1, at, item);
-        seq = w.s;
-        return more;
-    };
-    auto issue = [&](int i) {  // i: index among the warp's tiles
-        if ((i & 31) == 0) {
-            ids_old = ids;
-            const int k = k0 + i + (int)lane;
-            ids = k < k1 ? un.table[(uint32_t)(unit_tile(un, k) * kFewTile) >> a.block_shift] : -1;
-        }
-        const int id = __shfl_sync(0xffffffffu, ids, i & 31);
-        if (lane == 0) {
-            const uint32_t st = put % S, dst = ring + st * F::kStageBytes, b = bar + 8 * st;
-            const int y = (int)((uint32_t)(unit_tile(un, k0 + i) * kFewTile) & tok_mask);
-            const int blk = (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;  // a hole: out of range, zeros arrive
-            mbar_expect(b, F::kStageBytes);
-#pragma unroll
-            for (int h = 0; h < F::kHalves; ++h) {
-                tma_load_4d(dst + h * 2048, &kmap, h * 64, y, (int)c, blk, b);
-                tma_load_4d(dst + (F::kHalves + h) * 2048, &vmap, h * 64, y, (int)c, blk, b);
+    const int r0 = (int)lane / 4, r1 = r0 + 8;
+    uint32_t put = 0, got = 0;   // stages issued / consumed
+    uint32_t ahead = 0, cur = 0; // runs seen by the issue side / by the arithmetic
+    uint32_t holes = 0;          // a bit for each stage that holds a hole
+    // issue side: tiles ik .. ik1-1 of its run, block ids of tiles ibase + lane
+    const int32_t *itable = nullptr;
+    int ik = 0, ik1 = 0, isink = 0, ishift = 0, ibase = 0, ids = 0;
+    uint32_t ic = 0;
+    bool more = true;
+    // arithmetic side
+    Run run = {};
+    int ck = 0;
+    uint32_t q[D / 16][4];
+    int p0 = 0, p1 = 0;
+    Acc<D> x;
+    // Every part of the loop stands in the code once: a short call is bound by fetching instructions.
+#pragma unroll 1
+    for (;;) {
+#pragma unroll 1
+        while (put - got < (uint32_t)S) {
+            if (ik == ik1) {
+                if (!more) break;
+                Unit un = {};
+                int k0 = 0, k1 = 0;
+                uint32_t at = 0, item = 0;
+                more = walk_next<kFewRows, kFewTile>(a, p, w, un, ic, k0, k1, at, item);
+                if (ahead == 0 && lane == 0 && worker < p.workers) write_cut(p, worker, w, un, ic, more ? k0 : 0, at);
+                if (!more) break;
+                if (lane == 0) {
+                    Run &r = runs[ahead % kRuns];
+                    r.q0 = un.q0, r.row0 = un.row0, r.rows = un.rows, r.n = un.n, r.first = un.first, r.pos_min = un.pos_min, r.pos_max = un.pos_max;
+                    r.n_sink_tiles = un.n_sink_tiles, r.first_tile = un.first_tile, r.tiles = un.tiles, r.k0 = k0, r.k1 = k1;
+                    r.c = ic, r.seq = item / a.n_kv, r.whole = un.whole;
+                }
+                __syncwarp();
+                ++ahead;
+                itable = un.table, isink = un.n_sink_tiles, ishift = un.first_tile - un.n_sink_tiles;
+                ik = k0, ik1 = k1, ibase = k0 - 32;
             }
-        }
-        ++put;
-    };
-
-    bool live = segment();
-    if (live)
-        for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);
-    if (lane == 0 && worker < p.workers) write_cut(p, worker, w, un, c, live ? k0 : 0, at);
-    while (live) {
-        const int nt = k1 - k0;
-        const int r0 = lane / 4, r1 = r0 + 8;
-        // the item's query rows as matrix fragments; rows that do not exist are zero
-        uint32_t q[D / 16][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = i ? r1 : r0;
-            const bool on = r < un.rows;
-            const uint64_t tok = unit_tok(a, un, on ? r : 0);
-            const uint32_t h = unit_head(a, un, c, on ? r : 0);
-            const uint32_t *qp = reinterpret_cast<const uint32_t *>(a.q + tok * a.q_token_stride + h * a.q_head_stride) + (lane & 3u);
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                q[kk][i] = on ? qp[kk * 8] : 0u;
-                q[kk][i + 2] = on ? qp[kk * 8 + 4] : 0u;
+            if (ik - ibase == 32) {
+                ibase = ik;
+                const int k = ik + (int)lane;
+                ids = k < ik1 ? itable[(uint32_t)((k < isink ? k : k + ishift) * kFewTile) >> a.block_shift] : -1;
             }
+            const int id = __shfl_sync(0xffffffffu, ids, ik - ibase);
+            const uint32_t st = put % S;
+            const bool hole = (uint32_t)id >= a.n_blocks;
+            holes = hole ? holes | 1u << st : holes & ~(1u << st);
+            if (lane == 0) {
+                const uint32_t dst = ring + st * F::kStageBytes, b = bar + 8 * st;
+                const int y = (int)((uint32_t)((ik < isink ? ik : ik + ishift) * kFewTile) & tok_mask);
+                const int blk = hole ? (int)a.n_blocks : id;  // a hole: out of range, zeros arrive
+                mbar_expect(b, F::kStageBytes);
+#pragma unroll
+                for (int h = 0; h < F::kHalves; ++h) {
+                    tma_load_4d(dst + h * 2048, &kmap, h * 64, y, (int)ic, blk, b);
+                    tma_load_4d(dst + (F::kHalves + h) * 2048, &vmap, h * 64, y, (int)ic, blk, b);
+                }
+            }
+            ++ik;
+            ++put;
         }
-        const int p0 = unit_row_pos(a, un, r0), p1 = unit_row_pos(a, un, r1);
-        Acc<D> x;
+        if (got == put) break;
+        if (ck == run.k1) {  // the next run: its query rows as matrix fragments (rows that do not exist are zero)
+            run = runs[cur % kRuns];
+            ++cur;
+            ck = run.k0;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+            for (int i = 0; i < 2; ++i) {
+                const int r = i ? r1 : r0;
+                const bool on = r < run.rows;
+                const int row = run.row0 + (on ? r : 0);
+                const uint32_t h = run.c * a.group + (uint32_t)row % a.group;
+                const int tok = run.q0 + row / (int)a.group;
+                const uint32_t *qp = reinterpret_cast<const uint32_t *>(a.q + (uint64_t)tok * a.q_token_stride + h * a.q_head_stride) + (lane & 3u);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x.o[j][e] = 0.f;
-        x.m[0] = x.m[1] = neg_inf();
-        x.l[0] = x.l[1] = 0.f;
-
-        for (int i = 0; i < nt && !failed; ++i) {
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    q[kk][i] = on ? qp[kk * 8] : 0u;
+                    q[kk][i + 2] = on ? qp[kk * 8 + 4] : 0u;
+                }
+                (i ? p1 : p0) = run.whole ? run.n - 1 : run.first + (run.row0 + r) / (int)a.group;
+            }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x.o[j][e] = 0.f;
+            x.m[0] = x.m[1] = neg_inf();
+            x.l[0] = x.l[1] = 0.f;
+        }
+        {
             const uint32_t st = got % S, kt = ring + st * F::kStageBytes, vt = kt + F::kHalves * 2048;
             if (!__all_sync(0xffffffffu, mbar_wait(bar + 8 * st, (got / S) & 1u))) {
-                failed = true;
+                // give up: no more copies; those in flight are waited for (bounded)
+                if (lane == 0 && a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+                for (; got != put; ++got) (void)mbar_wait(bar + 8 * (got % S), (got / S) & 1u);
                 break;
             }
-            ++got;
-            // the batch that i belongs to is the current one unless the issue side has moved on
-            const int last = min(i + S, nt) - 1;  // newest tile issued so far
-            const int id = __shfl_sync(0xffffffffu, (last >> 5) == (i >> 5) ? ids : ids_old, i & 31);
-            const int t0 = unit_tile(un, k0 + i) * kFewTile;
+            const int t0 = (ck < run.n_sink_tiles ? ck : run.first_tile + ck - run.n_sink_tiles) * kFewTile;
+            const bool hole = holes >> st & 1u;
             float s[2][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -157,22 +188,21 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[j][e] *= c2;
             const int t1 = t0 + kFewTile - 1;
-            const bool hole = (uint32_t)id >= a.n_blocks;
-            const bool full = !hole && t1 <= un.pos_min &&
-                              (un.whole || a.window == 0 || (long long)t0 > (long long)un.pos_max - (long long)a.window || (uint32_t)t1 < a.sinks);
+            const bool full = !hole && t1 <= run.pos_min &&
+                              (run.whole || a.window == 0 || (long long)t0 > (long long)run.pos_max - (long long)a.window || (uint32_t)t1 < a.sinks);
             if (!full) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int t = t0 + j * 8 + (int)(lane & 3u) * 2 + (e & 1);
-                        const bool on = !hole && (un.whole ? t < un.n : sees(a, e < 2 ? p0 : p1, t));
+                        const bool on = !hole && (run.whole ? t < run.n : sees(a, e < 2 ? p0 : p1, t));
                         if (!on) s[j][e] = neg_inf();
                     }
                 // values that no row sees must not meet the matrix product, whatever bits they are
                 if (lane < kFewTile) {
                     const int t = t0 + (int)lane;
-                    const bool none = t > un.pos_max || (!un.whole && !sees(a, max(un.pos_min, t), t));
+                    const bool none = t > run.pos_max || (!run.whole && !sees(a, max(run.pos_min, t), t));
                     if (none)
 #pragma unroll
                         for (int h = 0; h < F::kHalves; ++h)
@@ -183,12 +213,12 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 __syncwarp();
             }
             if (p.logits) {
-                float *lp = p.logits + ((uint64_t)seq * a.n_kv + c) * a.max_q * a.group * p.logit_stride;
+                float *lp = p.logits + ((uint64_t)run.seq * a.n_kv + run.c) * a.max_q * a.group * p.logit_stride;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t t = t0 + j * 8 + (lane & 3u) * 2;
-                    if (r0 < un.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r0 * p.logit_stride + t) = make_float2(s[j][0], s[j][1]);
-                    if (HI && r1 < un.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r1 * p.logit_stride + t) = make_float2(s[j][2], s[j][3]);
+                    if (r0 < run.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r0 * p.logit_stride + t) = make_float2(s[j][0], s[j][1]);
+                    if (HI && r1 < run.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r1 * p.logit_stride + t) = make_float2(s[j][2], s[j][3]);
                 }
             }
             // online softmax; a row's 16 logits lie in the four lanes of a quad
@@ -234,32 +264,23 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 mma16816(x.o[j + 1], pa, b[2], b[3], T());
             }
             __syncwarp();  // every lane has read the slot
-            if (i + S < nt) issue(i + S);
         }
-        if (failed) {  // give up: no more copies; those in flight are waited for (bounded)
-            if (lane == 0 && a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
-            for (int i = 0; i < S && got != put; ++i, ++got) (void)mbar_wait(bar + 8 * (got % S), (got / S) & 1u);
-            got = put;
-        }
+        ++got;
+        if (++ck != run.k1) continue;
+        // the end of the run
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 1);
             x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 2);
         }
-        const Unit done = un;
-        const uint32_t dc = c;
-        const bool starts = k0 == 0, ends = k1 == un.tiles;
-        live = segment();
-        if (live && !failed)  // the next item's first tiles are on their way while this one is joined
-            for (int i = 0; i < S && i < k1 - k0; ++i) issue(i);
-
+        const bool starts = run.k0 == 0, ends = run.k1 == run.tiles;
         uint32_t again = 0;  // finished rows to be done once more
 #pragma unroll
         for (int r = 0; r < (HI ? 2 : 1); ++r) {
             const int row = r ? r1 : r0;
-            if (row >= done.rows) continue;
-            const uint64_t tok = unit_tok(a, done, row);
-            const uint32_t h = unit_head(a, done, dc, row);
+            if (row >= run.rows) continue;
+            const uint64_t tok = run.q0 + (run.row0 + row) / (int)a.group;
+            const uint32_t h = run.c * a.group + (uint32_t)(run.row0 + row) % a.group;
             const float m = x.m[r], l = x.l[r];
             if (starts && ends && !p.row_o) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -294,7 +315,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 for (int row = 0; row < 8; ++row)
                     if (rows >> (row * 4) & 15u) {
                         __syncwarp();
-                        attend_row<T, D>(a, unit_tok(a, done, row + 8 * r), unit_head(a, done, dc, row + 8 * r));
+                        const int at = run.row0 + row + 8 * r;
+                        attend_row<T, D>(a, run.q0 + at / (int)a.group, run.c * a.group + (uint32_t)at % a.group);
                     }
             }
         }

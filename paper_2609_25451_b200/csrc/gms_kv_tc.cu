@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         const uint32_t s_tm = tmem + slot * 128, o_tm = tmem + F::kO + slot * D;
         const uint32_t my_s = s_full + 16 * slot, my_p = p_full + 16 * slot, my_o = o_done + 16 * slot, my_q = 8 * slot;
         // S of one half of a K tile (k: its descriptor) into buffer b
-        auto scores = [&](int b, uint32_t k) {
+        auto scores = [&](uint32_t b, uint32_t k) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             }
             tc_commit(on, my_s + 8 * b);
         };
-        auto values = [&](int b, uint32_t v, bool add) {
+        auto values = [&](uint32_t b, uint32_t v, bool add) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) mma_ts(on, o_tm, s_tm + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o, add || kk > 0);
             tc_commit(on, my_o + 8 * b);
@@ -277,37 +277,32 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             GMS_WAIT(my_o, (tiles & 1u) ^ 1u);  // P V of the last item: its buffers are free
             GMS_WAIT(my_o + 8, (tiles & 1u) ^ 1u);
             tc_fence_after();
-            scores(0, k);
-            scores(1, k);
+#pragma unroll 1
+            for (uint32_t b = 0; b < 2; ++b) scores(b, k);
             tc_commit(on, empty + 8 * ks);
             if (nt == 1) tc_commit(on, q_empty + my_q);
             for (int j = 0; j < nt; ++j) {
-                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4), vph = kph;
+                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4);
                 const bool more = j + 1 < nt;
+                GMS_WAIT(full + 8 * vs, kph);
                 ks += 2;
                 if (ks == NS) ks = 0, kph ^= 1u;
                 k = k_lo + (ks * F::kTileBytes >> 4);
-                GMS_WAIT(full + 8 * vs, vph);
-                GMS_WAIT(my_p, tiles & 1u);
-                tc_fence_after();
-                values(0, v, j > 0);
-                if (more) {
-                    GMS_WAIT(full + 8 * ks, kph);
-                    GMS_WAIT(my_o, tiles & 1u);
+#pragma unroll 1
+                for (uint32_t b = 0; b < 2; ++b) {
+                    GMS_WAIT(my_p + 8 * b, tiles & 1u);
                     tc_fence_after();
-                    scores(0, k);
+                    values(b, v, j > 0 || b > 0);
+                    if (more) {
+                        if (b == 0) GMS_WAIT(full + 8 * ks, kph);
+                        GMS_WAIT(my_o + 8 * b, tiles & 1u);  // P lies over S
+                        tc_fence_after();
+                        scores(b, k);
+                    }
                 }
-                GMS_WAIT(my_p + 8, tiles & 1u);
-                tc_fence_after();
-                values(1, v, true);
                 tc_commit(on, empty + 8 * vs);
-                if (more) {
-                    GMS_WAIT(my_o + 8, tiles & 1u);
-                    tc_fence_after();
-                    scores(1, k);
-                    tc_commit(on, empty + 8 * ks);
-                    if (j + 2 == nt) tc_commit(on, q_empty + my_q);
-                }
+                if (more) tc_commit(on, empty + 8 * ks);
+                if (j + 2 == nt) tc_commit(on, q_empty + my_q);
                 ++tiles;
             }
             ++items;
@@ -373,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             float m = neg_inf(), l = 0.f;
             const int n_sink_tiles = g.n_sink_tiles, past_sinks = g.first_tile - n_sink_tiles;
             const bool holes = g.holes != 0;
-            // One step: 64 columns of S to P.  `half` and `edge` are constants where it is called.
+            // One step: 64 columns of S to P.  (In the code once: first runs are bound by fetching instructions.)
             auto step = [&](const int half, const bool edge, int k, int t0, uint32_t valid) {
                 if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) return;
                 tc_fence_after();
@@ -474,14 +469,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     valid = __ballot_sync(0xffffffffu, (uint32_t)id < a.n_blocks) & 0xffu;
                 }
                 const bool whole = valid == 0xffu && t0 + kTile - 1 <= pos_lo && (t0 >= low_hi || t0 + kTile - 1 < sink);
-                if (whole) {
-                    step(0, false, k, t0, valid);
-                    if (!ok) break;
-                    step(1, false, k, t0, valid);
-                } else {
 #pragma unroll 1
-                    for (int half = 0; ok && half < 2; ++half) step(half, true, k, t0, valid);
-                }
+                for (int half = 0; ok && half < 2; ++half) step(half, !whole, k, t0, valid);
                 ++n;
                 ++tiles;
             }
