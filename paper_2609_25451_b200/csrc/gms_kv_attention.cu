@@ -141,21 +141,30 @@ int encode_map(CUtensorMap *m, uint32_t dtype, uint32_t rank, const void *base, 
 {
     const Encode encode = encoder();
     if (!encode) return report_cuda_error(cudaErrorNotSupported);
-    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
     const CUresult r = encode(m, dtype == GMS_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
                               const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? GMS_OK : report_cuda_error(cudaErrorInvalidValue);
 }
-// One layer's keys or values as a 4-d tensor (d, token of block, head, block); boxes of 64 elements x `box_tokens` tokens.
-int encode_pool(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, uint32_t plane, uint32_t box_tokens)
+// One layer's keys or values.  For the many-row kernel (d, token of block, head, block), boxes of 64 elements x `box_tokens`
+// tokens; for the few-row kernel (d mod 64, token of block, d / 64, head, block), boxes of whole rows.
+int encode_pool(CUtensorMap *m, const gms_kv_pool *pool, const gms_kv_layout *l, uint32_t plane, uint32_t box_tokens, bool whole_rows)
 {
-    const cuuint64_t dims[4] = {l->head_dim, l->block_tokens, l->n_kv_heads, pool->n_blocks};
     // a stride along a dimension of one element is never used, but has to be a legal one
-    const cuuint64_t strides[3] = {l->token_stride, l->n_kv_heads > 1 ? l->head_stride : l->token_stride,
-                                   pool->n_blocks > 1 ? pool->block_stride : pool->block_bytes};
+    const cuuint64_t head = l->n_kv_heads > 1 ? l->head_stride : l->token_stride;
+    const cuuint64_t block = pool->n_blocks > 1 ? pool->block_stride : pool->block_bytes;
+    const uint8_t *base = static_cast<const uint8_t *>(pool->base) + plane * pool->plane_stride;
+    if (whole_rows) {
+        const cuuint64_t dims[5] = {64, l->block_tokens, l->head_dim / 64, l->n_kv_heads, pool->n_blocks};
+        const cuuint64_t strides[4] = {l->token_stride, 128, head, block};
+        const cuuint32_t box[5] = {64, box_tokens, l->head_dim / 64, 1, 1};
+        return encode_map(m, l->dtype, 5, base, dims, strides, box);
+    }
+    const cuuint64_t dims[4] = {l->head_dim, l->block_tokens, l->n_kv_heads, pool->n_blocks};
+    const cuuint64_t strides[3] = {l->token_stride, head, block};
     const cuuint32_t box[4] = {64, box_tokens, 1, 1};
-    return encode_map(m, l->dtype, 4, static_cast<const uint8_t *>(pool->base) + plane * pool->plane_stride, dims, strides, box);
+    return encode_map(m, l->dtype, 4, base, dims, strides, box);
 }
 // The queries as (d, head, token): 128 rows are the `group` heads of 128 / group tokens.  False where that does not come out even,
 // where the strides are not a tensor map's (heads or tokens that share bytes), or where the scale's sign has to go into Q.
@@ -288,8 +297,8 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         for (int i = 0; i < 2; ++i) {
             const uint32_t rows = i ? kTcRows : kFewRows;
             if (pl.own.rows != rows && !(prefix && pl.prefix.rows == rows)) continue;
-            rc = encode_pool(&kmap[i], pool, layout, layout->k_plane, i ? box : kFewTile);
-            if (rc == GMS_OK) rc = encode_pool(&vmap[i], pool, layout, layout->v_plane, i ? box : kFewTile);
+            rc = encode_pool(&kmap[i], pool, layout, layout->k_plane, i ? box : kFewTile, i == 0);
+            if (rc == GMS_OK) rc = encode_pool(&vmap[i], pool, layout, layout->v_plane, i ? box : kFewTile, i == 0);
             if (rc != GMS_OK) return rc;
         }
         CUtensorMap qmap;

@@ -70,6 +70,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 
     const float c2 = a.scale * kLog2e;
     const uint32_t tok_mask = (1u << a.block_shift) - 1u;
+    // K and V are read once by the call (more row tiles: several times): they go first, and code, tables and pieces stay in L2
+    const uint64_t policy = p.n_rt == 1 ? policy_evict_first() : policy_evict_normal();
     const int r0 = (int)lane / 4, r1 = r0 + 8;
     uint32_t put = 0, got = 0;   // stages issued / consumed
     uint32_t ahead = 0, cur = 0; // runs seen by the issue side / by the arithmetic
@@ -123,11 +125,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 const int y = (int)((uint32_t)((ik < isink ? ik : ik + ishift) * kFewTile) & tok_mask);
                 const int blk = hole ? (int)a.n_blocks : id;  // a hole: out of range, zeros arrive
                 mbar_expect(b, F::kStageBytes);
-#pragma unroll
-                for (int h = 0; h < F::kHalves; ++h) {
-                    tma_load_4d(dst + h * 2048, &kmap, h * 64, y, (int)ic, blk, b);
-                    tma_load_4d(dst + (F::kHalves + h) * 2048, &vmap, h * 64, y, (int)ic, blk, b);
-                }
+                tma_load_5d(dst, &kmap, 0, y, 0, (int)ic, blk, b, policy);
+                tma_load_5d(dst + F::kHalves * 2048, &vmap, 0, y, 0, (int)ic, blk, b, policy);
             }
             ++ik;
             ++put;
