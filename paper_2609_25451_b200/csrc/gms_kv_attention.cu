@@ -294,6 +294,7 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         CUtensorMap kmap[2], vmap[2];  // boxes of the few-row and of the many-row kernel
         const uint32_t box = layout->block_tokens < kTcTile ? layout->block_tokens : kTcTile;
         const bool prefix = pl.shared && pl.prefix.n_units;
+        pl.own.behind = prefix;
         for (int i = 0; i < 2; ++i) {
             const uint32_t rows = i ? kTcRows : kFewRows;
             if (pl.own.rows != rows && !(prefix && pl.prefix.rows == rows)) continue;
@@ -305,17 +306,17 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         const bool tc = pl.own.rows == kTcRows || (prefix && pl.prefix.rows == kTcRows), q_tma = tc && q_boxes(a, dim);
         if (q_tma) rc = encode_q(&qmap, a, dtype, dim);
         if (rc != GMS_OK) return rc;
-        auto launch = [&](const Pass &p, bool after_prefix) {
-            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], q_tma ? &qmap : nullptr, box, after_prefix, dtype, dim, s)
-                                     : launch_kv_attn_few(b, p, kmap[0], vmap[0], after_prefix, dtype, dim, s);
+        auto launch = [&](const Pass &p) {
+            return p.rows == kTcRows ? launch_kv_attn_tc(b, p, kmap[1], vmap[1], q_tma ? &qmap : nullptr, box, dtype, dim, s)
+                                     : launch_kv_attn_few(b, p, kmap[0], vmap[0], dtype, dim, s);
         };
-        if (prefix) e = launch(pl.prefix, false);
-        if (e == cudaSuccess) e = launch(pl.own, prefix);
+        if (prefix) e = launch(pl.prefix);
+        if (e == cudaSuccess) e = launch(pl.own);
         if (e == cudaSuccess)
             e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s) : launch_kv_attn_join(b, pl.own, dtype, dim, s);
         if (e == cudaSuccess && w && pl.logits) e = launch_kv_few_weights(b, pl.own, s);
     }
-    if (e == cudaSuccess && w && !(a.total_q && pl.logits)) e = launch_kv_weights(a, pl.lse, dtype, dim, s);
+    if (e == cudaSuccess && w && !(a.total_q && pl.logits)) e = launch_kv_weights(a, pl.lse, a.total_q != 0, dtype, dim, s);
     return e == cudaSuccess ? GMS_OK : report_cuda_error(e);
 }
 

@@ -55,6 +55,7 @@ struct Cut {               // the item into which the border before worker i fal
 };
 struct Pass {
     uint32_t prefix;       // 1: units are groups' query rows over their prefix, all of it seen
+    uint32_t behind;       // 1: launched behind the prefix pass of the same call, on which it does not depend
     uint32_t n_units, n_rt, workers;  // n_rt units a sequence (group)
     uint32_t rows, tile;   // rows a unit, tokens a tile
     uint32_t slot_rows;    // rows a slot of part_o has room for (at most `rows`)
@@ -84,25 +85,27 @@ struct EvictArgs {
     uint32_t n_layers, layer_planes, n_seq, n_kv, max_len, budget, sinks, recent;
 };
 
-cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+// behind: the attention kernels of the same call have been launched.
+cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, bool behind, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 // Joins the two passes of a shared-prefix call, row by row.
 cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &prefix, const Pass &own, uint32_t dtype, uint32_t head_dim,
                                        cudaStream_t s);
 // Few query rows a unit (at most 16): kv_attn_few; many: kv_attn_tc.
 constexpr uint32_t kFewRows = 16, kFewTile = 16, kFewWarps = 4, kFewMaxWorkers = 2 * 148 * kFewWarps;
-// after_prefix: launched behind the prefix pass of the same call, on which it does not depend.
-cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix,
-                               uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
+                               uint32_t head_dim, cudaStream_t s);
 // Many query rows a unit; box_tokens: tokens a TMA box of the maps holds; qmap: null, or boxes of 64 elements x group heads
 // x 128 / group tokens of the queries.
 constexpr uint32_t kTcRows = 256, kTcTile = 128, kTcMaxWorkers = 148, kTcExtra = 2;
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                              uint32_t box_tokens, bool after_prefix, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);
 
-// Launches a kernel that may start before the one ahead of it in the stream has drained (it waits for it itself).
+// Launches a kernel that may start before the one ahead of it in the stream has drained.  Every such kernel waits for the one
+// ahead before it touches what that may have written, and lets the next one start only after that wait (so what is complete
+// for a kernel is complete for all behind it).
 template <class K, class... A>
 cudaError_t launch_dependent(K kernel, uint32_t grid, uint32_t block, uint32_t smem, cudaStream_t s, const A &...args)
 {

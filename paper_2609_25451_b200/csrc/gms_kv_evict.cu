@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_evict_select_kernel(const __gr
     __shared__ uint32_t hist[kBins], wsum[2][kSelWarps], sh[2];
     const uint32_t row = blockIdx.x, tid = threadIdx.x;
     const uint32_t c = row % a.n_kv, s = row / a.n_kv % a.n_seq, l = row / a.n_kv / a.n_seq;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t n = (uint32_t)min(max(a.lens[s], 0), (int)a.max_len), keep = min(n, a.budget);
     const float *w = a.weights + l * a.w_layer_stride + s * a.w_seq_stride + c * a.w_head_stride;
     float *wo = a.weights_out ? a.weights_out + l * a.o_layer_stride + s * a.o_seq_stride + c * a.o_head_stride : nullptr;
@@ -155,10 +156,8 @@ cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s)
 {
     const uint32_t rows = a.n_layers * a.n_seq * a.n_kv, chunks = (min(a.max_len, a.budget) + 63) / 64;
     const bool held = a.max_len <= kHeldKeys;
-    if (held) kv_evict_select_kernel<true><<<rows, kSelThreads, min(a.max_len, kHeldKeys) * 4, s>>>(a);
-    else kv_evict_select_kernel<false><<<rows, kSelThreads, 0, s>>>(a);
-    count_launches(1);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = held ? launch_dependent(kv_evict_select_kernel<true>, rows, kSelThreads, min(a.max_len, kHeldKeys) * 4, s, a)
+                               : launch_dependent(kv_evict_select_kernel<false>, rows, kSelThreads, 0, s, a);
     if (e != cudaSuccess || chunks == 0) return e;
     return launch_dependent(kv_evict_move_kernel, rows * chunks, 256, 0, s, a, chunks);
 }

@@ -64,6 +64,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             tma_prefetch_map(&vmap);
         }
     }
+    if (!p.behind) grid_wait();
     grid_launch_dependents();
     Walk w = plan_walk<kFewRows, kFewTile, kThreads, kWarps>(a, p, plan);
     const uint32_t worker = blockIdx.x * kWarps + warp;
@@ -320,21 +321,18 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             }
         }
     }
-    grid_wait();  // behind a prefix pass: this kernel's end stands for both
+    if (p.behind) grid_wait();  // this kernel's end stands for both
 }
 
 template <class T, int D, bool HI>
-cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix, cudaStream_t s)
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
 {
     constexpr uint32_t smem = Few<D>::kSmem;
     static const cudaError_t ready =
         cudaFuncSetAttribute(kv_attn_few_kernel<T, D, HI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
     const uint32_t grid = (p.workers + kWarps - 1) / kWarps;
-    if (after_prefix) return launch_dependent(kv_attn_few_kernel<T, D, HI>, grid, kThreads, smem, s, kmap, vmap, a, p);
-    kv_attn_few_kernel<T, D, HI><<<grid, kThreads, smem, s>>>(kmap, vmap, a, p);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_dependent(kv_attn_few_kernel<T, D, HI>, grid, kThreads, smem, s, kmap, vmap, a, p);
 }
 
 // One thread a token: the logits that the attention kernel left, against the finished log-sum-exps, rows in order.
@@ -363,17 +361,17 @@ __global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_consta
 
 }  // namespace
 
-cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, bool after_prefix,
-                               uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, uint32_t dtype,
+                               uint32_t head_dim, cudaStream_t s)
 {
     const bool hi = (p.prefix ? a.max_group_q : a.max_q) * a.group > 8;
     if (dtype == GMS_DTYPE_BF16) {
         if (head_dim == 64)
-            return hi ? launch<__nv_bfloat16, 64, true>(a, p, kmap, vmap, after_prefix, s) : launch<__nv_bfloat16, 64, false>(a, p, kmap, vmap, after_prefix, s);
-        return hi ? launch<__nv_bfloat16, 128, true>(a, p, kmap, vmap, after_prefix, s) : launch<__nv_bfloat16, 128, false>(a, p, kmap, vmap, after_prefix, s);
+            return hi ? launch<__nv_bfloat16, 64, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 64, false>(a, p, kmap, vmap, s);
+        return hi ? launch<__nv_bfloat16, 128, true>(a, p, kmap, vmap, s) : launch<__nv_bfloat16, 128, false>(a, p, kmap, vmap, s);
     }
-    if (head_dim == 64) return hi ? launch<__half, 64, true>(a, p, kmap, vmap, after_prefix, s) : launch<__half, 64, false>(a, p, kmap, vmap, after_prefix, s);
-    return hi ? launch<__half, 128, true>(a, p, kmap, vmap, after_prefix, s) : launch<__half, 128, false>(a, p, kmap, vmap, after_prefix, s);
+    if (head_dim == 64) return hi ? launch<__half, 64, true>(a, p, kmap, vmap, s) : launch<__half, 64, false>(a, p, kmap, vmap, s);
+    return hi ? launch<__half, 128, true>(a, p, kmap, vmap, s) : launch<__half, 128, false>(a, p, kmap, vmap, s);
 }
 
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s)

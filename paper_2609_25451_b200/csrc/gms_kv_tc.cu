@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         if (q_tma) tma_prefetch_map(&qmap);
     }
     if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(shared_words)), F::kCols);
+    if (!p.behind) grid_wait();
     grid_launch_dependents();
     tc_fence_before();
     Walk w = plan_walk<kRows, kTile, kThreads, 1>(a, p, plan);  // ends with __syncthreads
@@ -175,6 +176,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         const uint32_t tok_mask = (1u << a.block_shift) - 1u;
         uint32_t n = 0, q_n[2] = {0, 0};  // stages filled; times each slot's Q was
         bool ok = true;
+        // K and V that one row tile reads go first in L2; those that several read stay
+        const uint64_t policy = p.n_rt == 1 ? policy_evict_first() : policy_evict_normal();
         for (;; ++seg) {
             ok = __all_sync(0xffffffffu, ok && wait_or_abort(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u, abort, a.status));
             if (!ok) break;
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     __syncwarp();
                     if ((int)lane < boxes)
                         tma_load_4d(ring + st * F::kTileBytes + half * F::kHalfBytes + part * box_tokens * 128, v ? &vmap : &kmap, half * 64,
-                                    (int)((uint32_t)t & tok_mask), head, blk, full + 8 * st);
+                                    (int)((uint32_t)t & tok_mask), head, blk, full + 8 * st, policy);
                     ++n;
                 }
             }
@@ -557,33 +560,30 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         tc_fence_after();
         tmem_free(tmem, F::kCols);
     }
-    grid_wait();  // behind a prefix pass: this kernel's end stands for both
+    if (p.behind) grid_wait();  // this kernel's end stands for both
 }
 
 template <class T, int D>
 cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                   uint32_t box_tokens, bool after_prefix, cudaStream_t s)
+                   uint32_t box_tokens, cudaStream_t s)
 {
     constexpr uint32_t smem = Tc<D>::kSmem;
     static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (ready != cudaSuccess) return ready;
     const CUtensorMap &qm = qmap ? *qmap : kmap;
     const uint32_t q_tma = qmap != nullptr;
-    if (after_prefix) return launch_dependent(kv_attn_tc_kernel<T, D>, p.workers, kThreads, smem, s, kmap, vmap, qm, a, p, box_tokens, q_tma);
-    kv_attn_tc_kernel<T, D><<<p.workers, kThreads, smem, s>>>(kmap, vmap, qm, a, p, box_tokens, q_tma);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_dependent(kv_attn_tc_kernel<T, D>, p.workers, kThreads, smem, s, kmap, vmap, qm, a, p, box_tokens, q_tma);
 }
 
 }  // namespace
 
 cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, const CUtensorMap *qmap,
-                              uint32_t box_tokens, bool after_prefix, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+                              uint32_t box_tokens, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
     if (dtype == GMS_DTYPE_BF16)
-        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s)
-                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s);
-    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s) : launch<__half, 128>(a, p, kmap, vmap, qmap, box_tokens, after_prefix, s);
+        return head_dim == 64 ? launch<__nv_bfloat16, 64>(a, p, kmap, vmap, qmap, box_tokens, s)
+                              : launch<__nv_bfloat16, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
+    return head_dim == 64 ? launch<__half, 64>(a, p, kmap, vmap, qmap, box_tokens, s) : launch<__half, 128>(a, p, kmap, vmap, qmap, box_tokens, s);
 }
 
 }  // namespace gms

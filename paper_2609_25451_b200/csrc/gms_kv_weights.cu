@@ -18,8 +18,10 @@ using namespace ptx;
 constexpr int kWarps = 4, kThreads = kWarps * 32, kTokens = kWarps * 32, kRows = 64;
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_constant__ AttnArgs a, const float *lse, uint32_t chunks)
+__global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_constant__ AttnArgs a, const float *lse, uint32_t chunks,
+                                                               uint32_t behind)
 {
+    if (!behind) grid_wait();  // else the attention kernels ahead have waited, and only their log-sum-exps are waited for below
     constexpr int kChunks = D / 8, kStride = D * 2 + 16;  // 16-byte pieces of a row; bytes between rows (no bank conflicts)
     __shared__ __align__(16) uint8_t rows_sh[kTokens * kStride];  // the keys, then the queries
     __shared__ float lse_sh[kRows];
@@ -136,15 +138,16 @@ __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_const
 
 }  // namespace
 
-cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+cudaError_t launch_kv_weights(const AttnArgs &a, const float *lse, bool behind, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
 {
     const uint32_t chunks = (a.max_kv + kTokens - 1) / kTokens, grid = a.n_seq * a.n_kv * chunks;
+    const uint32_t behind_word = behind;
     if (grid == 0) return cudaSuccess;
     if (dtype == GMS_DTYPE_BF16)
-        return head_dim == 64 ? launch_dependent(kv_weights_kernel<__nv_bfloat16, 64>, grid, kThreads, 0, s, a, lse, chunks)
-                              : launch_dependent(kv_weights_kernel<__nv_bfloat16, 128>, grid, kThreads, 0, s, a, lse, chunks);
-    return head_dim == 64 ? launch_dependent(kv_weights_kernel<__half, 64>, grid, kThreads, 0, s, a, lse, chunks)
-                          : launch_dependent(kv_weights_kernel<__half, 128>, grid, kThreads, 0, s, a, lse, chunks);
+        return head_dim == 64 ? launch_dependent(kv_weights_kernel<__nv_bfloat16, 64>, grid, kThreads, 0, s, a, lse, chunks, behind_word)
+                              : launch_dependent(kv_weights_kernel<__nv_bfloat16, 128>, grid, kThreads, 0, s, a, lse, chunks, behind_word);
+    return head_dim == 64 ? launch_dependent(kv_weights_kernel<__half, 64>, grid, kThreads, 0, s, a, lse, chunks, behind_word)
+                          : launch_dependent(kv_weights_kernel<__half, 128>, grid, kThreads, 0, s, a, lse, chunks, behind_word);
 }
 
 }  // namespace gms

@@ -94,15 +94,16 @@ __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *m)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
 }
-// x: element index in the innermost dimension (here always a multiple of 64 elements = 128 bytes).
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, int w, uint32_t bar)
+// x: element index in the innermost dimension (here always a multiple of 64 elements = 128 bytes); with an L2 eviction policy.
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, int w, uint32_t bar, uint64_t policy)
 {
     asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-        "l"(m), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint "
+        "[%0], [%1, {%2, %3, %4, %5}], [%6], %7;" ::"r"(dst),
+        "l"(m), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(policy)
         : "memory");
 }
-// The same in five dimensions, with an L2 eviction policy.
+// The same in five dimensions.
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *m, int x, int y, int z, int w, int v, uint32_t bar, uint64_t policy)
 {
     asm volatile(
