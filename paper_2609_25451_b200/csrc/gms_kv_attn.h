@@ -1,5 +1,6 @@
 // Internal declarations of the attention and eviction kernels on the paged KV pool.
 #pragma once
+#include <atomic>
 #include <cstdint>
 
 #include <cuda.h>
@@ -102,6 +103,18 @@ cudaError_t launch_kv_attn_tc(const AttnArgs &a, const Pass &p, const CUtensorMa
 cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s);
 cudaError_t launch_kv_evict(const EvictArgs &a, cudaStream_t s);
+
+// Lets a kernel have more than 48 KB of shared memory, once a device (`done` has a bit for each).
+template <class K>
+cudaError_t allow_smem(K kernel, uint32_t smem, std::atomic<uint64_t> &done)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && done.load(std::memory_order_relaxed) >> dev & 1u)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
+}
 
 // Launches a kernel that may start before the one ahead of it in the stream has drained.  Every such kernel waits for the one
 // ahead before it touches what that may have written, and lets the next one start only after that wait (so what is complete

@@ -328,14 +328,14 @@ template <class T, int D, bool HI>
 cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
 {
     constexpr uint32_t smem = Few<D>::kSmem;
-    static const cudaError_t ready =
-        cudaFuncSetAttribute(kv_attn_few_kernel<T, D, HI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (ready != cudaSuccess) return ready;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(kv_attn_few_kernel<T, D, HI>, smem, done);
+    if (e != cudaSuccess) return e;
     const uint32_t grid = (p.workers + kWarps - 1) / kWarps;
     return launch_dependent(kv_attn_few_kernel<T, D, HI>, grid, kThreads, smem, s, kmap, vmap, a, p);
 }
 
-// One thread a token: the logits that the attention kernel left, against the finished log-sum-exps, rows in order.
+// One thread four tokens: the logits that the attention kernel left, against the finished log-sum-exps, rows in order.
 __global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p, uint32_t chunks)
 {
     __shared__ float lse[kFewRows];
@@ -345,18 +345,31 @@ __global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_consta
     if ((int)threadIdx.x < u.rows)
         lse[threadIdx.x] = a.lse[(uint64_t)(u.q0 + threadIdx.x / a.group) * a.n_heads + c * a.group + threadIdx.x % a.group] * kLog2e;
     __syncthreads();
-    const int t = (int)(blockIdx.x % chunks * 256 + threadIdx.x);
+    const int t = (int)(blockIdx.x % chunks * 1024 + threadIdx.x * 4);
     if (t >= u.n) return;
     const uint64_t at = s * a.w_seq_stride + c * a.w_head_stride + t;
-    const float *lp = p.logits + (uint64_t)item * a.max_q * a.group * p.logit_stride + t;
-    float sum = 0.f;
-    const int tile = t / (int)kFewTile;
-    if (u.rows > 0 && (tile < u.n_sink_tiles || (tile >= u.first_tile && tile < u.first_tile + u.tiles - u.n_sink_tiles)))
+    const int left = min(u.n - t, 4), tile = t / (int)kFewTile;
+    float in[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) in[e] = a.w_in && e < left ? a.w_in[at + e] : 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    // tiles that nobody sees have no logits; in those of the list a token that a row does not see has -infinity
+    if (u.rows > 0 && (tile < u.n_sink_tiles || (tile >= u.first_tile && tile < u.first_tile + u.tiles - u.n_sink_tiles))) {
+        const float4 *lp = reinterpret_cast<const float4 *>(p.logits + (uint64_t)item * a.max_q * a.group * p.logit_stride + t);
+#pragma unroll 4
         for (int r = 0; r < u.rows; ++r) {
-            const float x = lp[(uint64_t)r * p.logit_stride];
-            if (x != neg_inf()) sum += ex2(x - lse[r]);
+            const float4 x = lp[(uint64_t)r * (p.logit_stride / 4)];
+            const float l = lse[r] == neg_inf() ? 0.f : lse[r];
+            sum.x += ex2(x.x - l);
+            sum.y += ex2(x.y - l);
+            sum.z += ex2(x.z - l);
+            sum.w += ex2(x.w - l);
         }
-    a.w_out[at] = (a.w_in ? a.decay * a.w_in[at] : 0.f) + sum;
+    }
+    const float add[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) a.w_out[at + e] = a.decay * in[e] + add[e];
 }
 
 }  // namespace
@@ -376,7 +389,7 @@ cudaError_t launch_kv_attn_few(const AttnArgs &a, const Pass &p, const CUtensorM
 
 cudaError_t launch_kv_few_weights(const AttnArgs &a, const Pass &p, cudaStream_t s)
 {
-    const uint32_t chunks = (a.max_kv + 255) / 256;
+    const uint32_t chunks = (a.max_kv + 1023) / 1024;
     if (chunks == 0) return cudaSuccess;
     return launch_dependent(kv_few_weights_kernel, a.n_seq * a.n_kv * chunks, 256, 0, s, a, p, chunks);
 }

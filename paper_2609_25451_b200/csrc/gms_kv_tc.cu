@@ -568,8 +568,9 @@ cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, co
                    uint32_t box_tokens, cudaStream_t s)
 {
     constexpr uint32_t smem = Tc<D>::kSmem;
-    static const cudaError_t ready = cudaFuncSetAttribute(kv_attn_tc_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (ready != cudaSuccess) return ready;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t e = allow_smem(kv_attn_tc_kernel<T, D>, smem, done);
+    if (e != cudaSuccess) return e;
     const CUtensorMap &qm = qmap ? *qmap : kmap;
     const uint32_t q_tma = qmap != nullptr;
     return launch_dependent(kv_attn_tc_kernel<T, D>, p.workers, kThreads, smem, s, kmap, vmap, qm, a, p, box_tokens, q_tma);
