@@ -233,8 +233,8 @@ cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype
     const uint32_t borders = p.workers < 2 ? 1 : p.workers - 1;
     const uint64_t items = (uint64_t)p.n_units * a.n_kv;
     const uint32_t by_item = items <= borders;
-    // sixteen rows a block; one row a block, its pieces spread over all warps, where an item is in many pieces
-    const uint32_t rows_a_block = by_item && p.workers / items >= 16 && p.slot_rows <= kFewRows ? 1 : kFewRows;
+    // sixteen rows a block; fewer, their pieces spread over the warps, where few items are in many pieces each
+    const uint32_t rows_a_block = !by_item || p.workers / items < 16 ? kFewRows : p.slot_rows <= kFewRows ? 1 : 4;
     const uint32_t parts = (p.slot_rows + rows_a_block - 1) / rows_a_block, grid = (by_item ? (uint32_t)items : borders) * parts;
     if (p.rows == kTcRows)
         GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)));

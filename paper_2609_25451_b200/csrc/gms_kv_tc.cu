@@ -40,7 +40,7 @@ struct Tc {
     static constexpr uint32_t kHalfBytes = 128 * 128;             // 128 rows x 64 elements
     static constexpr uint32_t kTileBytes = kHalves * kHalfBytes;  // a K, V or Q tile
     static constexpr int kStages = D == 128 ? 4 : 8;
-    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 2 * kSegments) * 8;
+    static constexpr uint32_t kBars = (2 * kStages + 2 + 2 + 4 + 4 + 4 + 1 + 3 * kSegments) * 8;
     static constexpr uint32_t kOutBytes = 8 * 4096;               // 32 rows x 128 bytes a softmax warp, for coalesced stores
     static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + kOutBytes + kBars + 128 + kSegments * sizeof(Segment) + 1024;
     static constexpr uint32_t kO = 256;                            // first column of O0
@@ -110,8 +110,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     const uint32_t q_smem = base, ring = base + 2 * F::kTileBytes;
     uint64_t *bars = reinterpret_cast<uint64_t *>(sm + (2 + NS) * F::kTileBytes + F::kOutBytes);
     const uint32_t full = smem_u32(bars), empty = full + 8 * NS, q_full = empty + 8 * NS, q_empty = q_full + 16, s_full = q_empty + 16,
-                   p_full = s_full + 32, o_done = p_full + 32, drain = o_done + 32, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments;
-    uint32_t *plan = reinterpret_cast<uint32_t *>(bars + 2 * NS + 17 + 2 * kSegments);
+                   p_full = s_full + 32, o_done = p_full + 32, drain = o_done + 32, seg_full = drain + 8, seg_empty = seg_full + 8 * kSegments,
+                   seg_holes = seg_empty + 8 * kSegments;
+    uint32_t *plan = reinterpret_cast<uint32_t *>(bars + 2 * NS + 17 + 3 * kSegments);
     volatile uint32_t *shared_words = plan + 16;  // behind the plan's 14  // [0] tensor memory, [1] abort
     volatile uint32_t *abort = shared_words + 1;
     Segment *const segs = reinterpret_cast<Segment *>(const_cast<uint32_t *>(shared_words) + 4);
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             }
         }
         mbar_init(drain, 2);
-        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_empty + 8 * i, 11);  // 8 softmax warps, 3 more
+        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_holes + 8 * i, 1), mbar_init(seg_empty + 8 * i, 11);  // 8 softmax warps, 3 more
         *abort = 0;
         fence_mbar_init();
         tma_prefetch_map(&kmap);
@@ -153,6 +154,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             if (!__all_sync(0xffffffffu, wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status))) break;
             Segment g;
             more = next_segment(a, p, w, g, seg == 0);
+            if (lane == 0) {
+                segs[at] = g;
+                mbar_arrive(seg_full + 8 * at);
+            }
             if (more) {  // whether any id of its tiles lies outside the pool (then the softmax looks at every tile's)
                 bool hole = false;
                 const int t_end = min(g.n, (seg_tile(g, g.k1 - 1) + 1) * kTile), step = 1 << a.block_shift;
@@ -161,11 +166,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                         hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
                 for (int t = (seg_tile(g, max(g.k0, g.n_sink_tiles)) * kTile & ~(step - 1)) + (int)lane * step; t < t_end; t += 32 * step)
                     hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
-                g.holes = __any_sync(0xffffffffu, hole);
-            }
-            if (lane == 0) {
-                segs[at] = g;
-                mbar_arrive(seg_full + 8 * at);
+                hole = __any_sync(0xffffffffu, hole);
+                if (lane == 0) {
+                    segs[at].holes = hole;
+                    mbar_arrive(seg_holes + 8 * at);
+                }
             }
         }
         __syncwarp();
@@ -370,6 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             const int low = low_of(pos), low_hi = low_of(pos_hi), sink = (int)min(a.sinks, 0x7fffffffu);
             float m = neg_inf(), l = 0.f;
             const int n_sink_tiles = g.n_sink_tiles, past_sinks = g.first_tile - n_sink_tiles;
+            if (!wait(seg_holes + 8 * (seg % kSegments), (seg / kSegments) & 1u)) break;
             const bool holes = g.holes != 0;
             // One step: 64 columns of S to P.  (In the code once: first runs are bound by fetching instructions.)
             auto step = [&](const int half, const bool edge, int k, int t0, uint32_t valid) {

@@ -3,7 +3,7 @@
 //   out[t] = decay * in[t] + sum over rows r that see t of 2^(c q_r.k_t - lse2_r)
 //
 // A CTA owns 128 tokens of one sequence and KV head: every warp keeps 32 tokens' keys in registers as matrix fragments and
-// walks all query rows, 64 at a time through shared memory (S^T = K Q^T, so a token's sum stays in a quad of lanes).  Each sum
+// walks all query rows, 128 at a time through shared memory (S^T = K Q^T, so a token's sum stays in a quad of lanes).  Each sum
 // has one owner and one order: no atomics, equal calls give equal bits.  Bound by the exponentials and the matrix unit for
 // many rows, by reading K for few.
 #include "gms_internal.h"
@@ -15,7 +15,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 4, kThreads = kWarps * 32, kTokens = kWarps * 32, kRows = 64;
+constexpr int kWarps = 4, kThreads = kWarps * 32, kTokens = kWarps * 32, kRows = kTokens;
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_constant__ AttnArgs a, const float *lse, uint32_t chunks,
