@@ -418,7 +418,7 @@ typedef struct {
     uint64_t table_stride;         /* entries; table_stride * block_tokens >= max_kv                     */
     uint32_t n_seq, n_heads;       /* n_heads: a multiple of n_kv_heads                                  */
     uint32_t total_q, max_q;       /* rows of q; longest query run of a sequence                         */
-    uint32_t max_kv;               /* longest kv_lens                                                    */
+    uint32_t max_kv;               /* longest kv_lens (at most 2^30)                                     */
     uint32_t window, sinks;        /* window 0: every token up to the query's own is seen                */
     float scale;
 } gms_kv_attn;
@@ -458,7 +458,7 @@ typedef struct {
     const int32_t *prefix_table;  /* (device) n_groups rows of prefix_stride ids                         */
     uint64_t prefix_stride;       /* entries; prefix_stride * block_tokens >= max_prefix                 */
     uint32_t n_groups;
-    uint32_t max_prefix;          /* longest prefix_lens                                                 */
+    uint32_t max_prefix;          /* longest prefix_lens (at most 2^30)                                  */
     uint32_t max_group_q;         /* most query rows in a group                                          */
     uint32_t reserved;            /* 0                                                                   */
 } gms_kv_prefix;

@@ -44,7 +44,7 @@ int make_args(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv
     if (rc == GMS_OK) rc = bad_layout(pool, layout);
     if (rc != GMS_OK) return rc;
     if (t->n_heads == 0 || t->n_heads % layout->n_kv_heads || !std::isfinite(t->scale)) return GMS_ERR_ARG;
-    if (t->total_q > 0x7fffffffu || t->n_seq > 0x7fffffffu || t->max_kv > 0x7fffffffu || t->max_q > t->total_q) return GMS_ERR_ARG;
+    if (t->total_q > 0x7fffffffu || t->n_seq > 0x7fffffffu || t->max_kv > 1u << 30 || t->max_q > t->total_q) return GMS_ERR_ARG;
     if ((uint64_t)t->total_q * t->n_heads > 0x7fffffffull) return GMS_ERR_RANGE;
     if (!t->cu_q && (t->total_q != t->n_seq || (t->n_seq && t->max_q != 1))) return GMS_ERR_ARG;
     const bool work = t->n_seq && t->total_q;
@@ -101,7 +101,7 @@ int make_args(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv
         a->decay = w->decay;
     }
     if (x) {
-        if (t->window || t->sinks || x->reserved || x->max_prefix > 0x7fffffffu || x->n_groups > t->n_seq || x->max_group_q > t->total_q)
+        if (t->window || t->sinks || x->reserved || x->max_prefix > 1u << 30 || x->n_groups > t->n_seq || x->max_group_q > t->total_q)
             return GMS_ERR_ARG;
         if (x->n_groups && (!x->group_start || !x->prefix_lens || (x->max_prefix && !x->prefix_table))) return GMS_ERR_NULL;
         if ((reinterpret_cast<uint64_t>(x->group_start) | reinterpret_cast<uint64_t>(x->prefix_lens) |
@@ -366,7 +366,7 @@ int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms
     int rc = gms::bad_pool(pool);
     if (rc == GMS_OK) rc = gms::bad_layout(pool, layout);
     if (rc != GMS_OK) return rc;
-    if (t->reserved || t->max_len > 0x7fffffffu || t->budget > 0x7fffffffu || (uint64_t)t->sinks + t->recent > t->budget)
+    if (t->reserved || t->max_len > 1u << 30 || t->budget > 1u << 30 || (uint64_t)t->sinks + t->recent > t->budget)
         return GMS_ERR_ARG;
     if (t->n_layers) {
         const uint64_t last = (uint64_t)(t->n_layers - 1) * t->layer_planes;

@@ -9,9 +9,10 @@
 // (128-token steps with one buffer a slot: 976 us for 2,048 new tokens over 16k, the softmax waiting 40 % of the time.)
 // O stays in tensor memory for the whole item; it is rescaled only when a row's maximum has grown by more than 2^8 (weights
 // are then at most 256 times too large against a stale maximum, which 16-bit P and 32-bit l and O hold without loss).
-// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 200 registers a thread.  Warps 8 and 11
-// issue the products of slots 0 and 1, warp 9 the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids of a tile at once, one lane
-// a box; warp 10 deals out the items (a ring of descriptors in shared memory); Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the softmax threads copy it).
+// Warps 0-3 and 4-7: softmax of slots 0 and 1, one thread a row (no shuffles), 200 registers a thread.  Warps 8 and 11 issue
+// the products of slots 0 and 1.  Warp 9 issues the TMA loads: one box of 64 elements x up to 128 tokens of one block, all ids
+// of a tile at once, one lane a box; Q as boxes of 64 elements x heads x tokens where 128 rows are whole tokens (else the
+// softmax threads copy it).  Warp 10 deals out the items (a ring of descriptors in shared memory).
 // Tensor memory: 2 x 2 S buffers of 64 columns, O0 O1 (D each) = 512 columns at D = 128, hence P over S.
 // Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
 #include "gms_internal.h"
@@ -128,7 +129,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             }
         }
         mbar_init(drain, 2);
-        for (uint32_t i = 0; i < kSegments; ++i) mbar_init(seg_full + 8 * i, 1), mbar_init(seg_holes + 8 * i, 1), mbar_init(seg_empty + 8 * i, 11);  // 8 softmax warps, 3 more
+        for (uint32_t i = 0; i < kSegments; ++i) {
+            mbar_init(seg_full + 8 * i, 1);
+            mbar_init(seg_holes + 8 * i, 1);
+            mbar_init(seg_empty + 8 * i, 11);  // 8 softmax warps, 3 more
+        }
         *abort = 0;
         fence_mbar_init();
         tma_prefetch_map(&kmap);
@@ -146,181 +151,183 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
     // 384 threads x 168 registers = 128 x 104 + 256 x 200
     uint32_t seg = 0;  // segments seen
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == 10) {
-        // ------------------------------------------------------------------ items
-        for (bool more = true; more; ++seg) {
-            const uint32_t at = seg % kSegments;
-            if (!__all_sync(0xffffffffu, wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status))) break;
-            Segment g;
-            more = next_segment(a, p, w, g, seg == 0);
-            if (lane == 0) {
-                segs[at] = g;
-                mbar_arrive(seg_full + 8 * at);
-            }
-            if (more) {  // whether any id of its tiles lies outside the pool (then the softmax looks at every tile's)
-                bool hole = false;
-                const int t_end = min(g.n, (seg_tile(g, g.k1 - 1) + 1) * kTile), step = 1 << a.block_shift;
-                for (int k = g.k0; k < min(g.k1, g.n_sink_tiles); ++k)
-                    for (int t = k * kTile + (int)lane * step; t < (k + 1) * kTile; t += 32 * step)
-                        hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
-                for (int t = (seg_tile(g, max(g.k0, g.n_sink_tiles)) * kTile & ~(step - 1)) + (int)lane * step; t < t_end; t += 32 * step)
-                    hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
-                hole = __any_sync(0xffffffffu, hole);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        if (warp == 10) {
+            // ------------------------------------------------------------------ items
+            for (bool more = true; more; ++seg) {
+                const uint32_t at = seg % kSegments;
+                if (!__all_sync(0xffffffffu, wait_or_abort(seg_empty + 8 * at, ((seg / kSegments) & 1u) ^ 1u, abort, a.status))) break;
+                Segment g;
+                more = next_segment(a, p, w, g, seg == 0);
                 if (lane == 0) {
-                    segs[at].holes = hole;
-                    mbar_arrive(seg_holes + 8 * at);
+                    segs[at] = g;
+                    mbar_arrive(seg_full + 8 * at);
                 }
-            }
-        }
-        __syncwarp();
-    } else if (warp == 9) {
-        // ------------------------------------------------------------------ loads
-        const int per = kTile / (int)box_tokens, boxes = per * F::kHalves;  // boxes a tile: at most 16
-        const int half = (int)lane % F::kHalves, part = (int)lane / F::kHalves;
-        const uint32_t tok_mask = (1u << a.block_shift) - 1u;
-        uint32_t n = 0, q_n[2] = {0, 0};  // stages filled; times each slot's Q was
-        bool ok = true;
-        // K and V that one row tile reads go first in L2; those that several read stay
-        const uint64_t policy = p.n_rt == 1 ? policy_evict_first() : policy_evict_normal();
-        for (;; ++seg) {
-            ok = __all_sync(0xffffffffu, ok && wait_or_abort(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u, abort, a.status));
-            if (!ok) break;
-            const Segment &g = segs[seg % kSegments];
-            if (g.k0 == g.k1) break;
-            const int32_t *table = g.table;
-            const int len = g.n, k1 = g.k1, head = (int)g.c;
-            auto block_of = [&](int k) -> int {  // a hole, or nothing left to read: out of range, zeros arrive
-                const int t = seg_tile(g, k) * kTile + part * (int)box_tokens;
-                int id = -1;
-                if ((int)lane < boxes && t < len) id = table[(uint32_t)t >> a.block_shift];
-                return (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;
-            };
-            int next = block_of(g.k0);
-            if (q_tma) {
-#pragma unroll
-                for (int slot = 0; slot < 2; ++slot) {
-                    if (!ok || slot * 128 >= g.rows) continue;
-                    ok = __all_sync(0xffffffffu, wait_or_abort(q_empty + 8 * slot, (q_n[slot] & 1u) ^ 1u, abort, a.status));
-                    if (!ok) continue;
+                if (more) {  // whether any id of its tiles lies outside the pool (then the softmax looks at every tile's)
+                    bool hole = false;
+                    const int t_end = min(g.n, (seg_tile(g, g.k1 - 1) + 1) * kTile), step = 1 << a.block_shift;
+                    for (int k = g.k0; k < min(g.k1, g.n_sink_tiles); ++k)
+                        for (int t = k * kTile + (int)lane * step; t < (k + 1) * kTile; t += 32 * step)
+                            hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
+                    for (int t = (seg_tile(g, max(g.k0, g.n_sink_tiles)) * kTile & ~(step - 1)) + (int)lane * step; t < t_end; t += 32 * step)
+                        hole |= (uint32_t)g.table[(uint32_t)t >> a.block_shift] >= a.n_blocks;
+                    hole = __any_sync(0xffffffffu, hole);
                     if (lane == 0) {
-                        mbar_expect(q_full + 8 * slot, F::kTileBytes);
-                        for (int h = 0; h < F::kHalves; ++h)
-                            tma_load_3d(q_smem + slot * F::kTileBytes + h * F::kHalfBytes, &qmap, h * 64, head * (int)a.group,
-                                        g.q0 + (g.row0 + slot * 128) / (int)a.group, q_full + 8 * slot);
+                        segs[at].holes = hole;
+                        mbar_arrive(seg_holes + 8 * at);
                     }
-                    ++q_n[slot];
-                }
-            }
-            for (int k = g.k0; ok && k < k1; ++k) {
-                const int blk = next, t = seg_tile(g, k) * kTile + part * (int)box_tokens;
-                if (k + 1 < k1) next = block_of(k + 1);
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    const uint32_t st = n % NS;
-                    ok = __all_sync(0xffffffffu, wait_or_abort(empty + 8 * st, ((n / NS) & 1u) ^ 1u, abort, a.status));
-                    if (!ok) break;
-                    if (lane == 0) mbar_expect(full + 8 * st, F::kTileBytes);
-                    __syncwarp();
-                    if ((int)lane < boxes)
-                        tma_load_4d(ring + st * F::kTileBytes + half * F::kHalfBytes + part * box_tokens * 128, v ? &vmap : &kmap, half * 64,
-                                    (int)((uint32_t)t & tok_mask), head, blk, full + 8 * st, policy);
-                    ++n;
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
-        }
-        if (!ok)  // give up: wait (bounded) for what is still on its way into this CTA's shared memory
-            for (uint32_t i = n > (uint32_t)NS ? n - NS : 0; i < n; ++i) (void)mbar_wait(full + 8 * (i % NS), (i / NS) & 1u);
-        for (int slot = 0; !ok && slot < 2; ++slot)
-            if (q_n[slot]) (void)mbar_wait(q_full + 8 * slot, (q_n[slot] - 1) & 1u);
-    } else {
-        // ------------------------------------------------------------------ products of one slot (warp 8: slot 0, warp 11: slot 1)
-        constexpr uint32_t id_s = f16_idesc(128, 64, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
-        // Straight-line code a tile: these warps compete for issue with two softmax warps each, every instruction counts.
-#define GMS_WAIT(bar, parity) \
-    if (!mbar_spin(bar, parity, 4096) && !wait_slow(bar, parity, abort, a.status)) goto products_done
-        const uint32_t on = one_lane(), slot = warp == 8 ? 0u : 1u;
-        constexpr uint32_t hi = desc_hi(1024), half_k = 64 * 128 >> 4, half_v = 4 * 2048 >> 4;
-        const uint32_t q_lo = desc_lo(q_smem + slot * F::kTileBytes, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
-        const uint32_t s_tm = tmem + slot * 128, o_tm = tmem + F::kO + slot * D;
-        const uint32_t my_s = s_full + 16 * slot, my_p = p_full + 16 * slot, my_o = o_done + 16 * slot, my_q = 8 * slot;
-        // S of one half of a K tile (k: its descriptor) into buffer b
-        auto scores = [&](uint32_t b, uint32_t k) {
+        } else if (warp == 9) {
+            // ------------------------------------------------------------------ loads
+            const int per = kTile / (int)box_tokens, boxes = per * F::kHalves;  // boxes a tile: at most 16
+            const int half = (int)lane % F::kHalves, part = (int)lane / F::kHalves;
+            const uint32_t tok_mask = (1u << a.block_shift) - 1u;
+            uint32_t n = 0, q_n[2] = {0, 0};  // stages filled; times each slot's Q was
+            bool ok = true;
+            // K and V that one row tile reads go first in L2; those that several read stay
+            const uint64_t policy = p.n_rt == 1 ? policy_evict_first() : policy_evict_normal();
+            for (;; ++seg) {
+                ok = __all_sync(0xffffffffu, ok && wait_or_abort(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u, abort, a.status));
+                if (!ok) break;
+                const Segment &g = segs[seg % kSegments];
+                if (g.k0 == g.k1) break;
+                const int32_t *table = g.table;
+                const int len = g.n, k1 = g.k1, head = (int)g.c;
+                auto block_of = [&](int k) -> int {  // a hole, or nothing left to read: out of range, zeros arrive
+                    const int t = seg_tile(g, k) * kTile + part * (int)box_tokens;
+                    int id = -1;
+                    if ((int)lane < boxes && t < len) id = table[(uint32_t)t >> a.block_shift];
+                    return (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;
+                };
+                int next = block_of(g.k0);
+                if (q_tma) {
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
-                mma_ss(on, s_tm + b * 64, q_lo + off, k + b * half_k + off, hi, id_s, kk > 0);
-            }
-            tc_commit(on, my_s + 8 * b);
-        };
-        auto values = [&](uint32_t b, uint32_t v, bool add) {
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) mma_ts(on, o_tm, s_tm + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o, add || kk > 0);
-            tc_commit(on, my_o + 8 * b);
-        };
-        uint32_t ks = 0, kph = 0;       // stage of the next K tile (V follows it) and its phase
-        uint32_t tiles = 0, items = 0;  // of this slot so far (low bits count)
-        for (;; ++seg) {
-            GMS_WAIT(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
-            const Segment &g = segs[seg % kSegments];
-            const bool mine = slot == 0 || __shfl_sync(0xffffffffu, g.rows, 0) > 128;
-            const int nt = __shfl_sync(0xffffffffu, g.k1 - g.k0, 0);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
-            if (nt == 0) break;
-            if (!mine) {  // no rows here: only hand the stages back
-                for (int j = 0; j < 2 * nt; ++j) {
-                    GMS_WAIT(full + 8 * ks, kph);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(empty + 8 * ks);
-                    if (++ks == NS) ks = 0, kph ^= 1u;
+                    for (int slot = 0; slot < 2; ++slot) {
+                        if (!ok || slot * 128 >= g.rows) continue;
+                        ok = __all_sync(0xffffffffu, wait_or_abort(q_empty + 8 * slot, (q_n[slot] & 1u) ^ 1u, abort, a.status));
+                        if (!ok) continue;
+                        if (lane == 0) {
+                            mbar_expect(q_full + 8 * slot, F::kTileBytes);
+                            for (int h = 0; h < F::kHalves; ++h)
+                                tma_load_3d(q_smem + slot * F::kTileBytes + h * F::kHalfBytes, &qmap, h * 64, head * (int)a.group,
+                                            g.q0 + (g.row0 + slot * 128) / (int)a.group, q_full + 8 * slot);
+                        }
+                        ++q_n[slot];
+                    }
                 }
-                continue;
+                for (int k = g.k0; ok && k < k1; ++k) {
+                    const int blk = next, t = seg_tile(g, k) * kTile + part * (int)box_tokens;
+                    if (k + 1 < k1) next = block_of(k + 1);
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t st = n % NS;
+                        ok = __all_sync(0xffffffffu, wait_or_abort(empty + 8 * st, ((n / NS) & 1u) ^ 1u, abort, a.status));
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect(full + 8 * st, F::kTileBytes);
+                        __syncwarp();
+                        if ((int)lane < boxes)
+                            tma_load_4d(ring + st * F::kTileBytes + half * F::kHalfBytes + part * box_tokens * 128, v ? &vmap : &kmap, half * 64,
+                                        (int)((uint32_t)t & tok_mask), head, blk, full + 8 * st, policy);
+                        ++n;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
             }
-            uint32_t k = k_lo + (ks * F::kTileBytes >> 4);
-            GMS_WAIT(full + 8 * ks, kph);
-            GMS_WAIT(q_full + my_q, items & 1u);
-            GMS_WAIT(my_o, (tiles & 1u) ^ 1u);  // P V of the last item: its buffers are free
-            GMS_WAIT(my_o + 8, (tiles & 1u) ^ 1u);
-            tc_fence_after();
+            if (!ok)  // give up: wait (bounded) for what is still on its way into this CTA's shared memory
+                for (uint32_t i = n > (uint32_t)NS ? n - NS : 0; i < n; ++i) (void)mbar_wait(full + 8 * (i % NS), (i / NS) & 1u);
+            for (int slot = 0; !ok && slot < 2; ++slot)
+                if (q_n[slot]) (void)mbar_wait(q_full + 8 * slot, (q_n[slot] - 1) & 1u);
+        } else {
+            // ------------------------------------------------------------------ products of one slot (warp 8: slot 0, warp 11: slot 1)
+            constexpr uint32_t id_s = f16_idesc(128, 64, IsBf16<T>::value, false), id_o = f16_idesc(128, D, IsBf16<T>::value, true);
+            // Straight-line code a tile: these warps compete for issue with two softmax warps each, every instruction counts.
+#define GMS_WAIT(bar, parity)                                                             \
+        if (!__all_sync(0xffffffffu, mbar_spin(bar, parity, 4096)) &&                         \
+            !__all_sync(0xffffffffu, wait_slow(bar, parity, abort, a.status)))                \
+            goto products_done
+            const uint32_t on = one_lane(), slot = warp == 8 ? 0u : 1u;
+            constexpr uint32_t hi = desc_hi(1024), half_k = 64 * 128 >> 4, half_v = 4 * 2048 >> 4;
+            const uint32_t q_lo = desc_lo(q_smem + slot * F::kTileBytes, 16), k_lo = desc_lo(ring, 16), v_lo = desc_lo(ring, F::kHalfBytes);
+            const uint32_t s_tm = tmem + slot * 128, o_tm = tmem + F::kO + slot * D;
+            const uint32_t my_s = s_full + 16 * slot, my_p = p_full + 16 * slot, my_o = o_done + 16 * slot, my_q = 8 * slot;
+            // S of one half of a K tile (k: its descriptor) into buffer b
+            auto scores = [&](uint32_t b, uint32_t k) {
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) {
+                    const uint32_t off = ((kk / 4) * F::kHalfBytes + (kk % 4) * 32) >> 4;
+                    mma_ss(on, s_tm + b * 64, q_lo + off, k + b * half_k + off, hi, id_s, kk > 0);
+                }
+                tc_commit(on, my_s + 8 * b);
+            };
+            auto values = [&](uint32_t b, uint32_t v, bool add) {
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) mma_ts(on, o_tm, s_tm + b * 64 + kk * 8, v + b * half_v + (kk * 2048 >> 4), hi, id_o, add || kk > 0);
+                tc_commit(on, my_o + 8 * b);
+            };
+            uint32_t ks = 0, kph = 0;       // stage of the next K tile (V follows it) and its phase
+            uint32_t tiles = 0, items = 0;  // of this slot so far (low bits count)
+            for (;; ++seg) {
+                GMS_WAIT(seg_full + 8 * (seg % kSegments), (seg / kSegments) & 1u);
+                const Segment &g = segs[seg % kSegments];
+                const bool mine = slot == 0 || __shfl_sync(0xffffffffu, g.rows, 0) > 128;
+                const int nt = __shfl_sync(0xffffffffu, g.k1 - g.k0, 0);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(seg_empty + 8 * (seg % kSegments));
+                if (nt == 0) break;
+                if (!mine) {  // no rows here: only hand the stages back
+                    for (int j = 0; j < 2 * nt; ++j) {
+                        GMS_WAIT(full + 8 * ks, kph);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(empty + 8 * ks);
+                        if (++ks == NS) ks = 0, kph ^= 1u;
+                    }
+                    continue;
+                }
+                uint32_t k = k_lo + (ks * F::kTileBytes >> 4);
+                GMS_WAIT(full + 8 * ks, kph);
+                GMS_WAIT(q_full + my_q, items & 1u);
+                GMS_WAIT(my_o, (tiles & 1u) ^ 1u);  // P V of the last item: its buffers are free
+                GMS_WAIT(my_o + 8, (tiles & 1u) ^ 1u);
+                tc_fence_after();
 #pragma unroll 1
-            for (uint32_t b = 0; b < 2; ++b) scores(b, k);
-            tc_commit(on, empty + 8 * ks);
-            if (nt == 1) tc_commit(on, q_empty + my_q);
-            for (int j = 0; j < nt; ++j) {
-                const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4);
-                const bool more = j + 1 < nt;
-                GMS_WAIT(full + 8 * vs, kph);
-                ks += 2;
-                if (ks == NS) ks = 0, kph ^= 1u;
-                k = k_lo + (ks * F::kTileBytes >> 4);
+                for (uint32_t b = 0; b < 2; ++b) scores(b, k);
+                tc_commit(on, empty + 8 * ks);
+                if (nt == 1) tc_commit(on, q_empty + my_q);
+                for (int j = 0; j < nt; ++j) {
+                    const uint32_t vs = ks + 1, v = v_lo + (vs * F::kTileBytes >> 4);
+                    const bool more = j + 1 < nt;
+                    GMS_WAIT(full + 8 * vs, kph);
+                    ks += 2;
+                    if (ks == NS) ks = 0, kph ^= 1u;
+                    k = k_lo + (ks * F::kTileBytes >> 4);
 #pragma unroll 1
-                for (uint32_t b = 0; b < 2; ++b) {
-                    GMS_WAIT(my_p + 8 * b, tiles & 1u);
-                    tc_fence_after();
-                    values(b, v, j > 0 || b > 0);
-                    if (more) {
-                        if (b == 0) GMS_WAIT(full + 8 * ks, kph);
-                        GMS_WAIT(my_o + 8 * b, tiles & 1u);  // P lies over S
+                    for (uint32_t b = 0; b < 2; ++b) {
+                        GMS_WAIT(my_p + 8 * b, tiles & 1u);
                         tc_fence_after();
-                        scores(b, k);
+                        values(b, v, j > 0 || b > 0);
+                        if (more) {
+                            if (b == 0) GMS_WAIT(full + 8 * ks, kph);
+                            GMS_WAIT(my_o + 8 * b, tiles & 1u);  // P lies over S
+                            tc_fence_after();
+                            scores(b, k);
+                        }
                     }
+                    tc_commit(on, empty + 8 * vs);
+                    if (more) tc_commit(on, empty + 8 * ks);
+                    if (j + 2 == nt) tc_commit(on, q_empty + my_q);
+                    ++tiles;
                 }
-                tc_commit(on, empty + 8 * vs);
-                if (more) tc_commit(on, empty + 8 * ks);
-                if (j + 2 == nt) tc_commit(on, q_empty + my_q);
-                ++tiles;
+                ++items;
             }
-            ++items;
-        }
-    products_done:
+        products_done:
 #undef GMS_WAIT
-        tc_commit(on, drain);  // nothing of this warp's is in flight when the CTA ends
-        (void)mbar_wait(drain, 0);
-        __syncwarp();
-    }
+            tc_commit(on, drain);  // nothing of this warp's is in flight when the CTA ends
+            (void)mbar_wait(drain, 0);
+            __syncwarp();
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ------------------------------------------------------------------ softmax, one thread a row
@@ -332,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
         uint32_t n = 0, tiles = 0;  // tiles of all segments so far; of this slot
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (!mbar_spin(bar, parity, 4096)) ok = wait_slow(bar, parity, abort, a.status);
-            __syncwarp();
+            if (!__all_sync(0xffffffffu, mbar_spin(bar, parity, 4096)))  // the warp goes on, or gives up, as one
+                ok = __all_sync(0xffffffffu, wait_slow(bar, parity, abort, a.status));
             return ok;
         };
         for (;; ++seg) {
@@ -382,70 +389,71 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 if (!wait(s_full + 8 * (2 * slot + half), tiles & 1u)) return;
                 tc_fence_after();
                 if (busy) {
-                uint32_t s[2][32];
-                tmem_ld32(s_col + half * 64, s[0]);
-                tmem_ld32(s_col + half * 64 + 32, s[1]);
-                tmem_wait32(s[0]);
-                tmem_wait32(s[1]);
-                if (edge) {
-                    const uint32_t v4 = valid >> (4 * half);
+                    uint32_t s[2][32];
+                    tmem_ld32(s_col + half * 64, s[0]);
+                    tmem_ld32(s_col + half * 64 + 32, s[1]);
+                    tmem_wait32(s[0]);
+                    tmem_wait32(s[1]);
+                    if (edge) {
+                        const uint32_t v4 = valid >> (4 * half);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int c0 = t0 + half * 64 + i * 32;
-                        const uint32_t held = ((v4 >> (2 * i) & 1u) ? 0xffffu : 0u) | ((v4 >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
-                        const uint32_t on = held & first_bits(pos + 1 - c0) & (~first_bits(low - c0) | first_bits(sink - c0));
-                        if (__all_sync(0xffffffffu, on == 0xffffffffu)) continue;
+                        for (int i = 0; i < 2; ++i) {
+                            const int c0 = t0 + half * 64 + i * 32;
+                            const uint32_t held = ((v4 >> (2 * i) & 1u) ? 0xffffu : 0u) | ((v4 >> (2 * i + 1) & 1u) ? 0xffff0000u : 0u);
+                            const uint32_t on = held & first_bits(pos + 1 - c0) & (~first_bits(low - c0) | first_bits(sink - c0));
+                            if (__all_sync(0xffffffffu, on == 0xffffffffu)) continue;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
-                    }
-                }
-                float tops[4];  // four chains
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(s[i / 2][(i % 2) * 16]);
-#pragma unroll
-                for (int j = 1; j < 15; j += 2)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + j])), __uint_as_float(s[i / 2][(i % 2) * 16 + j + 1]));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + 15]));
-                const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), neg_inf()) * c2;
-                const bool grow = top > m + kLag || (m == neg_inf() && top != m);
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
-                    if (grow) m = top;
-                    l *= f;
-                    if (k != k0 || half) {  // O is at rest between the last step's product and this step's handing over
-                        if (!wait(o_done + 8 * (2 * slot + (half ^ 1)), (tiles + (half ^ 1)) & 1u)) return;
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t o[32];
-                            tmem_ld32(o_col + i * 32, o);
-                            tmem_wait32(o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                            tmem_st32(o_col + i * 32, o);
+                            for (int j = 0; j < 32; ++j)
+                                if (!(on >> j & 1u)) s[i][j] = 0xff800000u;
                         }
                     }
-                }
-                const float z = m == neg_inf() ? 0.f : m;
-                const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
-                float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                uint32_t pk[32];
+                    float tops[4];  // four chains
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
-                    x = fma2(x, cc, zz);
-                    x.x = ex2(x.x);
-                    x.y = ex2(x.y);
-                    part[j & 1] = add2(part[j & 1], x);
-                    pk[j] = pack2(x.x, x.y, T());
-                }
-                tmem_st32(s_col + half * 64, pk);
-                part[0] = add2(part[0], part[1]);
-                l += part[0].x + part[0].y;
+                    for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(s[i / 2][(i % 2) * 16]);
+#pragma unroll
+                    for (int j = 1; j < 15; j += 2)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + j])),
+                                            __uint_as_float(s[i / 2][(i % 2) * 16 + j + 1]));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tops[i] = fmaxf(tops[i], __uint_as_float(s[i / 2][(i % 2) * 16 + 15]));
+                    const float top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), neg_inf()) * c2;
+                    const bool grow = top > m + kLag || (m == neg_inf() && top != m);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float f = grow ? (m == neg_inf() ? 0.f : ex2(m - top)) : 1.f;
+                        if (grow) m = top;
+                        l *= f;
+                        if (k != k0 || half) {  // O is at rest between the last step's product and this step's handing over
+                            if (!wait(o_done + 8 * (2 * slot + (half ^ 1)), (tiles + (half ^ 1)) & 1u)) return;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int i = 0; i < D / 32; ++i) {
+                                uint32_t o[32];
+                                tmem_ld32(o_col + i * 32, o);
+                                tmem_wait32(o);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                                tmem_st32(o_col + i * 32, o);
+                            }
+                        }
+                    }
+                    const float z = m == neg_inf() ? 0.f : m;
+                    const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        float2 x = make_float2(__uint_as_float(s[j / 16][(j * 2) % 32]), __uint_as_float(s[j / 16][(j * 2 + 1) % 32]));
+                        x = fma2(x, cc, zz);
+                        x.x = ex2(x.x);
+                        x.y = ex2(x.y);
+                        part[j & 1] = add2(part[j & 1], x);
+                        pk[j] = pack2(x.x, x.y, T());
+                    }
+                    tmem_st32(s_col + half * 64, pk);
+                    part[0] = add2(part[0], part[1]);
+                    l += part[0].x + part[0].y;
                 }
                 // Values of tokens that do not exist must not meet the product, whatever bits they are; nor those that no row
                 // of the unit sees, where rows are not done again.  Thread r of each slot clears token r of the tile before
@@ -461,7 +469,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                             for (int h = 0; h < F::kHalves; ++h)
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
-                                    st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 + ((e ^ (lane & 7)) << 4));
+                                    st_shared_zero16(ring + (vs % NS) * F::kTileBytes + h * F::kHalfBytes + row_in * 128 +
+                                                     ((e ^ (lane & 7)) << 4));
                         fence_proxy_async();
                     }
                 }
@@ -538,7 +547,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                     tmem_wait32(o);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                            make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                     __syncwarp();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {

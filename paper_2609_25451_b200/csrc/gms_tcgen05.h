@@ -5,7 +5,8 @@
 namespace gms {
 namespace ptx {
 
-// Shared-memory operand descriptor, 128-byte swizzle, as two words; (offset >> 4) may be added to the low one.  K-major operands: `sbo` bytes between groups of 8 rows (lbo unused).
+// Shared-memory operand descriptor, 128-byte swizzle, as two words; (offset >> 4) may be added to the low one.
+// K-major operands: `sbo` bytes between groups of 8 rows (lbo unused).
 // MN-major operands: `lbo` bytes between groups of 64 elements, `sbo` bytes between groups of 8 k.
 __host__ __device__ constexpr uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return (addr >> 4 & 0x3fffu) | (lbo >> 4 & 0x3fffu) << 16; }
 __host__ __device__ constexpr uint32_t desc_hi(uint32_t sbo) { return (sbo >> 4 & 0x3fffu) | 1u << 14 | 2u << 29; }
