@@ -251,3 +251,42 @@ def test_empty_calls():
     w = torch.ones((2, 2, 20), device="cuda")
     q.run(gms.kv_weights(w, w, decay=0.5))
     assert bool((w[0, :, :5] == 0.5).all()) and bool((w[0, :, 5:] == 1).all()) and bool((w[1] == 0.5).all())
+
+
+@pytest.mark.parametrize("dtype,dim,window", [(BF, 128, 0), (HF, 64, 9000)])
+def test_weights_of_a_long_cache(dtype, dim, window):
+    """Many chunks of tokens a CTA, more query rows than it holds at once, and few."""
+    for q_lens, kv_lens in (((33, 70), (20001, 3000)), ((9, 0), (30011, 77))):
+        p = Problem(18, dtype=dt(dtype), dim=dim, heads=24, kv_heads=8, block=16, q_lens=q_lens, kv_lens=kv_lens, window=window, sinks=5)
+        w = torch.zeros((2, 8, max(kv_lens)), device="cuda")
+        p.run(gms.kv_weights(None, w))
+        ref = p.reference()
+        p.check(ref)
+        for s, n in enumerate(kv_lens):
+            want = ref[s][4]
+            assert not bool(((w[s, :, :n].double() - want).abs() > ref[s][5] + 2.0 ** -23 * (q_lens[s] * 24 + 2) * want).any())
+
+
+def test_behind_a_call_that_is_still_writing():
+    """The kernels may be scheduled before their predecessor in the stream has drained; they must not read what it has yet to
+    write.  A restore of the pool's blocks (which lets its successors start early) goes directly before the attention."""
+    p = Problem(19, heads=8, kv_heads=2, q_lens=(1,) * 24, kv_lens=(3000,) * 24)
+    ids = torch.tensor(sum(p.table_h, []), dtype=torch.int32, device="cuda")
+    n_sel, per = len(ids), p.block_bytes // 4096
+    img = torch.empty((2, n_sel, p.block_bytes), dtype=torch.uint8, device="cuda")
+    bd = torch.zeros(n_sel * 2 * per, dtype=torch.int64, device="cuda")
+    st = torch.zeros(4, dtype=torch.int64, device="cuda")
+    gms.gms_kv_capture(p.desc, img, n_sel * p.block_bytes, p.block_bytes, gms.SRC_DEVICE, ids, n_sel, bd, None, st)
+    w = torch.zeros((24, 2, 3000), device="cuda")
+    weight = gms.kv_weights(None, w)
+    p.run(weight)
+    ref = p.reference()
+    p.check(ref)
+    want, lse, weights = p.out.clone(), p.lse.clone(), w.clone()
+    for _ in range(5):
+        p.raw.fill_(0xFF)
+        p.out.fill_(3)
+        gms.gms_kv_restore(p.desc, img, n_sel * p.block_bytes, p.block_bytes, gms.SRC_DEVICE, ids, n_sel, bd, None, st)
+        gms.gms_kv_attention(p.desc, p.layout, p.attn, weight)
+        torch.cuda.synchronize()
+        assert torch.equal(p.out, want) and torch.equal(p.lse, lse) and torch.equal(w, weights)
