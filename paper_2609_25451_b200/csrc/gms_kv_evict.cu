@@ -41,7 +41,8 @@ __device__ __forceinline__ uint32_t block_before(uint32_t x, uint32_t *sh, uint3
 // One CTA per (layer, sequence, KV head).  The weight that separates what stays from what goes is found in three passes from
 // the top (11, 11 and 10 bits of an order-preserving integer, a histogram each); then one pass in token order, four tokens a
 // thread, writes the kept positions.  The keys are held in shared memory (HELD: rows of up to 9,984 tokens; longer rows are
-// read again, from L2 mostly).  Latency counts: a row is a few thousand words, and one sequence has few rows.
+// read again, from L2 mostly).  Latency counts: a row is a few thousand words, and one sequence has few rows (601 tokens, 8 rows:
+// 8 us; with four 8-bit passes and one thread searching the bins 20 us).
 template <bool HELD>
 __global__ void __launch_bounds__(kSelThreads) kv_evict_select_kernel(const __grid_constant__ EvictArgs a)
 {
@@ -126,7 +127,9 @@ __global__ void __launch_bounds__(kSelThreads) kv_evict_select_kernel(const __gr
     for (uint32_t j = keep + tid; j < a.budget; j += kSelThreads) kept[j] = -1;
 }
 
-// Copies the kept rows: a CTA moves 64 tokens of one (layer, sequence, KV head), 16 bytes a lane.
+// Copies the kept rows: a CTA moves 64 tokens of one (layer, sequence, KV head), 16 bytes a lane; every row is read once and
+// written once, in whole 128- or 256-byte pieces.  Bound by memory: 4 sequences, 32 layers, 8 heads, 8k -> 2k tokens (2.15 GB):
+// 325 us = 6.6 TB/s of the call's 371 us.
 __global__ void __launch_bounds__(256) kv_evict_move_kernel(const __grid_constant__ EvictArgs a, uint32_t chunks)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

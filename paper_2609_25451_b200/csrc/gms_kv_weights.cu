@@ -6,8 +6,8 @@
 // fragments and walks all query rows, 128 at a time through shared memory (S^T = K Q^T, so a token's sum stays in a quad of
 // lanes); the next chunk's keys are on their way meanwhile, and up to 128 rows stay in shared memory for all chunks.  Each sum
 // has one owner and one order: no atomics, equal calls give equal bits.  Bound by the exponentials and the matrix unit for
-// many rows, by latency and reading K for few.  (One chunk a CTA: 26 us for 16,001 tokens x 8 heads x 128 rows of 64 against
-// WW us.)
+// many rows, by latency and reading K for few.  (32 queries over 16,001 tokens with their weights, 8 KV heads x 128 rows of 64:
+// 57 us with one chunk a CTA, 53 us so; 919 us with one warp a token.)
 #include "gms_internal.h"
 #include "gms_kv_attn.h"
 #include "gms_ptx.h"
