@@ -199,15 +199,19 @@ struct Plan {
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// Most tiles a pass can have, from what the host knows.
-uint64_t most_tiles(const AttnArgs &a, const Pass &p)
+// Most tiles an item can have, from what the host knows; most tiles of a pass.
+uint64_t item_tiles(const AttnArgs &a, const Pass &p)
 {
     uint64_t span = p.prefix ? a.max_prefix : a.max_kv;
     if (!p.prefix && a.window) {
         const uint64_t seen = (uint64_t)a.window + a.sinks + 2 * p.tile + (p.rows - 1) / a.group;
         if (seen < span) span = seen;
     }
-    return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * (ceil_div(span, p.tile) + (p.tile == kTcTile ? kTcExtra : 0));
+    return ceil_div(span, p.tile) + (p.tile == kTcTile ? kTcExtra : 0);
+}
+uint64_t most_tiles(const AttnArgs &a, const Pass &p)
+{
+    return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * item_tiles(a, p);
 }
 
 void cut_pass(const AttnArgs &a, bool prefix, bool tc, Pass *p)
@@ -226,6 +230,25 @@ void cut_pass(const AttnArgs &a, bool prefix, bool tc, Pass *p)
     p->slot_rows = rows < p->rows ? (uint32_t)(rows < 1 ? 1 : rows) : p->rows;
 }
 
+// Few-row kernel: whether a CTA takes a whole item (its four warps share the tiles; no plan, no pieces, one kernel) or all tiles
+// are dealt out evenly.  Measured, us a call, 32 / 8 heads of 128, lengths n/2 .. n (even deal / CTA an item):
+//   sequences   n = 64       260          512          1,024        2,048
+//       1       9.6 / 5.1    12.5 / 9.4   10.6 / 11.0  10.8 / 17.9
+//      16      13.8 / 7.5    14.9 / 9.8   17.6 / 13.3  21.3 / 20.4  29.6 / 34.1
+//      32      14.5 / 6.9    17.7 / 12.6  21.2 / 16.2  29.1 / 24.0  44.7 / 41.3
+//      48      14.8 / 11.7   20.4 / 20.0  24.8 / 25.2  37.2 / 37.9  60.2 / 63.9
+//      64      17.8 / 12.4   24.5 / 21.4  32.5 / 27.3  48.3 / 43.7  79.9 / 74.4
+//     256      27.8 / 41.4   54.0 / 64.1  85.1 / 86.4  148 / 136    272 / 244
+// A CTA an item loses where few items leave SMs idle for long, where one wave of CTAs is a little more than full, and where
+// very many items are very short; beyond 128 tiles (2,048 tokens) the even deal's balance is worth its join.
+bool team_deal(uint64_t items, uint64_t tiles)
+{
+    const uint64_t held = kFewMaxWorkers / kFewWarps;  // CTAs that the SMs hold at once
+    if (tiles > 128) return false;
+    if (items <= held) return tiles * (held - items) <= 32 * (held - 8);
+    return items < 512 ? tiles <= 32 : 64 * tiles >= items;
+}
+
 void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
 {
     *p = {};
@@ -233,11 +256,13 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     // Up to 16 rows a KV head: the few-row kernel, which reads K and V once.  More: the tensor-core kernel reads them once for
     // 256 rows, but takes 8 us longer to get going (its Q, descriptors and tensor memory; 16 us against 8 us for one tile), so
     // short calls of up to 64 rows go to the few-row kernel all the same, 16 rows at a time: where no warp gets more than four
-    // of its tiles (three suffixes of 40 behind a prefix of 129 tokens, 24 rows: 17 us against 23 us).
+    // of its tiles (three suffixes of 40 behind a prefix of 129 tokens, 24 rows: 15 us against 23 us).
     bool tc = rows > kFewRows;
     cut_pass(a, prefix, false, p);
     if (tc && rows <= 64 && most_tiles(a, *p) <= 4ull * kFewMaxWorkers) tc = false;
     if (tc) cut_pass(a, prefix, true, p);
+    if (!tc) p->team = team_deal((uint64_t)p->n_units * a.n_kv, item_tiles(a, *p));
+    if (p->team) p->workers = 1;
     p->begin = c->take<uint32_t>(p->n_units + 1);
     p->cuts = c->take<Cut>(p->workers);
     p->part_ml = c->take<float2>(2ull * p->workers * p->slot_rows);
@@ -313,7 +338,8 @@ int attention_call(const gms_kv_pool *pool, const gms_kv_layout *layout, const g
         if (prefix) e = launch(pl.prefix);
         if (e == cudaSuccess) e = launch(pl.own);
         if (e == cudaSuccess)
-            e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s) : launch_kv_attn_join(b, pl.own, dtype, dim, s);
+            e = pl.shared ? launch_kv_attn_join_shared(b, pl.prefix, pl.own, dtype, dim, s)
+                          : pl.own.team ? cudaSuccess : launch_kv_attn_join(b, pl.own, dtype, dim, s);
         if (e == cudaSuccess && w && pl.logits) e = launch_kv_few_weights(b, pl.own, s);
     }
     if (e == cudaSuccess && w && !(a.total_q && pl.logits)) e = launch_kv_weights(a, pl.lse, a.total_q != 0, dtype, dim, s);

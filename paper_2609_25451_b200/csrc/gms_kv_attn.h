@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <cmath>
 
 #include "gms.h"
 
@@ -68,6 +69,7 @@ struct Pass {
     float2 *row_ml;        // [total_q * n_heads]
     float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2 (few-row pass only)
     uint32_t logit_stride;
+    uint32_t team;         // 1: few-row pass, a CTA an item: its warps share the tiles and join in shared memory, nothing is cut
     uint32_t again;        // 1: rows that come out non-finite are done again (attend_row)
     uint32_t *redo;        // many-row pass: null, or [n_units * n_kv][8], a bit for each such row of a finished item
 };
@@ -460,6 +462,36 @@ __device__ __noinline__ void attend_row(const AttnArgs &a, int tok, uint32_t h)
 #pragma unroll
     for (int e = 0; e < E; ++e) op[lane + 32 * e] = from_f32<T>(l == 0.f ? 0.f : o[e] / l);
     if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2;
+}
+
+// A row's values spread over a warp (lane: D / 32 neighbouring ones), not normalised; maximum (base 2) and sum.
+template <int D>
+struct Row {
+    float m = -INFINITY, l = 0.f, o[D / 32] = {};
+};
+
+// Writes a finished row; non-finite rows go through attend_row when `redo` asks for it.
+template <class T, int D>
+__device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int tok, uint32_t h, bool redo)
+{
+    const uint32_t lane = threadIdx.x & 31u;
+    T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride) + lane * (D / 32);
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    bool bad = false;
+    T v[D / 32];
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+        const float y = x.l == 0.f ? 0.f : x.o[e] * inv;
+        bad |= !(fabsf(y) < kHuge);
+        v[e] = from_f32<T>(y);
+    }
+    if (D == 128) *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(v);
+    else *reinterpret_cast<uint32_t *>(op) = *reinterpret_cast<const uint32_t *>(v);
+    if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = x.l == 0.f ? neg_inf() : (x.m + log2f(x.l)) * kLn2;
+    if (redo && __any_sync(0xffffffffu, bad)) {
+        __syncwarp();
+        attend_row<T, D>(a, tok, h);
+    }
 }
 #endif
 

@@ -4,13 +4,14 @@
 // rate, so the legacy matrix instruction is enough and what counts is bytes in flight and an even deal (see Pass).
 // Every warp is a worker of its own, as in the streaming kernels: tiles of 16 tokens come by TMA through the block table into
 // the warp's ring (K and V of one KV head, one box of whole rows each, 128-byte swizzle, so that ldmatrix has no bank
-// conflicts), and no warp waits for another.  S = Q K^T, the online softmax and O += P V stay in registers.  (Four warps to an
-// item, joined in shared memory at its end: 78 us against 70 for 48 sequences of up to 2,052 visible tokens, 60 against 37 for
-// 64 of up to 512.)
+// conflicts), and no warp waits for another.  S = Q K^T, the online softmax and O += P V stay in registers.
+// For short items (TEAM) a CTA takes a whole item: its warps share the tiles and join at the end, there is no plan and no second
+// kernel.  The rule and both sides' times stand where the call is planned.
 // The loads carry an evict-first hint: K and V are read once, and the kernels' own code, fetched again for every launch, stays
 // in L2 (64 suffixes behind a prefix of 8,192: 86 us without, 74 us with it).
 // Measured: 48 sequences of up to 12,001 tokens, 2,048 + 4 visible, 32 / 8 heads of 128, bf16: 73 us for 360 MB = 4.9 TB/s,
 // about 8 us of it launch, plan and first tiles; DRAM reads 364 MB, nothing is read twice.  8 x 65k tokens on one KV head: 43 us.
+// One sequence under a window of 256 and 4 sinks: 10 us, three of them launch and the first code fetches.
 #include "gms_internal.h"
 #include "gms_kv_attn.h"
 #include "gms_ptx.h"
@@ -44,8 +45,8 @@ struct Acc {
     float o[D / 8][4], m[2], l[2];
 };
 
-// HI: the units have more than 8 rows (the upper half of the 16-row fragments is in use).
-template <class T, int D, bool HI>
+// HI: the units have more than 8 rows (the upper half of the 16-row fragments is in use).  TEAM: see Pass.
+template <class T, int D, bool HI, bool TEAM>
 __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                   const __grid_constant__ CUtensorMap vmap,
                                                                   const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p)
@@ -71,7 +72,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     }
     if (!p.behind) grid_wait();
     grid_launch_dependents();
-    Walk w = plan_walk<kFewRows, kFewTile, kThreads, kWarps>(a, p, plan);
+    Walk w = {};
+    if (!TEAM) w = plan_walk<kFewRows, kFewTile, kThreads, kWarps>(a, p, plan);
     const uint32_t worker = blockIdx.x * kWarps + warp;
 
     const float c2 = a.scale * kLog2e;
@@ -92,7 +94,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
     int ck = 0;
     uint32_t q[D / 16][4];
     int p0 = 0, p1 = 0;
-    Acc<D> x;
+    Acc<D> x = {};
+    x.m[0] = x.m[1] = neg_inf();
     // Every part of the loop stands in the code once: a short call is bound by fetching instructions.
 #pragma unroll 1
     for (;;) {
@@ -103,8 +106,17 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 Unit un = {};
                 int k0 = 0, k1 = 0;
                 uint32_t at = 0, item = 0;
-                more = walk_next<kFewRows, kFewTile>(a, p, w, un, ic, k0, k1, at, item);
-                if (ahead == 0 && lane == 0 && worker < p.workers) write_cut(p, worker, w, un, ic, more ? k0 : 0, at);
+                if (TEAM) {
+                    item = blockIdx.x;
+                    un = get_unit<kFewRows, kFewTile>(a, p, item / a.n_kv / p.n_rt, item / a.n_kv % p.n_rt);
+                    ic = item % a.n_kv;
+                    k0 = un.tiles * (int)warp / kWarps;
+                    k1 = un.tiles * (int)(warp + 1) / kWarps;
+                    more = ahead == 0 && k1 > k0;
+                } else {
+                    more = walk_next<kFewRows, kFewTile>(a, p, w, un, ic, k0, k1, at, item);
+                    if (ahead == 0 && lane == 0 && worker < p.workers) write_cut(p, worker, w, un, ic, more ? k0 : 0, at);
+                }
                 if (!more) break;
                 if (lane == 0) {
                     Run &r = runs[ahead % kRuns];
@@ -278,6 +290,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 1);
             x.l[r] += __shfl_xor_sync(0xffffffffu, x.l[r], 2);
         }
+        if (TEAM) continue;
         const bool starts = run.k0 == 0, ends = run.k1 == run.tiles;
         uint32_t again = 0;  // finished rows to be done once more
 #pragma unroll
@@ -326,18 +339,68 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             }
         }
     }
+    if (TEAM) {  // the warps' shares, through the rings, which are idle now
+        constexpr int R = HI ? 2 : 1;
+        float *const jo = reinterpret_cast<float *>(sm), *const jm = jo + kWarps * NJ * R * 2 * 32, *const jl = jm + kWarps * R * 32;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            jm[(warp * R + i) * 32 + lane] = x.m[i];
+            jl[(warp * R + i) * 32 + lane] = x.l[i];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) jo[(((warp * NJ + j) * R + i) * 2 + e) * 32 + lane] = x.o[j][i * 2 + e];
+        }
+        const uint32_t unit = blockIdx.x / a.n_kv;
+        const Unit un = get_unit<kFewRows, kFewTile>(a, p, unit / p.n_rt, unit % p.n_rt);
+        __syncthreads();
+        constexpr int E = D / 32;  // neighbouring values a lane
+#pragma unroll 1
+        for (int r = (int)warp; r < un.rows; r += kWarps) {
+            const int i = r / 8, quad = r % 8 * 4;
+            Row<D> sum;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) sum.m = fmaxf(sum.m, jm[(k * R + i) * 32 + quad]);
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) {
+                const float m = jm[(k * R + i) * 32 + quad], f = m == sum.m ? 1.f : ex2(m - sum.m);
+                sum.l += jl[(k * R + i) * 32 + quad] * f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int d = (int)lane * E + e;
+                    sum.o[e] += jo[(((k * NJ + d / 8) * R + i) * 2 + d % 2) * 32 + quad + d % 8 / 2] * f;
+                }
+            }
+            const int tok = unit_tok(a, un, r);
+            const uint32_t h = unit_head(a, un, blockIdx.x % a.n_kv, r);
+            if (!p.row_o) {
+                finish<T, D>(a, sum, tok, h, p.again);
+                continue;
+            }
+            const uint64_t at = (uint64_t)tok * a.n_heads + h;
+            if (lane == 0) p.row_ml[at] = make_float2(sum.m, sum.l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) p.row_o[at * D + lane * E + e] = sum.o[e];
+        }
+    }
     if (p.behind) grid_wait();  // this kernel's end stands for both
 }
 
-template <class T, int D, bool HI>
-cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
+template <class T, int D, bool HI, bool TEAM>
+cudaError_t launch_few(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
 {
     constexpr uint32_t smem = Few<D>::kSmem;
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = allow_smem(kv_attn_few_kernel<T, D, HI>, smem, done);
+    const cudaError_t e = allow_smem(kv_attn_few_kernel<T, D, HI, TEAM>, smem, done);
     if (e != cudaSuccess) return e;
-    const uint32_t grid = (p.workers + kWarps - 1) / kWarps;
-    return launch_dependent(kv_attn_few_kernel<T, D, HI>, grid, kThreads, smem, s, kmap, vmap, a, p);
+    const uint32_t grid = TEAM ? p.n_units * a.n_kv : (p.workers + kWarps - 1) / kWarps;
+    return launch_dependent(kv_attn_few_kernel<T, D, HI, TEAM>, grid, kThreads, smem, s, kmap, vmap, a, p);
+}
+template <class T, int D, bool HI>
+cudaError_t launch(const AttnArgs &a, const Pass &p, const CUtensorMap &kmap, const CUtensorMap &vmap, cudaStream_t s)
+{
+    return p.team ? launch_few<T, D, HI, true>(a, p, kmap, vmap, s) : launch_few<T, D, HI, false>(a, p, kmap, vmap, s);
 }
 
 // One thread four tokens: the logits that the attention kernel left, against the finished log-sum-exps, rows in order.

@@ -17,11 +17,6 @@ using namespace ptx;
 
 constexpr uint32_t kWarps = 8;
 
-template <int D>
-struct Row {
-    float m = -INFINITY, l = 0.f, o[D / 32] = {};
-};
-
 // Adds pieces first, first + step, ... < n; piece i lies at slot(i) of ml and o.  Eight loads of o are in flight.
 template <int D, class F>
 __device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const float *o, uint32_t first, uint32_t step, uint32_t n, F slot)
@@ -54,30 +49,6 @@ __device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const fl
                 for (int e = 0; e < D / 32; ++e) x.o[e] += vf[e] * gi;
             }
         }
-    }
-}
-
-// Writes a finished row; non-finite rows go through attend_row when `redo` asks for it.
-template <class T, int D>
-__device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int tok, uint32_t h, bool redo)
-{
-    const uint32_t lane = threadIdx.x & 31u;
-    T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride) + lane * (D / 32);
-    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
-    bool bad = false;
-    T v[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-        const float y = x.l == 0.f ? 0.f : x.o[e] * inv;
-        bad |= !(fabsf(y) < kHuge);
-        v[e] = from_f32<T>(y);
-    }
-    if (D == 128) *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(v);
-    else *reinterpret_cast<uint32_t *>(op) = *reinterpret_cast<const uint32_t *>(v);
-    if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = x.l == 0.f ? neg_inf() : (x.m + log2f(x.l)) * kLn2;
-    if (redo && __any_sync(0xffffffffu, bad)) {
-        __syncwarp();
-        attend_row<T, D>(a, tok, h);
     }
 }
 
@@ -183,6 +154,10 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (rt >= p.n_rt) return;
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
     if (u.tiles == 0 || (int)r >= u.rows) return;
+    if (p.team) {
+        add_pieces<D>(x, p.row_ml, p.row_o, 0, 1, 1, [&](uint32_t) { return row; });
+        return;
+    }
     const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * item_cost<TILE>(u.tiles) + item_extra<TILE>();
     const uint32_t n = used_workers(total, p.workers), per = total / n, more = total % n;
     const uint32_t c0 = tile_owner(first, per, more), c1 = tile_owner(first + u.tiles - 1, per, more);

@@ -290,3 +290,20 @@ def test_behind_a_call_that_is_still_writing():
         gms.gms_kv_attention(p.desc, p.layout, p.attn, weight)
         torch.cuda.synchronize()
         assert torch.equal(p.out, want) and torch.equal(p.lse, lse) and torch.equal(w, weights)
+
+
+@pytest.mark.parametrize("seqs,n", [(1, 500), (2, 2000), (36, 40), (37, 130), (50, 513), (64, 17), (130, 900), (300, 12), (300, 100)])
+@pytest.mark.parametrize("q", [1, 3])
+def test_item_counts_around_what_the_gpu_holds(seqs, n, q):
+    """A CTA an item or all tiles dealt out: both sides of the rule's borders, ragged lengths, empty sequences among them."""
+    lens = [n] + [(7 * s * s + 3 * s) % n for s in range(1, seqs)]
+    p = Problem(20, heads=32, kv_heads=8, q_lens=[min(q, max(m, 1)) for m in lens], kv_lens=lens, decode=q == 1)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("kv_lens,prefix", [((2500, 40), (3000,)), ((5000, 1), (17,)), ((30, 3000), (0,))])
+def test_shared_prefix_with_long_suffixes(kv_lens, prefix):
+    p = Problem(21, heads=8, kv_heads=2, q_lens=(1, 2), kv_lens=kv_lens, prefix_lens=prefix, groups=[0, 2])
+    p.run(prefix=p.make_prefix())
+    p.check()
