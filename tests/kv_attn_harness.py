@@ -166,7 +166,7 @@ class Problem:
                 c = h // G
                 k, v = K[:, c], V[:, c]
                 x = (Q[:, h] @ torch.where(torch.isfinite(k), k, 0.0).T) * self.scale
-                mag = (Q[:, h].abs() @ torch.where(torch.isfinite(k), k, 0.0).abs().T) * self.scale
+                mag = (Q[:, h].abs() @ torch.where(torch.isfinite(k), k, 0.0).abs().T) * abs(self.scale)
                 x = torch.where(vis, x, -math.inf)
                 has = vis.any(1)
                 m = torch.where(has, x.amax(1), 0.0)

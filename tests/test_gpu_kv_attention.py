@@ -307,3 +307,17 @@ def test_shared_prefix_with_long_suffixes(kv_lens, prefix):
     p = Problem(21, heads=8, kv_heads=2, q_lens=(1, 2), kv_lens=kv_lens, prefix_lens=prefix, groups=[0, 2])
     p.run(prefix=p.make_prefix())
     p.check()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.05, 1.0])
+@pytest.mark.parametrize("heads,kv_heads,q", [(8, 2, 1), (8, 2, 90), (12, 4, 60), (3, 3, 200)])
+def test_scales(scale, heads, kv_heads, q):
+    """Zero (the mean of what is seen), negative, and large; head groups that do and do not divide 128 rows."""
+    p = Problem(22, heads=heads, kv_heads=kv_heads, q_lens=(q, q), kv_lens=(q + 150, q + 11), window=70, sinks=2)
+    p.scale = p.attn.scale = scale
+    w = torch.zeros((2, kv_heads, q + 150), device="cuda")
+    p.run(gms.kv_weights(None, w))
+    ref = p.reference()
+    p.check(ref)
+    for s, n in enumerate(p.kv_lens):
+        assert not bool(((w[s, :, :n].double() - ref[s][4]).abs() > ref[s][5] + 2.0 ** -23 * (q * heads + 2) * ref[s][4]).any())
