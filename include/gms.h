@@ -475,18 +475,19 @@ int gms_kv_attention_shared(const gms_kv_pool *pool, const gms_kv_layout *layout
  * When n <= budget all stay.  The kept tokens keep their order:
  *   kept[l][s][c][j]         position of the j-th kept token, j < n' (-1 for n' <= j < budget)
  *   weights_out[l][s][c][j]  its weight (entries from n' on are left alone)
- *   lens_out[s] = n'
+ *   lens_out[s] = n'; lens_out may be lens (then the lengths are updated in place), but may not overlap it otherwise
  *   K and V of token kept[j] are copied to token j of the blocks dst_table[s*dst_stride + ...]
  * Destination blocks must be distinct and must not be source blocks (the old ones are free once the call has run); a row
  * whose source or destination id lies outside the pool is not copied.  Keys carry their positions (rotary embeddings)
  * with them; afterwards the sequence is n' tokens long for gms_kv_attention.  Lens above max_len count as max_len.
- * Errors: NULL, ALIGN, ARG (sinks + recent > budget; planes outside the pool), RANGE, CUDA.
+ * Errors: NULL, ALIGN, ARG (sinks + recent > budget; planes outside the pool; weights_out or lens_out where
+ * they may not be), RANGE, CUDA.
  */
 typedef struct {
     const float *weights;               /* (device) w_*_stride elements between layers, sequences, heads */
-    float *weights_out;                 /* (device) may be NULL; o_*_stride; not `weights` itself        */
+    float *weights_out;                 /* (device) may be NULL; o_*_stride; must not overlap `weights`   */
     const int32_t *lens;                /* (device) n_seq                                                */
-    int32_t *lens_out;                  /* (device) n_seq, may be NULL                                   */
+    int32_t *lens_out;                  /* (device) n_seq, may be NULL, may be lens                      */
     const int32_t *src_table, *dst_table;
     int32_t *kept;                      /* (device) [n_layers][n_seq][n_kv_heads][budget]                */
     uint64_t w_layer_stride, w_seq_stride, w_head_stride;

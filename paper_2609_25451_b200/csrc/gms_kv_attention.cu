@@ -416,6 +416,7 @@ int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms
     if (!t->lens || (t->max_len && (!t->weights || !t->src_table)) || (t->budget && !t->kept) || (most && !t->dst_table))
         return GMS_ERR_NULL;
     if (t->weights_out && t->weights_out == t->weights) return GMS_ERR_ARG;
+    if (t->lens_out && t->lens_out != t->lens && t->lens_out < t->lens + t->n_seq && t->lens < t->lens_out + t->n_seq) return GMS_ERR_ARG;
     gms::EvictArgs a = {};
     a.base = static_cast<uint8_t *>(pool->base);
     a.plane_stride = pool->plane_stride;

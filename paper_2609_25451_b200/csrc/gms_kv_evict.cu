@@ -56,7 +56,9 @@ __global__ void __launch_bounds__(kSelThreads) kv_evict_select_kernel(const __gr
     float *wo = a.weights_out ? a.weights_out + l * a.o_layer_stride + s * a.o_seq_stride + c * a.o_head_stride : nullptr;
     int32_t *kept = a.kept + (uint64_t)row * a.budget;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (l == 0 && c == 0 && tid == 0 && a.lens_out) a.lens_out[s] = (int32_t)keep;
+    // lens_out may be lens itself: the other CTAs of the sequence read it here, so the next kernel writes it.  Without one
+    // (budget or max_len 0) keep is 0 whatever they read.
+    if (min(a.max_len, a.budget) == 0 && l == 0 && c == 0 && tid == 0 && a.lens_out) a.lens_out[s] = 0;
     const uint32_t lo = a.sinks, hi = n > keep ? n - a.recent : 0;  // the tokens that compete (n > keep only)
     uint32_t limit = 0xffffffffu, take = 0;                        // kept: key > limit, and the first `take` equal to it
     auto key = [&](uint32_t t) { return HELD ? keys[t - lo] : weight_key(w[t]); };
@@ -135,7 +137,9 @@ __global__ void __launch_bounds__(256) kv_evict_move_kernel(const __grid_constan
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t row = blockIdx.x / chunks, j0 = blockIdx.x % chunks * 64;
     const uint32_t c = row % a.n_kv, s = row / a.n_kv % a.n_seq, l = row / a.n_kv / a.n_seq;
+    // whether this reads the length from before the call or the one that another CTA has just written over it, keep is the same
     const uint32_t keep = min((uint32_t)min(max(a.lens[s], 0), (int)a.max_len), a.budget);
+    if (l == 0 && c == 0 && j0 == 0 && threadIdx.x == 0 && a.lens_out) a.lens_out[s] = (int32_t)keep;
     const uint32_t per_row = a.row_bytes / 16, part = threadIdx.x % per_row, mask = (1u << a.block_shift) - 1u;
     const int32_t *kept = a.kept + (uint64_t)row * a.budget;
     uint8_t *kp = a.base + (uint64_t)(a.k_plane + l * a.layer_planes) * a.plane_stride;
