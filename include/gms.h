@@ -397,8 +397,10 @@ typedef struct {
  * over the t that it sees; if there are none, out is 0 and lse is -infinity.  What a query does not see cannot reach
  * its output, whatever bits it holds (NaN, infinities).  Products are taken in the pool's type with 32-bit sums; the
  * softmax weights are rounded to the pool's type before the product with V.
- * kv_lens above max_kv, and queries of a sequence beyond max_q, are not processed (the host sizes the launch by
- * these); rows of q that no sequence owns leave out and lse as they are.
+ * The host sizes the launch by max_q and max_kv.  Of a sequence with more queries the first max_q are processed, of one
+ * with more tokens only the first max_kv are seen (and have weights); what is left out changes no position: query i of
+ * q_len stands at kv_lens[s] - q_len + i all the same.  Rows of q that are not processed or that no sequence owns leave
+ * out and lse as they are.  Neither may overlap anything that is read.
  */
 typedef struct {
     const void *q;                 /* (device) [total_q][n_heads][head_dim], 16-byte aligned             */
@@ -450,7 +452,8 @@ int gms_kv_attention(const gms_kv_pool *pool, const gms_kv_layout *layout, const
  * after it.  Every query sees the whole prefix, then its own sequence's tokens up to its own.  The prefix is read once
  * for all rows of the group, not once a sequence.  attn->window and attn->sinks must be 0.
  * group_start[0] = 0 and group_start[n_groups] = n_seq: a sequence outside every group gets the tokens of its own
- * alone.  Errors: as gms_kv_attention.
+ * alone.  Rows of a group beyond its first max_group_q are not processed, tokens of a prefix beyond max_prefix not seen.
+ * Errors: as gms_kv_attention.
  */
 typedef struct {
     const int32_t *group_start;   /* (device) n_groups + 1, ascending                                    */

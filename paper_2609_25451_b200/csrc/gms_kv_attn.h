@@ -151,7 +151,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return 
 template <> __device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
 
 // Query rows and cached tokens of one sequence, clamped to what the host announced (so that no index leaves a buffer
-// whatever the device arrays hold).
+// whatever the device arrays hold).  Positions go by the lengths themselves: what is left out shifts nothing.
 __device__ __forceinline__ int seq_q_begin(const AttnArgs &a, uint32_t s)
 {
     return a.cu_q ? min(max(a.cu_q[s], 0), (int)a.total_q) : (int)s;
@@ -163,6 +163,11 @@ __device__ __forceinline__ int seq_q_len(const AttnArgs &a, uint32_t s)
     return min(max(min(a.cu_q[s + 1], (int)a.total_q) - b, 0), (int)a.max_q);
 }
 __device__ __forceinline__ int seq_kv_len(const AttnArgs &a, uint32_t s) { return min(max(a.kv_lens[s], 0), (int)a.max_kv); }
+// Position of a sequence's first query.
+__device__ __forceinline__ int seq_first(const AttnArgs &a, uint32_t s)
+{
+    return max(a.kv_lens[s], 0) - (a.cu_q ? max(min(a.cu_q[s + 1], (int)a.total_q) - seq_q_begin(a, s), 0) : 1);
+}
 __device__ __forceinline__ int prefix_len(const AttnArgs &a, uint32_t g)
 {
     return min(max(a.prefix_lens[g], 0), (int)a.max_prefix);
@@ -200,7 +205,7 @@ struct Unit {
     const int32_t *table;
     int q0, row0, rows;      // first query row of the sequence (group); first row of the unit and their number
     int n, first;            // cached tokens; position of the sequence's first query
-    int pos_min, pos_max;    // of the unit's rows
+    int pos_min, pos_max;    // of the unit's rows (at n or beyond it where the call leaves out the newest tokens)
     int n_sink_tiles, first_tile, tiles;  // tile list: 0 .. n_sink_tiles-1, then first_tile ..; `tiles` in all
     bool whole;              // every row sees every token
 };
@@ -229,14 +234,15 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
         u.n = prefix_len(a, s);
         u.table = a.prefix_table + s * a.prefix_stride;
         u.whole = true;
+        u.first = u.n - q_len;
     } else {
         u.q0 = seq_q_begin(a, s);
         q_len = seq_q_len(a, s);
         u.n = seq_kv_len(a, s);
         u.table = a.table + s * a.table_stride;
         u.whole = false;
+        u.first = seq_first(a, s);
     }
-    u.first = u.n - q_len;
     u.row0 = (int)rt * ROWS;
     u.rows = max(min(q_len * (int)a.group - u.row0, ROWS), 0);  // total_q * n_heads < 2^31
     u.n_sink_tiles = u.first_tile = u.tiles = 0;
@@ -244,17 +250,19 @@ __device__ __forceinline__ Unit get_unit(const AttnArgs &a, const Pass &p, uint3
     if (u.rows > 0) {
         if (!u.whole) {
             u.pos_min = u.first;
+            u.pos_max = u.first + q_len - 1;
             if (p.n_rt > 1) {
                 u.pos_min += u.row0 / (int)a.group;
                 u.pos_max = u.first + (u.row0 + u.rows - 1) / (int)a.group;
             }
         }
-        if (u.pos_max >= 0) {
+        const int last = min(u.pos_max, u.n - 1);
+        if (last >= 0) {
             if (!u.whole && a.window != 0 && u.pos_min >= 0 && (uint32_t)u.pos_min >= a.window) {
-                u.first_tile = (u.pos_min - (int)a.window + 1) / TILE;
+                u.first_tile = min((u.pos_min - (int)a.window + 1) / TILE, last / TILE + 1);
                 u.n_sink_tiles = (int)min((uint32_t)u.first_tile, a.sinks / TILE + (a.sinks % TILE != 0));
             }
-            u.tiles = u.n_sink_tiles + u.pos_max / TILE + 1 - u.first_tile;
+            u.tiles = u.n_sink_tiles + last / TILE + 1 - u.first_tile;
         }
     }
     return u;
@@ -457,7 +465,7 @@ __device__ __noinline__ void attend_row(const AttnArgs &a, int tok, uint32_t h)
     const uint32_t g = group_of_seq(a, s);
     if (g < a.n_groups) attend_tokens<T, D>(a, q, c, a.prefix_table + g * a.prefix_stride, prefix_len(a, g), 0, true, m, l, o);
     const int n = seq_kv_len(a, s);
-    attend_tokens<T, D>(a, q, c, a.table + s * a.table_stride, n, n - seq_q_len(a, s) + tok - seq_q_begin(a, s), false, m, l, o);
+    attend_tokens<T, D>(a, q, c, a.table + s * a.table_stride, n, seq_first(a, s) + tok - seq_q_begin(a, s), false, m, l, o);
     T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride);
 #pragma unroll
     for (int e = 0; e < E; ++e) op[lane + 32 * e] = from_f32<T>(l == 0.f ? 0.f : o[e] / l);

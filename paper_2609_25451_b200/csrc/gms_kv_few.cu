@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[j][e] *= c2;
             const int t1 = t0 + kFewTile - 1;
-            const bool full = !hole && t1 <= run.pos_min &&
+            const bool full = !hole && t1 <= run.pos_min && t1 < run.n &&
                               (run.whole || a.window == 0 || (long long)t0 > (long long)run.pos_max - (long long)a.window || (uint32_t)t1 < a.sinks);
             if (!full) {
 #pragma unroll
@@ -213,13 +213,13 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int t = t0 + j * 8 + (int)(lane & 3u) * 2 + (e & 1);
-                        const bool on = !hole && (run.whole ? t < run.n : sees(a, e < 2 ? p0 : p1, t));
+                        const bool on = !hole && t < run.n && (run.whole || sees(a, e < 2 ? p0 : p1, t));
                         if (!on) s[j][e] = neg_inf();
                     }
                 // values that no row sees must not meet the matrix product, whatever bits they are
                 if (lane < kFewTile) {
                     const int t = t0 + (int)lane;
-                    const bool none = t > run.pos_max || (!run.whole && !sees(a, max(run.pos_min, t), t));
+                    const bool none = t >= run.n || t > run.pos_max || (!run.whole && !sees(a, max(run.pos_min, t), t));
                     if (none)
 #pragma unroll
                         for (int h = 0; h < F::kHalves; ++h)

@@ -143,20 +143,22 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     }
 }
 
-// Adds what a pass has for one (query row, head); s: sequence, or group in the prefix pass.
+// Adds what a pass has for one (query row, head); s: sequence, or group in the prefix pass.  False: the pass has left the row out
+// (max_group_q).
 template <int D, int ROWS, int TILE>
-__device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s, int tok, uint32_t h)
+__device__ bool add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s, int tok, uint32_t h)
 {
     const uint64_t row = (uint64_t)tok * a.n_heads + h;
     const uint32_t c = h / a.group;
     Unit u = get_unit<ROWS, TILE>(a, p, s, 0);
     const uint32_t in = (uint32_t)(tok - u.q0) * a.group + h % a.group, rt = in / ROWS, r = in % ROWS;
-    if (rt >= p.n_rt) return;
+    if (rt >= p.n_rt) return false;
     if (rt) u = get_unit<ROWS, TILE>(a, p, s, rt);
-    if (u.tiles == 0 || (int)r >= u.rows) return;
+    if ((int)r >= u.rows) return false;
+    if (u.tiles == 0) return true;
     if (p.team) {
         add_pieces<D>(x, p.row_ml, p.row_o, 0, 1, 1, [&](uint32_t) { return row; });
-        return;
+        return true;
     }
     const uint32_t total = p.begin[p.n_units], first = p.begin[s * p.n_rt + rt] + c * item_cost<TILE>(u.tiles) + item_extra<TILE>();
     const uint32_t n = used_workers(total, p.workers), per = total / n, more = total % n;
@@ -164,6 +166,7 @@ __device__ void add_pass(const AttnArgs &a, const Pass &p, Row<D> &x, uint32_t s
     if (c0 == c1) add_pieces<D>(x, p.row_ml, p.row_o, 0, 1, 1, [&](uint32_t) { return row; });
     else
         add_pieces<D>(x, p.part_ml, p.part_o, 0, 1, c1 - c0 + 1, [&](uint32_t k) { return ((uint64_t)(c0 + k) * 2 + (k == 0)) * p.slot_rows + r; });
+    return true;
 }
 
 template <class T, int D>
@@ -179,8 +182,8 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
     Row<D> x;
     const uint32_t g = group_of_seq(a, s);
     if (g < a.n_groups) {
-        if (pre.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, pre, x, g, tok, h);
-        else add_pass<D, kFewRows, kFewTile>(a, pre, x, g, tok, h);
+        if (!(pre.rows == kTcRows ? add_pass<D, kTcRows, kTcTile>(a, pre, x, g, tok, h) : add_pass<D, kFewRows, kFewTile>(a, pre, x, g, tok, h)))
+            return;
     }
     if (own.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, own, x, s, tok, h);
     else add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);

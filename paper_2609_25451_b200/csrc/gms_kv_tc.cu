@@ -380,11 +380,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
             }
 
             const bool live = row < rows, busy = slot * 128 + (int)(warp % 4) * 32 < rows;  // a warp without rows computes nothing
-            const int pos = pos_of(live ? row : rows - 1), pos_lo = pos_of(slot * 128), pos_hi = pos_of(min(slot * 128 + 127, rows - 1));
+            const int pos_own = pos_of(live ? row : rows - 1), pos_hi = pos_of(min(slot * 128 + 127, rows - 1));
+            const int pos = min(pos_own, len - 1), pos_lo = min(pos_of(slot * 128), len - 1);  // the newest token seen, of the row and at least
             const int32_t *table = g.table;
             // the row's window starts at low; low_hi: the latest start among the slot's rows; sink: tokens always seen
             auto low_of = [&](int ps) { return all || a.window == 0 || (uint32_t)max(ps, 0) < a.window ? 0 : ps - (int)a.window + 1; };
-            const int low = low_of(pos), low_hi = low_of(pos_hi), sink = (int)min(a.sinks, 0x7fffffffu);
+            const int low = low_of(pos_own), low_hi = low_of(pos_hi), sink = (int)min(a.sinks, 0x7fffffffu);
             float m = neg_inf(), l = 0.f;
             const int n_sink_tiles = g.n_sink_tiles, past_sinks = g.first_tile - n_sink_tiles;
             if (!wait(seg_holes + 8 * (seg % kSegments), (seg / kSegments) & 1u)) break;

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_const
     int *const pos_sh = reinterpret_cast<int *>(lse_sh + kRows);
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
     const uint32_t item = blockIdx.x / parts, c = item % a.n_kv, s = item / a.n_kv;
-    const int n = seq_kv_len(a, s), q0 = seq_q_begin(a, s), q_len = seq_q_len(a, s), rows = q_len * (int)a.group, first = n - q_len;
+    const int n = seq_kv_len(a, s), q0 = seq_q_begin(a, s), q_len = seq_q_len(a, s), rows = q_len * (int)a.group, first = seq_first(a, s);
     const int32_t *const table = a.table + s * a.table_stride;
     const float c2 = a.scale * kLog2e;
     auto held = [&](int t) { return t < n && (uint32_t)table[(uint32_t)t >> a.block_shift] < a.n_blocks; };
