@@ -122,7 +122,8 @@ __global__ void __launch_bounds__(kThreads) kv_weights_kernel(const __grid_const
                 }
                 const int r = j + (int)(lane & 3u) * 2;
                 const float l0 = lse_sh[r], l1 = lse_sh[r + 1];
-                if (all_whole) {
+                // the rows that fill up the last eight go the masked way: their zeros times a key that holds an infinity are NaN
+                if (all_whole && j + 8 <= here) {
 #pragma unroll
                     for (int m = 0; m < 2; ++m) {
                         sum[2 * m] += ex2(fmaf(acc[m][0], c2, -l0)) + ex2(fmaf(acc[m][1], c2, -l1));
