@@ -15,7 +15,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr uint32_t kWarps = 8;
+constexpr uint32_t kWarps = 8, kLookers = 2 * 148;
 
 // Adds pieces first, first + step, ... < n; piece i lies at slot(i) of ml and o.  Eight loads of o are in flight.
 template <int D, class F>
@@ -56,7 +56,7 @@ __device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const fl
 // the item into which the border before worker i + 1 falls, if that is its first border.  Also: rows of units that see
 // nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
 template <class T, int D, int ROWS, int TILE>
-__global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
+__global__ void __launch_bounds__(kWarps * 32, D == 64 ? 4 : 3) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
                                                                    uint32_t parts, uint32_t rows_a_block,
                                                                    uint32_t by_item)
 {
@@ -76,17 +76,26 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_kernel(const __grid_
     grid_wait();
     const uint32_t i = blockIdx.x / parts, row_first = blockIdx.x % parts * rows_a_block, warp = threadIdx.x / 32;
     if (p.redo) {  // rows of finished items that came out non-finite; a cut item's words are zero
-        for (uint32_t w = blockIdx.x * kWarps + warp; w < p.n_units * a.n_kv; w += gridDim.x * kWarps) {
-            const uint32_t unit = w / a.n_kv;
-            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
-            if (u.tiles == 0) continue;  // sees nothing: no words were written
-            const uint32_t mine = (threadIdx.x & 31u) < 8 ? p.redo[(uint64_t)w * 8 + (threadIdx.x & 31u)] : 0u;
-            if (!__any_sync(0xffffffffu, mine)) continue;
-            for (uint32_t k = 0; k < 8; ++k)
-                for (uint32_t rows = __shfl_sync(0xffffffffu, mine, k); rows; rows &= rows - 1) {
-                    const int r = (int)k * 32 + __ffs(rows) - 1;
-                    attend_row<T, D>(a, unit_tok(a, u, r), unit_head(a, u, w % a.n_kv, r));
+        // a word has 32 rows, four for each warp; neighbouring words go to different blocks of the first ones (with all blocks
+        // looking, each wave of them paid for a load from L2: windowed prompt 247 us, so 242)
+        const uint64_t words = (uint64_t)p.n_units * a.n_kv * 8;
+        const uint32_t lookers = blockIdx.x < kLookers ? min(gridDim.x, kLookers) : 0;
+        const uint32_t lane = threadIdx.x & 31u;
+        for (uint64_t w0 = blockIdx.x; lookers && w0 < words; w0 += 32ull * lookers) {
+            const uint64_t mine = w0 + (uint64_t)lane * lookers;
+            const uint32_t rows = mine < words ? p.redo[mine] : 0u;
+            for (uint32_t some = __ballot_sync(0xffffffffu, rows != 0); some; some &= some - 1) {
+                const uint64_t word = w0 + (uint64_t)(__ffs(some) - 1) * lookers, item = word / 8;
+                const uint32_t unit = (uint32_t)(item / a.n_kv);
+                const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+                if (u.tiles == 0) continue;  // sees nothing: no words were written
+                uint32_t left = __shfl_sync(0xffffffffu, rows, __ffs(some) - 1);
+                for (uint32_t k = 0; left; ++k, left &= left - 1) {
+                    if (k % kWarps != warp) continue;
+                    const int r = (int)(word % 8) * 32 + __ffs(left) - 1;
+                    attend_row<T, D>(a, unit_tok(a, u, r), unit_head(a, u, (uint32_t)(item % a.n_kv), r));
                 }
+            }
         }
     }
     Cut x;

@@ -200,10 +200,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 if (g.k0 == g.k1) break;
                 const int32_t *table = g.table;
                 const int len = g.n, k1 = g.k1, head = (int)g.c;
-                auto block_of = [&](int k) -> int {  // a hole, or nothing left to read: out of range, zeros arrive
+                // A hole, nothing left to read, or nothing that any row sees (what has left the window and lies in a sinks' tile or
+                // in the first one behind may belong to someone else by now): out of range, zeros arrive.
+                const int last = min(len - 1, g.pos_max), past = g.whole ? 0 : max(g.pos_min, 0) - (int)min(a.window - 1u, 0x7fffffffu);
+                auto block_of = [&](int k) -> int {
                     const int t = seg_tile(g, k) * kTile + part * (int)box_tokens;
                     int id = -1;
-                    if ((int)lane < boxes && t < len) id = table[(uint32_t)t >> a.block_shift];
+                    if ((int)lane < boxes && t <= last && (t + (int)box_tokens > past || (uint32_t)t < a.sinks)) id = table[(uint32_t)t >> a.block_shift];
                     return (uint32_t)id < a.n_blocks ? id : (int)a.n_blocks;
                 };
                 int next = block_of(g.k0);
