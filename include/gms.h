@@ -439,7 +439,13 @@ typedef struct {
     uint32_t reserved;                  /* 0                                                             */
 } gms_kv_weight;
 
-/* Errors: NULL, ALIGN, ARG, RANGE (index limits; table_stride; workspace_bytes too small), CUDA. */
+/*
+ * gms_kv_attention_workspace: bytes for this call and for every later one with no larger n_seq, total_q, max_q and max_kv
+ * and the same pool layout, n_heads, window, sinks and outputs (lse given where it was not, and no weights where there were,
+ * take less).
+ * With weights and few queries a KV head the logits are kept: 4 bytes for each query row, head and cached token.
+ * Errors: NULL, ALIGN, ARG, RANGE (index limits; table_stride; workspace_bytes too small), CUDA.
+ */
 int gms_kv_attention_workspace(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
                                const gms_kv_weight *weight, uint64_t *nbytes);
 int gms_kv_attention(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,
@@ -453,7 +459,7 @@ int gms_kv_attention(const gms_kv_pool *pool, const gms_kv_layout *layout, const
  * for all rows of the group, not once a sequence.  attn->window and attn->sinks must be 0.
  * group_start[0] = 0 and group_start[n_groups] = n_seq: a sequence outside every group gets the tokens of its own
  * alone.  Rows of a group beyond its first max_group_q are not processed, tokens of a prefix beyond max_prefix not seen.
- * Errors: as gms_kv_attention.
+ * The workspace's size holds for smaller n_groups, max_prefix and max_group_q too.  Errors: as gms_kv_attention.
  */
 typedef struct {
     const int32_t *group_start;   /* (device) n_groups + 1, ascending                                    */

@@ -214,9 +214,9 @@ uint64_t most_tiles(const AttnArgs &a, const Pass &p)
     return p.n_units >= 1u << 30 ? 1ull << 31 : p.n_units * (uint64_t)a.n_kv * item_tiles(a, p);
 }
 
-void cut_pass(const AttnArgs &a, bool prefix, bool tc, Pass *p)
+uint64_t pass_rows(const AttnArgs &a, bool prefix) { return (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group; }
+void cut_pass(const AttnArgs &a, bool prefix, bool tc, uint64_t rows, Pass *p)
 {
-    const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
     p->prefix = prefix;
     p->rows = tc ? kTcRows : kFewRows;
     p->tile = tc ? kTcTile : kFewTile;
@@ -249,21 +249,23 @@ bool team_deal(uint64_t items, uint64_t tiles)
     return items < 512 ? tiles <= 32 : 64 * tiles >= items;
 }
 
+constexpr uint64_t kFewMostRows = 64;  // of a unit that goes to the few-row kernel
+
 void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c, Pass *p)
 {
     *p = {};
-    const uint64_t rows = (uint64_t)(prefix ? a.max_group_q : a.max_q) * a.group;
+    const uint64_t rows = pass_rows(a, prefix);
     // Up to 16 rows a KV head: the few-row kernel, which reads K and V once.  More: the tensor-core kernel reads them once for
     // 256 rows, but takes 8 us longer to get going (its Q, descriptors and tensor memory; 16 us against 8 us for one tile), so
     // short calls of up to 64 rows go to the few-row kernel all the same, 16 rows at a time: where no warp gets more than four
     // of its tiles (three suffixes of 40 behind a prefix of 129 tokens, 24 rows: 15 us against 23 us).
     bool tc = rows > kFewRows;
-    cut_pass(a, prefix, false, p);
-    if (tc && rows <= 64 && most_tiles(a, *p) <= 4ull * kFewMaxWorkers) tc = false;
-    if (tc) cut_pass(a, prefix, true, p);
+    cut_pass(a, prefix, false, rows, p);
+    if (tc && rows <= kFewMostRows && most_tiles(a, *p) <= 4ull * kFewMaxWorkers) tc = false;
+    if (tc) cut_pass(a, prefix, true, rows, p);
     if (!tc) p->team = team_deal((uint64_t)p->n_units * a.n_kv, item_tiles(a, *p));
     if (p->team) p->workers = 1;
-    p->begin = c->take<uint32_t>(p->n_units + 1);
+    p->begin = c->take<uint32_t>((uint64_t)p->n_units + 1);
     p->cuts = c->take<Cut>(p->workers);
     p->part_ml = c->take<float2>(2ull * p->workers * p->slot_rows);
     p->part_o = c->take<float>(2ull * p->workers * p->slot_rows * head_dim);
@@ -273,6 +275,42 @@ void plan_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out,
     }
     p->again = a.max_q > 1;  // with one query a sequence, what its rows do not see is cleared before the product
     if (tc && p->again && !rows_out) p->redo = c->take<uint32_t>((uint64_t)p->n_units * a.n_kv * (kTcRows / 32));
+}
+
+// What the plan above takes at most, for this call and for every one with no larger numbers: a smaller call may be cut in a
+// way that takes more than this one's (items dealt out instead of a CTA each, the other kernel, logits kept).  Every term grows
+// with n_seq, max_q, max_kv, total_q and a prefix's numbers alone.
+void most_of_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_out, Carve *c)
+{
+    const uint64_t rows = pass_rows(a, prefix);
+    Pass few = {}, many = {};
+    cut_pass(a, prefix, false, rows < kFewMostRows ? rows : kFewMostRows, &few);
+    if (rows > kFewRows) cut_pass(a, prefix, true, rows, &many);
+    auto larger = [](uint64_t x, uint64_t y) { return x > y ? x : y; };
+    const uint64_t slots = 2 * larger((uint64_t)few.workers * few.slot_rows, (uint64_t)many.workers * many.slot_rows);
+    c->take<uint32_t>(larger(few.n_units, many.n_units) + 1);
+    c->take<Cut>(larger(few.workers, many.workers));
+    c->take<float2>(slots);
+    c->take<float>(slots * head_dim);
+    if (rows_out) {
+        c->take<float2>((uint64_t)a.total_q * a.n_heads);
+        c->take<float>((uint64_t)a.total_q * a.n_heads * head_dim);
+    } else if (a.max_q > 1) {
+        c->take<uint32_t>((uint64_t)many.n_units * a.n_kv * (kTcRows / 32));
+    }
+}
+uint64_t logit_stride(const AttnArgs &a) { return ceil_div(a.max_kv, kFewTile) * kFewTile; }
+uint64_t most_of_call(const AttnArgs &a, uint32_t head_dim, bool shared)
+{
+    Carve c{nullptr};
+    most_of_pass(a, head_dim, false, shared, &c);
+    if (shared) most_of_pass(a, head_dim, true, true, &c);
+    if (a.w_out) {
+        if (!a.lse) c.take<float>((uint64_t)a.total_q * a.n_heads);
+        const uint32_t kept = kFewRows / a.group;  // queries whose logits are kept
+        c.take<float>((uint64_t)a.n_seq * a.n_heads * (a.max_q < kept ? a.max_q : kept) * logit_stride(a));
+    }
+    return c.used;
 }
 
 int plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace, Plan *pl, uint64_t *bytes)
@@ -287,11 +325,12 @@ int plan_call(const AttnArgs &a, uint32_t head_dim, bool shared, void *workspace
         if (!a.lse) pl->lse = c.take<float>((uint64_t)a.total_q * a.n_heads);
         if (pl->own.rows == kFewRows && pl->own.n_rt == 1) {
             pl->logits = true;
-            pl->own.logit_stride = (a.max_kv + kFewTile - 1) / kFewTile * kFewTile;
+            pl->own.logit_stride = (uint32_t)logit_stride(a);
             pl->own.logits = c.take<float>((uint64_t)a.n_seq * a.n_heads * a.max_q * pl->own.logit_stride);
         }
     }
-    *bytes = c.used;
+    const uint64_t most = most_of_call(a, head_dim, shared);
+    *bytes = c.used > most ? c.used : most;
     // the kernels count tiles in 31 bits
     const bool fits = most_tiles(a, pl->own) >> 31 == 0 && (!shared || most_tiles(a, pl->prefix) >> 31 == 0);
     return fits ? GMS_OK : GMS_ERR_RANGE;
