@@ -443,7 +443,8 @@ typedef struct {
  * gms_kv_attention_workspace: bytes for this call and for every later one with no larger n_seq, total_q, max_q and max_kv
  * and the same pool layout, n_heads, window, sinks and outputs (lse given where it was not, and no weights where there were,
  * take less).
- * With weights and few queries a KV head the logits are kept: 4 bytes for each query row, head and cached token.
+ * With weights and few queries a KV head the logits are kept: 4 bytes for each query, head and cached token that the
+ * sequence's queries see (of max_kv, or of window + sinks and up to 62 more).
  * Errors: NULL, ALIGN, ARG, RANGE (index limits; table_stride; workspace_bytes too small), CUDA.
  */
 int gms_kv_attention_workspace(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *attn,

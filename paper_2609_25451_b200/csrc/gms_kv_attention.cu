@@ -299,7 +299,13 @@ void most_of_pass(const AttnArgs &a, uint32_t head_dim, bool prefix, bool rows_o
         c->take<uint32_t>((uint64_t)many.n_units * a.n_kv * (kTcRows / 32));
     }
 }
-uint64_t logit_stride(const AttnArgs &a) { return ceil_div(a.max_kv, kFewTile) * kFewTile; }
+// Logits are kept tile by tile as the few-row kernel takes them, so under a window only for what it reaches.
+uint64_t logit_stride(const AttnArgs &a)
+{
+    Pass p = {};
+    p.rows = kFewRows, p.tile = kFewTile;
+    return item_tiles(a, p) * kFewTile;
+}
 uint64_t most_of_call(const AttnArgs &a, uint32_t head_dim, bool shared)
 {
     Carve c{nullptr};

@@ -68,7 +68,7 @@ struct Pass {
     float2 *part_ml;       // [2 * workers][slot_rows]: running maximum (base 2) and sum
     float *row_o;          // null: finished rows go to out / lse; else [total_q * n_heads][head_dim], not normalised
     float2 *row_ml;        // [total_q * n_heads]
-    float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2 (few-row pass only)
+    float *logits;         // null, or [n_units * n_kv][max_q * group][logit_stride], base 2, in tile list order (few-row pass only)
     uint32_t logit_stride;
     uint32_t team;         // 1: few-row pass, a CTA an item: its warps share the tiles and join in shared memory, nothing is cut
     uint32_t again;        // 1: rows that come out non-finite are done again (attend_row)

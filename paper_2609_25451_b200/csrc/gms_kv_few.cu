@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                 float *lp = p.logits + ((uint64_t)run.seq * a.n_kv + run.c) * a.max_q * a.group * p.logit_stride;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t t = t0 + j * 8 + (lane & 3u) * 2;
+                    const uint32_t t = ck * kFewTile + j * 8 + (lane & 3u) * 2;
                     if (r0 < run.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r0 * p.logit_stride + t) = make_float2(s[j][0], s[j][1]);
                     if (HI && r1 < run.rows) *reinterpret_cast<float2 *>(lp + (uint64_t)r1 * p.logit_stride + t) = make_float2(s[j][2], s[j][3]);
                 }
@@ -422,8 +422,10 @@ __global__ void __launch_bounds__(256) kv_few_weights_kernel(const __grid_consta
     for (int e = 0; e < 4; ++e) in[e] = a.w_in && e < left ? a.w_in[at + e] : 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     // tiles that nobody sees have no logits; in those of the list a token that a row does not see has -infinity
-    if (u.rows > 0 && (tile < u.n_sink_tiles || (tile >= u.first_tile && tile < u.first_tile + u.tiles - u.n_sink_tiles))) {
-        const float4 *lp = reinterpret_cast<const float4 *>(p.logits + (uint64_t)item * a.max_q * a.group * p.logit_stride + t);
+    const int k = tile < u.n_sink_tiles ? tile : tile - u.first_tile + u.n_sink_tiles;  // place in the list
+    if (u.rows > 0 && (tile < u.n_sink_tiles || (tile >= u.first_tile && k < u.tiles))) {
+        const float4 *lp = reinterpret_cast<const float4 *>(p.logits + (uint64_t)item * a.max_q * a.group * p.logit_stride + k * (int)kFewTile +
+                                                            t % (int)kFewTile);
 #pragma unroll 4
         for (int r = 0; r < u.rows; ++r) {
             const float4 x = lp[(uint64_t)r * (p.logit_stride / 4)];

@@ -60,3 +60,11 @@ def test_smaller_calls_never_take_more(heads, kv_heads, dim, kind):
         big = big[:3] + (big[0] * big[1],) + big[4:6] + (big[0] * big[1],)
         small = tuple(log(v) for v in big)
         assert of(*small) <= of(*big), (big, small)
+
+
+def test_kept_logits_under_a_window():
+    """4 bytes for each head and token in reach, whatever the longest sequence is."""
+    lay = layout_of(8, 128)
+    far = size(lay, 32, 256, 1, 1 << 20, 256, weight(), window=256)
+    near = size(lay, 32, 256, 1, 1 << 12, 256, weight(), window=256)
+    assert far == near and far < 256 * 32 * 400 * 4 + (32 << 20)
