@@ -101,6 +101,8 @@ extern "C" {
 /* bits of the device status word */
 #define GMS_DEV_TIMEOUT 1ull   /* a warp gave up waiting for one of its own bulk copies (2 s), then
                                   spent up to 2 s more draining the rest: worst case 4 s per call  */
+#define GMS_DEV_HOLE 2ull      /* gms_kv_evict kept a token whose rows could not be copied: its source or
+                                  destination id lies outside the pool                             */
 
 typedef struct gms_manifest gms_manifest; /* opaque */
 
@@ -487,8 +489,10 @@ int gms_kv_attention_shared(const gms_kv_pool *pool, const gms_kv_layout *layout
  *   weights_out[l][s][c][j]  its weight (entries from n' on are left alone)
  *   lens_out[s] = n'; lens_out may be lens (then the lengths are updated in place), but may not overlap it otherwise
  *   K and V of token kept[j] are copied to token j of the blocks dst_table[s*dst_stride + ...]
- * Destination blocks must be distinct and must not be source blocks (the old ones are free once the call has run); a row
- * whose source or destination id lies outside the pool is not copied.  Keys carry their positions (rotary embeddings)
+ * Destination blocks must be distinct and must not be source blocks (the old ones are free once the call has run).  The
+ * tables must not have holes where tokens can be kept: the choice goes by weights and positions alone, and a row whose source
+ * or destination id lies outside the pool is not copied, so that its place among the n' tokens holds whatever bits were there
+ * before, for gms_kv_attention to see.  GMS_DEV_HOLE in `status` tells of it.  Keys carry their positions (rotary embeddings)
  * with them; afterwards the sequence is n' tokens long for gms_kv_attention.  Lens above max_len count as max_len.
  * Errors: NULL, ALIGN, ARG (sinks + recent > budget; planes outside the pool; weights_out or lens_out where
  * they may not be), RANGE, CUDA.
@@ -506,6 +510,7 @@ typedef struct {
     uint32_t n_layers, layer_planes, n_seq, max_len;
     uint32_t budget, sinks, recent;
     uint32_t reserved;                  /* 0                                                             */
+    uint64_t *status;                   /* (device) may be NULL; GMS_DEV_HOLE is or-ed in                */
 } gms_kv_evict_args;
 int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_evict_args *args, void *stream);
 

@@ -449,7 +449,7 @@ int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms
     }
     if ((reinterpret_cast<uint64_t>(t->weights) | reinterpret_cast<uint64_t>(t->weights_out) | reinterpret_cast<uint64_t>(t->lens) |
          reinterpret_cast<uint64_t>(t->lens_out) | reinterpret_cast<uint64_t>(t->src_table) | reinterpret_cast<uint64_t>(t->dst_table) |
-         reinterpret_cast<uint64_t>(t->kept)) & 3u)
+         reinterpret_cast<uint64_t>(t->kept)) & 3u || reinterpret_cast<uint64_t>(t->status) & 7u)
         return GMS_ERR_ALIGN;
     const uint64_t rows = (uint64_t)t->n_layers * t->n_seq * layout->n_kv_heads;
     const uint32_t most = t->max_len < t->budget ? t->max_len : t->budget;
@@ -496,6 +496,7 @@ int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms
     a.budget = t->budget;
     a.sinks = t->sinks;
     a.recent = t->recent;
+    a.status = reinterpret_cast<unsigned long long *>(t->status);
     const cudaError_t e = gms::launch_kv_evict(a, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? GMS_OK : gms::report_cuda_error(e);
 }

@@ -87,6 +87,7 @@ struct EvictArgs {
     int32_t *kept;
     uint64_t w_layer_stride, w_seq_stride, w_head_stride, o_layer_stride, o_seq_stride, o_head_stride, src_stride, dst_stride;
     uint32_t n_layers, layer_planes, n_seq, n_kv, max_len, budget, sinks, recent;
+    unsigned long long *status;  // may be null
 };
 
 // behind: the attention kernels of the same call have been launched.

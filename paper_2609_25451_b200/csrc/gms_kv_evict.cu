@@ -147,7 +147,10 @@ __global__ void __launch_bounds__(256) kv_evict_move_kernel(const __grid_constan
     for (uint32_t j = j0 + threadIdx.x / per_row; j < min(j0 + 64, keep); j += 256 / per_row) {
         const uint32_t t = (uint32_t)kept[j];
         const int from = a.src_table[s * a.src_stride + (t >> a.block_shift)], to = a.dst_table[s * a.dst_stride + (j >> a.block_shift)];
-        if ((uint32_t)from >= a.n_blocks || (uint32_t)to >= a.n_blocks) continue;
+        if ((uint32_t)from >= a.n_blocks || (uint32_t)to >= a.n_blocks) {
+            if (a.status && part == 0) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+            continue;
+        }
         const uint64_t head = (uint64_t)c * a.head_stride + part * 16;
         const uint64_t so = (uint64_t)from * a.block_stride + (uint64_t)(t & mask) * a.token_stride + head;
         const uint64_t to_off = (uint64_t)to * a.block_stride + (uint64_t)(j & mask) * a.token_stride + head;

@@ -24,7 +24,8 @@ NOALLOC_MAX_BLOCKS = 4194304
 SRC_DEVICE, SRC_HOST_MAPPED = 0, 1
 BUILD_HOST_ONLY = 1
 BUILD_SELFTEST_STALL = 2  # test suites only: one warp's first wait runs out (see include/gms.h)
-DEV_TIMEOUT = 1  # bit of the device status word
+DEV_TIMEOUT = 1  # bits of the device status word
+DEV_HOLE = 2
 
 # numpy view of gms_entry / gms_mismatch (32 and 16 bytes)
 ENTRY_DTYPE = np.dtype([("tensor_id", "<u8"), ("src_offset", "<u8"), ("dst", "<u8"), ("nbytes", "<u8")])
@@ -104,7 +105,7 @@ class KvEvictArgs(C.Structure):
                 ("o_seq_stride", C.c_uint64), ("o_head_stride", C.c_uint64), ("src_stride", C.c_uint64),
                 ("dst_stride", C.c_uint64), ("n_layers", C.c_uint32), ("layer_planes", C.c_uint32), ("n_seq", C.c_uint32),
                 ("max_len", C.c_uint32), ("budget", C.c_uint32), ("sinks", C.c_uint32), ("recent", C.c_uint32),
-                ("reserved", C.c_uint32)]
+                ("reserved", C.c_uint32), ("status", C.c_void_p)]
 
 
 _lib = None
@@ -417,9 +418,9 @@ def kv_prefix(*, group_start, prefix_lens, prefix_table, max_prefix: int, max_gr
 
 
 def kv_evict_args(*, weights, lens, src_table, dst_table, kept, max_len: int, budget: int, sinks: int = 0, recent: int = 0,
-                  weights_out=None, lens_out=None, layer_planes: int = 2) -> KvEvictArgs:
+                  weights_out=None, lens_out=None, layer_planes: int = 2, status=None) -> KvEvictArgs:
     """gms_kv_evict_args from tensors: ``weights`` and ``weights_out`` float32 [layers, sequences, kv heads, tokens],
-    ``kept`` int32 [layers, sequences, kv heads, budget] contiguous, tables int32 [sequences, blocks]."""
+    ``kept`` int32 [layers, sequences, kv heads, budget] contiguous, tables int32 [sequences, blocks], ``status`` a 64-bit word."""
     _int32(lens, lens_out, src_table, dst_table, kept)
     _float32(weights, weights_out)
     n_layers, n_seq, n_kv, _ = weights.shape
@@ -432,8 +433,8 @@ def kv_evict_args(*, weights, lens, src_table, dst_table, kept, max_len: int, bu
                     src_table=_dev(src_table), dst_table=_dev(dst_table), kept=_dev(kept), w_layer_stride=weights.stride(0),
                     w_seq_stride=weights.stride(1), w_head_stride=weights.stride(2), o_layer_stride=o[0], o_seq_stride=o[1],
                     o_head_stride=o[2], src_stride=src_table.stride(0), dst_stride=dst_table.stride(0), n_layers=n_layers,
-                    layer_planes=layer_planes, n_seq=n_seq, max_len=max_len, budget=budget, sinks=sinks, recent=recent)
-    a._keep = (weights, weights_out, lens, lens_out, src_table, dst_table, kept)
+                    layer_planes=layer_planes, n_seq=n_seq, max_len=max_len, budget=budget, sinks=sinks, recent=recent, status=_dev(status))
+    a._keep = (weights, weights_out, lens, lens_out, src_table, dst_table, kept, status)
     return a
 
 

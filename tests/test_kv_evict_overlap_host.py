@@ -14,3 +14,7 @@ def built():
 @pytest.mark.parametrize("lens,lens_out", [(BASE, BASE + 4), (BASE + 8, BASE), (BASE, BASE + 8)])
 def test_lengths_that_overlap_are_refused(lens, lens_out):
     assert status(gms.gms_kv_evict, pool(), layout(), evict(lens=lens, lens_out=lens_out)) == gms.ERR_ARG
+
+
+def test_status_alignment():
+    assert status(gms.gms_kv_evict, pool(), layout(), evict(status=BASE + 4)) == gms.ERR_ALIGN
