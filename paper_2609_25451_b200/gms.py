@@ -73,6 +73,7 @@ class KvLayout(C.Structure):
 class KvAttn(C.Structure):
     """``gms_kv_attn``; usually made by :func:`kv_attn`, which also keeps the tensors alive."""
 
+    _made = None  # what the tensors that it was made of have room for
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("cu_q", C.c_void_p), ("kv_lens", C.c_void_p),
                 ("block_table", C.c_void_p), ("workspace", C.c_void_p), ("status", C.c_void_p), ("workspace_bytes", C.c_uint64),
                 ("q_token_stride", C.c_uint64), ("q_head_stride", C.c_uint64), ("out_token_stride", C.c_uint64),
@@ -82,23 +83,28 @@ class KvAttn(C.Structure):
 
     def set_workspace(self, t):
         """Hands over a uint8 device tensor of at least gms_kv_attention*_workspace bytes."""
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("the workspace is contiguous device memory")
         self._workspace = t
         self.workspace, self.workspace_bytes = t.data_ptr(), t.numel() * t.element_size()
 
 
 class KvWeight(C.Structure):
     # ("in" is a keyword: the field is called in_)
+    _made = None  # what the tensors that it was made of have room for
     _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("seq_stride", C.c_uint64), ("head_stride", C.c_uint64),
                 ("decay", C.c_float), ("reserved", C.c_uint32)]
 
 
 class KvPrefix(C.Structure):
+    _made = None  # what the tensors that it was made of have room for
     _fields_ = [("group_start", C.c_void_p), ("prefix_lens", C.c_void_p), ("prefix_table", C.c_void_p),
                 ("prefix_stride", C.c_uint64), ("n_groups", C.c_uint32), ("max_prefix", C.c_uint32),
                 ("max_group_q", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class KvEvictArgs(C.Structure):
+    _made = None  # what the tensors that it was made of have room for
     _fields_ = [("weights", C.c_void_p), ("weights_out", C.c_void_p), ("lens", C.c_void_p), ("lens_out", C.c_void_p),
                 ("src_table", C.c_void_p), ("dst_table", C.c_void_p), ("kept", C.c_void_p), ("w_layer_stride", C.c_uint64),
                 ("w_seq_stride", C.c_uint64), ("w_head_stride", C.c_uint64), ("o_layer_stride", C.c_uint64),
@@ -355,16 +361,28 @@ def gms_kv_verify(pool: KvPool, d_block_ids, n_sel: int, d_computed, d_expected,
                                _dev(d_count), _dev(d_scratch), _stream(stream)), "gms_kv_verify")
 
 
-def _int32(*tensors):
+def _rows(what, size, floating, tensors):
+    """Typed (``floating`` None: either), on a GPU (or pinned, which a GPU reads too), elements side by side in the last dimension."""
     for t in tensors:
-        if t is not None and (t.element_size() != 4 or t.is_floating_point() or t.stride(-1) not in (0, 1) and t.shape[-1] > 1):
-            raise ValueError("lengths, offsets and tables are int32 with contiguous rows")
+        if t is None:
+            continue
+        if t.element_size() != size or floating not in (None, t.is_floating_point()) or t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(what)
+        if not (t.is_cuda or t.is_pinned()):
+            raise ValueError("the kernels cannot read pageable host memory")
+
+
+def _int32(*tensors):
+    _rows("lengths, offsets and tables are int32 with contiguous rows", 4, False, tensors)
 
 
 def _float32(*tensors):
-    for t in tensors:
-        if t is not None and (t.element_size() != 4 or not t.is_floating_point() or t.stride(-1) != 1 and t.shape[-1] > 1):
-            raise ValueError("weights and log-sum-exps are float32 with contiguous rows")
+    _rows("weights and log-sum-exps are float32 with contiguous rows", 4, True, tensors)
+
+
+def _word(t):
+    if hasattr(t, "data_ptr"):
+        _rows("status is a 64-bit word", 8, False, (t,))
 
 
 def kv_attn(*, q, out, kv_lens, block_table, max_kv: int, scale: float, lse=None, cu_q=None, max_q: int = 1, window: int = 0,
@@ -373,12 +391,14 @@ def kv_attn(*, q, out, kv_lens, block_table, max_kv: int, scale: float, lse=None
     dimension), ``lse`` float32 [tokens, heads] contiguous, ``kv_lens`` and ``cu_q`` int32, ``block_table`` int32
     [sequences, blocks].  The result keeps the tensors alive."""
     for t in (q, out):
-        if t.dim() != 3 or t.element_size() != 2 or t.stride(2) != 1:
+        if t.dim() != 3:
             raise ValueError("q and out are 16-bit [tokens, heads, dim] with a contiguous last dimension")
+    _rows("q and out are 16-bit [tokens, heads, dim] with a contiguous last dimension", 2, None, (q, out))
     if out.shape != q.shape or out.dtype != q.dtype or block_table.dim() != 2:
         raise ValueError("out must match q, block_table is [sequences, blocks]")
     _int32(kv_lens, cu_q, block_table)
     _float32(lse)
+    _word(status)
     n_seq = kv_lens.shape[0]
     if block_table.shape[0] != n_seq or (cu_q is not None and cu_q.shape[0] != n_seq + 1):
         raise ValueError("kv_lens, cu_q and block_table disagree about the number of sequences")
@@ -390,6 +410,7 @@ def kv_attn(*, q, out, kv_lens, block_table, max_kv: int, scale: float, lse=None
                n_seq=n_seq, n_heads=q.shape[1], total_q=q.shape[0], max_q=max_q, max_kv=max_kv, window=window, sinks=sinks,
                scale=scale)
     a._keep = (q, out, lse, cu_q, kv_lens, block_table, status)
+    a._made = (q.shape[2], {"torch.bfloat16": DTYPE_BF16, "torch.float16": DTYPE_F16}.get(str(q.dtype)), block_table.shape[1])
     if workspace is not None:
         a.set_workspace(workspace)
     return a
@@ -397,11 +418,12 @@ def kv_attn(*, q, out, kv_lens, block_table, max_kv: int, scale: float, lse=None
 
 def kv_weights(w_in, w_out, decay: float = 1.0) -> KvWeight:
     """gms_kv_weight from float32 tensors [sequences, kv heads, tokens]; ``w_in`` None counts as zeros."""
+    if w_out.dim() != 3 or w_in is not None and (w_in.stride() != w_out.stride() or w_in.shape != w_out.shape):
+        raise ValueError("w_in and w_out are [sequences, kv heads, tokens] with equal strides")
     _float32(w_in, w_out)
-    if w_in is not None and w_in.stride() != w_out.stride():
-        raise ValueError("w_in and w_out need equal strides")
     w = KvWeight(in_=_dev(w_in), out=_dev(w_out), seq_stride=w_out.stride(0), head_stride=w_out.stride(1), decay=decay)
     w._keep = (w_in, w_out)
+    w._made = tuple(w_out.shape)
     return w
 
 
@@ -414,6 +436,7 @@ def kv_prefix(*, group_start, prefix_lens, prefix_table, max_prefix: int, max_gr
     p = KvPrefix(group_start=_dev(group_start), prefix_lens=_dev(prefix_lens), prefix_table=_dev(prefix_table),
                  prefix_stride=prefix_table.stride(0), n_groups=g, max_prefix=max_prefix, max_group_q=max_group_q)
     p._keep = (group_start, prefix_lens, prefix_table)
+    p._made = prefix_table.shape[1]
     return p
 
 
@@ -421,13 +444,17 @@ def kv_evict_args(*, weights, lens, src_table, dst_table, kept, max_len: int, bu
                   weights_out=None, lens_out=None, layer_planes: int = 2, status=None) -> KvEvictArgs:
     """gms_kv_evict_args from tensors: ``weights`` and ``weights_out`` float32 [layers, sequences, kv heads, tokens],
     ``kept`` int32 [layers, sequences, kv heads, budget] contiguous, tables int32 [sequences, blocks], ``status`` a 64-bit word."""
-    _int32(lens, lens_out, src_table, dst_table, kept)
-    _float32(weights, weights_out)
     n_layers, n_seq, n_kv, _ = weights.shape
     if tuple(kept.shape) != (n_layers, n_seq, n_kv, budget) or not kept.is_contiguous():
         raise ValueError("kept is int32 [layers, sequences, kv heads, budget], contiguous")
-    if src_table.shape[0] != n_seq or dst_table.shape[0] != n_seq or lens.shape[0] != n_seq:
-        raise ValueError("lens and tables disagree about the number of sequences")
+    if src_table.shape[0] != n_seq or dst_table.shape[0] != n_seq or lens.shape[0] != n_seq or lens_out is not None and lens_out.shape[0] != n_seq:
+        raise ValueError("lens, lens_out and tables disagree about the number of sequences")
+    most = min(max_len, budget)
+    if weights.shape[3] < max_len or weights_out is not None and (weights_out.shape[:3] != weights.shape[:3] or weights_out.shape[3] < most):
+        raise ValueError("weights have max_len tokens a row, weights_out the same rows with min(max_len, budget)")
+    _int32(lens, lens_out, src_table, dst_table, kept)
+    _float32(weights, weights_out)
+    _word(status)
     o = (0, 0, 0, 1) if weights_out is None else weights_out.stride()
     a = KvEvictArgs(weights=_dev(weights), weights_out=_dev(weights_out), lens=_dev(lens), lens_out=_dev(lens_out),
                     src_table=_dev(src_table), dst_table=_dev(dst_table), kept=_dev(kept), w_layer_stride=weights.stride(0),
@@ -435,11 +462,31 @@ def kv_evict_args(*, weights, lens, src_table, dst_table, kept, max_len: int, bu
                     o_head_stride=o[2], src_stride=src_table.stride(0), dst_stride=dst_table.stride(0), n_layers=n_layers,
                     layer_planes=layer_planes, n_seq=n_seq, max_len=max_len, budget=budget, sinks=sinks, recent=recent, status=_dev(status))
     a._keep = (weights, weights_out, lens, lens_out, src_table, dst_table, kept, status)
+    a._made = (n_kv, src_table.shape[1], dst_table.shape[1])
     return a
 
 
 def _ref(x):
     return None if x is None else C.byref(x)
+
+
+def _fits(layout, attn, weight=None, prefix=None):
+    """What only tensors and layout together tell (structures that were filled in by hand are the caller's)."""
+    if layout is None or attn is None:
+        return
+    tokens = layout.block_tokens
+    if attn._made is not None:
+        dim, dtype, blocks = attn._made
+        if dim != layout.head_dim or dtype not in (None, layout.dtype):
+            raise ValueError(f"q has heads of {dim} and GMS_DTYPE {dtype}, the layout {layout.head_dim} and {layout.dtype}")
+        if blocks * tokens < attn.max_kv:
+            raise ValueError(f"block_table has {blocks} blocks of {tokens} tokens a row, max_kv is {attn.max_kv}")
+    if weight is not None and weight._made is not None:
+        seqs, heads, length = weight._made
+        if seqs < attn.n_seq or heads < layout.n_kv_heads or length < attn.max_kv:
+            raise ValueError(f"weights of {seqs} x {heads} x {length} for {attn.n_seq} sequences, {layout.n_kv_heads} KV heads, max_kv {attn.max_kv}")
+    if prefix is not None and prefix._made is not None and prefix._made * tokens < prefix.max_prefix:
+        raise ValueError(f"prefix_table has {prefix._made} blocks of {tokens} tokens a row, max_prefix is {prefix.max_prefix}")
 
 
 def gms_kv_attention_workspace(pool: KvPool, layout: KvLayout, attn: KvAttn, weight: KvWeight | None = None) -> int:
@@ -450,6 +497,7 @@ def gms_kv_attention_workspace(pool: KvPool, layout: KvLayout, attn: KvAttn, wei
 
 
 def gms_kv_attention(pool: KvPool, layout: KvLayout, attn: KvAttn, weight: KvWeight | None = None, stream=None):
+    _fits(layout, attn, weight)
     _check(lib().gms_kv_attention(_ref(pool), _ref(layout), _ref(attn), _ref(weight), _stream(stream)), "gms_kv_attention")
 
 
@@ -461,11 +509,16 @@ def gms_kv_attention_shared_workspace(pool: KvPool, layout: KvLayout, attn: KvAt
 
 
 def gms_kv_attention_shared(pool: KvPool, layout: KvLayout, attn: KvAttn, prefix: KvPrefix, stream=None):
+    _fits(layout, attn, None, prefix)
     _check(lib().gms_kv_attention_shared(_ref(pool), _ref(layout), _ref(attn), _ref(prefix), _stream(stream)),
            "gms_kv_attention_shared")
 
 
 def gms_kv_evict(pool: KvPool, layout: KvLayout, args: KvEvictArgs, stream=None):
+    if layout is not None and args is not None and args._made is not None:
+        heads, src, dst = args._made
+        if heads != layout.n_kv_heads or src * layout.block_tokens < args.max_len or dst * layout.block_tokens < min(args.max_len, args.budget):
+            raise ValueError("weights have another number of KV heads than the layout, or tables too few blocks a row")
     _check(lib().gms_kv_evict(_ref(pool), _ref(layout), _ref(args), _stream(stream)), "gms_kv_evict")
 
 
