@@ -397,8 +397,9 @@ typedef struct {
  * t < sinks; an id outside [0, pool->n_blocks) is a hole whose tokens nobody sees.  With c = h / (n_heads/n_kv_heads):
  *   x_t = scale * q[i,h] . K[t,c];  lse[i,h] = log sum_t exp(x_t);  out[i,h] = sum_t exp(x_t - lse) V[t,c]
  * over the t that it sees; if there are none, out is 0 and lse is -infinity.  What a query does not see cannot reach
- * its output, whatever bits it holds (NaN, infinities).  Products are taken in the pool's type with 32-bit sums; the
- * softmax weights are rounded to the pool's type before the product with V.
+ * its output, whatever bits it holds (NaN, infinities); a value that it sees and that is not finite makes its output non-
+ * finite in that column (infinite or NaN).  Products are taken in the pool's type with 32-bit sums; the softmax weights are
+ * rounded to the pool's type before the product with V (fp16: so that they count down to 2^-32 of the largest), not in lse.
  * The host sizes the launch by max_q and max_kv.  Of a sequence with more queries the first max_q are processed, of one
  * with more tokens only the first max_kv are seen (and have weights); what is left out changes no position: query i of
  * q_len stands at kv_lens[s] - q_len + i all the same.  Rows of q that are not processed or that no sequence owns leave

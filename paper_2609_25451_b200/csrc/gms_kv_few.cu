@@ -53,6 +53,9 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
 {
     using F = Few<D>;
     constexpr int S = F::kStages, NJ = D / 8;
+    // fp16 weights are kept 2^15 times larger, the largest that fits: else those below 2^-25 of the maximum were nothing to the
+    // product with V, however many there are, and counted in l all the same
+    constexpr float kUp = std::is_same<T, __half>::value ? 15.f : 0.f;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -260,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                     }
                 }
             }
-            const float z0 = x.m[0] == neg_inf() ? 0.f : x.m[0], z1 = x.m[1] == neg_inf() ? 0.f : x.m[1];
+            const float z0 = x.m[0] == neg_inf() ? 0.f : x.m[0] - kUp, z1 = x.m[1] == neg_inf() ? 0.f : x.m[1] - kUp;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -268,7 +271,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
                     s[j][e] = (HI || e < 2) ? ex2(s[j][e] - (e < 2 ? z0 : z1)) : 0.f;
                     x.l[e / 2] += s[j][e];
                 }
-            // P is rounded to the pool's type for the matrix product; the sums l keep the unrounded weights
+            // P is rounded to the pool's type, because the matrix instruction takes both factors in one type and V is in that one;
+            // the sums l keep the unrounded weights (summing the rounded ones would cost a conversion back for each)
             const uint32_t pa[4] = {pack2(s[0][0], s[0][1], T()), pack2(s[0][2], s[0][3], T()), pack2(s[1][0], s[1][1], T()),
                                     pack2(s[1][2], s[1][3], T())};
             const uint32_t vrow = (lane & 7u) + ((lane >> 3) & 1u) * 8;
@@ -299,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             if (row >= run.rows) continue;
             const uint64_t tok = run.q0 + (run.row0 + row) / (int)a.group;
             const uint32_t h = run.c * a.group + (uint32_t)(run.row0 + row) % a.group;
-            const float m = x.m[r], l = x.l[r];
+            const float m = x.m[r] - kUp, l = x.l[r];  // what o and l stand against
             if (starts && ends && !p.row_o) {
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 uint32_t *op = reinterpret_cast<uint32_t *>(a.out + tok * a.out_token_stride + h * a.out_head_stride) + (lane & 3u);
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            jm[(warp * R + i) * 32 + lane] = x.m[i];
+            jm[(warp * R + i) * 32 + lane] = x.m[i] - kUp;
             jl[(warp * R + i) * 32 + lane] = x.l[i];
 #pragma unroll
             for (int j = 0; j < NJ; ++j)

@@ -31,6 +31,9 @@ using namespace ptx;
 
 constexpr int kThreads = 384, kRows = (int)kTcRows, kTile = (int)kTcTile;
 constexpr float kLag = 8.f;  // log2 of how far a maximum may have grown before O is rescaled
+// log2 of how much larger P is kept: with the lag the most that fp16 holds.  Else weights below 2^-25 of the maximum were nothing
+// to the product with V, however many there are, and counted in l all the same.
+template <class T> constexpr float kUp = std::is_same<T, __half>::value ? 7.f : 0.f;
 
 // A run of tiles of one item, as the roles read it from shared memory.  k0 == k1: no more.
 struct Segment {
@@ -447,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                             }
                         }
                     }
-                    const float z = m == neg_inf() ? 0.f : m;
+                    const float z = m == neg_inf() ? 0.f : m - kUp<T>;
                     const float2 cc = make_float2(c2, c2), zz = make_float2(-z, -z);
                     float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     uint32_t pk[32];
@@ -502,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_attn_tc_kernel(const __grid_co
                 ++tiles;
             }
             if (!ok) break;
+            m -= kUp<T>;  // what O and l stand against
             // the item's rows (or this CTA's piece of them)
             if (!wait(o_done + 16 * slot, (tiles - 1) & 1u) || !wait(o_done + 16 * slot + 8, (tiles - 1) & 1u)) break;
             tc_fence_after();
