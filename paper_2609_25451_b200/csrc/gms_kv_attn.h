@@ -120,9 +120,14 @@ cudaError_t allow_smem(K kernel, uint32_t smem, std::atomic<uint64_t> &done)
     return e;
 }
 
-// Launches a kernel that may start before the one ahead of it in the stream has drained.  Every such kernel waits for the one
-// ahead before it touches what that may have written, and lets the next one start only after that wait (so what is complete
-// for a kernel is complete for all behind it).
+// Launches a kernel that may start before the one ahead of it in the stream has drained.  What keeps that in order:
+//  - The first kernel of a call (an attention kernel, the selecting kernel of an eviction) waits for the one ahead before it
+//    touches anything, and lets the next one start only after that wait.  So whatever was there before the call is complete for
+//    every kernel of the call, waiting or not.
+//  - Each further kernel of the call (the own pass of a shared call, joins, weights, the moving kernel) may let its successor
+//    start at once and, before its own wait, read what was there before the call and write what no other kernel of the call
+//    touches, nothing more.
+//  - Every kernel waits for the one ahead at some time, so a kernel's end stands for all that were launched before it.
 template <class K, class... A>
 cudaError_t launch_dependent(K kernel, uint32_t grid, uint32_t block, uint32_t smem, cudaStream_t s, const A &...args)
 {
