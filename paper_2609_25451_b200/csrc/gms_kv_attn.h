@@ -517,7 +517,7 @@ __device__ __noinline__ bool any_not_finite(const AttnArgs &a, uint32_t c, const
 // sees (behind it, before its window, after the sinks) holds a non-finite value, and a row is given up as soon as everything in
 // it that was non-finite is known to be so.  One infinite value that 2,048 queries over 16k tokens see (32 / 8 heads, 0.6 ms
 // without it): 1.4 ms, with all rows done again 5.2 s.  Infinities from the newest 300 tokens on, which some rows of a unit
-// see and others do not: 45 ms.
+// see and others do not: 40 ms.
 template <class T, int D>
 __device__ __noinline__ void attend_row(const AttnArgs &a, int tok, uint32_t h)
 {
@@ -560,9 +560,9 @@ struct Row {
     float m = -INFINITY, l = 0.f, o[D / 32] = {};
 };
 
-// Writes a finished row; non-finite rows go through attend_row when `redo` asks for it.
+// Writes a finished row; whether it has a value that is not finite.
 template <class T, int D>
-__device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int tok, uint32_t h, bool redo)
+__device__ __forceinline__ bool finish(const AttnArgs &a, const Row<D> &x, int tok, uint32_t h)
 {
     const uint32_t lane = threadIdx.x & 31u;
     T *op = reinterpret_cast<T *>(a.out + (uint64_t)tok * a.out_token_stride + (uint64_t)h * a.out_head_stride) + lane * (D / 32);
@@ -578,10 +578,7 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Row<D> &x, int t
     if (D == 128) *reinterpret_cast<uint2 *>(op) = *reinterpret_cast<const uint2 *>(v);
     else *reinterpret_cast<uint32_t *>(op) = *reinterpret_cast<const uint32_t *>(v);
     if (a.lse && lane == 0) a.lse[(uint64_t)tok * a.n_heads + h] = x.l == 0.f ? neg_inf() : (x.m + log2f(x.l)) * kLn2;
-    if (redo && __any_sync(0xffffffffu, bad)) {
-        __syncwarp();
-        attend_row<T, D>(a, tok, h);
-    }
+    return __any_sync(0xffffffffu, bad);
 }
 #endif
 

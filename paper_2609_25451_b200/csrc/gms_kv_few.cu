@@ -379,7 +379,10 @@ __global__ void __launch_bounds__(kThreads, 2) kv_attn_few_kernel(const __grid_c
             const int tok = unit_tok(a, un, r);
             const uint32_t h = unit_head(a, un, blockIdx.x % a.n_kv, r);
             if (!p.row_o) {
-                finish<T, D>(a, sum, tok, h, p.again);
+                if (finish<T, D>(a, sum, tok, h) && p.again) {
+                    __syncwarp();
+                    attend_row<T, D>(a, tok, h);
+                }
                 continue;
             }
             const uint64_t at = (uint64_t)tok * a.n_heads + h;

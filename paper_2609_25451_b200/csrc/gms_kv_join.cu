@@ -52,13 +52,49 @@ __device__ __forceinline__ void add_pieces(Row<D> &x, const float2 *ml, const fl
     }
 }
 
+// Rows of finished items that came out non-finite (a cut item's words are zero): a word has 32 rows, four for each warp, and
+// neighbouring words go to different blocks of the first ones.  (With all blocks looking, each wave of them paid for a load from
+// L2: windowed prompt 247 us, so 242.)  A lane's word in its block's turn.
+__device__ __forceinline__ uint32_t redo_word(const AttnArgs &a, const Pass &p, uint32_t turn)
+{
+    const uint64_t w = blockIdx.x + ((uint64_t)turn * 32 + (threadIdx.x & 31u)) * min(gridDim.x, kLookers);
+    return p.redo && blockIdx.x < kLookers && w < (uint64_t)p.n_units * a.n_kv * 8 ? p.redo[w] : 0u;
+}
+// What a warp does again: rows row, row + 8, ... of the cut item (KV head c) that are marked in `bad`, and its share of the rows
+// that are marked in the block's words (`rows`: the first turn's).  Kept out of the join's own code, which is short of registers.
+template <class T, int D, int ROWS, int TILE>
+__device__ __noinline__ void redo(const AttnArgs &a, const Pass &p, int q0, int row, uint32_t c, uint32_t bad, uint32_t rows)
+{
+    __syncwarp();
+    for (; bad; bad &= bad - 1) {
+        const int r = row + (__ffs(bad) - 1) * (int)kWarps;
+        attend_row<T, D>(a, q0 + r / (int)a.group, c * a.group + (uint32_t)r % a.group);
+    }
+    if (!p.redo || blockIdx.x >= kLookers) return;
+    for (uint32_t turn = 0;; rows = redo_word(a, p, ++turn)) {
+        const uint64_t lookers = min(gridDim.x, kLookers), first = blockIdx.x + turn * 32 * lookers;
+        if (first >= (uint64_t)p.n_units * a.n_kv * 8) return;
+        for (uint32_t some = __ballot_sync(0xffffffffu, rows != 0); some; some &= some - 1) {
+            const uint64_t word = first + (__ffs(some) - 1) * lookers, item = word / 8;
+            const uint32_t unit = (uint32_t)(item / a.n_kv);
+            uint32_t left = __shfl_sync(0xffffffffu, rows, __ffs(some) - 1);
+            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+            if (u.tiles == 0) continue;  // sees nothing: no words were written
+            for (uint32_t k = 0; left; ++k, left &= left - 1) {
+                if (k % kWarps != threadIdx.x / 32) continue;
+                const int r = (int)(word % 8) * 32 + __ffs(left) - 1;
+                attend_row<T, D>(a, unit_tok(a, u, r), unit_head(a, u, (uint32_t)(item % a.n_kv), r));
+            }
+        }
+    }
+}
+
 // A block does `rows_a_block` rows (part `part` of them) of one cut item: of item i (by_item: fewer items than borders), or of
 // the item into which the border before worker i + 1 falls, if that is its first border.  Also: rows of units that see
-// nothing are zero, their log-sum-exps -infinity; and rows to be done again are.
-template <class T, int D, int ROWS, int TILE>
+// nothing are zero, their log-sum-exps -infinity; and (AGAIN) rows to be done again are.
+template <class T, int D, int ROWS, int TILE, bool AGAIN>
 __global__ void __launch_bounds__(kWarps * 32, D == 64 ? 4 : 3) kv_attn_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Pass p,
-                                                                   uint32_t parts, uint32_t rows_a_block,
-                                                                   uint32_t by_item)
+                                                                                    uint32_t parts, uint32_t rows_a_block, uint32_t by_item)
 {
     grid_launch_dependents();
     for (uint32_t x = blockIdx.x; x < p.n_units; x += gridDim.x) {  // while the attention kernel still runs
@@ -74,81 +110,68 @@ __global__ void __launch_bounds__(kWarps * 32, D == 64 ? 4 : 3) kv_attn_join_ker
         }
     }
     grid_wait();
-    const uint32_t i = blockIdx.x / parts, row_first = blockIdx.x % parts * rows_a_block, warp = threadIdx.x / 32;
-    if (p.redo) {  // rows of finished items that came out non-finite; a cut item's words are zero
-        // a word has 32 rows, four for each warp; neighbouring words go to different blocks of the first ones (with all blocks
-        // looking, each wave of them paid for a load from L2: windowed prompt 247 us, so 242)
-        const uint64_t words = (uint64_t)p.n_units * a.n_kv * 8;
-        const uint32_t lookers = blockIdx.x < kLookers ? min(gridDim.x, kLookers) : 0;
-        const uint32_t lane = threadIdx.x & 31u;
-        for (uint64_t w0 = blockIdx.x; lookers && w0 < words; w0 += 32ull * lookers) {
-            const uint64_t mine = w0 + (uint64_t)lane * lookers;
-            const uint32_t rows = mine < words ? p.redo[mine] : 0u;
-            for (uint32_t some = __ballot_sync(0xffffffffu, rows != 0); some; some &= some - 1) {
-                const uint64_t word = w0 + (uint64_t)(__ffs(some) - 1) * lookers, item = word / 8;
-                const uint32_t unit = (uint32_t)(item / a.n_kv);
-                const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
-                if (u.tiles == 0) continue;  // sees nothing: no words were written
-                uint32_t left = __shfl_sync(0xffffffffu, rows, __ffs(some) - 1);
-                for (uint32_t k = 0; left; ++k, left &= left - 1) {
-                    if (k % kWarps != warp) continue;
-                    const int r = (int)(word % 8) * 32 + __ffs(left) - 1;
-                    attend_row<T, D>(a, unit_tok(a, u, r), unit_head(a, u, (uint32_t)(item % a.n_kv), r));
-                }
-            }
-        }
-    }
-    Cut x;
-    if (by_item) {
-        const uint32_t unit = i / a.n_kv, first_tile = p.begin[unit], all = p.begin[unit + 1] - first_tile, total = p.begin[p.n_units];
-        if (all == 0) return;
-        const uint32_t n = used_workers(total, p.workers), per = total / n, more = total - per * n, size = all / a.n_kv, extra = item_extra<TILE>();
-        x.c = i % a.n_kv;
-        x.c0 = tile_owner(first_tile + x.c * size + extra, per, more);
-        x.c1 = tile_owner(first_tile + x.c * size + size - 1, per, more);
-        if (x.c0 == x.c1) return;
-        const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
-        x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows;
-    } else {
-        if (i + 1 >= p.workers) return;
-        x = p.cuts[i + 1];
-        if (x.c1 == 0 || x.c0 != i) return;  // the border lies between two items, or is not the item's first
-    }
-    // few rows: several warps share a row's pieces
-    const uint32_t here = min((uint32_t)max(x.rows - (int)row_first, 0), rows_a_block);  // rows of this block
-    const uint32_t share = here == 0 || here >= kWarps ? 1 : kWarps / here;
+    const uint32_t i = blockIdx.x / parts, row_first = blockIdx.x % parts * rows_a_block, warp = threadIdx.x / 32, lane = threadIdx.x & 31u;
+    const uint32_t rows = AGAIN ? redo_word(a, p, 0) : 0;  // on its way while the pieces are joined
+    Cut x = {};
+    uint32_t bad = 0;  // bit k: row warp + 8 k of the block came out non-finite
     __shared__ float m_sh[kWarps], l_sh[kWarps];
     __shared__ float o_sh[kWarps][D];
-    const uint32_t lane = threadIdx.x & 31u;
-    if (share > 1) {
-        Row<D> sum;
-        const uint32_t r = warp % here, g = warp / here;
-        if (g < share)
-            add_pieces<D>(sum, p.part_ml, p.part_o, g, share, x.c1 - x.c0 + 1,
-                          [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
-        if (lane == 0) m_sh[warp] = sum.m, l_sh[warp] = sum.l;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) o_sh[warp][lane * (D / 32) + e] = sum.o[e];
-        __syncthreads();
-        if (warp >= here) return;
-        for (uint32_t k = 1; k < share; ++k) {
-            const uint32_t other = warp + k * here;
-            const float m2 = m_sh[other], top = fmaxf(sum.m, m2), f1 = sum.m == top ? 1.f : ex2(sum.m - top), f2 = m2 == top ? 1.f : ex2(m2 - top);
-            sum.m = top;
-            sum.l = sum.l * f1 + l_sh[other] * f2;
-#pragma unroll
-            for (int e = 0; e < D / 32; ++e) sum.o[e] = sum.o[e] * f1 + o_sh[other][lane * (D / 32) + e] * f2;
-        }
-        const int row = x.row0 + (int)(row_first + warp);
-        finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
-        return;
-    }
-    for (uint32_t r = warp; r < here; r += kWarps) {
-        Row<D> sum;
-        add_pieces<D>(sum, p.part_ml, p.part_o, 0, 1, x.c1 - x.c0 + 1,
-                      [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
+    auto done = [&](const Row<D> &sum, uint32_t r) {
         const int row = x.row0 + (int)(row_first + r);
-        finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group, p.again);
+        if (finish<T, D>(a, sum, x.q0 + row / (int)a.group, x.c * a.group + (uint32_t)row % a.group)) bad |= 1u << (r / kWarps);
+    };
+    auto join = [&] {
+        if (by_item) {
+            const uint32_t unit = i / a.n_kv, first_tile = p.begin[unit], all = p.begin[unit + 1] - first_tile, total = p.begin[p.n_units];
+            if (all == 0) return;
+            const uint32_t n = used_workers(total, p.workers), per = total / n, more = total - per * n, size = all / a.n_kv, extra = item_extra<TILE>();
+            x.c = i % a.n_kv;
+            x.c0 = tile_owner(first_tile + x.c * size + extra, per, more);
+            x.c1 = tile_owner(first_tile + x.c * size + size - 1, per, more);
+            if (x.c0 == x.c1) return;
+            const Unit u = get_unit<ROWS, TILE>(a, p, unit / p.n_rt, unit % p.n_rt);
+            x.q0 = u.q0, x.row0 = u.row0, x.rows = u.rows;
+        } else {
+            if (i + 1 >= p.workers) return;
+            x = p.cuts[i + 1];
+            if (x.c1 == 0 || x.c0 != i) return;  // the border lies between two items, or is not the item's first
+        }
+        // few rows: several warps share a row's pieces
+        const uint32_t here = min((uint32_t)max(x.rows - (int)row_first, 0), rows_a_block);  // rows of this block
+        const uint32_t share = here == 0 || here >= kWarps ? 1 : kWarps / here;
+        if (share > 1) {
+            Row<D> sum;
+            const uint32_t r = warp % here, g = warp / here;
+            if (g < share)
+                add_pieces<D>(sum, p.part_ml, p.part_o, g, share, x.c1 - x.c0 + 1,
+                              [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
+            if (lane == 0) m_sh[warp] = sum.m, l_sh[warp] = sum.l;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) o_sh[warp][lane * (D / 32) + e] = sum.o[e];
+            __syncthreads();
+            if (warp >= here) return;
+            for (uint32_t k = 1; k < share; ++k) {
+                const uint32_t other = warp + k * here;
+                const float m2 = m_sh[other], top = fmaxf(sum.m, m2), f1 = sum.m == top ? 1.f : ex2(sum.m - top), f2 = m2 == top ? 1.f : ex2(m2 - top);
+                sum.m = top;
+                sum.l = sum.l * f1 + l_sh[other] * f2;
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) sum.o[e] = sum.o[e] * f1 + o_sh[other][lane * (D / 32) + e] * f2;
+            }
+            done(sum, warp);
+            return;
+        }
+        for (uint32_t r = warp; r < here; r += kWarps) {
+            Row<D> sum;
+            add_pieces<D>(sum, p.part_ml, p.part_o, 0, 1, x.c1 - x.c0 + 1,
+                          [&](uint32_t k) { return ((uint64_t)(x.c0 + k) * 2 + (k == 0)) * p.slot_rows + row_first + r; });
+            done(sum, r);
+        }
+    };
+    join();
+    if (AGAIN) {
+        const bool more = p.redo && blockIdx.x < kLookers && (uint64_t)p.n_units * a.n_kv * 8 > 32 * kLookers;  // turns to come
+        if (more || __any_sync(0xffffffffu, bad | rows)) redo<T, D, ROWS, TILE>(a, p, x.q0, x.row0 + (int)(row_first + warp), x.c, bad, rows);
     }
 }
 
@@ -196,7 +219,10 @@ __global__ void __launch_bounds__(kWarps * 32) kv_attn_join_shared_kernel(const 
     }
     if (own.rows == kTcRows) add_pass<D, kTcRows, kTcTile>(a, own, x, s, tok, h);
     else add_pass<D, kFewRows, kFewTile>(a, own, x, s, tok, h);
-    finish<T, D>(a, x, tok, h, own.again);
+    if (finish<T, D>(a, x, tok, h) && own.again) {
+        __syncwarp();
+        attend_row<T, D>(a, tok, h);
+    }
 }
 
 }  // namespace
@@ -223,9 +249,15 @@ cudaError_t launch_kv_attn_join(const AttnArgs &a, const Pass &p, uint32_t dtype
     // sixteen rows a block; fewer, their pieces spread over the warps, where few items are in many pieces each
     const uint32_t rows_a_block = !by_item || p.workers / items < 16 ? kFewRows : p.slot_rows <= kFewRows ? 1 : 4;
     const uint32_t parts = (p.slot_rows + rows_a_block - 1) / rows_a_block, grid = (by_item ? (uint32_t)items : borders) * parts;
-    if (p.rows == kTcRows)
-        GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kTcRows, kTcTile>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)));
-    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, kFewRows, kFewTile>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)));
+#define GMS_JOIN(ROWS, TILE, AGAIN) \
+    GMS_BY_TYPE((launch_dependent(kv_attn_join_kernel<T, D, ROWS, TILE, AGAIN>, grid, kWarps * 32, 0, s, a, p, parts, rows_a_block, by_item)))
+    if (p.rows == kTcRows) {
+        if (p.again) GMS_JOIN(kTcRows, kTcTile, true);
+        GMS_JOIN(kTcRows, kTcTile, false);
+    }
+    if (p.again) GMS_JOIN(kFewRows, kFewTile, true);
+    GMS_JOIN(kFewRows, kFewTile, false);
+#undef GMS_JOIN
 }
 
 cudaError_t launch_kv_attn_join_shared(const AttnArgs &a, const Pass &pre, const Pass &own, uint32_t dtype, uint32_t head_dim, cudaStream_t s)

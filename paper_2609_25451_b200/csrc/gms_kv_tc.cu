@@ -17,7 +17,7 @@
 // 1,024 and the tensor core 1,280 (64-column scores read both operands from shared memory at 1.5 times the cycles); tensor pipe
 // 47 % active.  Taking a part of the exponentials on the multiply-add units, loading the next S ahead, and making the slots
 // take turns were each slower.  2,048 + 2 new sequences over 16k cached tokens, 32 / 8 heads of 128, bf16, 728 GFLOP: 780 us
-// back to back (0.93 PFLOP/s), 870 to 900 us among other work.  8,192 tokens under a window of 1,024, f16: 240 us.
+// back to back (0.93 PFLOP/s), 870 to 890 us among other work.  8,192 tokens under a window of 1,024, f16: 238 us.
 // Tensor memory: 2 x 2 S buffers of 64 columns, O0 O1 (D each) = 512 columns at D = 128, hence P over S.
 // Shared memory: Q 2 x 128 x D, then a ring of K and V tiles.
 #include "gms_internal.h"

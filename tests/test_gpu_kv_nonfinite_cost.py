@@ -71,3 +71,15 @@ def test_behind_a_prefix(poison):
     b.record()
     torch.cuda.synchronize()
     assert a.elapsed_time(b) < 15.0
+
+
+def test_more_items_than_one_turn_looks_at():
+    """1,600 items of 256 rows; in some sequences, the last ones too, values that the newest queries alone see are infinite."""
+    def poison(p):
+        for s in (0, 7, 123, 250, 398, 399):
+            p.V[s][-1, :, s % 64] = math.inf
+            p.V[s][-40, 1, 3] = math.nan
+
+    p = Problem(4, heads=4, kv_heads=2, dim=64, block=64, q_lens=(140,) * 400, kv_lens=tuple(140 + s % 90 for s in range(400)), poison=poison)
+    p.run()
+    p.check()
