@@ -102,7 +102,8 @@ extern "C" {
 #define GMS_DEV_TIMEOUT 1ull   /* a warp gave up waiting for one of its own bulk copies (2 s), then
                                   spent up to 2 s more draining the rest: worst case 4 s per call  */
 #define GMS_DEV_HOLE 2ull      /* gms_kv_evict kept a token whose rows could not be copied: its source or
-                                  destination id lies outside the pool                             */
+                                  destination id lies outside the pool; gms_kv_delta, that a state's does  */
+#define GMS_DEV_FULL 4ull      /* gms_kv_plan had no free block, table entry, row or room in the ring for something */
 
 typedef struct gms_manifest gms_manifest; /* opaque */
 
@@ -514,6 +515,142 @@ typedef struct {
     uint64_t *status;                   /* (device) may be NULL; GMS_DEV_HOLE is or-ed in                */
 } gms_kv_evict_args;
 int gms_kv_evict(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_evict_args *args, void *stream);
+
+/*
+ * gms_kv_plan / gms_kv_append / gms_kv_delta -- the rest of an engine's step on the state that the calls above put back:
+ * which blocks and slots the step's tokens go to, putting their keys and values there, and layers whose state is recurrent.
+ * All asynchronous on `stream`; no allocation, no host synchronisation; can be captured into a CUDA graph and replayed on the
+ * step after (counters and lengths are on the device and may be updated in place).
+ *
+ * gms_kv_plan -- block tables and slot maps from request lengths.  With B = block_tokens, for every sequence s
+ *   base = max(lens - drop_lens, 0);  lens_out = base + rows;  had = ceil(lens / B);  need = ceil(lens_out / B)
+ * where rows = new_lens[s], cut off where the sum over the sequences so far would pass total_rows.  drop_lens takes tokens
+ * off a sequence's end first (speculated tokens that were rejected; all of them: the request has left, and its row is free for
+ * another).  Free blocks are kept in a ring: free_state[0] is the position of the next one in free_ids[free_cap],
+ * free_state[1] how many there are.
+ *   need > had: entries had .. need-1 of the row get the next blocks of the ring, sequences in ascending order
+ *   need < had: the blocks in entries need .. had-1 go to the ring's end, sequences and entries in ascending order; ids outside
+ *               [0, n_blocks) (holes) do not; the entries keep what they hold.  Blocks that come back in a call are free
+ *               from the next call on
+ *   cu_q[0] = 0, cu_q[s+1] = cu_q[s] + rows: offsets of the sequences' rows
+ *   for row cu_q[s] + i:  positions = base + i;  slots = id * B + positions % B with id = the row's entry positions / B
+ *   rows from cu_q[n_seq] on (a batch padded to a fixed size): slots = -1, positions = 0
+ * A token that has no block (the ring is empty: its entry gets -1; a position beyond table_blocks * B; a hole in the table) has
+ * slot -1; lens_out counts it all the same, for gms_kv_attention a token in a hole.  GMS_DEV_FULL in `status` tells of an empty
+ * ring, of a full table row, of rows cut off at total_rows and of blocks that a ring without room for them lost.  Lengths below 0
+ * count as 0, above 2^30 as 2^30.  Everything is exact and the same in every run.
+ * Neither table rows nor the ring may hold a block twice; free_cap >= n_blocks is always enough.  Outputs may not overlap inputs,
+ * but lens_out may be lens and free_state_out may be free_state.
+ * Errors: NULL, ALIGN, ARG, RANGE, CUDA.
+ */
+typedef struct {
+    const int32_t *lens;           /* (device) n_seq: tokens that are cached                             */
+    const int32_t *new_lens;       /* (device) n_seq: tokens to come                                     */
+    const int32_t *drop_lens;      /* (device) n_seq: tokens taken off the end first; NULL: none         */
+    int32_t *lens_out;             /* (device) n_seq, may be lens                                        */
+    int32_t *block_table;          /* (device) n_seq rows, table_stride entries apart                    */
+    int32_t *free_ids;             /* (device) free_cap                                                  */
+    const int32_t *free_state;     /* (device) 2: position of the next free block, number of free blocks */
+    int32_t *free_state_out;       /* (device) 2, may be free_state                                      */
+    int32_t *cu_q;                 /* (device) n_seq + 1                                                 */
+    int64_t *slots;                /* (device) total_rows                                                */
+    int32_t *positions;            /* (device) total_rows, may be NULL                                   */
+    uint64_t *status;              /* (device) may be NULL; GMS_DEV_FULL is or-ed in                     */
+    uint64_t table_stride;         /* entries                                                            */
+    uint32_t n_seq, total_rows;    /* total_rows < 2^31                                                  */
+    uint32_t table_blocks;         /* entries of a row that may be used, at most table_stride and 2^20   */
+    uint32_t free_cap;             /* < 2^31                                                             */
+    uint32_t n_blocks;             /* of the pool, 1 .. 2^31 - 1                                         */
+    uint32_t block_tokens;         /* a power of two, 16 .. 1024                                         */
+} gms_kv_plan_args;
+int gms_kv_plan(const gms_kv_plan_args *args, void *stream);
+
+/*
+ * gms_kv_append -- what stands between a layer's projections and gms_kv_attention, in one pass: queries and keys normed head by
+ * head, both rotated to their positions, queries to q_out, keys and values into the pool's blocks.  For a row x of q or k
+ * (head_dim elements, products and sums in 32 bits, one rounding at the end):
+ *   norm (q_weight / k_weight given):  x[d] <- x[d] / sqrt(mean x^2 + eps) * (weight[d] + weight_offset)
+ *   rotation: pair j < rotary_dim / 2 is elements (j, j + rotary_dim / 2) (GMS_PAIR_HALVES) or (2j, 2j + 1)
+ *     (GMS_PAIR_NEIGHBOURS); with angle = positions[axes[j]][i] * inv_freq[j] (in 64 bits), c = rope_scale * cos, s = rope_scale * sin:
+ *     (a, b) <- (a c - b s, b c + a s);  elements from rotary_dim on stay.
+ * Several axes (time, height, width of a picture's patches): positions has n_axes rows, and axes[j] says which of them pair j
+ * turns with (entries >= n_axes count as the last one; NULL: all with row 0).  Values are copied.
+ * Row i's keys and values go to slot slots[i] = block * block_tokens + token; a slot outside the pool (-1: padding, a token
+ * without a block) is skipped, the row's queries are written all the same.  Rows from *n_rows on are left alone altogether.
+ * Slots must be distinct (the caller's duty; duplicates race).  q_out may be q (same strides), else outputs may not overlap inputs.
+ * q may be NULL (n_heads 0: keys and values only), and so may k and v (both: queries only).
+ * Errors: NULL, ALIGN, ARG, RANGE, CUDA.
+ */
+#define GMS_DTYPE_F32 2u
+#define GMS_PAIR_HALVES 0u
+#define GMS_PAIR_NEIGHBOURS 1u
+typedef struct {
+    const void *q, *k, *v;         /* (device) [rows][heads][head_dim], the layout's dtype, 16-byte aligned */
+    void *q_out;                   /* (device) [rows][n_heads][head_dim]                                 */
+    const int64_t *slots;          /* (device) rows                                                      */
+    const int32_t *positions;      /* (device) n_axes rows of positions_stride; NULL if rotary_dim is 0  */
+    const int32_t *n_rows;         /* (device) may be NULL: rows that are there (cu_q + n_seq of a plan)  */
+    const float *inv_freq;         /* (device) rotary_dim / 2                                            */
+    const uint8_t *axes;           /* (device) rotary_dim / 2, may be NULL                               */
+    const void *q_weight, *k_weight; /* (device) head_dim of weight_dtype, each may be NULL (no norm); 16-byte aligned */
+    uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
+        out_token_stride, out_head_stride; /* bytes, multiples of 16                                     */
+    uint64_t positions_stride;     /* entries, >= rows                                                   */
+    uint32_t rows, n_heads;        /* rows < 2^31                                                        */
+    uint32_t rotary_dim;           /* multiple of 8, at most head_dim; 0: no rotation                    */
+    uint32_t n_axes, pairs;        /* 1 .. 8; GMS_PAIR_*                                                 */
+    uint32_t weight_dtype;         /* GMS_DTYPE_*                                                        */
+    float weight_offset, eps, rope_scale;
+    uint32_t reserved;             /* 0                                                                  */
+} gms_kv_append_args;
+int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_append_args *args, void *stream);
+
+/*
+ * gms_kv_delta -- the gated delta rule, the recurrent layers' counterpart of attention.  A head's state is a head_dim x head_dim
+ * matrix S of 32-bit numbers, [key][value], that lives in the pool, so that capture, restore, digest and verify keep it like any
+ * other block: head h of a sequence is in block table[h / per], at byte (h % per) * 4 * head_dim^2 of its plane, where
+ * per = block_bytes / (4 * head_dim^2) heads fit into a block.  For each of a sequence's rows in turn, with c = h / (n_heads / n_key_heads):
+ *   S <- exp(g[i,h]) S;   d = beta[i,h] (v[i,h] - S^T k[i,c]);   S <- S + k[i,c] d^T;   out[i,h] = scale S^T q[i,c]
+ * (unit_qk: q and k are first divided by sqrt(sum x^2 + unit_eps)).  S begins as the state in src_table, or as zeros where
+ * past_lens[s] is 0, and the state after the last row goes to dst_table (a sequence without rows: as it began).  g NULL counts as
+ * zeros, beta NULL as ones.  g is a logarithm, at most 0 in earnest; -infinity clears the state.
+ * Sequences of many rows are done in chunks of 64 on tensor cores: products of 16-bit inputs with S, d and decays, which enter as
+ * sums of two 16-bit terms (2^-16 relative) wherever they go on into a state; what goes into `out` alone enters as one.  State
+ * and sums are kept in 32 bits.  What a row does not depend on cannot reach it, whatever bits it holds.
+ * src_table and dst_table may be the same (states are updated in place), and rows of src_table may be equal (several sequences go on
+ * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence.  An id outside [0, n_blocks)
+ * reads as zeros and is not written; GMS_DEV_HOLE in `status` tells of it.  Rows that no sequence owns, and rows of a sequence
+ * beyond its first max_q, are not processed and leave `out` as it is.
+ * gms_kv_delta_workspace: bytes for this call and every later one with no larger n_seq, total_q and max_q and the same heads.
+ * Errors: NULL, ALIGN, ARG, RANGE, CUDA.
+ */
+typedef struct {
+    uint32_t plane;                /* of the pool                                                        */
+    uint32_t n_heads;              /* value heads, >= 1                                                  */
+    uint32_t head_dim;             /* 64 or 128                                                          */
+    uint32_t reserved;             /* 0                                                                  */
+} gms_kv_state;
+typedef struct {
+    const void *q, *k, *v;         /* (device) [total_q][n_key_heads or n_heads][head_dim], 16-byte aligned */
+    void *out;                     /* (device) [total_q][n_heads][head_dim]                              */
+    const float *g, *beta;         /* (device) [total_q][n_heads], rows *_stride elements apart          */
+    const int32_t *cu_q;           /* (device) n_seq + 1 ascending offsets; NULL: one row a sequence     */
+    const int32_t *past_lens;      /* (device) n_seq; NULL: every state is read                          */
+    const int32_t *src_table, *dst_table; /* (device) n_seq rows of ids, *_stride entries apart          */
+    void *workspace;               /* (device) 256-byte aligned; calls that overlap must not share it    */
+    uint64_t *status;              /* (device) may be NULL                                               */
+    uint64_t workspace_bytes;
+    uint64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
+        out_token_stride, out_head_stride; /* bytes, multiples of 16                                     */
+    uint64_t g_stride, beta_stride, src_stride, dst_stride;
+    uint32_t n_seq, n_key_heads;   /* n_heads is a multiple of n_key_heads                               */
+    uint32_t total_q, max_q;       /* rows; longest run of a sequence                                    */
+    uint32_t dtype;                /* GMS_DTYPE_BF16 or GMS_DTYPE_F16, of q, k, v and out                */
+    uint32_t unit_qk;              /* 0 or 1                                                             */
+    float unit_eps, scale;
+} gms_kv_delta_args;
+int gms_kv_delta_workspace(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_delta_args *args, uint64_t *nbytes);
+int gms_kv_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_delta_args *args, void *stream);
 
 /*
  * Pinned, device-mapped host memory for a GMS_SRC_HOST_MAPPED image (the

@@ -5,7 +5,6 @@
 #include "gms_kv_attn.h"
 
 namespace gms {
-namespace {
 
 int bad_pool(const gms_kv_pool *p)
 {
@@ -33,7 +32,7 @@ int bad_layout(const gms_kv_pool *p, const gms_kv_layout *l)
     return tokens_outside || heads_outside ? GMS_OK : GMS_ERR_ARG;
 }
 
-uint32_t log2_of(uint32_t x) { return 31u - (uint32_t)__builtin_clz(x); }
+namespace {
 
 // Checks everything a call is given and fills in the kernels' arguments.  `planning`: workspace pointers are not looked at.
 int make_args(const gms_kv_pool *pool, const gms_kv_layout *layout, const gms_kv_attn *t, const gms_kv_weight *w,

@@ -16,6 +16,11 @@ namespace gms {
 
 void count_launches(uint32_t n);
 
+// GMS_OK, or what is wrong with a pool or with a layout in it.
+int bad_pool(const gms_kv_pool *p);
+int bad_layout(const gms_kv_pool *p, const gms_kv_layout *l);
+inline uint32_t log2_of(uint32_t x) { return 31u - (uint32_t)__builtin_clz(x); }
+
 // What every attention kernel gets (by value).  Strides of pool and of q / out are in bytes.
 struct AttnArgs {
     const uint8_t *k_base, *v_base;  // planes of this layer

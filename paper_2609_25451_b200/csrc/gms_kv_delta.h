@@ -1,0 +1,40 @@
+// Internal declarations of the gated delta rule's kernels.
+#pragma once
+#include "gms_internal.h"
+#include "gms_kv_attn.h"
+#include "gms_ptx.h"
+
+namespace gms {
+
+struct DeltaArgs {
+    const uint8_t *q, *k, *v;
+    uint8_t *out;
+    const float *g, *beta;
+    const int32_t *cu_q, *past_lens, *src_table, *dst_table;
+    uint8_t *plane;
+    unsigned long long *status;
+    uint64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head, g_stride, beta_stride, src_stride, dst_stride, block_stride;
+    uint32_t n_blocks, per_block;        // states a block holds
+    uint32_t n_seq, n_heads, group;      // group = n_heads / n_key_heads
+    uint32_t total_q, max_q, unit_qk;
+    float unit_eps, scale;
+};
+
+#ifdef __CUDACC__
+__device__ __forceinline__ int delta_begin(const DeltaArgs &a, uint32_t s) { return a.cu_q ? min(max(a.cu_q[s], 0), (int)a.total_q) : (int)s; }
+__device__ __forceinline__ int delta_rows(const DeltaArgs &a, uint32_t s)
+{
+    if (!a.cu_q) return 1;
+    return min(max(min(a.cu_q[s + 1], (int)a.total_q) - delta_begin(a, s), 0), (int)a.max_q);
+}
+// Where a head's state lies; null: in a hole.
+template <int D>
+__device__ __forceinline__ float *delta_state(const DeltaArgs &a, const int32_t *table, uint64_t stride, uint32_t s, uint32_t h)
+{
+    const int id = table[s * stride + h / a.per_block];
+    if ((uint32_t)id >= a.n_blocks) return nullptr;
+    return reinterpret_cast<float *>(a.plane + (uint64_t)id * a.block_stride) + (uint64_t)(h % a.per_block) * D * D;
+}
+#endif
+
+}  // namespace gms

@@ -26,6 +26,7 @@ BUILD_HOST_ONLY = 1
 BUILD_SELFTEST_STALL = 2  # test suites only: one warp's first wait runs out (see include/gms.h)
 DEV_TIMEOUT = 1  # bits of the device status word
 DEV_HOLE = 2
+DEV_FULL = 4
 
 # numpy view of gms_entry / gms_mismatch (32 and 16 bytes)
 ENTRY_DTYPE = np.dtype([("tensor_id", "<u8"), ("src_offset", "<u8"), ("dst", "<u8"), ("nbytes", "<u8")])
@@ -37,6 +38,7 @@ EXPORTS = (
     "gms_manifest_chunk_count", "gms_manifest_chunk", "gms_manifest_set_expected", "gms_restore", "gms_capture", "gms_digest",
     "gms_verify", "gms_digest_verify", "gms_restore_verify", "gms_verify_tensors", "gms_verify_flat_noalloc", "gms_last_device_status", "gms_kv_restore", "gms_kv_capture", "gms_kv_digest", "gms_kv_verify",
     "gms_kv_attention_workspace", "gms_kv_attention", "gms_kv_attention_shared_workspace", "gms_kv_attention_shared", "gms_kv_evict",
+    "gms_kv_plan", "gms_kv_append", "gms_kv_delta_workspace", "gms_kv_delta",
     "gms_host_image_alloc", "gms_host_image_free",
     "gms_pipe_create", "gms_pipe_direct_io", "gms_pipe_mapped_writes", "gms_pipe_destroy", "gms_restore_fd", "gms_capture_fd", "gms_stage_create", "gms_stage_destroy", "gms_restore_staged",
     "gms_service_create", "gms_service_destroy", "gms_service_acquire_rw", "gms_service_alloc", "gms_service_commit",
@@ -62,7 +64,8 @@ class KvPool(C.Structure):
 
 
 KV_IMAGE_BY_ID = 1
-DTYPE_BF16, DTYPE_F16 = 0, 1
+DTYPE_BF16, DTYPE_F16, DTYPE_F32 = 0, 1, 2
+PAIR_HALVES, PAIR_NEIGHBOURS = 0, 1
 
 
 class KvLayout(C.Structure):
@@ -114,6 +117,40 @@ class KvEvictArgs(C.Structure):
                 ("reserved", C.c_uint32), ("status", C.c_void_p)]
 
 
+class KvPlanArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("lens", "new_lens", "drop_lens", "lens_out", "block_table", "free_ids", "free_state",
+                                          "free_state_out", "cu_q", "slots", "positions", "status")] + [("table_stride", C.c_uint64)] + [
+                (n, C.c_uint32) for n in ("n_seq", "total_rows", "table_blocks", "free_cap", "n_blocks", "block_tokens")]
+
+
+class KvAppendArgs(C.Structure):
+    _made = None  # what the tensors that it was made of have
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "slots", "positions", "n_rows", "inv_freq", "axes", "q_weight", "k_weight")] + [
+                (n, C.c_uint64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
+                                          "v_head_stride", "out_token_stride", "out_head_stride", "positions_stride")] + [
+                (n, C.c_uint32) for n in ("rows", "n_heads", "rotary_dim", "n_axes", "pairs", "weight_dtype")] + [
+                (n, C.c_float) for n in ("weight_offset", "eps", "rope_scale")] + [("reserved", C.c_uint32)]
+
+
+class KvState(C.Structure):
+    _fields_ = [("plane", C.c_uint32), ("n_heads", C.c_uint32), ("head_dim", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class KvDeltaArgs(C.Structure):
+    """``gms_kv_delta_args``; usually made by :func:`kv_delta_args`, which also keeps the tensors alive."""
+
+    _made = None  # what the tensors that it was made of have
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "out", "g", "beta", "cu_q", "past_lens", "src_table", "dst_table", "workspace",
+                                          "status")] + [
+                (n, C.c_uint64) for n in ("workspace_bytes", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                          "v_token_stride", "v_head_stride", "out_token_stride", "out_head_stride", "g_stride",
+                                          "beta_stride", "src_stride", "dst_stride")] + [
+                (n, C.c_uint32) for n in ("n_seq", "n_key_heads", "total_q", "max_q", "dtype", "unit_qk")] + [
+                ("unit_eps", C.c_float), ("scale", C.c_float)]
+
+    set_workspace = KvAttn.set_workspace
+
+
 _lib = None
 
 
@@ -153,6 +190,10 @@ def lib():
             "gms_kv_attention_shared_workspace": (i, [p, p, p, p, pu64]),
             "gms_kv_attention_shared": (i, [p, p, p, p, p]),
             "gms_kv_evict": (i, [p, p, p, p]),
+            "gms_kv_plan": (i, [p, p]),
+            "gms_kv_append": (i, [p, p, p, p]),
+            "gms_kv_delta_workspace": (i, [p, p, p, pu64]),
+            "gms_kv_delta": (i, [p, p, p, p]),
             "gms_host_image_alloc": (i, [u64, pp, pp]),
             "gms_host_image_free": (i, [p]),
             "gms_pipe_create": (i, [u32, u64, u32, pp]),
@@ -520,6 +561,161 @@ def gms_kv_evict(pool: KvPool, layout: KvLayout, args: KvEvictArgs, stream=None)
         if heads != layout.n_kv_heads or src * layout.block_tokens < args.max_len or dst * layout.block_tokens < min(args.max_len, args.budget):
             raise ValueError("weights have another number of KV heads than the layout, or tables too few blocks a row")
     _check(lib().gms_kv_evict(_ref(pool), _ref(layout), _ref(args), _stream(stream)), "gms_kv_evict")
+
+
+def _strides(t):
+    return (0, 0) if t is None else (t.stride(0) * t.element_size(), t.stride(1) * t.element_size())
+
+
+def _heads_dim(what, tensors):
+    """Rows [tokens, heads, dim] of one 16-bit type and one dim; the type (or None) and the dim."""
+    kinds = {(t.dtype, t.shape[0], t.shape[2]) if t.dim() == 3 else None for t in tensors if t is not None}
+    if len(kinds) != 1 or None in kinds:
+        raise ValueError(what)
+    _rows(what, 2, True, tensors)
+    dtype, n, dim = kinds.pop()
+    return {"torch.bfloat16": DTYPE_BF16, "torch.float16": DTYPE_F16}[str(dtype)], n, dim
+
+
+def kv_plan_args(*, n_blocks: int, block_tokens: int, lens, new_lens, block_table, free_ids, free_state, cu_q, slots, drop_lens=None,
+                 lens_out=None, free_state_out=None, positions=None, status=None) -> KvPlanArgs:
+    """gms_kv_plan_args from tensors: int32 but for ``slots`` (int64), ``block_table`` [sequences, blocks].  ``lens_out`` and
+    ``free_state_out`` None: updated in place."""
+    lens_out = lens if lens_out is None else lens_out
+    free_state_out = free_state if free_state_out is None else free_state_out
+    n_seq, rows = lens.shape[0], slots.shape[0]
+    if block_table.dim() != 2 or block_table.shape[0] != n_seq or cu_q.shape[0] != n_seq + 1 or any(
+            t is not None and tuple(t.shape) != (n_seq,) for t in (lens, new_lens, drop_lens, lens_out)):
+        raise ValueError("lengths, offsets and the table disagree about the number of sequences")
+    if free_state.numel() != 2 or free_state_out.numel() != 2 or slots.dim() != 1 or positions is not None and tuple(positions.shape) != (rows,):
+        raise ValueError("free_state has 2 entries, slots and positions are [rows]")
+    flat = (lens, new_lens, drop_lens, lens_out, free_ids, free_state, free_state_out, cu_q, positions)
+    _int32(block_table, *flat)
+    _rows("slots are int64", 8, False, (slots,))
+    if any(t is not None and not t.is_contiguous() for t in flat + (slots,)):
+        raise ValueError("lengths, offsets, the ring, slots and positions are contiguous")
+    _word(status)
+    a = KvPlanArgs(lens=_dev(lens), new_lens=_dev(new_lens), drop_lens=_dev(drop_lens), lens_out=_dev(lens_out), block_table=_dev(block_table),
+                   free_ids=_dev(free_ids), free_state=_dev(free_state), free_state_out=_dev(free_state_out), cu_q=_dev(cu_q),
+                   slots=_dev(slots), positions=_dev(positions), status=_dev(status), table_stride=block_table.stride(0) if n_seq > 1 else block_table.shape[1],
+                   n_seq=n_seq, total_rows=rows, table_blocks=block_table.shape[1], free_cap=free_ids.shape[0], n_blocks=n_blocks,
+                   block_tokens=block_tokens)
+    a._keep = flat + (block_table, slots, status)
+    return a
+
+
+def gms_kv_plan(args: KvPlanArgs, stream=None):
+    _check(lib().gms_kv_plan(_ref(args), _stream(stream)), "gms_kv_plan")
+
+
+def kv_append_args(*, slots=None, q=None, k=None, v=None, q_out=None, positions=None, inv_freq=None, axes=None, n_rows=None, q_weight=None,
+                   k_weight=None, pairs: int = PAIR_HALVES, weight_offset: float = 0.0, eps: float = 1e-6, rope_scale: float = 1.0) -> KvAppendArgs:
+    """gms_kv_append_args from tensors: ``q``, ``k``, ``v`` and ``q_out`` (None: in place) [rows, heads, dim] with any strides and a
+    contiguous last dimension, ``slots`` int64 [rows], ``positions`` int32 [rows] or [axes, rows], ``inv_freq`` float32 [rotated / 2]
+    (None: no rotation), ``axes`` uint8 [rotated / 2], ``n_rows`` an int32 word, weights [dim] of one type."""
+    if q is not None and q_out is None:
+        q_out = q
+    dtype, rows, dim = _heads_dim("q, k, v and q_out are 16-bit [rows, heads, dim] of one type", (q, k, v, q_out))
+    if q is not None and q.shape != q_out.shape or (k is None) != (v is None) or k is not None and (k.shape != v.shape or slots is None):
+        raise ValueError("q_out must match q, v must match k, and keys and values need slots")
+    if slots is not None:
+        _rows("slots are int64", 8, False, (slots,))
+        if tuple(slots.shape) != (rows,) or not slots.is_contiguous():
+            raise ValueError("slots are [rows]")
+    rotary = 0
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.shape[0]
+        if positions is None or positions.shape[-1] != rows or positions.dim() > 2 or not inv_freq.is_contiguous():
+            raise ValueError("positions are [rows] or [axes, rows]")
+        _int32(positions)
+        _float32(inv_freq)
+        if axes is not None:
+            _rows("axes are uint8", 1, False, (axes,))
+            if tuple(axes.shape) != tuple(inv_freq.shape) or not axes.is_contiguous():
+                raise ValueError("axes has an entry for each of inv_freq")
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    kinds = {str(w.dtype) for w in weights}
+    if len(kinds) > 1 or any(tuple(w.shape) != (dim,) or not w.is_contiguous() for w in weights):
+        raise ValueError("weights are [dim], both of one type")
+    for w in weights:
+        _rows("weights are on the GPU", w.element_size(), True, (w,))
+    weight_dtype = {"torch.bfloat16": DTYPE_BF16, "torch.float16": DTYPE_F16, "torch.float32": DTYPE_F32}.get(kinds.pop() if kinds else "torch.float32")
+    if weight_dtype is None:
+        raise ValueError("weights are bfloat16, float16 or float32")
+    _int32(n_rows)
+    (qt, qh), (kt, kh), (vt, vh), (ot, oh) = (_strides(t) for t in (q, k, v, q_out))
+    two = positions is not None and positions.dim() == 2
+    a = KvAppendArgs(q=_dev(q), k=_dev(k), v=_dev(v), q_out=_dev(q_out), slots=_dev(slots), positions=_dev(positions), n_rows=_dev(n_rows),
+                     inv_freq=_dev(inv_freq), axes=_dev(axes), q_weight=_dev(q_weight), k_weight=_dev(k_weight), q_token_stride=qt, q_head_stride=qh,
+                     k_token_stride=kt, k_head_stride=kh, v_token_stride=vt, v_head_stride=vh, out_token_stride=ot, out_head_stride=oh,
+                     positions_stride=positions.stride(0) if two and positions.shape[0] > 1 else rows, rows=rows,
+                     n_heads=0 if q is None else q.shape[1], rotary_dim=rotary, n_axes=positions.shape[0] if two else 1, pairs=pairs,
+                     weight_dtype=weight_dtype, weight_offset=weight_offset, eps=eps, rope_scale=rope_scale)
+    a._keep = (q, k, v, q_out, slots, positions, n_rows, inv_freq, axes, q_weight, k_weight)
+    a._made = (dtype, dim, None if k is None else k.shape[1])
+    return a
+
+
+def gms_kv_append(pool: KvPool, layout: KvLayout, args: KvAppendArgs, stream=None):
+    if layout is not None and args is not None and args._made is not None:
+        dtype, dim, heads = args._made
+        if dtype != layout.dtype or dim != layout.head_dim or heads not in (None, layout.n_kv_heads):
+            raise ValueError(f"tensors of GMS_DTYPE {dtype}, {heads} KV heads of {dim}; the layout has {layout.dtype}, {layout.n_kv_heads} of {layout.head_dim}")
+    _check(lib().gms_kv_append(_ref(pool), _ref(layout), _ref(args), _stream(stream)), "gms_kv_append")
+
+
+def kv_delta_args(*, q, k, v, out, src_table, dst_table=None, g=None, beta=None, cu_q=None, max_q: int = 1, past_lens=None, scale: float,
+                  unit_eps=None, workspace=None, status=None) -> KvDeltaArgs:
+    """gms_kv_delta_args from tensors: ``q`` and ``k`` [rows, key heads, dim], ``v`` and ``out`` [rows, heads, dim] with any strides and
+    a contiguous last dimension, ``g`` and ``beta`` float32 [rows, heads], tables int32 [sequences, blocks] (``dst_table`` None: in
+    place), ``unit_eps`` None: q and k as they are.  The result keeps the tensors alive."""
+    dst_table = src_table if dst_table is None else dst_table
+    dtype, rows, dim = _heads_dim("q, k, v and out are 16-bit [rows, heads, dim] of one type", (q, k, v, out))
+    if q.shape != k.shape or v.shape != out.shape or any(t is not None and tuple(t.shape) != tuple(v.shape[:2]) for t in (g, beta)):
+        raise ValueError("q and k, v and out must match, g and beta are [rows, heads]")
+    _float32(g, beta)
+    _int32(cu_q, past_lens, src_table, dst_table)
+    _word(status)
+    n_seq = src_table.shape[0]
+    if src_table.dim() != 2 or dst_table.dim() != 2 or dst_table.shape[0] != n_seq or cu_q is not None and cu_q.shape[0] != n_seq + 1 or (
+            past_lens is not None and past_lens.shape[0] != n_seq):
+        raise ValueError("tables, cu_q and past_lens disagree about the number of sequences")
+    (qt, qh), (kt, kh), (vt, vh), (ot, oh) = (_strides(t) for t in (q, k, v, out))
+
+    def row(t, width):
+        return 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(width, 1)
+
+    a = KvDeltaArgs(q=_dev(q), k=_dev(k), v=_dev(v), out=_dev(out), g=_dev(g), beta=_dev(beta), cu_q=_dev(cu_q), past_lens=_dev(past_lens),
+                    src_table=_dev(src_table), dst_table=_dev(dst_table), status=_dev(status), q_token_stride=qt, q_head_stride=qh,
+                    k_token_stride=kt, k_head_stride=kh, v_token_stride=vt, v_head_stride=vh, out_token_stride=ot, out_head_stride=oh,
+                    g_stride=row(g, v.shape[1]), beta_stride=row(beta, v.shape[1]), src_stride=row(src_table, src_table.shape[1]),
+                    dst_stride=row(dst_table, dst_table.shape[1]), n_seq=n_seq, n_key_heads=q.shape[1], total_q=rows, max_q=max_q, dtype=dtype,
+                    unit_qk=0 if unit_eps is None else 1, unit_eps=unit_eps or 0.0, scale=scale)
+    a._keep = (q, k, v, out, g, beta, cu_q, past_lens, src_table, dst_table, status)
+    a._made = (v.shape[1], dim, min(src_table.shape[1], dst_table.shape[1]))
+    if workspace is not None:
+        a.set_workspace(workspace)
+    return a
+
+
+def _fits_state(pool, state, args):
+    if pool is None or state is None or args is None or args._made is None:
+        return
+    heads, dim, blocks = args._made
+    per = pool.block_bytes // (4 * dim * dim)
+    if heads != state.n_heads or dim != state.head_dim or blocks * per < heads:
+        raise ValueError(f"{heads} heads of {dim} in rows of {blocks} blocks; the state has {state.n_heads} of {state.head_dim}, {per} a block")
+
+
+def gms_kv_delta_workspace(pool: KvPool, state: KvState, args: KvDeltaArgs) -> int:
+    v = C.c_uint64()
+    _check(lib().gms_kv_delta_workspace(_ref(pool), _ref(state), _ref(args), C.byref(v)), "gms_kv_delta_workspace")
+    return v.value
+
+
+def gms_kv_delta(pool: KvPool, state: KvState, args: KvDeltaArgs, stream=None):
+    _fits_state(pool, state, args)
+    _check(lib().gms_kv_delta(_ref(pool), _ref(state), _ref(args), _stream(stream)), "gms_kv_delta")
 
 
 def gms_host_image_alloc(nbytes: int):
