@@ -25,6 +25,7 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     ptx::grid_wait();
     ptx::grid_launch_dependents();
     const int first = delta_begin(a, s), rows = delta_rows(a, s);
+    if (delta_in_chunks(a, rows)) return;
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
@@ -142,7 +143,7 @@ int make_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_
         return GMS_ERR_ALIGN;
     if (t->n_seq && (t->src_stride < blocks || t->dst_stride < blocks || t->src_stride >> 40 || t->dst_stride >> 40)) return GMS_ERR_RANGE;
     if (t->total_q && ((t->g && t->g_stride < state->n_heads) || (t->beta && t->beta_stride < state->n_heads))) return GMS_ERR_RANGE;
-    if ((uint64_t)t->n_seq * state->n_heads > 1ull << 27) return GMS_ERR_RANGE;
+    if (((uint64_t)t->n_seq + t->total_q / kChunkRows) * state->n_heads > 1ull << 27) return GMS_ERR_RANGE;
     *a = {};
     a->q = static_cast<const uint8_t *>(t->q);
     a->k = static_cast<const uint8_t *>(t->k);
@@ -182,7 +183,8 @@ int make_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_
     return GMS_OK;
 }
 
-uint64_t delta_workspace(const DeltaArgs &, uint32_t) { return 0; }
+// Slots for every sequence's chunks, wherever its rows begin; 0: no sequence is long enough.
+uint64_t chunk_slots(const DeltaArgs &a) { return a.max_q > kMostByRow ? a.total_q / kChunkRows + a.n_seq : 0; }
 
 }  // namespace
 }  // namespace gms
@@ -194,7 +196,7 @@ int gms_kv_delta_workspace(const gms_kv_pool *pool, const gms_kv_state *state, c
     if (!nbytes) return GMS_ERR_NULL;
     gms::DeltaArgs a;
     const int rc = gms::make_delta(pool, state, args, &a);
-    if (rc == GMS_OK) *nbytes = gms::delta_workspace(a, state->head_dim);
+    if (rc == GMS_OK) *nbytes = gms::chunk_slots(a) * a.n_heads * sizeof(gms::ChunkWork);
     return rc;
 }
 
@@ -204,12 +206,18 @@ int gms_kv_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_k
     const int rc = gms::make_delta(pool, state, args, &a);
     if (rc != GMS_OK) return rc;
     if (a.n_seq == 0) return GMS_OK;
-    const uint64_t need = gms::delta_workspace(a, state->head_dim);
+    const uint64_t slots = gms::chunk_slots(a), need = slots * a.n_heads * sizeof(gms::ChunkWork);
     if (need && !args->workspace) return GMS_ERR_NULL;
     if (need > args->workspace_bytes) return GMS_ERR_RANGE;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool bf16 = args->dtype == GMS_DTYPE_BF16;
-    cudaError_t e;
+    cudaError_t e = cudaSuccess;
+    if (slots) {
+        a.chunks = static_cast<uint8_t *>(args->workspace);
+        a.n_slots = (uint32_t)slots;
+        e = gms::launch_delta_chunks(a, args->dtype, state->head_dim, s);
+        if (e != cudaSuccess) return gms::report_cuda_error(e);
+    }
     if (state->head_dim == 128)
         e = bf16 ? gms::launch_rows<__nv_bfloat16, 128>(a, s) : gms::launch_rows<__half, 128>(a, s);
     else

@@ -18,7 +18,23 @@ struct DeltaArgs {
     uint32_t n_seq, n_heads, group;      // group = n_heads / n_key_heads
     uint32_t total_q, max_q, unit_qk;
     float unit_eps, scale;
+    uint8_t *chunks;                     // workspace: ChunkWork [n_slots][n_heads]; null: no sequence is done in chunks
+    uint32_t n_slots;
 };
+
+// Sequences of more rows than this are done kChunkRows at a time.
+constexpr uint32_t kChunkRows = 64, kMostByRow = 24;
+
+// What the first of the two chunk kernels leaves for the second.
+struct alignas(256) ChunkWork {
+    uint8_t tile[3][kChunkRows * kChunkRows * 2];  // T in two terms, P; rows of 128 bytes, pieces swapped as `piece` says
+    float f[kChunkRows], w[kChunkRows], h[kChunkRows];
+    float gate[kChunkRows], beta[kChunkRows], rk[kChunkRows], rq[kChunkRows];  // for chunks that are done row by row
+    float all, t_unit, p_unit;                     // e^G of the chunk; f16: what the terms of T and P are multiples of
+    uint32_t by_row;
+};
+
+cudaError_t launch_delta_chunks(const DeltaArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ int delta_begin(const DeltaArgs &a, uint32_t s) { return a.cu_q ? min(max(a.cu_q[s], 0), (int)a.total_q) : (int)s; }
@@ -27,6 +43,9 @@ __device__ __forceinline__ int delta_rows(const DeltaArgs &a, uint32_t s)
     if (!a.cu_q) return 1;
     return min(max(min(a.cu_q[s + 1], (int)a.total_q) - delta_begin(a, s), 0), (int)a.max_q);
 }
+__device__ __forceinline__ bool delta_in_chunks(const DeltaArgs &a, int rows) { return a.chunks && rows > (int)kMostByRow; }
+// First slot of a sequence in the workspace.  A sequence of n rows has n / 64 + 1 slots at least, whatever comes before it.
+__device__ __forceinline__ uint32_t delta_slot(const DeltaArgs &a, uint32_t s) { return (uint32_t)delta_begin(a, s) / kChunkRows + s; }
 // Where a head's state lies; null: in a hole.
 template <int D>
 __device__ __forceinline__ float *delta_state(const DeltaArgs &a, const int32_t *table, uint64_t stride, uint32_t s, uint32_t h)
