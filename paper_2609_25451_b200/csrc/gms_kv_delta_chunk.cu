@@ -271,66 +271,89 @@ struct Stage {
     uint8_t k[kChunkRows * D * 2], q[kChunkRows * D * 2], v[kChunkRows * W * 32];
     ChunkWork w;
 };
+template <int D, int W>
+struct ChainSmem {
+    Stage<D, W> stage[2];
+    float4 swap[W][2][12][32];  // what the two warps of a slice send each other
+};
+constexpr uint32_t kFetchWarps = 2;
 
-// A warp has 16 value columns of a head's state, transposed, as accumulators of mma.sync (16 x D): what is an accumulator of one
-// product is, element for element, the first factor of the next, so nothing leaves the registers between the products and the
-// warps of a CTA (W of them, 16 W columns of one head) only share the operands that they read.  Chunks are fetched one ahead.
+// Two warps have 16 value columns of a head's state, half of its keys each, transposed, as accumulators of mma.sync (16 x D / 2):
+// what is an accumulator of one product is, element for element, the first factor of the next, so nothing leaves the registers
+// between the products but the halves of K S0 and Q S0, which the two warps send each other.  d is made by both (60 of a warp's 234
+// products), `out` of 32 rows by each.  W such slices share a chunk's operands, which two more warps fetch one chunk ahead.
 template <class T, int D, int W>
-__global__ void __launch_bounds__(W * 32) kv_delta_chain_kernel(const __grid_constant__ DeltaArgs a)
+__global__ void __launch_bounds__((2 * W + kFetchWarps) * 32) kv_delta_chain_kernel(const __grid_constant__ DeltaArgs a)
 {
     extern __shared__ __align__(16) uint8_t raw[];
-    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 8, CT = C / 8;
+    ChainSmem<D, W> &m = *reinterpret_cast<ChainSmem<D, W> *>(raw);
+    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, H = D / 2, NT = H / 8, CT = C / 8;
     constexpr bool kHalf = std::is_same<T, __half>::value;
-    using St = Stage<D, W>;
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kSlices = D / (16 * W);
-    const uint32_t slice = blockIdx.x % kSlices, h = blockIdx.x / kSlices % a.n_heads, s = blockIdx.x / kSlices / a.n_heads, kh = h / a.group;
-    const uint32_t col0 = slice * W * 16;  // of the CTA
+    const uint32_t part = blockIdx.x % kSlices, h = blockIdx.x / kSlices % a.n_heads, s = blockIdx.x / kSlices / a.n_heads, kh = h / a.group;
+    const uint32_t col0 = part * W * 16;  // of the CTA
     ptx::grid_launch_dependents();
     ptx::grid_wait();
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
     if (!delta_in_chunks(a, rows)) return;
+    const int chunks = (rows + C - 1) / C;
+    if (warp >= 2 * W) {  // the fetching warps
+        constexpr uint32_t kLanes = kFetchWarps * 32;
+        const uint32_t me = (warp - 2 * W) * 32 + lane;
+        const uint32_t slot = delta_slot(a, s);
+        for (int chunk = 0; chunk <= chunks; ++chunk) {
+            if (chunk < chunks) {
+                Stage<D, W> &st = m.stage[chunk & 1];
+                const int r0 = chunk * C;
+                const uint32_t kb = smem_u32(st.k), qb = smem_u32(st.q), vb = smem_u32(st.v);
+#pragma unroll 4
+                for (uint32_t i = me; i < (uint32_t)(C * P); i += kLanes) {
+                    const uint32_t r = i / P, c = i % P;
+                    const bool real = r0 + (int)r < rows;
+                    const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
+                    cp16(kb + piece<P>(r, c), a.k + row * a.k_token + kh * a.k_head + c * 16, real);
+                    cp16(qb + piece<P>(r, c), a.q + row * a.q_token + kh * a.q_head + c * 16, real);
+                }
+#pragma unroll 4
+                for (uint32_t i = me; i < (uint32_t)(C * VP); i += kLanes) {
+                    const uint32_t r = i / VP, c = i % VP;
+                    const bool real = r0 + (int)r < rows;
+                    const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
+                    cp16(vb + piece<VP>(r, c), a.v + row * a.v_token + h * a.v_head + col0 * 2 + c * 16, real);
+                }
+                const uint8_t *ws = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork);
+                const uint32_t wb = smem_u32(&st.w);
+#pragma unroll 4
+                for (uint32_t i = me; i < sizeof(ChunkWork) / 16; i += kLanes) cp16(wb + i * 16, ws + i * 16, true);
+                cp_commit();
+                cp_wait();
+            }
+            __syncthreads();  // chunk is here, and nobody reads the stage of the last one any more
+        }
+        return;
+    }
+    const uint32_t slice = warp / 2, half = warp & 1u;
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
-    if (a.status && tid == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+    if (a.status && threadIdx.x == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
     const uint32_t g = lane / 4, t2 = 2 * (lane & 3u);  // rows g and g + 8, columns 8 nt + t2 + {0, 1} of an accumulator
-    const uint32_t v0 = col0 + 16 * warp + g;
+    const uint32_t at0 = (half * H + t2) * D + col0 + 16 * slice + g;
+    const uint32_t b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;  // of a lane's address for two second factors
     float S[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[(uint64_t)(8 * nt + t2 + (e & 1)) * D + v0 + (e & 2) * 4] : 0.f;
-    const int chunks = (rows + C - 1) / C;
-    const uint32_t slot = delta_slot(a, s);
-    auto fetch = [&](int chunk) {
-        St &st = *reinterpret_cast<St *>(raw + (chunk & 1) * sizeof(St));
-        const int r0 = chunk * C;
-        for (uint32_t i = tid; i < (uint32_t)(C * P); i += W * 32) {
-            const uint32_t r = i / P, c = i % P;
-            const bool real = r0 + (int)r < rows;
-            const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
-            cp16(smem_u32(st.k) + piece<P>(r, c), a.k + row * a.k_token + kh * a.k_head + c * 16, real);
-            cp16(smem_u32(st.q) + piece<P>(r, c), a.q + row * a.q_token + kh * a.q_head + c * 16, real);
-        }
-        for (uint32_t i = tid; i < (uint32_t)(C * VP); i += W * 32) {
-            const uint32_t r = i / VP, c = i % VP;
-            const bool real = r0 + (int)r < rows;
-            const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
-            cp16(smem_u32(st.v) + piece<VP>(r, c), a.v + row * a.v_token + h * a.v_head + col0 * 2 + c * 16, real);
-        }
-        const uint8_t *ws = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork);
-        for (uint32_t i = tid; i < sizeof(ChunkWork) / 16; i += W * 32) cp16(smem_u32(&st.w) + i * 16, ws + i * 16, true);
-        cp_commit();
-    };
-    if (chunks) fetch(0);
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        cp_wait();
-        __syncthreads();  // the chunk is here, and nobody reads the stage of the last one any more
-        if (chunk + 1 < chunks) fetch(chunk + 1);
-        St &st = *reinterpret_cast<St *>(raw + (chunk & 1) * sizeof(St));
+        for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] : 0.f;
+    float4(*mine)[32] = m.swap[slice][half], (*other)[32] = m.swap[slice][half ^ 1u];
+    auto together = [&] { asm volatile("bar.sync %0, 64;" ::"r"(slice + 1) : "memory"); };
+    __syncthreads();
+#pragma unroll 1
+    for (int chunk = 0; chunk < chunks; ++chunk, __syncthreads()) {
+        Stage<D, W> &st = m.stage[chunk & 1];
         const int n = min(rows - chunk * C, C);
-        T *out = reinterpret_cast<T *>(a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head);
+        uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
         // the columns' values, transposed like everything else
         uint32_t V[CT][2];
         uint32_t odd = 0;
@@ -338,19 +361,21 @@ __global__ void __launch_bounds__(W * 32) kv_delta_chain_kernel(const __grid_con
 #pragma unroll
         for (int nt = 0; nt < CT; nt += 2) {
             uint32_t b[4];
-            ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * warp + (lane / 8 & 1u)), b);
+            ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * slice + b_piece), b);
             V[nt][0] = b[0], V[nt][1] = b[1], V[nt + 1][0] = b[2], V[nt + 1][1] = b[3];
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd |= ((b[e] & kOnes) == kOnes) | ((b[e] >> 16 & kOnes) == kOnes);
         }
         if (st.w.by_row || __any_sync(0xffffffffu, odd)) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
+#pragma unroll 1
             for (int r = 0; r < n; ++r) {
                 const float gate = st.w.gate[r], beta = st.w.beta[r], rk = st.w.rk[r], rq = st.w.rq[r];
                 float x[2] = {}, y[2] = {}, z = 0.f, kv[2 * NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, nt)) + t2, *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, nt)) + t2;
+                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, half * NT + nt)) + t2;
+                    const T *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, half * NT + nt)) + t2;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float k = to_f32(kp[e]) * rk, q = to_f32(qp[e]) * rq;
@@ -367,50 +392,47 @@ __global__ void __launch_bounds__(W * 32) kv_delta_chain_kernel(const __grid_con
 #pragma unroll
                     for (int e = 0; e < 2; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], o), y[e] += __shfl_xor_sync(0xffffffffu, y[e], o);
                 }
+                mine[2 * (r & 1)][lane] = make_float4(x[0], x[1], y[0], y[1]);
+                mine[2 * (r & 1) + 1][lane].x = z;
+                together();
+                const float4 u = other[2 * (r & 1)][lane];
+                x[0] += u.x, x[1] += u.y, y[0] += u.z, y[1] += u.w;
+                z += other[2 * (r & 1) + 1][lane].x;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t c = 16 * warp + g + 8 * e;
-                    const float v = to_f32(*reinterpret_cast<const T *>(st.v + piece<VP>(r, c / 8) + (c & 7u) * 2));
+                    const float v = to_f32(*reinterpret_cast<const T *>(st.v + piece<VP>(r, 2 * slice + e) + g * 2));
                     const float d = beta * (v - x[e]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) S[nt][2 * e] += kv[2 * nt] * d, S[nt][2 * e + 1] += kv[2 * nt + 1] * d;
-                    if ((lane & 3u) == 0) {
-                        T *op = reinterpret_cast<T *>(reinterpret_cast<uint8_t *>(out) + (uint64_t)r * a.o_token);
-                        op[col0 + c] = from_f32<T>(a.scale * (y[e] + z * d));
-                    }
+                    if (half == 0 && (lane & 3u) == 0)
+                        reinterpret_cast<T *>(out + (uint64_t)r * a.o_token)[g + 8 * e] = from_f32<T>(a.scale * (y[e] + z * d));
                 }
             }
             continue;
         }
-        // f16: each of the warp's columns is scaled by a power of two of its own
-        float su[2] = {1.f, 1.f}, si[2] = {1.f, 1.f};
-        if (kHalf) {
+        // f16: each of the columns is scaled by a power of two of its own, by both warps alike but for S
+        auto top_of = [](const float(*x)[4], int tiles, int e) {
+            float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) top = fmaxf(top, fmaxf(fabsf(S[nt][2 * e]), fabsf(S[nt][2 * e + 1])));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                su[e] = range_scale(top), si[e] = 1.f / su[e];
-            }
-        }
+            for (int nt = 0; nt < tiles; ++nt) top = fmaxf(top, fmaxf(fabsf(x[nt][2 * e]), fabsf(x[nt][2 * e + 1])));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        };
+        float su[2] = {1.f, 1.f};
+        if (kHalf) su[0] = range_scale(top_of(S, NT, 0)), su[1] = range_scale(top_of(S, NT, 1));
         // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
         float X[CT][4] = {}, Y[CT][4] = {};
 #pragma unroll
-        for (int kt = 0; kt < D / 16; ++kt) {
-            uint32_t hi[4], lo[4];
-            split2<T>(S[2 * kt][0] * su[0], S[2 * kt][1] * su[0], hi[0], lo[0]);
-            split2<T>(S[2 * kt][2] * su[1], S[2 * kt][3] * su[1], hi[1], lo[1]);
-            split2<T>(S[2 * kt + 1][0] * su[0], S[2 * kt + 1][1] * su[0], hi[2], lo[2]);
-            split2<T>(S[2 * kt + 1][2] * su[1], S[2 * kt + 1][3] * su[1], hi[3], lo[3]);
-            uint32_t b[CT][2];
+        for (int kt = 0; kt < H / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2];
 #pragma unroll
             for (int nt = 0; nt < CT; nt += 2) {
                 uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * kt + (lane / 8 & 1u)), x);
+                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, half * NT + 2 * kt + b_piece), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2<T>(S[2 * kt + e / 2][2 * (e & 1)] * su[e & 1], S[2 * kt + e / 2][2 * (e & 1) + 1] * su[e & 1], hi[e], lo[e]);
 #pragma unroll
             for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
 #pragma unroll
@@ -418,176 +440,173 @@ __global__ void __launch_bounds__(W * 32) kv_delta_chain_kernel(const __grid_con
 #pragma unroll
             for (int nt = 0; nt < CT; nt += 2) {
                 uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * kt + (lane / 8 & 1u)), x);
+                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + b_row, half * NT + 2 * kt + b_piece), x);
                 mma16816(Y[nt], hi, x[0], x[1], T());
                 mma16816(Y[nt + 1], hi, x[2], x[3], T());
             }
         }
+        if (kHalf) {
+            const float i0 = 1.f / su[0], i1 = 1.f / su[1];
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) {
+                X[nt][0] *= i0, X[nt][1] *= i0, X[nt][2] *= i1, X[nt][3] *= i1;
+                Y[nt][0] *= i0, Y[nt][1] *= i0, Y[nt][2] *= i1, Y[nt][3] *= i1;
+            }
+        }
+        // the other half of the keys: all of X, and Y for the 32 rows that this warp finishes
+        float O[CT / 2][4];
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) mine[nt][lane] = make_float4(X[nt][0], X[nt][1], X[nt][2], X[nt][3]);
+#pragma unroll
+        for (int nt = 0; nt < CT / 2; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[nt][e] = half ? Y[nt + CT / 2][e] : Y[nt][e];
+            mine[CT + nt][lane] = half ? make_float4(Y[nt][0], Y[nt][1], Y[nt][2], Y[nt][3])
+                                       : make_float4(Y[nt + CT / 2][0], Y[nt + CT / 2][1], Y[nt + CT / 2][2], Y[nt + CT / 2][3]);
+        }
+        together();
         // what the values differ by from what the state says: X <- V - f X
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
+            const float4 u = other[nt][lane];
             const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
-            X[nt][0] = to_f32(va[0]) - f.x * (X[nt][0] * si[0]);
-            X[nt][1] = to_f32(va[1]) - f.y * (X[nt][1] * si[0]);
-            X[nt][2] = to_f32(vb[0]) - f.x * (X[nt][2] * si[1]);
-            X[nt][3] = to_f32(vb[1]) - f.y * (X[nt][3] * si[1]);
+            X[nt][0] = to_f32(va[0]) - f.x * (X[nt][0] + u.x);
+            X[nt][1] = to_f32(va[1]) - f.y * (X[nt][1] + u.y);
+            X[nt][2] = to_f32(vb[0]) - f.x * (X[nt][2] + u.z);
+            X[nt][3] = to_f32(vb[1]) - f.y * (X[nt][3] + u.w);
         }
-        float xu[2] = {1.f, 1.f}, xi[2] = {1.f, 1.f};
-        if (kHalf) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < CT; ++nt) top = fmaxf(top, fmaxf(fabsf(X[nt][2 * e]), fabsf(X[nt][2 * e + 1])));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                xu[e] = range_scale(top), xi[e] = st.w.t_unit / xu[e];
-            }
-        }
+        float xu[2] = {1.f, 1.f};
+        if (kHalf) xu[0] = range_scale(top_of(X, CT, 0)), xu[1] = range_scale(top_of(X, CT, 1));
         // d = X T^T: two terms each (the product of the small ones left out); T's columns beyond a row's own are zero
         float d[CT][4] = {};
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4];
-            split2<T>(X[2 * kt][0] * xu[0], X[2 * kt][1] * xu[0], hi[0], lo[0]);
-            split2<T>(X[2 * kt][2] * xu[1], X[2 * kt][3] * xu[1], hi[1], lo[1]);
-            split2<T>(X[2 * kt + 1][0] * xu[0], X[2 * kt + 1][1] * xu[0], hi[2], lo[2]);
-            split2<T>(X[2 * kt + 1][2] * xu[1], X[2 * kt + 1][3] * xu[1], hi[3], lo[3]);
+            uint32_t hi[4], lo[4], b[CT][2];
 #pragma unroll
             for (int nt = 2 * kt; nt < CT; nt += 2) {
-                const uint32_t at = piece<8>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * kt + (lane / 8 & 1u));
-                uint32_t x[4], y[4];
-                ldmatrix_x4(smem_u32(st.w.tile[0]) + at, x);
-                ldmatrix_x4(smem_u32(st.w.tile[1]) + at, y);
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[0]) + piece<8>(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2<T>(X[2 * kt + e / 2][2 * (e & 1)] * xu[e & 1], X[2 * kt + e / 2][2 * (e & 1) + 1] * xu[e & 1], hi[e], lo[e]);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[1]) + piece<8>(8 * nt + b_row, 2 * kt + b_piece), x);
                 mma16816(d[nt], hi, x[0], x[1], T());
                 mma16816(d[nt + 1], hi, x[2], x[3], T());
-                mma16816(d[nt], lo, x[0], x[1], T());
-                mma16816(d[nt + 1], lo, x[2], x[3], T());
-                mma16816(d[nt], hi, y[0], y[1], T());
-                mma16816(d[nt + 1], hi, y[2], y[3], T());
             }
         }
         float du[2] = {1.f, 1.f}, di[2] = {1.f, 1.f};
         if (kHalf) {
+            const float i0 = st.w.t_unit / xu[0], i1 = st.w.t_unit / xu[1];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top = 0.f;
+            for (int nt = 0; nt < CT; ++nt) d[nt][0] *= i0, d[nt][1] *= i0, d[nt][2] *= i1, d[nt][3] *= i1;
 #pragma unroll
-                for (int nt = 0; nt < CT; ++nt) {
-                    d[nt][2 * e] *= xi[e], d[nt][2 * e + 1] *= xi[e];
-                    top = fmaxf(top, fmaxf(fabsf(d[nt][2 * e]), fabsf(d[nt][2 * e + 1])));
-                }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                du[e] = range_scale(top), di[e] = st.w.p_unit / du[e];
-            }
+            for (int e = 0; e < 2; ++e) du[e] = range_scale(top_of(d, CT, e)), di[e] = st.w.p_unit / du[e];
         }
-        // out = h Y + P d (one term each)
+        // out = h Y + P d for this warp's rows (one term each; f16: in units of P and d meanwhile)
 #pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
-            // (f16: in units of P and d)
-            const float u0 = kHalf ? si[0] / di[0] : 1.f, u1 = kHalf ? si[1] / di[1] : 1.f;
-            Y[nt][0] *= f.x * u0, Y[nt][1] *= f.y * u0, Y[nt][2] *= f.x * u1, Y[nt][3] *= f.y * u1;
+        for (int nt = 0; nt < CT / 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[half * (C / 2) + 8 * nt + t2]);
+            const float4 u = other[CT + nt][lane];
+            const float u0 = kHalf ? 1.f / di[0] : 1.f, u1 = kHalf ? 1.f / di[1] : 1.f;
+            O[nt][0] = (O[nt][0] + u.x) * f.x * u0, O[nt][1] = (O[nt][1] + u.y) * f.y * u0;
+            O[nt][2] = (O[nt][2] + u.z) * f.x * u1, O[nt][3] = (O[nt][3] + u.w) * f.y * u1;
         }
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            const uint32_t x[4] = {pack2(d[2 * kt][0] * du[0], d[2 * kt][1] * du[0], T()), pack2(d[2 * kt][2] * du[1], d[2 * kt][3] * du[1], T()),
-                                   pack2(d[2 * kt + 1][0] * du[0], d[2 * kt + 1][1] * du[0], T()),
-                                   pack2(d[2 * kt + 1][2] * du[1], d[2 * kt + 1][3] * du[1], T())};
+            if (half == 0 && kt >= C / 32) break;  // rows before the 32nd have nothing of d behind it
+            uint32_t x[4];
 #pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
+            for (int e = 0; e < 4; ++e) x[e] = pack2(d[2 * kt + e / 2][2 * (e & 1)] * du[e & 1], d[2 * kt + e / 2][2 * (e & 1) + 1] * du[e & 1], T());
+#pragma unroll
+            for (int nt = 0; nt < CT / 2; nt += 2) {
                 uint32_t b[4];
-                ldmatrix_x4(smem_u32(st.w.tile[2]) + piece<8>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * kt + (lane / 8 & 1u)), b);
-                mma16816(Y[nt], x, b[0], b[1], T());
-                mma16816(Y[nt + 1], x, b[2], b[3], T());
+                ldmatrix_x4(smem_u32(st.w.tile[2]) + piece<8>(half * (C / 2) + 8 * nt + b_row, 2 * kt + b_piece), b);
+                mma16816(O[nt], x, b[0], b[1], T());
+                mma16816(O[nt + 1], x, b[2], b[3], T());
             }
         }
-        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms' scale meanwhile)
-        const float all = st.w.all;
+        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
         float dw[2] = {1.f, 1.f};
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
             d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
         }
-        if (kHalf) {
+        if (kHalf) dw[0] = range_scale(top_of(d, CT, 0)), dw[1] = range_scale(top_of(d, CT, 1));
+        const float all0 = st.w.all * dw[0], all1 = st.w.all * dw[1];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < CT; ++nt) top = fmaxf(top, fmaxf(fabsf(d[nt][2 * e]), fabsf(d[nt][2 * e + 1])));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                dw[e] = range_scale(top);
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[nt][0] *= all * dw[0], S[nt][1] *= all * dw[0], S[nt][2] *= all * dw[1], S[nt][3] *= all * dw[1];
+        for (int nt = 0; nt < NT; ++nt) S[nt][0] *= all0, S[nt][1] *= all0, S[nt][2] *= all1, S[nt][3] *= all1;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4];
-            split2<T>(d[2 * kt][0] * dw[0], d[2 * kt][1] * dw[0], hi[0], lo[0]);
-            split2<T>(d[2 * kt][2] * dw[1], d[2 * kt][3] * dw[1], hi[1], lo[1]);
-            split2<T>(d[2 * kt + 1][0] * dw[0], d[2 * kt + 1][1] * dw[0], hi[2], lo[2]);
-            split2<T>(d[2 * kt + 1][2] * dw[1], d[2 * kt + 1][3] * dw[1], hi[3], lo[3]);
+            uint32_t hi[4], lo[4], b[NT][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 4) {
-                uint32_t x[4], y[4];
-                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), nt + lane / 16), x);
-                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), nt + 2 + lane / 16), y);
-                mma16816(S[nt], hi, x[0], x[1], T());
-                mma16816(S[nt + 1], hi, x[2], x[3], T());
-                mma16816(S[nt + 2], hi, y[0], y[1], T());
-                mma16816(S[nt + 3], hi, y[2], y[3], T());
-                mma16816(S[nt], lo, x[0], x[1], T());
-                mma16816(S[nt + 1], lo, x[2], x[3], T());
-                mma16816(S[nt + 2], lo, y[0], y[1], T());
-                mma16816(S[nt + 3], lo, y[2], y[3], T());
+            for (int nt = 0; nt < NT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), half * NT + nt + lane / 16), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2<T>(d[2 * kt + e / 2][2 * (e & 1)] * dw[e & 1], d[2 * kt + e / 2][2 * (e & 1) + 1] * dw[e & 1], hi[e], lo[e]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], lo, b[nt][0], b[nt][1], T());
         }
         if (kHalf) {
             const float u0 = 1.f / dw[0], u1 = 1.f / dw[1];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) S[nt][0] *= u0, S[nt][1] *= u0, S[nt][2] *= u1, S[nt][3] *= u1;
         }
-        // rows of 16 columns through the warp's own part of V's tile (its columns have been read)
-        __syncwarp();
+        // rows of 16 columns through the warp's own part of V's tile (both warps have read it)
 #pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const uint32_t lo = pack2(Y[nt][0] * di[0], Y[nt][1] * di[0], T()), hi = pack2(Y[nt][2] * di[1], Y[nt][3] * di[1], T());
-            const uint32_t at = smem_u32(st.v) + piece<VP>(8 * nt + (lane & 7u), 2 * warp + (lane / 8 & 1u));
-            asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(at), "r"(lo), "r"(hi) : "memory");
+        for (int nt = 0; nt < CT / 2; ++nt) {
+            const uint32_t x = pack2(O[nt][0] * di[0], O[nt][1] * di[0], T()), y = pack2(O[nt][2] * di[1], O[nt][3] * di[1], T());
+            const uint32_t at = smem_u32(st.v) + piece<VP>(half * (C / 2) + 8 * nt + (lane & 7u), 2 * slice + b_piece);
+            asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < C / 16; ++i) {
-            const int r = 16 * i + (int)lane / 2;
-            const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * warp + (lane & 1u)));
-            if (r < n)
-                *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(out) + (uint64_t)r * a.o_token + (col0 + 16 * warp) * 2 + (lane & 1u) * 16) = x;
+        for (int i = 0; i < C / 32; ++i) {
+            const uint32_t r = half * (C / 2) + 16 * i + lane / 2;
+            const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
+            if ((int)r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
         }
     }
     if (!to) return;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[(uint64_t)(8 * nt + t2 + (e & 1)) * D + v0 + (e & 2) * 4] = S[nt][e];
+        for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
+}
+
+template <class T, int D, int W>
+cudaError_t launch_chain(const DeltaArgs &a, cudaStream_t s)
+{
+    static std::atomic<uint64_t> done;
+    const cudaError_t e = allow_smem(kv_delta_chain_kernel<T, D, W>, sizeof(ChainSmem<D, W>), done);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(kv_delta_chain_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), (2 * W + kFetchWarps) * 32,
+                            sizeof(ChainSmem<D, W>), s, a);
 }
 
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
 {
-    constexpr int W = D == 128 ? 2 : 2;
-    static std::atomic<uint64_t> done[2];
-    cudaError_t e = allow_smem(kv_delta_prep_kernel<T, D>, sizeof(PrepSmem<D>), done[0]);
-    if (e == cudaSuccess) e = allow_smem(kv_delta_chain_kernel<T, D, W>, 2 * sizeof(Stage<D, W>), done[1]);
+    static std::atomic<uint64_t> done;
+    cudaError_t e = allow_smem(kv_delta_prep_kernel<T, D>, sizeof(PrepSmem<D>), done);
     if (e == cudaSuccess)
         e = launch_dependent(kv_delta_prep_kernel<T, D>, a.n_slots * (a.n_heads / a.group), kPrepThreads, sizeof(PrepSmem<D>), s, a);
-    if (e == cudaSuccess)
-        e = launch_dependent(kv_delta_chain_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), W * 32, 2 * sizeof(Stage<D, W>), s, a);
-    return e;
+    if (e != cudaSuccess) return e;
+    return (uint64_t)a.n_seq * a.n_heads * (D / 64) > 148 ? launch_chain<T, D, 4>(a, s) : launch_chain<T, D, 2>(a, s);
 }
 
 }  // namespace
