@@ -401,23 +401,79 @@ struct Stage {
     uint8_t k[kChunkRows * D * 2], q[kChunkRows * D * 2], v[kChunkRows * W * 32];
     ChunkWork w;
 };
-template <int D, int W>
-struct ChainSmem {
-    Stage<D, W> stage[2];
-    float4 swap[W][2][12][32];  // what the two warps of a slice send each other
+// What the four warps of a slice tell each other: first factors of products, a lane's part of 16 x 16 of them each.
+template <int D, bool UNITS>
+struct Shared {
+    uint4 s[D / 16][2][32];  // S, in two terms
+    uint4 x[4][2][32];       // V - f X of the 16 rows of each warp, in two terms
+    uint4 dw[4][2][32];      // w d, in two terms
+    uint4 d[4][32];
+    float2 s_unit[UNITS ? 4 : 1][32], x_unit[UNITS ? 4 : 1][32], dw_unit[UNITS ? 4 : 1][32], d_unit[UNITS ? 4 : 1][32];  // f16: powers of two
+    uint32_t odd[4];                                                                                                   // that terms are multiples of
 };
-constexpr uint32_t kFetchWarps = 2;
-
-// Two warps have 16 value columns of a head's state, half of its keys each, transposed, as accumulators of mma.sync (16 x D / 2):
-// what is an accumulator of one product is, element for element, the first factor of the next, so nothing leaves the registers
-// between the products but the halves of K S0 and Q S0, which the two warps send each other.  d is made by both (60 of a warp's 234
-// products), `out` of 32 rows by each.  W such slices share a chunk's operands, which two more warps fetch one chunk ahead.
 template <class T, int D, int W>
-__global__ void __launch_bounds__((2 * W + kFetchWarps) * 32) kv_delta_chain_kernel(const __grid_constant__ DeltaArgs a)
+struct ChainSmem {
+    static constexpr bool kUnits = std::is_same<T, __half>::value;
+    static constexpr int kStages = D == 64 || (W == 2 && !kUnits) ? 3 : 2;  // that fit
+    Stage<D, W> stage[kStages];
+    Shared<D, kUnits> shared[W];
+};
+constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32;
+
+// A tile of 64 rows, PR pieces each; rows from n on are zeros.  A lane keeps to one piece of the rows that it copies.
+template <int PR>
+__device__ __forceinline__ void fetch_rows(uint32_t tile, uint32_t me, const uint8_t *src, uint64_t stride, int n)
+{
+    constexpr uint32_t kStep = kFetchLanes / PR, N = kChunkRows / kStep;
+    const uint32_t c = me % PR, r0 = me / PR;
+    src += r0 * stride + c * 16;
+    if (n >= (int)kChunkRows) {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+            cp16(tile + piece<PR>(r0 + i * kStep, c), src, true);
+            src += kStep * stride;
+        }
+    } else {
+#pragma unroll 1
+        for (uint32_t r = r0; r < (uint32_t)kChunkRows; r += kStep) {
+            const bool real = (int)r < n;
+            cp16(tile + piece<PR>(r, c), real ? src : src - r * stride, real);
+            src += kStep * stride;
+        }
+    }
+}
+// Chunk `chunk` of a sequence, or nothing behind the last one; a group of copies either way.
+template <int D, int W>
+__device__ __forceinline__ void fetch_chunk(const DeltaArgs &a, Stage<D, W> &st, uint32_t me, int chunk, int rows, int first, uint32_t kh, uint32_t h,
+                                            uint32_t col0, uint32_t slot)
+{
+    const int n = rows - chunk * (int)kChunkRows;
+    if (n > 0) {
+        const uint64_t row = (uint64_t)(first + chunk * (int)kChunkRows);
+        const uint8_t *work = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork) + me * 16;
+        const uint32_t to = smem_u32(&st.w) + me * 16;
+        fetch_rows<D / 8>(smem_u32(st.k), me, a.k + row * a.k_token + kh * a.k_head, a.k_token, n);
+        fetch_rows<W * 2>(smem_u32(st.v), me, a.v + row * a.v_token + h * a.v_head + col0 * 2, a.v_token, n);
+        static_assert(sizeof(ChunkWork) % (16 * kFetchLanes) == 0, "");
+#pragma unroll
+        for (uint32_t i = 0; i < sizeof(ChunkWork) / (16 * kFetchLanes); ++i) cp16(to + i * 16 * kFetchLanes, work + i * 16 * kFetchLanes, true);
+        fetch_rows<D / 8>(smem_u32(st.q), me, a.q + row * a.q_token + kh * a.q_head, a.q_token, n);
+    }
+    cp_commit();
+}
+
+// Four warps have 16 value columns of a head's state, transposed, as accumulators of mma.sync: each the columns of D / 4 keys for
+// the state itself and 16 of the chunk's rows for everything that has rows.  What is an accumulator of one product is, element
+// for element, a first factor of the next: S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out.  Between those steps the warps
+// hand their parts round through shared memory, three exchanges a chunk.  W such slices share a chunk's operands, which two more
+// warps fetch one chunk ahead.
+template <class T, int D, int W>
+__global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_kernel(const __grid_constant__ DeltaArgs a)
 {
     extern __shared__ __align__(16) uint8_t raw[];
-    ChainSmem<D, W> &m = *reinterpret_cast<ChainSmem<D, W> *>(raw);
-    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, H = D / 2, NT = H / 8, CT = C / 8;
+    ChainSmem<T, D, W> &m = *reinterpret_cast<ChainSmem<T, D, W> *>(raw);
+    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 32, KQ = D / 64;  // tiles of 8 and of 16 keys that a warp has
+    constexpr int kStages = ChainSmem<T, D, W>::kStages;
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kSlices = D / (16 * W);
@@ -428,84 +484,87 @@ __global__ void __launch_bounds__((2 * W + kFetchWarps) * 32) kv_delta_chain_ker
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
     if (!delta_in_chunks(a, rows)) return;
     const int chunks = (rows + C - 1) / C;
-    if (warp >= 2 * W) {  // the fetching warps
-        constexpr uint32_t kLanes = kFetchWarps * 32;
-        const uint32_t me = (warp - 2 * W) * 32 + lane;
-        const uint32_t slot = delta_slot(a, s);
+    if (warp >= 4 * W) {  // the fetching warps
+        const uint32_t me = (warp - 4 * W) * 32 + lane, slot = delta_slot(a, s);
+        for (int i = 0; i < kStages - 1; ++i) fetch_chunk<D, W>(a, m.stage[i], me, i, rows, first, kh, h, col0, slot);
         for (int chunk = 0; chunk <= chunks; ++chunk) {
-            if (chunk < chunks) {
-                Stage<D, W> &st = m.stage[chunk & 1];
-                const int r0 = chunk * C;
-                const uint32_t kb = smem_u32(st.k), qb = smem_u32(st.q), vb = smem_u32(st.v);
-#pragma unroll 4
-                for (uint32_t i = me; i < (uint32_t)(C * P); i += kLanes) {
-                    const uint32_t r = i / P, c = i % P;
-                    const bool real = r0 + (int)r < rows;
-                    const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
-                    cp16(kb + piece<P>(r, c), a.k + row * a.k_token + kh * a.k_head + c * 16, real);
-                    cp16(qb + piece<P>(r, c), a.q + row * a.q_token + kh * a.q_head + c * 16, real);
-                }
-#pragma unroll 4
-                for (uint32_t i = me; i < (uint32_t)(C * VP); i += kLanes) {
-                    const uint32_t r = i / VP, c = i % VP;
-                    const bool real = r0 + (int)r < rows;
-                    const uint64_t row = (uint64_t)(first + (real ? r0 + (int)r : 0));
-                    cp16(vb + piece<VP>(r, c), a.v + row * a.v_token + h * a.v_head + col0 * 2 + c * 16, real);
-                }
-                const uint8_t *ws = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork);
-                const uint32_t wb = smem_u32(&st.w);
-#pragma unroll 4
-                for (uint32_t i = me; i < sizeof(ChunkWork) / 16; i += kLanes) cp16(wb + i * 16, ws + i * 16, true);
-                cp_commit();
-                cp_wait();
-            }
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
             __syncthreads();  // chunk is here, and nobody reads the stage of the last one any more
+            const int next = chunk + kStages - 1;
+            fetch_chunk<D, W>(a, m.stage[next % kStages], me, next, rows, first, kh, h, col0, slot);
         }
         return;
     }
-    const uint32_t slice = warp / 2, half = warp & 1u;
+    const uint32_t slice = warp / 4, mine = warp & 3u;
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
     if (a.status && threadIdx.x == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
     const uint32_t g = lane / 4, t2 = 2 * (lane & 3u);  // rows g and g + 8, columns 8 nt + t2 + {0, 1} of an accumulator
-    const uint32_t at0 = (half * H + t2) * D + col0 + 16 * slice + g;
-    const uint32_t b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;  // of a lane's address for two second factors
+    const uint32_t at0 = (mine * (D / 4) + t2) * D + col0 + 16 * slice + g;
+    const uint32_t row0 = 16 * mine, b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;  // of a lane's address for two second factors
     float S[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] : 0.f;
-    float4(*mine)[32] = m.swap[slice][half], (*other)[32] = m.swap[slice][half ^ 1u];
-    auto together = [&] { asm volatile("bar.sync %0, 64;" ::"r"(slice + 1) : "memory"); };
+    auto &sh = m.shared[slice];
+    auto together = [&] { asm volatile("bar.sync %0, 128;" ::"r"(slice + 1) : "memory"); };
+    // Two terms of the 16 x 16 tile in accumulators x and y; f16: rows scaled by a power of two of their own, which goes to `unit`.
+    auto top_of = [](const float *x, const float *y, int e) {
+        float top = fmaxf(fmaxf(fabsf(x[2 * e]), fabsf(x[2 * e + 1])), fmaxf(fabsf(y[2 * e]), fabsf(y[2 * e + 1])));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    };
+    auto put_terms = [&](uint4(*to)[32], const float *x, const float *y, float u0, float u1) {
+        uint4 hi, lo;
+        split2<T>(x[0] * u0, x[1] * u0, hi.x, lo.x);
+        split2<T>(x[2] * u1, x[3] * u1, hi.y, lo.y);
+        split2<T>(y[0] * u0, y[1] * u0, hi.z, lo.z);
+        split2<T>(y[2] * u1, y[3] * u1, hi.w, lo.w);
+        to[0][lane] = hi, to[1][lane] = lo;
+    };
     __syncthreads();
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk, __syncthreads()) {
-        Stage<D, W> &st = m.stage[chunk & 1];
+        Stage<D, W> &st = m.stage[chunk % kStages];
         const int n = min(rows - chunk * C, C);
         uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
-        // the columns' values, transposed like everything else
-        uint32_t V[CT][2];
-        uint32_t odd = 0;
-        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
+        float su[2] = {1.f, 1.f};
+        if (kHalf) {
 #pragma unroll
-        for (int nt = 0; nt < CT; nt += 2) {
-            uint32_t b[4];
-            ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * slice + b_piece), b);
-            V[nt][0] = b[0], V[nt][1] = b[1], V[nt + 1][0] = b[2], V[nt + 1][1] = b[3];
+            for (int e = 0; e < 2; ++e) {
+                float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= ((b[e] & kOnes) == kOnes) | ((b[e] >> 16 & kOnes) == kOnes);
+                for (int k = 0; k < KQ; ++k) top = fmaxf(top, top_of(S[2 * k], S[2 * k + 1], e));
+                su[e] = range_scale(top);
+            }
+            sh.s_unit[mine][lane] = make_float2(1.f / su[0], 1.f / su[1]);
         }
-        if (st.w.by_row || __any_sync(0xffffffffu, odd)) {
+#pragma unroll
+        for (int k = 0; k < KQ; ++k) put_terms(sh.s[mine * KQ + k], S[2 * k], S[2 * k + 1], su[0], su[1]);
+        // the rows' values, transposed like everything else
+        uint32_t V[4];
+        ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(row0 + b_row, 2 * slice + b_piece), V);
+        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
+        uint32_t odd = st.w.by_row;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= ((V[e] & kOnes) == kOnes) | ((V[e] >> 16 & kOnes) == kOnes);
+        odd = __any_sync(0xffffffffu, odd);
+        if (lane == 0) sh.odd[mine] = odd;
+        together();
+        if (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
+            float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(sh.s);  // [2][4][32], in the place of what is not needed
+            float(*zs)[4][32] = reinterpret_cast<float(*)[4][32]>(sh.dw);
 #pragma unroll 1
             for (int r = 0; r < n; ++r) {
                 const float gate = st.w.gate[r], beta = st.w.beta[r], rk = st.w.rk[r], rq = st.w.rq[r];
                 float x[2] = {}, y[2] = {}, z = 0.f, kv[2 * NT];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, half * NT + nt)) + t2;
-                    const T *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, half * NT + nt)) + t2;
+                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, mine * NT + nt)) + t2;
+                    const T *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, mine * NT + nt)) + t2;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const float k = to_f32(kp[e]) * rk, q = to_f32(qp[e]) * rq;
@@ -522,194 +581,185 @@ __global__ void __launch_bounds__((2 * W + kFetchWarps) * 32) kv_delta_chain_ker
 #pragma unroll
                     for (int e = 0; e < 2; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], o), y[e] += __shfl_xor_sync(0xffffffffu, y[e], o);
                 }
-                mine[2 * (r & 1)][lane] = make_float4(x[0], x[1], y[0], y[1]);
-                mine[2 * (r & 1) + 1][lane].x = z;
+                xy[r & 1][mine][lane] = make_float4(x[0], x[1], y[0], y[1]);
+                zs[r & 1][mine][lane] = z;
                 together();
-                const float4 u = other[2 * (r & 1)][lane];
-                x[0] += u.x, x[1] += u.y, y[0] += u.z, y[1] += u.w;
-                z += other[2 * (r & 1) + 1][lane].x;
+                x[0] = x[1] = y[0] = y[1] = z = 0.f;
+#pragma unroll
+                for (int o = 0; o < 4; ++o) {
+                    const float4 u = xy[r & 1][o][lane];
+                    x[0] += u.x, x[1] += u.y, y[0] += u.z, y[1] += u.w;
+                    z += zs[r & 1][o][lane];
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float v = to_f32(*reinterpret_cast<const T *>(st.v + piece<VP>(r, 2 * slice + e) + g * 2));
                     const float d = beta * (v - x[e]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) S[nt][2 * e] += kv[2 * nt] * d, S[nt][2 * e + 1] += kv[2 * nt + 1] * d;
-                    if (half == 0 && (lane & 3u) == 0)
+                    if (mine == 0 && (lane & 3u) == 0)
                         reinterpret_cast<T *>(out + (uint64_t)r * a.o_token)[g + 8 * e] = from_f32<T>(a.scale * (y[e] + z * d));
                 }
             }
             continue;
         }
-        // f16: each of the columns is scaled by a power of two of its own, by both warps alike but for S
-        auto top_of = [](const float(*x)[4], int tiles, int e) {
-            float top = 0.f;
+        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone), for the warp's rows
+        float X[2][4] = {}, Y[2][4] = {};
+        float2 unit = make_float2(1.f, 1.f);
+        // f16: accumulators go over to the unit of the next factors
+        auto change = [&](float(*x)[4], float2 now, float2 next) {
+            const float f0 = now.x / next.x, f1 = now.y / next.y;
 #pragma unroll
-            for (int nt = 0; nt < tiles; ++nt) top = fmaxf(top, fmaxf(fabsf(x[nt][2 * e]), fabsf(x[nt][2 * e + 1])));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
         };
-        float su[2] = {1.f, 1.f};
-        if (kHalf) su[0] = range_scale(top_of(S, NT, 0)), su[1] = range_scale(top_of(S, NT, 1));
-        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
-        float X[CT][4] = {}, Y[CT][4] = {};
 #pragma unroll
-        for (int kt = 0; kt < H / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[CT][2];
-#pragma unroll
-            for (int nt = 0; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, half * NT + 2 * kt + b_piece), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+        for (int kt = 0; kt < D / 16; ++kt) {
+            if (kHalf && kt % KQ == 0) {
+                const float2 next = sh.s_unit[kt / KQ][lane];
+                if (kt) change(X, unit, next), change(Y, unit, next);
+                unit = next;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) split2<T>(S[2 * kt + e / 2][2 * (e & 1)] * su[e & 1], S[2 * kt + e / 2][2 * (e & 1) + 1] * su[e & 1], hi[e], lo[e]);
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], lo, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + b_row, half * NT + 2 * kt + b_piece), x);
-                mma16816(Y[nt], hi, x[0], x[1], T());
-                mma16816(Y[nt + 1], hi, x[2], x[3], T());
-            }
+            const uint4 hi = sh.s[kt][0][lane], lo = sh.s[kt][1][lane];
+            uint32_t b[4], c[4];
+            ldmatrix_x4(smem_u32(st.k) + piece<P>(row0 + b_row, 2 * kt + b_piece), b);
+            ldmatrix_x4(smem_u32(st.q) + piece<P>(row0 + b_row, 2 * kt + b_piece), c);
+            mma16816(X[0], &hi.x, b[0], b[1], T());
+            mma16816(X[1], &hi.x, b[2], b[3], T());
+            mma16816(Y[0], &hi.x, c[0], c[1], T());
+            mma16816(Y[1], &hi.x, c[2], c[3], T());
+            mma16816(X[0], &lo.x, b[0], b[1], T());
+            mma16816(X[1], &lo.x, b[2], b[3], T());
         }
         if (kHalf) {
-            const float i0 = 1.f / su[0], i1 = 1.f / su[1];
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) {
-                X[nt][0] *= i0, X[nt][1] *= i0, X[nt][2] *= i1, X[nt][3] *= i1;
-                Y[nt][0] *= i0, Y[nt][1] *= i0, Y[nt][2] *= i1, Y[nt][3] *= i1;
-            }
+            const float2 one = make_float2(1.f, 1.f);
+            change(X, unit, one), change(Y, unit, one);
         }
-        // the other half of the keys: all of X, and Y for the 32 rows that this warp finishes
-        float O[CT / 2][4];
-#pragma unroll
-        for (int nt = 0; nt < CT; ++nt) mine[nt][lane] = make_float4(X[nt][0], X[nt][1], X[nt][2], X[nt][3]);
-#pragma unroll
-        for (int nt = 0; nt < CT / 2; ++nt) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) O[nt][e] = half ? Y[nt + CT / 2][e] : Y[nt][e];
-            mine[CT + nt][lane] = half ? make_float4(Y[nt][0], Y[nt][1], Y[nt][2], Y[nt][3])
-                                       : make_float4(Y[nt + CT / 2][0], Y[nt + CT / 2][1], Y[nt + CT / 2][2], Y[nt + CT / 2][3]);
-        }
-        together();
         // what the values differ by from what the state says: X <- V - f X
 #pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
-            const float4 u = other[nt][lane];
-            const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
-            X[nt][0] = to_f32(va[0]) - f.x * (X[nt][0] + u.x);
-            X[nt][1] = to_f32(va[1]) - f.y * (X[nt][1] + u.y);
-            X[nt][2] = to_f32(vb[0]) - f.x * (X[nt][2] + u.z);
-            X[nt][3] = to_f32(vb[1]) - f.y * (X[nt][3] + u.w);
+        for (int nt = 0; nt < 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[row0 + 8 * nt + t2]);
+            const T *va = reinterpret_cast<const T *>(&V[2 * nt]), *vb = reinterpret_cast<const T *>(&V[2 * nt + 1]);
+            X[nt][0] = to_f32(va[0]) - f.x * X[nt][0];
+            X[nt][1] = to_f32(va[1]) - f.y * X[nt][1];
+            X[nt][2] = to_f32(vb[0]) - f.x * X[nt][2];
+            X[nt][3] = to_f32(vb[1]) - f.y * X[nt][3];
         }
-        float xu[2] = {1.f, 1.f};
-        if (kHalf) xu[0] = range_scale(top_of(X, CT, 0)), xu[1] = range_scale(top_of(X, CT, 1));
-        // d = X T^T: two terms each (the product of the small ones left out); T's columns beyond a row's own are zero
-        float d[CT][4] = {};
-#pragma unroll
-        for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[CT][2];
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[0]) + piece<8>(8 * nt + b_row, 2 * kt + b_piece), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) split2<T>(X[2 * kt + e / 2][2 * (e & 1)] * xu[e & 1], X[2 * kt + e / 2][2 * (e & 1) + 1] * xu[e & 1], hi[e], lo[e]);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[1]) + piece<8>(8 * nt + b_row, 2 * kt + b_piece), x);
-                mma16816(d[nt], hi, x[0], x[1], T());
-                mma16816(d[nt + 1], hi, x[2], x[3], T());
-            }
-        }
-        float du[2] = {1.f, 1.f}, di[2] = {1.f, 1.f};
+        float u0 = 1.f, u1 = 1.f;
         if (kHalf) {
-            const float i0 = st.w.t_unit / xu[0], i1 = st.w.t_unit / xu[1];
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) d[nt][0] *= i0, d[nt][1] *= i0, d[nt][2] *= i1, d[nt][3] *= i1;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) du[e] = range_scale(top_of(d, CT, e)), di[e] = st.w.p_unit / du[e];
+            u0 = range_scale(top_of(X[0], X[1], 0)), u1 = range_scale(top_of(X[0], X[1], 1));
+            sh.x_unit[mine][lane] = make_float2(1.f / u0, 1.f / u1);
         }
-        // out = h Y + P d for this warp's rows (one term each; f16: in units of P and d meanwhile)
-#pragma unroll
-        for (int nt = 0; nt < CT / 2; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[half * (C / 2) + 8 * nt + t2]);
-            const float4 u = other[CT + nt][lane];
-            const float u0 = kHalf ? 1.f / di[0] : 1.f, u1 = kHalf ? 1.f / di[1] : 1.f;
-            O[nt][0] = (O[nt][0] + u.x) * f.x * u0, O[nt][1] = (O[nt][1] + u.y) * f.y * u0;
-            O[nt][2] = (O[nt][2] + u.z) * f.x * u1, O[nt][3] = (O[nt][3] + u.w) * f.y * u1;
-        }
+        put_terms(sh.x[mine], X[0], X[1], u0, u1);
+        together();
+        // d = X T^T: two terms each (the product of the small ones left out), from the rows up to the warp's own
+        float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            if (half == 0 && kt >= C / 32) break;  // rows before the 32nd have nothing of d behind it
-            uint32_t x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = pack2(d[2 * kt + e / 2][2 * (e & 1)] * du[e & 1], d[2 * kt + e / 2][2 * (e & 1) + 1] * du[e & 1], T());
-#pragma unroll
-            for (int nt = 0; nt < CT / 2; nt += 2) {
-                uint32_t b[4];
-                ldmatrix_x4(smem_u32(st.w.tile[2]) + piece<8>(half * (C / 2) + 8 * nt + b_row, 2 * kt + b_piece), b);
-                mma16816(O[nt], x, b[0], b[1], T());
-                mma16816(O[nt + 1], x, b[2], b[3], T());
+            if (kt > (int)mine) break;
+            if (kHalf) {
+                const float2 next = sh.x_unit[kt][lane];
+                if (kt) change(d, unit, next), change(dl, unit, next), change(dt, unit, next);
+                unit = next;
             }
+            const uint4 hi = sh.x[kt][0][lane], lo = sh.x[kt][1][lane];
+            uint32_t b[4], c[4];
+            ldmatrix_x4(smem_u32(st.w.tile[0]) + piece<8>(row0 + b_row, 2 * kt + b_piece), b);
+            ldmatrix_x4(smem_u32(st.w.tile[1]) + piece<8>(row0 + b_row, 2 * kt + b_piece), c);
+            mma16816(d[0], &hi.x, b[0], b[1], T());
+            mma16816(d[1], &hi.x, b[2], b[3], T());
+            mma16816(dl[0], &lo.x, b[0], b[1], T());
+            mma16816(dl[1], &lo.x, b[2], b[3], T());
+            mma16816(dt[0], &hi.x, c[0], c[1], T());
+            mma16816(dt[1], &hi.x, c[2], c[3], T());
         }
-        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
-        float dw[2] = {1.f, 1.f};
+        {
+            const float f0 = kHalf ? st.w.t_unit * unit.x : 1.f, f1 = kHalf ? st.w.t_unit * unit.y : 1.f;
 #pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[nt][e] = (d[nt][e] + (dl[nt][e] + dt[nt][e])) * (e & 2 ? f1 : f0);
+        }
+        if (kHalf) {
+            u0 = range_scale(top_of(d[0], d[1], 0)), u1 = range_scale(top_of(d[0], d[1], 1));
+            sh.d_unit[mine][lane] = make_float2(st.w.p_unit / u0, st.w.p_unit / u1);
+        }
+        sh.d[mine][lane] = make_uint4(pack2(d[0][0] * u0, d[0][1] * u0, T()), pack2(d[0][2] * u1, d[0][3] * u1, T()),
+                                      pack2(d[1][0] * u0, d[1][1] * u0, T()), pack2(d[1][2] * u1, d[1][3] * u1, T()));
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
             d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
         }
-        if (kHalf) dw[0] = range_scale(top_of(d, CT, 0)), dw[1] = range_scale(top_of(d, CT, 1));
-        const float all0 = st.w.all * dw[0], all1 = st.w.all * dw[1];
+        if (kHalf) {
+            u0 = range_scale(top_of(d[0], d[1], 0)), u1 = range_scale(top_of(d[0], d[1], 1));
+            sh.dw_unit[mine][lane] = make_float2(1.f / u0, 1.f / u1);
+        }
+        put_terms(sh.dw[mine], d[0], d[1], u0, u1);
+        together();
+        // S <- e^G S + (w d) K for the warp's keys
+        const float all = st.w.all;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[nt][0] *= all0, S[nt][1] *= all0, S[nt][2] *= all1, S[nt][3] *= all1;
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[nt][e] *= all;
+        unit = make_float2(1.f, 1.f);
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[NT][2];
+            if (kHalf) {
+                const float2 next = sh.dw_unit[kt][lane];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, next);
+                unit = next;
+            }
+            const uint4 hi = sh.dw[kt][0][lane], lo = sh.dw[kt][1][lane];
+            uint32_t b[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; nt += 2) {
                 uint32_t x[4];
-                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), half * NT + nt + lane / 16), x);
+                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + nt + lane / 16), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split2<T>(d[2 * kt + e / 2][2 * (e & 1)] * dw[e & 1], d[2 * kt + e / 2][2 * (e & 1) + 1] * dw[e & 1], hi[e], lo[e]);
+            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], &hi.x, b[nt][0], b[nt][1], T());
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], hi, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], lo, b[nt][0], b[nt][1], T());
+            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], &lo.x, b[nt][0], b[nt][1], T());
         }
         if (kHalf) {
-            const float u0 = 1.f / dw[0], u1 = 1.f / dw[1];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[nt][0] *= u0, S[nt][1] *= u0, S[nt][2] *= u1, S[nt][3] *= u1;
+            for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, make_float2(1.f, 1.f));
         }
-        // rows of 16 columns through the warp's own part of V's tile (both warps have read it)
+        // out = h Y + P d for the warp's rows (one term each)
 #pragma unroll
-        for (int nt = 0; nt < CT / 2; ++nt) {
-            const uint32_t x = pack2(O[nt][0] * di[0], O[nt][1] * di[0], T()), y = pack2(O[nt][2] * di[1], O[nt][3] * di[1], T());
-            const uint32_t at = smem_u32(st.v) + piece<VP>(half * (C / 2) + 8 * nt + (lane & 7u), 2 * slice + b_piece);
-            asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
+        for (int nt = 0; nt < 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[row0 + 8 * nt + t2]);
+            Y[nt][0] *= f.x, Y[nt][1] *= f.y, Y[nt][2] *= f.x, Y[nt][3] *= f.y;
         }
+        unit = make_float2(1.f, 1.f);
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kt > (int)mine) break;
+            if (kHalf) {
+                const float2 next = sh.d_unit[kt][lane];
+                change(Y, unit, next);
+                unit = next;
+            }
+            const uint4 x = sh.d[kt][lane];
+            uint32_t b[4];
+            ldmatrix_x4(smem_u32(st.w.tile[2]) + piece<8>(row0 + b_row, 2 * kt + b_piece), b);
+            mma16816(Y[0], &x.x, b[0], b[1], T());
+            mma16816(Y[1], &x.x, b[2], b[3], T());
+        }
+        if (kHalf) change(Y, unit, make_float2(1.f, 1.f));
+        // rows of 16 columns through the warp's own part of V's tile
+        const uint32_t y[4] = {pack2(Y[0][0], Y[0][1], T()), pack2(Y[0][2], Y[0][3], T()), pack2(Y[1][0], Y[1][1], T()), pack2(Y[1][2], Y[1][3], T())};
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                         smem_u32(st.v) + piece<VP>(row0 + b_row, 2 * slice + b_piece)),
+                     "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3])
+                     : "memory");
         __syncwarp();
-#pragma unroll
-        for (int i = 0; i < C / 32; ++i) {
-            const uint32_t r = half * (C / 2) + 16 * i + lane / 2;
-            const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
-            if ((int)r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
-        }
+        const uint32_t r = row0 + lane / 2;
+        const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
+        if ((int)r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
     }
     if (!to) return;
 #pragma unroll
@@ -721,11 +771,12 @@ __global__ void __launch_bounds__((2 * W + kFetchWarps) * 32) kv_delta_chain_ker
 template <class T, int D, int W>
 cudaError_t launch_chain(const DeltaArgs &a, cudaStream_t s)
 {
+    static_assert(sizeof(ChainSmem<T, D, W>) <= 232448, "");
     static std::atomic<uint64_t> done;
-    const cudaError_t e = allow_smem(kv_delta_chain_kernel<T, D, W>, sizeof(ChainSmem<D, W>), done);
+    const cudaError_t e = allow_smem(kv_delta_chain_kernel<T, D, W>, sizeof(ChainSmem<T, D, W>), done);
     if (e != cudaSuccess) return e;
-    return launch_dependent(kv_delta_chain_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), (2 * W + kFetchWarps) * 32,
-                            sizeof(ChainSmem<D, W>), s, a);
+    return launch_dependent(kv_delta_chain_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), (4 * W + kFetchWarps) * 32,
+                            sizeof(ChainSmem<T, D, W>), s, a);
 }
 
 template <class T, int D>
