@@ -51,117 +51,150 @@ __device__ __forceinline__ void load_weights(const AppendArgs &a, const void *w,
 }
 
 // D / 8 lanes hold a head's row, eight elements each: lane l the pairs of frequencies 4l .. 4l + 3 (both halves of them, so that
-// nothing is exchanged), the lanes behind those the elements that are not rotated.  A warp takes a run of a token's heads, 32 / (D / 8)
-// at a time, kUnroll loads in flight; angles are made once for all of them.
+// nothing is exchanged), the lanes behind those the elements that are not rotated.  A warp takes a run of a row's heads, first the
+// queries', then the keys', then the values', in batches of 4 x 32 / (D / 8), the next batch on its way while one is computed.
+// Cosines and sines are made once for all of them, by all lanes.  Bound by memory where there are many rows, by latency where there
+// are few (then a warp has one batch).
 constexpr uint32_t kAppendThreads = 256, kUnroll = 4;
 
 template <class T, int D>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(const __grid_constant__ AppendArgs a)
 {
-    constexpr uint32_t L = D / 8, G = 32 / L;  // lanes a row, rows at a time
+    constexpr uint32_t L = D / 8, G = 32 / L, B = G * kUnroll;  // lanes a row, rows at a time, rows a batch
     const uint32_t lane = threadIdx.x & 31u, l = lane % L, sub = lane / L;
     const uint64_t item = (uint64_t)blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
-    const uint32_t row = (uint32_t)(item / a.parts), part = (uint32_t)(item % a.parts);
+    const uint32_t row = a.parts == 1 ? (uint32_t)item : (uint32_t)(item / a.parts), part = a.parts == 1 ? 0 : (uint32_t)(item % a.parts);
     ptx::grid_wait();
     ptx::grid_launch_dependents();
-    if (row >= a.rows || (a.n_rows && (int64_t)row >= (int64_t)*a.n_rows)) return;
+    if (row >= a.rows) return;
     const uint32_t groups = a.rotary / 8;
-    const bool turned = l < groups;
+    const bool turned = l < groups, halves = a.pairs == GMS_PAIR_HALVES;
     uint32_t e0, e1;  // the lane's two runs of four elements
-    if (a.pairs == GMS_PAIR_NEIGHBOURS || !turned) e0 = 8 * l, e1 = e0 + 4;
-    else e0 = 4 * l, e1 = e0 + a.rotary / 2;
-    float c[4], s[4];
-    if (turned) {
+    if (halves && turned) e0 = 4 * l, e1 = e0 + a.rotary / 2;
+    else e0 = 8 * l, e1 = e0 + 4;
+    const uint32_t apart = (e1 - e0) * 2;
+    const uint8_t *q = a.q + row * a.q_token + e0 * 2, *k = a.k + row * a.k_token + e0 * 2, *v = a.v + row * a.v_token + e0 * 2;
+    // the part's heads: queries h0 .. q_end - 1 and so on, in the order q, k, v
+    const uint32_t heads = a.n_heads + 2 * a.n_kv, h0 = part * a.per_part, h1 = min(h0 + a.per_part, heads), k0 = a.n_heads, v0 = a.n_heads + a.n_kv;
+    auto kind_end = [&](uint32_t h) { return min(h1, h < k0 ? k0 : h < v0 ? v0 : heads); };  // of the kind that head h has
+    struct Batch {
+        uint2 x[kUnroll][2];
+    };
+    auto load = [&](uint32_t h, Batch &x) {
+        const uint32_t end = kind_end(h);
+        const uint8_t *p = h < k0 ? q : h < v0 ? k : v;
+        const uint64_t stride = h < k0 ? a.q_head : h < v0 ? a.k_head : a.v_head;
+        p += (h - (h < k0 ? 0 : h < v0 ? k0 : v0) + sub) * stride;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t j = 4 * l + i, axis = a.axes ? min((uint32_t)a.axes[j], a.n_axes - 1) : 0;
+        for (uint32_t u = 0; u < kUnroll; ++u) {
+            if (h + u * G + sub < end) {
+                x.x[u][0] = *reinterpret_cast<const uint2 *>(p);
+                x.x[u][1] = *reinterpret_cast<const uint2 *>(p + apart);
+            }
+            p += G * stride;
+        }
+    };
+    Batch x, y;
+    load(h0, x);
+    if (a.n_rows && (int64_t)row >= (int64_t)*a.n_rows) return;
+    uint64_t to = 0;
+    bool kept = false;
+    if (h1 > k0 && a.n_kv) {
+        const int64_t slot = a.slots[row];
+        kept = slot >= 0 && (slot >> a.block_shift) < (int64_t)a.n_blocks;
+        if (kept) to = (uint64_t)(slot >> a.block_shift) * a.block_stride + (uint64_t)(slot & ((1 << a.block_shift) - 1)) * a.token_stride + e0 * 2;
+    }
+    float c[4], s[4];
+    if (groups && h0 < v0) {  // the G lanes that need the same four angles make 4 / G each
+        constexpr uint32_t E = 4 / G;
+        float mc[E], ms[E];
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) {
+            const uint32_t j = min(4 * l + sub * E + i, a.rotary / 2 - 1), axis = a.axes ? min((uint32_t)a.axes[j], a.n_axes - 1) : 0;
             // in turns: what is left of them after the whole ones is exact enough in 32 bits, the product before is not
             const double turns = (double)a.positions[axis * a.positions_stride + row] * (double)a.inv_freq[j] * 0.15915494309189533577;
             float sn, cs;
             sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-            c[i] = cs * a.rope_scale;
-            s[i] = sn * a.rope_scale;
-        }
-    }
-    const uint32_t heads = a.n_heads + 2 * a.n_kv, h0 = part * a.per_part, h1 = min(h0 + a.per_part, heads);
-    float wq[8], wk[8];
-    if (a.q_weight && h0 < a.n_heads) load_weights(a, a.q_weight, e0, wq), load_weights(a, a.q_weight, e1, wq + 4);
-    if (a.k_weight && h0 < a.n_heads + a.n_kv && h1 > a.n_heads) load_weights(a, a.k_weight, e0, wk), load_weights(a, a.k_weight, e1, wk + 4);
-    uint64_t to = 0;
-    bool kept = false;
-    if (h1 > a.n_heads && a.n_kv) {
-        const int64_t slot = a.slots[row];
-        kept = slot >= 0 && (slot >> a.block_shift) < (int64_t)a.n_blocks;
-        if (kept) to = (uint64_t)(slot >> a.block_shift) * a.block_stride + (uint64_t)(slot & ((1 << a.block_shift) - 1)) * a.token_stride;
-    }
-    for (uint32_t h = h0; h < h1; h += G * kUnroll) {
-        uint2 x[kUnroll][2];
-#pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u) {
-            const uint32_t i = h + u * G + sub;
-            if (i >= h1) continue;
-            const uint8_t *p = i < a.n_heads ? a.q + row * a.q_token + i * a.q_head
-                               : i < a.n_heads + a.n_kv ? a.k + row * a.k_token + (i - a.n_heads) * a.k_head
-                                                        : a.v + row * a.v_token + (i - a.n_heads - a.n_kv) * a.v_head;
-            x[u][0] = *reinterpret_cast<const uint2 *>(p + e0 * 2);
-            x[u][1] = *reinterpret_cast<const uint2 *>(p + e1 * 2);
+            mc[i] = cs * a.rope_scale;
+            ms[i] = sn * a.rope_scale;
         }
 #pragma unroll
-        for (uint32_t u = 0; u < kUnroll; ++u) {
-            const uint32_t i = h + u * G + sub;
-            const bool in = i < h1, is_q = i < a.n_heads, is_v = i >= a.n_heads + a.n_kv;
-            uint8_t *p = nullptr;
-            if (in && is_q) p = a.q_out + row * a.o_token + i * a.o_head;
-            else if (in && kept) p = is_v ? a.v_base + to + (uint64_t)(i - a.n_heads - a.n_kv) * a.head_stride
-                                          : a.k_base + to + (uint64_t)(i - a.n_heads) * a.head_stride;
-            if (__any_sync(0xffffffffu, in && !is_v)) {
+        for (uint32_t i = 0; i < 4; ++i) {
+            c[i] = __shfl_sync(0xffffffffu, mc[i % E], l + i / E * L);
+            s[i] = __shfl_sync(0xffffffffu, ms[i % E], l + i / E * L);
+        }
+    }
+    for (uint32_t h = h0; h < h1;) {
+        const uint32_t end = kind_end(h), next = min(h + B, end);
+        if (next < h1) load(next, y);
+        const bool is_q = h < k0, is_v = h >= v0;
+        if (!is_v) {
+            const void *weight = is_q ? a.q_weight : a.k_weight;
+            float w[8];
+            if (weight) load_weights(a, weight, e0, w), load_weights(a, weight, e1, w + 4);
+#pragma unroll
+            for (uint32_t u = 0; u < kUnroll; ++u) {
+                if (h + u * G >= end) break;
                 float f[8];
-                unpack4<T>(x[u][0], f);
-                unpack4<T>(x[u][1], f + 4);
-                float sum = 0.f;
+                unpack4<T>(x.x[u][0], f);
+                unpack4<T>(x.x[u][1], f + 4);
+                if (weight) {
+                    float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += f[e] * f[e];
+                    for (int e = 0; e < 8; ++e) sum += f[e] * f[e];
 #pragma unroll
-                for (uint32_t o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const bool normed = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
-                if (normed) {
+                    for (uint32_t o = L / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                     const float r = rsqrtf(sum * (1.f / D) + a.eps);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] *= r * (is_q ? wq[e] : wk[e]);
+                    for (int e = 0; e < 8; ++e) f[e] *= r * w[e];
                 }
                 if (turned) {
-                    if (a.pairs == GMS_PAIR_NEIGHBOURS) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x0 = f[2 * e], x1 = f[2 * e + 1];
-                            f[2 * e] = x0 * c[e] - x1 * s[e];
-                            f[2 * e + 1] = x1 * c[e] + x0 * s[e];
-                        }
-                    } else {
+                    if (halves) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float x0 = f[e], x1 = f[e + 4];
                             f[e] = x0 * c[e] - x1 * s[e];
                             f[e + 4] = x1 * c[e] + x0 * s[e];
                         }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x0 = f[2 * e], x1 = f[2 * e + 1];
+                            f[2 * e] = x0 * c[e] - x1 * s[e];
+                            f[2 * e + 1] = x1 * c[e] + x0 * s[e];
+                        }
                     }
                 }
-                if (!is_v) x[u][0] = pack4<T>(f), x[u][1] = pack4<T>(f + 4);
-            }
-            if (p) {
-                *reinterpret_cast<uint2 *>(p + e0 * 2) = x[u][0];
-                *reinterpret_cast<uint2 *>(p + e1 * 2) = x[u][1];
+                x.x[u][0] = pack4<T>(f), x.x[u][1] = pack4<T>(f + 4);
             }
         }
+        if (is_q || kept) {
+            const uint64_t stride = is_q ? a.o_head : a.head_stride;
+            uint8_t *p = is_q ? a.q_out + row * a.o_token + e0 * 2 : (is_v ? a.v_base : a.k_base) + to;
+            p += (h - (is_q ? 0 : is_v ? v0 : k0) + sub) * stride;
+#pragma unroll
+            for (uint32_t u = 0; u < kUnroll; ++u) {
+                if (h + u * G + sub < end) {
+                    *reinterpret_cast<uint2 *>(p) = x.x[u][0];
+                    *reinterpret_cast<uint2 *>(p + apart) = x.x[u][1];
+                }
+                p += G * stride;
+            }
+        }
+        x = y;
+        h = next;
     }
 }
 
 template <class T>
 cudaError_t launch_append(AppendArgs &a, uint32_t dim, cudaStream_t s)
 {
-    const uint32_t heads = a.n_heads + 2 * a.n_kv, at_once = (dim == 128 ? 2 : 4) * kUnroll;
-    a.parts = (heads + at_once - 1) / at_once;
-    a.per_part = at_once;
+    const uint32_t heads = a.n_heads + 2 * a.n_kv, batch = (dim == 128 ? 2 : 4) * kUnroll;
+    // A warp a row where that fills the GPU; with fewer rows they are cut, down to a batch a warp.
+    const uint64_t fill = 148 * 24, batches = (heads + batch - 1) / batch;
+    const uint64_t want = a.rows >= fill ? 1 : (fill + a.rows - 1) / a.rows, cuts = want < batches ? want : batches;
+    a.per_part = (uint32_t)((batches + cuts - 1) / cuts) * batch;
+    a.parts = (heads + a.per_part - 1) / a.per_part;
     const uint64_t warps = (uint64_t)a.rows * a.parts, grid = (warps + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
     if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
     return dim == 128 ? launch_dependent(kv_append_kernel<T, 128>, (uint32_t)grid, kAppendThreads, 0, s, a)

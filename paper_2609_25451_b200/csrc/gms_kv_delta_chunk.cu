@@ -32,6 +32,13 @@ __device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c)
     return (r * P + (P >= 8 ? c ^ (r & 7u) : c ^ ((r * P / 8) & (P - 1u)))) * 16;
 }
 
+// The same in a lower triangle's blocks of 16 x 16 16-bit numbers: piece c (of the 8 of a whole row), c / 2 <= r / 16.
+__device__ __forceinline__ uint32_t block_piece(uint32_t r, uint32_t c)
+{
+    const uint32_t b = r / 16;
+    return (b * (b + 1) / 2 + c / 2) * 512 + (r % 16 * 2 + ((c ^ (r / 4)) & 1u)) * 16;
+}
+
 // x = hi + lo with both of type T (2^-17 relative in bf16, the rest of f16's range aside).
 template <class T>
 __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo)
@@ -48,6 +55,9 @@ __device__ __forceinline__ float range_scale(float top)
     const int e = (int)(__float_as_uint(top) >> 23 & 255u) - 127;  // 2^e <= top
     return __uint_as_float((uint32_t)(127 + min(max(11 - e, -30), 30)) << 23);
 }
+
+// 1 / u for a power of two.
+__device__ __forceinline__ float flipped(float u) { return __uint_as_float(0x7f000000u - __float_as_uint(u)); }
 
 // Which sequence and which of its chunks slot `id` stands for; false: none.
 __device__ __forceinline__ bool find_chunk(const DeltaArgs &a, uint32_t id, uint32_t &s, uint32_t &chunk)
@@ -73,7 +83,7 @@ struct PrepSmem {
         };
         struct {
             float a[kChunkRows][kRowPad], t[kChunkRows][kRowPad];  // A and the inverse of I + A, below their diagonals' 16 x 16 blocks
-            uint8_t p[kChunkRows * kChunkRows * 2];
+            uint8_t p[sizeof(ChunkWork::tile[0])];
         };
     };
     double sum[kPrepHeads][kChunkRows];  // G / ln 2
@@ -298,13 +308,14 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
             if (lane == 0) m.top[0][warp] = top;
             __syncthreads();
             ps = range_scale(fmaxf(fmaxf(m.top[0][0], m.top[0][1]), fmaxf(m.top[0][2], m.top[0][3])));
-            if (tid == 0) work->p_unit = 1.f / ps;
+            if (tid == 0) work->p_unit = flipped(ps);
         }
 #pragma unroll
         for (int nt = 0; nt < C / 8; ++nt) {
+            if (nt > 2 * (int)warp + 1) break;
             const uint32_t i = 16 * warp + g;
-            *reinterpret_cast<uint32_t *>(m.p + piece<8>(i, nt) + 2 * t2) = pack2(pv[nt][0] * ps, pv[nt][1] * ps, T());
-            *reinterpret_cast<uint32_t *>(m.p + piece<8>(i + 8, nt) + 2 * t2) = pack2(pv[nt][2] * ps, pv[nt][3] * ps, T());
+            *reinterpret_cast<uint32_t *>(m.p + block_piece(i, nt) + 2 * t2) = pack2(pv[nt][0] * ps, pv[nt][1] * ps, T());
+            *reinterpret_cast<uint32_t *>(m.p + block_piece(i + 8, nt) + 2 * t2) = pack2(pv[nt][2] * ps, pv[nt][3] * ps, T());
         }
         __syncwarp();
         if (lane < 16) {  // the warp's own diagonal block
@@ -372,7 +383,7 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
             if (lane == 0) m.top[1][warp] = most;
             __syncthreads();
             ts = range_scale(fmaxf(fmaxf(m.top[1][0], m.top[1][1]), fmaxf(m.top[1][2], m.top[1][3])));
-            if (tid == 0) work->t_unit = 1.f / ts;
+            if (tid == 0) work->t_unit = flipped(ts);
         }
 #pragma unroll
         for (uint32_t k = 0; k < 3; ++k) {
@@ -385,8 +396,8 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
             split2<T>(x[k][2] * ts, x[k][3] * ts, hi.y, lo.y);
             split2<T>(x[k][4] * ts, x[k][5] * ts, hi.z, lo.z);
             split2<T>(x[k][6] * ts, x[k][7] * ts, hi.w, lo.w);
-            *reinterpret_cast<uint4 *>(work->tile[0] + piece<8>(i, c)) = hi;
-            *reinterpret_cast<uint4 *>(work->tile[1] + piece<8>(i, c)) = lo;
+            *reinterpret_cast<uint4 *>(work->tile[0] + block_piece(i, c)) = hi;
+            *reinterpret_cast<uint4 *>(work->tile[1] + block_piece(i, c)) = lo;
         }
         for (uint32_t i = tid; i < sizeof(m.p) / 16; i += kPrepThreads)
             reinterpret_cast<uint4 *>(work->tile[2])[i] = reinterpret_cast<const uint4 *>(m.p)[i];
@@ -404,19 +415,20 @@ struct Stage {
 // What the four warps of a slice tell each other: first factors of products, a lane's part of 16 x 16 of them each.
 template <int D, bool UNITS>
 struct Shared {
-    uint4 s[D / 16][2][32];  // S, in two terms
-    uint4 x[4][2][32];       // V - f X of the 16 rows of each warp, in two terms
-    uint4 dw[4][2][32];      // w d, in two terms
+    uint4 s_hi[2][D / 16][32], s_lo[D / 16][32];  // S, in two terms; the first of this chunk and of the next
+    uint4 x[4][2][32];                            // V - f X of the 16 rows of each warp, in two terms
+    uint4 dw[4][2][32];                           // w d, in two terms
     uint4 d[4][32];
-    float2 s_unit[UNITS ? 4 : 1][32], x_unit[UNITS ? 4 : 1][32], dw_unit[UNITS ? 4 : 1][32], d_unit[UNITS ? 4 : 1][32];  // f16: powers of two
-    uint32_t odd[4];                                                                                                   // that terms are multiples of
+    float2 s_unit[2][UNITS ? 4 : 1][32], x_unit[UNITS ? 4 : 1][32], dw_unit[UNITS ? 4 : 1][32], d_unit[UNITS ? 4 : 1][32];  // f16: powers of
+    uint32_t odd[4];                                                                                        // two that terms are multiples of
 };
 template <class T, int D, int W>
 struct ChainSmem {
     static constexpr bool kUnits = std::is_same<T, __half>::value;
-    static constexpr int kStages = D == 64 || (W == 2 && !kUnits) ? 3 : 2;  // that fit
+    static constexpr int kStages = D == 64 || W == 2 ? 3 : 2;  // that fit
     Stage<D, W> stage[kStages];
     Shared<D, kUnits> shared[W];
+    uint64_t full[kStages], empty[kStages];
 };
 constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32;
 
@@ -442,24 +454,22 @@ __device__ __forceinline__ void fetch_rows(uint32_t tile, uint32_t me, const uin
         }
     }
 }
-// Chunk `chunk` of a sequence, or nothing behind the last one; a group of copies either way.
+// Chunk `chunk` of a sequence; `full` is told when it has landed.
 template <int D, int W>
 __device__ __forceinline__ void fetch_chunk(const DeltaArgs &a, Stage<D, W> &st, uint32_t me, int chunk, int rows, int first, uint32_t kh, uint32_t h,
-                                            uint32_t col0, uint32_t slot)
+                                            uint32_t col0, uint32_t slot, uint32_t full)
 {
     const int n = rows - chunk * (int)kChunkRows;
-    if (n > 0) {
-        const uint64_t row = (uint64_t)(first + chunk * (int)kChunkRows);
-        const uint8_t *work = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork) + me * 16;
-        const uint32_t to = smem_u32(&st.w) + me * 16;
-        fetch_rows<D / 8>(smem_u32(st.k), me, a.k + row * a.k_token + kh * a.k_head, a.k_token, n);
-        fetch_rows<W * 2>(smem_u32(st.v), me, a.v + row * a.v_token + h * a.v_head + col0 * 2, a.v_token, n);
-        static_assert(sizeof(ChunkWork) % (16 * kFetchLanes) == 0, "");
+    const uint64_t row = (uint64_t)(first + chunk * (int)kChunkRows);
+    const uint8_t *work = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork) + me * 16;
+    const uint32_t to = smem_u32(&st.w) + me * 16;
+    fetch_rows<D / 8>(smem_u32(st.k), me, a.k + row * a.k_token + kh * a.k_head, a.k_token, n);
+    fetch_rows<W * 2>(smem_u32(st.v), me, a.v + row * a.v_token + h * a.v_head + col0 * 2, a.v_token, n);
+    static_assert(sizeof(ChunkWork) % (16 * kFetchLanes) == 0, "");
 #pragma unroll
-        for (uint32_t i = 0; i < sizeof(ChunkWork) / (16 * kFetchLanes); ++i) cp16(to + i * 16 * kFetchLanes, work + i * 16 * kFetchLanes, true);
-        fetch_rows<D / 8>(smem_u32(st.q), me, a.q + row * a.q_token + kh * a.q_head, a.q_token, n);
-    }
-    cp_commit();
+    for (uint32_t i = 0; i < sizeof(ChunkWork) / (16 * kFetchLanes); ++i) cp16(to + i * 16 * kFetchLanes, work + i * 16 * kFetchLanes, true);
+    fetch_rows<D / 8>(smem_u32(st.q), me, a.q + row * a.q_token + kh * a.q_head, a.q_token, n);
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
 }
 
 // Four warps have 16 value columns of a head's state, transposed, as accumulators of mma.sync: each the columns of D / 4 keys for
@@ -484,18 +494,33 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
     if (!delta_in_chunks(a, rows)) return;
     const int chunks = (rows + C - 1) / C;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            ptx::mbar_init(smem_u32(&m.full[i]), kFetchLanes);
+            ptx::mbar_init(smem_u32(&m.empty[i]), 4 * W);
+        }
+        ptx::fence_mbar_init();
+    }
+    __syncthreads();
+    // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
+    bool late = false;
+    auto wait = [&](uint64_t *bar, int use) {
+        if (late || ptx::mbar_wait(smem_u32(bar), (uint32_t)(use & 1))) return;
+        late = true;
+        if (a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+    };
     if (warp >= 4 * W) {  // the fetching warps
         const uint32_t me = (warp - 4 * W) * 32 + lane, slot = delta_slot(a, s);
-        for (int i = 0; i < kStages - 1; ++i) fetch_chunk<D, W>(a, m.stage[i], me, i, rows, first, kh, h, col0, slot);
-        for (int chunk = 0; chunk <= chunks; ++chunk) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-            __syncthreads();  // chunk is here, and nobody reads the stage of the last one any more
-            const int next = chunk + kStages - 1;
-            fetch_chunk<D, W>(a, m.stage[next % kStages], me, next, rows, first, kh, h, col0, slot);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int i = chunk % kStages;
+            if (chunk >= kStages) wait(&m.empty[i], chunk / kStages - 1);
+            fetch_chunk<D, W>(a, m.stage[i], me, chunk, rows, first, kh, h, col0, slot, smem_u32(&m.full[i]));
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         return;
     }
-    const uint32_t slice = warp / 4, mine = warp & 3u;
+    // (the last rows have most to do: of two slices they go to different quarters of the SM)
+    const uint32_t slice = warp / 4, mine = (warp & 3u) ^ (slice & 1u ? 3u : 0u);
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
@@ -516,18 +541,24 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     };
-    auto put_terms = [&](uint4(*to)[32], const float *x, const float *y, float u0, float u1) {
+    auto put_terms = [&](uint4 *to_hi, uint4 *to_lo, const float *x, const float *y, float u0, float u1) {
         uint4 hi, lo;
         split2<T>(x[0] * u0, x[1] * u0, hi.x, lo.x);
         split2<T>(x[2] * u1, x[3] * u1, hi.y, lo.y);
         split2<T>(y[0] * u0, y[1] * u0, hi.z, lo.z);
         split2<T>(y[2] * u1, y[3] * u1, hi.w, lo.w);
-        to[0][lane] = hi, to[1][lane] = lo;
+        to_hi[lane] = hi, to_lo[lane] = lo;
     };
-    __syncthreads();
 #pragma unroll 1
-    for (int chunk = 0; chunk < chunks; ++chunk, __syncthreads()) {
-        Stage<D, W> &st = m.stage[chunk % kStages];
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int stage = chunk % kStages;
+        Stage<D, W> &st = m.stage[stage];
+        auto done = [&] {
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(smem_u32(&m.empty[stage]));
+        };
+        wait(&m.full[stage], chunk / kStages);
+        const uint32_t turn = chunk & 1;
         const int n = min(rows - chunk * C, C);
         uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
         float su[2] = {1.f, 1.f};
@@ -539,10 +570,10 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
                 for (int k = 0; k < KQ; ++k) top = fmaxf(top, top_of(S[2 * k], S[2 * k + 1], e));
                 su[e] = range_scale(top);
             }
-            sh.s_unit[mine][lane] = make_float2(1.f / su[0], 1.f / su[1]);
+            sh.s_unit[turn][mine][lane] = make_float2(flipped(su[0]), flipped(su[1]));
         }
 #pragma unroll
-        for (int k = 0; k < KQ; ++k) put_terms(sh.s[mine * KQ + k], S[2 * k], S[2 * k + 1], su[0], su[1]);
+        for (int k = 0; k < KQ; ++k) put_terms(sh.s_hi[turn][mine * KQ + k], sh.s_lo[mine * KQ + k], S[2 * k], S[2 * k + 1], su[0], su[1]);
         // the rows' values, transposed like everything else
         uint32_t V[4];
         ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(row0 + b_row, 2 * slice + b_piece), V);
@@ -552,10 +583,13 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         for (int e = 0; e < 4; ++e) odd |= ((V[e] & kOnes) == kOnes) | ((V[e] >> 16 & kOnes) == kOnes);
         odd = __any_sync(0xffffffffu, odd);
         if (lane == 0) sh.odd[mine] = odd;
+        uint32_t kb[D / 16][4];  // (what needs no news from the other warps is read before they meet)
+#pragma unroll
+        for (int kt = 0; kt < D / 16; ++kt) ldmatrix_x4(smem_u32(st.k) + piece<P>(row0 + b_row, 2 * kt + b_piece), kb[kt]);
         together();
         if (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
-            float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(sh.s);  // [2][4][32], in the place of what is not needed
+            float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(sh.x);  // [2][4][32], in the place of what is not needed
             float(*zs)[4][32] = reinterpret_cast<float(*)[4][32]>(sh.dw);
 #pragma unroll 1
             for (int r = 0; r < n; ++r) {
@@ -601,39 +635,37 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
                         reinterpret_cast<T *>(out + (uint64_t)r * a.o_token)[g + 8 * e] = from_f32<T>(a.scale * (y[e] + z * d));
                 }
             }
+            done();
             continue;
         }
-        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone), for the warp's rows
-        float X[2][4] = {}, Y[2][4] = {};
+        // X = S K^T for the warp's rows
+        float X[2][4] = {}, Xl[2][4] = {};
         float2 unit = make_float2(1.f, 1.f);
         // f16: accumulators go over to the unit of the next factors
         auto change = [&](float(*x)[4], float2 now, float2 next) {
-            const float f0 = now.x / next.x, f1 = now.y / next.y;
+            const float f0 = now.x * flipped(next.x), f1 = now.y * flipped(next.y);
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
         };
+        const float2 one = make_float2(1.f, 1.f);
 #pragma unroll
         for (int kt = 0; kt < D / 16; ++kt) {
             if (kHalf && kt % KQ == 0) {
-                const float2 next = sh.s_unit[kt / KQ][lane];
-                if (kt) change(X, unit, next), change(Y, unit, next);
+                const float2 next = sh.s_unit[turn][kt / KQ][lane];
+                if (kt) change(X, unit, next), change(Xl, unit, next);
                 unit = next;
             }
-            const uint4 hi = sh.s[kt][0][lane], lo = sh.s[kt][1][lane];
-            uint32_t b[4], c[4];
-            ldmatrix_x4(smem_u32(st.k) + piece<P>(row0 + b_row, 2 * kt + b_piece), b);
-            ldmatrix_x4(smem_u32(st.q) + piece<P>(row0 + b_row, 2 * kt + b_piece), c);
-            mma16816(X[0], &hi.x, b[0], b[1], T());
-            mma16816(X[1], &hi.x, b[2], b[3], T());
-            mma16816(Y[0], &hi.x, c[0], c[1], T());
-            mma16816(Y[1], &hi.x, c[2], c[3], T());
-            mma16816(X[0], &lo.x, b[0], b[1], T());
-            mma16816(X[1], &lo.x, b[2], b[3], T());
+            const uint4 hi = sh.s_hi[turn][kt][lane], lo = sh.s_lo[kt][lane];
+            mma16816(X[0], &hi.x, kb[kt][0], kb[kt][1], T());
+            mma16816(X[1], &hi.x, kb[kt][2], kb[kt][3], T());
+            mma16816(Xl[0], &lo.x, kb[kt][0], kb[kt][1], T());
+            mma16816(Xl[1], &lo.x, kb[kt][2], kb[kt][3], T());
         }
-        if (kHalf) {
-            const float2 one = make_float2(1.f, 1.f);
-            change(X, unit, one), change(Y, unit, one);
-        }
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) X[nt][e] += Xl[nt][e];
+        if (kHalf) change(X, unit, one);
         // what the values differ by from what the state says: X <- V - f X
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
@@ -647,9 +679,17 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         float u0 = 1.f, u1 = 1.f;
         if (kHalf) {
             u0 = range_scale(top_of(X[0], X[1], 0)), u1 = range_scale(top_of(X[0], X[1], 1));
-            sh.x_unit[mine][lane] = make_float2(1.f / u0, 1.f / u1);
+            sh.x_unit[mine][lane] = make_float2(flipped(u0), flipped(u1));
         }
-        put_terms(sh.x[mine], X[0], X[1], u0, u1);
+        put_terms(sh.x[mine][0], sh.x[mine][1], X[0], X[1], u0, u1);
+        uint32_t tb[2][C / 16][4];
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kt > (int)mine) break;
+            const uint32_t at = block_piece(row0 + b_row, 2 * kt + b_piece);
+            ldmatrix_x4(smem_u32(st.w.tile[0]) + at, tb[0][kt]);
+            ldmatrix_x4(smem_u32(st.w.tile[1]) + at, tb[1][kt]);
+        }
         together();
         // d = X T^T: two terms each (the product of the small ones left out), from the rows up to the warp's own
         float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
@@ -662,9 +702,7 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
                 unit = next;
             }
             const uint4 hi = sh.x[kt][0][lane], lo = sh.x[kt][1][lane];
-            uint32_t b[4], c[4];
-            ldmatrix_x4(smem_u32(st.w.tile[0]) + piece<8>(row0 + b_row, 2 * kt + b_piece), b);
-            ldmatrix_x4(smem_u32(st.w.tile[1]) + piece<8>(row0 + b_row, 2 * kt + b_piece), c);
+            const uint32_t *b = tb[0][kt], *c = tb[1][kt];
             mma16816(d[0], &hi.x, b[0], b[1], T());
             mma16816(d[1], &hi.x, b[2], b[3], T());
             mma16816(dl[0], &lo.x, b[0], b[1], T());
@@ -681,7 +719,7 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         }
         if (kHalf) {
             u0 = range_scale(top_of(d[0], d[1], 0)), u1 = range_scale(top_of(d[0], d[1], 1));
-            sh.d_unit[mine][lane] = make_float2(st.w.p_unit / u0, st.w.p_unit / u1);
+            sh.d_unit[mine][lane] = make_float2(st.w.p_unit * flipped(u0), st.w.p_unit * flipped(u1));
         }
         sh.d[mine][lane] = make_uint4(pack2(d[0][0] * u0, d[0][1] * u0, T()), pack2(d[0][2] * u1, d[0][3] * u1, T()),
                                       pack2(d[1][0] * u0, d[1][1] * u0, T()), pack2(d[1][2] * u1, d[1][3] * u1, T()));
@@ -692,9 +730,14 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         }
         if (kHalf) {
             u0 = range_scale(top_of(d[0], d[1], 0)), u1 = range_scale(top_of(d[0], d[1], 1));
-            sh.dw_unit[mine][lane] = make_float2(1.f / u0, 1.f / u1);
+            sh.dw_unit[mine][lane] = make_float2(flipped(u0), flipped(u1));
         }
-        put_terms(sh.dw[mine], d[0], d[1], u0, u1);
+        put_terms(sh.dw[mine][0], sh.dw[mine][1], d[0], d[1], u0, u1);
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt += 2)
+                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + nt + lane / 16), kb[kt * (NT / 2) + nt / 2]);
         together();
         // S <- e^G S + (w d) K for the warp's keys
         const float all = st.w.all;
@@ -702,7 +745,7 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[nt][e] *= all;
-        unit = make_float2(1.f, 1.f);
+        unit = one;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             if (kHalf) {
@@ -712,29 +755,39 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
                 unit = next;
             }
             const uint4 hi = sh.dw[kt][0][lane], lo = sh.dw[kt][1][lane];
-            uint32_t b[NT][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + nt + lane / 16), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
-            }
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], &hi.x, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], &lo.x, b[nt][0], b[nt][1], T());
+                for (int nt = 0; nt < NT; ++nt)
+                    mma16816(S[nt], t ? &lo.x : &hi.x, kb[kt * (NT / 2) + nt / 2][2 * (nt & 1)], kb[kt * (NT / 2) + nt / 2][2 * (nt & 1) + 1], T());
         }
         if (kHalf) {
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, make_float2(1.f, 1.f));
+            for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, one);
         }
-        // out = h Y + P d for the warp's rows (one term each)
+        // out = h Q S + P d for the warp's rows, with S before the chunk (one term each): nothing waits for it
+        float Y[2][4] = {};
+        unit = one;
+#pragma unroll
+        for (int kt = 0; kt < D / 16; ++kt) {
+            if (kHalf && kt % KQ == 0) {
+                const float2 next = sh.s_unit[turn][kt / KQ][lane];
+                if (kt) change(Y, unit, next);
+                unit = next;
+            }
+            const uint4 hi = sh.s_hi[turn][kt][lane];
+            uint32_t b[4];
+            ldmatrix_x4(smem_u32(st.q) + piece<P>(row0 + b_row, 2 * kt + b_piece), b);
+            mma16816(Y[0], &hi.x, b[0], b[1], T());
+            mma16816(Y[1], &hi.x, b[2], b[3], T());
+        }
+        if (kHalf) change(Y, unit, one);
+        unit = one;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[row0 + 8 * nt + t2]);
             Y[nt][0] *= f.x, Y[nt][1] *= f.y, Y[nt][2] *= f.x, Y[nt][3] *= f.y;
         }
-        unit = make_float2(1.f, 1.f);
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             if (kt > (int)mine) break;
@@ -745,11 +798,11 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
             }
             const uint4 x = sh.d[kt][lane];
             uint32_t b[4];
-            ldmatrix_x4(smem_u32(st.w.tile[2]) + piece<8>(row0 + b_row, 2 * kt + b_piece), b);
+            ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(row0 + b_row, 2 * kt + b_piece), b);
             mma16816(Y[0], &x.x, b[0], b[1], T());
             mma16816(Y[1], &x.x, b[2], b[3], T());
         }
-        if (kHalf) change(Y, unit, make_float2(1.f, 1.f));
+        if (kHalf) change(Y, unit, one);
         // rows of 16 columns through the warp's own part of V's tile
         const uint32_t y[4] = {pack2(Y[0][0], Y[0][1], T()), pack2(Y[0][2], Y[0][3], T()), pack2(Y[1][0], Y[1][1], T()), pack2(Y[1][2], Y[1][3], T())};
         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
@@ -760,6 +813,7 @@ __global__ void __launch_bounds__((4 * W + kFetchWarps) * 32) kv_delta_chain_ker
         const uint32_t r = row0 + lane / 2;
         const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
         if ((int)r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
+        done();
     }
     if (!to) return;
 #pragma unroll
