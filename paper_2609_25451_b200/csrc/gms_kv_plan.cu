@@ -18,11 +18,12 @@ struct PlanArgs {
     uint32_t n_seq, total_rows, table_blocks, free_cap, n_blocks, block_shift;
 };
 
-constexpr uint32_t kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanEach = 4, kPlanTile = kPlanThreads * kPlanEach;
-constexpr uint32_t kPlanCtas = 8;  // of a cluster
+constexpr uint32_t kPlanTile = 2048;  // sequences
+constexpr uint32_t kPlanCtas = 8;     // of a cluster
 constexpr int32_t kMostTokens = 1 << 30;
 
-// Sum over the threads before this one; `sh` has two words a warp and is free again after the caller's next two barriers.
+// Sum over the threads before this one; `sh` has a word a warp and is free again after the caller's next two barriers.
+template <uint32_t WARPS>
 __device__ __forceinline__ uint64_t sum_before(uint64_t x, uint64_t *sh, uint64_t *all)
 {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
@@ -36,7 +37,7 @@ __device__ __forceinline__ uint64_t sum_before(uint64_t x, uint64_t *sh, uint64_
     __syncthreads();
     uint64_t before = inc - x, sum = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kPlanWarps; ++i) {
+    for (uint32_t i = 0; i < WARPS; ++i) {
         if (i < warp) before += sh[i];
         sum += sh[i];
     }
@@ -77,13 +78,32 @@ __device__ __forceinline__ void all_here()
         __syncthreads();
 }
 
-// One CTA, or a cluster of eight that all scan the lengths for themselves and share rows and blocks out.  The last CTA (the only
-// one) also takes blocks back and writes what is one word a sequence.  Nothing that one CTA reads is written by another: taken
-// and returned places of the ring are different ones, so are entries that are looked up and entries that are new; lengths and the
-// ring's state, which may be updated in place, are written behind a barrier.
+// A word to the same place in every CTA of the cluster (a lane each).
 template <bool CLUSTER>
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_constant__ PlanArgs a)
+__device__ __forceinline__ void tell_all(uint32_t *place, uint32_t x)
 {
+    const uint32_t lane = threadIdx.x & 31u;
+    if (!CLUSTER) {
+        if (lane == 0) *place = x;
+    } else if (lane < kPlanCtas) {
+        asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.u32 [a], %2;\n\t}" ::"r"(ptx::smem_u32(place)),
+                     "r"(lane), "r"(x)
+                     : "memory");
+    }
+}
+
+// One CTA, or a cluster of eight that all scan the lengths for themselves and share rows and blocks out (a captured step costs one
+// launch either way; the last CTA writes what is one word a sequence).  Nothing that one CTA reads is written by another: taken
+// and returned places of the ring are different ones, so are entries that are looked up and entries that are new; lengths and the
+// ring's state, which may be updated in place, are written behind a barrier.  Blocks that come back are looked at twice, a run of
+// them a warp: how many are blocks, then, when all warps know what the others have, where they go.  Bound by latency: four lengths a
+// sequence, a scan, one or two words a row.
+template <bool CLUSTER>
+__global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __grid_constant__ PlanArgs a)
+{
+    constexpr uint32_t kPlanThreads = CLUSTER ? 1024 : 512, kPlanWarps = kPlanThreads / 32, kPlanEach = kPlanTile / kPlanThreads;
+    constexpr uint32_t kAllWarps = (CLUSTER ? kPlanCtas : 1) * kPlanWarps, kLook = 8;
+    __shared__ uint32_t found[kAllWarps];  // blocks that each warp's run has
     extern __shared__ uint8_t raw[];
     Tile &t = *reinterpret_cast<Tile *>(raw);
     __shared__ uint64_t sums[3][kPlanWarps];
@@ -95,7 +115,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
     const uint32_t cap = a.free_cap;
     const uint32_t head = cap ? (uint32_t)a.free_state[0] % cap : 0, count = cap ? (uint32_t)min(max(a.free_state[1], 0), (int)cap) : 0;
     uint64_t rows_before = 0, rank_before = 0;  // of all tiles before
-    uint32_t returned = 0;                      // by the leader: blocks that have come back so far
+    uint32_t returned = 0;                      // blocks that have come back so far
     const uint64_t most = a.total_rows;
     bool full = false;
     if (leader && tid == 0) a.cu_q[0] = 0;
@@ -114,7 +134,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             mine += rows[i];
         }
         uint64_t all_rows;
-        uint64_t row = rows_before + sum_before(mine, sums[0], &all_rows);
+        uint64_t row = rows_before + sum_before<kPlanWarps>(mine, sums[0], &all_rows);
         uint32_t more[kPlanEach], back[kPlanEach];
         uint64_t need_sum = 0, back_sum = 0;
 #pragma unroll
@@ -137,7 +157,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             row = end;
         }
         uint64_t all_need, all_back;
-        uint64_t rank = sum_before(need_sum, sums[1], &all_need), gone = sum_before(back_sum, sums[2], &all_back);
+        uint64_t rank = sum_before<kPlanWarps>(need_sum, sums[1], &all_need), gone = sum_before<kPlanWarps>(back_sum, sums[2], &all_back);
 #pragma unroll
         for (uint32_t i = 0; i < kPlanEach; ++i) {
             if (first + i < n) {
@@ -184,27 +204,58 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const __grid_cons
             a.slots[x] = (uint32_t)id < a.n_blocks ? ((int64_t)id << a.block_shift) + (pos & ((1u << a.block_shift) - 1u)) : -1;
             if (a.positions) a.positions[x] = (int32_t)pos;
         }
-        if (leader) {  // in order, so one CTA alone: the places of the ring go to the ids that are blocks
-            const uint32_t room = cap - count;
-            for (uint32_t r0 = 0; r0 < t.back[n]; r0 += kPlanThreads) {
-                const uint32_t r = r0 + tid;
-                int32_t id = -1;
-                if (r < t.back[n]) {
-                    const uint32_t i = owner(t.back, n, r), end = t.had[i], k = t.back[i + 1] - t.back[i];
-                    id = a.table[(uint64_t)(s0 + i) * a.table_stride + (end - k) + (r - t.back[i])];
+        if (t.back[n]) {
+            const uint32_t lane = tid & 31u, warp = cta * kPlanWarps + tid / 32, room = cap - count;
+            const uint32_t run = (t.back[n] + kAllWarps * 32 - 1) / (kAllWarps * 32) * 32, r0 = min(warp * run, t.back[n]), r1 = min(r0 + run, t.back[n]);
+            // the ids of up to kLook x 32 entries of the run from r on; owners go up with r
+            uint32_t i = 0;
+            auto look = [&](uint32_t r, int32_t *id) {
+                uint32_t at[kLook];
+#pragma unroll
+                for (uint32_t k = 0; k < kLook; ++k) {
+                    at[k] = r + 32 * k + lane;
+                    id[k] = -1;
+                    if (at[k] >= r1) continue;
+                    while (t.back[i + 1] <= at[k]) ++i;
+                    id[k] = a.table[(uint64_t)(s0 + i) * a.table_stride + t.had[i] - (t.back[i + 1] - at[k])];
                 }
-                const bool is = (uint32_t)id < a.n_blocks;
-                uint64_t all;
-                const uint32_t to = returned + (uint32_t)sum_before(is, sums[(r0 / kPlanThreads) % 3], &all);
-                if (is && to < room) {
-                    uint64_t p = (uint64_t)head + count + to;
-                    if (p >= cap) p -= cap;
-                    a.free_ids[p] = id;
-                } else {
-                    full |= is;
-                }
-                returned = min(returned + (uint32_t)all, room);
+            };
+            uint32_t mine_found = 0;
+            const uint32_t first_owner = r0 + lane < r1 ? owner(t.back, n, r0 + lane) : 0;
+            i = first_owner;
+            for (uint32_t r = r0; r < r1; r += 32 * kLook) {
+                int32_t id[kLook];
+                look(r, id);
+#pragma unroll
+                for (uint32_t k = 0; k < kLook; ++k) mine_found += __popc(__ballot_sync(0xffffffffu, (uint32_t)id[k] < a.n_blocks));
             }
+            tell_all<CLUSTER>(&found[warp], mine_found);
+            all_here<CLUSTER>();
+            uint32_t before = 0, all = 0;
+            for (uint32_t w = lane; w < kAllWarps; w += 32) {
+                all += found[w];
+                if (w < warp) before += found[w];
+            }
+            before = returned + __reduce_add_sync(0xffffffffu, before);
+            all = __reduce_add_sync(0xffffffffu, all);
+            i = first_owner;
+            for (uint32_t r = r0; r < r1; r += 32 * kLook) {
+                int32_t id[kLook];
+                look(r, id);
+#pragma unroll
+                for (uint32_t k = 0; k < kLook; ++k) {
+                    const bool is = (uint32_t)id[k] < a.n_blocks;
+                    const uint32_t which = __ballot_sync(0xffffffffu, is), to = before + __popc(which & ((1u << lane) - 1u));
+                    before += __popc(which);
+                    if (is && to < room) {
+                        const uint32_t p = head + count, q = (p >= cap ? p - cap : p) + to;
+                        a.free_ids[q >= cap ? q - cap : q] = id[k];
+                    } else {
+                        full |= is;
+                    }
+                }
+            }
+            returned = min(returned + all, room);
         }
         rows_before += all_rows;
         rank_before += all_need;
@@ -232,7 +283,7 @@ cudaError_t launch_plan(const PlanArgs &a, cudaStream_t s)
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(cluster ? kPlanCtas : 1);
-    cfg.blockDim = dim3(kPlanThreads);
+    cfg.blockDim = dim3(cluster ? 1024 : 512);
     cfg.dynamicSmemBytes = sizeof(Tile);
     cfg.stream = s;
     cudaLaunchAttribute at[2] = {};
