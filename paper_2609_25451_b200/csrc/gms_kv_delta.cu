@@ -6,22 +6,120 @@
 namespace gms {
 namespace {
 
-constexpr uint32_t kRowThreads = 256, kRowWarps = kRowThreads / 32, kRowBatch = 8;
+constexpr uint32_t kRowThreads = 256, kRowWarps = kRowThreads / 32, kRowBatch = kRowWarps;
 
-// A CTA has W value columns of one head's state in registers, four columns and D W / 1024 rows a thread, and goes through the
-// sequence's rows one by one.  Both S^T k and S^T q are taken of the state before the row (S_new^T q = e^g S^T q + (k.q) d), so
-// one exchange between the warps is all a row needs.  kRowBatch rows of q, k, v and gates are staged at a time.
+// W value columns of a head's state in a CTA's registers: four columns and D W / 1024 rows a thread.
+template <int D, int W>
+struct RowShape {
+    static constexpr int C = W / 4, R = kRowThreads / C, N = D / R;  // threads across, threads down, rows a thread
+    static_assert(C <= 32 && N >= 1, "");
+};
+// kRowBatch rows of q, k, v and gates, and what the warps tell each other.
+template <int D, int W>
+struct RowSmem {
+    float q[kRowBatch][D], k[kRowBatch][D], v[kRowBatch][W], gate[kRowBatch], strength[kRowBatch], qk[kRowBatch];
+    float4 part[2][kRowWarps][2][RowShape<D, W>::C];
+};
+
+// A row as a warp reads it, and puts it into shared memory.
+template <class T, int D, int W>
+struct Row1 {
+    T q[D / 32], k[D / 32], v[(W + 31) / 32];
+    float g, b;
+};
+template <class T, int D, int W>
+__device__ __forceinline__ void read_row(const DeltaArgs &a, uint64_t row, uint32_t h, uint32_t slice, Row1<T, D, W> &x)
+{
+    const uint32_t lane = threadIdx.x & 31u, c = h / a.group;
+    const T *qp = reinterpret_cast<const T *>(a.q + row * a.q_token + c * a.q_head), *kp = reinterpret_cast<const T *>(a.k + row * a.k_token + c * a.k_head);
+    const T *vp = reinterpret_cast<const T *>(a.v + row * a.v_token + h * a.v_head) + slice * W;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) x.q[i] = qp[lane + 32 * i], x.k[i] = kp[lane + 32 * i];
+#pragma unroll
+    for (int i = 0; i < W / 32; ++i) x.v[i] = vp[lane + 32 * i];
+    x.g = a.g ? a.g[row * a.g_stride + h] : 0.f;
+    x.b = a.beta ? a.beta[row * a.beta_stride + h] : 1.f;
+}
+template <class T, int D, int W>
+__device__ __forceinline__ void put_row(const DeltaArgs &a, const Row1<T, D, W> &x, uint32_t to, RowSmem<D, W> &m)
+{
+    const uint32_t lane = threadIdx.x & 31u;
+    float q[D / 32], k[D / 32], qq = 0.f, kk = 0.f, qk = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        q[i] = to_f32(x.q[i]), k[i] = to_f32(x.k[i]);
+        qq += q[i] * q[i], kk += k[i] * k[i], qk += q[i] * k[i];
+    }
+    qq = warp_sum(qq), kk = warp_sum(kk), qk = warp_sum(qk);
+    const float fq = a.unit_qk ? rsqrtf(qq + a.unit_eps) : 1.f, fk = a.unit_qk ? rsqrtf(kk + a.unit_eps) : 1.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) m.q[to][lane + 32 * i] = q[i] * fq, m.k[to][lane + 32 * i] = k[i] * fk;
+#pragma unroll
+    for (int i = 0; i < W / 32; ++i) m.v[to][lane + 32 * i] = to_f32(x.v[i]);
+    if (lane == 0) m.qk[to] = qk * fq * fk, m.gate[to] = expf(x.g), m.strength[to] = x.b;
+}
+
+// Takes the state over n rows that are in shared memory (the first is row `first` of the call).  Both S^T k and S^T q are taken of the
+// state before the row (S_new^T q = e^g S^T q + (k.q) d), so one exchange between the warps is all a row needs.
+template <class T, int D, int W>
+__device__ __forceinline__ void take_rows(const DeltaArgs &a, RowSmem<D, W> &m, int n, uint64_t first, uint32_t h, uint32_t slice,
+                                          float4 (&S)[RowShape<D, W>::N])
+{
+    constexpr int C = RowShape<D, W>::C, N = RowShape<D, W>::N, P = kRowWarps;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, col = threadIdx.x % C, down = threadIdx.x / C;
+    for (int r = 0; r < n; ++r) {
+        float4 x = {}, y = {};  // S^T k, S^T q
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float kr = m.k[r][down * N + i], qr = m.q[r][down * N + i];
+            x.x += kr * S[i].x, x.y += kr * S[i].y, x.z += kr * S[i].z, x.w += kr * S[i].w;
+            y.x += qr * S[i].x, y.y += qr * S[i].y, y.z += qr * S[i].z, y.w += qr * S[i].w;
+        }
+#pragma unroll
+        for (int o = C; o < 32; o <<= 1) {
+            x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
+            x.z += __shfl_xor_sync(0xffffffffu, x.z, o), x.w += __shfl_xor_sync(0xffffffffu, x.w, o);
+            y.x += __shfl_xor_sync(0xffffffffu, y.x, o), y.y += __shfl_xor_sync(0xffffffffu, y.y, o);
+            y.z += __shfl_xor_sync(0xffffffffu, y.z, o), y.w += __shfl_xor_sync(0xffffffffu, y.w, o);
+        }
+        if ((int)lane < C) m.part[r & 1][warp][0][col] = x, m.part[r & 1][warp][1][col] = y;
+        asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+        x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const float4 u = m.part[r & 1][p][0][col];
+            x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
+        }
+        const float e = m.gate[r], b = m.strength[r];
+        const float4 v = *reinterpret_cast<const float4 *>(&m.v[r][col * 4]);
+        const float4 d = make_float4(b * (v.x - e * x.x), b * (v.y - e * x.y), b * (v.z - e * x.z), b * (v.w - e * x.w));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float kr = m.k[r][down * N + i];
+            S[i].x = e * S[i].x + kr * d.x, S[i].y = e * S[i].y + kr * d.y, S[i].z = e * S[i].z + kr * d.z, S[i].w = e * S[i].w + kr * d.w;
+        }
+        if (down == 0) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float4 u = m.part[r & 1][p][1][col];
+                y.x += u.x, y.y += u.y, y.z += u.z, y.w += u.w;
+            }
+            const float z = m.qk[r];
+            T *op = reinterpret_cast<T *>(a.out + (first + r) * a.o_token + h * a.o_head) + slice * W + col * 4;
+            *reinterpret_cast<uint2 *>(op) = make_uint2(pack2(a.scale * (e * y.x + z * d.x), a.scale * (e * y.y + z * d.y), T()),
+                                                        pack2(a.scale * (e * y.z + z * d.z), a.scale * (e * y.w + z * d.w), T()));
+        }
+    }
+}
+
+// Few states: W value columns of one a CTA.  Bound by latency.
 template <class T, int D, int W>
 __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid_constant__ DeltaArgs a)
 {
-    constexpr int C = W / 4, R = kRowThreads / C, N = D / R;  // threads across, threads down, rows a thread
-    constexpr int P = R / (32 / C);                           // partial sums that meet in shared memory (a warp has 32 / C threads down)
-    static_assert(C <= 32 && N >= 1 && P == (int)kRowWarps, "");
-    __shared__ float qs[kRowBatch][D], ks[kRowBatch][D], vs[kRowBatch][W], gate[kRowBatch], strength[kRowBatch], qk[kRowBatch];
-    __shared__ float4 part[2][P][2][C];
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32;
-    const uint32_t slice = blockIdx.x % (D / W), h = blockIdx.x / (D / W) % a.n_heads, s = blockIdx.x / (D / W) / a.n_heads, c = h / a.group;
-    const uint32_t col = tid % C, down = tid / C;
+    constexpr int C = RowShape<D, W>::C, N = RowShape<D, W>::N;
+    __shared__ RowSmem<D, W> m;
+    const uint32_t tid = threadIdx.x, warp = tid / 32;
+    const uint32_t slice = blockIdx.x % (D / W), h = blockIdx.x / (D / W) % a.n_heads, s = blockIdx.x / (D / W) / a.n_heads;
     ptx::grid_wait();
     ptx::grid_launch_dependents();
     const int first = delta_begin(a, s), rows = delta_rows(a, s);
@@ -30,7 +128,7 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
     if (a.status && tid == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
-    const uint32_t at = (down * N) * D + slice * W + col * 4;
+    const uint32_t at = (tid / C * N) * D + slice * W + tid % C * 4;
     float4 S[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) S[i] = from ? *reinterpret_cast<const float4 *>(from + at + i * D) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -38,81 +136,162 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
         const int n = min(rows - r0, (int)kRowBatch);
         __syncthreads();
         if ((int)warp < n) {  // a warp stages a row
-            const uint64_t row = (uint64_t)(first + r0 + (int)warp);
-            const T *qp = reinterpret_cast<const T *>(a.q + row * a.q_token + c * a.q_head), *kp = reinterpret_cast<const T *>(a.k + row * a.k_token + c * a.k_head);
-            const T *vp = reinterpret_cast<const T *>(a.v + row * a.v_token + h * a.v_head) + slice * W;
-            float x[D / 32], y[D / 32], xx = 0.f, yy = 0.f, xy = 0.f;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                x[i] = to_f32(qp[lane + 32 * i]), y[i] = to_f32(kp[lane + 32 * i]);
-                xx += x[i] * x[i], yy += y[i] * y[i], xy += x[i] * y[i];
-            }
-            xx = warp_sum(xx), yy = warp_sum(yy), xy = warp_sum(xy);
-            const float fx = a.unit_qk ? rsqrtf(xx + a.unit_eps) : 1.f, fy = a.unit_qk ? rsqrtf(yy + a.unit_eps) : 1.f;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) qs[warp][lane + 32 * i] = x[i] * fx, ks[warp][lane + 32 * i] = y[i] * fy;
-            for (int i = lane; i < W; i += 32) vs[warp][i] = to_f32(vp[i]);
-            if (lane == 0) {
-                qk[warp] = xy * fx * fy;
-                gate[warp] = a.g ? expf(a.g[row * a.g_stride + h]) : 1.f;
-                strength[warp] = a.beta ? a.beta[row * a.beta_stride + h] : 1.f;
-            }
+            Row1<T, D, W> x;
+            read_row<T, D, W>(a, (uint64_t)(first + r0 + (int)warp), h, slice, x);
+            put_row<T, D, W>(a, x, warp, m);
         }
         __syncthreads();
-        for (int r = 0; r < n; ++r) {
-            float4 x = {}, y = {};  // S^T k, S^T q
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float kr = ks[r][down * N + i], qr = qs[r][down * N + i];
-                x.x += kr * S[i].x, x.y += kr * S[i].y, x.z += kr * S[i].z, x.w += kr * S[i].w;
-                y.x += qr * S[i].x, y.y += qr * S[i].y, y.z += qr * S[i].z, y.w += qr * S[i].w;
-            }
-#pragma unroll
-            for (int o = C; o < 32; o <<= 1) {
-                x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
-                x.z += __shfl_xor_sync(0xffffffffu, x.z, o), x.w += __shfl_xor_sync(0xffffffffu, x.w, o);
-                y.x += __shfl_xor_sync(0xffffffffu, y.x, o), y.y += __shfl_xor_sync(0xffffffffu, y.y, o);
-                y.z += __shfl_xor_sync(0xffffffffu, y.z, o), y.w += __shfl_xor_sync(0xffffffffu, y.w, o);
-            }
-            if ((int)lane < C) part[r & 1][warp][0][col] = x, part[r & 1][warp][1][col] = y;
-            __syncthreads();
-            x = y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const float4 u = part[r & 1][p][0][col];
-                x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
-            }
-            const float e = gate[r], b = strength[r];
-            const float4 v = *reinterpret_cast<const float4 *>(&vs[r][col * 4]);
-            const float4 d = make_float4(b * (v.x - e * x.x), b * (v.y - e * x.y), b * (v.z - e * x.z), b * (v.w - e * x.w));
-            if (down == 0) {
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const float4 u = part[r & 1][p][1][col];
-                    y.x += u.x, y.y += u.y, y.z += u.z, y.w += u.w;
-                }
-                const float z = qk[r];
-                T *op = reinterpret_cast<T *>(a.out + (uint64_t)(first + r0 + r) * a.o_token + h * a.o_head) + slice * W + col * 4;
-                *reinterpret_cast<uint2 *>(op) = make_uint2(pack2(a.scale * (e * y.x + z * d.x), a.scale * (e * y.y + z * d.y), T()),
-                                                            pack2(a.scale * (e * y.z + z * d.z), a.scale * (e * y.w + z * d.w), T()));
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float kr = ks[r][down * N + i];
-                S[i].x = e * S[i].x + kr * d.x, S[i].y = e * S[i].y + kr * d.y, S[i].z = e * S[i].z + kr * d.z, S[i].w = e * S[i].w + kr * d.w;
-            }
-        }
+        take_rows<T, D, W>(a, m, n, (uint64_t)(first + r0), h, slice, S);
     }
     if (!to) return;
 #pragma unroll
     for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(to + at + i * D) = S[i];
 }
 
+template <int D>
+struct StreamShape {
+    static constexpr int kBuffers = D == 128 ? 3 : 4, kCtas = D == 128 ? 1 : 2;
+};
+template <int D>
+struct StreamSmem {
+    float state[StreamShape<D>::kBuffers][D * D];
+    RowSmem<D, D> rows;
+    uint64_t full[StreamShape<D>::kBuffers], done[StreamShape<D>::kBuffers];
+};
+constexpr uint32_t kStreamThreads = kRowThreads + 32;
+
+// Many states: whole ones through a ring of buffers, brought and taken away by bulk copies that one thread issues, two on their way while
+// one is worked on, by CTAs that stay.  Bound by memory.
+template <class T, int D>
+__global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delta_stream_kernel(const __grid_constant__ DeltaArgs a)
+{
+    extern __shared__ __align__(128) uint8_t raw[];
+    StreamSmem<D> &m = *reinterpret_cast<StreamSmem<D> *>(raw);
+    constexpr int C = RowShape<D, D>::C, N = RowShape<D, D>::N, NB = StreamShape<D>::kBuffers;
+    const uint32_t tid = threadIdx.x, warp = tid / 32, items = a.n_seq * a.n_heads;
+    if (tid == 0) {
+        for (int i = 0; i < NB; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&m.full[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&m.done[i]), kRowWarps);
+        }
+        ptx::fence_mbar_init();
+    }
+    __syncthreads();
+    ptx::grid_wait();
+    ptx::grid_launch_dependents();
+    // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
+    bool late = false;
+    auto wait = [&](uint64_t *bar, uint32_t use) {
+        if (late || ptx::mbar_wait(ptx::smem_u32(bar), use & 1u)) return;
+        late = true;
+        if (a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+    };
+    if (warp == kRowWarps) {
+        if ((tid & 31u) != 0) return;
+        auto rows_of = [&](uint32_t item) { return delta_rows(a, item / a.n_heads); };
+        auto load = [&](uint32_t item, uint32_t k) {
+            const uint32_t s = item / a.n_heads, h = item % a.n_heads, b = k % NB, bar = ptx::smem_u32(&m.full[b]);
+            const bool fresh = a.past_lens && a.past_lens[s] <= 0;
+            const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
+            if (!from) {
+                if (!fresh && a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+                ptx::mbar_arrive(bar);
+                return;
+            }
+            ptx::mbar_expect(bar, D * D * 4);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(m.state[b])),
+                         "l"(from), "r"(D * D * 4), "r"(bar)
+                         : "memory");
+        };
+        auto store = [&](uint32_t item, uint32_t k) {
+            const uint32_t s = item / a.n_heads, h = item % a.n_heads;
+            float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
+            if (to)
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(ptx::smem_u32(m.state[k % NB])), "r"(D * D * 4)
+                             : "memory");
+            else if (a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        };
+        auto next = [&](uint32_t item) {  // of this CTA's items, those that are done here
+            while (item < items && delta_in_chunks(a, rows_of(item))) item += gridDim.x;
+            return item;
+        };
+        uint32_t ahead = next(blockIdx.x), k_ahead = 0;
+        for (; k_ahead < NB - 1 && ahead < items; ++k_ahead, ahead = next(ahead + gridDim.x)) load(ahead, k_ahead);
+        uint32_t k = 0;
+        for (uint32_t item = next(blockIdx.x); item < items; item = next(item + gridDim.x), ++k) {
+            wait(&m.done[k % NB], k / NB);
+            store(item, k);
+            if (ahead < items) {  // into the buffer of the state before, once that has been read
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                load(ahead, k_ahead);
+                ++k_ahead, ahead = next(ahead + gridDim.x);
+            }
+        }
+        if (late) {  // copies that may still be under way
+            late = false;
+            for (uint32_t i = k_ahead > NB ? k_ahead - NB : 0; i < k_ahead; ++i) wait(&m.full[i % NB], i / NB);
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        return;
+    }
+    // rows are read one state ahead
+    Row1<T, D, D> row;
+    auto first_rows = [&](uint32_t item) {
+        while (item < items) {
+            const int rows = delta_rows(a, item / a.n_heads);
+            if (!delta_in_chunks(a, rows)) {
+                if ((int)warp < rows) read_row<T, D, D>(a, (uint64_t)(delta_begin(a, item / a.n_heads) + (int)warp), item % a.n_heads, 0, row);
+                break;
+            }
+            item += gridDim.x;
+        }
+        return item;
+    };
+    uint32_t k = 0;
+    for (uint32_t item = first_rows(blockIdx.x), next; item < items; item = next, ++k) {
+        const uint32_t s = item / a.n_heads, h = item % a.n_heads, b = k % NB;
+        const int first = delta_begin(a, s), rows = delta_rows(a, s);
+        const bool zero = (a.past_lens && a.past_lens[s] <= 0) || !delta_state<D>(a, a.src_table, a.src_stride, s, h);
+        if ((int)warp < min(rows, (int)kRowBatch)) put_row<T, D, D>(a, row, warp, m.rows);
+        next = first_rows(item + gridDim.x);
+        wait(&m.full[b], k / NB);
+        float *state = m.state[b] + (tid / C * N) * D + tid % C * 4;
+        float4 S[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) S[i] = zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4 *>(state + i * D);
+        asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+        take_rows<T, D, D>(a, m.rows, min(rows, (int)kRowBatch), (uint64_t)first, h, 0, S);
+        for (int r0 = kRowBatch; r0 < rows; r0 += kRowBatch) {
+            const int n = min(rows - r0, (int)kRowBatch);
+            asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+            if ((int)warp < n) {
+                Row1<T, D, D> x;
+                read_row<T, D, D>(a, (uint64_t)(first + r0 + (int)warp), h, 0, x);
+                put_row<T, D, D>(a, x, warp, m.rows);
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+            take_rows<T, D, D>(a, m.rows, n, (uint64_t)(first + r0), h, 0, S);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(state + i * D) = S[i];
+        ptx::fence_proxy_async();
+        asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");  // (the rows have been read, too)
+        if ((tid & 31u) == 0) ptx::mbar_arrive(ptx::smem_u32(&m.done[b]));
+    }
+}
+
 template <class T, int D>
 cudaError_t launch_rows(const DeltaArgs &a, cudaStream_t s)
 {
     constexpr int W = 32;
-    return launch_dependent(kv_delta_rows_kernel<T, D, W>, a.n_seq * a.n_heads * (D / W), kRowThreads, 0, s, a);
+    const uint64_t items = (uint64_t)a.n_seq * a.n_heads, held = 148 * StreamShape<D>::kCtas;
+    if (items <= 2 * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);
+    static std::atomic<uint64_t> done;
+    static_assert(sizeof(StreamSmem<D>) * StreamShape<D>::kCtas <= 231424, "");
+    const cudaError_t e = allow_smem(kv_delta_stream_kernel<T, D>, sizeof(StreamSmem<D>), done);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(kv_delta_stream_kernel<T, D>, (uint32_t)held, kStreamThreads, sizeof(StreamSmem<D>), s, a);
 }
 
 int make_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_delta_args *t, DeltaArgs *a)
