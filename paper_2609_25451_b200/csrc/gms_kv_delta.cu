@@ -6,20 +6,22 @@
 namespace gms {
 namespace {
 
-constexpr uint32_t kRowThreads = 256, kRowWarps = kRowThreads / 32, kRowBatch = kRowWarps;
+constexpr uint32_t kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
 // W value columns of a head's state in a CTA's registers: four columns and D W / 1024 rows a thread.
 template <int D, int W>
 struct RowShape {
     static constexpr int C = W / 4, R = kRowThreads / C, N = D / R;  // threads across, threads down, rows a thread
-    static_assert(C <= 32 && N >= 1, "");
+    static_assert(C <= 32 && N % 2 == 0, "");
 };
-// kRowBatch rows of q, k, v and gates, and what the warps tell each other.
-template <int D, int W>
+// B rows of q, k, v and gates, and what the warps tell each other.
+template <int D, int W, int B>
 struct RowSmem {
-    float q[kRowBatch][D], k[kRowBatch][D], v[kRowBatch][W], gate[kRowBatch], strength[kRowBatch], qk[kRowBatch];
-    float4 part[2][kRowWarps][2][RowShape<D, W>::C];
+    float q[B][D], k[B][D], v[B][W], gate[B], strength[B], qk[B];
+    float part[kRowWarps][2][W], d[W];
 };
+
+__device__ __forceinline__ void get4(float4 x, float2 *to) { to[0] = make_float2(x.x, x.y), to[1] = make_float2(x.z, x.w); }
 
 // A row as a warp reads it, and puts it into shared memory.
 template <class T, int D, int W>
@@ -40,8 +42,8 @@ __device__ __forceinline__ void read_row(const DeltaArgs &a, uint64_t row, uint3
     x.g = a.g ? a.g[row * a.g_stride + h] : 0.f;
     x.b = a.beta ? a.beta[row * a.beta_stride + h] : 1.f;
 }
-template <class T, int D, int W>
-__device__ __forceinline__ void put_row(const DeltaArgs &a, const Row1<T, D, W> &x, uint32_t to, RowSmem<D, W> &m)
+template <class T, int D, int W, int B>
+__device__ __forceinline__ void put_row(const DeltaArgs &a, const Row1<T, D, W> &x, uint32_t to, RowSmem<D, W, B> &m)
 {
     const uint32_t lane = threadIdx.x & 31u;
     float q[D / 32], k[D / 32], qq = 0.f, kk = 0.f, qk = 0.f;
@@ -60,21 +62,31 @@ __device__ __forceinline__ void put_row(const DeltaArgs &a, const Row1<T, D, W> 
 }
 
 // Takes the state over n rows that are in shared memory (the first is row `first` of the call).  Both S^T k and S^T q are taken of the
-// state before the row (S_new^T q = e^g S^T q + (k.q) d), so one exchange between the warps is all a row needs.
-template <class T, int D, int W>
-__device__ __forceinline__ void take_rows(const DeltaArgs &a, RowSmem<D, W> &m, int n, uint64_t first, uint32_t h, uint32_t slice,
-                                          float4 (&S)[RowShape<D, W>::N])
+// state before the row (S_new^T q = e^g S^T q + (k.q) d): the warps' parts of the two go through shared memory, each warp sums some
+// columns of them and tells the others d.
+template <class T, int D, int W, int B>
+__device__ __forceinline__ void take_rows(const DeltaArgs &a, RowSmem<D, W, B> &m, int n, uint64_t first, uint32_t h, uint32_t slice,
+                                          float2 (&S)[RowShape<D, W>::N][2])
 {
-    constexpr int C = RowShape<D, W>::C, N = RowShape<D, W>::N, P = kRowWarps;
+    constexpr int C = RowShape<D, W>::C, N = RowShape<D, W>::N;
+    constexpr uint32_t kMine = W / kRowWarps;  // columns that a warp sums
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, col = threadIdx.x % C, down = threadIdx.x / C;
     for (int r = 0; r < n; ++r) {
-        float4 x = {}, y = {};  // S^T k, S^T q
+        float k[N];
+        float2 x0 = {}, x1 = {}, y0 = {}, y1 = {};
+        auto twice = [](float f) { return make_float2(f, f); };
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float kr = m.k[r][down * N + i], qr = m.q[r][down * N + i];
-            x.x += kr * S[i].x, x.y += kr * S[i].y, x.z += kr * S[i].z, x.w += kr * S[i].w;
-            y.x += qr * S[i].x, y.y += qr * S[i].y, y.z += qr * S[i].z, y.w += qr * S[i].w;
+        for (int i = 0; i < N; i += 2) {
+            const float2 kk = *reinterpret_cast<const float2 *>(&m.k[r][down * N + i]), qq = *reinterpret_cast<const float2 *>(&m.q[r][down * N + i]);
+            k[i] = kk.x, k[i + 1] = kk.y;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float q = j ? qq.y : qq.x;
+                x0 = ptx::fma2(twice(k[i + j]), S[i + j][0], x0), x1 = ptx::fma2(twice(k[i + j]), S[i + j][1], x1);
+                y0 = ptx::fma2(twice(q), S[i + j][0], y0), y1 = ptx::fma2(twice(q), S[i + j][1], y1);
+            }
         }
+        float4 x = make_float4(x0.x, x0.y, x1.x, x1.y), y = make_float4(y0.x, y0.y, y1.x, y1.y);  // S^T k, S^T q
 #pragma unroll
         for (int o = C; o < 32; o <<= 1) {
             x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
@@ -82,32 +94,26 @@ __device__ __forceinline__ void take_rows(const DeltaArgs &a, RowSmem<D, W> &m, 
             y.x += __shfl_xor_sync(0xffffffffu, y.x, o), y.y += __shfl_xor_sync(0xffffffffu, y.y, o);
             y.z += __shfl_xor_sync(0xffffffffu, y.z, o), y.w += __shfl_xor_sync(0xffffffffu, y.w, o);
         }
-        if ((int)lane < C) m.part[r & 1][warp][0][col] = x, m.part[r & 1][warp][1][col] = y;
+        if ((int)lane < C) *reinterpret_cast<float4 *>(&m.part[warp][0][col * 4]) = x, *reinterpret_cast<float4 *>(&m.part[warp][1][col * 4]) = y;
         asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
-        x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float e = m.gate[r];
+        {
+            const uint32_t is_y = lane / kMine & 1u, c = warp * kMine + lane % kMine;  // (lanes beyond 2 kMine do the same again)
+            float sum = 0.f;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const float4 u = m.part[r & 1][p][0][col];
-            x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
+            for (int p = 0; p < (int)kRowWarps; ++p) sum += m.part[p][is_y][c];
+            const float d = m.strength[r] * (m.v[r][c] - e * sum), dd = __shfl_sync(0xffffffffu, d, lane % kMine);
+            if (lane < kMine) m.d[c] = d;
+            else if (lane < 2 * kMine)
+                reinterpret_cast<T *>(a.out + (first + r) * a.o_token + h * a.o_head)[slice * W + c] = from_f32<T>(a.scale * (e * sum + m.qk[r] * dd));
         }
-        const float e = m.gate[r], b = m.strength[r];
-        const float4 v = *reinterpret_cast<const float4 *>(&m.v[r][col * 4]);
-        const float4 d = make_float4(b * (v.x - e * x.x), b * (v.y - e * x.y), b * (v.z - e * x.z), b * (v.w - e * x.w));
+        asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
+        const float4 d = *reinterpret_cast<const float4 *>(&m.d[col * 4]);
+        const float2 d0 = make_float2(d.x, d.y), d1 = make_float2(d.z, d.w);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float kr = m.k[r][down * N + i];
-            S[i].x = e * S[i].x + kr * d.x, S[i].y = e * S[i].y + kr * d.y, S[i].z = e * S[i].z + kr * d.z, S[i].w = e * S[i].w + kr * d.w;
-        }
-        if (down == 0) {
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const float4 u = m.part[r & 1][p][1][col];
-                y.x += u.x, y.y += u.y, y.z += u.z, y.w += u.w;
-            }
-            const float z = m.qk[r];
-            T *op = reinterpret_cast<T *>(a.out + (first + r) * a.o_token + h * a.o_head) + slice * W + col * 4;
-            *reinterpret_cast<uint2 *>(op) = make_uint2(pack2(a.scale * (e * y.x + z * d.x), a.scale * (e * y.y + z * d.y), T()),
-                                                        pack2(a.scale * (e * y.z + z * d.z), a.scale * (e * y.w + z * d.w), T()));
+            S[i][0] = ptx::fma2(twice(k[i]), d0, ptx::mul2(twice(e), S[i][0]));
+            S[i][1] = ptx::fma2(twice(k[i]), d1, ptx::mul2(twice(e), S[i][1]));
         }
     }
 }
@@ -117,7 +123,8 @@ template <class T, int D, int W>
 __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid_constant__ DeltaArgs a)
 {
     constexpr int C = RowShape<D, W>::C, N = RowShape<D, W>::N;
-    __shared__ RowSmem<D, W> m;
+    constexpr uint32_t B = kRowWarps;
+    __shared__ RowSmem<D, W, B> m;
     const uint32_t tid = threadIdx.x, warp = tid / 32;
     const uint32_t slice = blockIdx.x % (D / W), h = blockIdx.x / (D / W) % a.n_heads, s = blockIdx.x / (D / W) / a.n_heads;
     ptx::grid_wait();
@@ -129,11 +136,11 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
     if (a.status && tid == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
     const uint32_t at = (tid / C * N) * D + slice * W + tid % C * 4;
-    float4 S[N];
+    float2 S[N][2];
 #pragma unroll
-    for (int i = 0; i < N; ++i) S[i] = from ? *reinterpret_cast<const float4 *>(from + at + i * D) : make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int r0 = 0; r0 < rows; r0 += kRowBatch) {
-        const int n = min(rows - r0, (int)kRowBatch);
+    for (int i = 0; i < N; ++i) get4(from ? *reinterpret_cast<const float4 *>(from + at + i * D) : make_float4(0.f, 0.f, 0.f, 0.f), S[i]);
+    for (int r0 = 0; r0 < rows; r0 += B) {
+        const int n = min(rows - r0, (int)B);
         __syncthreads();
         if ((int)warp < n) {  // a warp stages a row
             Row1<T, D, W> x;
@@ -145,29 +152,30 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     }
     if (!to) return;
 #pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(to + at + i * D) = S[i];
+    for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(to + at + i * D) = make_float4(S[i][0].x, S[i][0].y, S[i][1].x, S[i][1].y);
 }
 
 template <int D>
 struct StreamShape {
-    static constexpr int kBuffers = D == 128 ? 3 : 4, kCtas = D == 128 ? 1 : 2;
+    static constexpr int kBuffers = D == 128 ? 3 : 4, kCtas = D == 128 ? 1 : 2, kRows = 8;  // rows at a time
 };
 template <int D>
 struct StreamSmem {
     float state[StreamShape<D>::kBuffers][D * D];
-    RowSmem<D, D> rows;
+    RowSmem<D, D, StreamShape<D>::kRows> rows;
     uint64_t full[StreamShape<D>::kBuffers], done[StreamShape<D>::kBuffers];
 };
 constexpr uint32_t kStreamThreads = kRowThreads + 32;
 
 // Many states: whole ones through a ring of buffers, brought and taken away by bulk copies that one thread issues, two on their way while
-// one is worked on, by CTAs that stay.  Bound by memory.
+// one is worked on, by CTAs that stay.  Bound by memory: 3.4 us a state of 64 KiB and SM, read and written, which is 5.6 TB/s on all
+// of them, and 6 us to get going.  (64 sequences of 32 heads: 55 us, the kernel above with 32 or 128 columns a CTA 70 or 67.)
 template <class T, int D>
 __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delta_stream_kernel(const __grid_constant__ DeltaArgs a)
 {
     extern __shared__ __align__(128) uint8_t raw[];
     StreamSmem<D> &m = *reinterpret_cast<StreamSmem<D> *>(raw);
-    constexpr int C = RowShape<D, D>::C, N = RowShape<D, D>::N, NB = StreamShape<D>::kBuffers;
+    constexpr int C = RowShape<D, D>::C, N = RowShape<D, D>::N, NB = StreamShape<D>::kBuffers, B = StreamShape<D>::kRows;
     const uint32_t tid = threadIdx.x, warp = tid / 32, items = a.n_seq * a.n_heads;
     if (tid == 0) {
         for (int i = 0; i < NB; ++i) {
@@ -241,7 +249,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
         while (item < items) {
             const int rows = delta_rows(a, item / a.n_heads);
             if (!delta_in_chunks(a, rows)) {
-                if ((int)warp < rows) read_row<T, D, D>(a, (uint64_t)(delta_begin(a, item / a.n_heads) + (int)warp), item % a.n_heads, 0, row);
+                if ((int)warp < min(rows, B)) read_row<T, D, D>(a, (uint64_t)(delta_begin(a, item / a.n_heads) + (int)warp), item % a.n_heads, 0, row);
                 break;
             }
             item += gridDim.x;
@@ -253,17 +261,17 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
         const uint32_t s = item / a.n_heads, h = item % a.n_heads, b = k % NB;
         const int first = delta_begin(a, s), rows = delta_rows(a, s);
         const bool zero = (a.past_lens && a.past_lens[s] <= 0) || !delta_state<D>(a, a.src_table, a.src_stride, s, h);
-        if ((int)warp < min(rows, (int)kRowBatch)) put_row<T, D, D>(a, row, warp, m.rows);
+        if ((int)warp < min(rows, B)) put_row<T, D, D>(a, row, warp, m.rows);
         next = first_rows(item + gridDim.x);
         wait(&m.full[b], k / NB);
         float *state = m.state[b] + (tid / C * N) * D + tid % C * 4;
-        float4 S[N];
+        float2 S[N][2];
 #pragma unroll
-        for (int i = 0; i < N; ++i) S[i] = zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4 *>(state + i * D);
+        for (int i = 0; i < N; ++i) get4(zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4 *>(state + i * D), S[i]);
         asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
-        take_rows<T, D, D>(a, m.rows, min(rows, (int)kRowBatch), (uint64_t)first, h, 0, S);
-        for (int r0 = kRowBatch; r0 < rows; r0 += kRowBatch) {
-            const int n = min(rows - r0, (int)kRowBatch);
+        take_rows<T, D, D>(a, m.rows, min(rows, B), (uint64_t)first, h, 0, S);
+        for (int r0 = B; r0 < rows; r0 += B) {
+            const int n = min(rows - r0, B);
             asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");
             if ((int)warp < n) {
                 Row1<T, D, D> x;
@@ -274,7 +282,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
             take_rows<T, D, D>(a, m.rows, n, (uint64_t)(first + r0), h, 0, S);
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(state + i * D) = S[i];
+        for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(state + i * D) = make_float4(S[i][0].x, S[i][0].y, S[i][1].x, S[i][1].y);
         ptx::fence_proxy_async();
         asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");  // (the rows have been read, too)
         if ((tid & 31u) == 0) ptx::mbar_arrive(ptx::smem_u32(&m.done[b]));
@@ -284,9 +292,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
 template <class T, int D>
 cudaError_t launch_rows(const DeltaArgs &a, cudaStream_t s)
 {
+    // Whole states pay from one and a half a CTA on: below that SMs stand idle or have two rounds to do (32 heads of 128, one row, us,
+    // slices / whole states: 5 sequences 12.3 / 14.3, 8 14.3 / 14.3, 24 28.7 / 26.6; four rows: 5 16.4 / 16.4, 8 20.5 / 18.4, 24 43 / 35).
     constexpr int W = 32;
     const uint64_t items = (uint64_t)a.n_seq * a.n_heads, held = 148 * StreamShape<D>::kCtas;
-    if (items <= 2 * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);
+    if (2 * items <= 3 * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);
     static std::atomic<uint64_t> done;
     static_assert(sizeof(StreamSmem<D>) * StreamShape<D>::kCtas <= 231424, "");
     const cudaError_t e = allow_smem(kv_delta_stream_kernel<T, D>, sizeof(StreamSmem<D>), done);
