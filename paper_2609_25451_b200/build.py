@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libgms.so")
 SOURCES = ["gms_api.cu", "gms_stream_kernels.cu", "gms_verify_kernels.cu", "gms_build_kernels.cu", "gms_noalloc.cu", "gms_pipe.cu",
            "gms_service.cu", "gms_kv_attention.cu", "gms_kv_few.cu", "gms_kv_tc.cu", "gms_kv_join.cu", "gms_kv_weights.cu",
            "gms_kv_evict.cu", "gms_kv_plan.cu", "gms_kv_append.cu", "gms_kv_delta.cu",
-           "gms_kv_delta_chunk.cu"]
+           "gms_kv_delta_prep.cu", "gms_kv_delta_chain.cu"]
 HEADERS = [os.path.join(CSRC, "gms_internal.h"), os.path.join(CSRC, "gms_kv_attn.h"), os.path.join(CSRC, "gms_ptx.h"), os.path.join(CSRC, "gms_tcgen05.h"),
            os.path.join(CSRC, "gms_kv_delta.h"),
            os.path.join(ROOT, "include", "gms.h")]

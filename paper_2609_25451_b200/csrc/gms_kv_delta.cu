@@ -404,7 +404,8 @@ int gms_kv_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_k
     if (slots) {
         a.chunks = static_cast<uint8_t *>(args->workspace);
         a.n_slots = (uint32_t)slots;
-        e = gms::launch_delta_chunks(a, args->dtype, state->head_dim, s);
+        e = gms::launch_delta_prep(a, args->dtype, state->head_dim, s);
+        if (e == cudaSuccess) e = gms::launch_delta_chain(a, args->dtype, state->head_dim, s);
         if (e != cudaSuccess) return gms::report_cuda_error(e);
     }
     if (state->head_dim == 128)

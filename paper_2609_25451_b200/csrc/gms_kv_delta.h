@@ -34,7 +34,9 @@ struct alignas(256) ChunkWork {
     uint32_t by_row;
 };
 
-cudaError_t launch_delta_chunks(const DeltaArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+// What comes before the states' chain, for all chunks at once; the chain.
+cudaError_t launch_delta_prep(const DeltaArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
+cudaError_t launch_delta_chain(const DeltaArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ int delta_begin(const DeltaArgs &a, uint32_t s) { return a.cu_q ? min(max(a.cu_q[s], 0), (int)a.total_q) : (int)s; }
@@ -54,6 +56,45 @@ __device__ __forceinline__ float *delta_state(const DeltaArgs &a, const int32_t 
     if ((uint32_t)id >= a.n_blocks) return nullptr;
     return reinterpret_cast<float *>(a.plane + (uint64_t)id * a.block_stride) + (uint64_t)(h % a.per_block) * D * D;
 }
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+
+// Byte offset of 16-byte piece c of row r in a tile of P pieces a row, so that eight neighbouring rows' pieces c lie in different banks.
+template <int P>
+__device__ __forceinline__ uint32_t piece(uint32_t r, uint32_t c)
+{
+    return (r * P + (P >= 8 ? c ^ (r & 7u) : c ^ ((r * P / 8) & (P - 1u)))) * 16;
+}
+
+// The same in a lower triangle's blocks of 16 x 16 16-bit numbers: piece c (of the 8 of a whole row), c / 2 <= r / 16.
+__device__ __forceinline__ uint32_t block_piece(uint32_t r, uint32_t c)
+{
+    const uint32_t b = r / 16;
+    return (b * (b + 1) / 2 + c / 2) * 512 + (r % 16 * 2 + ((c ^ (r / 4)) & 1u)) * 16;
+}
+
+// x = hi + lo with both of type T (2^-17 relative in bf16, the rest of f16's range aside).
+template <class T>
+__device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo)
+{
+    hi = pack2(x, y, T());
+    const T *e = reinterpret_cast<const T *>(&hi);
+    lo = pack2(x - to_f32(e[0]), y - to_f32(e[1]), T());
+}
+
+// A power of two by which a row of f16 terms is scaled so that its largest is below 2^12 (bf16 has the range of 32 bits); within
+// 2^-30 .. 2^30, so that three such factors together stay far from the ends of 32 bits.
+__device__ __forceinline__ float range_scale(float top)
+{
+    const int e = (int)(__float_as_uint(top) >> 23 & 255u) - 127;  // 2^e <= top
+    return __uint_as_float((uint32_t)(127 + min(max(11 - e, -30), 30)) << 23);
+}
+
+// 1 / u for a power of two.
+__device__ __forceinline__ float flipped(float u) { return __uint_as_float(0x7f000000u - __float_as_uint(u)); }
 #endif
 
 }  // namespace gms

@@ -1,0 +1,828 @@
+// The gated delta rule in chunks: the chain of the states (what its operands are stands at the kernel that makes them).
+#include "gms_kv_delta.h"
+
+namespace gms {
+namespace {
+
+using ptx::ldmatrix_x4;
+using ptx::ldmatrix_x4_trans;
+using ptx::smem_u32;
+
+// A chunk's operands.  V is the columns of the CTA, 16 for each of its W slices.
+template <int D, int W>
+struct Stage {
+    uint8_t k[kChunkRows * D * 2], q[kChunkRows * D * 2], v[kChunkRows * W * 32];
+    ChunkWork w;
+};
+
+// A tile of 64 rows, PR pieces each; rows from n on are zeros.  A lane keeps to one piece of the rows that it copies.
+template <int PR, uint32_t kFetchLanes>
+__device__ __forceinline__ void fetch_rows(uint32_t tile, uint32_t me, const uint8_t *src, uint64_t stride, int n)
+{
+    constexpr uint32_t kStep = kFetchLanes / PR, N = kChunkRows / kStep;
+    static_assert(kStep * PR == kFetchLanes, "");
+    const uint32_t c = me % PR, r0 = me / PR;
+    src += r0 * stride + c * 16;
+    if (n >= (int)kChunkRows) {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+            cp16(tile + piece<PR>(r0 + i * kStep, c), src, true);
+            src += kStep * stride;
+        }
+    } else {
+#pragma unroll 1
+        for (uint32_t r = r0; r < (uint32_t)kChunkRows; r += kStep) {
+            const bool real = (int)r < n;
+            cp16(tile + piece<PR>(r, c), real ? src : src - r * stride, real);
+            src += kStep * stride;
+        }
+    }
+}
+// Chunk `chunk` of a sequence; `full` is told when it has landed.
+template <int D, int W, uint32_t kLanes>
+__device__ __forceinline__ void fetch_chunk(const DeltaArgs &a, Stage<D, W> &st, uint32_t me, int chunk, int rows, int first, uint32_t kh, uint32_t h,
+                                            uint32_t col0, uint32_t slot, uint32_t full)
+{
+    const int n = rows - chunk * (int)kChunkRows;
+    const uint64_t row = (uint64_t)(first + chunk * (int)kChunkRows);
+    const uint8_t *work = a.chunks + ((uint64_t)(slot + chunk) * a.n_heads + h) * sizeof(ChunkWork) + me * 16;
+    const uint32_t to = smem_u32(&st.w) + me * 16;
+    fetch_rows<D / 8, kLanes>(smem_u32(st.k), me, a.k + row * a.k_token + kh * a.k_head, a.k_token, n);
+    fetch_rows<W * 2, kLanes>(smem_u32(st.v), me, a.v + row * a.v_token + h * a.v_head + col0 * 2, a.v_token, n);
+    constexpr uint32_t kPieces = sizeof(ChunkWork) / 16;
+#pragma unroll
+    for (uint32_t i = 0; i < kPieces / kLanes; ++i) cp16(to + i * 16 * kLanes, work + i * 16 * kLanes, true);
+    if (kPieces % kLanes && me < kPieces % kLanes) cp16(to + kPieces / kLanes * 16 * kLanes, work + kPieces / kLanes * 16 * kLanes, true);
+    fetch_rows<D / 8, kLanes>(smem_u32(st.q), me, a.q + row * a.q_token + kh * a.q_head, a.q_token, n);
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------------ few states
+// What the warps of a slice tell each other: accumulators, and first factors of products (a lane's part of 16 x 16).
+template <int D>
+struct Talk {
+    uint4 s[2][D / 16][32];    // S before a chunk and the next, the first of its two terms
+    float4 sum[4][3][2][32];   // [to][from the others]: what X is the sum of
+    uint4 x[4][2][32];         // V - f X of the 16 rows of each warp, in two terms
+    uint4 dw[4][2][32];        // w d, in two terms
+    uint4 d[2][4][32];
+    float2 s_unit[2][4][8], x_unit[4][8], dw_unit[4][8], d_unit[2][4][8];  // f16: powers of two that rows' terms are multiples of
+    uint32_t odd[2][4];        // the chunk is done row by row
+};
+template <int D, int W>
+struct RelayShape {
+    static constexpr int kStages = 3;
+    static constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32, kThreads = (5 * W + kFetchWarps) * 32;
+};
+template <int D, int W>
+struct RelaySmem {
+    Stage<D, W> stage[3];
+    Talk<D> talk[W];
+    uint64_t full[3], empty[3], ready[W][2], taken[W][2];
+};
+
+// A slice, 16 value columns of a head's state, has four warps that carry the state on and one that makes `out`.  The state lies,
+// transposed, in accumulators of mma.sync, the columns of D / 4 keys a warp; what is an accumulator of one product is, element for
+// element, a first factor of the next: S -> X = S K^T (each warp its keys' part, for all rows) -> d = (V - f X) T^T -> S, each warp
+// 16 of the rows in between, with three exchanges through shared memory a chunk.  The fifth warp gets S and d handed and works
+// beside the next chunk.  W slices share a chunk's operands, which two more warps fetch ahead.  Bound by the latency of that
+// sequence of small products and exchanges: @@
+template <class T, int D, int W>
+__global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_kernel(const __grid_constant__ DeltaArgs a)
+{
+    extern __shared__ __align__(16) uint8_t raw[];
+    RelaySmem<D, W> &m = *reinterpret_cast<RelaySmem<D, W> *>(raw);
+    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 32, KQ = D / 64;  // tiles of 8 and of 16 keys that a warp has
+    constexpr int kStages = RelayShape<D, W>::kStages;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
+    constexpr uint32_t kParts = D / (16 * W);
+    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, s = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
+    const uint32_t col0 = part * W * 16;  // of the CTA
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+    const int rows = delta_rows(a, s), first = delta_begin(a, s);
+    if (!delta_in_chunks(a, rows)) return;
+    const int chunks = (rows + C - 1) / C;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            ptx::mbar_init(smem_u32(&m.full[i]), RelayShape<D, W>::kFetchLanes);
+            ptx::mbar_init(smem_u32(&m.empty[i]), 5 * W);
+        }
+        for (int i = 0; i < W; ++i)
+            for (int j = 0; j < 2; ++j) {
+                ptx::mbar_init(smem_u32(&m.ready[i][j]), 4);
+                ptx::mbar_init(smem_u32(&m.taken[i][j]), 1);
+            }
+        ptx::fence_mbar_init();
+    }
+    __syncthreads();
+    // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
+    bool late = false;
+    auto wait = [&](uint64_t *bar, int use) {
+        if (late || ptx::mbar_wait(smem_u32(bar), (uint32_t)(use & 1))) return;
+        late = true;
+        if (a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+    };
+    auto arrive = [&](uint64_t *bar) {  // of a warp
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(smem_u32(bar));
+    };
+    if (warp >= 5 * W) {  // the fetching warps
+        const uint32_t me = (warp - 5 * W) * 32 + lane, slot = delta_slot(a, s);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int i = chunk % kStages;
+            if (chunk >= kStages) wait(&m.empty[i], chunk / kStages - 1);
+            fetch_chunk<D, W, RelayShape<D, W>::kFetchLanes>(a, m.stage[i], me, chunk, rows, first, kh, h, col0, slot, smem_u32(&m.full[i]));
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
+    const uint32_t g = lane / 4, t2 = 2 * (lane & 3u);  // rows g and g + 8, columns 8 nt + t2 + {0, 1} of an accumulator
+    const uint32_t b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;  // of a lane's address for two second factors
+    const float2 one = make_float2(1.f, 1.f);
+    // f16: accumulators go over to the unit of the next factors
+    auto change = [](float(*x)[4], float2 now, float2 next) {
+        const float f0 = now.x * flipped(next.x), f1 = now.y * flipped(next.y);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
+    };
+    if (warp >= 4 * W) {
+        // out = h Q S + P d, with S before the chunk (one term each), two tiles of 16 rows at a time
+        const uint32_t slice = warp - 4 * W;
+        Talk<D> &talk = m.talk[slice];
+#pragma unroll 1
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int stage = chunk % kStages, turn = chunk & 1, n = min(rows - chunk * C, C);
+            Stage<D, W> &st = m.stage[stage];
+            uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
+            wait(&m.full[stage], chunk / kStages);
+            wait(&m.ready[slice][turn], chunk / 2);
+            if (!(talk.odd[turn][0] | talk.odd[turn][1] | talk.odd[turn][2] | talk.odd[turn][3])) {
+                uint4 sf[D / 16], df[4];
+#pragma unroll
+                for (int kt = 0; kt < D / 16; ++kt) sf[kt] = talk.s[turn][kt][lane];
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) df[kt] = talk.d[turn][kt][lane];
+#pragma unroll
+                for (int pair = 0; pair < 2; ++pair) {
+                    float Y[2][2][4] = {};
+                    float2 unit = one;
+#pragma unroll
+                    for (int kt = 0; kt < D / 16; ++kt) {
+                        if (kHalf && kt % KQ == 0) {
+                            const float2 next = talk.s_unit[turn][kt / KQ][g];
+                            if (kt) change(Y[0], unit, next), change(Y[1], unit, next);
+                            unit = next;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t b[4];
+                            ldmatrix_x4(smem_u32(st.q) + piece<P>(32 * pair + 16 * i + b_row, 2 * kt + b_piece), b);
+                            mma16816(Y[i][0], &sf[kt].x, b[0], b[1], T());
+                            mma16816(Y[i][1], &sf[kt].x, b[2], b[3], T());
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int tile = 2 * pair + i;
+                        if (kHalf) change(Y[i], unit, one);
+#pragma unroll
+                        for (int nt = 0; nt < 2; ++nt) {
+                            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[16 * tile + 8 * nt + t2]);
+                            Y[i][nt][0] *= f.x, Y[i][nt][1] *= f.y, Y[i][nt][2] *= f.x, Y[i][nt][3] *= f.y;
+                        }
+                        float2 u = one;
+#pragma unroll
+                        for (int kt = 0; kt < 4; ++kt) {
+                            if (kt > tile) break;
+                            if (kHalf) {
+                                const float2 next = talk.d_unit[turn][kt][g];
+                                change(Y[i], u, next);
+                                u = next;
+                            }
+                            uint32_t b[4];
+                            ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(16 * tile + b_row, 2 * kt + b_piece), b);
+                            mma16816(Y[i][0], &df[kt].x, b[0], b[1], T());
+                            mma16816(Y[i][1], &df[kt].x, b[2], b[3], T());
+                        }
+                        if (kHalf) change(Y[i], u, one);
+                        // (through the slice's part of V's tile, which the other warps have read)
+                        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                                         smem_u32(st.v) + piece<VP>(16 * tile + b_row, 2 * slice + b_piece)),
+                                     "r"(pack2(Y[i][0][0], Y[i][0][1], T())), "r"(pack2(Y[i][0][2], Y[i][0][3], T())),
+                                     "r"(pack2(Y[i][1][0], Y[i][1][1], T())), "r"(pack2(Y[i][1][2], Y[i][1][3], T()))
+                                     : "memory");
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < C / 16; ++i) {
+                    const int r = 16 * i + (int)lane / 2;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
+                    if (r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
+                }
+            }
+            arrive(&m.taken[slice][turn]);
+            arrive(&m.empty[stage]);
+        }
+        return;
+    }
+    // (the last rows have most to do: of two slices they go to different quarters of the SM)
+    const uint32_t slice = warp / 4, mine = (warp & 3u) ^ (slice & 1u ? 3u : 0u), row0 = 16 * mine;
+    Talk<D> &talk = m.talk[slice];
+    const bool fresh = a.past_lens && a.past_lens[s] <= 0;
+    const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
+    float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
+    if (a.status && threadIdx.x == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+    const uint32_t at0 = (mine * (D / 4) + t2) * D + col0 + 16 * slice + g;
+    float S[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] : 0.f;
+    auto together = [&] { asm volatile("bar.sync %0, 128;" ::"r"(slice + 1) : "memory"); };
+    auto seat = [](uint32_t to, uint32_t from) { return from < to ? from : from - 1; };  // the place that one of four has among the other three
+    // f16: the scales of a lane's two rows of the 16 x 16 in accumulators x and y
+    auto top_of = [](const float *x, const float *y, int e) {
+        float top = fmaxf(fmaxf(fabsf(x[2 * e]), fabsf(x[2 * e + 1])), fmaxf(fabsf(y[2 * e]), fabsf(y[2 * e + 1])));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    };
+    auto scales = [&](const float *x, const float *y) { return make_float2(range_scale(top_of(x, y, 0)), range_scale(top_of(x, y, 1))); };
+    auto inverse = [](float2 u) { return make_float2(flipped(u.x), flipped(u.y)); };
+    auto tell = [&](float2 *unit, float2 u) {
+        if ((lane & 3u) == 0) unit[g] = u;
+    };
+    auto terms = [](const float *x, const float *y, float2 u, uint4 &hi, uint4 &lo) {
+        split2<T>(x[0] * u.x, x[1] * u.x, hi.x, lo.x);
+        split2<T>(x[2] * u.y, x[3] * u.y, hi.y, lo.y);
+        split2<T>(y[0] * u.x, y[1] * u.x, hi.z, lo.z);
+        split2<T>(y[2] * u.y, y[3] * u.y, hi.w, lo.w);
+    };
+#pragma unroll 1
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int stage = chunk % kStages, turn = chunk & 1, n = min(rows - chunk * C, C);
+        Stage<D, W> &st = m.stage[stage];
+        wait(&m.full[stage], chunk / kStages);
+        if (chunk >= 2) wait(&m.taken[slice][turn], chunk / 2 - 1);
+        // what needs no news from the other warps is read before they meet
+        uint32_t kb[4][KQ][4], V[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < KQ; ++k) ldmatrix_x4(smem_u32(st.k) + piece<P>(16 * i + b_row, 2 * (mine * KQ + k) + b_piece), kb[i][k]);
+        ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(row0 + b_row, 2 * slice + b_piece), V);
+        // S in two terms
+        uint4 hi[KQ], lo[KQ];
+        float2 su = one;
+        if (kHalf) {
+            su = scales(S[0], S[1]);
+#pragma unroll
+            for (int k = 1; k < KQ; ++k) {
+                const float2 u = scales(S[2 * k], S[2 * k + 1]);
+                su = make_float2(fminf(su.x, u.x), fminf(su.y, u.y));
+            }
+            tell(talk.s_unit[turn][mine], inverse(su));
+        }
+#pragma unroll
+        for (int k = 0; k < KQ; ++k) {
+            terms(S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
+            talk.s[turn][mine * KQ + k][lane] = hi[k];
+        }
+        // its part of X = S K^T for all rows
+        float x[4][2][4] = {};
+#pragma unroll
+        for (int k = 0; k < KQ; ++k)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    mma16816(x[i][0], t ? &lo[k].x : &hi[k].x, kb[i][k][0], kb[i][k][1], T());
+                    mma16816(x[i][1], t ? &lo[k].x : &hi[k].x, kb[i][k][2], kb[i][k][3], T());
+                }
+        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
+        uint32_t odd = st.w.by_row;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= ((V[e] & kOnes) == kOnes) | ((V[e] >> 16 & kOnes) == kOnes);
+        odd = __any_sync(0xffffffffu, odd);
+        if (lane == 0) talk.odd[turn][mine] = odd;
+        float X[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (kHalf) change(x[i], inverse(su), one);
+            if (i == (int)mine) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) X[0][e] = x[i][0][e], X[1][e] = x[i][1][e];
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) talk.sum[i][seat(i, mine)][nt][lane] = make_float4(x[i][nt][0], x[i][nt][1], x[i][nt][2], x[i][nt][3]);
+            }
+        }
+        uint32_t tb[2][C / 16][4];
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kt > (int)mine) break;
+            const uint32_t at = block_piece(row0 + b_row, 2 * kt + b_piece);
+            ldmatrix_x4(smem_u32(st.w.tile[0]) + at, tb[0][kt]);
+            ldmatrix_x4(smem_u32(st.w.tile[1]) + at, tb[1][kt]);
+        }
+        together();
+        if (talk.odd[turn][0] | talk.odd[turn][1] | talk.odd[turn][2] | talk.odd[turn][3]) {
+            // row by row: something here is not finite, and in a product it would reach rows that come before it
+            arrive(&m.ready[slice][turn]);
+            uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
+            float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(talk.x);  // [2][4][32], in the place of what is not needed
+            float(*zs)[4][32] = reinterpret_cast<float(*)[4][32]>(talk.dw);
+#pragma unroll 1
+            for (int r = 0; r < n; ++r) {
+                const float gate = st.w.gate[r], beta = st.w.beta[r], rk = st.w.rk[r], rq = st.w.rq[r];
+                float p[2] = {}, y[2] = {}, z = 0.f, kv[2 * NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, mine * NT + nt)) + t2;
+                    const T *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, mine * NT + nt)) + t2;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float k = to_f32(kp[e]) * rk, q = to_f32(qp[e]) * rq;
+                        kv[2 * nt + e] = k;
+                        z += k * q;
+                        S[nt][e] *= gate, S[nt][2 + e] *= gate;
+                        p[0] += S[nt][e] * k, p[1] += S[nt][2 + e] * k;
+                        y[0] += S[nt][e] * q, y[1] += S[nt][2 + e] * q;
+                    }
+                }
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    z += __shfl_xor_sync(0xffffffffu, z, o);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) p[e] += __shfl_xor_sync(0xffffffffu, p[e], o), y[e] += __shfl_xor_sync(0xffffffffu, y[e], o);
+                }
+                xy[r & 1][mine][lane] = make_float4(p[0], p[1], y[0], y[1]);
+                zs[r & 1][mine][lane] = z;
+                together();
+                p[0] = p[1] = y[0] = y[1] = z = 0.f;
+#pragma unroll
+                for (int o = 0; o < 4; ++o) {
+                    const float4 u = xy[r & 1][o][lane];
+                    p[0] += u.x, p[1] += u.y, y[0] += u.z, y[1] += u.w;
+                    z += zs[r & 1][o][lane];
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float v = to_f32(*reinterpret_cast<const T *>(st.v + piece<VP>(r, 2 * slice + e) + g * 2));
+                    const float d = beta * (v - p[e]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) S[nt][2 * e] += kv[2 * nt] * d, S[nt][2 * e + 1] += kv[2 * nt + 1] * d;
+                    if (mine == 0 && (lane & 3u) == 0)
+                        reinterpret_cast<T *>(out + (uint64_t)r * a.o_token)[g + 8 * e] = from_f32<T>(a.scale * (y[e] + z * d));
+                }
+            }
+            arrive(&m.empty[stage]);
+            continue;
+        }
+        // what the values differ by from what the state says: X <- V - f X, for the warp's rows
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+            for (int o = 0; o < 3; ++o) {
+                const float4 u = talk.sum[mine][o][nt][lane];
+                X[nt][0] += u.x, X[nt][1] += u.y, X[nt][2] += u.z, X[nt][3] += u.w;
+            }
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[row0 + 8 * nt + t2]);
+            const T *va = reinterpret_cast<const T *>(&V[2 * nt]), *vb = reinterpret_cast<const T *>(&V[2 * nt + 1]);
+            X[nt][0] = to_f32(va[0]) - f.x * X[nt][0];
+            X[nt][1] = to_f32(va[1]) - f.y * X[nt][1];
+            X[nt][2] = to_f32(vb[0]) - f.x * X[nt][2];
+            X[nt][3] = to_f32(vb[1]) - f.y * X[nt][3];
+        }
+        float2 u = one;
+        if (kHalf) {
+            u = scales(X[0], X[1]);
+            tell(talk.x_unit[mine], inverse(u));
+        }
+        uint4 own_hi, own_lo;
+        terms(X[0], X[1], u, own_hi, own_lo);
+        talk.x[mine][0][lane] = own_hi, talk.x[mine][1][lane] = own_lo;
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt)
+#pragma unroll
+            for (int k = 0; k < KQ; ++k)
+                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + 2 * k + lane / 16), kb[kt][k]);
+        together();
+        // d = X T^T: two terms each (the product of the small ones left out), from the rows up to the warp's own
+        float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
+        float2 unit = one;
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kt > (int)mine) break;
+            if (kHalf) {
+                const float2 next = talk.x_unit[kt][g];
+                if (kt) change(d, unit, next), change(dl, unit, next), change(dt, unit, next);
+                unit = next;
+            }
+            const uint4 p = kt == (int)mine ? own_hi : talk.x[kt][0][lane], q = kt == (int)mine ? own_lo : talk.x[kt][1][lane];
+            mma16816(d[0], &p.x, tb[0][kt][0], tb[0][kt][1], T());
+            mma16816(d[1], &p.x, tb[0][kt][2], tb[0][kt][3], T());
+            mma16816(dl[0], &q.x, tb[0][kt][0], tb[0][kt][1], T());
+            mma16816(dl[1], &q.x, tb[0][kt][2], tb[0][kt][3], T());
+            mma16816(dt[0], &p.x, tb[1][kt][0], tb[1][kt][1], T());
+            mma16816(dt[1], &p.x, tb[1][kt][2], tb[1][kt][3], T());
+        }
+        const float f0 = kHalf ? st.w.t_unit * unit.x : 1.f, f1 = kHalf ? st.w.t_unit * unit.y : 1.f;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[nt][e] = (d[nt][e] + (dl[nt][e] + dt[nt][e])) * (e & 2 ? f1 : f0);
+        u = one;
+        if (kHalf) {
+            u = scales(d[0], d[1]);
+            tell(talk.d_unit[turn][mine], make_float2(st.w.p_unit * flipped(u.x), st.w.p_unit * flipped(u.y)));
+        }
+        talk.d[turn][mine][lane] = make_uint4(pack2(d[0][0] * u.x, d[0][1] * u.x, T()), pack2(d[0][2] * u.y, d[0][3] * u.y, T()),
+                                              pack2(d[1][0] * u.x, d[1][1] * u.x, T()), pack2(d[1][2] * u.y, d[1][3] * u.y, T()));
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
+            d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
+        }
+        u = one;
+        if (kHalf) {
+            u = scales(d[0], d[1]);
+            tell(talk.dw_unit[mine], inverse(u));
+        }
+        terms(d[0], d[1], u, own_hi, own_lo);
+        talk.dw[mine][0][lane] = own_hi, talk.dw[mine][1][lane] = own_lo;
+        // S <- e^G S + (w d) K for the warp's keys
+        const float all = st.w.all;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[nt][e] *= all;
+        arrive(&m.ready[slice][turn]);
+        together();
+        unit = one;
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kHalf) {
+                const float2 next = talk.dw_unit[kt][g];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, next);
+                unit = next;
+            }
+            const uint4 p = kt == (int)mine ? own_hi : talk.dw[kt][0][lane], q = kt == (int)mine ? own_lo : talk.dw[kt][1][lane];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], t ? &q.x : &p.x, kb[kt][nt / 2][2 * (nt & 1)], kb[kt][nt / 2][2 * (nt & 1) + 1], T());
+        }
+        if (kHalf) {
+#pragma unroll
+            for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, one);
+        }
+        arrive(&m.empty[stage]);
+    }
+    if (!to) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
+}
+
+// ------------------------------------------------------------------------------------------------ many states
+// W warps with states, and warps that fetch.
+template <int D, int W>
+struct SoloShape {
+    static constexpr int kStages = D == 64 && W == 4 ? 2 : 3;  // that fit (two CTAs an SM there)
+    static constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32, kThreads = (W + kFetchWarps) * 32;
+    static constexpr uint32_t kCtas = D == 64 && W == 4 ? 2 : 1;
+};
+template <int D, int W>
+struct SoloSmem {
+    Stage<D, W> stage[SoloShape<D, W>::kStages];
+    uint64_t full[3], empty[3];
+};
+
+// A warp has 16 value columns of a head's state, transposed, as accumulators of mma.sync (16 x D): what is an accumulator of one
+// product is, element for element, a first factor of the next, S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out, so nothing
+// leaves the registers between the products and no warp waits for another.  W of them (16 W columns of a head) share a chunk's
+// operands, which further warps fetch ahead.  Bound by the rate of the products: 400 of them a chunk and warp, 8.3 cycles each.
+template <class T, int D, int W>
+__global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kCtas) kv_delta_solo_kernel(const __grid_constant__ DeltaArgs a)
+{
+    extern __shared__ __align__(16) uint8_t raw[];
+    SoloSmem<D, W> &m = *reinterpret_cast<SoloSmem<D, W> *>(raw);
+    constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 8, CT = C / 8;
+    constexpr int kStages = SoloShape<D, W>::kStages;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
+    constexpr uint32_t kParts = D / (16 * W);
+    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, s = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
+    const uint32_t col0 = part * W * 16;  // of the CTA
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+    const int rows = delta_rows(a, s), first = delta_begin(a, s);
+    if (!delta_in_chunks(a, rows)) return;
+    const int chunks = (rows + C - 1) / C;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            ptx::mbar_init(smem_u32(&m.full[i]), SoloShape<D, W>::kFetchLanes);
+            ptx::mbar_init(smem_u32(&m.empty[i]), W);
+        }
+        ptx::fence_mbar_init();
+    }
+    __syncthreads();
+    // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
+    bool late = false;
+    auto wait = [&](uint64_t *bar, int use) {
+        if (late || ptx::mbar_wait(smem_u32(bar), (uint32_t)(use & 1))) return;
+        late = true;
+        if (a.status) atomicOr(a.status, (unsigned long long)GMS_DEV_TIMEOUT);
+    };
+    if (warp >= W) {  // the fetching warps
+        const uint32_t me = (warp - W) * 32 + lane, slot = delta_slot(a, s);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int i = chunk % kStages;
+            if (chunk >= kStages) wait(&m.empty[i], chunk / kStages - 1);
+            fetch_chunk<D, W, SoloShape<D, W>::kFetchLanes>(a, m.stage[i], me, chunk, rows, first, kh, h, col0, slot, smem_u32(&m.full[i]));
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
+    const bool fresh = a.past_lens && a.past_lens[s] <= 0;
+    const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
+    float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
+    if (a.status && threadIdx.x == 0 && ((!fresh && !from) || !to)) atomicOr(a.status, (unsigned long long)GMS_DEV_HOLE);
+    const uint32_t g = lane / 4, t2 = 2 * (lane & 3u);  // rows g and g + 8, columns 8 nt + t2 + {0, 1} of an accumulator
+    const uint32_t at0 = t2 * D + col0 + 16 * warp + g;
+    const uint32_t b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;  // of a lane's address for two second factors
+    float S[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] : 0.f;
+    // f16: rows (e = 0, 1: g and g + 8) are scaled by powers of two of their own before they are rounded
+    auto scale_of = [](const float(*x)[4], int tiles, int e) {
+        float top = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < tiles; ++nt) top = fmaxf(top, fmaxf(fabsf(x[nt][2 * e]), fabsf(x[nt][2 * e + 1])));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        return range_scale(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
+    };
+    auto terms = [](const float(*x)[4], float u0, float u1, uint32_t *hi, uint32_t *lo) {  // of the 16 x 16 in accumulators x[0] and x[1]
+        split2<T>(x[0][0] * u0, x[0][1] * u0, hi[0], lo[0]);
+        split2<T>(x[0][2] * u1, x[0][3] * u1, hi[1], lo[1]);
+        split2<T>(x[1][0] * u0, x[1][1] * u0, hi[2], lo[2]);
+        split2<T>(x[1][2] * u1, x[1][3] * u1, hi[3], lo[3]);
+    };
+#pragma unroll 1
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int stage = chunk % kStages;
+        Stage<D, W> &st = m.stage[stage];
+        const int n = min(rows - chunk * C, C);
+        uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * warp) * 2;
+        auto done = [&] {
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(smem_u32(&m.empty[stage]));
+        };
+        wait(&m.full[stage], chunk / kStages);
+        // the columns' values, transposed like everything else
+        uint32_t V[CT][2];
+        uint32_t odd = st.w.by_row;
+        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
+#pragma unroll
+        for (int nt = 0; nt < CT; nt += 2) {
+            uint32_t b[4];
+            ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * warp + b_piece), b);
+            V[nt][0] = b[0], V[nt][1] = b[1], V[nt + 1][0] = b[2], V[nt + 1][1] = b[3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= ((b[e] & kOnes) == kOnes) | ((b[e] >> 16 & kOnes) == kOnes);
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+            // row by row: something here is not finite, and in a product it would reach rows that come before it
+#pragma unroll 1
+            for (int r = 0; r < n; ++r) {
+                const float gate = st.w.gate[r], beta = st.w.beta[r], rk = st.w.rk[r], rq = st.w.rq[r];
+                float x[2] = {}, y[2] = {}, z = 0.f;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, nt)) + t2, *qp = reinterpret_cast<const T *>(st.q + piece<P>(r, nt)) + t2;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float k = to_f32(kp[e]) * rk, q = to_f32(qp[e]) * rq;
+                        z += k * q;
+                        S[nt][e] *= gate, S[nt][2 + e] *= gate;
+                        x[0] += S[nt][e] * k, x[1] += S[nt][2 + e] * k;
+                        y[0] += S[nt][e] * q, y[1] += S[nt][2 + e] * q;
+                    }
+                }
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    z += __shfl_xor_sync(0xffffffffu, z, o);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], o), y[e] += __shfl_xor_sync(0xffffffffu, y[e], o);
+                }
+                float d[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    d[e] = beta * (to_f32(*reinterpret_cast<const T *>(st.v + piece<VP>(r, 2 * warp + e) + g * 2)) - x[e]);
+                    if ((lane & 3u) == 0) reinterpret_cast<T *>(out + (uint64_t)r * a.o_token)[g + 8 * e] = from_f32<T>(a.scale * (y[e] + z * d[e]));
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const T *kp = reinterpret_cast<const T *>(st.k + piece<P>(r, nt)) + t2;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float k = to_f32(kp[e]) * rk;
+                        S[nt][e] += k * d[0], S[nt][2 + e] += k * d[1];
+                    }
+                }
+            }
+            done();
+            continue;
+        }
+        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
+        float X[CT][4] = {}, Y[CT][4] = {};
+        float u0 = 1.f, u1 = 1.f;
+        if (kHalf) u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
+#pragma unroll
+        for (int kt = 0; kt < D / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2], c[CT][2];
+#pragma unroll
+            for (int nt = 0; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+            terms(S + 2 * kt, u0, u1, hi, lo);
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 0; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
+                c[nt][0] = x[0], c[nt][1] = x[1], c[nt + 1][0] = x[2], c[nt + 1][1] = x[3];
+            }
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], lo, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(Y[nt], hi, c[nt][0], c[nt][1], T());
+        }
+        // what the values differ by from what the state says: X <- V - f X
+        const float si0 = flipped(u0), si1 = flipped(u1);
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
+            const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
+            X[nt][0] = to_f32(va[0]) - f.x * (kHalf ? X[nt][0] * si0 : X[nt][0]);
+            X[nt][1] = to_f32(va[1]) - f.y * (kHalf ? X[nt][1] * si0 : X[nt][1]);
+            X[nt][2] = to_f32(vb[0]) - f.x * (kHalf ? X[nt][2] * si1 : X[nt][2]);
+            X[nt][3] = to_f32(vb[1]) - f.y * (kHalf ? X[nt][3] * si1 : X[nt][3]);
+        }
+        if (kHalf) u0 = scale_of(X, CT, 0), u1 = scale_of(X, CT, 1);
+        // d = X T^T: two terms each (the product of the small ones left out); T's columns beyond a row's own are zero
+        float d[CT][4] = {};
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2];
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[0]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+            terms(X + 2 * kt, u0, u1, hi, lo);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[1]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                mma16816(d[nt], hi, x[0], x[1], T());
+                mma16816(d[nt + 1], hi, x[2], x[3], T());
+            }
+        }
+        float di0 = 1.f, di1 = 1.f;
+        if (kHalf) {
+            const float i0 = st.w.t_unit * flipped(u0), i1 = st.w.t_unit * flipped(u1);
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) d[nt][0] *= i0, d[nt][1] *= i0, d[nt][2] *= i1, d[nt][3] *= i1;
+            u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
+            di0 = st.w.p_unit * flipped(u0), di1 = st.w.p_unit * flipped(u1);
+        }
+        // out = h Y + P d (one term each; f16: in units of P and d meanwhile)
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
+            if (kHalf) Y[nt][0] *= si0 * flipped(di0), Y[nt][1] *= si0 * flipped(di0), Y[nt][2] *= si1 * flipped(di1), Y[nt][3] *= si1 * flipped(di1);
+            Y[nt][0] *= f.x, Y[nt][1] *= f.y, Y[nt][2] *= f.x, Y[nt][3] *= f.y;
+        }
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            const uint32_t x[4] = {pack2(d[2 * kt][0] * u0, d[2 * kt][1] * u0, T()), pack2(d[2 * kt][2] * u1, d[2 * kt][3] * u1, T()),
+                                   pack2(d[2 * kt + 1][0] * u0, d[2 * kt + 1][1] * u0, T()), pack2(d[2 * kt + 1][2] * u1, d[2 * kt + 1][3] * u1, T())};
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t b[4];
+                ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), b);
+                mma16816(Y[nt], x, b[0], b[1], T());
+                mma16816(Y[nt + 1], x, b[2], b[3], T());
+            }
+        }
+        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
+            d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
+        }
+        if (kHalf) u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
+        const float all0 = st.w.all * u0, all1 = st.w.all * u1;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) S[nt][0] *= all0, S[nt][1] *= all0, S[nt][2] *= all1, S[nt][3] *= all1;
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            uint32_t hi[4], lo[4];
+            terms(d + 2 * kt, u0, u1, hi, lo);
+#pragma unroll
+            for (int n0 = 0; n0 < NT; n0 += 8) {
+                uint32_t b[8][2];
+#pragma unroll
+                for (int nt = 0; nt < 8; nt += 2) {
+                    uint32_t x[4];
+                    ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), n0 + nt + lane / 16), x);
+                    b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+                }
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) mma16816(S[n0 + nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt) mma16816(S[n0 + nt], lo, b[nt][0], b[nt][1], T());
+            }
+        }
+        if (kHalf) {
+            const float i0 = flipped(u0), i1 = flipped(u1);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[nt][0] *= i0, S[nt][1] *= i0, S[nt][2] *= i1, S[nt][3] *= i1;
+        }
+        // rows of 16 columns through the warp's own part of V's tile
+#pragma unroll
+        for (int nt = 0; nt < CT; nt += 2)
+            asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                             smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * warp + b_piece)),
+                         "r"(pack2(Y[nt][0] * di0, Y[nt][1] * di0, T())), "r"(pack2(Y[nt][2] * di1, Y[nt][3] * di1, T())),
+                         "r"(pack2(Y[nt + 1][0] * di0, Y[nt + 1][1] * di0, T())), "r"(pack2(Y[nt + 1][2] * di1, Y[nt + 1][3] * di1, T()))
+                         : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < C / 16; ++i) {
+            const int r = 16 * i + (int)lane / 2;
+            const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * warp + (lane & 1u)));
+            if (r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
+        }
+        done();
+    }
+    if (!to) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
+}
+
+template <class T, int D, int W>
+cudaError_t launch_relay(const DeltaArgs &a, cudaStream_t s)
+{
+    static_assert(sizeof(RelaySmem<D, W>) <= 232448, "");
+    static std::atomic<uint64_t> done;
+    const cudaError_t e = allow_smem(kv_delta_relay_kernel<T, D, W>, 232448, done);
+    if (e != cudaSuccess) return e;
+    // (more than half of an SM's shared memory: two CTAs must not share one while others stand idle)
+    const uint32_t smem = sizeof(RelaySmem<D, W>) > 118784 ? sizeof(RelaySmem<D, W>) : 118784;
+    return launch_dependent(kv_delta_relay_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), RelayShape<D, W>::kThreads, smem, s, a);
+}
+template <class T, int D, int W>
+cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
+{
+    static_assert(sizeof(SoloSmem<D, W>) <= 232448, "");
+    static std::atomic<uint64_t> done;
+    const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W>, sizeof(SoloSmem<D, W>), done);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(kv_delta_solo_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s, a);
+}
+template <class T, int D>
+cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
+{
+    const uint64_t slices = (uint64_t)a.n_seq * a.n_heads * (D / 16);
+    if (slices <= 148) return launch_relay<T, D, 1>(a, s);
+    return slices <= 2 * 148 ? launch_relay<T, D, 2>(a, s) : launch_solo<T, D, 4>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_chain(const DeltaArgs &a, uint32_t dtype, uint32_t head_dim, cudaStream_t s)
+{
+    if (head_dim == 128) return dtype == GMS_DTYPE_BF16 ? launch<__nv_bfloat16, 128>(a, s) : launch<__half, 128>(a, s);
+    return dtype == GMS_DTYPE_BF16 ? launch<__nv_bfloat16, 64>(a, s) : launch<__half, 64>(a, s);
+}
+
+}  // namespace gms
