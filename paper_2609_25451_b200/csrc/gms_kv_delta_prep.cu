@@ -15,6 +15,7 @@ namespace {
 constexpr float kMostNegative = -200.f;  // a gate of e^-200 is 0 in 32 bits, as is every product with it
 
 using ptx::ldmatrix_x4;
+using ptx::ldmatrix_x4_trans;
 using ptx::smem_u32;
 
 // Which sequence and which of its chunks slot `id` stands for; false: none.
@@ -31,8 +32,12 @@ __device__ __forceinline__ bool find_chunk(const DeltaArgs &a, uint32_t id, uint
     return id >= first;
 }
 
-constexpr uint32_t kPrepThreads = 128, kPrepHeads = 4, kRowPad = kChunkRows + 4;
+constexpr uint32_t kPrepThreads = 128, kPrepHeads = 4;
 
+// A lower triangle of 64 x 64, in blocks of 16 x 16, as two bf16 terms (2^-17 relative together).
+struct Terms64 {
+    uint8_t hi[sizeof(ChunkWork::tile[0])], lo[sizeof(ChunkWork::tile[0])];
+};
 template <int D>
 struct PrepSmem {
     union {
@@ -40,89 +45,78 @@ struct PrepSmem {
             uint8_t k[kChunkRows * D * 2], q[kChunkRows * D * 2];
         };
         struct {
-            float a[kChunkRows][kRowPad], t[kChunkRows][kRowPad];  // A and the inverse of I + A, below their diagonals' 16 x 16 blocks
+            Terms64 a, inv, t;           // A below its diagonal blocks, the inverse of I + A, the same times diag(beta)
+            float diag[4][16][20];       // A's diagonal blocks
             uint8_t p[sizeof(ChunkWork::tile[0])];
         };
     };
-    double sum[kPrepHeads][kChunkRows];  // G / ln 2
-    float b[kPrepHeads][kChunkRows];
-    float rk[kChunkRows], rq[kChunkRows];
+    float2 sum[kPrepHeads][kChunkRows];  // G / ln 2, as the sum of two
+    float b[kPrepHeads][kChunkRows], rk[kChunkRows], rq[kChunkRows];
     float top[2][4];
 };
 
-// Factors of products of two 32-bit matrices in shared memory, as two bf16 terms each: rows r0 + g (+ 8), columns c0 + t2 + {0, 1, 8, 9}
-// of the first factor; rows k0 + t2 + {0, 1, 8, 9}, column n0 + g of the second.
-struct Terms {
+// Byte offset of a block of 16 x 16, and of 16-byte piece c (0, 1) of row r in it.
+__device__ __forceinline__ uint32_t block_at(uint32_t i, uint32_t j) { return (i * (i + 1) / 2 + j) * 512; }
+__device__ __forceinline__ uint32_t piece_in(uint32_t r, uint32_t c) { return (r * 2 + ((c ^ (r / 4)) & 1u)) * 16; }
+
+// A block as a first factor; and c += x y with y a block: two terms each, the product of the small ones left out.
+struct First {
     uint32_t hi[4], lo[4];
 };
-__device__ __forceinline__ Terms first_factor(const float (*x)[kRowPad], uint32_t r, uint32_t c)
+__device__ __forceinline__ First first_of(const Terms64 &x, uint32_t block)
 {
-    Terms f;
-#pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-        const float2 v = *reinterpret_cast<const float2 *>(&x[r + (e & 1) * 8][c + (e & 2) * 4]);
-        split2<__nv_bfloat16>(v.x, v.y, f.hi[e], f.lo[e]);
-    }
+    const uint32_t lane = threadIdx.x & 31u, at = block + piece_in(lane & 15u, lane / 16);
+    First f;
+    ldmatrix_x4(smem_u32(x.hi) + at, f.hi);
+    ldmatrix_x4(smem_u32(x.lo) + at, f.lo);
     return f;
 }
-__device__ __forceinline__ void second_factor(const float (*x)[kRowPad], uint32_t k, uint32_t n, uint32_t *hi, uint32_t *lo)
+__device__ __forceinline__ First first_of(const float (*x)[4])  // minus the accumulators of a 16 x 16
 {
+    First f;
 #pragma unroll
-    for (uint32_t e = 0; e < 2; ++e) split2<__nv_bfloat16>(x[k + 8 * e][n], x[k + 8 * e + 1][n], hi[e], lo[e]);
+    for (int e = 0; e < 4; ++e) split2<__nv_bfloat16>(-x[e / 2][2 * (e & 1)], -x[e / 2][2 * (e & 1) + 1], f.hi[e], f.lo[e]);
+    return f;
 }
-__device__ __forceinline__ void mma_terms(float *c, const Terms &f, const uint32_t *hi, const uint32_t *lo)
+__device__ __forceinline__ void add_product(float (*c)[4], const First &x, const Terms64 &y, uint32_t block)
 {
-    mma16816(c, f.hi, hi[0], hi[1], __nv_bfloat16());
-    mma16816(c, f.lo, hi[0], hi[1], __nv_bfloat16());
-    mma16816(c, f.hi, lo[0], lo[1], __nv_bfloat16());
+    const uint32_t lane = threadIdx.x & 31u, at = block + piece_in(lane & 15u, lane / 16);
+    uint32_t hi[4], lo[4];
+    ldmatrix_x4_trans(smem_u32(y.hi) + at, hi);
+    ldmatrix_x4_trans(smem_u32(y.lo) + at, lo);
+    const __nv_bfloat16 type{};
+    mma16816(c[0], x.hi, hi[0], hi[1], type);
+    mma16816(c[1], x.hi, hi[2], hi[3], type);
+    mma16816(c[0], x.lo, hi[0], hi[1], type);
+    mma16816(c[1], x.lo, hi[2], hi[3], type);
+    mma16816(c[0], x.hi, lo[0], lo[1], type);
+    mma16816(c[1], x.hi, lo[2], lo[3], type);
 }
-// -(X Y) Z with X 16 x 16 K, Y 16 K x 8 N, Z 8 N x 8 M; the first `used` of X's K tiles are not zero, nor are Z's rows from 16 `from` on.
-// X Y stays in registers: an accumulator is, element for element, a first factor.
-template <int K, int N, int M>
-__device__ __forceinline__ void two_products(const float (*x)[kRowPad], uint32_t x_row, uint32_t x_col, const float (*y)[kRowPad], uint32_t y_row,
-                                             uint32_t y_col, const float (*z)[kRowPad], uint32_t z_row, uint32_t z_col, uint32_t used, uint32_t from,
-                                             float (*out)[4])
+// Two neighbours of a row as two terms; a 16 x 16 of accumulators.
+__device__ __forceinline__ void put_pair(Terms64 &t, uint32_t at, float x, float y)
 {
-    const uint32_t lane = threadIdx.x & 31u, g = lane / 4, t2 = 2 * (lane & 3u);
-    float mid[N][4] = {};
+    uint32_t hi, lo;
+    split2<__nv_bfloat16>(x, y, hi, lo);
+    *reinterpret_cast<uint32_t *>(t.hi + at) = hi;
+    *reinterpret_cast<uint32_t *>(t.lo + at) = lo;
+}
+__device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const float (*x)[4], float &finite)
+{
+    const uint32_t lane = threadIdx.x & 31u, g = lane / 4, q = (lane & 3u) * 4;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (k >= (int)used) break;
-        const Terms f = first_factor(x, x_row + g, x_col + 16 * k + t2);
+    for (uint32_t nt = 0; nt < 2; ++nt) {
+        put_pair(t, block + piece_in(g, nt) + q, x[nt][0], x[nt][1]);
+        put_pair(t, block + piece_in(g + 8, nt) + q, x[nt][2], x[nt][3]);
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            uint32_t hi[2], lo[2];
-            second_factor(y, y_row + 16 * k + t2, y_col + 8 * n + g, hi, lo);
-            mma_terms(mid[n], f, hi, lo);
-        }
+        for (int e = 0; e < 4; ++e) finite = fmaf(x[nt][e], 0.f, finite);
     }
-#pragma unroll
-    for (int k = 0; k < N / 2; ++k) {
-        if (k < (int)from) continue;
-        Terms f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            split2<__nv_bfloat16>(-mid[2 * k + e / 2][2 * (e & 1)], -mid[2 * k + e / 2][2 * (e & 1) + 1], f.hi[e], f.lo[e]);
-#pragma unroll
-        for (int n = 0; n < M; ++n) {
-            uint32_t hi[2], lo[2];
-            second_factor(z, z_row + 16 * k + t2, z_col + 8 * n + g, hi, lo);
-            mma_terms(out[n], f, hi, lo);
-        }
-    }
-}
-__device__ __forceinline__ void put_tile(float (*t)[kRowPad], uint32_t r, uint32_t c, const float *x)
-{
-    const uint32_t lane = threadIdx.x & 31u, g = lane / 4, t2 = 2 * (lane & 3u);
-    *reinterpret_cast<float2 *>(&t[r + g][c + t2]) = make_float2(x[0], x[1]);
-    *reinterpret_cast<float2 *>(&t[r + g + 8][c + t2]) = make_float2(x[2], x[3]);
 }
 
-// One CTA per chunk and key head.  k_i.k_j and q_i.k_j on mma.sync (a warp has 16 rows i), then for each value head of the key
-// head the decays, the inverse and what goes to the workspace.  The inverse of I + A: its diagonal blocks of 16 x 16 a warp each
-// (a lane has a column and goes down it: x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
+// One CTA per chunk and key head.  k_i.k_j and q_i.k_j on mma.sync (a warp has 16 rows i; the diagonals are the rows' lengths), then
+// for each value head of the key head the decays, the inverse and what goes to the workspace.  The inverse of I + A: its diagonal
+// blocks of 16 x 16 a warp each (a lane has a column and goes down it: x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
 //   (X 0; Y Z)^-1 = (X^-1 0; -Z^-1 Y X^-1 Z^-1)
-// in products of two-term factors (2^-16 relative, as T itself is handed on).
+// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by issue and shared memory, @@PREP@@
 template <class T, int D>
 __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -139,123 +133,140 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
     const int all_rows = delta_rows(a, s);
     if (!delta_in_chunks(a, all_rows) || chunk > (uint32_t)(all_rows - 1) / C) return;
     const int n = min(all_rows - (int)chunk * C, C), first = delta_begin(a, s) + (int)chunk * C;
-#pragma unroll 4
-    for (uint32_t i = tid; i < (uint32_t)(C * P); i += kPrepThreads) {
-        const uint32_t r = i / P, c = i % P;
-        const bool real = (int)r < n;
-        const uint64_t row = (uint64_t)(first + (real ? (int)r : 0));
-        cp16(smem_u32(m.k) + piece<P>(r, c), a.k + row * a.k_token + kh * a.k_head + c * 16, real);
-        cp16(smem_u32(m.q) + piece<P>(r, c), a.q + row * a.q_token + kh * a.q_head + c * 16, real);
+    {
+        const uint32_t c = tid % P, r0 = tid / P;
+        const uint8_t *kp = a.k + (uint64_t)first * a.k_token + kh * a.k_head + c * 16, *qp = a.q + (uint64_t)first * a.q_token + kh * a.q_head + c * 16;
+#pragma unroll
+        for (uint32_t i = 0; i < (uint32_t)(C * P) / kPrepThreads; ++i) {
+            const uint32_t r = r0 + i * (kPrepThreads / P), real = (int)r < n ? r : 0;
+            cp16(smem_u32(m.k) + piece<P>(r, c), kp + real * a.k_token, (int)r < n);
+            cp16(smem_u32(m.q) + piece<P>(r, c), qp + real * a.q_token, (int)r < n);
+        }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    // lengths: two threads a row
-    uint32_t bad = 0;
-    {
-        const uint32_t r = tid / 2;
-        float kk = 0.f, qq = 0.f;
-#pragma unroll
-        for (uint32_t c = 0; c < (uint32_t)P; c += 2) {
-            const uint32_t at = piece<P>(r, c + (tid & 1u));
-            const uint4 kv = *reinterpret_cast<const uint4 *>(m.k + at), qv = *reinterpret_cast<const uint4 *>(m.q + at);
-            const T *ke = reinterpret_cast<const T *>(&kv), *qe = reinterpret_cast<const T *>(&qv);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) kk += to_f32(ke[e]) * to_f32(ke[e]), qq += to_f32(qe[e]) * to_f32(qe[e]);
-        }
-        kk += __shfl_xor_sync(0xffffffffu, kk, 1);
-        qq += __shfl_xor_sync(0xffffffffu, qq, 1);
-        if (!(kk < kHuge) || !(qq < kHuge)) bad = 1;
-        if ((tid & 1u) == 0) {
-            m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(kk + a.unit_eps) : 1.f;
-            m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(qq + a.unit_eps) : 1.f;
-        }
-    }
-    // products of rows 16 warp .. with rows 0 .. of the keys
-    float kk[C / 8][4] = {}, qk[C / 8][4] = {};
+    // products of rows 16 warp .. with rows 0 .. of the keys, and of the queries with themselves
+    const uint32_t i0 = 16 * warp + g, b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;
+    float kk[C / 8][4] = {}, qk[C / 8][4] = {}, qq[2][4] = {};
 #pragma unroll
     for (int kt = 0; kt < D / 16; ++kt) {
-        uint32_t ka[4], qa[4];
+        uint32_t ka[4], qa[4], b[4];
         const uint32_t at = piece<P>(16 * warp + (lane & 15u), 2 * kt + lane / 16);
         ldmatrix_x4(smem_u32(m.k) + at, ka);
         ldmatrix_x4(smem_u32(m.q) + at, qa);
+        ldmatrix_x4(smem_u32(m.q) + piece<P>(16 * warp + b_row, 2 * kt + b_piece), b);
+        mma16816(qq[0], qa, b[0], b[1], T());
+        mma16816(qq[1], qa, b[2], b[3], T());
 #pragma unroll
         for (int nt = 0; nt < C / 8; nt += 2) {
             if (nt > 2 * (int)warp) break;
-            uint32_t b[4];
-            ldmatrix_x4(smem_u32(m.k) + piece<P>(8 * nt + (lane & 7u) + (lane & 16u) / 2, 2 * kt + (lane / 8 & 1u)), b);
+            ldmatrix_x4(smem_u32(m.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), b);
             mma16816(kk[nt], ka, b[0], b[1], T());
             mma16816(kk[nt + 1], ka, b[2], b[3], T());
             mma16816(qk[nt], qa, b[0], b[1], T());
             mma16816(qk[nt + 1], qa, b[2], b[3], T());
         }
     }
+    float finite = 0.f;  // NaN once something was not finite
+#pragma unroll
+    for (int nt = 0; nt < C / 8; ++nt) {
+        if (nt / 2 != (int)warp) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (8 * (nt & 1) + t2 + (e & 1) == g + (e & 2) * 4) {  // on the diagonal
+                const uint32_t r = i0 + (e & 2) * 4;
+                const float k2 = kk[nt][e], q2 = qq[nt & 1][e];
+                finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
+                m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
+                m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
+            }
+    }
     for (uint32_t j = 0; j < a.group; ++j) {
         ChunkWork *work = reinterpret_cast<ChunkWork *>(a.chunks + ((uint64_t)id * a.n_heads + kh * a.group + j) * sizeof(ChunkWork));
         const uint32_t jj = j % kPrepHeads;
         __syncthreads();  // the keys and queries, or the last head's matrices, have been read
-        if (jj == 0 && j + warp < a.group) {  // gates of four heads, a warp each: two rows a lane, sums in 64 bits
-            const uint32_t h = kh * a.group + j + warp;
-            ChunkWork &w = work[warp];
-            double x[2], sum_g = 0.;
-            float beta[2], raw_g[2];
+        if (jj == 0) {
+            if (j + warp < a.group) {  // gates of four heads, a warp each: two rows a lane, sums in 64 bits
+                const uint32_t h = kh * a.group + j + warp;
+                ChunkWork &w = work[warp];
+                double x[2], sum_g = 0.;
+                float beta[2], raw_g[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = 2 * (int)lane + e;
-                const uint64_t row = (uint64_t)(first + r);
-                raw_g[e] = r < n && a.g ? a.g[row * a.g_stride + h] : 0.f;
-                beta[e] = r < n ? a.beta ? a.beta[row * a.beta_stride + h] : 1.f : 0.f;
-                if (!(raw_g[e] < kHuge) || !(fabsf(beta[e]) < kHuge)) bad = 1;
-                sum_g += 1.4426950408889634 * (double)(raw_g[e] < kMostNegative ? kMostNegative : raw_g[e]);
-                x[e] = sum_g;
-            }
-            double inc = sum_g;
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 2 * (int)lane + e;
+                    const uint64_t row = (uint64_t)(first + r);
+                    raw_g[e] = r < n && a.g ? a.g[row * a.g_stride + h] : 0.f;
+                    beta[e] = r < n ? a.beta ? a.beta[row * a.beta_stride + h] : 1.f : 0.f;
+                    if (!(raw_g[e] < kHuge)) finite = __int_as_float(0x7fffffff);  // (-infinity clears the state)
+                    finite = fmaf(beta[e], 0.f, finite);
+                    sum_g += 1.4426950408889634 * (double)(raw_g[e] < kMostNegative ? kMostNegative : raw_g[e]);
+                    x[e] = sum_g;
+                }
+                double inc = sum_g;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double y = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= (uint32_t)o) inc += y;
-            }
-            const double last = __shfl_sync(0xffffffffu, inc, 31);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const double y = __shfl_up_sync(0xffffffffu, inc, o);
+                    if (lane >= (uint32_t)o) inc += y;
+                }
+                const double last = __shfl_sync(0xffffffffu, inc, 31);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = 2 * (int)lane + e;
-                const double sum = inc - sum_g + x[e];
-                const bool in = r < n;
-                m.sum[warp][r] = sum;
-                m.b[warp][r] = beta[e];
-                const float gate = exp2f((float)sum), f = in ? m.rk[r] * gate : 0.f, hh = in ? a.scale * m.rq[r] * gate : 0.f,
-                            ww = in ? m.rk[r] * exp2f((float)(last - sum)) : 0.f;
-                w.f[r] = f, w.h[r] = hh, w.w[r] = ww;
-                w.gate[r] = expf(raw_g[e]), w.beta[r] = beta[e], w.rk[r] = m.rk[r], w.rq[r] = m.rq[r];
-                if (!(fabsf(f) < kHuge) || !(fabsf(hh) < kHuge) || !(fabsf(ww) < kHuge)) bad = 1;
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 2 * (int)lane + e;
+                    const double sum = inc - sum_g + x[e];
+                    const bool in = r < n;
+                    m.sum[warp][r] = make_float2((float)sum, (float)(sum - (double)(float)sum));
+                    m.b[warp][r] = beta[e];
+                    const float gate = exp2f((float)sum), f = in ? m.rk[r] * gate : 0.f, hh = in ? a.scale * m.rq[r] * gate : 0.f,
+                                ww = in ? m.rk[r] * exp2f((float)(last - sum)) : 0.f;
+                    w.f[r] = f, w.h[r] = hh, w.w[r] = ww;
+                    w.gate[r] = expf(raw_g[e]), w.beta[r] = beta[e], w.rk[r] = m.rk[r], w.rq[r] = m.rq[r];
+                    finite = fmaf(f, 0.f, fmaf(hh, 0.f, fmaf(ww, 0.f, finite)));
+                }
+                const float all = exp2f((float)last);
+                finite = fmaf(all, 0.f, finite);
+                if (lane == 0) w.all = all;
             }
-            const float all = exp2f((float)last);
-            if (!(all < kHuge)) bad = 1;
-            if (lane == 0) w.all = all;
+            __syncthreads();
         }
-        __syncthreads();
-        // A and P: rows i = 16 warp + g (+ 8), columns 8 nt + t2 + {0, 1}
+        // A and P: rows i0 and i0 + 8, columns 8 nt + t2 + {0, 1}
         float pv[C / 8][4], top = 0.f;
         {
-            const uint32_t i0 = 16 * warp + g;
-            const double sum[2] = {m.sum[jj][i0], m.sum[jj][i0 + 8]};
+            const float2 sum[2] = {m.sum[jj][i0], m.sum[jj][i0 + 8]};
             const float bk[2] = {m.b[jj][i0] * m.rk[i0], m.b[jj][i0 + 8] * m.rk[i0 + 8]};
             const float sq[2] = {(int)i0 < n ? a.scale * m.rq[i0] : 0.f, (int)i0 + 8 < n ? a.scale * m.rq[i0 + 8] : 0.f};
 #pragma unroll
             for (int nt = 0; nt < C / 8; ++nt) {
                 pv[nt][0] = pv[nt][1] = pv[nt][2] = pv[nt][3] = 0.f;
                 if (nt > 2 * (int)warp + 1) continue;
-                const uint32_t c0 = 8 * nt + t2;
+                const float4 sc = *reinterpret_cast<const float4 *>(&m.sum[jj][8 * nt + t2]);  // of two columns
+                const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[8 * nt + t2]);
                 float av[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t i = i0 + (e & 2) * 4, c = c0 + (e & 1);
-                    const float z = m.rk[c] * (c <= i ? ptx::ex2((float)(sum[e / 2] - m.sum[jj][c])) : 0.f);
-                    av[e] = c < i ? bk[e / 2] * (kk[nt][e] * z) : 0.f;
-                    pv[nt][e] = c <= i ? sq[e / 2] * (qk[nt][e] * z) : 0.f;
-                    if (!(fabsf(av[e]) < kHuge) || !(fabsf(pv[nt][e]) < kHuge)) bad = 1;
-                    top = fmaxf(top, fabsf(pv[nt][e]));
+                    const float decay = ptx::ex2((sum[e / 2].x - (e & 1 ? sc.z : sc.x)) + (sum[e / 2].y - (e & 1 ? sc.w : sc.y)));
+                    const float z = (e & 1 ? rc.y : rc.x) * decay;
+                    av[e] = bk[e / 2] * (kk[nt][e] * z);
+                    pv[nt][e] = sq[e / 2] * (qk[nt][e] * z);
                 }
-                put_tile(m.a, 16 * warp, 8 * nt, av);
+                if (nt / 2 == (int)warp) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t r = g + (e & 2) * 4, c = 8 * (nt & 1) + t2 + (e & 1);
+                        if (c >= r) av[e] = 0.f;
+                        if (c > r) pv[nt][e] = 0.f;
+                    }
+                    *reinterpret_cast<float2 *>(&m.diag[warp][g][8 * (nt & 1) + t2]) = make_float2(av[0], av[1]);
+                    *reinterpret_cast<float2 *>(&m.diag[warp][g + 8][8 * (nt & 1) + t2]) = make_float2(av[2], av[3]);
+                } else {
+                    const uint32_t block = block_at(warp, nt / 2);
+                    put_pair(m.a, block + piece_in(g, nt & 1) + 2 * t2, av[0], av[1]);
+                    put_pair(m.a, block + piece_in(g + 8, nt & 1) + 2 * t2, av[2], av[3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    finite = fmaf(av[e], 0.f, fmaf(pv[nt][e], 0.f, finite));
+                    if (kHalf) top = fmaxf(top, fabsf(pv[nt][e]));
+                }
             }
         }
         float ps = 1.f;
@@ -270,95 +281,96 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
 #pragma unroll
         for (int nt = 0; nt < C / 8; ++nt) {
             if (nt > 2 * (int)warp + 1) break;
-            const uint32_t i = 16 * warp + g;
-            *reinterpret_cast<uint32_t *>(m.p + block_piece(i, nt) + 2 * t2) = pack2(pv[nt][0] * ps, pv[nt][1] * ps, T());
-            *reinterpret_cast<uint32_t *>(m.p + block_piece(i + 8, nt) + 2 * t2) = pack2(pv[nt][2] * ps, pv[nt][3] * ps, T());
+            const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
+            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(pv[nt][0] * ps, pv[nt][1] * ps, T());
+            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(pv[nt][2] * ps, pv[nt][3] * ps, T());
         }
         __syncwarp();
         if (lane < 16) {  // the warp's own diagonal block
-            const uint32_t d0 = 16 * warp;
             float x[16];
+            const float b = m.b[jj][16 * warp + lane];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 float sum = i == (int)lane ? 1.f : 0.f;
 #pragma unroll
                 for (int c = 0; c < i; c += 4) {
-                    const float4 r = *reinterpret_cast<const float4 *>(&m.a[d0 + i][d0 + c]);
+                    const float4 r = *reinterpret_cast<const float4 *>(&m.diag[warp][i][c]);
                     sum -= r.x * x[c];
                     if (c + 1 < i) sum -= r.y * x[c + 1];
                     if (c + 2 < i) sum -= r.z * x[c + 2];
                     if (c + 3 < i) sum -= r.w * x[c + 3];
                 }
                 x[i] = sum;
-                m.t[d0 + i][d0 + lane] = sum;
+            }
+            const uint32_t block = block_at(warp, warp);
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {  // neighbouring lanes are neighbours of a row: each stores one row's pair of them
+                const float other = __shfl_xor_sync(0xffffu, lane & 1u ? x[i] : x[i + 1], 1), ob = __shfl_xor_sync(0xffffu, b, 1);
+                const float mine = lane & 1u ? x[i + 1] : x[i];
+                const float l = lane & 1u ? other : mine, r = lane & 1u ? mine : other;
+                const uint32_t at = block + piece_in(i + (lane & 1u), lane / 8) + (lane & 6u) * 2;
+                put_pair(m.inv, at, l, r);
+                put_pair(m.t, at, l * (lane & 1u ? ob : b), r * (lane & 1u ? b : ob));
+                finite = fmaf(x[i], 0.f, fmaf(x[i + 1], 0.f, finite));
             }
         }
         __syncthreads();
-        if ((warp & 1u) == 0) {
+        if (warp != 1) {  // blocks (1, 0) and (3, 2) of T; (3, 2) of the inverse, too
+            const uint32_t i = warp == 0 ? 0 : 2;
+            float mid[2][4] = {}, o[2][4] = {};
+            add_product(mid, first_of(m.inv, block_at(i + 1, i + 1)), m.a, block_at(i + 1, i));
+            add_product(o, first_of(mid), warp == 3 ? m.inv : m.t, block_at(i, i));
+            put_block(warp == 3 ? m.inv : m.t, block_at(i + 1, i), o, finite);
+        }
+        __syncthreads();
+        {  // blocks (2 .. 3, 0 .. 1) of T, one a warp
+            const uint32_t i = 2 + (warp & 1u), c = warp / 2;
             float o[2][4] = {};
-            const uint32_t d0 = 16 * warp;
-            two_products<1, 2, 2>(m.t, d0 + 16, d0 + 16, m.a, d0 + 16, d0, m.t, d0, d0, 1, 0, o);
-            put_tile(m.t, d0 + 16, d0, o[0]);
-            put_tile(m.t, d0 + 16, d0 + 8, o[1]);
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k) {
+                if (k < c) continue;
+                float mid[2][4] = {};
+                add_product(mid, first_of(m.inv, block_at(i, 2)), m.a, block_at(2, k));
+                if (i == 3) add_product(mid, first_of(m.inv, block_at(3, 3)), m.a, block_at(3, k));
+                add_product(o, first_of(mid), m.t, block_at(k, c));
+            }
+            put_block(m.t, block_at(i, c), o, finite);
         }
         __syncthreads();
-        {
-            const uint32_t r = 16 * (warp & 1u), c = 16 * (warp / 2);
-            float o[2][4] = {};
-            two_products<2, 4, 2>(m.t, 32 + r, 32, m.a, 32, 0, m.t, 0, c, (warp & 1u) + 1, warp / 2, o);
-            put_tile(m.t, 32 + r, c, o[0]);
-            put_tile(m.t, 32 + r, c + 8, o[1]);
-        }
-        __syncthreads();
-        // T = inverse times diag(beta), eight neighbours a thread, below and in the diagonal blocks (nobody reads the rest)
-        float x[3][8], most = 0.f;
-        auto place = [&](uint32_t u, uint32_t &i, uint32_t &c) {  // piece u of 16 (2 + 4 + 6 + 8)
-            const uint32_t block = u < 32 ? 0 : u < 96 ? 1 : u < 192 ? 2 : 3, in = u - 16 * block * (block + 1), width = 2 * block + 2;
-            i = 16 * block + in / width, c = in % width;
-        };
+        constexpr uint32_t kPieces = sizeof(m.p) / 16;
+        if (kHalf) {  // to f16, all numbers scaled alike
+            float most = 0.f;
+            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
+                const uint4 hi = reinterpret_cast<const uint4 *>(m.t.hi)[u];
+                const __nv_bfloat16 *e = reinterpret_cast<const __nv_bfloat16 *>(&hi);
 #pragma unroll
-        for (uint32_t k = 0; k < 3; ++k) {
-            const uint32_t u = k * kPrepThreads + tid;
-            uint32_t i, c;
-            place(u < 320 ? u : 0, i, c);
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(&m.t[i][8 * c + e]), b = *reinterpret_cast<const float4 *>(&m.b[jj][8 * c + e]);
-                x[k][e] = v.x * b.x, x[k][e + 1] = v.y * b.y, x[k][e + 2] = v.z * b.z, x[k][e + 3] = v.w * b.w;
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(to_f32(e[i])));
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (8 * c + e > i) x[k][e] = 0.f;
-                if (!(fabsf(x[k][e]) < kHuge)) bad = 1;
-                most = fmaxf(most, fabsf(x[k][e]));
-            }
-        }
-        float ts = 1.f;
-        if (kHalf) {
 #pragma unroll
             for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
             if (lane == 0) m.top[1][warp] = most;
             __syncthreads();
-            ts = range_scale(fmaxf(fmaxf(m.top[1][0], m.top[1][1]), fmaxf(m.top[1][2], m.top[1][3])));
+            const float ts = range_scale(fmaxf(fmaxf(m.top[1][0], m.top[1][1]), fmaxf(m.top[1][2], m.top[1][3])));
             if (tid == 0) work->t_unit = flipped(ts);
-        }
+            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
+                const uint4 x = reinterpret_cast<const uint4 *>(m.t.hi)[u], y = reinterpret_cast<const uint4 *>(m.t.lo)[u];
+                const __nv_bfloat16 *p = reinterpret_cast<const __nv_bfloat16 *>(&x), *q = reinterpret_cast<const __nv_bfloat16 *>(&y);
+                uint32_t hi[4], lo[4];
 #pragma unroll
-        for (uint32_t k = 0; k < 3; ++k) {
-            const uint32_t u = k * kPrepThreads + tid;
-            if (u >= 320) break;
-            uint32_t i, c;
-            place(u, i, c);
-            uint4 hi, lo;
-            split2<T>(x[k][0] * ts, x[k][1] * ts, hi.x, lo.x);
-            split2<T>(x[k][2] * ts, x[k][3] * ts, hi.y, lo.y);
-            split2<T>(x[k][4] * ts, x[k][5] * ts, hi.z, lo.z);
-            split2<T>(x[k][6] * ts, x[k][7] * ts, hi.w, lo.w);
-            *reinterpret_cast<uint4 *>(work->tile[0] + block_piece(i, c)) = hi;
-            *reinterpret_cast<uint4 *>(work->tile[1] + block_piece(i, c)) = lo;
+                for (int i = 0; i < 4; ++i)
+                    split2<T>((to_f32(p[2 * i]) + to_f32(q[2 * i])) * ts, (to_f32(p[2 * i + 1]) + to_f32(q[2 * i + 1])) * ts, hi[i], lo[i]);
+                reinterpret_cast<uint4 *>(work->tile[0])[u] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                reinterpret_cast<uint4 *>(work->tile[1])[u] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
+            }
+        } else {
+            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
+                reinterpret_cast<uint4 *>(work->tile[0])[u] = reinterpret_cast<const uint4 *>(m.t.hi)[u];
+                reinterpret_cast<uint4 *>(work->tile[1])[u] = reinterpret_cast<const uint4 *>(m.t.lo)[u];
+                reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
+            }
         }
-        for (uint32_t i = tid; i < sizeof(m.p) / 16; i += kPrepThreads)
-            reinterpret_cast<uint4 *>(work->tile[2])[i] = reinterpret_cast<const uint4 *>(m.p)[i];
-        const bool any = __syncthreads_or(bad);
+        const bool any = __syncthreads_or(finite != 0.f);
         if (tid == 0) work->by_row = any;
     }
 }
