@@ -118,7 +118,7 @@ __device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const floa
 //   (X 0; Y Z)^-1 = (X^-1 0; -Z^-1 Y X^-1 Z^-1)
 // in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by issue and shared memory, @@PREP@@
 template <class T, int D>
-__global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
+__global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ? 4 : 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
     extern __shared__ __align__(16) uint8_t raw[];
     PrepSmem<D> &m = *reinterpret_cast<PrepSmem<D> *>(raw);
@@ -229,15 +229,20 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
             __syncthreads();
         }
         // A and P: rows i0 and i0 + 8, columns 8 nt + t2 + {0, 1}
-        float pv[C / 8][4], top = 0.f;
+        float pv[kHalf ? C / 8 : 1][4], top = 0.f;
+        auto put_p = [&](int nt, const float *p, float scale) {
+            const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
+            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(p[0] * scale, p[1] * scale, T());
+            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(p[2] * scale, p[3] * scale, T());
+        };
         {
             const float2 sum[2] = {m.sum[jj][i0], m.sum[jj][i0 + 8]};
             const float bk[2] = {m.b[jj][i0] * m.rk[i0], m.b[jj][i0 + 8] * m.rk[i0 + 8]};
             const float sq[2] = {(int)i0 < n ? a.scale * m.rq[i0] : 0.f, (int)i0 + 8 < n ? a.scale * m.rq[i0 + 8] : 0.f};
 #pragma unroll
             for (int nt = 0; nt < C / 8; ++nt) {
-                pv[nt][0] = pv[nt][1] = pv[nt][2] = pv[nt][3] = 0.f;
-                if (nt > 2 * (int)warp + 1) continue;
+                if (nt > 2 * (int)warp + 1) break;
+                float *pn = pv[kHalf ? nt : 0];
                 const float4 sc = *reinterpret_cast<const float4 *>(&m.sum[jj][8 * nt + t2]);  // of two columns
                 const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[8 * nt + t2]);
                 float av[4];
@@ -246,14 +251,14 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
                     const float decay = ptx::ex2((sum[e / 2].x - (e & 1 ? sc.z : sc.x)) + (sum[e / 2].y - (e & 1 ? sc.w : sc.y)));
                     const float z = (e & 1 ? rc.y : rc.x) * decay;
                     av[e] = bk[e / 2] * (kk[nt][e] * z);
-                    pv[nt][e] = sq[e / 2] * (qk[nt][e] * z);
+                    pn[e] = sq[e / 2] * (qk[nt][e] * z);
                 }
                 if (nt / 2 == (int)warp) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint32_t r = g + (e & 2) * 4, c = 8 * (nt & 1) + t2 + (e & 1);
                         if (c >= r) av[e] = 0.f;
-                        if (c > r) pv[nt][e] = 0.f;
+                        if (c > r) pn[e] = 0.f;
                     }
                     *reinterpret_cast<float2 *>(&m.diag[warp][g][8 * (nt & 1) + t2]) = make_float2(av[0], av[1]);
                     *reinterpret_cast<float2 *>(&m.diag[warp][g + 8][8 * (nt & 1) + t2]) = make_float2(av[2], av[3]);
@@ -264,26 +269,24 @@ __global__ void __launch_bounds__(kPrepThreads, 4) kv_delta_prep_kernel(const __
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    finite = fmaf(av[e], 0.f, fmaf(pv[nt][e], 0.f, finite));
-                    if (kHalf) top = fmaxf(top, fabsf(pv[nt][e]));
+                    finite = fmaf(av[e], 0.f, fmaf(pn[e], 0.f, finite));
+                    if (kHalf) top = fmaxf(top, fabsf(pn[e]));
                 }
+                if (!kHalf) put_p(nt, pn, 1.f);
             }
         }
-        float ps = 1.f;
         if (kHalf) {
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             if (lane == 0) m.top[0][warp] = top;
             __syncthreads();
-            ps = range_scale(fmaxf(fmaxf(m.top[0][0], m.top[0][1]), fmaxf(m.top[0][2], m.top[0][3])));
+            const float ps = range_scale(fmaxf(fmaxf(m.top[0][0], m.top[0][1]), fmaxf(m.top[0][2], m.top[0][3])));
             if (tid == 0) work->p_unit = flipped(ps);
-        }
 #pragma unroll
-        for (int nt = 0; nt < C / 8; ++nt) {
-            if (nt > 2 * (int)warp + 1) break;
-            const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
-            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(pv[nt][0] * ps, pv[nt][1] * ps, T());
-            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(pv[nt][2] * ps, pv[nt][3] * ps, T());
+            for (int nt = 0; nt < C / 8; ++nt) {
+                if (nt > 2 * (int)warp + 1) break;
+                put_p(nt, pv[kHalf ? nt : 0], ps);
+            }
         }
         __syncwarp();
         if (lane < 16) {  // the warp's own diagonal block
