@@ -789,6 +789,9 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
 }
 
+// More than half of an SM's shared memory: while the kernel ahead drains, two CTAs would come to share the first SMs that are free.
+constexpr uint32_t kOneAnSm = 118784;
+
 template <class T, int D, int W>
 cudaError_t launch_relay(const DeltaArgs &a, cudaStream_t s)
 {
@@ -796,8 +799,7 @@ cudaError_t launch_relay(const DeltaArgs &a, cudaStream_t s)
     static std::atomic<uint64_t> done;
     const cudaError_t e = allow_smem(kv_delta_relay_kernel<T, D, W>, 232448, done);
     if (e != cudaSuccess) return e;
-    // (more than half of an SM's shared memory: two CTAs must not share one while others stand idle)
-    const uint32_t smem = sizeof(RelaySmem<D, W>) > 118784 ? sizeof(RelaySmem<D, W>) : 118784;
+    const uint32_t smem = sizeof(RelaySmem<D, W>) > kOneAnSm ? sizeof(RelaySmem<D, W>) : kOneAnSm;
     return launch_dependent(kv_delta_relay_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), RelayShape<D, W>::kThreads, smem, s, a);
 }
 template <class T, int D, int W>
@@ -805,9 +807,10 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
 {
     static_assert(sizeof(SoloSmem<D, W>) <= 232448, "");
     static std::atomic<uint64_t> done;
-    const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W>, sizeof(SoloSmem<D, W>), done);
+    const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W>, 232448, done);
     if (e != cudaSuccess) return e;
-    return launch_dependent(kv_delta_solo_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s, a);
+    const uint32_t ctas = a.n_seq * a.n_heads * (D / (16 * W)), smem = ctas <= 148 && sizeof(SoloSmem<D, W>) < kOneAnSm ? kOneAnSm : sizeof(SoloSmem<D, W>);
+    return launch_dependent(kv_delta_solo_kernel<T, D, W>, ctas, SoloShape<D, W>::kThreads, smem, s, a);
 }
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)

@@ -35,14 +35,15 @@ __device__ __forceinline__ uint64_t sum_before(uint64_t x, uint64_t *sh, uint64_
     }
     if (lane == 31) sh[warp] = inc;
     __syncthreads();
-    uint64_t before = inc - x, sum = 0;
+    uint64_t w = lane < WARPS ? sh[lane] : 0;
 #pragma unroll
-    for (uint32_t i = 0; i < WARPS; ++i) {
-        if (i < warp) before += sh[i];
-        sum += sh[i];
+    for (uint32_t o = 1; o < WARPS; o <<= 1) {
+        const uint64_t y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
     }
-    *all = sum;
-    return before;
+    *all = __shfl_sync(0xffffffffu, w, WARPS - 1);
+    const uint64_t warps = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+    return inc - x + (warp ? warps : 0);
 }
 
 // What a tile's sequences have, for whoever looks for the owner of a row or of a block.
@@ -102,11 +103,11 @@ template <bool CLUSTER>
 __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __grid_constant__ PlanArgs a)
 {
     constexpr uint32_t kPlanThreads = CLUSTER ? 1024 : 512, kPlanWarps = kPlanThreads / 32, kPlanEach = kPlanTile / kPlanThreads;
-    constexpr uint32_t kAllWarps = (CLUSTER ? kPlanCtas : 1) * kPlanWarps, kLook = 8;
+    constexpr uint32_t kAllWarps = (CLUSTER ? kPlanCtas : 1) * kPlanWarps, kLook = 8, kRows = 4;
     __shared__ uint32_t found[kAllWarps];  // blocks that each warp's run has
     extern __shared__ uint8_t raw[];
     Tile &t = *reinterpret_cast<Tile *>(raw);
-    __shared__ uint64_t sums[3][kPlanWarps];
+    __shared__ uint64_t sums[2][kPlanWarps];
     const uint32_t tid = threadIdx.x, n_cta = CLUSTER ? kPlanCtas : 1, cta = CLUSTER ? blockIdx.x : 0;
     const bool leader = cta == n_cta - 1;
     const uint32_t at = cta * kPlanThreads + tid, step = n_cta * kPlanThreads;
@@ -135,8 +136,7 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
         }
         uint64_t all_rows;
         uint64_t row = rows_before + sum_before<kPlanWarps>(mine, sums[0], &all_rows);
-        uint32_t more[kPlanEach], back[kPlanEach];
-        uint64_t need_sum = 0, back_sum = 0;
+        uint64_t moved[kPlanEach], mine_moved = 0;  // blocks taken in the low half, given back in the high half: at most 2^31 of a tile's each
 #pragma unroll
         for (uint32_t i = 0; i < kPlanEach; ++i) {
             const uint64_t end = row + rows[i];
@@ -145,10 +145,8 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
                 rows[i] = row < a.total_rows ? (uint32_t)(a.total_rows - row) : 0;
             }
             const uint32_t had = blocks_of(len[i], a), need = blocks_of(base[i] + rows[i], a);
-            more[i] = need > had ? need - had : 0;
-            back[i] = had > need ? had - need : 0;
-            need_sum += more[i];
-            back_sum += back[i];
+            moved[i] = need > had ? need - had : (uint64_t)(had - need) << 32;
+            mine_moved += moved[i];
             if (first + i < n) {
                 t.row[first + i] = (uint32_t)min(row, most);
                 t.base[first + i] = base[i];
@@ -156,22 +154,21 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
             }
             row = end;
         }
-        uint64_t all_need, all_back;
-        uint64_t rank = sum_before<kPlanWarps>(need_sum, sums[1], &all_need), gone = sum_before<kPlanWarps>(back_sum, sums[2], &all_back);
+        uint64_t all_moved;
+        uint64_t before = sum_before<kPlanWarps>(mine_moved, sums[1], &all_moved);
 #pragma unroll
         for (uint32_t i = 0; i < kPlanEach; ++i) {
             if (first + i < n) {
-                t.rank[first + i] = (uint32_t)rank;
-                t.back[first + i] = (uint32_t)gone;
+                t.rank[first + i] = (uint32_t)before;
+                t.back[first + i] = (uint32_t)(before >> 32);
             }
-            rank += more[i];
-            gone += back[i];
+            before += moved[i];
         }
         const uint32_t row0 = (uint32_t)min(rows_before, most), row1 = (uint32_t)min(rows_before + all_rows, most);
         if (tid == 0) {
             t.row[n] = row1;
-            t.rank[n] = (uint32_t)all_need;
-            t.back[n] = (uint32_t)all_back;
+            t.rank[n] = (uint32_t)all_moved;
+            t.back[n] = (uint32_t)(all_moved >> 32);
         }
         all_here<CLUSTER>();  // the tile is there, and nobody reads the lengths any more
         if (leader) {
@@ -182,27 +179,45 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
                 a.cu_q[s0 + first + i + 1] = (int32_t)(t.row[first + i] + rows[i]);
             }
         }
-        // the ring's r-th block (from the tile's first); -1 when it is empty
-        auto taken = [&](uint32_t r) {
+        // where the ring's r-th block (from the tile's first) stands; null when it is empty
+        auto place = [&](uint32_t r) -> const int32_t * {
             const uint64_t k = rank_before + r;
-            if (k >= count) return -1;
+            if (k >= count) return nullptr;
             const uint32_t p = head + (uint32_t)k;
-            return a.free_ids[p < cap ? p : p - cap];
+            return a.free_ids + (p < cap ? p : p - cap);
         };
         for (uint32_t r = at; r < t.rank[n]; r += step) {
             const uint32_t i = owner(t.rank, n, r);
-            const int32_t id = taken(r);
-            full |= rank_before + r >= count;
+            const int32_t *from = place(r);
+            const int32_t id = from ? *from : -1;
+            full |= !from;
             a.table[(uint64_t)(s0 + i) * a.table_stride + t.had[i] + (r - t.rank[i])] = id;
         }
-        for (uint32_t x = row0 + at; x < row1; x += step) {
-            const uint32_t i = owner(t.row, n, x), pos = t.base[i] + (x - t.row[i]), b = pos >> a.block_shift, had = t.had[i];
-            int32_t id = -1;
-            if (b < had) id = a.table[(uint64_t)(s0 + i) * a.table_stride + b];
-            else if (b < a.table_blocks) id = taken(t.rank[i] + (b - had));
-            else full = true;
-            a.slots[x] = (uint32_t)id < a.n_blocks ? ((int64_t)id << a.block_shift) + (pos & ((1u << a.block_shift) - 1u)) : -1;
-            if (a.positions) a.positions[x] = (int32_t)pos;
+        for (uint64_t x0 = row0 + at; x0 < row1; x0 += kRows * (uint64_t)step) {  // kRows look-ups a thread under way at once
+            const int32_t *where[kRows];
+            uint32_t pos[kRows];
+            int32_t id[kRows];
+#pragma unroll
+            for (uint32_t k = 0; k < kRows; ++k) {
+                const uint64_t x = x0 + k * (uint64_t)step;
+                where[k] = nullptr;
+                if (x >= row1) continue;
+                const uint32_t i = owner(t.row, n, (uint32_t)x), had = t.had[i];
+                pos[k] = t.base[i] + ((uint32_t)x - t.row[i]);
+                const uint32_t b = pos[k] >> a.block_shift;
+                if (b < had) where[k] = a.table + (uint64_t)(s0 + i) * a.table_stride + b;
+                else if (b < a.table_blocks) where[k] = place(t.rank[i] + (b - had));
+                else full = true;
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kRows; ++k) id[k] = where[k] ? *where[k] : -1;
+#pragma unroll
+            for (uint32_t k = 0; k < kRows; ++k) {
+                const uint64_t x = x0 + k * (uint64_t)step;
+                if (x >= row1) continue;
+                a.slots[x] = (uint32_t)id[k] < a.n_blocks ? ((int64_t)id[k] << a.block_shift) + (pos[k] & ((1u << a.block_shift) - 1u)) : -1;
+                if (a.positions) a.positions[x] = (int32_t)pos[k];
+            }
         }
         if (t.back[n]) {
             const uint32_t lane = tid & 31u, warp = cta * kPlanWarps + tid / 32, room = cap - count;
@@ -210,6 +225,14 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
             // the ids of up to kLook x 32 entries of the run from r on; owners go up with r
             uint32_t i = 0;
             auto look = [&](uint32_t r, int32_t *id) {
+                const uint32_t o = __shfl_sync(0xffffffffu, i, 0), end = t.back[o + 1];  // (lane 0 has the lowest owner)
+                if (r + 32 * kLook <= min(end, r1)) {  // all of one sequence
+                    const int32_t *p = a.table + (uint64_t)(s0 + o) * a.table_stride + t.had[o] - (end - r) + lane;
+#pragma unroll
+                    for (uint32_t k = 0; k < kLook; ++k) id[k] = p[32 * k];
+                    i = o;
+                    return;
+                }
                 uint32_t at[kLook];
 #pragma unroll
                 for (uint32_t k = 0; k < kLook; ++k) {
@@ -258,7 +281,7 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
             returned = min(returned + all, room);
         }
         rows_before += all_rows;
-        rank_before += all_need;
+        rank_before += (uint32_t)all_moved;
         __syncthreads();  // the tile and the sums may be written again
     }
     for (uint64_t x = min(rows_before, most) + at; x < a.total_rows; x += step) {

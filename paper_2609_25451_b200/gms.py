@@ -118,13 +118,14 @@ class KvEvictArgs(C.Structure):
 
 
 class KvPlanArgs(C.Structure):
+    _device = None  # of the tensors that it was made of
     _fields_ = [(n, C.c_void_p) for n in ("lens", "new_lens", "drop_lens", "lens_out", "block_table", "free_ids", "free_state",
                                           "free_state_out", "cu_q", "slots", "positions", "status")] + [("table_stride", C.c_uint64)] + [
                 (n, C.c_uint32) for n in ("n_seq", "total_rows", "table_blocks", "free_cap", "n_blocks", "block_tokens")]
 
 
 class KvAppendArgs(C.Structure):
-    _made = None  # what the tensors that it was made of have
+    _made = _device = None  # what the tensors that it was made of have, and where they are
     _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "slots", "positions", "n_rows", "inv_freq", "axes", "q_weight", "k_weight")] + [
                 (n, C.c_uint64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
                                           "v_head_stride", "out_token_stride", "out_head_stride", "positions_stride")] + [
@@ -139,7 +140,7 @@ class KvState(C.Structure):
 class KvDeltaArgs(C.Structure):
     """``gms_kv_delta_args``; usually made by :func:`kv_delta_args`, which also keeps the tensors alive."""
 
-    _made = None  # what the tensors that it was made of have
+    _made = _device = None  # what the tensors that it was made of have, and where they are
     _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "out", "g", "beta", "cu_q", "past_lens", "src_table", "dst_table", "workspace",
                                           "status")] + [
                 (n, C.c_uint64) for n in ("workspace_bytes", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
@@ -563,6 +564,22 @@ def gms_kv_evict(pool: KvPool, layout: KvLayout, args: KvEvictArgs, stream=None)
     _check(lib().gms_kv_evict(_ref(pool), _ref(layout), _ref(args), _stream(stream)), "gms_kv_evict")
 
 
+def _one_device(tensors):
+    """The index of the GPU that all of them are on (pinned ones aside; None: none is on one)."""
+    found = {t.device.index for t in tensors if t is not None and t.is_cuda}
+    if len(found) > 1:
+        raise ValueError(f"tensors are on different devices: {sorted(found)}")
+    return found.pop() if found else None
+
+
+def _on_current_device(args):
+    if args is not None and args._device is not None:
+        import torch
+
+        if args._device != torch.cuda.current_device():
+            raise ValueError(f"tensors are on device {args._device}, the current one is {torch.cuda.current_device()}")
+
+
 def _strides(t):
     return (0, 0) if t is None else (t.stride(0) * t.element_size(), t.stride(1) * t.element_size())
 
@@ -601,10 +618,12 @@ def kv_plan_args(*, n_blocks: int, block_tokens: int, lens, new_lens, block_tabl
                    n_seq=n_seq, total_rows=rows, table_blocks=block_table.shape[1], free_cap=free_ids.shape[0], n_blocks=n_blocks,
                    block_tokens=block_tokens)
     a._keep = flat + (block_table, slots, status)
+    a._device = _one_device(tuple(t for t in a._keep if hasattr(t, "is_cuda")))
     return a
 
 
 def gms_kv_plan(args: KvPlanArgs, stream=None):
+    _on_current_device(args)
     _check(lib().gms_kv_plan(_ref(args), _stream(stream)), "gms_kv_plan")
 
 
@@ -652,11 +671,13 @@ def kv_append_args(*, slots=None, q=None, k=None, v=None, q_out=None, positions=
                      n_heads=0 if q is None else q.shape[1], rotary_dim=rotary, n_axes=positions.shape[0] if two else 1, pairs=pairs,
                      weight_dtype=weight_dtype, weight_offset=weight_offset, eps=eps, rope_scale=rope_scale)
     a._keep = (q, k, v, q_out, slots, positions, n_rows, inv_freq, axes, q_weight, k_weight)
+    a._device = _one_device(tuple(t for t in a._keep if hasattr(t, "is_cuda")))
     a._made = (dtype, dim, None if k is None else k.shape[1])
     return a
 
 
 def gms_kv_append(pool: KvPool, layout: KvLayout, args: KvAppendArgs, stream=None):
+    _on_current_device(args)
     if layout is not None and args is not None and args._made is not None:
         dtype, dim, heads = args._made
         if dtype != layout.dtype or dim != layout.head_dim or heads not in (None, layout.n_kv_heads):
@@ -692,6 +713,7 @@ def kv_delta_args(*, q, k, v, out, src_table, dst_table=None, g=None, beta=None,
                     dst_stride=row(dst_table, dst_table.shape[1]), n_seq=n_seq, n_key_heads=q.shape[1], total_q=rows, max_q=max_q, dtype=dtype,
                     unit_qk=0 if unit_eps is None else 1, unit_eps=unit_eps or 0.0, scale=scale)
     a._keep = (q, k, v, out, g, beta, cu_q, past_lens, src_table, dst_table, status)
+    a._device = _one_device(tuple(t for t in a._keep if hasattr(t, "is_cuda")))
     a._made = (v.shape[1], dim, min(src_table.shape[1], dst_table.shape[1]))
     if workspace is not None:
         a.set_workspace(workspace)
@@ -714,6 +736,7 @@ def gms_kv_delta_workspace(pool: KvPool, state: KvState, args: KvDeltaArgs) -> i
 
 
 def gms_kv_delta(pool: KvPool, state: KvState, args: KvDeltaArgs, stream=None):
+    _on_current_device(args)
     _fits_state(pool, state, args)
     _check(lib().gms_kv_delta(_ref(pool), _ref(state), _ref(args), _stream(stream)), "gms_kv_delta")
 

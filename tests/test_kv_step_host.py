@@ -172,3 +172,21 @@ def test_binding_refuses_tensors_that_do_not_fit():
     for bad in ({}, dict(q=x[:, :, :32]), dict(out=x[:, :2]), dict(g=torch.zeros(5, 3)), dict(cu_q=torch.zeros(1, **i32))):
         with pytest.raises(ValueError):
             gms.kv_delta_args(**{**dict(q=x, k=x, v=x, out=x, src_table=torch.zeros(3, 2, **i32), scale=1.0), **bad})
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+
+    def on(i):
+        return SimpleNamespace(is_cuda=i is not None, device=SimpleNamespace(index=i))
+
+    assert gms._one_device((on(1), None, on(1), on(None))) == 1 and gms._one_device((None, on(None))) is None
+    with pytest.raises(ValueError):
+        gms._one_device((on(0), on(1)))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    for args, call in ((plan(), gms.gms_kv_plan), (append(), lambda a: gms.gms_kv_append(pool(), layout(), a)),
+                       (delta(), lambda a: gms.gms_kv_delta(pool(), state(), a))):
+        args._device = 1
+        with pytest.raises(ValueError):
+            call(args)
