@@ -614,9 +614,10 @@ int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gm
  * (unit_qk: q and k are first divided by sqrt(sum x^2 + unit_eps)).  S begins as the state in src_table, or as zeros where
  * past_lens[s] is 0, and the state after the last row goes to dst_table (a sequence without rows: as it began).  g NULL counts as
  * zeros, beta NULL as ones.  g is a logarithm, at most 0 in earnest; -infinity clears the state.
- * Sequences of many rows are done in chunks of 64 on tensor cores: products of 16-bit inputs with S, d and decays, which enter as
- * sums of two 16-bit terms (2^-16 relative) wherever they go on into a state; what goes into `out` alone enters as one.  State
- * and sums are kept in 32 bits.  What a row does not depend on cannot reach it, whatever bits it holds.
+ * Sequences of more than 24 rows are done in chunks of 64 on tensor cores: products of the 16-bit inputs with S, d and decays, which
+ * enter as sums of two 16-bit terms (2^-16 relative) wherever they go on into a state; for `out` the state before the chunk and the
+ * weights of its rows enter as one (its error is 1.5 times that of its last rounding).  States and sums are kept in 32 bits.  What a row
+ * does not depend on cannot reach it, whatever bits it holds.
  * src_table and dst_table may be the same (states are updated in place), and rows of src_table may be equal (several sequences go on
  * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence.  An id outside [0, n_blocks)
  * reads as zeros and is not written; GMS_DEV_HOLE in `status` tells of it.  Rows that no sequence owns, and rows of a sequence

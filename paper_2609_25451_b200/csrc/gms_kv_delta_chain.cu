@@ -61,13 +61,12 @@ __device__ __forceinline__ void fetch_chunk(const DeltaArgs &a, Stage<D, W> &st,
 // What the warps of a slice tell each other: accumulators, and first factors of products (a lane's part of 16 x 16).
 template <int D>
 struct Talk {
-    uint4 s[2][D / 16][32];    // S before a chunk and the next, the first of its two terms
+    uint4 s[D / 16][32];       // S before the chunk, the first of its two terms
     float4 sum[4][3][2][32];   // [to][from the others]: what X is the sum of
     uint4 x[4][2][32];         // V - f X of the 16 rows of each warp, in two terms
-    uint4 dw[4][2][32];        // w d, in two terms
-    uint4 d[2][4][32];
-    float2 s_unit[2][4][8], x_unit[4][8], dw_unit[4][8], d_unit[2][4][8];  // f16: powers of two that rows' terms are multiples of
-    uint32_t odd[2][4];        // the chunk is done row by row
+    uint4 d[4][2][32], dw[4][2][32];                           // d and w d, the same
+    float2 s_unit[4][8], x_unit[4][8], dw_unit[4][8], d_unit[4][8];  // f16: powers of two that rows' terms are multiples of
+    uint32_t odd[4];           // the chunk is done row by row
 };
 template <int D, int W>
 struct RelayShape {
@@ -78,7 +77,7 @@ template <int D, int W>
 struct RelaySmem {
     Stage<D, W> stage[3];
     Talk<D> talk[W];
-    uint64_t full[3], empty[3], ready[W][2], taken[W][2];
+    uint64_t full[3], empty[3], ready[W], taken[W];
 };
 
 // A slice, 16 value columns of a head's state, has four warps that carry the state on and one that makes `out`.  The state lies,
@@ -109,11 +108,10 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             ptx::mbar_init(smem_u32(&m.full[i]), RelayShape<D, W>::kFetchLanes);
             ptx::mbar_init(smem_u32(&m.empty[i]), 5 * W);
         }
-        for (int i = 0; i < W; ++i)
-            for (int j = 0; j < 2; ++j) {
-                ptx::mbar_init(smem_u32(&m.ready[i][j]), 4);
-                ptx::mbar_init(smem_u32(&m.taken[i][j]), 1);
-            }
+        for (int i = 0; i < W; ++i) {
+            ptx::mbar_init(smem_u32(&m.ready[i]), 4);
+            ptx::mbar_init(smem_u32(&m.taken[i]), 1);
+        }
         ptx::fence_mbar_init();
     }
     __syncthreads();
@@ -148,22 +146,28 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
     };
     if (warp >= 4 * W) {
-        // out = h Q S + P d, with S before the chunk (one term each), two tiles of 16 rows at a time
+        // out = h Q S + P d, with S before the chunk (one term of S and of P, two of d), two tiles of 16 rows at a time
         const uint32_t slice = warp - 4 * W;
         Talk<D> &talk = m.talk[slice];
 #pragma unroll 1
         for (int chunk = 0; chunk < chunks; ++chunk) {
-            const int stage = chunk % kStages, turn = chunk & 1, n = min(rows - chunk * C, C);
+            const int stage = chunk % kStages, n = min(rows - chunk * C, C);
             Stage<D, W> &st = m.stage[stage];
             uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
             wait(&m.full[stage], chunk / kStages);
-            wait(&m.ready[slice][turn], chunk / 2);
-            if (!(talk.odd[turn][0] | talk.odd[turn][1] | talk.odd[turn][2] | talk.odd[turn][3])) {
-                uint4 sf[D / 16], df[4];
+            wait(&m.ready[slice], chunk);
+            const bool by_row = talk.odd[0] | talk.odd[1] | talk.odd[2] | talk.odd[3];
+            uint4 sf[D / 16], df[4][2];
+            float2 su[4], du[4];
 #pragma unroll
-                for (int kt = 0; kt < D / 16; ++kt) sf[kt] = talk.s[turn][kt][lane];
+            for (int kt = 0; kt < D / 16; ++kt) sf[kt] = talk.s[kt][lane];
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt) df[kt] = talk.d[turn][kt][lane];
+            for (int kt = 0; kt < 4; ++kt) {
+                df[kt][0] = talk.d[kt][0][lane], df[kt][1] = talk.d[kt][1][lane];
+                if (kHalf) su[kt] = talk.s_unit[kt][g], du[kt] = talk.d_unit[kt][g];
+            }
+            arrive(&m.taken[slice]);
+            if (!by_row) {
 #pragma unroll
                 for (int pair = 0; pair < 2; ++pair) {
                     float Y[2][2][4] = {};
@@ -171,7 +175,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
 #pragma unroll
                     for (int kt = 0; kt < D / 16; ++kt) {
                         if (kHalf && kt % KQ == 0) {
-                            const float2 next = talk.s_unit[turn][kt / KQ][g];
+                            const float2 next = su[kt / KQ];
                             if (kt) change(Y[0], unit, next), change(Y[1], unit, next);
                             unit = next;
                         }
@@ -197,14 +201,17 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
                         for (int kt = 0; kt < 4; ++kt) {
                             if (kt > tile) break;
                             if (kHalf) {
-                                const float2 next = talk.d_unit[turn][kt][g];
+                                const float2 next = du[kt];
                                 change(Y[i], u, next);
                                 u = next;
                             }
                             uint32_t b[4];
                             ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(16 * tile + b_row, 2 * kt + b_piece), b);
-                            mma16816(Y[i][0], &df[kt].x, b[0], b[1], T());
-                            mma16816(Y[i][1], &df[kt].x, b[2], b[3], T());
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                mma16816(Y[i][0], &df[kt][t].x, b[0], b[1], T());
+                                mma16816(Y[i][1], &df[kt][t].x, b[2], b[3], T());
+                            }
                         }
                         if (kHalf) change(Y[i], u, one);
                         // (through the slice's part of V's tile, which the other warps have read)
@@ -223,7 +230,6 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
                     if (r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
                 }
             }
-            arrive(&m.taken[slice][turn]);
             arrive(&m.empty[stage]);
         }
         return;
@@ -262,10 +268,9 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
     };
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk) {
-        const int stage = chunk % kStages, turn = chunk & 1, n = min(rows - chunk * C, C);
+        const int stage = chunk % kStages, n = min(rows - chunk * C, C);
         Stage<D, W> &st = m.stage[stage];
         wait(&m.full[stage], chunk / kStages);
-        if (chunk >= 2) wait(&m.taken[slice][turn], chunk / 2 - 1);
         // what needs no news from the other warps is read before they meet
         uint32_t kb[4][KQ][4], V[4];
 #pragma unroll
@@ -273,6 +278,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
 #pragma unroll
             for (int k = 0; k < KQ; ++k) ldmatrix_x4(smem_u32(st.k) + piece<P>(16 * i + b_row, 2 * (mine * KQ + k) + b_piece), kb[i][k]);
         ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(row0 + b_row, 2 * slice + b_piece), V);
+        if (chunk) wait(&m.taken[slice], chunk - 1);
         // S in two terms
         uint4 hi[KQ], lo[KQ];
         float2 su = one;
@@ -283,12 +289,12 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
                 const float2 u = scales(S[2 * k], S[2 * k + 1]);
                 su = make_float2(fminf(su.x, u.x), fminf(su.y, u.y));
             }
-            tell(talk.s_unit[turn][mine], inverse(su));
+            tell(talk.s_unit[mine], inverse(su));
         }
 #pragma unroll
         for (int k = 0; k < KQ; ++k) {
             terms(S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
-            talk.s[turn][mine * KQ + k][lane] = hi[k];
+            talk.s[mine * KQ + k][lane] = hi[k];
         }
         // its part of X = S K^T for all rows
         float x[4][2][4] = {};
@@ -306,7 +312,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
 #pragma unroll
         for (int e = 0; e < 4; ++e) odd |= ((V[e] & kOnes) == kOnes) | ((V[e] >> 16 & kOnes) == kOnes);
         odd = __any_sync(0xffffffffu, odd);
-        if (lane == 0) talk.odd[turn][mine] = odd;
+        if (lane == 0) talk.odd[mine] = odd;
         float X[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -328,9 +334,9 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             ldmatrix_x4(smem_u32(st.w.tile[1]) + at, tb[1][kt]);
         }
         together();
-        if (talk.odd[turn][0] | talk.odd[turn][1] | talk.odd[turn][2] | talk.odd[turn][3]) {
+        if (talk.odd[0] | talk.odd[1] | talk.odd[2] | talk.odd[3]) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
-            arrive(&m.ready[slice][turn]);
+            arrive(&m.ready[slice]);
             uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
             float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(talk.x);  // [2][4][32], in the place of what is not needed
             float(*zs)[4][32] = reinterpret_cast<float(*)[4][32]>(talk.dw);
@@ -437,10 +443,10 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         u = one;
         if (kHalf) {
             u = scales(d[0], d[1]);
-            tell(talk.d_unit[turn][mine], make_float2(st.w.p_unit * flipped(u.x), st.w.p_unit * flipped(u.y)));
+            tell(talk.d_unit[mine], make_float2(st.w.p_unit * flipped(u.x), st.w.p_unit * flipped(u.y)));
         }
-        talk.d[turn][mine][lane] = make_uint4(pack2(d[0][0] * u.x, d[0][1] * u.x, T()), pack2(d[0][2] * u.y, d[0][3] * u.y, T()),
-                                              pack2(d[1][0] * u.x, d[1][1] * u.x, T()), pack2(d[1][2] * u.y, d[1][3] * u.y, T()));
+        terms(d[0], d[1], u, own_hi, own_lo);
+        talk.d[mine][0][lane] = own_hi, talk.d[mine][1][lane] = own_lo;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
@@ -459,7 +465,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[nt][e] *= all;
-        arrive(&m.ready[slice][turn]);
+        arrive(&m.ready[slice]);
         together();
         unit = one;
 #pragma unroll
@@ -712,7 +718,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
             u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
             di0 = st.w.p_unit * flipped(u0), di1 = st.w.p_unit * flipped(u1);
         }
-        // out = h Y + P d (one term each; f16: in units of P and d meanwhile)
+        // out = h Y + P d (one term of P, two of d; f16: in units of P and d meanwhile)
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
@@ -721,15 +727,18 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         }
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            const uint32_t x[4] = {pack2(d[2 * kt][0] * u0, d[2 * kt][1] * u0, T()), pack2(d[2 * kt][2] * u1, d[2 * kt][3] * u1, T()),
-                                   pack2(d[2 * kt + 1][0] * u0, d[2 * kt + 1][1] * u0, T()), pack2(d[2 * kt + 1][2] * u1, d[2 * kt + 1][3] * u1, T())};
+            uint32_t hi[4], lo[4], b[CT][2];
 #pragma unroll
             for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t b[4];
-                ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), b);
-                mma16816(Y[nt], x, b[0], b[1], T());
-                mma16816(Y[nt + 1], x, b[2], b[3], T());
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
+            terms(d + 2 * kt, u0, u1, hi, lo);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], lo, b[nt][0], b[nt][1], T());
         }
         // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
 #pragma unroll
