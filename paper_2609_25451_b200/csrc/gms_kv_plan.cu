@@ -301,7 +301,10 @@ __global__ void __launch_bounds__(CLUSTER ? 1024 : 512) kv_plan_kernel(const __g
 cudaError_t launch_plan(const PlanArgs &a, cudaStream_t s)
 {
     static std::atomic<uint64_t> done[2];
-    const bool cluster = (uint64_t)a.total_rows + 4ull * a.n_seq > 8192;
+    // Eight CTAs pay where there is more to do than a second start and their exchange cost (us, one CTA / eight; rows a sequence x sequences:
+    // 1 x 512 4.9 / 5.8, 1 x 1,024 6.3 / 6.4, 1 x 2,048 9.1 / 6.7, 16 x 128 6.4 / 5.7, 2,000 x 1 4.2 / 4.8, 4,000 x 1 5.3 / 4.8,
+    // 1,000 x 8 9.8 / 5.2, 64 x 511 53.8 / 8.9).
+    const bool cluster = (uint64_t)a.total_rows + a.n_seq > 2048;
     cudaError_t e = cluster ? allow_smem(kv_plan_kernel<true>, sizeof(Tile), done[1]) : allow_smem(kv_plan_kernel<false>, sizeof(Tile), done[0]);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
