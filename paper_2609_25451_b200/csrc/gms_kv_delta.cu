@@ -374,6 +374,12 @@ int make_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_
 
 // Slots for every sequence's chunks, wherever its rows begin; 0: no sequence is long enough.
 uint64_t chunk_slots(const DeltaArgs &a) { return a.max_q > kMostByRow ? a.total_q / kChunkRows + a.n_seq : 0; }
+// They and the order of the sequences.
+uint64_t work_bytes(const DeltaArgs &a)
+{
+    const uint64_t slots = chunk_slots(a);
+    return slots ? slots * a.n_heads * sizeof(ChunkWork) + ((uint64_t)a.n_seq * 4 + 255) / 256 * 256 : 0;
+}
 
 }  // namespace
 }  // namespace gms
@@ -385,7 +391,7 @@ int gms_kv_delta_workspace(const gms_kv_pool *pool, const gms_kv_state *state, c
     if (!nbytes) return GMS_ERR_NULL;
     gms::DeltaArgs a;
     const int rc = gms::make_delta(pool, state, args, &a);
-    if (rc == GMS_OK) *nbytes = gms::chunk_slots(a) * a.n_heads * sizeof(gms::ChunkWork);
+    if (rc == GMS_OK) *nbytes = gms::work_bytes(a);
     return rc;
 }
 
@@ -395,7 +401,7 @@ int gms_kv_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_k
     const int rc = gms::make_delta(pool, state, args, &a);
     if (rc != GMS_OK) return rc;
     if (a.n_seq == 0) return GMS_OK;
-    const uint64_t slots = gms::chunk_slots(a), need = slots * a.n_heads * sizeof(gms::ChunkWork);
+    const uint64_t slots = gms::chunk_slots(a), need = gms::work_bytes(a);
     if (need && !args->workspace) return GMS_ERR_NULL;
     if (need > args->workspace_bytes) return GMS_ERR_RANGE;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -404,6 +410,7 @@ int gms_kv_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_k
     if (slots) {
         a.chunks = static_cast<uint8_t *>(args->workspace);
         a.n_slots = (uint32_t)slots;
+        a.order = reinterpret_cast<uint32_t *>(a.chunks + slots * a.n_heads * sizeof(gms::ChunkWork));
         e = gms::launch_delta_prep(a, args->dtype, state->head_dim, s);
         if (e == cudaSuccess) e = gms::launch_delta_chain(a, args->dtype, state->head_dim, s);
         if (e != cudaSuccess) return gms::report_cuda_error(e);

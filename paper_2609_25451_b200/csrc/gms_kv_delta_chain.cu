@@ -85,7 +85,8 @@ struct RelaySmem {
 // element, a first factor of the next: S -> X = S K^T (each warp its keys' part, for all rows) -> d = (V - f X) T^T -> S, each warp
 // 16 of the rows in between, with three exchanges through shared memory a chunk.  The fifth warp gets S and d handed and works
 // beside the next chunk.  W slices share a chunk's operands, which two more warps fetch ahead.  Bound by the latency of that
-// sequence of small products and exchanges: @@
+// sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 275 us or 4,080 cycles a chunk (one: 3,060),
+// in which the products take 48 % of the tensor cores' cycles and loads, stores and exchanges 76 % of shared memory's.
 template <class T, int D, int W>
 __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -96,12 +97,13 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kParts = D / (16 * W);
-    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, s = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
+    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, rank = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
     const uint32_t col0 = part * W * 16;  // of the CTA
     ptx::grid_launch_dependents();
     ptx::grid_wait();
+    const uint32_t s = a.order[rank];
+    if (s >= a.n_seq) return;
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
-    if (!delta_in_chunks(a, rows)) return;
     const int chunks = (rows + C - 1) / C;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -512,7 +514,8 @@ struct SoloSmem {
 // A warp has 16 value columns of a head's state, transposed, as accumulators of mma.sync (16 x D): what is an accumulator of one
 // product is, element for element, a first factor of the next, S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out, so nothing
 // leaves the registers between the products and no warp waits for another.  W of them (16 W columns of a head) share a chunk's
-// operands, which further warps fetch ahead.  Bound by the rate of the products: 400 of them a chunk and warp, 8.3 cycles each.
+// operands, which further warps fetch ahead.  Bound by the rate of the products, 420 of them a chunk and warp at 128 keys, 8.3 cycles
+// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,500 cycles a chunk.
 template <class T, int D, int W>
 __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kCtas) kv_delta_solo_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -523,12 +526,13 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kParts = D / (16 * W);
-    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, s = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
+    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, rank = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
     const uint32_t col0 = part * W * 16;  // of the CTA
     ptx::grid_launch_dependents();
     ptx::grid_wait();
+    const uint32_t s = a.order[rank];
+    if (s >= a.n_seq) return;
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
-    if (!delta_in_chunks(a, rows)) return;
     const int chunks = (rows + C - 1) / C;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -818,13 +822,23 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
     static std::atomic<uint64_t> done;
     const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W>, 232448, done);
     if (e != cudaSuccess) return e;
-    const uint32_t ctas = a.n_seq * a.n_heads * (D / (16 * W)), smem = ctas <= 148 && sizeof(SoloSmem<D, W>) < kOneAnSm ? kOneAnSm : sizeof(SoloSmem<D, W>);
-    return launch_dependent(kv_delta_solo_kernel<T, D, W>, ctas, SoloShape<D, W>::kThreads, smem, s, a);
+    const uint32_t ctas = a.n_seq * a.n_heads * (D / (16 * W));
+    if (SoloShape<D, W>::kCtas == 1) return launch_dependent(kv_delta_solo_kernel<T, D, W>, ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s, a);
+    // Two an SM: they start when the kernel ahead has ended, or the first two, the longest, come to share the first SM that is free
+    // (13 sequences of up to 2,001 rows, 16 heads of 64: 204 us so, 163 us waiting; fp16 198 and 183 us).
+    kv_delta_solo_kernel<T, D, W><<<ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s>>>(a);
+    const cudaError_t f = cudaGetLastError();
+    if (f == cudaSuccess) count_launches(1);
+    return f;
 }
+// The lengths are on the device: as many sequences count as have max_q rows together.  While an SM each is enough for their slices (a
+// pair of slices each), relays are faster, beyond that solos (us, first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows,
+// 4 heads of 128 228 / 402; 32 heads of 128 335 / 466; the same and 31 single rows 364 / 492; 2 of 4,000 335 / 269; 8 of 1,000 325 / 278;
+// 4 of 100 to 4,000 417 / 375; 1 of 8,192, 32 heads of 64, one slice an SM 260, two 306, solo 396).
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
 {
-    const uint64_t slices = (uint64_t)a.n_seq * a.n_heads * (D / 16);
+    const uint64_t alike = ((uint64_t)a.total_q + a.max_q / 2) / a.max_q, slices = (alike < a.n_seq ? alike : a.n_seq) * a.n_heads * (D / 16);
     if (slices <= 148) return launch_relay<T, D, 1>(a, s);
     return slices <= 2 * 148 ? launch_relay<T, D, 2>(a, s) : launch_solo<T, D, 4>(a, s);
 }

@@ -34,6 +34,43 @@ __device__ __forceinline__ bool find_chunk(const DeltaArgs &a, uint32_t id, uint
 
 constexpr uint32_t kPrepThreads = 128, kPrepHeads = 4;
 
+// The sequences that are done in chunks, longest first (by their share of the longest possible, in 256 steps; which of two in the
+// same step comes first is open, and no result depends on it): the chain's CTAs start in this order, so that short sequences fill up
+// what the long ones leave.
+__device__ void put_order(const DeltaArgs &a, uint32_t *count)
+{
+    const uint32_t tid = threadIdx.x;
+    auto step_of = [&](int rows) { return 255u - (uint32_t)((uint64_t)(rows - 1) * 256 / a.max_q); };
+    for (uint32_t i = tid; i < 256; i += kPrepThreads) count[i] = 0;
+    __syncthreads();
+    for (uint32_t s = tid; s < a.n_seq; s += kPrepThreads) {
+        const int rows = delta_rows(a, s);
+        if (delta_in_chunks(a, rows)) atomicAdd(&count[step_of(rows)], 1u);
+    }
+    __syncthreads();
+    if (tid < 32) {
+        uint32_t n[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] = count[8 * tid + i], sum += n[i];
+        uint32_t before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
+            if (tid >= (uint32_t)o) before += x;
+        }
+        if (tid == 31) count[256] = before;
+        before -= sum;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) count[8 * tid + i] = before, before += n[i];
+    }
+    __syncthreads();
+    for (uint32_t s = tid; s < a.n_seq; s += kPrepThreads) {
+        const int rows = delta_rows(a, s);
+        if (delta_in_chunks(a, rows)) a.order[atomicAdd(&count[step_of(rows)], 1u)] = s;
+        if (s >= count[256]) a.order[s] = kNone;
+    }
+}
+
 // A lower triangle of 64 x 64, in blocks of 16 x 16, as two bf16 terms (2^-17 relative together).
 struct Terms64 {
     uint8_t hi[sizeof(ChunkWork::tile[0])], lo[sizeof(ChunkWork::tile[0])];
@@ -116,7 +153,9 @@ __device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const floa
 // for each value head of the key head the decays, the inverse and what goes to the workspace.  The inverse of I + A: its diagonal
 // blocks of 16 x 16 a warp each (a lane has a column and goes down it: x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
 //   (X 0; Y Z)^-1 = (X^-1 0; -Z^-1 Y X^-1 Z^-1)
-// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by issue and shared memory, @@PREP@@
+// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by the issue of its 7,100 instructions
+// a chunk and head and by its warps' waits for one another, which five CTAs an SM fill up: 8,192 rows of 32 heads of 128, bf16, 59 us
+// (T, P and factors a CTA in 32 bits 172; as blocks of two-term factors 62.5, four CTAs an SM).
 template <class T, int D>
 __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ? 4 : 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -125,9 +164,13 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
     constexpr int C = kChunkRows, P = D / 8;
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32, g = lane / 4, t2 = 2 * (lane & 3u);
-    const uint32_t n_key = a.n_heads / a.group, kh = blockIdx.x % n_key, id = blockIdx.x / n_key;
     ptx::grid_wait();
     ptx::grid_launch_dependents();
+    if (blockIdx.x == 0) {
+        put_order(a, reinterpret_cast<uint32_t *>(raw));
+        return;
+    }
+    const uint32_t n_key = a.n_heads / a.group, kh = (blockIdx.x - 1) % n_key, id = (blockIdx.x - 1) / n_key;
     uint32_t s, chunk;
     if (!find_chunk(a, id, s, chunk)) return;
     const int all_rows = delta_rows(a, s);
@@ -384,7 +427,7 @@ cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
     static std::atomic<uint64_t> done;
     const cudaError_t e = allow_smem(kv_delta_prep_kernel<T, D>, sizeof(PrepSmem<D>), done);
     if (e != cudaSuccess) return e;
-    return launch_dependent(kv_delta_prep_kernel<T, D>, a.n_slots * (a.n_heads / a.group), kPrepThreads, sizeof(PrepSmem<D>), s, a);
+    return launch_dependent(kv_delta_prep_kernel<T, D>, a.n_slots * (a.n_heads / a.group) + 1, kPrepThreads, sizeof(PrepSmem<D>), s, a);
 }
 
 }  // namespace

@@ -6,6 +6,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from kv_delta_harness import BF16, F16, Delta  # noqa: E402
+from paper_2609_25451_b200 import gms  # noqa: E402
 
 
 @pytest.mark.parametrize("D,per", [(64, 8), (128, 2)])
@@ -58,3 +59,51 @@ def test_equal_calls_give_equal_bits():
     for _ in range(5):
         d.run()
         assert torch.equal(out, d.out_full) and torch.equal(raw, d.raw)
+
+
+@pytest.mark.parametrize("D,per,H", [(64, 8, 16), (128, 2, 4), (128, 2, 32)])
+def test_a_long_sequence_among_single_rows(D, per, H):
+    lens = tuple(700 if i == 21 else 1 for i in range(40))
+    Delta(11, lens=lens, D=D, per=per, H=H, K=H // 2, dtype=F16 if D == 64 else BF16, fresh=(21,)).check()
+
+
+def test_more_sequences_than_threads_make_the_order():
+    lens = tuple((i * 37) % 90 for i in range(300))  # most of them in chunks, some alike, some without rows
+    Delta(12, lens=lens, D=64, per=2, H=2, K=1, fresh=(0, 299)).check()
+
+
+def test_a_bound_above_the_longest_sequence():
+    Delta(13, lens=(30, 64, 3, 100, 90) * 6, D=128, per=2, H=4, K=4, max_q=1500).check()
+
+
+def test_a_replayed_call_orders_the_sequences_anew():
+    lens = [1] * 30
+    lens[2] = 400
+    d = Delta(14, lens=lens, D=128, per=2, H=4, K=2)
+    d.run()
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        gms.gms_kv_delta(d.desc, d.state, d.args, s.cuda_stream)
+    for at in ([(27, 400)], [(5, 140), (6, 200), (29, 62)]):
+        lens = [1] * 30
+        for i, n in at:
+            lens[i] = n
+        lens[0] += d.T - sum(lens)
+        d.lens = lens
+        d.cu_h = [0]
+        for n in lens:
+            d.cu_h.append(d.cu_h[-1] + n)
+        d.cu.copy_(torch.tensor(d.cu_h, dtype=torch.int32))
+        d.out_full.fill_(3.0)
+        before = d.raw.clone()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        after, out = d.raw.clone(), d.out_full.clone()
+        d.raw.copy_(before)
+        d.run()                                     # the same call without a graph
+        assert torch.equal(after, d.raw) and torch.equal(out, d.out_full)
+        d.raw.copy_(before)
+        d.check()
+        assert torch.equal(out, d.out_full)
