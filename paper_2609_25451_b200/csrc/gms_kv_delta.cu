@@ -127,8 +127,11 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     __shared__ RowSmem<D, W, B> m;
     const uint32_t tid = threadIdx.x, warp = tid / 32;
     const uint32_t slice = blockIdx.x % (D / W), h = blockIdx.x / (D / W) % a.n_heads, s = blockIdx.x / (D / W) / a.n_heads;
-    ptx::grid_wait();
+    // Beside the chunk kernels, which have waited for what was before them and have nothing to do with these sequences: what they leave
+    // of the GPU is filled up.  The last CTA waits for them, so that nothing after this kernel starts before they have ended.
+    if (!a.chunks) ptx::grid_wait();
     ptx::grid_launch_dependents();
+    if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
     const int first = delta_begin(a, s), rows = delta_rows(a, s);
     if (delta_in_chunks(a, rows)) return;
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
@@ -185,8 +188,9 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
         ptx::fence_mbar_init();
     }
     __syncthreads();
-    ptx::grid_wait();
+    if (!a.chunks) ptx::grid_wait();  // (as above)
     ptx::grid_launch_dependents();
+    if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
     // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
     bool late = false;
     auto wait = [&](uint64_t *bar, uint32_t use) {
@@ -294,9 +298,11 @@ cudaError_t launch_rows(const DeltaArgs &a, cudaStream_t s)
 {
     // Whole states pay from one and a half a CTA on: below that SMs stand idle or have two rounds to do (32 heads of 128, one row, us,
     // slices / whole states: 5 sequences 12.3 / 14.3, 8 14.3 / 14.3, 24 28.7 / 26.6; four rows: 5 16.4 / 16.4, 8 20.5 / 18.4, 24 43 / 35).
+    // Beside the chunk kernels small CTAs fill up better, up to eight times as many states (the whole call, a long prompt and single
+    // rows: 32 sequences 341 / 359, 64 243 / 228; 44 sequences of 9 to 51 rows, 24 heads 161 / 175).
     constexpr int W = 32;
     const uint64_t items = (uint64_t)a.n_seq * a.n_heads, held = 148 * StreamShape<D>::kCtas;
-    if (2 * items <= 3 * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);
+    if (2 * items <= (a.chunks ? 16 : 3) * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);
     static std::atomic<uint64_t> done;
     static_assert(sizeof(StreamSmem<D>) * StreamShape<D>::kCtas <= 231424, "");
     const cudaError_t e = allow_smem(kv_delta_stream_kernel<T, D>, sizeof(StreamSmem<D>), done);

@@ -831,14 +831,15 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
     if (f == cudaSuccess) count_launches(1);
     return f;
 }
-// The lengths are on the device: as many sequences count as have max_q rows together.  While an SM each is enough for their slices (a
-// pair of slices each), relays are faster, beyond that solos (us, first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows,
-// 4 heads of 128 228 / 402; 32 heads of 128 335 / 466; the same and 31 single rows 364 / 492; 2 of 4,000 335 / 269; 8 of 1,000 325 / 278;
-// 4 of 100 to 4,000 417 / 375; 1 of 8,192, 32 heads of 64, one slice an SM 260, two 306, solo 396).
+// The lengths are on the device: where there are more than two sequences for every max_q rows, as many count as have max_q rows, the
+// others being short.  While an SM each is enough for their slices (a pair of slices each), relays are faster, beyond that solos (us,
+// the first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows, 4 heads of 128 228 / 402, 32 heads of 128 335 / 466; 2 of
+// 4,000 335 / 269; 8 of 1,000 325 / 278; 4 of 100 to 4,000 417 / 375; 1 of 8,192, 32 heads of 64, one slice an SM 260, two 306, solo 396).
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
 {
-    const uint64_t alike = ((uint64_t)a.total_q + a.max_q / 2) / a.max_q, slices = (alike < a.n_seq ? alike : a.n_seq) * a.n_heads * (D / 16);
+    const uint64_t alike = ((uint64_t)a.total_q + a.max_q / 2) / a.max_q;
+    const uint64_t slices = (a.n_seq <= 2 * alike ? a.n_seq : alike) * a.n_heads * (D / 16);
     if (slices <= 148) return launch_relay<T, D, 1>(a, s);
     return slices <= 2 * 148 ? launch_relay<T, D, 2>(a, s) : launch_solo<T, D, 4>(a, s);
 }

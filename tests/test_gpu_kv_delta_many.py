@@ -107,3 +107,22 @@ def test_a_replayed_call_orders_the_sequences_anew():
         d.raw.copy_(before)
         d.check()
         assert torch.equal(out, d.out_full)
+
+
+@pytest.mark.parametrize("lens", [(1, 300, 2, 70, 24, 25) * 3, (900,) + (1,) * 60])
+def test_calls_one_behind_the_other(lens):
+    """What follows on the stream finds states and outputs, of long sequences and of short ones."""
+    a, b = (Delta(15, lens=lens, H=8, K=4, in_place=True) for _ in range(2))
+    seen = []
+    for _ in range(4):
+        a.run()
+        seen.append(a.out_full.clone())
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        for want in seen:
+            b.out_full.fill_(3.0)
+            gms.gms_kv_delta(b.desc, b.state, b.args, s.cuda_stream)
+            want.sub_(b.out_full)
+    torch.cuda.synchronize()
+    assert all(not x.any() for x in seen) and torch.equal(a.raw, b.raw)
