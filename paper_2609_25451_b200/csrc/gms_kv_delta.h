@@ -32,7 +32,7 @@ struct alignas(256) ChunkWork {
     uint8_t tile[3][10 * 512];  // T in two terms, P: blocks of 16 x 16 in and below the diagonal, laid out as `block_piece` says
     float f[kChunkRows], w[kChunkRows], h[kChunkRows];
     float gate[kChunkRows], beta[kChunkRows], rk[kChunkRows], rq[kChunkRows];  // for chunks that are done row by row
-    float all, t_unit, p_unit;                     // e^G of the chunk; f16: what the terms of T and P are multiples of
+    float all, p_unit;                             // e^G of the chunk; f16: what P is a multiple of
     uint32_t by_row;
 };
 

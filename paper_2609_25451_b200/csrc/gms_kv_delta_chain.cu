@@ -8,6 +8,8 @@ using ptx::ldmatrix_x4;
 using ptx::ldmatrix_x4_trans;
 using ptx::smem_u32;
 
+constexpr __nv_bfloat16 kWide{};  // the type of terms that have 32 bits' range
+
 // A chunk's operands.  V is the columns of the CTA, 16 for each of its W slices.
 template <int D, int W>
 struct Stage {
@@ -65,7 +67,7 @@ struct Talk {
     float4 sum[4][3][2][32];   // [to][from the others]: what X is the sum of
     uint4 x[4][2][32];         // V - f X of the 16 rows of each warp, in two terms
     uint4 d[4][2][32], dw[4][2][32];                           // d and w d, the same
-    float2 s_unit[4][8], x_unit[4][8], dw_unit[4][8], d_unit[4][8];  // f16: powers of two that rows' terms are multiples of
+    float2 s_unit[4][8], dw_unit[4][8], d_unit[4][8];  // f16: powers of two that rows' terms are multiples of
     uint32_t odd[4];           // the chunk is done row by row
 };
 template <int D, int W>
@@ -262,11 +264,12 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
     auto tell = [&](float2 *unit, float2 u) {
         if ((lane & 3u) == 0) unit[g] = u;
     };
-    auto terms = [](const float *x, const float *y, float2 u, uint4 &hi, uint4 &lo) {
-        split2<T>(x[0] * u.x, x[1] * u.x, hi.x, lo.x);
-        split2<T>(x[2] * u.y, x[3] * u.y, hi.y, lo.y);
-        split2<T>(y[0] * u.x, y[1] * u.x, hi.z, lo.z);
-        split2<T>(y[2] * u.y, y[3] * u.y, hi.w, lo.w);
+    auto terms = [](auto type, const float *x, const float *y, float2 u, uint4 &hi, uint4 &lo) {
+        using Term = decltype(type);
+        split2<Term>(x[0] * u.x, x[1] * u.x, hi.x, lo.x);
+        split2<Term>(x[2] * u.y, x[3] * u.y, hi.y, lo.y);
+        split2<Term>(y[0] * u.x, y[1] * u.x, hi.z, lo.z);
+        split2<Term>(y[2] * u.y, y[3] * u.y, hi.w, lo.w);
     };
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         }
 #pragma unroll
         for (int k = 0; k < KQ; ++k) {
-            terms(S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
+            terms(T(), S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
             talk.s[mine * KQ + k][lane] = hi[k];
         }
         // its part of X = S K^T for all rows
@@ -404,13 +407,8 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             X[nt][2] = to_f32(vb[0]) - f.x * X[nt][2];
             X[nt][3] = to_f32(vb[1]) - f.y * X[nt][3];
         }
-        float2 u = one;
-        if (kHalf) {
-            u = scales(X[0], X[1]);
-            tell(talk.x_unit[mine], inverse(u));
-        }
         uint4 own_hi, own_lo;
-        terms(X[0], X[1], u, own_hi, own_lo);
+        terms(kWide, X[0], X[1], one, own_hi, own_lo);
         talk.x[mine][0][lane] = own_hi, talk.x[mine][1][lane] = own_lo;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt)
@@ -418,36 +416,30 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             for (int k = 0; k < KQ; ++k)
                 ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + 2 * k + lane / 16), kb[kt][k]);
         together();
-        // d = X T^T: two terms each (the product of the small ones left out), from the rows up to the warp's own
+        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range, from the rows up to the
+        // warp's own
         float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
-        float2 unit = one;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             if (kt > (int)mine) break;
-            if (kHalf) {
-                const float2 next = talk.x_unit[kt][g];
-                if (kt) change(d, unit, next), change(dl, unit, next), change(dt, unit, next);
-                unit = next;
-            }
             const uint4 p = kt == (int)mine ? own_hi : talk.x[kt][0][lane], q = kt == (int)mine ? own_lo : talk.x[kt][1][lane];
-            mma16816(d[0], &p.x, tb[0][kt][0], tb[0][kt][1], T());
-            mma16816(d[1], &p.x, tb[0][kt][2], tb[0][kt][3], T());
-            mma16816(dl[0], &q.x, tb[0][kt][0], tb[0][kt][1], T());
-            mma16816(dl[1], &q.x, tb[0][kt][2], tb[0][kt][3], T());
-            mma16816(dt[0], &p.x, tb[1][kt][0], tb[1][kt][1], T());
-            mma16816(dt[1], &p.x, tb[1][kt][2], tb[1][kt][3], T());
+            mma16816(d[0], &p.x, tb[0][kt][0], tb[0][kt][1], kWide);
+            mma16816(d[1], &p.x, tb[0][kt][2], tb[0][kt][3], kWide);
+            mma16816(dl[0], &q.x, tb[0][kt][0], tb[0][kt][1], kWide);
+            mma16816(dl[1], &q.x, tb[0][kt][2], tb[0][kt][3], kWide);
+            mma16816(dt[0], &p.x, tb[1][kt][0], tb[1][kt][1], kWide);
+            mma16816(dt[1], &p.x, tb[1][kt][2], tb[1][kt][3], kWide);
         }
-        const float f0 = kHalf ? st.w.t_unit * unit.x : 1.f, f1 = kHalf ? st.w.t_unit * unit.y : 1.f;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[nt][e] = (d[nt][e] + (dl[nt][e] + dt[nt][e])) * (e & 2 ? f1 : f0);
-        u = one;
+            for (int e = 0; e < 4; ++e) d[nt][e] += dl[nt][e] + dt[nt][e];
+        float2 u = one;
         if (kHalf) {
             u = scales(d[0], d[1]);
             tell(talk.d_unit[mine], make_float2(st.w.p_unit * flipped(u.x), st.w.p_unit * flipped(u.y)));
         }
-        terms(d[0], d[1], u, own_hi, own_lo);
+        terms(T(), d[0], d[1], u, own_hi, own_lo);
         talk.d[mine][0][lane] = own_hi, talk.d[mine][1][lane] = own_lo;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
@@ -459,7 +451,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             u = scales(d[0], d[1]);
             tell(talk.dw_unit[mine], inverse(u));
         }
-        terms(d[0], d[1], u, own_hi, own_lo);
+        terms(T(), d[0], d[1], u, own_hi, own_lo);
         talk.dw[mine][0][lane] = own_hi, talk.dw[mine][1][lane] = own_lo;
         // S <- e^G S + (w d) K for the warp's keys
         const float all = st.w.all;
@@ -469,7 +461,7 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
             for (int e = 0; e < 4; ++e) S[nt][e] *= all;
         arrive(&m.ready[slice]);
         together();
-        unit = one;
+        float2 unit = one;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             if (kHalf) {
@@ -579,11 +571,12 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         return range_scale(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
     };
-    auto terms = [](const float(*x)[4], float u0, float u1, uint32_t *hi, uint32_t *lo) {  // of the 16 x 16 in accumulators x[0] and x[1]
-        split2<T>(x[0][0] * u0, x[0][1] * u0, hi[0], lo[0]);
-        split2<T>(x[0][2] * u1, x[0][3] * u1, hi[1], lo[1]);
-        split2<T>(x[1][0] * u0, x[1][1] * u0, hi[2], lo[2]);
-        split2<T>(x[1][2] * u1, x[1][3] * u1, hi[3], lo[3]);
+    auto terms = [](auto type, const float(*x)[4], float u0, float u1, uint32_t *hi, uint32_t *lo) {  // of the 16 x 16 in accumulators x[0] and x[1]
+        using Term = decltype(type);
+        split2<Term>(x[0][0] * u0, x[0][1] * u0, hi[0], lo[0]);
+        split2<Term>(x[0][2] * u1, x[0][3] * u1, hi[1], lo[1]);
+        split2<Term>(x[1][0] * u0, x[1][1] * u0, hi[2], lo[2]);
+        split2<Term>(x[1][2] * u1, x[1][3] * u1, hi[3], lo[3]);
     };
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -664,7 +657,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
                 ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
-            terms(S + 2 * kt, u0, u1, hi, lo);
+            terms(T(), S + 2 * kt, u0, u1, hi, lo);
 #pragma unroll
             for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
 #pragma unroll
@@ -689,8 +682,8 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
             X[nt][2] = to_f32(vb[0]) - f.x * (kHalf ? X[nt][2] * si1 : X[nt][2]);
             X[nt][3] = to_f32(vb[1]) - f.y * (kHalf ? X[nt][3] * si1 : X[nt][3]);
         }
-        if (kHalf) u0 = scale_of(X, CT, 0), u1 = scale_of(X, CT, 1);
-        // d = X T^T: two terms each (the product of the small ones left out); T's columns beyond a row's own are zero
+        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range; T's columns beyond a row's
+        // own are zero
         float d[CT][4] = {};
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
@@ -701,24 +694,21 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
                 ldmatrix_x4(smem_u32(st.w.tile[0]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
-            terms(X + 2 * kt, u0, u1, hi, lo);
+            terms(kWide, X + 2 * kt, 1.f, 1.f, hi, lo);
 #pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], T());
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], kWide);
 #pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], T());
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], kWide);
 #pragma unroll
             for (int nt = 2 * kt; nt < CT; nt += 2) {
                 uint32_t x[4];
                 ldmatrix_x4(smem_u32(st.w.tile[1]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
-                mma16816(d[nt], hi, x[0], x[1], T());
-                mma16816(d[nt + 1], hi, x[2], x[3], T());
+                mma16816(d[nt], hi, x[0], x[1], kWide);
+                mma16816(d[nt + 1], hi, x[2], x[3], kWide);
             }
         }
         float di0 = 1.f, di1 = 1.f;
         if (kHalf) {
-            const float i0 = st.w.t_unit * flipped(u0), i1 = st.w.t_unit * flipped(u1);
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) d[nt][0] *= i0, d[nt][1] *= i0, d[nt][2] *= i1, d[nt][3] *= i1;
             u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
             di0 = st.w.p_unit * flipped(u0), di1 = st.w.p_unit * flipped(u1);
         }
@@ -738,7 +728,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
                 ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
-            terms(d + 2 * kt, u0, u1, hi, lo);
+            terms(T(), d + 2 * kt, u0, u1, hi, lo);
 #pragma unroll
             for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], T());
 #pragma unroll
@@ -757,7 +747,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             uint32_t hi[4], lo[4];
-            terms(d + 2 * kt, u0, u1, hi, lo);
+            terms(T(), d + 2 * kt, u0, u1, hi, lo);
 #pragma unroll
             for (int n0 = 0; n0 < NT; n0 += 8) {
                 uint32_t b[8][2];

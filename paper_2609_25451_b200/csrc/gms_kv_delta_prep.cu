@@ -89,7 +89,7 @@ struct PrepSmem {
     };
     float2 sum[kPrepHeads][kChunkRows];  // G / ln 2, as the sum of two
     float b[kPrepHeads][kChunkRows], rk[kChunkRows], rq[kChunkRows];
-    float top[2][4];
+    float lk[kChunkRows], lq[kChunkRows], p_scale[kPrepHeads];  // f16: lengths; what P is multiplied with
 };
 
 // Byte offset of a block of 16 x 16, and of 16-byte piece c (0, 1) of row r in it.
@@ -157,7 +157,7 @@ __device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const floa
 // a chunk and head and by its warps' waits for one another, which five CTAs an SM fill up: 8,192 rows of 32 heads of 128, bf16, 59 us
 // (T, P and factors a CTA in 32 bits 172; as blocks of two-term factors 62.5, four CTAs an SM).
 template <class T, int D>
-__global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ? 4 : 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
+__global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
     extern __shared__ __align__(16) uint8_t raw[];
     PrepSmem<D> &m = *reinterpret_cast<PrepSmem<D> *>(raw);
@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
                 finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
                 m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
                 m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
+                if (kHalf) m.lk[r] = sqrtf(k2) * m.rk[r], m.lq[r] = sqrtf(q2) * m.rq[r];
             }
     }
     for (uint32_t j = 0; j < a.group; ++j) {
@@ -252,6 +253,19 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
                     if (lane >= (uint32_t)o) inc += y;
                 }
                 const double last = __shfl_sync(0xffffffffu, inc, 31);
+                if (kHalf) {  // no element of P is above scale |q| |k| e^(sum of the gates above 0)
+                    float k = fmaxf(m.lk[2 * lane], m.lk[2 * lane + 1]), q = fmaxf(m.lq[2 * lane], m.lq[2 * lane + 1]);
+                    float up = fmaxf(raw_g[0], 0.f) + fmaxf(raw_g[1], 0.f);
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) {
+                        k = fmaxf(k, __shfl_xor_sync(0xffffffffu, k, o));
+                        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, o));
+                        up += __shfl_xor_sync(0xffffffffu, up, o);
+                    }
+                    const float most = fabsf(a.scale) * k * q * expf(up), by = range_scale(most);
+                    if (!(most < 1e12f)) finite = __int_as_float(0x7fffffff);  // row by row
+                    if (lane == 0) m.p_scale[warp] = by, w.p_unit = flipped(by);
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = 2 * (int)lane + e;
@@ -272,23 +286,17 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
             __syncthreads();
         }
         // A and P: rows i0 and i0 + 8, columns 8 nt + t2 + {0, 1}
-        float pv[kHalf ? C / 8 : 1][4], top = 0.f;
-        auto put_p = [&](int nt, const float *p, float scale) {
-            const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
-            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(p[0] * scale, p[1] * scale, T());
-            *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(p[2] * scale, p[3] * scale, T());
-        };
+        const float ps = kHalf ? m.p_scale[jj] : 1.f;
         {
             const float2 sum[2] = {m.sum[jj][i0], m.sum[jj][i0 + 8]};
             const float bk[2] = {m.b[jj][i0] * m.rk[i0], m.b[jj][i0 + 8] * m.rk[i0 + 8]};
-            const float sq[2] = {(int)i0 < n ? a.scale * m.rq[i0] : 0.f, (int)i0 + 8 < n ? a.scale * m.rq[i0 + 8] : 0.f};
+            const float sq[2] = {(int)i0 < n ? a.scale * m.rq[i0] * ps : 0.f, (int)i0 + 8 < n ? a.scale * m.rq[i0 + 8] * ps : 0.f};
 #pragma unroll
             for (int nt = 0; nt < C / 8; ++nt) {
                 if (nt > 2 * (int)warp + 1) break;
-                float *pn = pv[kHalf ? nt : 0];
                 const float4 sc = *reinterpret_cast<const float4 *>(&m.sum[jj][8 * nt + t2]);  // of two columns
                 const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[8 * nt + t2]);
-                float av[4];
+                float av[4], pn[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float decay = ptx::ex2((sum[e / 2].x - (e & 1 ? sc.z : sc.x)) + (sum[e / 2].y - (e & 1 ? sc.w : sc.y)));
@@ -311,24 +319,10 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
                     put_pair(m.a, block + piece_in(g + 8, nt & 1) + 2 * t2, av[2], av[3]);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    finite = fmaf(av[e], 0.f, fmaf(pn[e], 0.f, finite));
-                    if (kHalf) top = fmaxf(top, fabsf(pn[e]));
-                }
-                if (!kHalf) put_p(nt, pn, 1.f);
-            }
-        }
-        if (kHalf) {
-#pragma unroll
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            if (lane == 0) m.top[0][warp] = top;
-            __syncthreads();
-            const float ps = range_scale(fmaxf(fmaxf(m.top[0][0], m.top[0][1]), fmaxf(m.top[0][2], m.top[0][3])));
-            if (tid == 0) work->p_unit = flipped(ps);
-#pragma unroll
-            for (int nt = 0; nt < C / 8; ++nt) {
-                if (nt > 2 * (int)warp + 1) break;
-                put_p(nt, pv[kHalf ? nt : 0], ps);
+                for (int e = 0; e < 4; ++e) finite = fmaf(av[e], 0.f, fmaf(pn[e], 0.f, finite));
+                const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
+                *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(pn[0], pn[1], T());
+                *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(pn[2], pn[3], T());
             }
         }
         __syncwarp();
@@ -384,37 +378,10 @@ __global__ void __launch_bounds__(kPrepThreads, std::is_same<T, __half>::value ?
         }
         __syncthreads();
         constexpr uint32_t kPieces = sizeof(m.p) / 16;
-        if (kHalf) {  // to f16, all numbers scaled alike
-            float most = 0.f;
-            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
-                const uint4 hi = reinterpret_cast<const uint4 *>(m.t.hi)[u];
-                const __nv_bfloat16 *e = reinterpret_cast<const __nv_bfloat16 *>(&hi);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(to_f32(e[i])));
-            }
-#pragma unroll
-            for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            if (lane == 0) m.top[1][warp] = most;
-            __syncthreads();
-            const float ts = range_scale(fmaxf(fmaxf(m.top[1][0], m.top[1][1]), fmaxf(m.top[1][2], m.top[1][3])));
-            if (tid == 0) work->t_unit = flipped(ts);
-            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
-                const uint4 x = reinterpret_cast<const uint4 *>(m.t.hi)[u], y = reinterpret_cast<const uint4 *>(m.t.lo)[u];
-                const __nv_bfloat16 *p = reinterpret_cast<const __nv_bfloat16 *>(&x), *q = reinterpret_cast<const __nv_bfloat16 *>(&y);
-                uint32_t hi[4], lo[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    split2<T>((to_f32(p[2 * i]) + to_f32(q[2 * i])) * ts, (to_f32(p[2 * i + 1]) + to_f32(q[2 * i + 1])) * ts, hi[i], lo[i]);
-                reinterpret_cast<uint4 *>(work->tile[0])[u] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                reinterpret_cast<uint4 *>(work->tile[1])[u] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
-            }
-        } else {
-            for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
-                reinterpret_cast<uint4 *>(work->tile[0])[u] = reinterpret_cast<const uint4 *>(m.t.hi)[u];
-                reinterpret_cast<uint4 *>(work->tile[1])[u] = reinterpret_cast<const uint4 *>(m.t.lo)[u];
-                reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
-            }
+        for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
+            reinterpret_cast<uint4 *>(work->tile[0])[u] = reinterpret_cast<const uint4 *>(m.t.hi)[u];
+            reinterpret_cast<uint4 *>(work->tile[1])[u] = reinterpret_cast<const uint4 *>(m.t.lo)[u];
+            reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
         }
         const bool any = __syncthreads_or(finite != 0.f);
         if (tid == 0) work->by_row = any;

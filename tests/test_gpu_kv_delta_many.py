@@ -126,3 +126,12 @@ def test_calls_one_behind_the_other(lens):
             want.sub_(b.out_full)
     torch.cuda.synchronize()
     assert all(not x.any() for x in seen) and torch.equal(a.raw, b.raw)
+
+
+# (with row 40's own strength, f16 and up = 30 have no finite answer: the row's d k^T, of about 1, times e^30 = 10^13 is read at row 41)
+@pytest.mark.parametrize("dtype,up,strength", [(BF16, 3.0, 1), (BF16, 30.0, 1), (F16, 3.0, 1), (BF16, 30.0, 0), (F16, 30.0, 0)])
+def test_a_gate_far_above_zero(dtype, up, strength):
+    d = Delta(16, lens=(130,), H=4, K=2, dtype=dtype)
+    d.g[40], d.g[41] = -up, up  # what is lost comes back
+    d.beta[40] *= strength
+    d.check()
