@@ -128,12 +128,14 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
     const uint32_t tid = threadIdx.x, warp = tid / 32;
     const uint32_t slice = blockIdx.x % (D / W), h = blockIdx.x / (D / W) % a.n_heads, s = blockIdx.x / (D / W) / a.n_heads;
     // Beside the chunk kernels, which have waited for what was before them and have nothing to do with these sequences: what they leave
-    // of the GPU is filled up.  The last CTA waits for them, so that nothing after this kernel starts before they have ended.
+    // of the GPU is filled up.  The last CTA ends by waiting for them, so that nothing after this kernel starts before they have ended.
     if (!a.chunks) ptx::grid_wait();
     ptx::grid_launch_dependents();
-    if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
+    auto leave = [&] {
+        if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
+    };
     const int first = delta_begin(a, s), rows = delta_rows(a, s);
-    if (delta_in_chunks(a, rows)) return;
+    if (delta_in_chunks(a, rows)) return leave();
     const bool fresh = a.past_lens && a.past_lens[s] <= 0;
     const float *from = fresh ? nullptr : delta_state<D>(a, a.src_table, a.src_stride, s, h);
     float *to = delta_state<D>(a, a.dst_table, a.dst_stride, s, h);
@@ -153,9 +155,10 @@ __global__ void __launch_bounds__(kRowThreads) kv_delta_rows_kernel(const __grid
         __syncthreads();
         take_rows<T, D, W>(a, m, n, (uint64_t)(first + r0), h, slice, S);
     }
-    if (!to) return;
+    if (!to) return leave();
 #pragma unroll
     for (int i = 0; i < N; ++i) *reinterpret_cast<float4 *>(to + at + i * D) = make_float4(S[i][0].x, S[i][0].y, S[i][1].x, S[i][1].y);
+    leave();
 }
 
 template <int D>
@@ -190,7 +193,6 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
     __syncthreads();
     if (!a.chunks) ptx::grid_wait();  // (as above)
     ptx::grid_launch_dependents();
-    if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
     // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
     bool late = false;
     auto wait = [&](uint64_t *bar, uint32_t use) {
@@ -291,6 +293,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamShape<D>::kCtas) kv_delt
         asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory");  // (the rows have been read, too)
         if ((tid & 31u) == 0) ptx::mbar_arrive(ptx::smem_u32(&m.done[b]));
     }
+    if (a.chunks && blockIdx.x == gridDim.x - 1 && tid == 0) ptx::grid_wait();
 }
 
 template <class T, int D>
