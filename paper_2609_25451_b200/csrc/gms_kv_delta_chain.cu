@@ -518,7 +518,12 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kParts = D / (16 * W);
-    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, rank = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
+    // Where some SMs have a second CTA from the start, they are those of the first CTAs, which therefore take the shorter sequences of
+    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 176 us without, 168 us).
+    constexpr uint32_t kSms = 148;
+    const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
+    const uint32_t item = turned ? kSms - 1 - blockIdx.x : blockIdx.x;
+    const uint32_t part = item % kParts, h = item / kParts % a.n_heads, rank = item / kParts / a.n_heads, kh = h / a.group;
     const uint32_t col0 = part * W * 16;  // of the CTA
     ptx::grid_launch_dependents();
     ptx::grid_wait();
