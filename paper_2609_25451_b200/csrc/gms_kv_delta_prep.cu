@@ -71,9 +71,13 @@ __device__ void put_order(const DeltaArgs &a, uint32_t *count)
     }
 }
 
-// A lower triangle of 64 x 64, in blocks of 16 x 16, as two bf16 terms (2^-17 relative together).
-struct Terms64 {
-    uint8_t hi[sizeof(ChunkWork::tile[0])], lo[sizeof(ChunkWork::tile[0])];
+// Blocks of 16 x 16, as two bf16 terms (2^-17 relative together).
+template <int N>
+struct Terms {
+    uint8_t hi[N * 512], lo[N * 512];
+};
+struct View {
+    uint8_t *hi, *lo;
 };
 template <int D>
 struct PrepSmem {
@@ -82,25 +86,28 @@ struct PrepSmem {
             uint8_t k[kChunkRows * D * 2], q[kChunkRows * D * 2];
         };
         struct {
-            Terms64 a, inv, t;           // A below its diagonal blocks, the inverse of I + A, the same times diag(beta)
+            Terms<6> a;                  // A below its diagonal blocks
+            Terms<5> inv;                // of I + A: the diagonal blocks' inverses and block (3, 2) of the inverse
+            Terms<10> t;                 // the inverse times diag(beta)
             float diag[4][16][20];       // A's diagonal blocks
             uint8_t p[sizeof(ChunkWork::tile[0])];
         };
     };
-    float2 sum[kPrepHeads][kChunkRows];  // G / ln 2, as the sum of two
+    float sum[kPrepHeads][2][kChunkRows];  // G / ln 2, as the sum of two
     float b[kPrepHeads][kChunkRows], rk[kChunkRows], rq[kChunkRows];
     float lk[kChunkRows], lq[kChunkRows], p_scale[kPrepHeads];  // f16: lengths; what P is multiplied with
 };
 
-// Byte offset of a block of 16 x 16, and of 16-byte piece c (0, 1) of row r in it.
+// Byte offset of block (i, j) in a triangle, in one without its diagonal, and of 16-byte piece c (0, 1) of row r in a block.
 __device__ __forceinline__ uint32_t block_at(uint32_t i, uint32_t j) { return (i * (i + 1) / 2 + j) * 512; }
+__device__ __forceinline__ uint32_t below_at(uint32_t i, uint32_t j) { return (i * (i - 1) / 2 + j) * 512; }
 __device__ __forceinline__ uint32_t piece_in(uint32_t r, uint32_t c) { return (r * 2 + ((c ^ (r / 4)) & 1u)) * 16; }
 
 // A block as a first factor; and c += x y with y a block: two terms each, the product of the small ones left out.
 struct First {
     uint32_t hi[4], lo[4];
 };
-__device__ __forceinline__ First first_of(const Terms64 &x, uint32_t block)
+__device__ __forceinline__ First first_of(View x, uint32_t block)
 {
     const uint32_t lane = threadIdx.x & 31u, at = block + piece_in(lane & 15u, lane / 16);
     First f;
@@ -115,7 +122,7 @@ __device__ __forceinline__ First first_of(const float (*x)[4])  // minus the acc
     for (int e = 0; e < 4; ++e) split2<__nv_bfloat16>(-x[e / 2][2 * (e & 1)], -x[e / 2][2 * (e & 1) + 1], f.hi[e], f.lo[e]);
     return f;
 }
-__device__ __forceinline__ void add_product(float (*c)[4], const First &x, const Terms64 &y, uint32_t block)
+__device__ __forceinline__ void add_product(float (*c)[4], const First &x, View y, uint32_t block)
 {
     const uint32_t lane = threadIdx.x & 31u, at = block + piece_in(lane & 15u, lane / 16);
     uint32_t hi[4], lo[4];
@@ -130,14 +137,14 @@ __device__ __forceinline__ void add_product(float (*c)[4], const First &x, const
     mma16816(c[1], x.hi, lo[2], lo[3], type);
 }
 // Two neighbours of a row as two terms; a 16 x 16 of accumulators.
-__device__ __forceinline__ void put_pair(Terms64 &t, uint32_t at, float x, float y)
+__device__ __forceinline__ void put_pair(View t, uint32_t at, float x, float y)
 {
     uint32_t hi, lo;
     split2<__nv_bfloat16>(x, y, hi, lo);
     *reinterpret_cast<uint32_t *>(t.hi + at) = hi;
     *reinterpret_cast<uint32_t *>(t.lo + at) = lo;
 }
-__device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const float (*x)[4], float &finite)
+__device__ __forceinline__ void put_block(View t, uint32_t block, const float (*x)[4], float &finite)
 {
     const uint32_t lane = threadIdx.x & 31u, g = lane / 4, q = (lane & 3u) * 4;
 #pragma unroll
@@ -149,13 +156,14 @@ __device__ __forceinline__ void put_block(Terms64 &t, uint32_t block, const floa
     }
 }
 
-// One CTA per chunk and key head.  k_i.k_j and q_i.k_j on mma.sync (a warp has 16 rows i; the diagonals are the rows' lengths), then
-// for each value head of the key head the decays, the inverse and what goes to the workspace.  The inverse of I + A: its diagonal
-// blocks of 16 x 16 a warp each (a lane has a column and goes down it: x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
+// One CTA per chunk and key head.  k_i.k_j and q_i.k_j on mma.sync (the diagonals are the rows' lengths), the ten blocks of the
+// triangle shared out as three, two, three and two, then for each value head of the key head the decays, the inverse and what goes to
+// the workspace.  The inverse of I + A: its diagonal blocks of 16 x 16 a warp each (a lane has a column and goes down it:
+// x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
 //   (X 0; Y Z)^-1 = (X^-1 0; -Z^-1 Y X^-1 Z^-1)
-// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by the issue of its 7,100 instructions
-// a chunk and head and by its warps' waits for one another, which five CTAs an SM fill up: 8,192 rows of 32 heads of 128, bf16, 59 us
-// (T, P and factors a CTA in 32 bits 172; as blocks of two-term factors 62.5, four CTAs an SM).
+// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by the issue of its 6,500 instructions a chunk and
+// head and by its warps' waits for one another, which five CTAs an SM fill up (six, with fewer registers: 3 us more): 8,192 rows of 32
+// heads of 128, bf16, 52 us (T, P and factors in 32 bits 172; as blocks of two-term factors 62.5, with a warp for each 16 rows 59.5).
 template <class T, int D>
 __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -188,43 +196,55 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    // products of rows 16 warp .. with rows 0 .. of the keys, and of the queries with themselves
-    const uint32_t i0 = 16 * warp + g, b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;
-    float kk[C / 8][4] = {}, qk[C / 8][4] = {}, qq[2][4] = {};
-#pragma unroll
-    for (int kt = 0; kt < D / 16; ++kt) {
-        uint32_t ka[4], qa[4], b[4];
-        const uint32_t at = piece<P>(16 * warp + (lane & 15u), 2 * kt + lane / 16);
-        ldmatrix_x4(smem_u32(m.k) + at, ka);
-        ldmatrix_x4(smem_u32(m.q) + at, qa);
-        ldmatrix_x4(smem_u32(m.q) + piece<P>(16 * warp + b_row, 2 * kt + b_piece), b);
-        mma16816(qq[0], qa, b[0], b[1], T());
-        mma16816(qq[1], qa, b[2], b[3], T());
-#pragma unroll
-        for (int nt = 0; nt < C / 8; nt += 2) {
-            if (nt > 2 * (int)warp) break;
-            ldmatrix_x4(smem_u32(m.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), b);
-            mma16816(kk[nt], ka, b[0], b[1], T());
-            mma16816(kk[nt + 1], ka, b[2], b[3], T());
-            mma16816(qk[nt], qa, b[0], b[1], T());
-            mma16816(qk[nt + 1], qa, b[2], b[3], T());
-        }
-    }
     float finite = 0.f;  // NaN once something was not finite
+    // products of keys and queries with keys, block by block: a warp has its diagonal block and one or two below (warp 0, two of the
+    // last row of blocks), and of its queries with themselves
+    const bool far = warp == 0;
+    const int blocks = warp & 1u ? 2 : 3;
+    auto row_of = [&](int b) { return b && far ? 3u : warp; };
+    auto col_of = [&](int b) { return b == 0 ? warp : b == 2 ? 1u : warp == 3 ? 2u : 0u; };
+    const uint32_t b_row = (lane & 7u) + (lane & 16u) / 2, b_piece = lane / 8 & 1u;
+    float kk[3][2][4] = {}, qk[3][2][4] = {};
+    {
+        float qq[2][4] = {};
 #pragma unroll
-    for (int nt = 0; nt < C / 8; ++nt) {
-        if (nt / 2 != (int)warp) continue;
+        for (int kt = 0; kt < D / 16; ++kt) {
+            uint32_t ka[4], qa[4], x[4];
+            const uint32_t at = piece<P>(16 * warp + (lane & 15u), 2 * kt + lane / 16);
+            ldmatrix_x4(smem_u32(m.k) + at, ka);
+            ldmatrix_x4(smem_u32(m.q) + at, qa);
+            ldmatrix_x4(smem_u32(m.q) + piece<P>(16 * warp + b_row, 2 * kt + b_piece), x);
+            mma16816(qq[0], qa, x[0], x[1], T());
+            mma16816(qq[1], qa, x[2], x[3], T());
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (8 * (nt & 1) + t2 + (e & 1) == g + (e & 2) * 4) {  // on the diagonal
-                const uint32_t r = i0 + (e & 2) * 4;
-                const float k2 = kk[nt][e], q2 = qq[nt & 1][e];
-                finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
-                m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
-                m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
-                if (kHalf) m.lk[r] = sqrtf(k2) * m.rk[r], m.lq[r] = sqrtf(q2) * m.rq[r];
+            for (int b = 0; b < 3; ++b) {
+                if (b >= blocks) break;
+                if (b == 1 && far) {
+                    const uint32_t last = piece<P>(48 + (lane & 15u), 2 * kt + lane / 16);
+                    ldmatrix_x4(smem_u32(m.k) + last, ka);
+                    ldmatrix_x4(smem_u32(m.q) + last, qa);
+                }
+                ldmatrix_x4(smem_u32(m.k) + piece<P>(16 * col_of(b) + b_row, 2 * kt + b_piece), x);
+                mma16816(kk[b][0], ka, x[0], x[1], T());
+                mma16816(kk[b][1], ka, x[2], x[3], T());
+                mma16816(qk[b][0], qa, x[0], x[1], T());
+                mma16816(qk[b][1], qa, x[2], x[3], T());
             }
+        }
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (8 * nt + t2 + (e & 1) == g + (e & 2) * 4) {  // on the diagonal
+                    const uint32_t r = 16 * warp + g + (e & 2) * 4;
+                    const float k2 = kk[0][nt][e], q2 = qq[nt][e];
+                    finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
+                    m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
+                    m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
+                    if (kHalf) m.lk[r] = sqrtf(k2) * m.rk[r], m.lq[r] = sqrtf(q2) * m.rq[r];
+                }
     }
+    const View va = {m.a.hi, m.a.lo}, vi = {m.inv.hi, m.inv.lo}, vt = {m.t.hi, m.t.lo};
     for (uint32_t j = 0; j < a.group; ++j) {
         ChunkWork *work = reinterpret_cast<ChunkWork *>(a.chunks + ((uint64_t)id * a.n_heads + kh * a.group + j) * sizeof(ChunkWork));
         const uint32_t jj = j % kPrepHeads;
@@ -271,7 +291,7 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     const int r = 2 * (int)lane + e;
                     const double sum = inc - sum_g + x[e];
                     const bool in = r < n;
-                    m.sum[warp][r] = make_float2((float)sum, (float)(sum - (double)(float)sum));
+                    m.sum[warp][0][r] = (float)sum, m.sum[warp][1][r] = (float)(sum - (double)(float)sum);
                     m.b[warp][r] = beta[e];
                     const float gate = exp2f((float)sum), f = in ? m.rk[r] * gate : 0.f, hh = in ? a.scale * m.rq[r] * gate : 0.f,
                                 ww = in ? m.rk[r] * exp2f((float)(last - sum)) : 0.f;
@@ -285,44 +305,47 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
             }
             __syncthreads();
         }
-        // A and P: rows i0 and i0 + 8, columns 8 nt + t2 + {0, 1}
+        // A and P: rows r0 and r0 + 8, columns c0 + {0, 1} and c0 + 8 + {0, 1} of a block (something in A that is not finite comes
+        // through to T)
         const float ps = kHalf ? m.p_scale[jj] : 1.f;
-        {
-            const float2 sum[2] = {m.sum[jj][i0], m.sum[jj][i0 + 8]};
-            const float bk[2] = {m.b[jj][i0] * m.rk[i0], m.b[jj][i0 + 8] * m.rk[i0 + 8]};
-            const float sq[2] = {(int)i0 < n ? a.scale * m.rq[i0] * ps : 0.f, (int)i0 + 8 < n ? a.scale * m.rq[i0 + 8] * ps : 0.f};
+        const float2 minus = make_float2(-1.f, -1.f);
+        auto twice = [](float x) { return make_float2(x, x); };
 #pragma unroll
-            for (int nt = 0; nt < C / 8; ++nt) {
-                if (nt > 2 * (int)warp + 1) break;
-                const float4 sc = *reinterpret_cast<const float4 *>(&m.sum[jj][8 * nt + t2]);  // of two columns
-                const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[8 * nt + t2]);
-                float av[4], pn[4];
+        for (int b = 0; b < 3; ++b) {
+            if (b >= blocks) break;
+            const uint32_t bi = row_of(b), bj = col_of(b), r0 = 16 * bi + g, c0 = 16 * bj + t2;
+            float2 sh[2], sl[2], bk[2], sq[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float decay = ptx::ex2((sum[e / 2].x - (e & 1 ? sc.z : sc.x)) + (sum[e / 2].y - (e & 1 ? sc.w : sc.y)));
-                    const float z = (e & 1 ? rc.y : rc.x) * decay;
-                    av[e] = bk[e / 2] * (kk[nt][e] * z);
-                    pn[e] = sq[e / 2] * (qk[nt][e] * z);
-                }
-                if (nt / 2 == (int)warp) {
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t r = r0 + 8 * e;
+                sh[e] = twice(m.sum[jj][0][r]), sl[e] = twice(m.sum[jj][1][r]);
+                bk[e] = twice(m.b[jj][r] * m.rk[r]), sq[e] = twice((int)r < n ? a.scale * m.rq[r] * ps : 0.f);
+            }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t r = g + (e & 2) * 4, c = 8 * (nt & 1) + t2 + (e & 1);
-                        if (c >= r) av[e] = 0.f;
-                        if (c > r) pn[e] = 0.f;
+            for (int nt = 0; nt < 2; ++nt) {
+                const uint32_t c = c0 + 8 * nt;
+                const float2 ch = *reinterpret_cast<const float2 *>(&m.sum[jj][0][c]), cl = *reinterpret_cast<const float2 *>(&m.sum[jj][1][c]);
+                const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[c]);
+                const uint32_t at = block_at(bi, bj) + 2 * t2;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float2 d = ptx::add2(ptx::fma2(ch, minus, sh[e]), ptx::fma2(cl, minus, sl[e]));
+                    const float2 z = ptx::mul2(rc, make_float2(ptx::ex2(d.x), ptx::ex2(d.y)));
+                    float2 av = ptx::mul2(bk[e], ptx::mul2(make_float2(kk[b][nt][2 * e], kk[b][nt][2 * e + 1]), z));
+                    float2 pn = ptx::mul2(sq[e], ptx::mul2(make_float2(qk[b][nt][2 * e], qk[b][nt][2 * e + 1]), z));
+                    if (b == 0) {
+                        const uint32_t r = g + 8 * e, x = 8 * nt + t2;
+                        if (x >= r) av.x = 0.f;
+                        if (x + 1 >= r) av.y = 0.f;
+                        if (x > r) pn.x = 0.f;
+                        if (x + 1 > r) pn.y = 0.f;
+                        *reinterpret_cast<float2 *>(&m.diag[warp][r][x]) = av;
+                    } else {
+                        put_pair(va, below_at(bi, bj) + piece_in(g + 8 * e, nt) + 2 * t2, av.x, av.y);
                     }
-                    *reinterpret_cast<float2 *>(&m.diag[warp][g][8 * (nt & 1) + t2]) = make_float2(av[0], av[1]);
-                    *reinterpret_cast<float2 *>(&m.diag[warp][g + 8][8 * (nt & 1) + t2]) = make_float2(av[2], av[3]);
-                } else {
-                    const uint32_t block = block_at(warp, nt / 2);
-                    put_pair(m.a, block + piece_in(g, nt & 1) + 2 * t2, av[0], av[1]);
-                    put_pair(m.a, block + piece_in(g + 8, nt & 1) + 2 * t2, av[2], av[3]);
+                    finite = fmaf(pn.x, 0.f, fmaf(pn.y, 0.f, finite));
+                    *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8 * e, nt)) = pack2(pn.x, pn.y, T());
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) finite = fmaf(av[e], 0.f, fmaf(pn[e], 0.f, finite));
-                const uint32_t at = block_at(warp, nt / 2) + 2 * t2;
-                *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g, nt & 1)) = pack2(pn[0], pn[1], T());
-                *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8, nt & 1)) = pack2(pn[2], pn[3], T());
             }
         }
         __syncwarp();
@@ -342,25 +365,25 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                 }
                 x[i] = sum;
             }
-            const uint32_t block = block_at(warp, warp);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {  // neighbouring lanes are neighbours of a row: each stores one row's pair of them
                 const float other = __shfl_xor_sync(0xffffu, lane & 1u ? x[i] : x[i + 1], 1), ob = __shfl_xor_sync(0xffffu, b, 1);
                 const float mine = lane & 1u ? x[i + 1] : x[i];
                 const float l = lane & 1u ? other : mine, r = lane & 1u ? mine : other;
-                const uint32_t at = block + piece_in(i + (lane & 1u), lane / 8) + (lane & 6u) * 2;
-                put_pair(m.inv, at, l, r);
-                put_pair(m.t, at, l * (lane & 1u ? ob : b), r * (lane & 1u ? b : ob));
+                const uint32_t at = piece_in(i + (lane & 1u), lane / 8) + (lane & 6u) * 2;
+                put_pair(vi, warp * 512 + at, l, r);
+                put_pair(vt, block_at(warp, warp) + at, l * (lane & 1u ? ob : b), r * (lane & 1u ? b : ob));
                 finite = fmaf(x[i], 0.f, fmaf(x[i + 1], 0.f, finite));
             }
         }
         __syncthreads();
+        constexpr uint32_t kInv32 = 4 * 512;  // where block (3, 2) of the inverse is
         if (warp != 1) {  // blocks (1, 0) and (3, 2) of T; (3, 2) of the inverse, too
             const uint32_t i = warp == 0 ? 0 : 2;
             float mid[2][4] = {}, o[2][4] = {};
-            add_product(mid, first_of(m.inv, block_at(i + 1, i + 1)), m.a, block_at(i + 1, i));
-            add_product(o, first_of(mid), warp == 3 ? m.inv : m.t, block_at(i, i));
-            put_block(warp == 3 ? m.inv : m.t, block_at(i + 1, i), o, finite);
+            add_product(mid, first_of(vi, (i + 1) * 512), va, below_at(i + 1, i));
+            add_product(o, first_of(mid), warp == 3 ? vi : vt, warp == 3 ? i * 512 : block_at(i, i));
+            put_block(warp == 3 ? vi : vt, warp == 3 ? kInv32 : block_at(i + 1, i), o, finite);
         }
         __syncthreads();
         {  // blocks (2 .. 3, 0 .. 1) of T, one a warp
@@ -370,11 +393,11 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
             for (uint32_t k = 0; k < 2; ++k) {
                 if (k < c) continue;
                 float mid[2][4] = {};
-                add_product(mid, first_of(m.inv, block_at(i, 2)), m.a, block_at(2, k));
-                if (i == 3) add_product(mid, first_of(m.inv, block_at(3, 3)), m.a, block_at(3, k));
-                add_product(o, first_of(mid), m.t, block_at(k, c));
+                add_product(mid, first_of(vi, i == 2 ? 2 * 512 : kInv32), va, below_at(2, k));
+                if (i == 3) add_product(mid, first_of(vi, 3 * 512), va, below_at(3, k));
+                add_product(o, first_of(mid), vt, block_at(k, c));
             }
-            put_block(m.t, block_at(i, c), o, finite);
+            put_block(vt, block_at(i, c), o, finite);
         }
         __syncthreads();
         constexpr uint32_t kPieces = sizeof(m.p) / 16;
