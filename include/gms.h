@@ -614,7 +614,7 @@ int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gm
  * (unit_qk: q and k are first divided by sqrt(sum x^2 + unit_eps)).  S begins as the state in src_table, or as zeros where
  * past_lens[s] is 0, and the state after the last row goes to dst_table (a sequence without rows: as it began).  g NULL counts as
  * zeros, beta NULL as ones.  g is a logarithm, at most 0 in earnest; -infinity clears the state.
- * Sequences of more than 24 rows are done in chunks of 64 on tensor cores: products of the 16-bit inputs with S, d and decays, which
+ * Sequences of more than 20 rows are done in chunks of 64 on tensor cores: products of the 16-bit inputs with S, d and decays, which
  * enter as sums of two 16-bit terms (2^-16 relative) wherever they go on into a state; for `out` the state before the chunk and the
  * weights of its rows enter as one (its error is 1.4 to 1.6 times that of its last rounding).  States and sums are kept in 32 bits.  What a row
  * does not depend on cannot reach it, whatever bits it holds.  (fp16 in chunks: states and differences d within 2^45.)

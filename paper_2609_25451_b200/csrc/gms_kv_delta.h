@@ -24,8 +24,8 @@ struct DeltaArgs {
 };
 
 // Sequences of more rows than kMostByRow are done kChunkRows at a time (us, in chunks / row by row, 32 heads of 128, bf16: 1 sequence of
-// 24 rows 24.5 / 20.5, of 32 24.5 / 24.5; 8 of 24 49 / 43, of 32 49 / 53; 32 of 24 127 / 129).
-constexpr uint32_t kChunkRows = 64, kMostByRow = 24, kNone = 0xffffffffu;
+// 20 rows 20.5 / 20.5, of 24 20.5 / 22.5; 8 of 16 41 / 33, of 20 43 / 39, of 24 43 / 43, of 32 43 / 53; 32 of 20 119 / 115, of 24 119 / 131).
+constexpr uint32_t kChunkRows = 64, kMostByRow = 20, kNone = 0xffffffffu;
 
 // What the first of the two chunk kernels leaves for the second.
 struct alignas(256) ChunkWork {

@@ -135,3 +135,8 @@ def test_a_gate_far_above_zero(dtype, up, strength):
     d.g[40], d.g[41] = -up, up  # what is lost comes back
     d.beta[40] *= strength
     d.check()
+
+
+@pytest.mark.parametrize("n", [19, 20, 21, 22])
+def test_around_the_length_from_which_chunks_are_taken(n):
+    Delta(17, lens=(n, 40, n), H=4, K=2).check()
