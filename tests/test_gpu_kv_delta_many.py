@@ -140,3 +140,27 @@ def test_a_gate_far_above_zero(dtype, up, strength):
 @pytest.mark.parametrize("n", [19, 20, 21, 22])
 def test_around_the_length_from_which_chunks_are_taken(n):
     Delta(17, lens=(n, 40, n), H=4, K=2).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_long_sequences_captured(D, dtype):
+    d = Delta(18, lens=tuple(90 + i for i in range(30)), D=D, H=4, K=2, dtype=dtype, in_place=True)
+    first = d.raw.clone()
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=s):
+        gms.gms_kv_delta(d.desc, d.state, d.args, s.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(d.raw, first)
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    after, out = d.raw.clone(), d.out_full.clone()
+    d.raw.copy_(first)
+    for _ in range(2):
+        d.run()
+    before = d.raw.clone()
+    d.run()
+    assert torch.equal(after, d.raw) and torch.equal(out, d.out_full)
+    d.raw.copy_(before)
+    d.check()
