@@ -224,3 +224,13 @@ def test_replayed_step_by_step_in_place(S):
         assert dev["lens"].tolist() == lens and dev["table"].tolist() == table and dev["ring"].tolist() == ring and dev["state"].tolist() == state
         assert slots.tolist() == sl and positions.tolist() == po and dev["cu"].tolist() == cu
         assert int(status) == (gms.DEV_FULL if full else int(status))
+
+
+@pytest.mark.parametrize("extra", [-33, -1, 0, 1, 700])
+@pytest.mark.parametrize("many", [1, 4096])
+def test_around_the_most_blocks_that_are_fetched_at_once(extra, many):
+    """One CTA of 16 warps, or a cluster of 256 (a short sequence each): 1,024 blocks a warp."""
+    most = 1024 * (16 if many == 1 else 256) + extra
+    lens = [16 * (most // many)] * many
+    lens[many // 2] += 16 * (most % many)
+    run(lens + [20, 3], [0] * many + [1, 1], lens + [0, 0], holes=[(0, 1, -7)])
