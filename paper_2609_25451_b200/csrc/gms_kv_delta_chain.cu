@@ -606,6 +606,33 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd |= ((b[e] & kOnes) == kOnes) | ((b[e] >> 16 & kOnes) == kOnes);
         }
+        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
+        float X[CT][4] = {}, Y[CT][4] = {};
+        float u0 = 1.f, u1 = 1.f;
+        if (kHalf) u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
+#pragma unroll
+        for (int kt = 0; kt < D / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2], c[CT][2];
+#pragma unroll
+            for (int nt = 0; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+            terms(T(), S + 2 * kt, u0, u1, hi, lo);
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 0; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
+                c[nt][0] = x[0], c[nt][1] = x[1], c[nt + 1][0] = x[2], c[nt + 1][1] = x[3];
+            }
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], lo, b[nt][0], b[nt][1], T());
+#pragma unroll
+            for (int nt = 0; nt < CT; ++nt) mma16816(Y[nt], hi, c[nt][0], c[nt][1], T());
+        }
         if (__any_sync(0xffffffffu, odd)) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
 #pragma unroll 1
@@ -648,33 +675,6 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
             }
             done();
             continue;
-        }
-        // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
-        float X[CT][4] = {}, Y[CT][4] = {};
-        float u0 = 1.f, u1 = 1.f;
-        if (kHalf) u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
-#pragma unroll
-        for (int kt = 0; kt < D / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[CT][2], c[CT][2];
-#pragma unroll
-            for (int nt = 0; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.k) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
-            }
-            terms(T(), S + 2 * kt, u0, u1, hi, lo);
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], hi, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.q) + piece<P>(8 * nt + b_row, 2 * kt + b_piece), x);
-                c[nt][0] = x[0], c[nt][1] = x[1], c[nt + 1][0] = x[2], c[nt + 1][1] = x[3];
-            }
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) mma16816(X[nt], lo, b[nt][0], b[nt][1], T());
-#pragma unroll
-            for (int nt = 0; nt < CT; ++nt) mma16816(Y[nt], hi, c[nt][0], c[nt][1], T());
         }
         // what the values differ by from what the state says: X <- V - f X
         const float si0 = flipped(u0), si1 = flipped(u1);
