@@ -596,15 +596,12 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         wait(&m.full[stage], chunk / kStages);
         // the columns' values, transposed like everything else
         uint32_t V[CT][2];
-        uint32_t odd = st.w.by_row;
-        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
+        const uint32_t by_row = st.w.by_row;
 #pragma unroll
         for (int nt = 0; nt < CT; nt += 2) {
             uint32_t b[4];
             ldmatrix_x4_trans(smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * warp + b_piece), b);
             V[nt][0] = b[0], V[nt][1] = b[1], V[nt + 1][0] = b[2], V[nt + 1][1] = b[3];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd |= ((b[e] & kOnes) == kOnes) | ((b[e] >> 16 & kOnes) == kOnes);
         }
         // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
         float X[CT][4] = {}, Y[CT][4] = {};
@@ -633,7 +630,21 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
 #pragma unroll
             for (int nt = 0; nt < CT; ++nt) mma16816(Y[nt], hi, c[nt][0], c[nt][1], T());
         }
-        if (__any_sync(0xffffffffu, odd)) {
+        // what the values differ by from what the state says: X <- V - f X
+        const float si0 = flipped(u0), si1 = flipped(u1);
+        float finite = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
+            const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
+            X[nt][0] = to_f32(va[0]) - f.x * (kHalf ? X[nt][0] * si0 : X[nt][0]);
+            X[nt][1] = to_f32(va[1]) - f.y * (kHalf ? X[nt][1] * si0 : X[nt][1]);
+            X[nt][2] = to_f32(vb[0]) - f.x * (kHalf ? X[nt][2] * si1 : X[nt][2]);
+            X[nt][3] = to_f32(vb[1]) - f.y * (kHalf ? X[nt][3] * si1 : X[nt][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) finite = fmaf(X[nt][e], 0.f, finite);
+        }
+        if (__any_sync(0xffffffffu, by_row | (finite != 0.f))) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
 #pragma unroll 1
             for (int r = 0; r < n; ++r) {
@@ -675,17 +686,6 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
             }
             done();
             continue;
-        }
-        // what the values differ by from what the state says: X <- V - f X
-        const float si0 = flipped(u0), si1 = flipped(u1);
-#pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
-            const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
-            X[nt][0] = to_f32(va[0]) - f.x * (kHalf ? X[nt][0] * si0 : X[nt][0]);
-            X[nt][1] = to_f32(va[1]) - f.y * (kHalf ? X[nt][1] * si0 : X[nt][1]);
-            X[nt][2] = to_f32(vb[0]) - f.x * (kHalf ? X[nt][2] * si1 : X[nt][2]);
-            X[nt][3] = to_f32(vb[1]) - f.y * (kHalf ? X[nt][3] * si1 : X[nt][3]);
         }
         // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range; T's columns beyond a row's
         // own are zero
