@@ -568,6 +568,10 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[nt][e] = from ? from[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] : 0.f;
+    auto times = [](float *x, float2 f, float2 g) {  // rows g and g + 8 of an accumulator
+        const float2 a = ptx::mul2(make_float2(x[0], x[1]), f), b = ptx::mul2(make_float2(x[2], x[3]), g);
+        x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+    };
     // f16: rows (e = 0, 1: g and g + 8) are scaled by powers of two of their own before they are rounded
     auto scale_of = [](const float(*x)[4], int tiles, int e) {
         float top = 0.f;
@@ -632,19 +636,18 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         }
         // what the values differ by from what the state says: X <- V - f X
         const float si0 = flipped(u0), si1 = flipped(u1);
-        float finite = 0.f;
+        float2 finite = make_float2(0.f, 0.f);
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
             const T *va = reinterpret_cast<const T *>(&V[nt][0]), *vb = reinterpret_cast<const T *>(&V[nt][1]);
-            X[nt][0] = to_f32(va[0]) - f.x * (kHalf ? X[nt][0] * si0 : X[nt][0]);
-            X[nt][1] = to_f32(va[1]) - f.y * (kHalf ? X[nt][1] * si0 : X[nt][1]);
-            X[nt][2] = to_f32(vb[0]) - f.x * (kHalf ? X[nt][2] * si1 : X[nt][2]);
-            X[nt][3] = to_f32(vb[1]) - f.y * (kHalf ? X[nt][3] * si1 : X[nt][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) finite = fmaf(X[nt][e], 0.f, finite);
+            const float2 m0 = kHalf ? ptx::mul2(f, make_float2(-si0, -si0)) : make_float2(-f.x, -f.y), m1 = kHalf ? ptx::mul2(f, make_float2(-si1, -si1)) : m0;
+            const float2 x0 = ptx::fma2(m0, make_float2(X[nt][0], X[nt][1]), make_float2(to_f32(va[0]), to_f32(va[1])));
+            const float2 x1 = ptx::fma2(m1, make_float2(X[nt][2], X[nt][3]), make_float2(to_f32(vb[0]), to_f32(vb[1])));
+            X[nt][0] = x0.x, X[nt][1] = x0.y, X[nt][2] = x1.x, X[nt][3] = x1.y;
+            finite = ptx::fma2(x0, make_float2(0.f, 0.f), ptx::fma2(x1, make_float2(0.f, 0.f), finite));
         }
-        if (__any_sync(0xffffffffu, by_row | (finite != 0.f))) {
+        if (__any_sync(0xffffffffu, by_row | (finite.x + finite.y != 0.f))) {
             // row by row: something here is not finite, and in a product it would reach rows that come before it
 #pragma unroll 1
             for (int r = 0; r < n; ++r) {
@@ -718,11 +721,11 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
             di0 = st.w.p_unit * flipped(u0), di1 = st.w.p_unit * flipped(u1);
         }
         // out = h Y + P d (one term of P, two of d; f16: in units of P and d meanwhile)
+        const float y0 = si0 * flipped(di0), y1 = si1 * flipped(di1);
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
-            if (kHalf) Y[nt][0] *= si0 * flipped(di0), Y[nt][1] *= si0 * flipped(di0), Y[nt][2] *= si1 * flipped(di1), Y[nt][3] *= si1 * flipped(di1);
-            Y[nt][0] *= f.x, Y[nt][1] *= f.y, Y[nt][2] *= f.x, Y[nt][3] *= f.y;
+            times(Y[nt], kHalf ? ptx::mul2(f, make_float2(y0, y0)) : f, kHalf ? ptx::mul2(f, make_float2(y1, y1)) : f);
         }
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
@@ -743,12 +746,12 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
-            d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
+            times(d[nt], f, f);
         }
         if (kHalf) u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
         const float all0 = st.w.all * u0, all1 = st.w.all * u1;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[nt][0] *= all0, S[nt][1] *= all0, S[nt][2] *= all1, S[nt][3] *= all1;
+        for (int nt = 0; nt < NT; ++nt) times(S[nt], make_float2(all0, all0), make_float2(all1, all1));
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
             uint32_t hi[4], lo[4];
@@ -771,7 +774,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         if (kHalf) {
             const float i0 = flipped(u0), i1 = flipped(u1);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[nt][0] *= i0, S[nt][1] *= i0, S[nt][2] *= i1, S[nt][3] *= i1;
+            for (int nt = 0; nt < NT; ++nt) times(S[nt], make_float2(i0, i0), make_float2(i1, i1));
         }
         // rows of 16 columns through the warp's own part of V's tile
 #pragma unroll
