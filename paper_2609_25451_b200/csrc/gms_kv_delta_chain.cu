@@ -507,7 +507,7 @@ struct SoloSmem {
 // product is, element for element, a first factor of the next, S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out, so nothing
 // leaves the registers between the products and no warp waits for another.  W of them (16 W columns of a head) share a chunk's
 // operands, which further warps fetch ahead.  Bound by the rate of the products, 420 of them a chunk and warp at 128 keys, 8.3 cycles
-// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,500 cycles a chunk.
+// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,600 cycles a chunk (64 keys: 264, 4,250).
 template <class T, int D, int W>
 __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kCtas) kv_delta_solo_kernel(const __grid_constant__ DeltaArgs a)
 {
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     constexpr uint32_t kParts = D / (16 * W);
     // Where some SMs have a second CTA from the start, they are those of the first CTAs, which therefore take the shorter sequences of
-    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 176 us without, 168 us).
+    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 154.6 us without, 146.4 us).
     constexpr uint32_t kSms = 148;
     const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
     const uint32_t item = turned ? kSms - 1 - blockIdx.x : blockIdx.x;
@@ -823,7 +823,7 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
     const uint32_t ctas = a.n_seq * a.n_heads * (D / (16 * W));
     if (SoloShape<D, W>::kCtas == 1) return launch_dependent(kv_delta_solo_kernel<T, D, W>, ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s, a);
     // Two an SM: they start when the kernel ahead has ended, or the first two, the longest, come to share the first SM that is free
-    // (13 sequences of up to 2,001 rows, 16 heads of 64: 204 us so, 163 us waiting; fp16 198 and 183 us).
+    // (13 sequences of up to 2,001 rows, 16 heads of 64: 167 us so, 136 us waiting; fp16 177 and 146 us).
     kv_delta_solo_kernel<T, D, W><<<ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s>>>(a);
     const cudaError_t f = cudaGetLastError();
     if (f == cudaSuccess) count_launches(1);
@@ -831,8 +831,9 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
 }
 // The lengths are on the device: where there are more than two sequences for every max_q rows, as many count as have max_q rows, the
 // others being short.  While an SM each is enough for their slices (a pair of slices each), relays are faster, beyond that solos (us,
-// the first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows, 4 heads of 128 228 / 402, 32 heads of 128 335 / 466; 2 of
-// 4,000 335 / 269; 8 of 1,000 325 / 278; 4 of 100 to 4,000 417 / 375; 1 of 8,192, 32 heads of 64, one slice an SM 260, two 306, solo 396).
+// the first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows, 4 heads of 128 226 / 388, 32 heads of 128 325 / 429; 8 of
+// 1,232 to 2,632, 6 heads of 64 114 / 124; 2 of 4,000, 32 heads of 128 325 / 245; 8 of 1,000 316 / 261; 4 of 100 to 4,000 403 / 351;
+// 1 of 8,192, 32 heads of 64, one slice an SM 253, two 296, solo 327).
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
 {
