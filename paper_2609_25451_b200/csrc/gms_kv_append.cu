@@ -68,10 +68,11 @@ __device__ __forceinline__ void weights_of(const AppendArgs &a, const void *w, u
 // nothing is exchanged), the lanes behind those the elements that are not rotated.  A warp takes 256 / D neighbouring rows, and a
 // run of their heads, first the queries', then the keys', then the values', kUnroll at a time, the next ones on their way while these
 // are computed; what differs between the lanes (row, angles) stays the same for all of them.  Two pairs are computed an instruction.
-// Bound by memory where there are many rows (52,367 of 32 / 8 heads of 64: 115 us, 5.6 TB/s, with 970 instructions a row; a
+// Bound by memory where there are many rows (52,367 of 32 / 8 heads of 64: 111 us, 5.8 TB/s, with 970 instructions a row; a
 // warp with several heads of one row took 1,800 and 145 us), by latency where there are few (then a warp has kUnroll heads).  20
-// warps an SM: with 24 and fewer registers, or 16, the same rows take 125 us.
-constexpr uint32_t kAppendThreads = 128, kAppendCtas = 5, kUnroll = 4;
+// warps an SM: with 24 and fewer registers, or 16, the same rows take 125 us; each a CTA of its own, so that none waits for others
+// to end (in fours 115 us, and 6,776 rows of 16 / 4 heads of 128 21.0 us against 19.9).
+constexpr uint32_t kAppendThreads = 32, kAppendCtas = 20, kUnroll = 4;
 
 template <class T, int D, bool HALVES>
 __global__ void __launch_bounds__(kAppendThreads, kAppendCtas) kv_append_kernel(const __grid_constant__ AppendArgs a)
@@ -221,15 +222,15 @@ template <class T>
 cudaError_t launch_append(AppendArgs &a, uint32_t dim, cudaStream_t s)
 {
     // Four rows of 64 or two of 128 a warp, with all their heads where that fills the GPU twice; with fewer rows they are cut, down to
-    // kUnroll heads a warp (6,776 rows of 16 / 4 heads of 128: 26.6 us where they fill it once, 24.5 twice or four times, 30.7 eight
-    // times, as more warps make the same angles; 52,367 rows of 32 / 8 heads of 64: 114.7 us in all of these).
+    // kUnroll heads a warp (6,776 rows of 16 / 4 heads of 128: 23.0 us where they fill it once, 21.5 twice or four times, 26.6 six
+    // times, as more warps make the same angles; 52,367 rows of 32 / 8 heads of 64: 106 to 108 us in all of these).
     const uint32_t heads = a.n_heads + 2 * a.n_kv, together = dim == 128 ? 2 : 4;
     const uint64_t fill = 148 * 20 * 2, row_warps = (a.rows + together - 1) / together, batches = (heads + kUnroll - 1) / kUnroll;
     const uint64_t want = (fill + row_warps - 1) / row_warps, cuts = want < batches ? want : batches;
     a.per_part = (uint32_t)((batches + cuts - 1) / cuts) * kUnroll;
     a.parts = (heads + a.per_part - 1) / a.per_part;
     const uint64_t warps = row_warps * a.parts, grid = (warps + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
-    if (grid > 0x3fffffffull) return cudaErrorInvalidValue;
+    if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
     if (a.pairs == GMS_PAIR_HALVES)
         return dim == 128 ? launch_dependent(kv_append_kernel<T, 128, true>, (uint32_t)grid, kAppendThreads, 0, s, a)
                           : launch_dependent(kv_append_kernel<T, 64, true>, (uint32_t)grid, kAppendThreads, 0, s, a);
