@@ -164,3 +164,45 @@ def test_many_long_sequences_captured(D, dtype):
     assert torch.equal(after, d.raw) and torch.equal(out, d.out_full)
     d.raw.copy_(before)
     d.check()
+
+
+@pytest.mark.parametrize("D,per,S", [(64, 8, 12), (64, 8, 34), (128, 2, 6), (128, 2, 15)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("what", ["v", "k", "q", "beta", "g", "state"])
+def test_what_is_not_finite_stays_with_what_depends_on_it(D, per, S, dtype, what):
+    """As for few sequences, with as many as let a CTA have two slices of a state or a warp one of its own."""
+    n, at, bad = 130, 70, float("inf") if what in ("v", "beta") else float("nan")
+    kw = dict(lens=(n,) * S, H=4, K=2, D=D, per=per, dtype=dtype)
+    clean, d = Delta(19, **kw), Delta(19, **kw)
+    row, start = d.cu_h[1] + at, d.cu_h[1]
+    if what == "v":
+        d.v[row, 1, 5] = bad
+    elif what in "kq":
+        getattr(d, what)[row, 0, 5] = bad
+    elif what == "state":
+        d.place(d.raw, d.src_h, 1, 1)[3, 5] = bad
+        row = start
+    else:
+        getattr(d, what)[row, 1] = bad
+    clean.run()
+    d.run()
+    cols = [5] if what in ("v", "state") else list(range(D))
+    end = row + 1 if what == "q" else d.cu_h[2]
+    for h in [0, 1] if what in ("k", "q") else [1]:
+        assert not torch.isfinite(d.out[row:end, h][:, cols].float()).any()
+        d.out[row:end, h, cols[0]:cols[-1] + 1] = clean.out[row:end, h, cols[0]:cols[-1] + 1]
+        if what != "q":
+            st, want = d.place(d.raw, d.dst_h, 1, h), clean.place(clean.raw, clean.dst_h, 1, h)
+            assert not torch.isfinite(st[:, cols]).all()
+            st[:, cols[0]:cols[-1] + 1] = want[:, cols[0]:cols[-1] + 1]
+    if what == "state":
+        d.place(d.raw, d.src_h, 1, 1)[3, 5] = clean.place(clean.raw, clean.src_h, 1, 1)[3, 5]
+    n1, out, want, bound, e = clean.reference(clean.raw)[1]
+    r = slice(start, d.cu_h[2])
+    assert ((d.out[r].double() - out).abs() <= bound).all()
+    for h in range(4):
+        assert (d.place(d.raw, d.dst_h, 1, h).double() - want[h]).norm() <= e[h]
+    d.out[r] = clean.out[r]
+    for h in range(4):
+        d.place(d.raw, d.dst_h, 1, h).copy_(clean.place(clean.raw, clean.dst_h, 1, h))
+    assert torch.equal(d.out_full, clean.out_full) and torch.equal(d.raw, clean.raw)  # nothing else differs
