@@ -90,21 +90,13 @@ struct RelaySmem {
 // sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 275 us or 4,080 cycles a chunk (one: 3,060),
 // in which the products take 48 % of the tensor cores' cycles and loads, stores and exchanges 76 % of shared memory's.
 template <class T, int D, int W>
-__global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_kernel(const __grid_constant__ DeltaArgs a)
+__device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    RelaySmem<D, W> &m = *reinterpret_cast<RelaySmem<D, W> *>(raw);
     constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 32, KQ = D / 64;  // tiles of 8 and of 16 keys that a warp has
     constexpr int kStages = RelayShape<D, W>::kStages;
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
-    constexpr uint32_t kParts = D / (16 * W);
-    const uint32_t part = blockIdx.x % kParts, h = blockIdx.x / kParts % a.n_heads, rank = blockIdx.x / kParts / a.n_heads, kh = h / a.group;
-    const uint32_t col0 = part * W * 16;  // of the CTA
-    ptx::grid_launch_dependents();
-    ptx::grid_wait();
-    const uint32_t s = a.order[rank];
-    if (s >= a.n_seq) return;
+    const uint32_t kh = h / a.group, col0 = part * W * 16;  // of the CTA
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
     const int chunks = (rows + C - 1) / C;
     if (threadIdx.x == 0) {
@@ -489,6 +481,31 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
 }
 
+// Most items of a batch in which few sequences are long are none: they come last.  Where there are many for each SM, CTAs go through
+// several (AGAIN) instead of being started for each (us, one CTA an item / so: a prompt of 2,048 rows among 255 single rows, 32 heads of
+// 128 368 / 284, of 64 214 / 140; of 4,096 among 95 259 / 245; of 8,192 among 31, 4,096 items, 329 / 341, as the loop costs registers).
+constexpr uint32_t kMany = 148 * 32;
+template <class T, int D, int W, bool AGAIN>
+__global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_kernel(const __grid_constant__ DeltaArgs a)
+{
+    extern __shared__ __align__(16) uint8_t raw[];
+    RelaySmem<D, W> &m = *reinterpret_cast<RelaySmem<D, W> *>(raw);
+    constexpr uint32_t kParts = D / (16 * W);
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+    for (uint32_t item = blockIdx.x; item < a.n_seq * a.n_heads * kParts; item += gridDim.x) {
+        const uint32_t s = a.order[item / kParts / a.n_heads];
+        if (s >= a.n_seq) return;
+        relay<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts);
+        if (!AGAIN) return;
+        __syncthreads();
+        if (threadIdx.x == 0) {  // (made anew for the next item)
+            for (int i = 0; i < RelayShape<D, W>::kStages; ++i) ptx::mbar_inval(smem_u32(&m.full[i])), ptx::mbar_inval(smem_u32(&m.empty[i]));
+            for (int i = 0; i < W; ++i) ptx::mbar_inval(smem_u32(&m.ready[i])), ptx::mbar_inval(smem_u32(&m.taken[i]));
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ many states
 // W warps with states, and warps that fetch.
 template <int D, int W>
@@ -509,26 +526,13 @@ struct SoloSmem {
 // operands, which further warps fetch ahead.  Bound by the rate of the products, 420 of them a chunk and warp at 128 keys, 8.3 cycles
 // each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,600 cycles a chunk (64 keys: 264, 4,250).
 template <class T, int D, int W>
-__global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kCtas) kv_delta_solo_kernel(const __grid_constant__ DeltaArgs a)
+__device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    SoloSmem<D, W> &m = *reinterpret_cast<SoloSmem<D, W> *>(raw);
     constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 8, CT = C / 8;
     constexpr int kStages = SoloShape<D, W>::kStages;
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
-    constexpr uint32_t kParts = D / (16 * W);
-    // Where some SMs have a second CTA from the start, they are those of the first CTAs, which therefore take the shorter sequences of
-    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 154.6 us without, 146.4 us).
-    constexpr uint32_t kSms = 148;
-    const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
-    const uint32_t item = turned ? kSms - 1 - blockIdx.x : blockIdx.x;
-    const uint32_t part = item % kParts, h = item / kParts % a.n_heads, rank = item / kParts / a.n_heads, kh = h / a.group;
-    const uint32_t col0 = part * W * 16;  // of the CTA
-    ptx::grid_launch_dependents();
-    ptx::grid_wait();
-    const uint32_t s = a.order[rank];
-    if (s >= a.n_seq) return;
+    const uint32_t kh = h / a.group, col0 = part * W * 16;  // of the CTA
     const int rows = delta_rows(a, s), first = delta_begin(a, s);
     const int chunks = (rows + C - 1) / C;
     if (threadIdx.x == 0) {
@@ -800,34 +804,70 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
         for (int e = 0; e < 4; ++e) to[at0 + (8 * nt + (e & 1)) * D + (e & 2) * 4] = S[nt][e];
 }
 
+template <class T, int D, int W, bool AGAIN>
+__global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kCtas) kv_delta_solo_kernel(const __grid_constant__ DeltaArgs a)
+{
+    extern __shared__ __align__(16) uint8_t raw[];
+    SoloSmem<D, W> &m = *reinterpret_cast<SoloSmem<D, W> *>(raw);
+    constexpr uint32_t kParts = D / (16 * W);
+    // Where some SMs have a second CTA from the start, they are those of the first CTAs, which therefore take the shorter sequences of
+    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 154.6 us without, 146.4 us).
+    constexpr uint32_t kSms = 148;
+    const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+    for (uint32_t item = turned ? kSms - 1 - blockIdx.x : blockIdx.x; item < a.n_seq * a.n_heads * kParts; item += gridDim.x) {
+        const uint32_t s = a.order[item / kParts / a.n_heads];
+        if (s >= a.n_seq) return;
+        solo<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts);
+        if (!AGAIN) return;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < SoloShape<D, W>::kStages; ++i) ptx::mbar_inval(smem_u32(&m.full[i])), ptx::mbar_inval(smem_u32(&m.empty[i]));
+        }
+    }
+}
+
 // More than half of an SM's shared memory: while the kernel ahead drains, two CTAs would come to share the first SMs that are free.
 constexpr uint32_t kOneAnSm = 118784;
 
-template <class T, int D, int W>
-cudaError_t launch_relay(const DeltaArgs &a, cudaStream_t s)
+template <class T, int D, int W, bool AGAIN>
+cudaError_t launch_relay(const DeltaArgs &a, uint32_t ctas, cudaStream_t s)
 {
     static_assert(sizeof(RelaySmem<D, W>) <= 232448, "");
     static std::atomic<uint64_t> done;
-    const cudaError_t e = allow_smem(kv_delta_relay_kernel<T, D, W>, 232448, done);
+    const cudaError_t e = allow_smem(kv_delta_relay_kernel<T, D, W, AGAIN>, 232448, done);
     if (e != cudaSuccess) return e;
     const uint32_t smem = sizeof(RelaySmem<D, W>) > kOneAnSm ? sizeof(RelaySmem<D, W>) : kOneAnSm;
-    return launch_dependent(kv_delta_relay_kernel<T, D, W>, a.n_seq * a.n_heads * (D / (16 * W)), RelayShape<D, W>::kThreads, smem, s, a);
+    return launch_dependent(kv_delta_relay_kernel<T, D, W, AGAIN>, ctas, RelayShape<D, W>::kThreads, smem, s, a);
+}
+template <class T, int D, int W>
+cudaError_t launch_relay(const DeltaArgs &a, cudaStream_t s)
+{
+    const uint32_t items = a.n_seq * a.n_heads * (D / (16 * W));
+    return items <= kMany ? launch_relay<T, D, W, false>(a, items, s) : launch_relay<T, D, W, true>(a, 148 * 4, s);
+}
+template <class T, int D, int W, bool AGAIN>
+cudaError_t launch_solo(const DeltaArgs &a, uint32_t ctas, cudaStream_t s)
+{
+    static_assert(sizeof(SoloSmem<D, W>) <= 232448, "");
+    static std::atomic<uint64_t> done;
+    const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W, AGAIN>, 232448, done);
+    if (e != cudaSuccess) return e;
+    const uint32_t threads = SoloShape<D, W>::kThreads, smem = sizeof(SoloSmem<D, W>);
+    if (SoloShape<D, W>::kCtas == 1) return launch_dependent(kv_delta_solo_kernel<T, D, W, AGAIN>, ctas, threads, smem, s, a);
+    // Two an SM: they start when the kernel ahead has ended, or the first two, the longest, come to share the first SM that is free
+    // (13 sequences of up to 2,001 rows, 16 heads of 64: 167 us so, 136 us waiting; fp16 177 and 146 us).
+    kv_delta_solo_kernel<T, D, W, AGAIN><<<ctas, threads, smem, s>>>(a);
+    const cudaError_t f = cudaGetLastError();
+    if (f == cudaSuccess) count_launches(1);
+    return f;
 }
 template <class T, int D, int W>
 cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
 {
-    static_assert(sizeof(SoloSmem<D, W>) <= 232448, "");
-    static std::atomic<uint64_t> done;
-    const cudaError_t e = allow_smem(kv_delta_solo_kernel<T, D, W>, 232448, done);
-    if (e != cudaSuccess) return e;
-    const uint32_t ctas = a.n_seq * a.n_heads * (D / (16 * W));
-    if (SoloShape<D, W>::kCtas == 1) return launch_dependent(kv_delta_solo_kernel<T, D, W>, ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s, a);
-    // Two an SM: they start when the kernel ahead has ended, or the first two, the longest, come to share the first SM that is free
-    // (13 sequences of up to 2,001 rows, 16 heads of 64: 167 us so, 136 us waiting; fp16 177 and 146 us).
-    kv_delta_solo_kernel<T, D, W><<<ctas, SoloShape<D, W>::kThreads, sizeof(SoloSmem<D, W>), s>>>(a);
-    const cudaError_t f = cudaGetLastError();
-    if (f == cudaSuccess) count_launches(1);
-    return f;
+    const uint32_t items = a.n_seq * a.n_heads * (D / (16 * W));
+    return items <= kMany ? launch_solo<T, D, W, false>(a, items, s) : launch_solo<T, D, W, true>(a, 148 * 8 * SoloShape<D, W>::kCtas, s);
 }
 // The lengths are on the device: where there are more than two sequences for every max_q rows, as many count as have max_q rows, the
 // others being short.  While an SM each is enough for their slices (a pair of slices each), relays are faster, beyond that solos (us,

@@ -206,3 +206,11 @@ def test_what_is_not_finite_stays_with_what_depends_on_it(D, per, S, dtype, what
     for h in range(4):
         d.place(d.raw, d.dst_h, 1, h).copy_(clean.place(clean.raw, clean.dst_h, 1, h))
     assert torch.equal(d.out_full, clean.out_full) and torch.equal(d.raw, clean.raw)  # nothing else differs
+
+
+@pytest.mark.parametrize("D,per,H,S,loose", [(128, 2, 4, 150, True), (128, 2, 32, 38, True), (64, 8, 8, 160, True), (64, 8, 16, 300, False), (128, 2, 8, 300, False)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_more_long_sequences_than_ctas(D, per, H, S, loose, dtype):
+    """CTAs that go through several sequences; `loose`: more of them are long than the largest length lets expect."""
+    lens = tuple(15 + (i * 29) % 60 + (130 if i % 31 == 5 else 0) for i in range(S))
+    Delta(20, lens=lens, D=D, per=per, H=H, K=H // 2, dtype=dtype, fresh=(0, 7), max_q=sum(lens) if loose else None).check()
