@@ -41,7 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     cmd = [
-        _nvcc(), "-std=c++17", "-O3", "-lineinfo",
+        _nvcc(), "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
         "-gencode", "arch=compute_100a,code=sm_100a",
         "-Xcompiler", "-fPIC,-Wall,-Wextra", "-shared",
         "-I", os.path.join(ROOT, "include"),
