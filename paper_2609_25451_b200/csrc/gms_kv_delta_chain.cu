@@ -90,7 +90,7 @@ struct RelaySmem {
 // sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 275 us or 4,080 cycles a chunk (one: 3,060),
 // in which the products take 48 % of the tensor cores' cycles and loads, stores and exchanges 76 % of shared memory's.
 template <class T, int D, int W>
-__device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part)
+__device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part, bool &late)
 {
     constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 32, KQ = D / 64;  // tiles of 8 and of 16 keys that a warp has
     constexpr int kStages = RelayShape<D, W>::kStages;
@@ -112,7 +112,6 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
     }
     __syncthreads();
     // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
-    bool late = false;
     auto wait = [&](uint64_t *bar, int use) {
         if (late || ptx::mbar_wait(smem_u32(bar), (uint32_t)(use & 1))) return;
         late = true;
@@ -491,12 +490,13 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
     extern __shared__ __align__(16) uint8_t raw[];
     RelaySmem<D, W> &m = *reinterpret_cast<RelaySmem<D, W> *>(raw);
     constexpr uint32_t kParts = D / (16 * W);
+    bool late = false;  // a wait has run out
     ptx::grid_launch_dependents();
     ptx::grid_wait();
     for (uint32_t item = blockIdx.x; item < a.n_seq * a.n_heads * kParts; item += gridDim.x) {
         const uint32_t s = a.order[item / kParts / a.n_heads];
         if (s >= a.n_seq) return;
-        relay<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts);
+        relay<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts, late);
         if (!AGAIN) return;
         __syncthreads();
         if (threadIdx.x == 0) {  // (made anew for the next item)
@@ -526,7 +526,7 @@ struct SoloSmem {
 // operands, which further warps fetch ahead.  Bound by the rate of the products, 420 of them a chunk and warp at 128 keys, 8.3 cycles
 // each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,600 cycles a chunk (64 keys: 264, 4,250).
 template <class T, int D, int W>
-__device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part)
+__device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part, bool &late)
 {
     constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 8, CT = C / 8;
     constexpr int kStages = SoloShape<D, W>::kStages;
@@ -544,7 +544,6 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
     }
     __syncthreads();
     // A wait that runs out (it cannot, but for a fault in here) is told in the status word; everybody goes on without waiting.
-    bool late = false;
     auto wait = [&](uint64_t *bar, int use) {
         if (late || ptx::mbar_wait(smem_u32(bar), (uint32_t)(use & 1))) return;
         late = true;
@@ -814,12 +813,13 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 154.6 us without, 146.4 us).
     constexpr uint32_t kSms = 148;
     const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
+    bool late = false;  // a wait has run out
     ptx::grid_launch_dependents();
     ptx::grid_wait();
     for (uint32_t item = turned ? kSms - 1 - blockIdx.x : blockIdx.x; item < a.n_seq * a.n_heads * kParts; item += gridDim.x) {
         const uint32_t s = a.order[item / kParts / a.n_heads];
         if (s >= a.n_seq) return;
-        solo<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts);
+        solo<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts, late);
         if (!AGAIN) return;
         __syncthreads();
         if (threadIdx.x == 0) {
