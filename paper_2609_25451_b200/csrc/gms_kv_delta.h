@@ -29,10 +29,10 @@ constexpr uint32_t kChunkRows = 64, kMostByRow = 20, kNone = 0xffffffffu;
 
 // What the first of the two chunk kernels leaves for the second.
 struct alignas(256) ChunkWork {
-    uint8_t tile[3][10 * 512];  // T in two terms, P: blocks of 16 x 16 in and below the diagonal, laid out as `block_piece` says
+    uint8_t tile[4][10 * 512];  // T, P, two bf16 terms each: blocks of 16 x 16 in and below the diagonal, laid out as `block_piece` says
     float f[kChunkRows], w[kChunkRows], h[kChunkRows];
     float gate[kChunkRows], beta[kChunkRows], rk[kChunkRows], rq[kChunkRows];  // for chunks that are done row by row
-    float all, p_unit;                             // e^G of the chunk; f16: what P is a multiple of
+    float all;                                     // e^G of the chunk
     uint32_t by_row;
 };
 

@@ -64,10 +64,13 @@ __device__ __forceinline__ void fetch_chunk(const DeltaArgs &a, Stage<D, W> &st,
 template <int D>
 struct Talk {
     uint4 s[D / 16][32];       // S before the chunk, the first of its two terms
-    float4 sum[4][3][2][32];   // [to][from the others]: what X is the sum of
+    union {
+        float4 sum[4][3][2][32];  // [to][from the others]: what X is the sum of
+        uint4 d[4][2][32];        // d, in two terms, once all sums have been read (and gone before the next ones are written)
+    };
     uint4 x[4][2][32];         // V - f X of the 16 rows of each warp, in two terms
-    uint4 d[4][2][32], dw[4][2][32];                           // d and w d, the same
-    float2 s_unit[4][8], dw_unit[4][8], d_unit[4][8];  // f16: powers of two that rows' terms are multiples of
+    uint4 dw[4][2][32];        // w d, the same
+    float2 s_unit[4][8], dw_unit[4][8];  // f16: powers of two that rows' terms are multiples of
     uint32_t odd[4];           // the chunk is done row by row
 };
 template <int D, int W>
@@ -141,7 +144,8 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
         for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
     };
     if (warp >= 4 * W) {
-        // out = h Q S + P d, with S before the chunk (one term of S and of P, two of d), two tiles of 16 rows at a time
+        // out = h Q S + P d, with S before the chunk (one term of S, two of P and d without the product of the small ones), two tiles of
+        // 16 rows at a time
         const uint32_t slice = warp - 4 * W;
         Talk<D> &talk = m.talk[slice];
 #pragma unroll 1
@@ -153,13 +157,13 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             wait(&m.ready[slice], chunk);
             const bool by_row = talk.odd[0] | talk.odd[1] | talk.odd[2] | talk.odd[3];
             uint4 sf[D / 16], df[4][2];
-            float2 su[4], du[4];
+            float2 su[4];
 #pragma unroll
             for (int kt = 0; kt < D / 16; ++kt) sf[kt] = talk.s[kt][lane];
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
                 df[kt][0] = talk.d[kt][0][lane], df[kt][1] = talk.d[kt][1][lane];
-                if (kHalf) su[kt] = talk.s_unit[kt][g], du[kt] = talk.d_unit[kt][g];
+                if (kHalf) su[kt] = talk.s_unit[kt][g];
             }
             arrive(&m.taken[slice]);
             if (!by_row) {
@@ -191,24 +195,21 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
                             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[16 * tile + 8 * nt + t2]);
                             Y[i][nt][0] *= f.x, Y[i][nt][1] *= f.y, Y[i][nt][2] *= f.x, Y[i][nt][3] *= f.y;
                         }
-                        float2 u = one;
 #pragma unroll
                         for (int kt = 0; kt < 4; ++kt) {
                             if (kt > tile) break;
-                            if (kHalf) {
-                                const float2 next = du[kt];
-                                change(Y[i], u, next);
-                                u = next;
-                            }
-                            uint32_t b[4];
-                            ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(16 * tile + b_row, 2 * kt + b_piece), b);
+                            uint32_t b[4], c[4];
+                            const uint32_t at = block_piece(16 * tile + b_row, 2 * kt + b_piece);
+                            ldmatrix_x4(smem_u32(st.w.tile[2]) + at, b);
+                            ldmatrix_x4(smem_u32(st.w.tile[3]) + at, c);
 #pragma unroll
                             for (int t = 0; t < 2; ++t) {
-                                mma16816(Y[i][0], &df[kt][t].x, b[0], b[1], T());
-                                mma16816(Y[i][1], &df[kt][t].x, b[2], b[3], T());
+                                mma16816(Y[i][0], &df[kt][t].x, b[0], b[1], kWide);
+                                mma16816(Y[i][1], &df[kt][t].x, b[2], b[3], kWide);
                             }
+                            mma16816(Y[i][0], &df[kt][0].x, c[0], c[1], kWide);
+                            mma16816(Y[i][1], &df[kt][0].x, c[2], c[3], kWide);
                         }
-                        if (kHalf) change(Y[i], u, one);
                         // (through the slice's part of V's tile, which the other warps have read)
                         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
                                          smem_u32(st.v) + piece<VP>(16 * tile + b_row, 2 * slice + b_piece)),
@@ -425,19 +426,14 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) d[nt][e] += dl[nt][e] + dt[nt][e];
-        float2 u = one;
-        if (kHalf) {
-            u = scales(d[0], d[1]);
-            tell(talk.d_unit[mine], make_float2(st.w.p_unit * flipped(u.x), st.w.p_unit * flipped(u.y)));
-        }
-        terms(T(), d[0], d[1], u, own_hi, own_lo);
+        terms(kWide, d[0], d[1], one, own_hi, own_lo);
         talk.d[mine][0][lane] = own_hi, talk.d[mine][1][lane] = own_lo;
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
             d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
         }
-        u = one;
+        float2 u = one;
         if (kHalf) {
             u = scales(d[0], d[1]);
             tell(talk.dw_unit[mine], inverse(u));
@@ -718,17 +714,11 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
                 mma16816(d[nt + 1], hi, x[2], x[3], kWide);
             }
         }
-        float di0 = 1.f, di1 = 1.f;
-        if (kHalf) {
-            u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
-            di0 = st.w.p_unit * flipped(u0), di1 = st.w.p_unit * flipped(u1);
-        }
-        // out = h Y + P d (one term of P, two of d; f16: in units of P and d meanwhile)
-        const float y0 = si0 * flipped(di0), y1 = si1 * flipped(di1);
+        // out = h Y + P d (two terms each without the product of the small ones)
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
-            times(Y[nt], kHalf ? ptx::mul2(f, make_float2(y0, y0)) : f, kHalf ? ptx::mul2(f, make_float2(y1, y1)) : f);
+            times(Y[nt], kHalf ? ptx::mul2(f, make_float2(si0, si0)) : f, kHalf ? ptx::mul2(f, make_float2(si1, si1)) : f);
         }
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
@@ -739,11 +729,18 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
                 ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
                 b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
             }
-            terms(T(), d + 2 * kt, u0, u1, hi, lo);
+            terms(kWide, d + 2 * kt, 1.f, 1.f, hi, lo);
 #pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], T());
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], kWide);
 #pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], lo, b[nt][0], b[nt][1], T());
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], lo, b[nt][0], b[nt][1], kWide);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[3]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                mma16816(Y[nt], hi, x[0], x[1], kWide);
+                mma16816(Y[nt + 1], hi, x[2], x[3], kWide);
+            }
         }
         // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
 #pragma unroll
@@ -784,8 +781,8 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
         for (int nt = 0; nt < CT; nt += 2)
             asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
                              smem_u32(st.v) + piece<VP>(8 * nt + b_row, 2 * warp + b_piece)),
-                         "r"(pack2(Y[nt][0] * di0, Y[nt][1] * di0, T())), "r"(pack2(Y[nt][2] * di1, Y[nt][3] * di1, T())),
-                         "r"(pack2(Y[nt + 1][0] * di0, Y[nt + 1][1] * di0, T())), "r"(pack2(Y[nt + 1][2] * di1, Y[nt + 1][3] * di1, T()))
+                         "r"(pack2(Y[nt][0], Y[nt][1], T())), "r"(pack2(Y[nt][2], Y[nt][3], T())),
+                         "r"(pack2(Y[nt + 1][0], Y[nt + 1][1], T())), "r"(pack2(Y[nt + 1][2], Y[nt + 1][3], T()))
                          : "memory");
         __syncwarp();
 #pragma unroll

@@ -6,7 +6,8 @@
 //   out = diag(h) Q S0 + P d,            P_ij = scale s_i r_j (q_i.k_j) e^(G_i - G_j) for j <= i,  h = scale s e^G
 //   S1 = e^G_last S0 + K^T diag(w) d,    w = r e^(G_last - G)
 // T, P, f, h and w do not depend on the state: the first kernel makes them for all chunks at once.  The second goes through each
-// sequence's chunks.  q, k and v enter the products as they are; differences of G are taken in 64 bits.
+// sequence's chunks.  q, k and v enter the products as they are; differences of G are taken in 64 bits.  T, P and what they meet are
+// terms of bf16 for both types: elements of one chunk lie as far apart as its decays do, and no scale would fit all of them into fp16.
 #include "gms_kv_delta.h"
 
 namespace gms {
@@ -90,12 +91,11 @@ struct PrepSmem {
             Terms<5> inv;                // of I + A: the diagonal blocks' inverses and block (3, 2) of the inverse
             Terms<10> t;                 // the inverse times diag(beta)
             float diag[4][16][20];       // A's diagonal blocks
-            uint8_t p[sizeof(ChunkWork::tile[0])];
+            Terms<10> p;
         };
     };
     float sum[kPrepHeads][2][kChunkRows];  // G / ln 2, as the sum of two
     float b[kPrepHeads][kChunkRows], rk[kChunkRows], rq[kChunkRows];
-    float lk[kChunkRows], lq[kChunkRows], p_scale[kPrepHeads];  // f16: lengths; what P is multiplied with
 };
 
 // Byte offset of block (i, j) in a triangle, in one without its diagonal, and of 16-byte piece c (0, 1) of row r in a block.
@@ -170,7 +170,6 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
     extern __shared__ __align__(16) uint8_t raw[];
     PrepSmem<D> &m = *reinterpret_cast<PrepSmem<D> *>(raw);
     constexpr int C = kChunkRows, P = D / 8;
-    constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32, g = lane / 4, t2 = 2 * (lane & 3u);
     ptx::grid_wait();
     ptx::grid_launch_dependents();
@@ -241,10 +240,9 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
                     m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
                     m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
-                    if (kHalf) m.lk[r] = sqrtf(k2) * m.rk[r], m.lq[r] = sqrtf(q2) * m.rq[r];
                 }
     }
-    const View va = {m.a.hi, m.a.lo}, vi = {m.inv.hi, m.inv.lo}, vt = {m.t.hi, m.t.lo};
+    const View va = {m.a.hi, m.a.lo}, vi = {m.inv.hi, m.inv.lo}, vt = {m.t.hi, m.t.lo}, vp = {m.p.hi, m.p.lo};
     for (uint32_t j = 0; j < a.group; ++j) {
         ChunkWork *work = reinterpret_cast<ChunkWork *>(a.chunks + ((uint64_t)id * a.n_heads + kh * a.group + j) * sizeof(ChunkWork));
         const uint32_t jj = j % kPrepHeads;
@@ -273,19 +271,6 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     if (lane >= (uint32_t)o) inc += y;
                 }
                 const double last = __shfl_sync(0xffffffffu, inc, 31);
-                if (kHalf) {  // no element of P is above scale |q| |k| e^(sum of the gates above 0)
-                    float k = fmaxf(m.lk[2 * lane], m.lk[2 * lane + 1]), q = fmaxf(m.lq[2 * lane], m.lq[2 * lane + 1]);
-                    float up = fmaxf(raw_g[0], 0.f) + fmaxf(raw_g[1], 0.f);
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) {
-                        k = fmaxf(k, __shfl_xor_sync(0xffffffffu, k, o));
-                        q = fmaxf(q, __shfl_xor_sync(0xffffffffu, q, o));
-                        up += __shfl_xor_sync(0xffffffffu, up, o);
-                    }
-                    const float most = fabsf(a.scale) * k * q * expf(up), by = range_scale(most);
-                    if (!(most < 1e12f)) finite = __int_as_float(0x7fffffff);  // row by row
-                    if (lane == 0) m.p_scale[warp] = by, w.p_unit = flipped(by);
-                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = 2 * (int)lane + e;
@@ -307,7 +292,6 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
         }
         // A and P: rows r0 and r0 + 8, columns c0 + {0, 1} and c0 + 8 + {0, 1} of a block (something in A that is not finite comes
         // through to T)
-        const float ps = kHalf ? m.p_scale[jj] : 1.f;
         const float2 minus = make_float2(-1.f, -1.f);
         auto twice = [](float x) { return make_float2(x, x); };
 #pragma unroll
@@ -319,14 +303,13 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
             for (int e = 0; e < 2; ++e) {
                 const uint32_t r = r0 + 8 * e;
                 sh[e] = twice(m.sum[jj][0][r]), sl[e] = twice(m.sum[jj][1][r]);
-                bk[e] = twice(m.b[jj][r] * m.rk[r]), sq[e] = twice((int)r < n ? a.scale * m.rq[r] * ps : 0.f);
+                bk[e] = twice(m.b[jj][r] * m.rk[r]), sq[e] = twice((int)r < n ? a.scale * m.rq[r] : 0.f);
             }
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
                 const uint32_t c = c0 + 8 * nt;
                 const float2 ch = *reinterpret_cast<const float2 *>(&m.sum[jj][0][c]), cl = *reinterpret_cast<const float2 *>(&m.sum[jj][1][c]);
                 const float2 rc = *reinterpret_cast<const float2 *>(&m.rk[c]);
-                const uint32_t at = block_at(bi, bj) + 2 * t2;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float2 d = ptx::add2(ptx::fma2(ch, minus, sh[e]), ptx::fma2(cl, minus, sl[e]));
@@ -344,7 +327,7 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                         put_pair(va, below_at(bi, bj) + piece_in(g + 8 * e, nt) + 2 * t2, av.x, av.y);
                     }
                     finite = fmaf(pn.x, 0.f, fmaf(pn.y, 0.f, finite));
-                    *reinterpret_cast<uint32_t *>(m.p + at + piece_in(g + 8 * e, nt)) = pack2(pn.x, pn.y, T());
+                    put_pair(vp, block_at(bi, bj) + piece_in(g + 8 * e, nt) + 2 * t2, pn.x, pn.y);
                 }
             }
         }
@@ -400,11 +383,12 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
             put_block(vt, block_at(i, c), o, finite);
         }
         __syncthreads();
-        constexpr uint32_t kPieces = sizeof(m.p) / 16;
+        constexpr uint32_t kPieces = sizeof(m.p.hi) / 16;
         for (uint32_t u = tid; u < kPieces; u += kPrepThreads) {
             reinterpret_cast<uint4 *>(work->tile[0])[u] = reinterpret_cast<const uint4 *>(m.t.hi)[u];
             reinterpret_cast<uint4 *>(work->tile[1])[u] = reinterpret_cast<const uint4 *>(m.t.lo)[u];
-            reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p)[u];
+            reinterpret_cast<uint4 *>(work->tile[2])[u] = reinterpret_cast<const uint4 *>(m.p.hi)[u];
+            reinterpret_cast<uint4 *>(work->tile[3])[u] = reinterpret_cast<const uint4 *>(m.p.lo)[u];
         }
         const bool any = __syncthreads_or(finite != 0.f);
         if (tid == 0) work->by_row = any;
