@@ -617,7 +617,7 @@ int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gm
  * Sequences of more than 20 rows are done in chunks of 64 on tensor cores: products of the 16-bit inputs with S, d and decays, which
  * enter as sums of two 16-bit terms (2^-16 relative) wherever they go on into a state; for `out` the state before the chunk and the
  * weights of its rows enter as one (its error is 1.4 to 1.6 times that of its last rounding).  States and sums are kept in 32 bits.  What a row
- * does not depend on cannot reach it, whatever bits it holds.  (fp16 in chunks: states and differences d within 2^45.)
+ * does not depend on cannot reach it, whatever bits it holds.
  * src_table and dst_table may be the same (states are updated in place), and rows of src_table may be equal (several sequences go on
  * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence.  An id outside [0, n_blocks)
  * reads as zeros and is not written; GMS_DEV_HOLE in `status` tells of it.  Rows that no sequence owns, and rows of a sequence

@@ -95,6 +95,9 @@ __device__ __forceinline__ float range_scale(float top)
     return __uint_as_float((uint32_t)(127 + min(max(11 - e, -30), 30)) << 23);
 }
 
+// The largest numbers cannot be scaled so far down.
+__device__ __forceinline__ bool beyond_scale(float u) { return u <= 0x1p-30f; }
+
 // 1 / u for a power of two.
 __device__ __forceinline__ float flipped(float u) { return __uint_as_float(0x7f000000u - __float_as_uint(u)); }
 #endif

@@ -1,4 +1,6 @@
 // The gated delta rule in chunks: the chain of the states (what its operands are stands at the kernel that makes them).
+#include <cmath>
+
 #include "gms_kv_delta.h"
 
 namespace gms {
@@ -288,6 +290,7 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             }
             tell(talk.s_unit[mine], inverse(su));
         }
+        uint32_t odd = kHalf && (beyond_scale(su.x) || beyond_scale(su.y));
 #pragma unroll
         for (int k = 0; k < KQ; ++k) {
             terms(T(), S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
@@ -304,12 +307,6 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
                     mma16816(x[i][0], t ? &lo[k].x : &hi[k].x, kb[i][k][0], kb[i][k][1], T());
                     mma16816(x[i][1], t ? &lo[k].x : &hi[k].x, kb[i][k][2], kb[i][k][3], T());
                 }
-        constexpr uint32_t kOnes = kHalf ? 0x7c00u : 0x7f80u;
-        uint32_t odd = st.w.by_row;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= ((V[e] & kOnes) == kOnes) | ((V[e] >> 16 & kOnes) == kOnes);
-        odd = __any_sync(0xffffffffu, odd);
-        if (lane == 0) talk.odd[mine] = odd;
         float X[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -331,9 +328,74 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             ldmatrix_x4(smem_u32(st.w.tile[1]) + at, tb[1][kt]);
         }
         together();
+        // what the values differ by from what the state says: X <- V - f X, for the warp's rows
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+            for (int o = 0; o < 3; ++o) {
+                const float4 u = talk.sum[mine][o][nt][lane];
+                X[nt][0] += u.x, X[nt][1] += u.y, X[nt][2] += u.z, X[nt][3] += u.w;
+            }
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[row0 + 8 * nt + t2]);
+            const T *va = reinterpret_cast<const T *>(&V[2 * nt]), *vb = reinterpret_cast<const T *>(&V[2 * nt + 1]);
+            X[nt][0] = to_f32(va[0]) - f.x * X[nt][0];
+            X[nt][1] = to_f32(va[1]) - f.y * X[nt][1];
+            X[nt][2] = to_f32(vb[0]) - f.x * X[nt][2];
+            X[nt][3] = to_f32(vb[1]) - f.y * X[nt][3];
+        }
+        uint4 own_hi, own_lo;
+        terms(kWide, X[0], X[1], one, own_hi, own_lo);
+        talk.x[mine][0][lane] = own_hi, talk.x[mine][1][lane] = own_lo;
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt)
+#pragma unroll
+            for (int k = 0; k < KQ; ++k)
+                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + 2 * k + lane / 16), kb[kt][k]);
+        together();
+        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range, from the rows up to the
+        // warp's own
+        float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            if (kt > (int)mine) break;
+            const uint4 p = kt == (int)mine ? own_hi : talk.x[kt][0][lane], q = kt == (int)mine ? own_lo : talk.x[kt][1][lane];
+            mma16816(d[0], &p.x, tb[0][kt][0], tb[0][kt][1], kWide);
+            mma16816(d[1], &p.x, tb[0][kt][2], tb[0][kt][3], kWide);
+            mma16816(dl[0], &q.x, tb[0][kt][0], tb[0][kt][1], kWide);
+            mma16816(dl[1], &q.x, tb[0][kt][2], tb[0][kt][3], kWide);
+            mma16816(dt[0], &p.x, tb[1][kt][0], tb[1][kt][1], kWide);
+            mma16816(dt[1], &p.x, tb[1][kt][2], tb[1][kt][3], kWide);
+        }
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[nt][e] += dl[nt][e] + dt[nt][e];
+        float size = 0.f;  // (infinite from 2^64 on, NaN with one in d or what it was made of)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) size = fmaf(d[nt][e], d[nt][e], size);
+        terms(kWide, d[0], d[1], one, own_hi, own_lo);
+        talk.d[mine][0][lane] = own_hi, talk.d[mine][1][lane] = own_lo;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
+            d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
+        }
+        float2 u = one;
+        if (kHalf) {
+            u = scales(d[0], d[1]);
+            tell(talk.dw_unit[mine], inverse(u));
+        }
+        terms(T(), d[0], d[1], u, own_hi, own_lo);
+        talk.dw[mine][0][lane] = own_hi, talk.dw[mine][1][lane] = own_lo;
+        odd |= st.w.by_row | !(size < INFINITY) | (kHalf && (beyond_scale(u.x) || beyond_scale(u.y)));
+        odd = __any_sync(0xffffffffu, odd);
+        if (lane == 0) talk.odd[mine] = odd;
+        arrive(&m.ready[slice]);
+        together();
         if (talk.odd[0] | talk.odd[1] | talk.odd[2] | talk.odd[3]) {
-            // row by row: something here is not finite, and in a product it would reach rows that come before it
-            arrive(&m.ready[slice]);
+            // row by row, from the state as it was: something here is not finite, or far from it, and in a product would reach rows before it
             uint8_t *out = a.out + (uint64_t)(first + chunk * C) * a.o_token + h * a.o_head + (col0 + 16 * slice) * 2;
             float4(*xy)[4][32] = reinterpret_cast<float4(*)[4][32]>(talk.x);  // [2][4][32], in the place of what is not needed
             float(*zs)[4][32] = reinterpret_cast<float(*)[4][32]>(talk.dw);
@@ -384,70 +446,12 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             arrive(&m.empty[stage]);
             continue;
         }
-        // what the values differ by from what the state says: X <- V - f X, for the warp's rows
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-#pragma unroll
-            for (int o = 0; o < 3; ++o) {
-                const float4 u = talk.sum[mine][o][nt][lane];
-                X[nt][0] += u.x, X[nt][1] += u.y, X[nt][2] += u.z, X[nt][3] += u.w;
-            }
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[row0 + 8 * nt + t2]);
-            const T *va = reinterpret_cast<const T *>(&V[2 * nt]), *vb = reinterpret_cast<const T *>(&V[2 * nt + 1]);
-            X[nt][0] = to_f32(va[0]) - f.x * X[nt][0];
-            X[nt][1] = to_f32(va[1]) - f.y * X[nt][1];
-            X[nt][2] = to_f32(vb[0]) - f.x * X[nt][2];
-            X[nt][3] = to_f32(vb[1]) - f.y * X[nt][3];
-        }
-        uint4 own_hi, own_lo;
-        terms(kWide, X[0], X[1], one, own_hi, own_lo);
-        talk.x[mine][0][lane] = own_hi, talk.x[mine][1][lane] = own_lo;
-#pragma unroll
-        for (int kt = 0; kt < C / 16; ++kt)
-#pragma unroll
-            for (int k = 0; k < KQ; ++k)
-                ldmatrix_x4_trans(smem_u32(st.k) + piece<P>(16 * kt + (lane & 15u), mine * NT + 2 * k + lane / 16), kb[kt][k]);
-        together();
-        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range, from the rows up to the
-        // warp's own
-        float d[2][4] = {}, dl[2][4] = {}, dt[2][4] = {};
-#pragma unroll
-        for (int kt = 0; kt < C / 16; ++kt) {
-            if (kt > (int)mine) break;
-            const uint4 p = kt == (int)mine ? own_hi : talk.x[kt][0][lane], q = kt == (int)mine ? own_lo : talk.x[kt][1][lane];
-            mma16816(d[0], &p.x, tb[0][kt][0], tb[0][kt][1], kWide);
-            mma16816(d[1], &p.x, tb[0][kt][2], tb[0][kt][3], kWide);
-            mma16816(dl[0], &q.x, tb[0][kt][0], tb[0][kt][1], kWide);
-            mma16816(dl[1], &q.x, tb[0][kt][2], tb[0][kt][3], kWide);
-            mma16816(dt[0], &p.x, tb[1][kt][0], tb[1][kt][1], kWide);
-            mma16816(dt[1], &p.x, tb[1][kt][2], tb[1][kt][3], kWide);
-        }
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[nt][e] += dl[nt][e] + dt[nt][e];
-        terms(kWide, d[0], d[1], one, own_hi, own_lo);
-        talk.d[mine][0][lane] = own_hi, talk.d[mine][1][lane] = own_lo;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[row0 + 8 * nt + t2]);
-            d[nt][0] *= f.x, d[nt][1] *= f.y, d[nt][2] *= f.x, d[nt][3] *= f.y;
-        }
-        float2 u = one;
-        if (kHalf) {
-            u = scales(d[0], d[1]);
-            tell(talk.dw_unit[mine], inverse(u));
-        }
-        terms(T(), d[0], d[1], u, own_hi, own_lo);
-        talk.dw[mine][0][lane] = own_hi, talk.dw[mine][1][lane] = own_lo;
         // S <- e^G S + (w d) K for the warp's keys
         const float all = st.w.all;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[nt][e] *= all;
-        arrive(&m.ready[slice]);
-        together();
         float2 unit = one;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
@@ -609,7 +613,11 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
         // X = S K^T (S in two terms), Y = S Q^T (one term: it goes into `out` alone)
         float X[CT][4] = {}, Y[CT][4] = {};
         float u0 = 1.f, u1 = 1.f;
-        if (kHalf) u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
+        uint32_t odd = by_row;  // the chunk is done row by row
+        if (kHalf) {
+            u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
+            odd |= beyond_scale(u0) || beyond_scale(u1);
+        }
 #pragma unroll
         for (int kt = 0; kt < D / 16; ++kt) {
             uint32_t hi[4], lo[4], b[CT][2], c[CT][2];
@@ -635,7 +643,6 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
         }
         // what the values differ by from what the state says: X <- V - f X
         const float si0 = flipped(u0), si1 = flipped(u1);
-        float2 finite = make_float2(0.f, 0.f);
 #pragma unroll
         for (int nt = 0; nt < CT; ++nt) {
             const float2 f = *reinterpret_cast<const float2 *>(&st.w.f[8 * nt + t2]);
@@ -644,10 +651,78 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
             const float2 x0 = ptx::fma2(m0, make_float2(X[nt][0], X[nt][1]), make_float2(to_f32(va[0]), to_f32(va[1])));
             const float2 x1 = ptx::fma2(m1, make_float2(X[nt][2], X[nt][3]), make_float2(to_f32(vb[0]), to_f32(vb[1])));
             X[nt][0] = x0.x, X[nt][1] = x0.y, X[nt][2] = x1.x, X[nt][3] = x1.y;
-            finite = ptx::fma2(x0, make_float2(0.f, 0.f), ptx::fma2(x1, make_float2(0.f, 0.f), finite));
         }
-        if (__any_sync(0xffffffffu, by_row | (finite.x + finite.y != 0.f))) {
-            // row by row: something here is not finite, and in a product it would reach rows that come before it
+        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range; T's columns beyond a row's
+        // own are zero
+        float d[CT][4] = {};
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2];
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[0]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+            terms(kWide, X + 2 * kt, 1.f, 1.f, hi, lo);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], kWide);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], kWide);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[1]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                mma16816(d[nt], hi, x[0], x[1], kWide);
+                mma16816(d[nt + 1], hi, x[2], x[3], kWide);
+            }
+        }
+        float2 size = make_float2(0.f, 0.f);  // (infinite from 2^64 on, NaN with one in d or what it was made of)
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt)
+            size = ptx::fma2(make_float2(d[nt][0], d[nt][1]), make_float2(d[nt][0], d[nt][1]),
+                             ptx::fma2(make_float2(d[nt][2], d[nt][3]), make_float2(d[nt][2], d[nt][3]), size));
+        odd |= !(size.x + size.y < INFINITY);
+        // out = h Y + P d (two terms each without the product of the small ones)
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
+            times(Y[nt], kHalf ? ptx::mul2(f, make_float2(si0, si0)) : f, kHalf ? ptx::mul2(f, make_float2(si1, si1)) : f);
+        }
+#pragma unroll
+        for (int kt = 0; kt < C / 16; ++kt) {
+            uint32_t hi[4], lo[4], b[CT][2];
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
+            }
+            terms(kWide, d + 2 * kt, 1.f, 1.f, hi, lo);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], kWide);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], lo, b[nt][0], b[nt][1], kWide);
+#pragma unroll
+            for (int nt = 2 * kt; nt < CT; nt += 2) {
+                uint32_t x[4];
+                ldmatrix_x4(smem_u32(st.w.tile[3]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
+                mma16816(Y[nt], hi, x[0], x[1], kWide);
+                mma16816(Y[nt + 1], hi, x[2], x[3], kWide);
+            }
+        }
+        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
+#pragma unroll
+        for (int nt = 0; nt < CT; ++nt) {
+            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
+            times(d[nt], f, f);
+        }
+        if (kHalf) {
+            u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
+            odd |= beyond_scale(u0) || beyond_scale(u1);
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+            // row by row: something here is not finite, or far from it, and in a product would reach rows before it
 #pragma unroll 1
             for (int r = 0; r < n; ++r) {
                 const float gate = st.w.gate[r], beta = st.w.beta[r], rk = st.w.rk[r], rq = st.w.rq[r];
@@ -689,66 +764,6 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
             done();
             continue;
         }
-        // d = X T^T: two terms each (the product of the small ones left out), of bf16, which has the range; T's columns beyond a row's
-        // own are zero
-        float d[CT][4] = {};
-#pragma unroll
-        for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[CT][2];
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[0]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
-            }
-            terms(kWide, X + 2 * kt, 1.f, 1.f, hi, lo);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], hi, b[nt][0], b[nt][1], kWide);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(d[nt], lo, b[nt][0], b[nt][1], kWide);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[1]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
-                mma16816(d[nt], hi, x[0], x[1], kWide);
-                mma16816(d[nt + 1], hi, x[2], x[3], kWide);
-            }
-        }
-        // out = h Y + P d (two terms each without the product of the small ones)
-#pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[8 * nt + t2]);
-            times(Y[nt], kHalf ? ptx::mul2(f, make_float2(si0, si0)) : f, kHalf ? ptx::mul2(f, make_float2(si1, si1)) : f);
-        }
-#pragma unroll
-        for (int kt = 0; kt < C / 16; ++kt) {
-            uint32_t hi[4], lo[4], b[CT][2];
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[2]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
-                b[nt][0] = x[0], b[nt][1] = x[1], b[nt + 1][0] = x[2], b[nt + 1][1] = x[3];
-            }
-            terms(kWide, d + 2 * kt, 1.f, 1.f, hi, lo);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], hi, b[nt][0], b[nt][1], kWide);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; ++nt) mma16816(Y[nt], lo, b[nt][0], b[nt][1], kWide);
-#pragma unroll
-            for (int nt = 2 * kt; nt < CT; nt += 2) {
-                uint32_t x[4];
-                ldmatrix_x4(smem_u32(st.w.tile[3]) + block_piece(8 * nt + b_row, 2 * kt + b_piece), x);
-                mma16816(Y[nt], hi, x[0], x[1], kWide);
-                mma16816(Y[nt + 1], hi, x[2], x[3], kWide);
-            }
-        }
-        // S <- e^G S + (w d) K, w d in two terms (f16: S in units of the terms meanwhile)
-#pragma unroll
-        for (int nt = 0; nt < CT; ++nt) {
-            const float2 f = *reinterpret_cast<const float2 *>(&st.w.w[8 * nt + t2]);
-            times(d[nt], f, f);
-        }
-        if (kHalf) u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
         const float all0 = st.w.all * u0, all1 = st.w.all * u1;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) times(S[nt], make_float2(all0, all0), make_float2(all1, all1));

@@ -326,7 +326,8 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     } else {
                         put_pair(va, below_at(bi, bj) + piece_in(g + 8 * e, nt) + 2 * t2, av.x, av.y);
                     }
-                    finite = fmaf(pn.x, 0.f, fmaf(pn.y, 0.f, finite));
+                    const float2 twofold = ptx::add2(pn, pn);  // (what rounds to an infinite term counts, too)
+                    finite = fmaf(twofold.x, 0.f, fmaf(twofold.y, 0.f, finite));
                     put_pair(vp, block_at(bi, bj) + piece_in(g + 8 * e, nt) + 2 * t2, pn.x, pn.y);
                 }
             }

@@ -1,4 +1,4 @@
-"""gms_kv_delta where numbers of one chunk are far apart: gates above 0, rows much longer than others."""
+"""gms_kv_delta where numbers of one chunk are far apart: gates above 0, rows much longer than others, values near the types' ends."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -6,7 +6,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from kv_delta_harness import BF16, F16, Delta  # noqa: E402
-from kv_delta_norms import check  # noqa: E402
+from kv_delta_norms import check, expected, out_errors  # noqa: E402
 
 # head_dim, sequences of 4 heads: one slice of a state a CTA, two, a warp each
 FORMS = [(128, 1), (128, 6), (128, 12), (64, 1), (64, 12), (64, 20)]
@@ -48,3 +48,54 @@ def test_a_long_row(what, D, S, dtype):
         d.k[rows] *= 2.0 ** 10
         d.beta[rows] *= 2.0 ** -20
     check(d)
+
+
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("at", [40, 72, 79, 127])
+@pytest.mark.parametrize("what", ["value", "two values", "state"])
+def test_a_difference_beyond_the_range(what, at, D, S):
+    """A row whose difference between value and state 32 bits cannot hold: rows before it, and columns beside it, are as without it."""
+    kw = dict(lens=(130,) * S, D=D, unit=False, gates=False)
+    clean, d = Delta(6, **kw), Delta(6, **kw)
+    row, col = d.cu_h[S - 1] + at, 5
+    if what == "state":  # finite, but not its product with the row's key
+        for x in (clean, d):
+            x.place(x.raw, x.src_h, S - 1, 1)[:, col] = 2e37
+        d.k[row, 0] = 16.0
+        heads = [0, 1]  # (of the key)
+    else:
+        for x in (clean, d):
+            x.beta[row - 1:row + 1] = 2.0
+            x.k[row] = x.k[row - 1]
+        if what == "two values":
+            d.v[row - 1, 1, col] = -3e38
+        d.v[row, 1, col] = 3e38
+        heads = [1]
+    before = clean.raw.clone()
+    clean.run()
+    d.run()
+    for s, (r, out, _, size) in enumerate(expected(clean, before)):
+        stop = r.stop if s < S - 1 else row - (what == "two values")
+        part = slice(r.start, stop)
+        n = stop - r.start
+        for x in (clean, d):
+            got = x.out[part]
+            assert torch.isfinite(got.float()).all(), s
+            assert out_errors(got, out[:n], size[:n], BF16).max() <= 1, s
+    for h in range(4):
+        cols = slice(0, D) if h in heads and what == "state" else slice(col, col + 1)
+        if h in heads:
+            d.out[row - 1:, h, cols] = clean.out[row - 1:, h, cols]
+            got = d.place(d.raw, d.dst_h, S - 1, h)
+            got[:, cols] = clean.place(clean.raw, clean.dst_h, S - 1, h)[:, cols]
+    assert torch.isfinite(d.out.float()).all() and torch.isfinite(d.raw).all()
+    # (what is left of the sequence may have been computed row by row)
+    assert ((d.out.float() - clean.out.float()).abs() <= 2.0 ** -7 * clean.out.float().abs() + 0.02).all() or what == "state"
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("size", [1e9, 1e13, 1e16, 1e22])
+def test_states_far_from_one(size, D, S, dtype):
+    """Also beyond what fp16's terms can be scaled to."""
+    check(Delta(7, lens=(130,) * S, D=D, dtype=dtype, state_scale=size, scale=0.1 / size))
