@@ -78,7 +78,8 @@ struct Talk {
 template <int D, int W>
 struct RelayShape {
     static constexpr int kStages = 3;
-    static constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32, kThreads = (5 * W + kFetchWarps) * 32;
+    static constexpr uint32_t kOuts = W == 1 ? 2 : 1;  // warps of a slice that make `out`
+    static constexpr uint32_t kFetchWarps = 2, kFetchLanes = kFetchWarps * 32, kWorkers = (4 + kOuts) * W, kThreads = (kWorkers + kFetchWarps) * 32;
 };
 template <int D, int W>
 struct RelaySmem {
@@ -87,11 +88,11 @@ struct RelaySmem {
     uint64_t full[3], empty[3], ready[W], taken[W];
 };
 
-// A slice, 16 value columns of a head's state, has four warps that carry the state on and one that makes `out`.  The state lies,
+// A slice, 16 value columns of a head's state, has four warps that carry the state on and one or two that make `out`.  The state lies,
 // transposed, in accumulators of mma.sync, the columns of D / 4 keys a warp; what is an accumulator of one product is, element for
 // element, a first factor of the next: S -> X = S K^T (each warp its keys' part, for all rows) -> d = (V - f X) T^T -> S, each warp
-// 16 of the rows in between, with three exchanges through shared memory a chunk.  The fifth warp gets S and d handed and works
-// beside the next chunk.  W slices share a chunk's operands, which two more warps fetch ahead.  Bound by the latency of that
+// 16 of the rows in between, with three exchanges through shared memory a chunk.  The others get S and d handed and work beside the
+// next chunk.  W slices share a chunk's operands, which two more warps fetch ahead.  Bound by the latency of that
 // sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 275 us or 4,080 cycles a chunk (one: 3,060),
 // in which the products take 48 % of the tensor cores' cycles and loads, stores and exchanges 76 % of shared memory's.
 template <class T, int D, int W>
@@ -99,6 +100,7 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
 {
     constexpr int C = kChunkRows, P = D / 8, VP = W * 2, NT = D / 32, KQ = D / 64;  // tiles of 8 and of 16 keys that a warp has
     constexpr int kStages = RelayShape<D, W>::kStages;
+    constexpr uint32_t kOuts = RelayShape<D, W>::kOuts, kWorkers = RelayShape<D, W>::kWorkers;
     constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
     const uint32_t kh = h / a.group, col0 = part * W * 16;  // of the CTA
@@ -107,11 +109,11 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             ptx::mbar_init(smem_u32(&m.full[i]), RelayShape<D, W>::kFetchLanes);
-            ptx::mbar_init(smem_u32(&m.empty[i]), 5 * W);
+            ptx::mbar_init(smem_u32(&m.empty[i]), kWorkers);
         }
         for (int i = 0; i < W; ++i) {
             ptx::mbar_init(smem_u32(&m.ready[i]), 4);
-            ptx::mbar_init(smem_u32(&m.taken[i]), 1);
+            ptx::mbar_init(smem_u32(&m.taken[i]), kOuts);
         }
         ptx::fence_mbar_init();
     }
@@ -126,8 +128,8 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(smem_u32(bar));
     };
-    if (warp >= 5 * W) {  // the fetching warps
-        const uint32_t me = (warp - 5 * W) * 32 + lane, slot = delta_slot(a, s);
+    if (warp >= kWorkers) {  // the fetching warps
+        const uint32_t me = (warp - kWorkers) * 32 + lane, slot = delta_slot(a, s);
         for (int chunk = 0; chunk < chunks; ++chunk) {
             const int i = chunk % kStages;
             if (chunk >= kStages) wait(&m.empty[i], chunk / kStages - 1);
@@ -147,8 +149,8 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
     };
     if (warp >= 4 * W) {
         // out = h Q S + P d, with S before the chunk (one term of S, two of P and d without the product of the small ones), two tiles of
-        // 16 rows at a time
-        const uint32_t slice = warp - 4 * W;
+        // 16 rows at a time: the first and the last, then, or by another warp, those between them
+        const uint32_t slice = (warp - 4 * W) / kOuts;
         Talk<D> &talk = m.talk[slice];
 #pragma unroll 1
         for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -170,7 +172,9 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             arrive(&m.taken[slice]);
             if (!by_row) {
 #pragma unroll
-                for (int pair = 0; pair < 2; ++pair) {
+                for (uint32_t pair = 0; pair < 2 / kOuts; ++pair) {
+                    const bool inner = kOuts == 1 ? pair : warp & 1u;
+                    const int tile[2] = {inner ? 1 : 0, inner ? 2 : 3};
                     float Y[2][2][4] = {};
                     float2 unit = one;
 #pragma unroll
@@ -183,49 +187,49 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             uint32_t b[4];
-                            ldmatrix_x4(smem_u32(st.q) + piece<P>(32 * pair + 16 * i + b_row, 2 * kt + b_piece), b);
+                            ldmatrix_x4(smem_u32(st.q) + piece<P>(16 * tile[i] + b_row, 2 * kt + b_piece), b);
                             mma16816(Y[i][0], &sf[kt].x, b[0], b[1], T());
                             mma16816(Y[i][1], &sf[kt].x, b[2], b[3], T());
                         }
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int tile = 2 * pair + i;
                         if (kHalf) change(Y[i], unit, one);
 #pragma unroll
                         for (int nt = 0; nt < 2; ++nt) {
-                            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[16 * tile + 8 * nt + t2]);
+                            const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[16 * tile[i] + 8 * nt + t2]);
                             Y[i][nt][0] *= f.x, Y[i][nt][1] *= f.y, Y[i][nt][2] *= f.x, Y[i][nt][3] *= f.y;
                         }
+                    }
 #pragma unroll
-                        for (int kt = 0; kt < 4; ++kt) {
-                            if (kt > tile) break;
-                            uint32_t b[4], c[4];
-                            const uint32_t at = block_piece(16 * tile + b_row, 2 * kt + b_piece);
-                            ldmatrix_x4(smem_u32(st.w.tile[2]) + at, b);
-                            ldmatrix_x4(smem_u32(st.w.tile[3]) + at, c);
+                    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                            for (int t = 0; t < 2; ++t) {
-                                mma16816(Y[i][0], &df[kt][t].x, b[0], b[1], kWide);
-                                mma16816(Y[i][1], &df[kt][t].x, b[2], b[3], kWide);
+                        for (int i = 0; i < 2; ++i) {
+                            if (kt > tile[i]) continue;
+                            uint32_t b[2][4];
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) ldmatrix_x4(smem_u32(st.w.tile[2 + t]) + block_piece(16 * tile[i] + b_row, 2 * kt + b_piece), b[t]);
+#pragma unroll
+                            for (int t = 0; t < 3; ++t) {  // d's terms with P's first one, d's first one with P's second
+                                mma16816(Y[i][0], &df[kt][t & 1].x, b[t / 2][0], b[t / 2][1], kWide);
+                                mma16816(Y[i][1], &df[kt][t & 1].x, b[t / 2][2], b[t / 2][3], kWide);
                             }
-                            mma16816(Y[i][0], &df[kt][0].x, c[0], c[1], kWide);
-                            mma16816(Y[i][1], &df[kt][0].x, c[2], c[3], kWide);
                         }
-                        // (through the slice's part of V's tile, which the other warps have read)
+                    // (through the slice's part of V's tile, which the other warps have read)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
                         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
-                                         smem_u32(st.v) + piece<VP>(16 * tile + b_row, 2 * slice + b_piece)),
+                                         smem_u32(st.v) + piece<VP>(16 * tile[i] + b_row, 2 * slice + b_piece)),
                                      "r"(pack2(Y[i][0][0], Y[i][0][1], T())), "r"(pack2(Y[i][0][2], Y[i][0][3], T())),
                                      "r"(pack2(Y[i][1][0], Y[i][1][1], T())), "r"(pack2(Y[i][1][2], Y[i][1][3], T()))
                                      : "memory");
-                    }
-                }
-                __syncwarp();
+                    __syncwarp();
 #pragma unroll
-                for (int i = 0; i < C / 16; ++i) {
-                    const int r = 16 * i + (int)lane / 2;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
-                    if (r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
+                    for (int i = 0; i < 2; ++i) {
+                        const int r = 16 * tile[i] + (int)lane / 2;
+                        const uint4 x = *reinterpret_cast<const uint4 *>(st.v + piece<VP>(r, 2 * slice + (lane & 1u)));
+                        if (r < n) *reinterpret_cast<uint4 *>(out + (uint64_t)r * a.o_token + (lane & 1u) * 16) = x;
+                    }
                 }
             }
             arrive(&m.empty[stage]);
