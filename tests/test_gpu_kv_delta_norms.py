@@ -1,0 +1,34 @@
+"""gms_kv_delta's states and outputs by their norms (tests/kv_delta_norms.py says how far they may be off)."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from kv_delta_harness import BF16, F16, Delta  # noqa: E402
+from kv_delta_norms import check  # noqa: E402
+
+# head_dim, sequences of 4 heads: one slice of a state a CTA, two, a warp each
+FORMS = [(128, 1), (128, 6), (128, 12), (64, 1), (64, 12), (64, 20)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("n", [1, 4, 20, 21, 64, 65, 130, 500])
+def test_lengths(n, D, S, dtype):
+    if n * S > 3000:
+        S = max(3000 // n, 1)
+    check(Delta(n, lens=(n,) * S, D=D, dtype=dtype, fresh=(0,) if S > 1 else ()))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("kw", [dict(unit=False), dict(gates=False), dict(betas=False), dict(decay=0.01), dict(decay=30.0), dict(beta_scale=2.0),
+                                dict(scale=-3.0), dict(key_noise=0.3)])
+def test_forms(kw, dtype):
+    check(Delta(2, lens=(150, 1, 70), dtype=dtype, **kw))
+    check(Delta(3, lens=(100, 90) * 8, dtype=dtype, D=64, per=8, **kw))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_a_long_prompt(dtype):
+    check(Delta(4, lens=(2500,), H=2, K=1, decay=0.01, D=64, per=8, dtype=dtype))
