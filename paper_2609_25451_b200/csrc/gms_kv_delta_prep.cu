@@ -96,6 +96,7 @@ struct PrepSmem {
     };
     float sum[kPrepHeads][2][kChunkRows];  // G / ln 2, as the sum of two
     float b[kPrepHeads][kChunkRows], rk[kChunkRows], rq[kChunkRows];
+    float k2[kChunkRows];  // fp16: |k|^2
 };
 
 // Byte offset of block (i, j) in a triangle, in one without its diagonal, and of 16-byte piece c (0, 1) of row r in a block.
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
     extern __shared__ __align__(16) uint8_t raw[];
     PrepSmem<D> &m = *reinterpret_cast<PrepSmem<D> *>(raw);
     constexpr int C = kChunkRows, P = D / 8;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid / 32, g = lane / 4, t2 = 2 * (lane & 3u);
     ptx::grid_wait();
     ptx::grid_launch_dependents();
@@ -237,6 +239,7 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                 if (8 * nt + t2 + (e & 1) == g + (e & 2) * 4) {  // on the diagonal
                     const uint32_t r = 16 * warp + g + (e & 2) * 4;
                     const float k2 = kk[0][nt][e], q2 = qq[nt][e];
+                    if (kHalf) m.k2[r] = k2;
                     finite = fmaf(k2, 0.f, fmaf(q2, 0.f, finite));
                     m.rk[r] = a.unit_qk && (int)r < n ? rsqrtf(k2 + a.unit_eps) : 1.f;
                     m.rq[r] = a.unit_qk && (int)r < n ? rsqrtf(q2 + a.unit_eps) : 1.f;
@@ -271,6 +274,20 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     if (lane >= (uint32_t)o) inc += y;
                 }
                 const double last = __shfl_sync(0xffffffffu, inc, 31);
+                // fp16: terms of w d have one scale for many rows, so an error of 2^-37 of the largest of them, which meets the longest key
+                // where the shortest is the largest's own.  Keys more than 2^18 apart go row by row; those of zero, whose w may be any
+                // size, add nothing
+                float2 k2 = make_float2(1.f, 1.f);
+                if (kHalf) {
+                    k2 = *reinterpret_cast<const float2 *>(&m.k2[2 * lane]);
+                    float most = fmaxf(k2.x, k2.y), least = fminf(k2.x > 0.f ? k2.x : kHuge, k2.y > 0.f ? k2.y : kHuge);
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) {
+                        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+                    }
+                    if (most * 0x1p-36f > least) finite = __int_as_float(0x7fffffff);
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = 2 * (int)lane + e;
@@ -279,7 +296,7 @@ __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __
                     m.sum[warp][0][r] = (float)sum, m.sum[warp][1][r] = (float)(sum - (double)(float)sum);
                     m.b[warp][r] = beta[e];
                     const float gate = exp2f((float)sum), f = in ? m.rk[r] * gate : 0.f, hh = in ? a.scale * m.rq[r] * gate : 0.f,
-                                ww = in ? m.rk[r] * exp2f((float)(last - sum)) : 0.f;
+                                ww = in && (e ? k2.y : k2.x) > 0.f ? m.rk[r] * exp2f((float)(last - sum)) : 0.f;
                     w.f[r] = f, w.h[r] = hh, w.w[r] = ww;
                     w.gate[r] = expf(raw_g[e]), w.beta[r] = beta[e], w.rk[r] = m.rk[r], w.rq[r] = m.rq[r];
                     finite = fmaf(f, 0.f, fmaf(hh, 0.f, fmaf(ww, 0.f, finite)));

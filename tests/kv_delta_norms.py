@@ -6,6 +6,9 @@ How far they may be off:
          either sign); one term instead (2^-9 for bf16, 2^-12 for fp16 at the least) is 2e-4 to 4e-3.
   out:   its last rounding is off by at most u of each element (2^-8, fp16 2^-11), so by u of a block's norm; what an error of the
          state allows comes to it: 3e-5 |scale| |q_i| |S_i| of each row (Frobenius norms); fp16: 2^-25 an element below its normal range.
+         In chunks the state before the chunk, S_0, enters an output as one 16-bit term: each element off by u of itself at most, so
+         a column's part scale e^G q^T S_0 by u |scale| e^G |q|^T |S_0|, element for element.  Where that part does not cancel, this
+         is within what the last rounding is allowed above its average; where it may, `one_term` adds it.
 """
 from __future__ import annotations
 
@@ -20,16 +23,21 @@ BLOCK = 16
 
 def rule(q, k, v, g, beta, S, scale):
     """Row by row in 64 bits.  q, k, v [rows, heads, dim], g, beta [rows, heads], S [heads, key, value]: outputs, state, and what
-    each row's output is measured by (|scale| |q| |S|), all in 64 bits."""
+    each row's output is measured by, all in 64 bits: |scale| |q| |S|, and the norm of |scale| e^G |q|^T |S_0| with S_0 the state before
+    the row's 64 (0 where a sequence has no more than 20 rows, which are not done in chunks)."""
     q, k, v, g, beta, S = (x.double() for x in (q, k, v, g, beta, S))
-    out, size = torch.zeros_like(v), torch.zeros(v.shape[:2], dtype=torch.float64, device=v.device)
+    out, size = torch.zeros_like(v), torch.zeros(v.shape[:2] + (2,), dtype=torch.float64, device=v.device)
     gate = g.exp()
     for t in range(v.shape[0]):
+        if t % 64 == 0:
+            start = S.abs() if v.shape[0] > 20 else torch.zeros_like(S)
+        start = start * gate[t][:, None, None]
         S = S * gate[t][:, None, None]
         d = beta[t][:, None] * (v[t] - torch.einsum("hkv,hk->hv", S, k[t]))
         S = S + k[t][:, :, None] * d[:, None, :]
         out[t] = scale * torch.einsum("hkv,hk->hv", S, q[t])
-        size[t] = abs(scale) * q[t].norm(dim=-1) * S.flatten(1).norm(dim=1)
+        size[t, :, 0] = abs(scale) * q[t].norm(dim=-1) * S.flatten(1).norm(dim=1)
+        size[t, :, 1] = abs(scale) * torch.einsum("hkv,hk->hv", start, q[t].abs()).norm(dim=1)
     return out, S, size
 
 
@@ -43,7 +51,7 @@ def state_errors(got, want):
     return (got.double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1).clamp(min=1e-300)
 
 
-def out_errors(got, want, size, dtype):
+def out_errors(got, want, size, dtype, one_term=False):
     """Errors of outputs [rows, heads, dim] over what they may be, a block of rows and head each."""
     n, H, D = want.shape
     pad = -n % BLOCK
@@ -52,7 +60,7 @@ def out_errors(got, want, size, dtype):
         x = torch.cat([x, torch.zeros((pad, H, x.shape[2]), dtype=torch.float64, device=x.device)])
         return x.reshape(-1, BLOCK, H, x.shape[2]).transpose(1, 2).flatten(2).norm(dim=2)
 
-    may = U[dtype] * blocks(want) + STATE * blocks(size[:, :, None])
+    may = U[dtype] * blocks(want) + STATE * blocks(size[:, :, :1]) + (U[dtype] * blocks(size[:, :, 1:]) if one_term else 0)
     if dtype == torch.float16:
         may = may + 2.0 ** -25 * math.sqrt(BLOCK * D)
     return blocks(got.double() - want) / may.clamp(min=1e-300)
@@ -76,7 +84,7 @@ def expected(d, raw):
     return res
 
 
-def check(d, run=True):
+def check(d, run=True, one_term=False):
     """Runs a problem (without holes) and holds its outputs and states to the limits; returns the largest errors, over the limits."""
     before = d.raw.clone()
     if run:
@@ -88,7 +96,7 @@ def check(d, run=True):
         assert torch.isfinite(got).all() and errs.max() <= 1, ("state", s, errs.tolist())
         worst[0] = max(worst[0], float(errs.max()))
         if out.shape[0]:
-            errs = out_errors(d.out[r], out, size, d.dtype)
+            errs = out_errors(d.out[r], out, size, d.dtype, one_term)
             assert torch.isfinite(d.out[r].float()).all() and errs.max() <= 1, ("out", s, errs.max(), errs.argmax())
             worst[1] = max(worst[1], float(errs.max()))
     return worst

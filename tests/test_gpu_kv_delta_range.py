@@ -1,4 +1,4 @@
-"""gms_kv_delta where numbers of one chunk are far apart: gates above 0, rows much longer than others, values near the types' ends."""
+"""gms_kv_delta where numbers of one chunk are far apart: gates above 0, rows and keys of very different lengths, values near the types' ends."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -48,6 +48,27 @@ def test_a_long_row(what, D, S, dtype):
         d.k[rows] *= 2.0 ** 10
         d.beta[rows] *= 2.0 ** -20
     check(d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("apart", [16, 20, 26])
+def test_keys_of_many_lengths(apart, D, S, dtype):
+    """Keys that are brought to unit length, from 2^-12 of it on."""
+    d = Delta(4, lens=(130,) * S, D=D, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(apart)
+    d.k.mul_(torch.exp2(-12 + apart * torch.rand((d.T, d.K, 1), device="cuda", generator=g)))
+    check(d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+def test_keys_of_zero(D, S, dtype):
+    d = Delta(5, lens=(130,) * S, D=D, dtype=dtype)
+    d.eps = 1e-12
+    d.k[3::5] = 0
+    d.make()
+    check(d, one_term=True)  # (a row without a key has nothing but the state's part, which its query may all but miss)
 
 
 @pytest.mark.parametrize("D,S", FORMS)
