@@ -619,8 +619,9 @@ int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gm
  * weights of its rows enter as one (its error is 1.4 to 1.6 times that of its last rounding).  States and sums are kept in 32 bits.  What a row
  * does not depend on cannot reach it, whatever bits it holds.
  * src_table and dst_table may be the same (states are updated in place), and rows of src_table may be equal (several sequences go on
- * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence.  An id outside [0, n_blocks)
- * reads as zeros and is not written; GMS_DEV_HOLE in `status` tells of it.  Rows that no sequence owns, and rows of a sequence
+ * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence or stand at another place of
+ * its own sequence's source row (heads are done in no order: a state that is still to be read would be overwritten).  An id outside
+ * [0, n_blocks) reads as zeros and is not written; GMS_DEV_HOLE in `status` tells of it.  Rows that no sequence owns, and rows of a sequence
  * beyond its first max_q, are not processed and leave `out` as it is.
  * gms_kv_delta_workspace: bytes for this call and every later one with no larger n_seq, total_q and max_q and the same heads.
  * Errors: NULL, ALIGN, ARG, RANGE, CUDA.
