@@ -149,7 +149,11 @@ class KvDeltaArgs(C.Structure):
                 (n, C.c_uint32) for n in ("n_seq", "n_key_heads", "total_q", "max_q", "dtype", "unit_qk")] + [
                 ("unit_eps", C.c_float), ("scale", C.c_float)]
 
-    set_workspace = KvAttn.set_workspace
+    def set_workspace(self, t):
+        """Hands over a uint8 device tensor of at least gms_kv_delta_workspace bytes, where the other tensors are."""
+        if self._device is not None and t.is_cuda and t.device.index != self._device:
+            raise ValueError(f"tensors are on device {self._device}, the workspace is on device {t.device.index}")
+        KvAttn.set_workspace(self, t)
 
 
 _lib = None
@@ -689,7 +693,8 @@ def kv_delta_args(*, q, k, v, out, src_table, dst_table=None, g=None, beta=None,
                   unit_eps=None, workspace=None, status=None) -> KvDeltaArgs:
     """gms_kv_delta_args from tensors: ``q`` and ``k`` [rows, key heads, dim], ``v`` and ``out`` [rows, heads, dim] with any strides and
     a contiguous last dimension, ``g`` and ``beta`` float32 [rows, heads], tables int32 [sequences, blocks] (``dst_table`` None: in
-    place; else its blocks are no source blocks, but for one in the same place of the same row), ``unit_eps`` None: q and k as they are.  The result keeps the tensors alive."""
+    place; else its blocks are no source blocks, but for one in the same place of the same row), ``unit_eps`` None: q and k as they
+    are.  The result keeps the tensors alive."""
     dst_table = src_table if dst_table is None else dst_table
     dtype, rows, dim = _heads_dim("q, k, v and out are 16-bit [rows, heads, dim] of one type", (q, k, v, out))
     if q.shape != k.shape or v.shape != out.shape or any(t is not None and tuple(t.shape) != tuple(v.shape[:2]) for t in (g, beta)):
