@@ -666,6 +666,8 @@ def kv_append_args(*, slots=None, q=None, k=None, v=None, q_out=None, positions=
     if weight_dtype is None:
         raise ValueError("weights are bfloat16, float16 or float32")
     _int32(n_rows)
+    if n_rows is not None and n_rows.numel() == 0:
+        raise ValueError("n_rows is a word")
     (qt, qh), (kt, kh), (vt, vh), (ot, oh) = (_strides(t) for t in (q, k, v, q_out))
     two = positions is not None and positions.dim() == 2
     a = KvAppendArgs(q=_dev(q), k=_dev(k), v=_dev(v), q_out=_dev(q_out), slots=_dev(slots), positions=_dev(positions), n_rows=_dev(n_rows),

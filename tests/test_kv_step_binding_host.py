@@ -27,6 +27,11 @@ def delta(**kw):
     return gms.kv_delta_args(**{**dict(q=gpu(5, 2, 64, **x), k=gpu(5, 2, 64, **x), v=gpu(5, 4, 64, **x), out=gpu(5, 4, 64, **x), src_table=gpu(3, 2), scale=1.0), **kw})
 
 
+def append(**kw):
+    x = dict(dtype=torch.bfloat16)
+    return gms.kv_append_args(**{**dict(q=gpu(5, 4, 64, **x), k=gpu(5, 2, 64, **x), v=gpu(5, 2, 64, **x), slots=gpu(5, dtype=torch.int64)), **kw})
+
+
 def test_a_workspace_on_another_device_is_refused():
     here, there = gpu(1024, dtype=torch.uint8), gpu(1024, dtype=torch.uint8, index=1)
     a = delta(workspace=here)
@@ -41,3 +46,12 @@ def test_a_workspace_on_another_device_is_refused():
     byhand = gms.KvDeltaArgs()  # (of no tensors: any device)
     byhand.set_workspace(there)
     assert byhand.workspace == there.data_ptr()
+
+
+def test_a_number_of_rows_is_a_word():
+    """An empty tensor has no address, which would stand for every row."""
+    cu = gpu(4)
+    assert append(n_rows=OnGpu(cu.t[3:])).n_rows == cu.t[3:].data_ptr()
+    assert append().n_rows is None
+    with pytest.raises(ValueError, match="n_rows"):
+        append(n_rows=OnGpu(cu.t[4:]))
