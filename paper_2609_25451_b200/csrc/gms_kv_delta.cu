@@ -381,10 +381,17 @@ int make_delta(const gms_kv_pool *pool, const gms_kv_state *state, const gms_kv_
     return GMS_OK;
 }
 
-// Slots for every sequence's chunks, wherever its rows begin; 0: no sequence is long enough.
-uint64_t chunk_slots(const DeltaArgs &a) { return a.max_q > kMostByRow ? a.total_q / kChunkRows + a.n_seq : 0; }
+// Slots for every sequence's chunks, wherever its rows begin; 0: no sequence is long enough.  The smaller one of two numbers, each of
+// which grows with the call: 255 single rows beside a prompt of 2,048, 32 heads, take 79 MB so, with a slot for each of them 210.
+uint64_t chunk_slots(DeltaArgs &a)
+{
+    if (a.max_q <= kMostByRow) return 0;
+    const uint64_t each = (uint64_t)a.total_q / kChunkRows + a.n_seq, by_begin = a.total_q / (kMostByRow + 1) + 1;
+    a.by_begin = by_begin < each;
+    return by_begin < each ? by_begin : each;
+}
 // They and the order of the sequences.
-uint64_t work_bytes(const DeltaArgs &a)
+uint64_t work_bytes(DeltaArgs &a)
 {
     const uint64_t slots = chunk_slots(a);
     return slots ? slots * a.n_heads * sizeof(ChunkWork) + ((uint64_t)a.n_seq * 4 + 255) / 256 * 256 : 0;

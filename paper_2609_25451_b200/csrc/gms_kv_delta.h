@@ -19,7 +19,7 @@ struct DeltaArgs {
     uint32_t total_q, max_q, unit_qk;
     float unit_eps, scale;
     uint8_t *chunks;                     // workspace: ChunkWork [n_slots][n_heads]; null: no sequence is done in chunks
-    uint32_t n_slots;
+    uint32_t n_slots, by_begin;
     uint32_t *order;                     // workspace: the sequences done in chunks, longest first, then kNone
 };
 
@@ -48,8 +48,13 @@ __device__ __forceinline__ int delta_rows(const DeltaArgs &a, uint32_t s)
     return min(max(min(a.cu_q[s + 1], (int)a.total_q) - delta_begin(a, s), 0), (int)a.max_q);
 }
 __device__ __forceinline__ bool delta_in_chunks(const DeltaArgs &a, int rows) { return a.chunks && rows > (int)kMostByRow; }
-// First slot of a sequence in the workspace.  A sequence of n rows has n / 64 + 1 slots at least, whatever comes before it.
-__device__ __forceinline__ uint32_t delta_slot(const DeltaArgs &a, uint32_t s) { return (uint32_t)delta_begin(a, s) / kChunkRows + s; }
+// First slot of a sequence in the workspace.  A sequence of n rows has n / 64 + 1 slots at least, whatever comes before it; or, where
+// many are short, n / 21 if it is done in chunks (no fewer than its chunks, and sequences that are not may have none).
+__device__ __forceinline__ uint32_t delta_slot(const DeltaArgs &a, uint32_t s)
+{
+    const uint32_t begin = (uint32_t)delta_begin(a, s);
+    return a.by_begin ? begin / (kMostByRow + 1) : begin / kChunkRows + s;
+}
 // Where a head's state lies; null: in a hole.
 template <int D>
 __device__ __forceinline__ float *delta_state(const DeltaArgs &a, const int32_t *table, uint64_t stride, uint32_t s, uint32_t h)
