@@ -93,15 +93,17 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t 
 }
 
 // A power of two by which a row of f16 terms is scaled so that its largest is below 2^12 (bf16 has the range of 32 bits); within
-// 2^-30 .. 2^30, so that three such factors together stay far from the ends of 32 bits.
+// 2^-30 .. 2^74.  (A state may have decayed far below what a later gate above 0 brings it back to.)
 __device__ __forceinline__ float range_scale(float top)
 {
     const int e = (int)(__float_as_uint(top) >> 23 & 255u) - 127;  // 2^e <= top
-    return __uint_as_float((uint32_t)(127 + min(max(11 - e, -30), 30)) << 23);
+    return __uint_as_float((uint32_t)(127 + min(max(11 - e, -30), 74)) << 23);
 }
 
-// The largest numbers cannot be scaled so far down.
+// What the largest numbers are not scaled down to: differences from 2^41 on; states from 2^25 on, so that what part of one gives an
+// output (terms below 2^12, queries below 2^16, 128 of each) may go over to another part's unit: 2^35 2^14 2^74 < 2^127.
 __device__ __forceinline__ bool beyond_scale(float u) { return u <= 0x1p-30f; }
+__device__ __forceinline__ bool state_beyond_scale(float u) { return u <= 0x1p-14f; }
 
 // 1 / u for a power of two.
 __device__ __forceinline__ float flipped(float u) { return __uint_as_float(0x7f000000u - __float_as_uint(u)); }

@@ -147,6 +147,14 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) x[nt][0] *= f0, x[nt][1] *= f0, x[nt][2] *= f1, x[nt][3] *= f1;
     };
+    // or, in a unit of their own, are added to others (units may lie too far apart for both)
+    auto add_in = [](float(*x)[4], const float(*part)[4], float2 unit) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            x[nt][0] = fmaf(part[nt][0], unit.x, x[nt][0]), x[nt][1] = fmaf(part[nt][1], unit.x, x[nt][1]);
+            x[nt][2] = fmaf(part[nt][2], unit.y, x[nt][2]), x[nt][3] = fmaf(part[nt][3], unit.y, x[nt][3]);
+        }
+    };
     if (warp >= 4 * W) {
         // out = h Q S + P d, with S before the chunk (one term of S, two of P and d without the product of the small ones), two tiles of
         // 16 rows at a time: the first and the last, then, or by another warp, those between them
@@ -192,9 +200,9 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
                             mma16816(Y[i][1], &sf[kt].x, b[2], b[3], T());
                         }
                     }
+                    if (kHalf) change(Y[0], unit, one), change(Y[1], unit, one);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        if (kHalf) change(Y[i], unit, one);
 #pragma unroll
                         for (int nt = 0; nt < 2; ++nt) {
                             const float2 f = *reinterpret_cast<const float2 *>(&st.w.h[16 * tile[i] + 8 * nt + t2]);
@@ -294,7 +302,7 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
             }
             tell(talk.s_unit[mine], inverse(su));
         }
-        uint32_t odd = kHalf && (beyond_scale(su.x) || beyond_scale(su.y));
+        uint32_t odd = kHalf && (state_beyond_scale(su.x) || state_beyond_scale(su.y));
 #pragma unroll
         for (int k = 0; k < KQ; ++k) {
             terms(T(), S[2 * k], S[2 * k + 1], su, hi[k], lo[k]);
@@ -314,7 +322,11 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
         float X[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (kHalf) change(x[i], inverse(su), one);
+            if (kHalf) {
+                const float2 u = inverse(su);
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) x[i][nt][0] *= u.x, x[i][nt][1] *= u.x, x[i][nt][2] *= u.y, x[i][nt][3] *= u.y;
+            }
             if (i == (int)mine) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) X[0][e] = x[i][0][e], X[1][e] = x[i][1][e];
@@ -456,24 +468,20 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[nt][e] *= all;
-        float2 unit = one;
 #pragma unroll
         for (int kt = 0; kt < C / 16; ++kt) {
-            if (kHalf) {
-                const float2 next = talk.dw_unit[kt][g];
-#pragma unroll
-                for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, next);
-                unit = next;
-            }
             const uint4 p = kt == (int)mine ? own_hi : talk.dw[kt][0][lane], q = kt == (int)mine ? own_lo : talk.dw[kt][1][lane];
+            float part[NT][4] = {};
+            float(*to)[4] = kHalf ? part : S;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma16816(S[nt], t ? &q.x : &p.x, kb[kt][nt / 2][2 * (nt & 1)], kb[kt][nt / 2][2 * (nt & 1) + 1], T());
-        }
-        if (kHalf) {
+                for (int nt = 0; nt < NT; ++nt) mma16816(to[nt], t ? &q.x : &p.x, kb[kt][nt / 2][2 * (nt & 1)], kb[kt][nt / 2][2 * (nt & 1) + 1], T());
+            if (kHalf) {
+                const float2 unit = talk.dw_unit[kt][g];
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) change(S + nt, unit, one);
+                for (int nt = 0; nt < NT; nt += 2) add_in(S + nt, part + nt, unit);
+            }
         }
         arrive(&m.empty[stage]);
     }
@@ -580,12 +588,12 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
         x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
     };
     // f16: rows (e = 0, 1: g and g + 8) are scaled by powers of two of their own before they are rounded
-    auto scale_of = [](const float(*x)[4], int tiles, int e) {
+    auto top_of = [](const float(*x)[4], int tiles, int e) {
         float top = 0.f;
 #pragma unroll
         for (int nt = 0; nt < tiles; ++nt) top = fmaxf(top, fmaxf(fabsf(x[nt][2 * e]), fabsf(x[nt][2 * e + 1])));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        return range_scale(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)));
+        return fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     };
     auto terms = [](auto type, const float(*x)[4], float u0, float u1, uint32_t *hi, uint32_t *lo) {  // of the 16 x 16 in accumulators x[0] and x[1]
         using Term = decltype(type);
@@ -619,8 +627,8 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
         float u0 = 1.f, u1 = 1.f;
         uint32_t odd = by_row;  // the chunk is done row by row
         if (kHalf) {
-            u0 = scale_of(S, NT, 0), u1 = scale_of(S, NT, 1);
-            odd |= beyond_scale(u0) || beyond_scale(u1);
+            u0 = range_scale(top_of(S, NT, 0)), u1 = range_scale(top_of(S, NT, 1));
+            odd |= state_beyond_scale(u0) || state_beyond_scale(u1);
         }
 #pragma unroll
         for (int kt = 0; kt < D / 16; ++kt) {
@@ -722,7 +730,8 @@ __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint
             times(d[nt], f, f);
         }
         if (kHalf) {
-            u0 = scale_of(d, CT, 0), u1 = scale_of(d, CT, 1);
+            // (the state's part, below 2^12 all / its own scale, may be up to 2^20 larger in that unit)
+            u0 = range_scale(fmaxf(top_of(d, CT, 0), st.w.all * si0 * 0x1p-8f)), u1 = range_scale(fmaxf(top_of(d, CT, 1), st.w.all * si1 * 0x1p-8f));
             odd |= beyond_scale(u0) || beyond_scale(u1);
         }
         if (__any_sync(0xffffffffu, odd)) {

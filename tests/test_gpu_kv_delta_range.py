@@ -120,3 +120,40 @@ def test_a_difference_beyond_the_range(what, at, D, S):
 def test_states_far_from_one(size, D, S, dtype):
     """Also beyond what fp16's terms can be scaled to."""
     check(Delta(7, lens=(130,) * S, D=D, dtype=dtype, state_scale=size, scale=0.1 / size))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("up", [12.0, 20.0, 30.0, 40.0, 55.0])
+def test_a_gate_above_zero_in_the_next_chunk(up, D, S, dtype):
+    """The state between the two chunks is e^-up of what it was and becomes."""
+    d = Delta(8, lens=(150,) * S, D=D, dtype=dtype)
+    for s in range(S):
+        r = d.cu_h[s] + (63 if s % 2 == 0 else 127)
+        d.g[r], d.g[r + 1] = -up, up
+        d.beta[r] = 0
+    check(d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+@pytest.mark.parametrize("size", [1e-6, 1e-12, 1e-20])
+def test_states_near_zero(size, D, S, dtype):
+    """Values of zero: nothing else is in them.  (Gates that leave e^-2 of a state: full decay, e^-60, ends where 32 bits do, 2^-126, or
+    where the second of two bf16 terms does, 2^-109.)"""
+    d = Delta(9, lens=(150,) * S, D=D, dtype=dtype, state_scale=size, scale=0.1 / size, decay=0.03)
+    d.v.zero_()
+    check(d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,S", FORMS)
+def test_states_of_zero_under_a_gate_above_zero(D, S, dtype):
+    d = Delta(10, lens=(70,) * S, D=D, dtype=dtype, fresh=tuple(range(S)))
+    d.v.zero_()
+    d.g[20] = 75.0
+    d.run()
+    assert (d.out == 0).all()
+    for s in range(S):
+        for h in range(4):
+            assert (d.place(d.raw, d.dst_h, s, h) == 0).all()
