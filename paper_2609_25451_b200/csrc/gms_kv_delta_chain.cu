@@ -86,6 +86,7 @@ struct RelaySmem {
     Stage<D, W> stage[3];
     Talk<D> talk[W];
     uint64_t full[3], empty[3], ready[W], taken[W];
+    uint32_t nth;  // of the items that a CTA goes through (no register is free for it)
 };
 
 // A slice, 16 value columns of a head's state, has four warps that carry the state on and one or two that make `out`.  The state lies,
@@ -505,7 +506,14 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
     bool late = false;  // a wait has run out
     ptx::grid_launch_dependents();
     ptx::grid_wait();
-    for (uint32_t item = blockIdx.x; item < a.n_seq * a.n_heads * kParts; item += gridDim.x) {
+    volatile uint32_t &nth = m.nth;
+    if (AGAIN) {
+        if (threadIdx.x == 0) nth = 0;
+        __syncthreads();
+    }
+    for (;;) {
+        const uint32_t item = blockIdx.x + (AGAIN ? nth * gridDim.x : 0);
+        if (item >= a.n_seq * a.n_heads * kParts) return;
         const uint32_t s = a.order[item / kParts / a.n_heads];
         if (s >= a.n_seq) return;
         relay<T, D, W>(a, m, s, item / kParts % a.n_heads, item % kParts, late);
@@ -514,7 +522,9 @@ __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_ker
         if (threadIdx.x == 0) {  // (made anew for the next item)
             for (int i = 0; i < RelayShape<D, W>::kStages; ++i) ptx::mbar_inval(smem_u32(&m.full[i])), ptx::mbar_inval(smem_u32(&m.empty[i]));
             for (int i = 0; i < W; ++i) ptx::mbar_inval(smem_u32(&m.ready[i])), ptx::mbar_inval(smem_u32(&m.taken[i]));
+            nth = nth + 1;
         }
+        __syncthreads();
     }
 }
 
