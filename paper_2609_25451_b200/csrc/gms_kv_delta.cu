@@ -302,7 +302,7 @@ cudaError_t launch_rows(const DeltaArgs &a, cudaStream_t s)
     // Whole states pay from one and a half a CTA on: below that SMs stand idle or have two rounds to do (32 heads of 128, one row, us,
     // slices / whole states: 5 sequences 12.3 / 14.3, 8 14.3 / 14.3, 24 28.7 / 26.6; four rows: 5 16.4 / 16.4, 8 20.5 / 18.4, 24 43 / 35).
     // Beside the chunk kernels small CTAs fill up better, up to eight times as many states (the whole call, a long prompt and single
-    // rows: 32 sequences 329 / 329, 64 237 / 222; 44 sequences of 9 to 51 rows, 24 heads 132 / 140).
+    // rows: 32 sequences 340 / 336, 64 233 / 235; 44 sequences of 9 to 51 rows, 24 heads 137 / 147).
     constexpr int W = 32;
     const uint64_t items = (uint64_t)a.n_seq * a.n_heads, held = 148 * StreamShape<D>::kCtas;
     if (2 * items <= (a.chunks ? 16 : 3) * held) return launch_dependent(kv_delta_rows_kernel<T, D, W>, (uint32_t)items * (D / W), kRowThreads, 0, s, a);

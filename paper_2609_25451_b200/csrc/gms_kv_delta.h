@@ -24,7 +24,8 @@ struct DeltaArgs {
 };
 
 // Sequences of more rows than kMostByRow are done kChunkRows at a time (us, in chunks / row by row, 32 heads of 128, bf16: 1 sequence of
-// 20 rows 20.5 / 20.5, of 24 20.5 / 22.5; 8 of 16 41 / 33, of 20 43 / 39, of 24 43 / 43, of 32 43 / 53; 32 of 20 119 / 115, of 24 119 / 131).
+// 20 rows 21.5 / 20.5, of 24 21.5 / 22.5; 8 of 16 46 / 34, of 20 47 / 40, of 24 47 / 44, of 32 48 / 55; 32 of 20 128 / 117, of 24 129 / 131; 44 of
+// 9 to 51 rows, 24 heads, in chunks from 21 rows on 138, from 25 on 157).
 constexpr uint32_t kChunkRows = 64, kMostByRow = 20, kNone = 0xffffffffu;
 
 // What the first of the two chunk kernels leaves for the second.

@@ -93,9 +93,12 @@ struct RelaySmem {
 // transposed, in accumulators of mma.sync, the columns of D / 4 keys a warp; what is an accumulator of one product is, element for
 // element, a first factor of the next: S -> X = S K^T (each warp its keys' part, for all rows) -> d = (V - f X) T^T -> S, each warp
 // 16 of the rows in between, with three exchanges through shared memory a chunk.  The others get S and d handed and work beside the
-// next chunk.  W slices share a chunk's operands, which two more warps fetch ahead.  Bound by the latency of that
-// sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 275 us or 4,080 cycles a chunk (one: 3,060),
-// in which the products take 48 % of the tensor cores' cycles and loads, stores and exchanges 76 % of shared memory's.
+// next chunk: of two slices one each, which leaves 168 registers a thread (two each, of 14 warps, 128); of one slice two, which one
+// alone would hold up (8,192 rows of 4 heads of 128 235 us, so 243).  W slices share a chunk's operands, which two more warps fetch
+// ahead.  Bound by the latency of that sequence of small products and exchanges: 8,192 rows of 32 heads of 128, two slices a CTA, 280 us
+// or 4,060 cycles a chunk (one: 3,190), in which the products take 45 % of the tensor cores' cycles and loads, stores and exchanges
+// 69 % of shared memory's.  `out` could have S in two terms, too: 64 products a slice and chunk more, on the warp that has most, and
+// 386 us instead of 335 for that call (one slice a CTA 241 instead of 233), for an error of 1.65 instead of 1.78 thousandths in bf16.
 template <class T, int D, int W>
 __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part, bool &late)
 {
@@ -495,7 +498,7 @@ __device__ __forceinline__ void relay(const DeltaArgs &a, RelaySmem<D, W> &m, ui
 
 // Most items of a batch in which few sequences are long are none: they come last.  Where there are many for each SM, CTAs go through
 // several (AGAIN) instead of being started for each (us, one CTA an item / so: a prompt of 2,048 rows among 255 single rows, 32 heads of
-// 128 368 / 284, of 64 214 / 140; of 4,096 among 95 259 / 245; of 8,192 among 31, 4,096 items, 329 / 341, as the loop costs registers).
+// 128 368 / 296, of 64 212 / 144; of 4,096 among 95 265 / 257; of 8,192 among 31, 4,096 items, 337 / 364, as the loop costs registers).
 constexpr uint32_t kMany = 148 * 32;
 template <class T, int D, int W, bool AGAIN>
 __global__ void __launch_bounds__(RelayShape<D, W>::kThreads) kv_delta_relay_kernel(const __grid_constant__ DeltaArgs a)
@@ -545,8 +548,9 @@ struct SoloSmem {
 // A warp has 16 value columns of a head's state, transposed, as accumulators of mma.sync (16 x D): what is an accumulator of one
 // product is, element for element, a first factor of the next, S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out, so nothing
 // leaves the registers between the products and no warp waits for another.  W of them (16 W columns of a head) share a chunk's
-// operands, which further warps fetch ahead.  Bound by the rate of the products, 420 of them a chunk and warp at 128 keys, 8.3 cycles
-// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,600 cycles a chunk (64 keys: 264, 4,250).
+// operands, which further warps fetch ahead.  Bound by the rate of the products, 440 of them a chunk and warp at 128 keys, 8.3 cycles
+// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,800 cycles a chunk (64 keys: 280, two CTAs an SM side by
+// side, 7,600).
 template <class T, int D, int W>
 __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part, bool &late)
 {
@@ -845,7 +849,7 @@ __global__ void __launch_bounds__(SoloShape<D, W>::kThreads, SoloShape<D, W>::kC
     SoloSmem<D, W> &m = *reinterpret_cast<SoloSmem<D, W> *>(raw);
     constexpr uint32_t kParts = D / (16 * W);
     // Where some SMs have a second CTA from the start, they are those of the first CTAs, which therefore take the shorter sequences of
-    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, f16: 154.6 us without, 146.4 us).
+    // the first 148 (13 sequences of up to 2,001 rows, 16 heads of 64, us without / with: f16 154.7 / 146.5, bf16 150.5 / 142.4).
     constexpr uint32_t kSms = 148;
     const bool turned = SoloShape<D, W>::kCtas == 2 && gridDim.x > kSms && gridDim.x <= 2 * kSms && blockIdx.x < kSms;
     bool late = false;  // a wait has run out
@@ -892,7 +896,7 @@ cudaError_t launch_solo(const DeltaArgs &a, uint32_t ctas, cudaStream_t s)
     const uint32_t threads = SoloShape<D, W>::kThreads, smem = sizeof(SoloSmem<D, W>);
     if (SoloShape<D, W>::kCtas == 1) return launch_dependent(kv_delta_solo_kernel<T, D, W, AGAIN>, ctas, threads, smem, s, a);
     // Two an SM: they start when the kernel ahead has ended, or the first two, the longest, come to share the first SM that is free
-    // (13 sequences of up to 2,001 rows, 16 heads of 64: 167 us so, 136 us waiting; fp16 177 and 146 us).
+    // (13 sequences of up to 2,001 rows, 16 heads of 64: 179 us so, 142 us waiting; fp16 185 and 146 us).
     kv_delta_solo_kernel<T, D, W, AGAIN><<<ctas, threads, smem, s>>>(a);
     const cudaError_t f = cudaGetLastError();
     if (f == cudaSuccess) count_launches(1);
@@ -906,9 +910,9 @@ cudaError_t launch_solo(const DeltaArgs &a, cudaStream_t s)
 }
 // The lengths are on the device: where there are more than two sequences for every max_q rows, as many count as have max_q rows, the
 // others being short.  While an SM each is enough for their slices (a pair of slices each), relays are faster, beyond that solos (us,
-// the first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows, 4 heads of 128 226 / 388, 32 heads of 128 325 / 429; 8 of
-// 1,232 to 2,632, 6 heads of 64 114 / 124; 2 of 4,000, 32 heads of 128 325 / 245; 8 of 1,000 316 / 261; 4 of 100 to 4,000 403 / 351;
-// 1 of 8,192, 32 heads of 64, one slice an SM 253, two 296, solo 327).
+// the first kernel included, relay / solo, bf16: 1 sequence of 8,192 rows, 4 heads of 128 235 / 398, 32 heads of 128 335 / 443; 8 of
+// 1,232 to 2,632, 6 heads of 64 116 / 128; 2 of 4,000, 32 heads of 128 331 / 253; 8 of 1,000 321 / 271; 4 of 100 to 4,000 411 / 366;
+// 1 of 8,192, 32 heads of 64, one slice an SM 239, two 296, solo 337).
 template <class T, int D>
 cudaError_t launch(const DeltaArgs &a, cudaStream_t s)
 {

@@ -162,9 +162,10 @@ __device__ __forceinline__ void put_block(View t, uint32_t block, const float (*
 // the workspace.  The inverse of I + A: its diagonal blocks of 16 x 16 a warp each (a lane has a column and goes down it:
 // x_i = -sum_(j<i) A_ij x_j), then, for blocks of 16 and of 32,
 //   (X 0; Y Z)^-1 = (X^-1 0; -Z^-1 Y X^-1 Z^-1)
-// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by the issue of its 6,500 instructions a chunk and
+// in products of two-term factors (2^-16 relative, as T itself is handed on).  Bound by the issue of its 7,000 instructions a chunk and
 // head and by its warps' waits for one another, which five CTAs an SM fill up (six, with fewer registers: 3 us more): 8,192 rows of 32
-// heads of 128, bf16, 52 us (T, P and factors in 32 bits 172; as blocks of two-term factors 62.5, with a warp for each 16 rows 59.5).
+// heads of 128, bf16, 56 us (with P in one term 53; earlier steps: T, P and factors in 32 bits 172, blocks of two-term factors 62.5, with
+// a warp for each 16 rows 59.5).
 template <class T, int D>
 __global__ void __launch_bounds__(kPrepThreads, 5) kv_delta_prep_kernel(const __grid_constant__ DeltaArgs a)
 {
