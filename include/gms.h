@@ -618,7 +618,8 @@ int gms_kv_append(const gms_kv_pool *pool, const gms_kv_layout *layout, const gm
  * enter as sums of two 16-bit terms (2^-16 relative); for `out` the state before the chunk enters as one (its error is 1.1 to 1.3 times
  * that of its last rounding).  States and sums are kept in 32 bits.  What a row does not depend on cannot reach it, whatever bits it
  * holds.  Chunks in which something is not finite or near the end of the range (differences from 2^64 on; fp16: states from 2^25 on,
- * differences from 2^41 on, keys whose lengths are 2^18 apart) are done row by row: right, and slower.
+ * differences from 2^41 on, keys whose lengths are 2^18 apart) are done row by row: right, and slower.  (fp16: what is left of a state
+ * below 2^-80 has fewer bits.)
  * src_table and dst_table may be the same (states are updated in place), and rows of src_table may be equal (several sequences go on
  * from one state).  Destination blocks must be distinct, and none may be a source block of another sequence or stand at another place of
  * its own sequence's source row (heads are done in no order: a state that is still to be read would be overwritten).  An id outside

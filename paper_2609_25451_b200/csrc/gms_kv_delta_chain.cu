@@ -549,8 +549,8 @@ struct SoloSmem {
 // product is, element for element, a first factor of the next, S -> X = S K^T, Y = S Q^T -> d = (V - f X) T^T -> S, out, so nothing
 // leaves the registers between the products and no warp waits for another.  W of them (16 W columns of a head) share a chunk's
 // operands, which further warps fetch ahead.  Bound by the rate of the products, 440 of them a chunk and warp at 128 keys, 8.3 cycles
-// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,800 cycles a chunk (64 keys: 280, two CTAs an SM side by
-// side, 7,600).
+// each, and what a warp alone on its quarter of an SM does not hide of their latencies: 5,800 cycles a chunk (64 keys: 280, 7,600 with
+// two CTAs an SM).
 template <class T, int D, int W>
 __device__ __forceinline__ void solo(const DeltaArgs &a, SoloSmem<D, W> &m, uint32_t s, uint32_t h, uint32_t part, bool &late)
 {
